@@ -280,7 +280,7 @@ __global__ __launch_bounds__(SM_NT, KT <= 4 ? 4 : 2) void solve_small_kernel(Tau
     const bool conv = !row_ok || fabsf(f) <= a.tol;
     const bool stop = __syncthreads_and(conv) || it >= a.max_iter;
     evals = it + 1;
-    if (row_ok) {
+    if (row_ok && (newton_bound || !(fabsf(f) <= a.tol))) {
       // the update rules of solve_kernel; the last evaluation's update is
       // taken as well (the mask is built afterwards)
       if (f < 0.f)

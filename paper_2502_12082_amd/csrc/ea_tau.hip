@@ -1019,6 +1019,10 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
 #pragma unroll
     for (int gq = 0; gq < G; ++gq) {
       if (!row_ok[gq]) continue;
+      // gamma < 1: a row that has converged keeps its tau while others go on
+      // (its |f| cannot halve any more, and the midpoint that follows from
+      // that is as far away as the bracket is wide)
+      if (!newton_bound && fabsf(f[gq]) <= a.tol) continue;
       // The update rules: B_f (Eq. 4); for gamma >= 1, where f is convex, the
       // Newton step from tau bounds the root from below (less a slack for the
       // rounding of f); H_f (Eq. 5) where it lands inside the bracket, widened
