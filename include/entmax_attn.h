@@ -303,6 +303,144 @@ ea_status entmax_rows_bwd(int64_t rows, int32_t n, ea_dtype dtype, const ea_para
                           const void* s, const float* tau, const float* dp, float* ds,
                           void* stream);
 
+/* Elements from row to row (token to token, request to request) and from head
+ * to head of a tensor whose last dimension is contiguous.  Rows start at
+ * multiples of 16 bytes, so both are multiples of 8 (bf16) or 4 (fp32), and
+ * not negative. */
+typedef struct {
+  int64_t row, head;
+} ea_strides;
+
+/*
+ * RMS norm of every query and key head and the rotation by the token's
+ * position, in one pass: for each row x of d values (one head of one token)
+ *   y = x * w / sqrt(mean(x^2) + eps),
+ *   (a, b) -> (a cos phi - b sin phi, a sin phi + b cos phi)
+ * for the pairs (y_i, y_{i + rot_dim/2}), i < rot_dim/2 (interleaved: (y_2i,
+ * y_2i+1)); the values behind rot_dim are y.  phi = position * freqs[i], the
+ * position being that of axis a for the sections[a] pairs that follow those of
+ * the axes before it (one axis: the token's position; three: time, height and
+ * width).  Angles are exact for every int32 position (reduced in fp64).
+ *   q, k       [tokens, heads, d] and [tokens, kv_heads, d] of `dtype`, any
+ *              strides (for instance parts of a fused projection's rows)
+ *   q_out, k_out  (written); may be q and k themselves, and otherwise must not
+ *              overlap them
+ *   positions  int32 [axes, tokens], rows `position_stride` elements apart
+ *   freqs      fp32 [rot_dim / 2], radians per position
+ *   q_weight, k_weight  [d] of weight_dtype (that of q, or fp32), or NULL: 1
+ * rot_dim: a multiple of 16, 0 (norm alone) to d.  tokens may be 0.  One launch.
+ */
+typedef struct {
+  int32_t tokens, heads, kv_heads, head_dim; /* head_dim in {64, 128} */
+  int32_t dtype, weight_dtype;               /* ea_dtype */
+  int32_t rot_dim, interleaved;
+  int32_t axes, sections[4];                 /* 1..4 axes; sections add up to rot_dim / 2 */
+  float eps;                                 /* >= 0, finite */
+} ea_rotary;
+ea_status entmax_norm_rotary(const ea_rotary* r, const void* q, const ea_strides* q_strides, const void* k,
+                             const ea_strides* k_strides, const int32_t* positions, int64_t position_stride,
+                             const float* freqs, const void* q_weight, const void* k_weight, void* q_out,
+                             const ea_strides* q_out_strides, void* k_out, const ea_strides* k_out_strides,
+                             void* stream);
+
+/*
+ * Gradients of sum(dq_out * q_out) + sum(dk_out * k_out) of entmax_norm_rotary:
+ * dq, dk (of `dtype`, [tokens, heads, d] contiguous) with respect to q and k,
+ * and dq_weight, dk_weight (fp32 [d], or NULL).  dq and dk may be dq_out and
+ * dk_out where those are contiguous.  workspace: entmax_norm_rotary_workspace
+ * bytes, 16-byte aligned.  Sums are taken in a fixed order.  Two launches.
+ */
+ea_status entmax_norm_rotary_workspace(const ea_rotary* r, size_t* bytes);
+ea_status entmax_norm_rotary_bwd(const ea_rotary* r, const void* dq_out, const ea_strides* dq_out_strides,
+                                 const void* dk_out, const ea_strides* dk_out_strides, const void* q,
+                                 const ea_strides* q_strides, const void* k, const ea_strides* k_strides,
+                                 const int32_t* positions, int64_t position_stride, const float* freqs,
+                                 const void* q_weight, const void* k_weight, void* dq, void* dk,
+                                 float* dq_weight, float* dk_weight, void* workspace, size_t ws_bytes,
+                                 void* stream);
+
+/*
+ * Attention of packed sequences.  Sequence s is the rows cu[s] .. cu[s + 1] of
+ * tensors [tokens, heads, d] (cu: int32 [seqs + 1], ascending, on the device);
+ * its queries attend to its keys alone (causal: to those up to their own).
+ * heads / kv_heads query heads share a key head: query head h has key head
+ * h / (heads / kv_heads).
+ *
+ * entmax_packed_plan lists the sequences' tiles, for every call on the same
+ * cu, from the device's cu in one launch; the host does not wait.  A range of
+ * cu that is empty holds no rows; one that is negative, overlaps an earlier
+ * one, ends behind `tokens` or is longer than max_seqlen is not computed (its
+ * rows of the outputs are unspecified).
+ */
+typedef struct {
+  int32_t tokens, seqs;            /* tokens >= 1, seqs >= 1 */
+  int32_t max_seqlen;              /* 1..131072: no sequence is longer */
+  int32_t heads, kv_heads;         /* heads a multiple of kv_heads */
+  int32_t head_dim, dtype;         /* as ea_shape */
+} ea_packed_shape;
+
+/* Bytes of a plan, of the residuals that the forward writes and the backward
+ * reads (params->need_bwd; without it, scratch of the forward), and of the
+ * workspaces (the forward's is optional, as entmax_attn_fwd's). */
+typedef struct {
+  size_t residuals, ws_fwd, ws_bwd;
+} ea_packed_sizes;
+typedef struct {
+  ea_strides q, k, v, o;
+} ea_packed_strides;
+
+ea_status entmax_packed_plan_bytes(int32_t tokens, int32_t seqs, size_t* bytes);
+ea_status entmax_packed_plan(int32_t tokens, int32_t seqs, int32_t max_seqlen, int32_t causal,
+                             const int32_t* cu, void* plan, size_t plan_bytes, void* stream);
+ea_status entmax_packed_sizes(const ea_packed_shape* shape, const ea_params* params, ea_packed_sizes* out);
+
+/*
+ * Forward and backward.  plan: of the same tokens, seqs and max_seqlen (its
+ * causal only orders the work).  Every buffer 16-byte aligned.  dout has the
+ * strides strides->o.  dq [tokens, heads, d], dk and dv [tokens, kv_heads, d]
+ * are contiguous and of the inputs' dtype (each rounded once, from fp32 sums).
+ * Rows that belong to no sequence (before cu[0], behind cu[seqs]) are left as
+ * they are, or with zero_rest != 0 set to 0.  Launches: 2 (forward; the solver
+ * one more per workspace slot count), 3 or 4 (backward).
+ */
+ea_status entmax_packed_fwd(const ea_packed_shape* shape, const ea_params* params, const void* plan,
+                            const void* q, const void* k, const void* v, void* o,
+                            const ea_packed_strides* strides, int32_t zero_rest, void* residuals,
+                            size_t residual_bytes, void* workspace, size_t ws_bytes, void* stream);
+ea_status entmax_packed_bwd(const ea_packed_shape* shape, const ea_params* params, const void* plan,
+                            const void* q, const void* k, const void* v, const void* dout,
+                            const ea_packed_strides* strides, int32_t zero_rest, const void* residuals,
+                            size_t residual_bytes, void* dq, void* dk, void* dv, void* workspace,
+                            size_t ws_bytes, void* stream);
+
+/*
+ * One new token per request: o[b, h] = sum_j p_j v_j over the `prefix` keys
+ * that all requests share, then the first lengths[b] keys of the request's own
+ * cache (lengths: int32 on the device, taken as 0 .. capacity).  A request
+ * without keys has o = 0.  The scores of the prefix are computed once for all
+ * requests that share a key head.
+ *   q, o   [requests, heads, d], row strides from request to request
+ *   k, v   [requests, capacity, kv_heads, d]
+ *   k_prefix, v_prefix  [prefix, kv_heads, d] (not read where prefix is 0)
+ *   params alpha, scale, max_iter and tol are used
+ * prefix + capacity <= 131072.  workspace: entmax_prefix_decode_workspace
+ * bytes, 16-byte aligned (4 bytes a score).  Two launches.
+ */
+typedef struct {
+  int32_t requests, heads, kv_heads, head_dim, dtype;
+  int32_t prefix, capacity;
+} ea_decode_shape;
+typedef struct {
+  ea_strides q, o, k, v, k_prefix, v_prefix;
+  int64_t k_request, v_request; /* from request to request */
+} ea_decode_strides;
+ea_status entmax_prefix_decode_workspace(const ea_decode_shape* shape, size_t* bytes);
+ea_status entmax_prefix_decode(const ea_decode_shape* shape, const ea_params* params,
+                               const ea_decode_strides* strides, const void* q, const void* k,
+                               const void* v, const int32_t* lengths, const void* k_prefix,
+                               const void* v_prefix, void* o, void* workspace, size_t ws_bytes,
+                               void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* entmax_attn_status_string(ea_status s);
 

@@ -8,6 +8,19 @@ fallback: importing this module without the built library raises.
     import paper_2502_12082_amd as ea
     o, res = ea.forward(q, k, v, alpha=1.5, scale=d ** -0.5, causal=False)
     dq, dk, dv = ea.backward(q, k, v, do, res)
+
+A transformer's layer on tokens packed from several sequences, with grouped
+heads ([tokens, heads, d] tensors, such as parts of a fused projection's rows):
+
+    plan = ea.packed_plan(cu_seqlens, tokens)                  # once a batch
+    q, k = ea.norm_rotary(q, k, positions, freqs, q_weight, k_weight)
+    o, res = ea.packed_forward(q, k, v, plan, alpha=1.5)
+    dq, dk, dv = ea.packed_backward(q, k, v, do, res)
+    dq, dk, dwq, dwk = ea.norm_rotary_backward(dq, dk, q_in, k_in, positions, freqs, q_weight, k_weight)
+
+and one decoding step, for requests that share a prefix:
+
+    o = ea.prefix_decode(q, k_cache, v_cache, lengths, k_prefix, v_prefix)
 """
 from __future__ import annotations
 
@@ -38,8 +51,12 @@ SYMBOLS = ("entmax_attn_default_params", "entmax_attn_sizes", "entmax_attn_fwd",
            "entmax_rows_bwd", "entmax_attn_fwd_dense", "entmax_attn_bwd_dense",
            "entmax_attn_bwd_noalloc", "entmax_attn_lists_bytes", "entmax_attn_fwd_lists",
            "entmax_attn_bwd_lists", "entmax_attn_fwd_dense_lists", "entmax_attn_bwd_dense_lists",
-           "entmax_attn_bwd_lists_workspace")
+           "entmax_attn_bwd_lists_workspace", "entmax_norm_rotary", "entmax_norm_rotary_workspace",
+           "entmax_norm_rotary_bwd", "entmax_packed_plan_bytes", "entmax_packed_plan",
+           "entmax_packed_sizes", "entmax_packed_fwd", "entmax_packed_bwd",
+           "entmax_prefix_decode_workspace", "entmax_prefix_decode")
 EA_ALL_STAGES = -1
+MAX_SEQLEN = 131072  # the longest sequence of every attention call
 NOALLOC_MAX_ROWS = 1048576  # EA_NOALLOC_MAX_ROWS of include/entmax_attn.h
 
 
@@ -730,3 +747,499 @@ def backward_dense(q, k, v, dout, tau, o2, alpha=1.5, scale=None, causal=False, 
         o2.data_ptr(), lists_ptr, lists_bytes, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
         ws.data_ptr(), ws.numel(), _stream_handle(q.device)), "entmax_attn_bwd_dense")
     return dq, dk, dv
+
+
+# ------------------------------------------- layouts of a transformer's layer
+#
+# The calls below take [tokens, heads, d] tensors, in the strides that the
+# caller has them in.  They run on the tensors' device, whichever is current.
+
+class Strides(ctypes.Structure):
+    _fields_ = [("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class Rotary(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("weight_dtype", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("sections", ctypes.c_int32 * 4), ("eps", ctypes.c_float)]
+
+
+class PackedShape(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in
+                ("tokens", "seqs", "max_seqlen", "heads", "kv_heads", "head_dim", "dtype")]
+
+
+class PackedSizes(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_size_t) for f in ("residuals", "ws_fwd", "ws_bwd")]
+
+
+class PackedStrides(ctypes.Structure):
+    _fields_ = [(f, Strides) for f in ("q", "k", "v", "o")]
+
+
+class DecodeShape(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in
+                ("requests", "heads", "kv_heads", "head_dim", "dtype", "prefix", "capacity")]
+
+
+class DecodeStrides(ctypes.Structure):
+    _fields_ = ([(f, Strides) for f in ("q", "o", "k", "v", "k_prefix", "v_prefix")] +
+                [("k_request", ctypes.c_int64), ("v_request", ctypes.c_int64)])
+
+
+_i32, _i64, _sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+for _name, _args in (
+        ("entmax_norm_rotary", [_P(Rotary), _v, _P(Strides), _v, _P(Strides), _v, _i64, _v, _v, _v, _v,
+                                _P(Strides), _v, _P(Strides), _v]),
+        ("entmax_norm_rotary_workspace", [_P(Rotary), _P(_sz)]),
+        ("entmax_norm_rotary_bwd", [_P(Rotary), _v, _P(Strides), _v, _P(Strides), _v, _P(Strides), _v,
+                                    _P(Strides), _v, _i64, _v, _v, _v, _v, _v, _v, _v, _v, _sz, _v]),
+        ("entmax_packed_plan_bytes", [_i32, _i32, _P(_sz)]),
+        ("entmax_packed_plan", [_i32, _i32, _i32, _i32, _v, _v, _sz, _v]),
+        ("entmax_packed_sizes", [_P(PackedShape), _P(Params), _P(PackedSizes)]),
+        ("entmax_packed_fwd", [_P(PackedShape), _P(Params), _v, _v, _v, _v, _v, _P(PackedStrides), _i32,
+                               _v, _sz, _v, _sz, _v]),
+        ("entmax_packed_bwd", [_P(PackedShape), _P(Params), _v, _v, _v, _v, _v, _P(PackedStrides), _i32,
+                               _v, _sz, _v, _v, _v, _v, _sz, _v]),
+        ("entmax_prefix_decode_workspace", [_P(DecodeShape), _P(_sz)]),
+        ("entmax_prefix_decode", [_P(DecodeShape), _P(Params), _P(DecodeStrides), _v, _v, _v, _v, _v, _v,
+                                  _v, _v, _sz, _v])):
+    getattr(_lib, _name).argtypes = _args
+    getattr(_lib, _name).restype = ctypes.c_int
+
+
+def _ea_dtype(t, name):
+    if t.dtype == torch.bfloat16:
+        return EA_BF16
+    if t.dtype == torch.float32:
+        return EA_F32
+    raise ValueError("%s must be bfloat16 or float32, not %s" % (name, t.dtype))
+
+
+def _strided(t, name, shape, dtype, device, written=False):
+    """Raises ValueError unless t is a tensor of this shape, dtype and device
+    whose last dimension is contiguous and whose rows start at multiples of 16
+    bytes; a tensor to be written must not hold an element twice."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError("%s must be a torch tensor" % name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+    if t.dtype != dtype:
+        raise ValueError("%s has dtype %s, expected %s" % (name, t.dtype, dtype))
+    if t.device != device:
+        raise ValueError("%s is on %s, expected %s" % (name, t.device, device))
+    if t.numel() == 0:
+        return
+    vec = 16 // t.element_size()
+    if t.stride(-1) != 1:
+        raise ValueError("%s must be contiguous in its last dimension" % name)
+    # (the stride of a dimension of one element is never used)
+    used = [s for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n > 1]
+    if t.data_ptr() % 16 or any(s % vec for s in used):
+        raise ValueError("%s: rows must start at multiples of 16 bytes" % name)
+    if written:
+        # each dimension steps over all of the smaller ones
+        end = t.shape[-1]
+        for n, s in sorted(((n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n > 1), key=lambda x: x[1]):
+            if s < end:
+                raise ValueError("%s has elements that share memory" % name)
+            end = s * (n - 1) + end
+
+
+def _stride(t, dim):
+    return t.stride(dim) if t.shape[dim] > 1 else 0
+
+
+def _row_head(t, row=0, head=1):
+    return Strides(_stride(t, row), _stride(t, head))
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _overlap(a, b):
+    """Whether two tensors' memory ranges meet."""
+    def span(t):
+        lo = t.data_ptr()
+        return lo, lo + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
+    if a.numel() == 0 or b.numel() == 0:
+        return False
+    (a0, a1), (b0, b1) = span(a), span(b)
+    return a0 < b1 and b0 < a1
+
+
+class _on_device:
+    """Makes a device current for a call where it is not (a launch goes to a
+    stream of the current device)."""
+
+    def __init__(self, device):
+        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+# ------------------------------------------------------ norm and rotation
+
+def _check_rotary(q, k, positions, freqs, q_weight, k_weight, sections, eps, interleaved):
+    """(Rotary, positions' row stride) of a call's arguments."""
+    for name, t in (("q", q), ("k", k)):
+        if not isinstance(t, torch.Tensor) or t.dim() != 3:
+            raise ValueError("%s must be a [tokens, heads, head_dim] tensor" % name)
+    dt = _ea_dtype(q, "q")
+    tokens, hq, d = q.shape
+    hk, dev = k.shape[1], q.device
+    _strided(q, "q", q.shape, q.dtype, dev)
+    _strided(k, "k", (tokens, hk, d), q.dtype, dev)
+    if not isinstance(freqs, torch.Tensor) or freqs.dim() != 1:
+        raise ValueError("freqs must be a [rot_dim / 2] tensor")
+    _need(freqs, "freqs", freqs.shape, torch.float32, dev)
+    pairs = freqs.shape[0]
+    sections = (pairs,) if sections is None else tuple(int(s) for s in sections)
+    if not 1 <= len(sections) <= 4 or min(sections) < 0 or sum(sections) != pairs:
+        raise ValueError("sections must be 1 to 4 numbers of pairs that add up to len(freqs) = %d" % pairs)
+    if 2 * pairs > d or pairs % 8:
+        raise ValueError("freqs must hold a multiple of 8 pairs, at most half of head_dim")
+    shape = (len(sections), tokens)
+    if not isinstance(positions, torch.Tensor) or tuple(positions.shape) not in ((shape,) if len(sections) > 1
+                                                                                 else (shape, (tokens,))):
+        raise ValueError("positions must be a %s tensor" % (list(shape),))
+    if positions.dtype != torch.int32 or positions.device != dev:
+        raise ValueError("positions must be int32 and on %s" % dev)
+    if tokens > 1 and positions.stride(-1) != 1:
+        raise ValueError("positions must be contiguous in its last dimension")
+    weights = [(n, w) for n, w in (("q_weight", q_weight), ("k_weight", k_weight)) if w is not None]
+    wt = q.dtype
+    for name, w in weights:
+        wt = weights[0][1].dtype if isinstance(weights[0][1], torch.Tensor) else None
+        if wt not in (q.dtype, torch.float32):
+            raise ValueError("weights must have the dtype of q, or be float32")
+        _need(w, name, (d,), wt, dev)
+        if w.data_ptr() % 16:
+            raise ValueError("%s must start at a multiple of 16 bytes" % name)
+    r = Rotary(tokens, hq, hk, d, dt, EA_F32 if wt == torch.float32 else EA_BF16, 2 * pairs,
+               int(bool(interleaved)), len(sections), (ctypes.c_int32 * 4)(*sections), float(eps))
+    return r, positions.stride(0) if positions.dim() == 2 else 0
+
+
+def norm_rotary(q, k, positions, freqs, q_weight=None, k_weight=None, sections=None, eps=1e-6,
+                interleaved=False, q_out=None, k_out=None):
+    """(q_out, k_out): every head of q [tokens, heads, d] and k [tokens, kv_heads, d]
+    (bf16 or fp32, any strides with a contiguous last dimension) divided by
+    sqrt(mean(x^2) + eps), times its weights ([d], of q's dtype or fp32; None:
+    1), and rotated: pair i by positions * freqs[i] radians.
+
+    freqs: fp32 [rot_dim / 2]; the pairs are (i, i + rot_dim / 2), or (2 i, 2 i + 1)
+    with interleaved=True, and dimensions behind rot_dim are not rotated.
+    positions: int32 [tokens]; with several axes [axes, tokens], and sections
+    gives the number of consecutive pairs that each axis rotates.
+    q_out, k_out: tensors to write, which may be q and k themselves."""
+    r, pos_stride = _check_rotary(q, k, positions, freqs, q_weight, k_weight, sections, eps, interleaved)
+    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+    k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
+    for name, out, like in (("q_out", q_out, q), ("k_out", k_out, k)):
+        _strided(out, name, like.shape, like.dtype, like.device, written=True)
+        for other_name, t in (("q", q), ("k", k)):
+            if _overlap(out, t) and not (t is like and out.data_ptr() == t.data_ptr() and out.stride() == t.stride()):
+                if not _apart(out, t):
+                    raise ValueError("%s overlaps %s" % (name, other_name))
+    _on_gpu(q.device)
+    with _on_device(q.device):
+        _check(_lib.entmax_norm_rotary(
+            ctypes.byref(r), q.data_ptr(), _row_head(q), k.data_ptr(), _row_head(k), positions.data_ptr(),
+            pos_stride, freqs.data_ptr(), _ptr(q_weight), _ptr(k_weight), q_out.data_ptr(), _row_head(q_out),
+            k_out.data_ptr(), _row_head(k_out), _stream_handle(q.device)), "entmax_norm_rotary")
+    return q_out, k_out
+
+
+def _apart(a, b):
+    """Whether two tensors whose ranges meet are different columns of the same
+    rows (parts of one fused projection)."""
+    row = a.stride(0)
+    if a.dim() != b.dim() or a.shape[0] != b.shape[0] or a.shape[0] < 2 or row != b.stride(0):
+        return False
+    width = lambda t: 1 + sum((n - 1) * s for n, s in zip(t.shape[1:], t.stride()[1:]))
+    first, second = sorted((a, b), key=lambda t: t.data_ptr())
+    gap = (second.data_ptr() - first.data_ptr()) // a.element_size()
+    return gap >= width(first) and gap + width(second) <= row
+
+
+def norm_rotary_backward(dq_out, dk_out, q, k, positions, freqs, q_weight=None, k_weight=None, sections=None,
+                         eps=1e-6, interleaved=False):
+    """(dq, dk, dq_weight, dk_weight) of sum(dq_out * q_out) + sum(dk_out * k_out)
+    for (q_out, k_out) = norm_rotary(q, k, ...): dq, dk in q's dtype, the
+    weights' gradients in fp32 (None for a weight that is None).  dq_out and
+    dk_out have q's dtype."""
+    r, pos_stride = _check_rotary(q, k, positions, freqs, q_weight, k_weight, sections, eps, interleaved)
+    _strided(dq_out, "dq_out", q.shape, q.dtype, q.device)
+    _strided(dk_out, "dk_out", k.shape, q.dtype, q.device)
+    _on_gpu(q.device)
+    with _on_device(q.device):
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        dk = torch.empty(k.shape, dtype=k.dtype, device=q.device)
+        make = torch.empty if q.shape[0] else torch.zeros
+        dwq, dwk = (None if w is None else make(q.shape[-1], dtype=torch.float32, device=q.device)
+                    for w in (q_weight, k_weight))
+        n = ctypes.c_size_t()
+        _check(_lib.entmax_norm_rotary_workspace(ctypes.byref(r), ctypes.byref(n)), "entmax_norm_rotary_workspace")
+        ws = torch.empty(max(n.value, 16), dtype=torch.uint8, device=q.device)
+        _check(_lib.entmax_norm_rotary_bwd(
+            ctypes.byref(r), dq_out.data_ptr(), _row_head(dq_out), dk_out.data_ptr(), _row_head(dk_out),
+            q.data_ptr(), _row_head(q), k.data_ptr(), _row_head(k), positions.data_ptr(), pos_stride,
+            freqs.data_ptr(), _ptr(q_weight), _ptr(k_weight), dq.data_ptr(), dk.data_ptr(), _ptr(dwq),
+            _ptr(dwk), ws.data_ptr(), ws.numel(), _stream_handle(q.device)), "entmax_norm_rotary_bwd")
+    return dq, dk, dwq, dwk
+
+
+# ------------------------------------------------------ packed sequences
+
+class PackedPlan:
+    """The tiles of a batch's sequences, listed on the device by packed_plan:
+    for every packed_forward and packed_backward on these sequences, of any
+    layer and head counts.  It lives on the stream that made it, as a tensor does."""
+
+    def __init__(self, buffer, tokens, seqs, max_seqlen, causal):
+        self.buffer, self.tokens, self.seqs = buffer, tokens, seqs
+        self.max_seqlen, self.causal = max_seqlen, causal
+
+    @property
+    def device(self):
+        return self.buffer.device
+
+
+def packed_plan(cu_seqlens, tokens, max_seqlen=None, causal=True) -> PackedPlan:
+    """Lists the tiles of the sequences cu_seqlens[s] .. cu_seqlens[s + 1] (int32
+    [seqs + 1] on the device, ascending) of tensors with `tokens` rows.  One
+    launch; the host does not wait for cu_seqlens.  max_seqlen: no sequence is
+    longer (default: tokens); the residuals' tables grow with it.  A sequence
+    that is longer, reaches outside the tensors or overlaps an earlier one is
+    not computed: its rows of the outputs are unspecified."""
+    if not isinstance(cu_seqlens, torch.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 2:
+        raise ValueError("cu_seqlens must be a [seqs + 1] tensor of at least one sequence")
+    _need(cu_seqlens, "cu_seqlens", cu_seqlens.shape, torch.int32)
+    tokens, seqs = int(tokens), cu_seqlens.shape[0] - 1
+    if tokens < 1:
+        raise ValueError("tokens must be at least 1")
+    # (no sequence is longer than its tensors, or than the kernels take)
+    max_seqlen = min(tokens, MAX_SEQLEN) if max_seqlen is None else int(max_seqlen)
+    if max_seqlen < 1:
+        raise ValueError("max_seqlen must be at least 1")
+    max_seqlen = min(max_seqlen, tokens)
+    _on_gpu(cu_seqlens.device)
+    n = ctypes.c_size_t()
+    _check(_lib.entmax_packed_plan_bytes(tokens, seqs, ctypes.byref(n)), "entmax_packed_plan_bytes")
+    with _on_device(cu_seqlens.device):
+        buffer = torch.empty(n.value, dtype=torch.uint8, device=cu_seqlens.device)
+        _check(_lib.entmax_packed_plan(tokens, seqs, max_seqlen, int(bool(causal)), cu_seqlens.data_ptr(),
+                                       buffer.data_ptr(), n.value, _stream_handle(cu_seqlens.device)),
+               "entmax_packed_plan")
+    return PackedPlan(buffer, tokens, seqs, max_seqlen, bool(causal))
+
+
+class PackedResiduals:
+    """What packed_forward leaves for packed_backward: thresholds, O^(2) and the
+    block tables in one device buffer, and the plan."""
+
+    def __init__(self, shape: PackedShape, params: Params, plan: PackedPlan, sizes: PackedSizes, device):
+        self.shape, self.params, self.plan, self.sizes = shape, params, plan, sizes
+        self.buffer = torch.empty(sizes.residuals, dtype=torch.uint8, device=device)
+
+
+def _packed_shape(q, k, v, plan):
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        if not isinstance(t, torch.Tensor) or t.dim() != 3:
+            raise ValueError("%s must be a [tokens, heads, head_dim] tensor" % name)
+    if not isinstance(plan, PackedPlan):
+        raise ValueError("plan must come from packed_plan")
+    dt = _ea_dtype(q, "q")
+    tokens, hq, d = q.shape
+    hk = k.shape[1]
+    if tokens != plan.tokens:
+        raise ValueError("q has %d rows, the plan is for %d" % (tokens, plan.tokens))
+    if plan.device != q.device:
+        raise ValueError("the plan is on %s, q on %s" % (plan.device, q.device))
+    if hk < 1 or hq % hk:
+        raise ValueError("q's %d heads must be a multiple of k's %d" % (hq, hk))
+    _strided(q, "q", q.shape, q.dtype, q.device)
+    _strided(k, "k", (tokens, hk, d), q.dtype, q.device)
+    _strided(v, "v", (tokens, hk, d), q.dtype, q.device)
+    return PackedShape(tokens, plan.seqs, plan.max_seqlen, hq, hk, d, dt)
+
+
+def _packed_strides(q, k, v, o):
+    return PackedStrides(_row_head(q), _row_head(k), _row_head(v), _row_head(o))
+
+
+def packed_forward(q, k, v, plan: PackedPlan, alpha=1.5, scale=None, need_bwd=True, max_iter=None, tol=None,
+                   out=None, workspace=None):
+    """(O, residuals) of alpha-entmax attention within each sequence of the plan
+    (causal if the plan is): q [tokens, heads, d], k and v [tokens, kv_heads, d],
+    bf16 or fp32, any strides with a contiguous last dimension; query head h
+    attends to key head h // (heads // kv_heads).
+
+    Rows of no sequence (before cu_seqlens[0], behind the last) are 0 in an O
+    that the call makes and left as they are in `out`.  need_bwd=False gives
+    residuals that packed_backward does not take.  tol: default 1e-5, for fp32
+    1e-6.  workspace: as for forward (sizes.ws_fwd bytes of the residuals)."""
+    shape = _packed_shape(q, k, v, plan)
+    if tol is None and shape.dtype == EA_F32:
+        tol = 1e-6  # (Sum p is off by up to tol, which the fp32 outputs show)
+    params = make_params(alpha, scale, plan.causal, need_bwd, max_iter, tol, head_dim=q.shape[-1])
+    sizes = PackedSizes()
+    _check(_lib.entmax_packed_sizes(ctypes.byref(shape), ctypes.byref(params), ctypes.byref(sizes)),
+           "entmax_packed_sizes")
+    made = out is None
+    if not made:
+        _strided(out, "out", q.shape, q.dtype, q.device, written=True)
+        for name, t in (("q", q), ("k", k), ("v", v)):
+            if _overlap(out, t):
+                raise ValueError("out overlaps %s" % name)
+    if workspace is not None and workspace is not False:
+        _check_bytes(workspace, "workspace", 0, q.device)
+    _on_gpu(q.device)
+    with _on_device(q.device):
+        if made:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        res = PackedResiduals(shape, params, plan, sizes, q.device)
+        if workspace is None:
+            workspace = torch.empty(max(sizes.ws_fwd, 16), dtype=torch.uint8, device=q.device)
+        ws, ws_bytes = (None, 0) if workspace is False else (workspace.data_ptr(),
+                                                            workspace.numel() * workspace.element_size())
+        _check(_lib.entmax_packed_fwd(
+            ctypes.byref(shape), ctypes.byref(params), plan.buffer.data_ptr(), q.data_ptr(), k.data_ptr(),
+            v.data_ptr(), out.data_ptr(), _packed_strides(q, k, v, out), int(made), res.buffer.data_ptr(),
+            res.buffer.numel(), ws, ws_bytes, _stream_handle(q.device)), "entmax_packed_fwd")
+    return out, res
+
+
+def packed_backward(q, k, v, dout, res: PackedResiduals, dq=None, dk=None, dv=None, workspace=None):
+    """(dQ, dK, dV) of sum(dout * O) for the packed_forward that made res, in the
+    inputs' dtype: [tokens, heads, d] and [tokens, kv_heads, d], contiguous.
+    dout has any strides with a contiguous last dimension.  Rows of no sequence
+    are 0 in gradients that the call makes; they are left as they are if dq, dk
+    and dv are given (all three or none)."""
+    if not isinstance(res, PackedResiduals):
+        raise ValueError("res must be the residuals of a packed_forward call")
+    shape = _packed_shape(q, k, v, res.plan)
+    if any(getattr(shape, f) != getattr(res.shape, f) for f, _ in PackedShape._fields_):
+        raise ValueError("res was made for another shape or dtype")
+    if not res.params.need_bwd:
+        raise ValueError("res comes from a forward with need_bwd=False")
+    if res.buffer.device != q.device:
+        raise ValueError("res is on %s, q on %s" % (res.buffer.device, q.device))
+    _strided(dout, "dout", q.shape, q.dtype, q.device)
+    given = [t is not None for t in (dq, dk, dv)]
+    if any(given) != all(given):
+        raise ValueError("dq, dk and dv must be given together")
+    made = not given[0]
+    if not made:
+        for name, t, like in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)):
+            _need(t, name, like.shape, q.dtype, q.device)
+            if t.data_ptr() % 16:
+                raise ValueError("%s must start at a multiple of 16 bytes" % name)
+            for other_name, other in (("q", q), ("k", k), ("v", v), ("dout", dout)):
+                if _overlap(t, other):
+                    raise ValueError("%s overlaps %s" % (name, other_name))
+        if _overlap(dq, dk) or _overlap(dq, dv) or _overlap(dk, dv):
+            raise ValueError("dq, dk and dv overlap")
+    if workspace is not None:
+        _check_bytes(workspace, "workspace", res.sizes.ws_bwd, q.device)
+    _on_gpu(q.device)
+    with _on_device(q.device):
+        if made:
+            dq, dk, dv = (torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v))
+        if workspace is None:
+            workspace = torch.empty(res.sizes.ws_bwd, dtype=torch.uint8, device=q.device)
+        _check(_lib.entmax_packed_bwd(
+            ctypes.byref(shape), ctypes.byref(res.params), res.plan.buffer.data_ptr(), q.data_ptr(),
+            k.data_ptr(), v.data_ptr(), dout.data_ptr(), _packed_strides(q, k, v, dout), int(made),
+            res.buffer.data_ptr(), res.buffer.numel(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+            workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_handle(q.device)),
+            "entmax_packed_bwd")
+    return dq, dk, dv
+
+
+# ------------------------------------------------------ single tokens
+
+def prefix_decode_workspace(q, k_cache, prefix=0):
+    """Bytes of the workspace of prefix_decode for these tensors and a prefix of
+    that many keys (4 bytes for every query head's score of every key)."""
+    shape = DecodeShape(q.shape[0], q.shape[1], k_cache.shape[2], q.shape[2], _ea_dtype(q, "q"), int(prefix),
+                        k_cache.shape[1])
+    n = ctypes.c_size_t()
+    _check(_lib.entmax_prefix_decode_workspace(ctypes.byref(shape), ctypes.byref(n)),
+           "entmax_prefix_decode_workspace")
+    return n.value
+
+
+def prefix_decode(q, k_cache, v_cache, lengths, k_prefix=None, v_prefix=None, alpha=1.5, scale=None,
+                  max_iter=None, tol=None, out=None, workspace=None):
+    """O [requests, heads, d] of one new token per request: q [requests, heads, d]
+    attends to the keys of k_prefix, v_prefix [prefix, kv_heads, d] (None: no
+    prefix), which all requests share, and to the first lengths[b] keys (int32
+    on the device, taken as 0 .. capacity) of its own k_cache, v_cache
+    [requests, capacity, kv_heads, d].  bf16 or fp32, any strides with a
+    contiguous last dimension.  A request without any key has O = 0.
+
+    tol: default 1e-6.  workspace: a device buffer of prefix_decode_workspace
+    bytes, to keep from call to call (one call at a time)."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a [requests, heads, head_dim] tensor")
+    dt = _ea_dtype(q, "q")
+    B, hq, d = q.shape
+    dev = q.device
+    if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+        raise ValueError("k_cache must be a [requests, capacity, kv_heads, head_dim] tensor")
+    cap, hk = k_cache.shape[1:3]
+    if hk < 1 or hq % hk:
+        raise ValueError("q's %d heads must be a multiple of k_cache's %d" % (hq, hk))
+    _strided(q, "q", q.shape, q.dtype, dev)
+    _strided(k_cache, "k_cache", (B, cap, hk, d), q.dtype, dev)
+    _strided(v_cache, "v_cache", (B, cap, hk, d), q.dtype, dev)
+    _need(lengths, "lengths", (B,), torch.int32, dev)
+    if (k_prefix is None) != (v_prefix is None):
+        raise ValueError("k_prefix and v_prefix must be given together")
+    P = 0
+    if k_prefix is not None:
+        if not isinstance(k_prefix, torch.Tensor) or k_prefix.dim() != 3:
+            raise ValueError("k_prefix must be a [prefix, kv_heads, head_dim] tensor")
+        P = k_prefix.shape[0]
+        _strided(k_prefix, "k_prefix", (P, hk, d), q.dtype, dev)
+        _strided(v_prefix, "v_prefix", (P, hk, d), q.dtype, dev)
+    if out is not None:
+        _strided(out, "out", q.shape, q.dtype, dev, written=True)
+        for name, t in (("q", q), ("k_cache", k_cache), ("v_cache", v_cache), ("k_prefix", k_prefix),
+                        ("v_prefix", v_prefix)):
+            if t is not None and _overlap(out, t):
+                raise ValueError("out overlaps %s" % name)
+    params = make_params(alpha, scale, False, False, max_iter, 1e-6 if tol is None else tol, head_dim=d)
+    shape = DecodeShape(B, hq, hk, d, dt, P, cap)
+    n = ctypes.c_size_t()
+    _check(_lib.entmax_prefix_decode_workspace(ctypes.byref(shape), ctypes.byref(n)),
+           "entmax_prefix_decode_workspace")
+    if workspace is not None:
+        _check_bytes(workspace, "workspace", n.value, dev)
+    _on_gpu(dev)
+    none = Strides(0, 0)
+    with _on_device(dev):
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        if workspace is None:
+            workspace = torch.empty(max(n.value, 16), dtype=torch.uint8, device=dev)
+        strides = DecodeStrides(_row_head(q), _row_head(out), _row_head(k_cache, 1, 2), _row_head(v_cache, 1, 2),
+                                none if P == 0 else _row_head(k_prefix), none if P == 0 else _row_head(v_prefix),
+                                _stride(k_cache, 0), _stride(v_cache, 0))
+        _check(_lib.entmax_prefix_decode(
+            ctypes.byref(shape), ctypes.byref(params), strides, q.data_ptr(), k_cache.data_ptr(),
+            v_cache.data_ptr(), lengths.data_ptr(), _ptr(k_prefix), _ptr(v_prefix), out.data_ptr(),
+            workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_handle(dev)),
+            "entmax_prefix_decode")
+    return out

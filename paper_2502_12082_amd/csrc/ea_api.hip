@@ -4,6 +4,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include <mutex>
 
 #include "../../include/entmax_attn.h"
@@ -108,8 +110,21 @@ void fill_sizes(const Dims& d, ea_sizes* z) {
   z->tau_lo = d.dtype == EA_F32 ? (size_t)(d.BH * d.n) * 4 : 0;
 }
 
-// Element lists: one ListBlock per query block, then what each serves.
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
+
+// The parts of one buffer, each 256-byte aligned; `at` sums up its size.
+struct Parts {
+  char* base;
+  size_t at = 0;
+  template <typename T>
+  T* take(size_t count) {
+    char* p = base ? base + at : nullptr;
+    at += up256(count * sizeof(T));
+    return reinterpret_cast<T*>(p);
+  }
+};
+
+// Element lists: one ListBlock per query block, then what each serves.
 size_t lists_bytes_of(const Dims& d) {
   if (d.n > LIST_MAX_SEQLEN) return 0;
   const size_t blocks = (size_t)(d.BH * d.T);
@@ -595,6 +610,489 @@ ea_status entmax_attn_bwd_dense(const ea_shape* shape, const ea_params* params, 
                                 float* dv, void* workspace, size_t ws_bytes, void* stream) {
   return entmax_attn_bwd_dense_lists(shape, params, q, k, v, dout, tau, tau_lo, o2, nullptr, 0, dq, dk, dv,
                                      workspace, ws_bytes, stream);
+}
+
+// ------------------------------------------------ norm and rotation
+
+namespace {
+
+constexpr int64_t MAX_STRIDE = (int64_t)1 << 40;
+// Strides of rows of `esize`-byte elements that start at multiples of 16 bytes.
+bool strides_ok(const ea_strides* s, size_t esize) {
+  const int64_t vec = 16 / (int64_t)esize;
+  return s && s->row >= 0 && s->head >= 0 && s->row % vec == 0 && s->head % vec == 0 && s->row <= MAX_STRIDE &&
+         s->head <= MAX_STRIDE;
+}
+
+bool dtype_ok(int32_t t) { return t == EA_BF16 || t == EA_F32; }
+size_t size_of(int32_t t) { return t == EA_BF16 ? 2 : 4; }
+
+ea_status check_rotary(const ea_rotary* r) {
+  if (!r) return EA_ERR_INVALID_ARG;
+  if (r->tokens < 0 || r->heads < 1 || r->kv_heads < 1) return EA_ERR_INVALID_ARG;
+  if (!dtype_ok(r->dtype) || (r->head_dim != 64 && r->head_dim != 128)) return EA_ERR_UNSUPPORTED;
+  if (r->weight_dtype != r->dtype && r->weight_dtype != EA_F32) return EA_ERR_UNSUPPORTED;
+  if (r->rot_dim < 0 || r->rot_dim > r->head_dim || r->rot_dim % 16 != 0) return EA_ERR_INVALID_ARG;
+  if (r->interleaved != 0 && r->interleaved != 1) return EA_ERR_INVALID_ARG;
+  if (!std::isfinite(r->eps) || r->eps < 0.0f) return EA_ERR_INVALID_ARG;
+  if (r->axes < 1 || r->axes > ROT_MAX_AXES) return EA_ERR_INVALID_ARG;
+  int64_t pairs = 0;
+  for (int a = 0; a < r->axes; ++a) {
+    if (r->sections[a] < 0) return EA_ERR_INVALID_ARG;
+    pairs += r->sections[a];
+  }
+  if (2 * pairs != r->rot_dim) return EA_ERR_INVALID_ARG;
+  // heads and waves of a launch are 32-bit numbers
+  if ((int64_t)r->heads + r->kv_heads > (1 << 20) || (int64_t)r->tokens > INT32_MAX / 2) return EA_ERR_UNSUPPORTED;
+  return EA_OK;
+}
+
+ea_status prep_rotary(const ea_rotary* r, const void* q, const ea_strides* qs, const void* k, const ea_strides* ks,
+                      const int32_t* positions, int64_t position_stride, const float* freqs, const void* q_weight,
+                      const void* k_weight, RotaryArgs* out) {
+  const size_t es = size_of(r->dtype);
+  if (!tensor_ok(q) || !tensor_ok(k) || !strides_ok(qs, es) || !strides_ok(ks, es)) return EA_ERR_INVALID_ARG;
+  if (r->rot_dim && (!small_ok(positions) || !small_ok(freqs))) return EA_ERR_INVALID_ARG;
+  if (position_stride < 0) return EA_ERR_INVALID_ARG;
+  if ((q_weight && !tensor_ok(q_weight)) || (k_weight && !tensor_ok(k_weight))) return EA_ERR_INVALID_ARG;
+  RotaryArgs a{};
+  a.q = {const_cast<void*>(q), qs->row, qs->head};
+  a.k = {const_cast<void*>(k), ks->row, ks->head};
+  a.positions = positions;
+  a.position_stride = position_stride;
+  a.freqs = freqs;
+  int end = 0;
+  for (int x = 0; x < r->axes; ++x) a.axis_end[x] = end += r->sections[x];
+  a.axes = r->axes;
+  a.tokens = r->tokens;
+  a.hq = r->heads;
+  a.hk = r->kv_heads;
+  a.d = r->head_dim;
+  a.rot = r->rot_dim;
+  a.interleaved = r->interleaved;
+  a.eps = r->eps;
+  a.q_weight = q_weight;
+  a.k_weight = k_weight;
+  a.weight_f32 = r->weight_dtype == EA_F32;
+  *out = a;
+  return EA_OK;
+}
+
+size_t rotary_ws(const ea_rotary* r) { return (size_t)rotary_partials(r->tokens) * 2 * r->head_dim * 4; }
+
+}  // namespace
+
+ea_status entmax_norm_rotary(const ea_rotary* r, const void* q, const ea_strides* q_strides, const void* k,
+                             const ea_strides* k_strides, const int32_t* positions, int64_t position_stride,
+                             const float* freqs, const void* q_weight, const void* k_weight, void* q_out,
+                             const ea_strides* q_out_strides, void* k_out, const ea_strides* k_out_strides,
+                             void* stream) {
+  ea_status st = check_rotary(r);
+  if (st != EA_OK || r->tokens == 0) return st;
+  RotaryArgs a;
+  st = prep_rotary(r, q, q_strides, k, k_strides, positions, position_stride, freqs, q_weight, k_weight, &a);
+  if (st != EA_OK) return st;
+  const size_t es = size_of(r->dtype);
+  if (!tensor_ok(q_out) || !tensor_ok(k_out) || !strides_ok(q_out_strides, es) || !strides_ok(k_out_strides, es))
+    return EA_ERR_INVALID_ARG;
+  a.q_out = {q_out, q_out_strides->row, q_out_strides->head};
+  a.k_out = {k_out, k_out_strides->row, k_out_strides->head};
+  return from_hip(launch_rotary_fwd(a, r->dtype, static_cast<hipStream_t>(stream)));
+}
+
+ea_status entmax_norm_rotary_workspace(const ea_rotary* r, size_t* bytes) {
+  const ea_status st = check_rotary(r);
+  if (st != EA_OK) return st;
+  if (!bytes) return EA_ERR_INVALID_ARG;
+  *bytes = rotary_ws(r);
+  return EA_OK;
+}
+
+ea_status entmax_norm_rotary_bwd(const ea_rotary* r, const void* dq_out, const ea_strides* dq_out_strides,
+                                 const void* dk_out, const ea_strides* dk_out_strides, const void* q,
+                                 const ea_strides* q_strides, const void* k, const ea_strides* k_strides,
+                                 const int32_t* positions, int64_t position_stride, const float* freqs,
+                                 const void* q_weight, const void* k_weight, void* dq, void* dk,
+                                 float* dq_weight, float* dk_weight, void* workspace, size_t ws_bytes,
+                                 void* stream) {
+  ea_status st = check_rotary(r);
+  if (st != EA_OK || r->tokens == 0) return st;
+  RotaryArgs a;
+  st = prep_rotary(r, q, q_strides, k, k_strides, positions, position_stride, freqs, q_weight, k_weight, &a);
+  if (st != EA_OK) return st;
+  const size_t es = size_of(r->dtype);
+  if (!tensor_ok(dq_out) || !tensor_ok(dk_out) || !strides_ok(dq_out_strides, es) || !strides_ok(dk_out_strides, es))
+    return EA_ERR_INVALID_ARG;
+  if (!tensor_ok(dq) || !tensor_ok(dk) || !aligned(dq_weight, 4) || !aligned(dk_weight, 4)) return EA_ERR_INVALID_ARG;
+  if (!tensor_ok(workspace)) return EA_ERR_INVALID_ARG;
+  if (ws_bytes < rotary_ws(r)) return EA_ERR_WORKSPACE;
+  const int64_t d = r->head_dim;
+  a.dq = {const_cast<void*>(dq_out), dq_out_strides->row, dq_out_strides->head};
+  a.dk = {const_cast<void*>(dk_out), dk_out_strides->row, dk_out_strides->head};
+  a.q_out = {dq, r->heads * d, d};
+  a.k_out = {dk, r->kv_heads * d, d};
+  a.partials = static_cast<float*>(workspace);
+  a.partial_count = rotary_partials(r->tokens);
+  a.dq_weight = dq_weight;
+  a.dk_weight = dk_weight;
+  return from_hip(launch_rotary_bwd(a, r->dtype, static_cast<hipStream_t>(stream)));
+}
+
+// ------------------------------------------------ packed sequences
+
+namespace {
+
+ea_status check_plan(int32_t tokens, int32_t seqs) {
+  if (tokens < 1 || seqs < 1) return EA_ERR_INVALID_ARG;
+  // tiles and rows are 32-bit numbers
+  return (int64_t)tokens / 64 + seqs > (1 << 26) ? EA_ERR_UNSUPPORTED : EA_OK;
+}
+
+size_t plan_parts(int32_t tokens, int32_t seqs, void* base, PlanArgs* a) {
+  Parts p{static_cast<char*>(base)};
+  a->header = p.take<PackedHeader>(1);
+  a->seqs = p.take<PackedSeq>((size_t)seqs);
+  for (int z = 0; z < 3; ++z) a->tiles[z] = p.take<PackedTile>((size_t)packed_tiles(tokens, seqs, z));
+  return p.at;
+}
+
+struct PackedResiduals {
+  float *tau, *tau_lo, *o2;
+  int32_t *q_count, *q_index, *k_count, *k_index;
+  uint8_t* mask;
+};
+
+size_t residual_parts(const ea_packed_shape* s, const ea_params* p, void* base, PackedResiduals* r) {
+  const size_t rows = (size_t)s->heads * s->tokens, width = ((size_t)s->max_seqlen + 63) / 64;
+  const size_t blocks = (size_t)s->heads * packed_tiles(s->tokens, s->seqs, 0);
+  Parts x{static_cast<char*>(base)};
+  r->tau = x.take<float>(rows);
+  r->tau_lo = x.take<float>(s->dtype == EA_F32 ? rows : 0);
+  r->q_count = x.take<int32_t>(blocks);
+  r->q_index = x.take<int32_t>(blocks * width);
+  r->mask = x.take<uint8_t>(blocks * width);
+  r->o2 = x.take<float>(p->need_bwd ? rows * s->head_dim : 0);
+  r->k_count = x.take<int32_t>(p->need_bwd ? blocks : 0);
+  r->k_index = x.take<int32_t>(p->need_bwd ? blocks * width : 0);
+  return x.at;
+}
+
+ea_status check_packed(const ea_packed_shape* s, const ea_params* p) {
+  if (!s || !p) return EA_ERR_INVALID_ARG;
+  ea_status st = check_plan(s->tokens, s->seqs);
+  if (st != EA_OK) return st;
+  if (s->max_seqlen < 1 || s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads != 0) return EA_ERR_INVALID_ARG;
+  if (!dtype_ok(s->dtype) || (s->head_dim != 64 && s->head_dim != 128)) return EA_ERR_UNSUPPORTED;
+  if (s->max_seqlen > MAX_SEQLEN) return EA_ERR_UNSUPPORTED;
+  if ((st = check_params(p)) != EA_OK) return st;
+  // grids and row numbers over all heads are 32-bit numbers
+  if ((int64_t)s->heads * packed_tiles(s->tokens, s->seqs, 0) > INT32_MAX / 2) return EA_ERR_UNSUPPORTED;
+  return EA_OK;
+}
+
+int packed_parts(const ea_packed_shape* s) {
+  return dkdv_packed_parts(s->tokens, s->seqs, s->heads, s->kv_heads, s->dtype, s->head_dim);
+}
+
+size_t packed_ws_fwd(const ea_packed_shape* s) {
+  const int64_t tiles = (int64_t)s->heads * packed_tiles(s->tokens, s->seqs, 2);
+  return (size_t)(tiles < MAX_SOLVE_SLOTS ? tiles : MAX_SOLVE_SLOTS) * SOLVE_SLOT_BYTES;
+}
+size_t packed_ws_bwd(const ea_packed_shape* s) {
+  const int parts = packed_parts(s);
+  const size_t sums = parts > 1 ? 2 * (size_t)parts * s->tokens * s->kv_heads * s->head_dim * 4 : 0;
+  return up256((size_t)s->heads * s->tokens * 4) + sums;
+}
+
+// A tile copy's offsets are 32-bit numbers of elements.
+bool packed_strides_ok(const ea_packed_strides* st, size_t es) {
+  if (!st) return false;
+  for (const ea_strides* s : {&st->q, &st->k, &st->v, &st->o})
+    if (!strides_ok(s, es) || s->row > (1 << 24)) return false;
+  return true;
+}
+
+PackedArgs packed_args(const ea_packed_shape* s, const void* plan, const ea_packed_strides* st, int32_t zero_rest) {
+  PlanArgs parts{};
+  plan_parts(s->tokens, s->seqs, const_cast<void*>(plan), &parts);
+  PackedArgs a{};
+  a.header = parts.header;
+  a.seqs = parts.seqs;
+  for (int z = 0; z < 3; ++z) a.lists[z] = parts.tiles[z];
+  a.seq_count = s->seqs;
+  a.heads = s->heads;
+  a.kv_heads = s->kv_heads;
+  a.group = s->heads / s->kv_heads;
+  a.tokens = s->tokens;
+  a.blocks = packed_tiles(s->tokens, s->seqs, 0);
+  a.width = (s->max_seqlen + 63) / 64;
+  auto strides = [](const ea_strides& x) { return Strides{(int)x.row, x.head}; };
+  a.q = strides(st->q);
+  a.k = strides(st->k);
+  a.v = strides(st->v);
+  a.o = strides(st->o);
+  a.zero_rest = zero_rest;
+  a.parts = 1;
+  return a;
+}
+
+// Checks shared by the two passes.
+ea_status prep_packed(const ea_packed_shape* shape, const ea_params* params, const void* plan, const void* q,
+                      const void* k, const void* v, const void* o, const ea_packed_strides* strides,
+                      const void* residuals, size_t residual_bytes, PackedResiduals* r) {
+  const ea_status st = check_packed(shape, params);
+  if (st != EA_OK) return st;
+  if (!tensor_ok(plan) || !tensor_ok(q) || !tensor_ok(k) || !tensor_ok(v) || !tensor_ok(o) || !tensor_ok(residuals))
+    return EA_ERR_INVALID_ARG;
+  if (!packed_strides_ok(strides, size_of(shape->dtype))) return EA_ERR_INVALID_ARG;
+  return residual_bytes < residual_parts(shape, params, const_cast<void*>(residuals), r) ? EA_ERR_WORKSPACE : EA_OK;
+}
+
+}  // namespace
+
+ea_status entmax_packed_plan_bytes(int32_t tokens, int32_t seqs, size_t* bytes) {
+  const ea_status st = check_plan(tokens, seqs);
+  if (st != EA_OK) return st;
+  if (!bytes) return EA_ERR_INVALID_ARG;
+  PlanArgs a{};
+  *bytes = plan_parts(tokens, seqs, nullptr, &a);
+  return EA_OK;
+}
+
+ea_status entmax_packed_plan(int32_t tokens, int32_t seqs, int32_t max_seqlen, int32_t causal, const int32_t* cu,
+                             void* plan, size_t plan_bytes, void* stream) {
+  const ea_status st = check_plan(tokens, seqs);
+  if (st != EA_OK) return st;
+  if (max_seqlen < 1 || (causal != 0 && causal != 1)) return EA_ERR_INVALID_ARG;
+  if (max_seqlen > MAX_SEQLEN) return EA_ERR_UNSUPPORTED;
+  if (!small_ok(cu) || !tensor_ok(plan)) return EA_ERR_INVALID_ARG;
+  PlanArgs a{};
+  if (plan_bytes < plan_parts(tokens, seqs, plan, &a)) return EA_ERR_WORKSPACE;
+  a.cu = cu;
+  a.seq_count = seqs;
+  a.tokens = tokens;
+  a.max_seqlen = max_seqlen;
+  a.causal = causal;
+  return from_hip(launch_plan(a, static_cast<hipStream_t>(stream)));
+}
+
+ea_status entmax_packed_sizes(const ea_packed_shape* shape, const ea_params* params, ea_packed_sizes* out) {
+  const ea_status st = check_packed(shape, params);
+  if (st != EA_OK) return st;
+  if (!out) return EA_ERR_INVALID_ARG;
+  PackedResiduals r;
+  out->residuals = residual_parts(shape, params, nullptr, &r);
+  out->ws_fwd = packed_ws_fwd(shape);
+  out->ws_bwd = packed_ws_bwd(shape);
+  return EA_OK;
+}
+
+ea_status entmax_packed_fwd(const ea_packed_shape* shape, const ea_params* params, const void* plan, const void* q,
+                            const void* k, const void* v, void* o, const ea_packed_strides* strides,
+                            int32_t zero_rest, void* residuals, size_t residual_bytes, void* workspace,
+                            size_t ws_bytes, void* stream) {
+  PackedResiduals r;
+  ea_status st = prep_packed(shape, params, plan, q, k, v, o, strides, residuals, residual_bytes, &r);
+  if (st != EA_OK) return st;
+  if (workspace && !aligned(workspace, 16)) return EA_ERR_INVALID_ARG;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const PackedArgs pk = packed_args(shape, plan, strides, zero_rest);
+  const int64_t most = (int64_t)shape->heads * packed_tiles(shape->tokens, shape->seqs, 2);
+  int64_t slots = workspace ? (int64_t)(ws_bytes / SOLVE_SLOT_BYTES) : 0;
+  if (slots > most) slots = most;
+  Packed<TauArgs> ta{};
+  ta.pk = pk;
+  ta.q = q;
+  ta.k = k;
+  ta.tau = r.tau;
+  ta.tau_lo = r.tau_lo;
+  ta.mask = r.mask;
+  ta.q_count = r.q_count;
+  ta.q_index = r.q_index;
+  ta.cand = slots > 0 ? workspace : nullptr;
+  ta.cap = SOLVE_QUAD_CAP;
+  ta.slots = (int)slots;
+  ta.c = (params->alpha - 1.0f) * params->scale;
+  ta.alpha = params->alpha;
+  ta.gamma = 1.0f / (params->alpha - 1.0f);
+  ta.causal = params->causal;
+  ta.max_iter = params->max_iter;
+  ta.tol = params->tol;
+  ta.gk = gamma_kind(params->alpha);
+  ta.c64 = c64_of(params);
+  ta.g64 = g64_of(params);
+  if ((st = from_hip(launch_tau_packed(ta, shape->dtype, shape->head_dim, s))) != EA_OK) return st;
+  Packed<FwdArgs> fa{};
+  fa.pk = pk;
+  fa.q = q;
+  fa.k = k;
+  fa.v = v;
+  fa.o = o;
+  fa.o2 = r.o2;
+  fa.tau = r.tau;
+  fa.tau_lo = shape->dtype == EA_F32 ? r.tau_lo : nullptr;
+  fa.q_count = r.q_count;
+  fa.q_index = r.q_index;
+  fa.mask = r.mask;
+  fa.k_count = r.k_count;
+  fa.k_index = r.k_index;
+  fa.c = ta.c;
+  fa.gamma = ta.gamma;
+  fa.causal = params->causal;
+  fa.gk = ta.gk;
+  fa.c64 = ta.c64;
+  fa.g64 = ta.g64;
+  return from_hip(launch_fwd_packed(fa, shape->dtype, shape->head_dim, params->need_bwd != 0, s));
+}
+
+ea_status entmax_packed_bwd(const ea_packed_shape* shape, const ea_params* params, const void* plan, const void* q,
+                            const void* k, const void* v, const void* dout, const ea_packed_strides* strides,
+                            int32_t zero_rest, const void* residuals, size_t residual_bytes, void* dq, void* dk,
+                            void* dv, void* workspace, size_t ws_bytes, void* stream) {
+  PackedResiduals r;
+  ea_status st = prep_packed(shape, params, plan, q, k, v, dout, strides, residuals, residual_bytes, &r);
+  if (st != EA_OK) return st;
+  if (!params->need_bwd || !tensor_ok(dq) || !tensor_ok(dk) || !tensor_ok(dv) || !tensor_ok(workspace))
+    return EA_ERR_INVALID_ARG;
+  if (ws_bytes < packed_ws_bwd(shape)) return EA_ERR_WORKSPACE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  Packed<DeltaArgs> da{};
+  da.pk = packed_args(shape, plan, strides, zero_rest);
+  da.dout = dout;
+  da.o2 = r.o2;
+  da.delta = static_cast<float*>(workspace);
+  da.rows = (int64_t)shape->heads * shape->tokens;
+  if ((st = from_hip(launch_delta_packed(da, shape->dtype, shape->head_dim, s))) != EA_OK) return st;
+  Packed<BwdArgs> ba{};
+  ba.pk = da.pk;
+  ba.pk.parts = packed_parts(shape);
+  if (ba.pk.parts > 1) {
+    ba.pk.dk_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + up256((size_t)da.rows * 4));
+    ba.pk.dv_part = ba.pk.dk_part + (size_t)ba.pk.parts * shape->tokens * shape->kv_heads * shape->head_dim;
+  }
+  ba.q = q;
+  ba.k = k;
+  ba.v = v;
+  ba.dout = dout;
+  ba.tau = r.tau;
+  ba.tau_lo = shape->dtype == EA_F32 ? r.tau_lo : nullptr;
+  ba.delta = da.delta;
+  ba.q_count = r.q_count;
+  ba.q_index = r.q_index;
+  ba.k_count = r.k_count;
+  ba.k_index = r.k_index;
+  ba.dq = static_cast<float*>(dq);  // (of the inputs' type: see the kernels)
+  ba.dk = static_cast<float*>(dk);
+  ba.dv = static_cast<float*>(dv);
+  ba.c = (params->alpha - 1.0f) * params->scale;
+  ba.gamma = 1.0f / (params->alpha - 1.0f);
+  ba.scale = params->scale;
+  ba.causal = params->causal;
+  ba.gk = gamma_kind(params->alpha);
+  ba.c64 = c64_of(params);
+  ba.g64 = g64_of(params);
+  if ((st = from_hip(launch_bwd_dkdv_packed(ba, shape->dtype, shape->head_dim, s))) != EA_OK) return st;
+  return from_hip(launch_bwd_dq_packed(ba, shape->dtype, shape->head_dim, s));
+}
+
+// ------------------------------------------------ single tokens
+
+namespace {
+
+ea_status check_decode(const ea_decode_shape* s) {
+  if (!s) return EA_ERR_INVALID_ARG;
+  if (s->requests < 0 || s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads != 0) return EA_ERR_INVALID_ARG;
+  if (s->prefix < 0 || s->capacity < 0) return EA_ERR_INVALID_ARG;
+  if (!dtype_ok(s->dtype) || (s->head_dim != 64 && s->head_dim != 128)) return EA_ERR_UNSUPPORTED;
+  if ((int64_t)s->prefix + s->capacity > MAX_SEQLEN) return EA_ERR_UNSUPPORTED;
+  if ((int64_t)s->requests * s->heads > INT32_MAX / 2) return EA_ERR_UNSUPPORTED;
+  return EA_OK;
+}
+
+size_t decode_parts(const ea_decode_shape* s, void* base, DecodeArgs* a) {
+  const size_t rows = (size_t)s->requests * s->heads;
+  const size_t pb = ((size_t)s->prefix + DEC_KEYS - 1) / DEC_KEYS, ob = ((size_t)s->capacity + DEC_KEYS - 1) / DEC_KEYS;
+  Parts p{static_cast<char*>(base)};
+  a->ps = p.take<float>(rows * pb * DEC_KEYS);
+  a->pm = p.take<float>(rows * pb);
+  a->os = p.take<float>(rows * ob * DEC_KEYS);
+  a->om = p.take<float>(rows * ob);
+  return p.at;
+}
+
+}  // namespace
+
+ea_status entmax_prefix_decode_workspace(const ea_decode_shape* shape, size_t* bytes) {
+  const ea_status st = check_decode(shape);
+  if (st != EA_OK) return st;
+  if (!bytes) return EA_ERR_INVALID_ARG;
+  DecodeArgs a{};
+  *bytes = decode_parts(shape, nullptr, &a);
+  return EA_OK;
+}
+
+ea_status entmax_prefix_decode(const ea_decode_shape* shape, const ea_params* params,
+                               const ea_decode_strides* st, const void* q, const void* k, const void* v,
+                               const int32_t* lengths, const void* k_prefix, const void* v_prefix, void* o,
+                               void* workspace, size_t ws_bytes, void* stream) {
+  ea_status status = check_decode(shape);
+  if (status != EA_OK) return status;
+  if (!params) return EA_ERR_INVALID_ARG;
+  if ((status = check_params(params)) != EA_OK) return status;
+  if (shape->requests == 0) return EA_OK;
+  const size_t es = size_of(shape->dtype);
+  const int64_t vec = 16 / (int64_t)es;
+  if (!st || !strides_ok(&st->q, es) || !strides_ok(&st->o, es)) return EA_ERR_INVALID_ARG;
+  if (!tensor_ok(q) || !tensor_ok(o) || !small_ok(lengths)) return EA_ERR_INVALID_ARG;
+  if (shape->capacity) {
+    if (!tensor_ok(k) || !tensor_ok(v) || !strides_ok(&st->k, es) || !strides_ok(&st->v, es)) return EA_ERR_INVALID_ARG;
+    for (int64_t x : {st->k_request, st->v_request})
+      if (x < 0 || x % vec != 0 || x > MAX_STRIDE) return EA_ERR_INVALID_ARG;
+  }
+  if (shape->prefix && (!tensor_ok(k_prefix) || !tensor_ok(v_prefix) || !strides_ok(&st->k_prefix, es) ||
+                        !strides_ok(&st->v_prefix, es)))
+    return EA_ERR_INVALID_ARG;
+  DecodeArgs a{};
+  const size_t need = decode_parts(shape, workspace, &a);
+  if (need && !tensor_ok(workspace)) return EA_ERR_INVALID_ARG;
+  if (ws_bytes < need) return EA_ERR_WORKSPACE;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.pk = k_prefix;
+  a.pv = v_prefix;
+  a.o = o;
+  a.q_row = st->q.row;
+  a.q_head = st->q.head;
+  a.o_row = st->o.row;
+  a.o_head = st->o.head;
+  a.k_batch = st->k_request;
+  a.k_row = st->k.row;
+  a.k_head = st->k.head;
+  a.v_batch = st->v_request;
+  a.v_row = st->v.row;
+  a.v_head = st->v.head;
+  a.pk_row = st->k_prefix.row;
+  a.pk_head = st->k_prefix.head;
+  a.pv_row = st->v_prefix.row;
+  a.pv_head = st->v_prefix.head;
+  a.lengths = lengths;
+  a.requests = shape->requests;
+  a.heads = shape->heads;
+  a.kv_heads = shape->kv_heads;
+  a.group = shape->heads / shape->kv_heads;
+  a.prefix = shape->prefix;
+  a.capacity = shape->capacity;
+  constexpr int RUN_KEYS = DEC_KEYS * DEC_RUN;
+  a.prefix_runs = (shape->prefix + RUN_KEYS - 1) / RUN_KEYS;
+  a.own_runs = (shape->capacity + RUN_KEYS - 1) / RUN_KEYS;
+  a.c = (params->alpha - 1.0f) * params->scale;
+  a.alpha = params->alpha;
+  a.gamma = 1.0f / (params->alpha - 1.0f);
+  a.tol = params->tol;
+  a.max_iter = params->max_iter;
+  a.gk = gamma_kind(params->alpha);
+  return from_hip(launch_decode(a, shape->dtype, shape->head_dim, static_cast<hipStream_t>(stream)));
 }
 
 const char* entmax_attn_status_string(ea_status s) {

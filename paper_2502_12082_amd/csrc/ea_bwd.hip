@@ -30,6 +30,7 @@
 
 #include "ea_common.h"
 #include "ea_internal.h"
+#include "ea_packed.h"
 
 namespace ea {
 
@@ -47,6 +48,25 @@ __global__ __launch_bounds__(256) void delta_kernel(DeltaArgs a) {
   float acc = 0.f;
   if (row < a.rows) {
     const E* dO = static_cast<const E*>(a.dout) + row * D + sl * PER;
+    const float* o2 = a.o2 + row * D + sl * PER;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) acc = fmaf((float)dO[e], o2[e], acc);
+  }
+#pragma unroll
+  for (int m = 8; m >= 1; m >>= 1) acc += __shfl_xor(acc, m);
+  if (row < a.rows && sl == 0) a.delta[row] = acc;
+}
+
+// Packed sequences: rows are (head, token), dO is given as the caller holds it.
+template <typename E, int D>
+__global__ __launch_bounds__(256) void delta_packed_kernel(Packed<DeltaArgs> a) {
+  constexpr int PER = D / 16;  // 16 lanes per row
+  const long long row = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const int sl = threadIdx.x & 15;
+  float acc = 0.f;
+  if (row < a.rows) {
+    const int h = (int)(row / a.pk.tokens), t = (int)(row % a.pk.tokens);
+    const E* dO = static_cast<const E*>(a.dout) + (int64_t)t * a.pk.o.row + h * a.pk.o.head + sl * PER;
     const float* o2 = a.o2 + row * D + sl * PER;
 #pragma unroll
     for (int e = 0; e < PER; ++e) acc = fmaf((float)dO[e], o2[e], acc);
@@ -528,8 +548,41 @@ __device__ int unlisted_blocks(const int32_t* list, int first, int cnt, const in
   return total;
 }
 
-template <typename E, int D, int GK>
-__global__ __launch_bounds__(BWD_NT) void dkdv_kernel(BwdArgs a) {
+// The packed forms' key head of a workgroup and its share of the query heads.
+struct KeyHead {
+  int first, count;  // query heads
+  int kb;            // key tile: those that most queries see come first
+};
+__device__ __forceinline__ KeyHead key_head(const PackedArgs& pk, const Place& at, bool causal) {
+  const int count = pk.group / pk.parts, tiles = (at.n + (64 << pk.size) - 1) / (64 << pk.size);
+  return {at.head * pk.group + at.part * count, count, causal ? tiles - 1 - at.tile : at.tile};
+}
+
+// Where a packed form writes value `x` of dK or dV: the gradient in the
+// inputs' type, or one of `parts` fp32 sums that reduce_parts_kernel adds up.
+template <typename E, int D>
+__device__ __forceinline__ void store_packed(const PackedArgs& pk, const Place& at, float* out, float* part,
+                                             int row, int col, float x) {
+  const int64_t off = ((int64_t)(at.start + row) * pk.kv_heads + at.head) * D + col;
+  if (pk.parts > 1)
+    part[(int64_t)at.part * pk.tokens * pk.kv_heads * D + off] = x;
+  else
+    reinterpret_cast<E*>(out)[off] = (E)x;
+}
+// dK and dV rows of no sequence (where they are not reduced from parts).
+template <typename E, int D, int NT, typename A>
+__device__ __forceinline__ void zero_rest_dkdv(const A& a, const Place& at) {
+  if (at.item != 0 || !a.pk.zero_rest || a.pk.parts > 1) return;
+  const Strides rows{a.pk.kv_heads * D, D};
+  zero_rest<E, D, NT>(a.pk, reinterpret_cast<E*>(a.dk), rows, at.head);
+  zero_rest<E, D, NT>(a.pk, reinterpret_cast<E*>(a.dv), rows, at.head);
+}
+
+// A = Packed<BwdArgs>: packed sequences; a workgroup adds up its share of the
+// query heads of a key head, one after another.
+template <typename E, int D, int GK, typename A>
+__global__ __launch_bounds__(BWD_NT) void dkdv_kernel(A a) {
+  constexpr bool PK = is_packed<A>::value;
   using TL = Tile<E, D>;
   using M = Mma<E>;
   constexpr int KS = D / M::KW;
@@ -541,19 +594,47 @@ __global__ __launch_bounds__(BWD_NT) void dkdv_kernel(BwdArgs a) {
   __shared__ __attribute__((aligned(16))) float del_s[2][BLK];
 
   const int lane = lane_id(), w = wave_id();
-  const int n = a.n, T = a.T;
-  const int bh = blockIdx.x % a.BH;
-  const int kb = blockIdx.x / a.BH;  // causal: small kb has the longest list
+  [[maybe_unused]] Place at;
+  [[maybe_unused]] KeyHead kh{};
+  if constexpr (PK) {
+    const bool work = packed_place(a.pk, blockIdx.x, a.pk.kv_heads * a.pk.parts, true, at);
+    zero_rest_dkdv<E, D, BWD_NT>(a, at);
+    if (!work) return;
+    kh = key_head(a.pk, at, a.causal);
+  }
+  const int n = PK ? at.n : a.n, T = PK ? at.T : a.T;
+  int bh = PK ? kh.first : blockIdx.x % a.BH;
+  const int kb = PK ? kh.kb : blockIdx.x / a.BH;  // causal: small kb has the longest list
   const int k0 = kb * BLK + 32 * w;
   const int j = k0 + (lane & 31);
   const bool wave_ok = k0 < n;
-  const size_t head = (size_t)bh * n * D;
-  const E* Qg = static_cast<const E*>(a.q) + head;
-  const E* Kg = static_cast<const E*>(a.k) + head;
-  const E* Vg = static_cast<const E*>(a.v) + head;
-  const E* dOg = static_cast<const E*>(a.dout) + head;
-  const float* taug = a.tau + (size_t)bh * n;
-  const float* delg = a.delta + (size_t)bh * n;
+  int ldq = D, ldk = D, ldv = D, ldo = D, width = T;
+  size_t row0 = (size_t)bh * n, blk = (size_t)bh * T + kb;
+  const size_t head = row0 * D;
+  const E* Qg = static_cast<const E*>(a.q);
+  const E* Kg = static_cast<const E*>(a.k);
+  const E* Vg = static_cast<const E*>(a.v);
+  const E* dOg = static_cast<const E*>(a.dout);
+  if constexpr (PK) {
+    ldq = a.pk.q.row;
+    ldk = a.pk.k.row;
+    ldv = a.pk.v.row;
+    ldo = a.pk.o.row;
+    width = a.pk.width;
+    row0 = (size_t)bh * a.pk.tokens + at.start;
+    blk = (size_t)bh * a.pk.blocks + at.block + kb;
+    Qg += (int64_t)at.start * ldq + bh * a.pk.q.head;
+    dOg += (int64_t)at.start * ldo + bh * a.pk.o.head;
+    Kg += (int64_t)at.start * ldk + at.head * a.pk.k.head;
+    Vg += (int64_t)at.start * ldv + at.head * a.pk.v.head;
+  } else {
+    Qg += head;
+    Kg += head;
+    Vg += head;
+    dOg += head;
+  }
+  const float* taug = a.tau + row0;
+  const float* delg = a.delta + row0;
   const float c = a.c, g = a.gamma;
   constexpr bool PRECISE = precise_path<E, GK>();
 
@@ -561,13 +642,13 @@ __global__ __launch_bounds__(BWD_NT) void dkdv_kernel(BwdArgs a) {
   // With element lists only the query blocks without them are: their entries
   // are compacted into `unlisted` first, and a key block that has none is
   // left to the list kernel.
-  const bool dense = a.k_index == nullptr;
-  const int32_t* list = dense ? nullptr : a.k_index + ((size_t)bh * T + kb) * T;
-  int cnt = dense ? (a.causal ? T - kb : T) : a.k_count[(size_t)bh * T + kb];
-  __shared__ uint16_t unlisted[LIST_MAX_SEQLEN / BLK];
-  const int sorted = a.lists ? sorted_blocks<BWD_NT>(a.buckets, bh, T) : 0;
-  if (a.lists && sorted == T) return;
-  const bool some = sorted > 0;
+  const bool dense = !PK && a.k_index == nullptr;
+  const int32_t* list = dense ? nullptr : a.k_index + blk * width;
+  int cnt = dense ? (a.causal ? T - kb : T) : a.k_count[blk];
+  __shared__ uint16_t unlisted[PK ? 1 : LIST_MAX_SEQLEN / BLK];
+  const int sorted = !PK && a.lists ? sorted_blocks<BWD_NT>(a.buckets, bh, T) : 0;
+  if (!PK && a.lists && sorted == T) return;
+  const bool some = !PK && sorted > 0;
   if (some) {
     cnt = unlisted_blocks<BWD_NT>(list, a.causal ? kb : 0, cnt, a.buckets.used + (size_t)bh * T, unlisted);
     if (cnt == 0) return;
@@ -577,8 +658,8 @@ __global__ __launch_bounds__(BWD_NT) void dkdv_kernel(BwdArgs a) {
   typename M::frag kf[KS], vf[KS];
 #pragma unroll
   for (int kk = 0; kk < KS; ++kk) {
-    kf[kk] = load_row_frag_global<E, D>(Kg, j, n, kk);
-    vf[kk] = load_row_frag_global<E, D>(Vg, j, n, kk);
+    kf[kk] = load_row_frag_global<E, D>(Kg, j, n, kk, ldk);
+    vf[kk] = load_row_frag_global<E, D>(Vg, j, n, kk, ldv);
   }
 
   f32x16 dk[NTD], dv[NTD];
@@ -625,10 +706,10 @@ __global__ __launch_bounds__(BWD_NT) void dkdv_kernel(BwdArgs a) {
           const float band = PRECISE_BAND * fmaxf(1.f, fabsf(tq[e]));
           const float raw = fmaf(c, s[r], -tq[e]);
           double t64 = tq[e];
-          if (ok && fabsf(raw) < band && a.tau_lo) t64 += (double)a.tau_lo[(size_t)bh * n + i];
+          if (ok && fabsf(raw) < band && a.tau_lo) t64 += (double)a.tau_lo[row0 + i];
           zp = precise_relu_z<D>(ok, c, s[r], tq[e], band, t64,
-                                 reinterpret_cast<const float*>(Qg) + (size_t)i * D,
-                                 reinterpret_cast<const float*>(Kg) + (size_t)j * D, a.c64);
+                                 reinterpret_cast<const float*>(Qg) + (size_t)i * ldq,
+                                 reinterpret_cast<const float*>(Kg) + (size_t)j * ldk, a.c64);
         } else {
           zp = relu_z(c, s[r], tq[e]);
         }
@@ -653,41 +734,72 @@ __global__ __launch_bounds__(BWD_NT) void dkdv_kernel(BwdArgs a) {
   };
 
   float tv = 0.f, dlv = 0.f;
-  DmaPlan<E, D, BWD_NT> dma;
-  dma.init();
+  DmaPlan<E, D, BWD_NT, PK> dma, dma_o;
+  dma.init(ldq);
+  if constexpr (PK) dma_o.init(ldo);
   auto issue = [&](int e) {
     const int qb = qb_of(e);
     dma.issue(qbuf[e & 1], Qg, qb * BLK, n);
-    dma.issue(dobuf[e & 1], dOg, qb * BLK, n);
+    (PK ? dma_o : dma).issue(dobuf[e & 1], dOg, qb * BLK, n);
     if (threadIdx.x < BLK) {
       const int r = min(qb * BLK + (int)threadIdx.x, n - 1);
       tv = taug[r];
       dlv = delg[r];
     }
   };
-  if (cnt > 0) issue(0);
-  for (int e = 0; e < cnt; ++e) {
-    dma_wait();
-    if (threadIdx.x < BLK) {
-      tau_s[e & 1][threadIdx.x] = tv;
-      del_s[e & 1][threadIdx.x] = dlv;
-    }
-    __syncthreads();
-    const int qb = qb_of(e);
-    if (e + 1 < cnt) issue(e + 1);
-    if (!wave_ok) continue;
-    const E* qt = qbuf[e & 1];
-    const E* dt = dobuf[e & 1];
+  for (int x = 0;;) {
+    if (cnt > 0) issue(0);
+    for (int e = 0; e < cnt; ++e) {
+      dma_wait();
+      if (threadIdx.x < BLK) {
+        tau_s[e & 1][threadIdx.x] = tv;
+        del_s[e & 1][threadIdx.x] = dlv;
+      }
+      __syncthreads();
+      const int qb = qb_of(e);
+      if (e + 1 < cnt) issue(e + 1);
+      if (!wave_ok) continue;
+      const E* qt = qbuf[e & 1];
+      const E* dt = dobuf[e & 1];
 #pragma unroll
-    for (int qh = 0; qh < 2; ++qh) {
-      const int i0 = qb * BLK + 32 * qh;
-      if (i0 >= n || (a.causal && k0 > i0 + 31)) continue;
-      const bool masked = i0 + 31 >= n || k0 + 31 >= n || (a.causal && k0 + 31 > i0);
-      block(masked, qt, dt, tau_s[e & 1], del_s[e & 1], qh, i0);
+      for (int qh = 0; qh < 2; ++qh) {
+        const int i0 = qb * BLK + 32 * qh;
+        if (i0 >= n || (a.causal && k0 > i0 + 31)) continue;
+        const bool masked = i0 + 31 >= n || k0 + 31 >= n || (a.causal && k0 + 31 > i0);
+        block(masked, qt, dt, tau_s[e & 1], del_s[e & 1], qh, i0);
+      }
+    }
+    if constexpr (PK) {  // the next query head of this key head
+      if (++x == kh.count) break;
+      __syncthreads();  // (every wave is done with the tiles)
+      Qg += a.pk.q.head;
+      dOg += a.pk.o.head;
+      row0 += a.pk.tokens;
+      blk += a.pk.blocks;
+      taug = a.tau + row0;
+      delg = a.delta + row0;
+      list = a.k_index + blk * width;
+      cnt = a.k_count[blk];
+    } else {
+      break;
     }
   }
 
   if (!wave_ok) return;
+  if constexpr (PK) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int key = k0 + crow(r);
+      if (key < n) {
+#pragma unroll
+        for (int nt = 0; nt < NTD; ++nt) {
+          store_packed<E, D>(a.pk, at, a.dk, a.pk.dk_part, key, 32 * nt + (lane & 31), a.scale * dk[nt][r]);
+          store_packed<E, D>(a.pk, at, a.dv, a.pk.dv_part, key, 32 * nt + (lane & 31), dv[nt][r]);
+        }
+      }
+    }
+    return;
+  }
   float* dK = a.dk + head;
   float* dV = a.dv + head;
 #pragma unroll
@@ -725,8 +837,11 @@ __global__ __launch_bounds__(BWD_NT) void dkdv_kernel(BwdArgs a) {
 // flight.  The tables are read by scalar loads for the same reason.
 constexpr int BWD2_NT = 512;
 
-template <int D, int GK>
-__global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(BwdArgs a) {
+// A = Packed<BwdArgs>: packed sequences; the lists of a workgroup's query heads
+// follow one another, so that the copies never run dry between heads.
+template <int D, int GK, typename A>
+__global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(A a) {
+  constexpr bool PK = is_packed<A>::value;
   using E = __bf16;
   using TL = Tile<E, D>;
   using M = Mma<E>;
@@ -744,42 +859,71 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(BwdArgs a) {
 
   const int lane = lane_id(), w = wave_id();
   const int kh = (w >> 1) & 1, ch = w & 1;
-  const int n = a.n, T = a.T;
-  const int bh = blockIdx.x % a.BH;
-  const int kbA = 2 * (blockIdx.x / a.BH);  // causal: small key blocks have the longest lists
+  [[maybe_unused]] Place at;
+  [[maybe_unused]] KeyHead khead{};
+  if constexpr (PK) {
+    const bool work = packed_place(a.pk, blockIdx.x, a.pk.kv_heads * a.pk.parts, true, at);
+    zero_rest_dkdv<E, D, BWD2_NT>(a, at);
+    if (!work) return;
+    khead = key_head(a.pk, at, a.causal);
+  }
+  const int n = PK ? at.n : a.n, T = PK ? at.T : a.T;
+  const int bh = PK ? khead.first : blockIdx.x % a.BH;
+  const int kbA = 2 * (PK ? khead.kb : blockIdx.x / a.BH);  // causal: small key blocks have the longest lists
   const int kbB = kbA + 1;
   const bool mineA = (w >> 2) == 0;
   const int k0 = (mineA ? kbA : kbB) * BLK + 32 * kh;
   const int j = k0 + (lane & 31);
   const bool wave_ok = k0 < n;
-  const size_t head = (size_t)bh * n * D;
-  const E* Qg = static_cast<const E*>(a.q) + head;
-  const E* Kg = static_cast<const E*>(a.k) + head;
-  const E* Vg = static_cast<const E*>(a.v) + head;
-  const E* dOg = static_cast<const E*>(a.dout) + head;
-  [[maybe_unused]] const float* taug = a.tau + (size_t)bh * n;  // read by tile copies
-  [[maybe_unused]] const float* delg = a.delta + (size_t)bh * n;
+  int ldq = D, ldk = D, ldv = D, ldo = D, width = T;
+  size_t row0 = (size_t)bh * n, blk0 = (size_t)bh * T;
+  const size_t head = row0 * D;
+  const E* Qg = static_cast<const E*>(a.q);
+  const E* Kg = static_cast<const E*>(a.k);
+  const E* Vg = static_cast<const E*>(a.v);
+  const E* dOg = static_cast<const E*>(a.dout);
+  if constexpr (PK) {
+    ldq = a.pk.q.row;
+    ldk = a.pk.k.row;
+    ldv = a.pk.v.row;
+    ldo = a.pk.o.row;
+    width = a.pk.width;
+    row0 = (size_t)bh * a.pk.tokens + at.start;
+    blk0 = (size_t)bh * a.pk.blocks + at.block;
+    Qg += (int64_t)at.start * ldq + bh * a.pk.q.head;
+    dOg += (int64_t)at.start * ldo + bh * a.pk.o.head;
+    Kg += (int64_t)at.start * ldk + at.head * a.pk.k.head;
+    Vg += (int64_t)at.start * ldv + at.head * a.pk.v.head;
+  } else {
+    Qg += head;
+    Kg += head;
+    Vg += head;
+    dOg += head;
+  }
+  [[maybe_unused]] const float* taug = a.tau + row0;  // read by tile copies
+  [[maybe_unused]] const float* delg = a.delta + row0;
   const float c = a.c, g = a.gamma;
 
   // Query-block lists of the two key blocks (without tables, in the no-mask
   // mode, every valid query block), merged in ascending order.
-  const bool dense = a.k_index == nullptr;
+  const bool dense = !PK && a.k_index == nullptr;
   const ci32* kcount = (const ci32*)a.k_count;
   const ci32* kindex = (const ci32*)a.k_index;
-  __shared__ uint16_t unlisted[2][LIST_MAX_SEQLEN / BLK];
-  const int sorted = a.lists ? sorted_blocks<BWD2_NT>(a.buckets, bh, T) : 0;
-  if (a.lists && sorted == T) return;
-  const bool some = sorted > 0;
+  __shared__ uint16_t unlisted[2][PK ? 1 : LIST_MAX_SEQLEN / BLK];
+  const int sorted = !PK && a.lists ? sorted_blocks<BWD2_NT>(a.buckets, bh, T) : 0;
+  if (!PK && a.lists && sorted == T) return;
+  const bool some = !PK && sorted > 0;
   auto count_of = [&](int kb) {
     if (kb >= T) return 0;
-    return dense ? (a.causal ? T - kb : T) : kcount[(size_t)bh * T + kb];
+    return dense ? (a.causal ? T - kb : T) : kcount[blk0 + kb];
   };
   auto entry_of = [&](auto left, int kb, int e) {
     if constexpr (decltype(left)::value) return __builtin_amdgcn_readfirstlane((int)unlisted[kb - kbA][e]);
-    return dense ? (a.causal ? kb + e : e) : kindex[((size_t)bh * T + kb) * T + e];
+    return dense ? (a.causal ? kb + e : e) : kindex[(blk0 + kb) * width + e];
   };
   int nA = count_of(kbA), nB = count_of(kbB);
   int pA = 0, pB = 0;
+  int hn = 0;  // query head of the next entry, after the first (packed forms)
   // With element lists, only the query blocks without them (see dkdv_kernel).
   if (some) {
     const int32_t* used = a.buckets.used + (size_t)bh * T;
@@ -793,7 +937,17 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(BwdArgs a) {
     nB = __builtin_amdgcn_readfirstlane(nB);
   }
   // the next query block of the union, and whether each key block lists it
-  auto next = [&](auto left, int& qb, bool& inA, bool& inB) {
+  auto next = [&](auto left, int& h, int& qb, bool& inA, bool& inB) {
+    if constexpr (PK) {
+      while (pA >= nA && pB >= nB) {
+        if (++hn >= khead.count) return false;
+        blk0 += a.pk.blocks;
+        nA = count_of(kbA);
+        nB = count_of(kbB);
+        pA = pB = 0;
+      }
+      h = hn;
+    }
     const int hA = pA < nA ? entry_of(left, kbA, pA) : T;
     const int hB = pB < nB ? entry_of(left, kbB, pB) : T;
     qb = min(hA, hB);
@@ -807,8 +961,8 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(BwdArgs a) {
   F kf[KS], vf[KS];
 #pragma unroll
   for (int kk = 0; kk < KS; ++kk) {
-    kf[kk] = load_row_frag_global<E, D>(Kg, j, n, kk);
-    vf[kk] = load_row_frag_global<E, D>(Vg, j, n, kk);
+    kf[kk] = load_row_frag_global<E, D>(Kg, j, n, kk, ldk);
+    vf[kk] = load_row_frag_global<E, D>(Vg, j, n, kk, ldv);
   }
 
   f32x16 dk[NTH], dv[NTH];
@@ -875,18 +1029,26 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(BwdArgs a) {
     return i0 + 31 >= n || k0 + 31 >= n || (a.causal && k0 + 31 > i0);
   };
 
-  using Plan = DmaPlan<E, D, BWD2_NT>;
+  using Plan = DmaPlan<E, D, BWD2_NT, PK>;
   static_assert(Plan::NI % Plan::NW == 0 && 2 * Plan::PER + 2 <= 15, "copy counts");
-  Plan dma;
-  dma.init();
-  // Copies of query block qb into stage b: the Q and dO tiles, and (wave 0)
-  // its tau and delta values, all by global_load_lds.
-  auto issue = [&](int qb, int b) {
-    dma.issue(qbuf[b], Qg, qb * BLK, n);
-    dma.issue(dobuf[b], dOg, qb * BLK, n);
+  Plan dma, dma_o;
+  dma.init(ldq);
+  if constexpr (PK) dma_o.init(ldo);
+  // Copies of query block qb (of the workgroup's query head h) into stage b:
+  // the Q and dO tiles, and (wave 0) its tau and delta values, all by
+  // global_load_lds.
+  auto issue = [&](int h, int qb, int b) {
+    if constexpr (PK) {
+      dma.issue(qbuf[b], Qg + h * a.pk.q.head, qb * BLK, n);
+      dma_o.issue(dobuf[b], dOg + h * a.pk.o.head, qb * BLK, n);
+    } else {
+      dma.issue(qbuf[b], Qg, qb * BLK, n);
+      dma.issue(dobuf[b], dOg, qb * BLK, n);
+    }
 #if defined(__HIP_DEVICE_COMPILE__)
     if (w == 0) {
-      const int r = min(qb * BLK + lane, n - 1);
+      size_t r = (size_t)min(qb * BLK + lane, n - 1);
+      if constexpr (PK) r += (size_t)h * a.pk.tokens;
       __builtin_amdgcn_global_load_lds(taug + r, to_lds(&tau_s[b][0]), 4, 0, 0);
       __builtin_amdgcn_global_load_lds(delg + r, to_lds(&del_s[b][0]), 4, 0, 0);
     }
@@ -938,17 +1100,17 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(BwdArgs a) {
   // that the one over whole tables keeps its scalar loads alone.
   auto run = [&](auto left) {
     // Union entries e (stage b0), e + 1 and e + 2 (in flight).
-    int q0 = 0, q1 = 0;
+    int q0 = 0, q1 = 0, g0 = 0, g1 = 0;
     bool a0 = false, b0_ = false, a1 = false, b1_ = false;
-    bool h0 = next(left, q0, a0, b0_);
-    bool h1 = h0 && next(left, q1, a1, b1_);
-    if (h0) issue(q0, 0);
-    if (h1) issue(q1, 1);
+    bool h0 = next(left, g0, q0, a0, b0_);
+    bool h1 = h0 && next(left, g1, q1, a1, b1_);
+    if (h0) issue(g0, q0, 0);
+    if (h1) issue(g1, q1, 1);
     int st = 0;
     while (h0) {
-      int q2 = 0;
+      int q2 = 0, g2 = 0;
       bool a2 = false, b2_ = false;
-      const bool h2 = h1 && next(left, q2, a2, b2_);
+      const bool h2 = h1 && next(left, g2, q2, a2, b2_);
       if (h1) {
         wait_all_but_latest();
       } else {
@@ -957,7 +1119,7 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(BwdArgs a) {
       // block q0 is staged (each wave waited for its own copies); every wave
       // is done with the previous step, whose stage receives block q2
       lds_barrier();
-      if (h2) issue(q2, st == 0 ? 2 : st - 1);
+      if (h2) issue(g2, q2, st == 0 ? 2 : st - 1);
       const bool act = wave_ok && (mineA ? a0 : b0_);
       if (act) phase1(q0, st, st);
       lds_barrier();  // the posted operands are visible
@@ -979,6 +1141,21 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(BwdArgs a) {
     run(std::false_type{});
 
   if (!wave_ok) return;
+  if constexpr (PK) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int key = k0 + crow(r);
+      if (key < n) {
+#pragma unroll
+        for (int nt = 0; nt < NTH; ++nt) {
+          const int col = 32 * (ch * NTH + nt) + (lane & 31);
+          store_packed<E, D>(a.pk, at, a.dk, a.pk.dk_part, key, col, a.scale * dk[nt][r]);
+          store_packed<E, D>(a.pk, at, a.dv, a.pk.dv_part, key, col, dv[nt][r]);
+        }
+      }
+    }
+    return;
+  }
   float* dK = a.dk + head;
   float* dV = a.dv + head;
 #pragma unroll
@@ -1368,8 +1545,10 @@ __device__ __forceinline__ void gather_dq(const BwdArgs& a, const ListBlock& lb,
   }
 }
 
-template <typename E, int D, int GK>
-__global__ __launch_bounds__(DQ_NT, 2) void dq_kernel(BwdArgs a) {
+// A = Packed<BwdArgs>: packed sequences, dQ in the inputs' type.
+template <typename E, int D, int GK, typename A>
+__global__ __launch_bounds__(DQ_NT, 2) void dq_kernel(A a) {
+  constexpr bool PK = is_packed<A>::value;
   using TL = Tile<E, D>;
   using M = Mma<E>;
   constexpr int KS = D / M::KW;
@@ -1381,44 +1560,73 @@ __global__ __launch_bounds__(DQ_NT, 2) void dq_kernel(BwdArgs a) {
 
   const int lane = lane_id(), w = wave_id();
   const int qh = w & 1, kh = w >> 1;
-  const int n = a.n, T = a.T;
-  int bh = blockIdx.x % a.BH;
-  int qb = blockIdx.x / a.BH;
-  if (a.lists) head_major(blockIdx.x, a.BH, T, bh, qb, head_group<E, D>(n, 2));
-  if (a.causal) qb = T - 1 - qb;  // longest lists first
-  if (a.lists && (a.buckets.used[(size_t)bh * T + qb] & LISTED)) {
-    gather_dq<E, D, GK>(a, a.lists[(size_t)bh * T + qb], bh, qb);
-    return;
+  [[maybe_unused]] Place at;
+  if constexpr (PK) {
+    const bool work = packed_place(a.pk, blockIdx.x, a.pk.heads, false, at);
+    if (at.item == 0 && a.pk.zero_rest)
+      zero_rest<E, D, DQ_NT>(a.pk, reinterpret_cast<E*>(a.dq), Strides{a.pk.heads * D, D}, at.head);
+    if (!work) return;
+  }
+  const int n = PK ? at.n : a.n, T = PK ? at.T : a.T;
+  int bh = PK ? at.head : blockIdx.x % a.BH;
+  int qb = PK ? at.tile : blockIdx.x / a.BH;
+  if constexpr (!PK) {
+    if (a.lists) head_major(blockIdx.x, a.BH, T, bh, qb, head_group<E, D>(n, 2));
+    if (a.causal) qb = T - 1 - qb;  // longest lists first
+    if (a.lists && (a.buckets.used[(size_t)bh * T + qb] & LISTED)) {
+      gather_dq<E, D, GK>(a, a.lists[(size_t)bh * T + qb], bh, qb);
+      return;
+    }
   }
   const int q0 = qb * BLK + 32 * qh;
   const int i = q0 + (lane & 31);
   const bool wave_ok = q0 < n;
   const int wave_last = min(n - 1, q0 + 31);
-  const size_t head = (size_t)bh * n * D;
-  const E* Qg = static_cast<const E*>(a.q) + head;
-  const E* Kg = static_cast<const E*>(a.k) + head;
-  const E* Vg = static_cast<const E*>(a.v) + head;
-  const E* dOg = static_cast<const E*>(a.dout) + head;
-  const float tau = i < n ? a.tau[(size_t)bh * n + i] : 0.f;
-  const float del = i < n ? a.delta[(size_t)bh * n + i] : 0.f;
+  const size_t row0 = PK ? at.row0 : (size_t)bh * n;
+  const size_t blk = (PK ? at.blk0 : (size_t)bh * T) + qb;
+  const size_t head = row0 * D;
+  int width = T, ldq = D, ldk = D, ldv = D, ldo = D;
+  const E* Qg = static_cast<const E*>(a.q);
+  const E* Kg = static_cast<const E*>(a.k);
+  const E* Vg = static_cast<const E*>(a.v);
+  const E* dOg = static_cast<const E*>(a.dout);
+  if constexpr (PK) {
+    width = a.pk.width;
+    ldq = a.pk.q.row;
+    ldk = a.pk.k.row;
+    ldv = a.pk.v.row;
+    ldo = a.pk.o.row;
+    const int kv = bh / a.pk.group;
+    Qg += (int64_t)at.start * ldq + bh * a.pk.q.head;
+    dOg += (int64_t)at.start * ldo + bh * a.pk.o.head;
+    Kg += (int64_t)at.start * ldk + kv * a.pk.k.head;
+    Vg += (int64_t)at.start * ldv + kv * a.pk.v.head;
+  } else {
+    Qg += head;
+    Kg += head;
+    Vg += head;
+    dOg += head;
+  }
+  const float tau = i < n ? a.tau[row0 + i] : 0.f;
+  const float del = i < n ? a.delta[row0 + i] : 0.f;
   const float c = a.c, g = a.gamma;
   constexpr bool PRECISE = precise_path<E, GK>();
   // fp32 inputs, general alpha: fp64 z near the support edge (ea_common.h)
   [[maybe_unused]] const double tau64 =
-      (double)tau + (PRECISE && a.tau_lo && i < n ? (double)a.tau_lo[(size_t)bh * n + i] : 0.0);
+      (double)tau + (PRECISE && a.tau_lo && i < n ? (double)a.tau_lo[row0 + i] : 0.0);
   [[maybe_unused]] const float band = PRECISE_BAND * fmaxf(1.f, fabsf(tau));
 
   typename M::frag qf[KS], df[KS];
 #pragma unroll
   for (int kk = 0; kk < KS; ++kk) {
-    qf[kk] = load_row_frag_global<E, D>(Qg, i, n, kk);
-    df[kk] = load_row_frag_global<E, D>(dOg, i, n, kk);
+    qf[kk] = load_row_frag_global<E, D>(Qg, i, n, kk, ldq);
+    df[kk] = load_row_frag_global<E, D>(dOg, i, n, kk, ldo);
   }
 
   // Without tables (the no-mask mode) every valid key block is visited.
-  const bool dense = a.q_index == nullptr;
-  const ci32* list = (const ci32*)(dense ? nullptr : a.q_index + ((size_t)bh * T + qb) * T);
-  const int cnt = dense ? (a.causal ? qb + 1 : T) : ((const ci32*)a.q_count)[(size_t)bh * T + qb];
+  const bool dense = !PK && a.q_index == nullptr;
+  const ci32* list = (const ci32*)(dense ? nullptr : a.q_index + blk * width);
+  const int cnt = dense ? (a.causal ? qb + 1 : T) : ((const ci32*)a.q_count)[blk];
   auto kb_of = [&](int e) { return dense ? e : list[e]; };
 
   f32x16 dq[NTD];
@@ -1432,11 +1640,12 @@ __global__ __launch_bounds__(DQ_NT, 2) void dq_kernel(BwdArgs a) {
     return 1;
   };
 
-  DmaPlan<E, D, DQ_NT> dma;
-  dma.init();
+  DmaPlan<E, D, DQ_NT, PK> dma, dma_v;
+  dma.init(ldk);
+  if constexpr (PK) dma_v.init(ldv);
   auto issue = [&](int kb, int e) {
     dma.issue(kbuf[e & 1], Kg, kb * BLK, n);
-    dma.issue(vbuf[e & 1], Vg, kb * BLK, n);
+    (PK ? dma_v : dma).issue(vbuf[e & 1], Vg, kb * BLK, n);
   };
   // key block of this step, and of the next, read a step ahead
   int kb = cnt > 0 ? kb_of(0) : 0, kb_next = cnt > 1 ? kb_of(1) : 0;
@@ -1472,8 +1681,8 @@ __global__ __launch_bounds__(DQ_NT, 2) void dq_kernel(BwdArgs a) {
       float zp;
       if constexpr (PRECISE) {
         zp = precise_relu_z<D>(i < n, c, s[r], tau, band, tau64,
-                               reinterpret_cast<const float*>(Qg) + (size_t)i * D,
-                               reinterpret_cast<const float*>(Kg) + (size_t)(j0 + crow(r)) * D, a.c64);
+                               reinterpret_cast<const float*>(Qg) + (size_t)i * ldq,
+                               reinterpret_cast<const float*>(Kg) + (size_t)(j0 + crow(r)) * ldk, a.c64);
       } else {
         zp = relu_z(c, s[r], tau);
       }
@@ -1507,6 +1716,20 @@ __global__ __launch_bounds__(DQ_NT, 2) void dq_kernel(BwdArgs a) {
   }
   __syncthreads();
   if (kh == 1 || !wave_ok) return;
+  if constexpr (PK) {
+    E* const dQ = reinterpret_cast<E*>(a.dq) + ((int64_t)at.start * a.pk.heads + bh) * D;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int ir = q0 + crow(r);
+      if (ir < n) {
+#pragma unroll
+        for (int nt = 0; nt < NTD; ++nt)
+          dQ[(int64_t)ir * a.pk.heads * D + 32 * nt + (lane & 31)] =
+              (E)(a.scale * (dq[nt][r] + xch[((qh * NTD + nt) * 16 + r) * 64 + lane]));
+      }
+    }
+    return;
+  }
   float* dQ = a.dq + head;
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
@@ -1520,6 +1743,37 @@ __global__ __launch_bounds__(DQ_NT, 2) void dq_kernel(BwdArgs a) {
   }
 }
 
+// dK and dV as the sums of the `parts` partial ones, in the inputs' type; rows
+// of no sequence are set to 0 or left alone.
+template <typename E, int D>
+__global__ __launch_bounds__(256) void reduce_parts_kernel(Packed<BwdArgs> a) {
+  const int64_t values = (int64_t)a.pk.tokens * a.pk.kv_heads * D;
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (at >= 2 * values) return;
+  const bool second = at >= values;
+  const int64_t x = second ? at - values : at;
+  const int token = (int)(x / (a.pk.kv_heads * D));
+  const bool mine = token >= a.pk.header->begin && token < a.pk.header->end;
+  if (!mine && !a.pk.zero_rest) return;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  const float* part = (second ? a.pk.dv_part : a.pk.dk_part) + x;
+  if (mine)
+    for (int p = 0; p < a.pk.parts; ++p) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(part + p * values);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += v[e];
+    }
+  E* out = reinterpret_cast<E*>(second ? a.dv : a.dk) + x;
+  if constexpr (sizeof(E) == 2) {
+    bf16x4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = (__bf16)sum[e];
+    *reinterpret_cast<bf16x4*>(out) = o;
+  } else {
+    *reinterpret_cast<f32x4*>(out) = sum;
+  }
+}
+
 template <typename E, int D>
 hipError_t launch_dkdv_d(const BwdArgs& a, hipStream_t s) {
   // d = 128 bf16 takes the column-split kernel; at d = 64 (and for fp32)
@@ -1527,28 +1781,76 @@ hipError_t launch_dkdv_d(const BwdArgs& a, hipStream_t s) {
   // of two query-block lists, and is faster on sparse masks.
   if constexpr (sizeof(E) == 2 && D == 128) {
     dim3 grid((unsigned)(a.BH * ((a.T + 1) / 2))), block(BWD2_NT);
-    auto kernel = dkdv2_kernel<D, 0>;
-    if (a.gk == 1) kernel = dkdv2_kernel<D, 1>;
-    if (a.gk == 2) kernel = dkdv2_kernel<D, 2>;
-    if (a.gk == 4) kernel = dkdv2_kernel<D, 4>;
+    auto kernel = dkdv2_kernel<D, 0, BwdArgs>;
+    if (a.gk == 1) kernel = dkdv2_kernel<D, 1, BwdArgs>;
+    if (a.gk == 2) kernel = dkdv2_kernel<D, 2, BwdArgs>;
+    if (a.gk == 4) kernel = dkdv2_kernel<D, 4, BwdArgs>;
     return launch_kernel(kernel, grid, block, s, a);
   }
   dim3 grid((unsigned)(a.BH * a.T)), block(BWD_NT);
-  auto kernel = dkdv_kernel<E, D, 0>;
-  if (a.gk == 1) kernel = dkdv_kernel<E, D, 1>;
-  if (a.gk == 2) kernel = dkdv_kernel<E, D, 2>;
-  if (a.gk == 4) kernel = dkdv_kernel<E, D, 4>;
+  auto kernel = dkdv_kernel<E, D, 0, BwdArgs>;
+  if (a.gk == 1) kernel = dkdv_kernel<E, D, 1, BwdArgs>;
+  if (a.gk == 2) kernel = dkdv_kernel<E, D, 2, BwdArgs>;
+  if (a.gk == 4) kernel = dkdv_kernel<E, D, 4, BwdArgs>;
   return launch_kernel(kernel, grid, block, s, a);
 }
 
 template <typename E, int D>
 hipError_t launch_dq_d(const BwdArgs& a, hipStream_t s) {
   dim3 grid((unsigned)(a.BH * a.T)), block(DQ_NT);
-  auto kernel = dq_kernel<E, D, 0>;
-  if (a.gk == 1) kernel = dq_kernel<E, D, 1>;
-  if (a.gk == 2) kernel = dq_kernel<E, D, 2>;
-  if (a.gk == 4) kernel = dq_kernel<E, D, 4>;
+  auto kernel = dq_kernel<E, D, 0, BwdArgs>;
+  if (a.gk == 1) kernel = dq_kernel<E, D, 1, BwdArgs>;
+  if (a.gk == 2) kernel = dq_kernel<E, D, 2, BwdArgs>;
+  if (a.gk == 4) kernel = dq_kernel<E, D, 4, BwdArgs>;
   return launch_kernel(kernel, grid, block, s, a);
+}
+
+// The packed forms: `tiles` workgroups per key head and part, or query head.
+template <typename E, int D>
+constexpr bool split_columns() { return sizeof(E) == 2 && D == 128; }
+
+template <typename E, int D>
+hipError_t launch_dkdv_packed_d(Packed<BwdArgs> a, hipStream_t s) {
+  using A = Packed<BwdArgs>;
+  constexpr int size = split_columns<E, D>() ? 1 : 0;
+  a.pk.size = size;
+  a.pk.tiles = a.pk.lists[size];
+  const dim3 grid((unsigned)(a.pk.kv_heads * a.pk.parts * packed_tiles(a.pk.tokens, a.pk.seq_count, size)));
+  hipError_t e;
+  if constexpr (split_columns<E, D>()) {
+    auto kernel = dkdv2_kernel<D, 0, A>;
+    if (a.gk == 1) kernel = dkdv2_kernel<D, 1, A>;
+    if (a.gk == 2) kernel = dkdv2_kernel<D, 2, A>;
+    if (a.gk == 4) kernel = dkdv2_kernel<D, 4, A>;
+    e = launch_kernel(kernel, grid, dim3(BWD2_NT), s, a);
+  } else {
+    auto kernel = dkdv_kernel<E, D, 0, A>;
+    if (a.gk == 1) kernel = dkdv_kernel<E, D, 1, A>;
+    if (a.gk == 2) kernel = dkdv_kernel<E, D, 2, A>;
+    if (a.gk == 4) kernel = dkdv_kernel<E, D, 4, A>;
+    e = launch_kernel(kernel, grid, dim3(BWD_NT), s, a);
+  }
+  if (e != hipSuccess || a.pk.parts == 1) return e;
+  const int64_t quads = (int64_t)a.pk.tokens * a.pk.kv_heads * D / 2;
+  return launch_kernel(reduce_parts_kernel<E, D>, dim3((unsigned)((quads + 255) / 256)), dim3(256), s, a);
+}
+
+template <typename E, int D>
+hipError_t launch_dq_packed_d(Packed<BwdArgs> a, hipStream_t s) {
+  using A = Packed<BwdArgs>;
+  a.pk.size = 0;
+  a.pk.tiles = a.pk.lists[0];
+  const dim3 grid((unsigned)(a.pk.heads * packed_tiles(a.pk.tokens, a.pk.seq_count, 0)));
+  auto kernel = dq_kernel<E, D, 0, A>;
+  if (a.gk == 1) kernel = dq_kernel<E, D, 1, A>;
+  if (a.gk == 2) kernel = dq_kernel<E, D, 2, A>;
+  if (a.gk == 4) kernel = dq_kernel<E, D, 4, A>;
+  return launch_kernel(kernel, grid, dim3(DQ_NT), s, a);
+}
+
+template <typename E, int D>
+hipError_t launch_delta_packed_d(const Packed<DeltaArgs>& a, hipStream_t s) {
+  return launch_kernel(delta_packed_kernel<E, D>, dim3((unsigned)((a.rows + 15) / 16)), dim3(256), s, a);
 }
 
 template <typename E, int D>
@@ -1607,6 +1909,39 @@ hipError_t launch_bwd_dkdv_lists(const BwdArgs& a, int dtype, int head_dim, hipS
 hipError_t launch_bwd_dq(const BwdArgs& a, int dtype, int head_dim, hipStream_t s) {
   if (dtype == 0) return head_dim == 64 ? launch_dq_d<__bf16, 64>(a, s) : launch_dq_d<__bf16, 128>(a, s);
   return head_dim == 64 ? launch_dq_d<float, 64>(a, s) : launch_dq_d<float, 128>(a, s);
+}
+
+hipError_t launch_delta_packed(const Packed<DeltaArgs>& a, int dtype, int head_dim, hipStream_t s) {
+  if (dtype == 0)
+    return head_dim == 64 ? launch_delta_packed_d<__bf16, 64>(a, s) : launch_delta_packed_d<__bf16, 128>(a, s);
+  return head_dim == 64 ? launch_delta_packed_d<float, 64>(a, s) : launch_delta_packed_d<float, 128>(a, s);
+}
+
+hipError_t launch_bwd_dkdv_packed(const Packed<BwdArgs>& a, int dtype, int head_dim, hipStream_t s) {
+  if (dtype == 0)
+    return head_dim == 64 ? launch_dkdv_packed_d<__bf16, 64>(a, s) : launch_dkdv_packed_d<__bf16, 128>(a, s);
+  return head_dim == 64 ? launch_dkdv_packed_d<float, 64>(a, s) : launch_dkdv_packed_d<float, 128>(a, s);
+}
+
+hipError_t launch_bwd_dq_packed(const Packed<BwdArgs>& a, int dtype, int head_dim, hipStream_t s) {
+  if (dtype == 0)
+    return head_dim == 64 ? launch_dq_packed_d<__bf16, 64>(a, s) : launch_dq_packed_d<__bf16, 128>(a, s);
+  return head_dim == 64 ? launch_dq_packed_d<float, 64>(a, s) : launch_dq_packed_d<float, 128>(a, s);
+}
+
+// A workgroup that adds up all query heads of a key head writes dK and dV
+// once; grids that would leave compute units idle are split into `parts`
+// workgroups per key head (a divisor of the heads of a group), whose sums go
+// through memory.  Two workgroups of the column-split form (one runs on a
+// compute unit) or eight of the other (four) per compute unit of 256 are
+// enough.
+int dkdv_packed_parts(int tokens, int seqs, int heads, int kv_heads, int dtype, int head_dim) {
+  const bool split = dtype == 0 && head_dim == 128;
+  const int64_t tiles = (int64_t)packed_tiles(tokens, seqs, split ? 1 : 0) * kv_heads;
+  const int group = heads / kv_heads;
+  for (int parts = 1; parts < group; ++parts)
+    if (group % parts == 0 && tiles * parts >= (split ? 512 : 2048)) return parts;
+  return group;
 }
 
 }  // namespace ea

@@ -170,18 +170,18 @@ __device__ __forceinline__ int perm_key(int t, int e) {
 
 // Row fragment for k step kk of row `row` of a [*, D] row-major global
 // matrix: bf16 -> 8 values at k = 16kk + 8h; fp32 -> 1 value at k = 2kk + h.
-// Rows outside [0, nrows) read as zero.
+// Rows outside [0, nrows) read as zero.  `ld`: elements from row to row.
 template <typename E, int D>
 __device__ __forceinline__ typename Mma<E>::frag load_row_frag_global(const E* base, int row,
-                                                                      int nrows, int kk) {
+                                                                      int nrows, int kk, int ld = D) {
   const int h = lane_id() >> 5;
   if constexpr (Mma<E>::EPL == 8) {
     u32x4 v = {0u, 0u, 0u, 0u};
-    if (row < nrows) v = *reinterpret_cast<const u32x4*>(base + (size_t)row * D + 16 * kk + 8 * h);
+    if (row < nrows) v = *reinterpret_cast<const u32x4*>(base + (size_t)row * ld + 16 * kk + 8 * h);
     return __builtin_bit_cast(bf16x8, v);
   } else {
     float v = 0.f;
-    if (row < nrows) v = base[(size_t)row * D + 2 * kk + h];
+    if (row < nrows) v = base[(size_t)row * ld + 2 * kk + h];
     return v;
   }
 }
@@ -207,6 +207,8 @@ struct Tile {
   static constexpr int VEC = 16 / (int)sizeof(E);  // elements per 16-byte chunk
   static constexpr int CPR = D / VEC;              // chunks per row
   static constexpr int CHUNKS = BLK * CPR;
+  // whether rows `step` apart have the same chunk pattern (see swz)
+  static constexpr bool same_pattern(int step) { return CPR <= 16 && step % 16 == 0; }
   static constexpr int ELEMS = BLK * D;
   // Chunk XOR pattern of tile row r, a bijection on the rows of each
   // 16-row group (32 lanes reading one chunk column hit distinct banks);
@@ -229,11 +231,12 @@ struct Tile {
   __device__ __forceinline__ static int elem(int r, int col) {
     return chunk_pos(r, col / VEC) * VEC + (col & (VEC - 1));
   }
-  // global element offset (within the 64-row block) of the chunk stored at
-  // chunk position p
-  __device__ __forceinline__ static int src_off(int p) {
+  // tile row of the chunk stored at chunk position p, and its global element
+  // offset (within the 64-row block, rows `ld` elements apart)
+  __device__ __forceinline__ static int src_row(int p) { return p / CPR; }
+  __device__ __forceinline__ static int src_off(int p, int ld = D) {
     const int r = p / CPR;
-    return r * D + ((p % CPR) ^ swz(r)) * VEC;
+    return r * ld + ((p % CPR) ^ swz(r)) * VEC;
   }
 };
 
@@ -249,15 +252,17 @@ struct PadTile {
   static constexpr int VEC = 16 / (int)sizeof(E);
   static constexpr int CPR = D / VEC;
   static constexpr int RS = CPR + 1;  // row stride in chunks
+  static constexpr bool same_pattern(int) { return false; }
   static constexpr int CHUNKS = BLK * RS;
   static constexpr int ELEMS = CHUNKS * VEC;
   __device__ __forceinline__ static int chunk_pos(int r, int c) { return r * RS + c; }
   __device__ __forceinline__ static int elem(int r, int col) {
     return chunk_pos(r, col / VEC) * VEC + (col & (VEC - 1));
   }
-  __device__ __forceinline__ static int src_off(int p) {
+  __device__ __forceinline__ static int src_row(int p) { return p / RS; }
+  __device__ __forceinline__ static int src_off(int p, int ld = D) {
     const int r = p / RS, c = p % RS;
-    return r * D + (c == CPR ? 0 : c) * VEC;
+    return r * ld + (c == CPR ? 0 : c) * VEC;
   }
 };
 
@@ -274,30 +279,40 @@ __device__ __forceinline__ lds_void_t* to_lds(const void* p) {
 // wave instruction k (k = i * NW + wave) fills chunk positions
 // [64k, 64k + 64).  The element offset of every chunk this lane fetches is
 // computed once (init); a copy is then one uniform base plus those offsets,
-// with the row clamp only on the last, partial tile.
-template <typename TL, int D, int NT>
+// with the row clamp only on the last, partial tile.  STRIDED: rows `ld`
+// elements apart instead of D.
+template <typename TL, int D, int NT, bool STRIDED = false>
 struct TileDma {
   static constexpr int NW = NT / 64;
   static constexpr int NI = TL::CHUNKS / 64;        // wave instructions per tile
   static constexpr int PER = (NI + NW - 1) / NW;    // per wave (the last may be idle)
   static_assert(TL::CHUNKS % 64 == 0, "tile chunks must fill whole wave instructions");
-  int off[PER];
+  // Strided rows: a wave's instructions are STEP rows apart, so that where the
+  // chunk pattern repeats after as many, one offset serves them all (and eight
+  // registers less in kernels that copy two operands).
+  static constexpr int STEP = 64 * NW / TL::CPR;
+  static constexpr bool ONE = STRIDED && TL::same_pattern(STEP) && NI % NW == 0;
+  int off[ONE ? 1 : PER];
+  int ld;
 
-  __device__ __forceinline__ void init() {
+  __device__ __forceinline__ void init(int row_stride = D) {
+    ld = STRIDED ? row_stride : D;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) off[i] = TL::src_off(64 * min(i * NW + wave_id(), NI - 1) + lane_id());
+    for (int i = 0; i < (ONE ? 1 : PER); ++i)
+      off[i] = TL::src_off(64 * min(i * NW + wave_id(), NI - 1) + lane_id(), STRIDED ? ld : D);
   }
 
   template <typename E>
   __device__ __forceinline__ void issue(E* tile, const E* g, int row0, int nrows) const {
 #if defined(__HIP_DEVICE_COMPILE__)  // gfx950 builtin; kernels' lambdas are also parsed for the host
-    const E* base = g + (size_t)row0 * D;
+    const E* base = g + (size_t)row0 * (STRIDED ? ld : D);
     if (row0 + BLK <= nrows) {
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int k = i * NW + wave_id();
         if (NI % NW != 0 && k >= NI) break;
-        __builtin_amdgcn_global_load_lds(base + off[i], to_lds(tile + 64 * k * TL::VEC), 16, 0, 0);
+        const E* from = ONE ? base + (size_t)(i * STEP) * ld : base;
+        __builtin_amdgcn_global_load_lds(from + off[ONE ? 0 : i], to_lds(tile + 64 * k * TL::VEC), 16, 0, 0);
       }
     } else {
       const int last = nrows - 1 - row0;  // rows past the end repeat the last row
@@ -305,8 +320,8 @@ struct TileDma {
       for (int i = 0; i < PER; ++i) {
         const int k = i * NW + wave_id();
         if (NI % NW != 0 && k >= NI) break;
-        const int r = off[i] / D;
-        const int o = off[i] + (min(r, last) - r) * D;
+        const int r = STRIDED ? TL::src_row(64 * k + lane_id()) : off[ONE ? 0 : i] / D;
+        const int o = (ONE ? off[0] + i * STEP * ld : off[i]) + (min(r, last) - r) * (STRIDED ? ld : D);
         __builtin_amdgcn_global_load_lds(base + o, to_lds(tile + 64 * k * TL::VEC), 16, 0, 0);
       }
     }
@@ -314,8 +329,8 @@ struct TileDma {
   }
 };
 
-template <typename E, int D, int NT>
-using DmaPlan = TileDma<Tile<E, D>, D, NT>;
+template <typename E, int D, int NT, bool STRIDED = false>
+using DmaPlan = TileDma<Tile<E, D>, D, NT, STRIDED>;
 
 // Waits for this wave's outstanding global loads, global_load_lds included
 // (s_waitcnt vmcnt(0)); follow with a barrier before reading the tiles.

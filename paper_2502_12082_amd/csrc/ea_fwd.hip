@@ -34,6 +34,7 @@
 
 #include "ea_common.h"
 #include "ea_internal.h"
+#include "ea_packed.h"
 
 namespace ea {
 
@@ -41,22 +42,22 @@ namespace {
 
 // --------------------------------------------------------------- tables
 
-// K_j of key block `col` (= bh * T + j), one wave: a ballot and a prefix
-// count per 64 query blocks of the mask's column j.
-__device__ void column_table(const FwdArgs& a, int col) {
-  const int lane = lane_id(), T = a.T;
-  const int bh = col / T, j = col % T;
-  const uint8_t* M = a.mask + (size_t)bh * T * T;
-  int32_t* const out = a.k_index + (size_t)col * T;
+// K_j of key block j of the head whose first block is blk0, with tables of
+// `width` entries a row, one wave: a ballot and a prefix count per 64 query
+// blocks of the mask's column j.
+__device__ void column_table(const FwdArgs& a, size_t blk0, int j, int T, int width) {
+  const int lane = lane_id();
+  const uint8_t* M = a.mask + blk0 * width;
+  int32_t* const out = a.k_index + (blk0 + j) * width;
   int listed = 0;
   for (int i0 = 0; i0 < T; i0 += 64) {
     const int i = i0 + lane;
-    const bool b = i < T && M[(size_t)i * T + j] != 0;
+    const bool b = i < T && M[(size_t)i * width + j] != 0;
     const unsigned long long m = __ballot(b);
     if (b) out[listed + __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u))] = i;
     listed += __popcll(m);
   }
-  if (lane == 0) a.k_count[col] = listed;
+  if (lane == 0) a.k_count[blk0 + j] = listed;
 }
 
 // ------------------------------------------------- listed query blocks
@@ -157,13 +158,30 @@ constexpr int FWD_COLS_PER_WG = FWD_NT / 64;  // column tables per extra workgro
 //
 // The bf16 d = 64 inference instances fit 128 registers, so four waves share
 // each SIMD instead of three (B8 H12 n1024: 0.049 against 0.052 ms).
-template <typename E, int D, int GK, bool TRAIN>
-__global__ __launch_bounds__(FWD_NT, !TRAIN && D == 64 && sizeof(E) == 2 ? 4 : 2) void fwd_kernel(FwdArgs a) {
-  const int nqb = a.BH * a.T;
-  if ((int)blockIdx.x >= nqb) {
-    const int col = ((int)blockIdx.x - nqb) * FWD_COLS_PER_WG + wave_id();
-    if (col < nqb) column_table(a, col);
-    return;
+//
+// A = Packed<FwdArgs>: packed sequences with grouped heads.
+template <typename E, int D, int GK, bool TRAIN, typename A>
+__global__ __launch_bounds__(FWD_NT, !TRAIN && D == 64 && sizeof(E) == 2 ? 4 : 2) void fwd_kernel(A a) {
+  constexpr bool PK = is_packed<A>::value;
+  [[maybe_unused]] Place at;
+  if constexpr (PK) {
+    const int nqb = a.pk.heads * packed_tiles(a.pk.tokens, a.pk.seq_count, 0);
+    if ((int)blockIdx.x >= nqb) {  // (the key blocks are listed as the query blocks are)
+      const int col = ((int)blockIdx.x - nqb) * FWD_COLS_PER_WG + wave_id();
+      if (col < nqb && packed_place(a.pk, col, a.pk.heads, false, at))
+        column_table(a, at.blk0, at.tile, at.T, a.pk.width);
+      return;
+    }
+    const bool work = packed_place(a.pk, blockIdx.x, a.pk.heads, false, at);
+    if (at.item == 0 && a.pk.zero_rest) zero_rest<E, D, FWD_NT>(a.pk, static_cast<E*>(a.o), a.pk.o, at.head);
+    if (!work) return;
+  } else {
+    const int nqb = a.BH * a.T;
+    if ((int)blockIdx.x >= nqb) {
+      const int col = ((int)blockIdx.x - nqb) * FWD_COLS_PER_WG + wave_id();
+      if (col < nqb) column_table(a, (size_t)(col / a.T) * a.T, col % a.T, a.T, a.T);
+      return;
+    }
   }
   using TL = Tile<E, D>;
   using M = Mma<E>;
@@ -177,34 +195,57 @@ __global__ __launch_bounds__(FWD_NT, !TRAIN && D == 64 && sizeof(E) == 2 ? 4 : 2
 
   const int lane = lane_id(), w = wave_id();
   const int qh = w & 1, kh = w >> 1;
-  const int n = a.n, T = a.T;
-  int bh = blockIdx.x % a.BH;
-  int qb = blockIdx.x / a.BH;
-  if (a.lists) head_major(blockIdx.x, a.BH, T, bh, qb, head_group<E, D>(n, 1));
-  if (a.causal) qb = T - 1 - qb;  // longest lists first
-  if (a.lists && (((const ci32*)a.use)[(size_t)bh * T + qb] & LIST_FWD)) {
-    gather_fwd<E, D, GK, TRAIN>(a, a.lists[(size_t)bh * T + qb], bh, qb);
-    return;
+  const int n = PK ? at.n : a.n, T = PK ? at.T : a.T;
+  int bh = PK ? at.head : blockIdx.x % a.BH;
+  int qb = PK ? at.tile : blockIdx.x / a.BH;
+  if constexpr (!PK) {
+    if (a.lists) head_major(blockIdx.x, a.BH, T, bh, qb, head_group<E, D>(n, 1));
+    if (a.causal) qb = T - 1 - qb;  // longest lists first
+    if (a.lists && (((const ci32*)a.use)[(size_t)bh * T + qb] & LIST_FWD)) {
+      gather_fwd<E, D, GK, TRAIN>(a, a.lists[(size_t)bh * T + qb], bh, qb);
+      return;
+    }
   }
+  const size_t row0 = PK ? at.row0 : (size_t)bh * n;
+  const size_t blk = (PK ? at.blk0 : (size_t)bh * T) + qb;
+  int width = T, ldq = D, ldk = D, ldv = D, ldo = D;
   const int q0 = qb * BLK + 32 * qh;
   const int i = q0 + (lane & 31);
   const bool wave_ok = q0 < n;
   const int wave_last = min(n - 1, q0 + 31);
-  const size_t head = (size_t)bh * n * D;
-  const E* Q = static_cast<const E*>(a.q) + head;
-  const E* K = static_cast<const E*>(a.k) + head;
-  const E* V = static_cast<const E*>(a.v) + head;
-  const float tau = i < n ? a.tau[(size_t)bh * n + i] : 0.f;
+  const size_t head = row0 * D;
+  const E* Q = static_cast<const E*>(a.q);
+  const E* K = static_cast<const E*>(a.k);
+  const E* V = static_cast<const E*>(a.v);
+  E* O = static_cast<E*>(a.o);
+  if constexpr (PK) {
+    width = a.pk.width;
+    ldq = a.pk.q.row;
+    ldk = a.pk.k.row;
+    ldv = a.pk.v.row;
+    ldo = a.pk.o.row;
+    const int kv = bh / a.pk.group;
+    Q += (int64_t)at.start * ldq + bh * a.pk.q.head;
+    K += (int64_t)at.start * ldk + kv * a.pk.k.head;
+    V += (int64_t)at.start * ldv + kv * a.pk.v.head;
+    O += (int64_t)at.start * ldo + bh * a.pk.o.head;
+  } else {
+    Q += head;
+    K += head;
+    V += head;
+    O += head;
+  }
+  const float tau = i < n ? a.tau[row0 + i] : 0.f;
   const float c = a.c, g = a.gamma;
   constexpr bool PRECISE = precise_path<E, GK>();
   // fp32 inputs, general alpha: fp64 z near the support edge (ea_common.h)
   [[maybe_unused]] const double tau64 =
-      (double)tau + (PRECISE && a.tau_lo && i < n ? (double)a.tau_lo[(size_t)bh * n + i] : 0.0);
+      (double)tau + (PRECISE && a.tau_lo && i < n ? (double)a.tau_lo[row0 + i] : 0.0);
   [[maybe_unused]] const float band = PRECISE_BAND * fmaxf(1.f, fabsf(tau));
 
   typename M::frag qf[KS];
 #pragma unroll
-  for (int kk = 0; kk < KS; ++kk) qf[kk] = load_row_frag_global<E, D>(Q, i, n, kk);
+  for (int kk = 0; kk < KS; ++kk) qf[kk] = load_row_frag_global<E, D>(Q, i, n, kk, ldq);
 
   // A wave raises its issue priority over its MFMA chains, so that the two
   // waves of a SIMD drift apart (one in its MFMAs while the other maps
@@ -223,8 +264,8 @@ __global__ __launch_bounds__(FWD_NT, !TRAIN && D == 64 && sizeof(E) == 2 ? 4 : 2
 
   // Without tables (the no-mask mode) every valid key block is visited.
   const bool dense = a.q_index == nullptr;
-  const ci32* list = (const ci32*)(dense ? nullptr : a.q_index + ((size_t)bh * T + qb) * T);
-  const int cnt = dense ? (a.causal ? qb + 1 : T) : ((const ci32*)a.q_count)[(size_t)bh * T + qb];
+  const ci32* list = (const ci32*)(dense ? nullptr : a.q_index + blk * width);
+  const int cnt = dense ? (a.causal ? qb + 1 : T) : ((const ci32*)a.q_count)[blk];
   auto kb_of = [&](int e) { return dense ? e : list[e]; };
 
   f32x16 o[NTD], o2[NTD];
@@ -242,11 +283,12 @@ __global__ __launch_bounds__(FWD_NT, !TRAIN && D == 64 && sizeof(E) == 2 ? 4 : 2
     return 1;
   };
 
-  DmaPlan<E, D, FWD_NT> dma;
-  dma.init();
+  DmaPlan<E, D, FWD_NT, PK> dma, dma_v;
+  dma.init(ldk);
+  if constexpr (PK) dma_v.init(ldv);
   auto issue = [&](int kb, int e) {
     dma.issue(kbuf[e & 1], K, kb * BLK, n);
-    dma.issue(vbuf[e & 1], V, kb * BLK, n);
+    (PK ? dma_v : dma).issue(vbuf[e & 1], V, kb * BLK, n);
   };
   // key block of this step, and of the next, read a step ahead
   int kb = cnt > 0 ? kb_of(0) : 0, kb_next = cnt > 1 ? kb_of(1) : 0;
@@ -318,8 +360,8 @@ __global__ __launch_bounds__(FWD_NT, !TRAIN && D == 64 && sizeof(E) == 2 ? 4 : 2
       float zp;
       if constexpr (PRECISE) {
         zp = precise_relu_z<D>(i < n, c, s[r], tau, band, tau64,
-                               reinterpret_cast<const float*>(Q) + (size_t)i * D,
-                               reinterpret_cast<const float*>(K) + (size_t)(j0 + crow(r)) * D, a.c64);
+                               reinterpret_cast<const float*>(Q) + (size_t)i * ldq,
+                               reinterpret_cast<const float*>(K) + (size_t)(j0 + crow(r)) * ldk, a.c64);
       } else {
         zp = relu_z(c, s[r], tau);
       }
@@ -389,7 +431,6 @@ __global__ __launch_bounds__(FWD_NT, !TRAIN && D == 64 && sizeof(E) == 2 ? 4 : 2
   }
   if (kh == 1 || !wave_ok) return;
 
-  E* O = static_cast<E*>(a.o) + head;
   float* O2 = a.o2 + head;
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
@@ -401,7 +442,7 @@ __global__ __launch_bounds__(FWD_NT, !TRAIN && D == 64 && sizeof(E) == 2 ? 4 : 2
 #pragma unroll
       for (int nt = 0; nt < NTD; ++nt) {
         const size_t off = (size_t)ir * D + 32 * nt + (lane & 31);
-        O[off] = (E)o[nt][r];
+        O[(size_t)ir * ldo + 32 * nt + (lane & 31)] = (E)o[nt][r];
         if constexpr (TRAIN) O2[off] = us > 0.f ? o2[nt][r] / us : 0.f;
       }
     }
@@ -415,10 +456,10 @@ hipError_t launch_fwd_dt(const FwdArgs& a, hipStream_t s) {
   const int nqb = a.BH * a.T;
   const int ncol = TRAIN && a.k_index ? (nqb + FWD_COLS_PER_WG - 1) / FWD_COLS_PER_WG : 0;
   dim3 grid((unsigned)(nqb + ncol)), block(FWD_NT);
-  auto kernel = fwd_kernel<E, D, 0, TRAIN>;
-  if (a.gk == 1) kernel = fwd_kernel<E, D, 1, TRAIN>;
-  if (a.gk == 2) kernel = fwd_kernel<E, D, 2, TRAIN>;
-  if (a.gk == 4) kernel = fwd_kernel<E, D, 4, TRAIN>;
+  auto kernel = fwd_kernel<E, D, 0, TRAIN, FwdArgs>;
+  if (a.gk == 1) kernel = fwd_kernel<E, D, 1, TRAIN, FwdArgs>;
+  if (a.gk == 2) kernel = fwd_kernel<E, D, 2, TRAIN, FwdArgs>;
+  if (a.gk == 4) kernel = fwd_kernel<E, D, 4, TRAIN, FwdArgs>;
   return launch_kernel(kernel, grid, block, s, a);
 }
 
@@ -427,7 +468,32 @@ hipError_t launch_fwd_d(const FwdArgs& a, bool train, hipStream_t s) {
   return train ? launch_fwd_dt<E, D, true>(a, s) : launch_fwd_dt<E, D, false>(a, s);
 }
 
+template <typename E, int D, bool TRAIN>
+hipError_t launch_fwd_packed_dt(Packed<FwdArgs> a, hipStream_t s) {
+  using A = Packed<FwdArgs>;
+  a.pk.size = 0;
+  a.pk.tiles = a.pk.lists[0];
+  const int nqb = a.pk.heads * packed_tiles(a.pk.tokens, a.pk.seq_count, 0);
+  const int ncol = TRAIN ? (nqb + FWD_COLS_PER_WG - 1) / FWD_COLS_PER_WG : 0;
+  auto kernel = fwd_kernel<E, D, 0, TRAIN, A>;
+  if (a.gk == 1) kernel = fwd_kernel<E, D, 1, TRAIN, A>;
+  if (a.gk == 2) kernel = fwd_kernel<E, D, 2, TRAIN, A>;
+  if (a.gk == 4) kernel = fwd_kernel<E, D, 4, TRAIN, A>;
+  return launch_kernel(kernel, dim3((unsigned)(nqb + ncol)), dim3(FWD_NT), s, a);
+}
+
+template <typename E, int D>
+hipError_t launch_fwd_packed_d(const Packed<FwdArgs>& a, bool train, hipStream_t s) {
+  return train ? launch_fwd_packed_dt<E, D, true>(a, s) : launch_fwd_packed_dt<E, D, false>(a, s);
+}
+
 }  // namespace
+
+hipError_t launch_fwd_packed(const Packed<FwdArgs>& a, int dtype, int head_dim, bool train, hipStream_t s) {
+  if (dtype == 0)
+    return head_dim == 64 ? launch_fwd_packed_d<__bf16, 64>(a, train, s) : launch_fwd_packed_d<__bf16, 128>(a, train, s);
+  return head_dim == 64 ? launch_fwd_packed_d<float, 64>(a, train, s) : launch_fwd_packed_d<float, 128>(a, train, s);
+}
 
 hipError_t launch_fwd(const FwdArgs& a, int dtype, int head_dim, bool train, hipStream_t s) {
   if (dtype == 0)

@@ -94,6 +94,103 @@ __host__ __device__ inline int list_use(int entries, int blocks, int T, bool f32
 }
 #endif
 
+// Packed sequences: rows [start, start + len) of [tokens, heads, D] tensors,
+// `group` query heads to a key head.  The sequences' tiles of 64, 128 and 256
+// rows are listed by plan_kernel (ea_packed.hip), those with the most keys
+// first; a launch takes one workgroup per head and possible tile (the host
+// does not know their number), and those beyond the list return.  Tables and
+// statistics are per query head: tau of head h and token t at h tokens + t,
+// tables of its query block b (counted over all sequences) at h blocks + b,
+// with rows of `width` entries.
+struct Strides {
+  int row;       // elements from token to token
+  int64_t head;  // and from head to head
+};
+struct PackedSeq {
+  int32_t start, len, block, unused;  // block: its first query block
+};
+struct PackedTile {
+  int32_t seq, tile;
+};
+struct PackedHeader {
+  int32_t count[3];    // tiles of 64, 128 and 256 rows
+  int32_t begin, end;  // the rows that belong to sequences
+  int32_t unused[3];
+};
+struct PackedArgs {
+  const PackedHeader* header;
+  const PackedSeq* seqs;
+  const PackedTile* lists[3];  // of 64, 128 and 256 rows
+  const PackedTile* tiles;     // those of this launch, 64 << size rows
+  int size, seq_count;
+  int heads, kv_heads, group, tokens, blocks, width;
+  Strides q, k, v, o;  // (o: also of its gradient)
+  int zero_rest;       // whether the rows of no sequence are set to 0 in what is written
+  int parts;           // dK/dV: workgroups that share the query heads of a key head
+  float *dk_part, *dv_part;  // parts > 1: [parts, tokens, kv_heads, D] sums to add up
+};
+// The arguments of a kernel's packed form.
+template <typename A>
+struct Packed : A {
+  PackedArgs pk;
+};
+
+// The most tiles of 64 << size rows that `seqs` sequences of `tokens` rows in
+// all can have.
+constexpr int packed_tiles(int tokens, int seqs, int size) { return tokens / (64 << size) + seqs; }
+
+struct PlanArgs {
+  const int32_t* cu;  // [seqs + 1]
+  PackedHeader* header;
+  PackedSeq* seqs;
+  PackedTile* tiles[3];  // packed_tiles() of each size
+  int seq_count, tokens, max_seqlen, causal;
+};
+
+// Rows of D values, one per head of a token.
+struct RotaryRows {
+  void* p;
+  int64_t row, head;
+};
+constexpr int ROT_MAX_PARTIALS = 1024;  // workgroups of the backward
+constexpr int ROT_MAX_AXES = 4;
+struct RotaryArgs {
+  RotaryRows q, k, q_out, k_out;  // (the backward's outputs are the gradients of q and k)
+  RotaryRows dq, dk;              // gradients of the forward's outputs
+  const int32_t* positions;       // [axes, tokens], rows `position_stride` apart
+  int64_t position_stride;
+  const float* freqs;             // [rot / 2] radians per position
+  int axis_end[ROT_MAX_AXES];     // first pair behind each axis
+  int axes, tokens, hq, hk, d, rot, interleaved;
+  float eps;
+  const void *q_weight, *k_weight;  // or null: 1
+  int weight_f32;                   // else the type of q
+  float* partials;                  // [partial_count, 2, d]
+  int partial_count;
+  float *dq_weight, *dk_weight;     // or null
+  int parts;                        // waves per token (forward)
+};
+
+// One query per request against a shared prefix and the request's own cache.
+// Key blocks are of 32 keys, `run` of them to a run (one wave's unit of work).
+constexpr int DEC_KEYS = 32, DEC_RUN = 4;
+struct DecodeArgs {
+  const void *q, *k, *v, *pk, *pv;  // own caches, and the prefix
+  void* o;
+  int64_t q_row, q_head, o_row, o_head;         // request to request, head to head
+  int64_t k_batch, k_row, k_head, v_batch, v_row, v_head;
+  int64_t pk_row, pk_head, pv_row, pv_head;
+  const int32_t* lengths;  // [requests], clamped to 0 .. capacity
+  int requests, heads, kv_heads, group, prefix, capacity;
+  int prefix_runs, own_runs;  // per key head, and per request and key head
+  // workspace: raw scores [kv_heads, prefix blocks, requests * group, 32] and
+  // [requests, kv_heads, own blocks, group, 32], and their maxima
+  // [kv_heads, requests * group, prefix blocks], [requests, kv_heads, group, own blocks]
+  float *ps, *os, *pm, *om;
+  float c, alpha, gamma, tol;
+  int max_iter, gk;
+};
+
 struct TauArgs {
   const void* q;
   const void* k;
@@ -252,6 +349,23 @@ hipError_t launch_bwd_dkdv_lists(const BwdArgs& a, int dtype, int head_dim, hipS
 // (a sample of the density, then the lists of heads that look sparse)
 hipError_t launch_collect(const CollectArgs& a, int dtype, int head_dim, hipStream_t s);
 hipError_t launch_bwd_dq(const BwdArgs& a, int dtype, int head_dim, hipStream_t s);
+// The packed forms (no lists; T and n of the arguments are not used).
+hipError_t launch_plan(const PlanArgs& a, hipStream_t s);
+hipError_t launch_tau_packed(const Packed<TauArgs>& a, int dtype, int head_dim, hipStream_t s);
+hipError_t launch_tau_packed_bf16_64(const Packed<TauArgs>& a, hipStream_t s);
+hipError_t launch_tau_packed_bf16_128(const Packed<TauArgs>& a, hipStream_t s);
+hipError_t launch_tau_packed_f32_64(const Packed<TauArgs>& a, hipStream_t s);
+hipError_t launch_tau_packed_f32_128(const Packed<TauArgs>& a, hipStream_t s);
+hipError_t launch_fwd_packed(const Packed<FwdArgs>& a, int dtype, int head_dim, bool train, hipStream_t s);
+hipError_t launch_delta_packed(const Packed<DeltaArgs>& a, int dtype, int head_dim, hipStream_t s);
+hipError_t launch_bwd_dkdv_packed(const Packed<BwdArgs>& a, int dtype, int head_dim, hipStream_t s);
+hipError_t launch_bwd_dq_packed(const Packed<BwdArgs>& a, int dtype, int head_dim, hipStream_t s);
+// Workgroups that share the query heads of a key head in launch_bwd_dkdv_packed.
+int dkdv_packed_parts(int tokens, int seqs, int heads, int kv_heads, int dtype, int head_dim);
+hipError_t launch_decode(const DecodeArgs& a, int dtype, int head_dim, hipStream_t s);
+int rotary_partials(int tokens);
+hipError_t launch_rotary_fwd(const RotaryArgs& a, int dtype, hipStream_t s);
+hipError_t launch_rotary_bwd(const RotaryArgs& a, int dtype, hipStream_t s);
 hipError_t launch_rows_fwd(const RowsArgs& a, int dtype, hipStream_t s);
 hipError_t launch_rows_bwd(const RowsArgs& a, int dtype, hipStream_t s);
 

@@ -26,6 +26,7 @@
 
 #include "ea_common.h"
 #include "ea_internal.h"
+#include "ea_packed.h"
 
 namespace ea {
 
@@ -71,8 +72,11 @@ static_assert(SV_ROWS == 64 * SV_WAVES, "one 64-row query block per wave (G = 2)
 // work, with half the state each, so that more of them share each SIMD.
 // fp32 operands at d = 128 (128 registers of query fragments) run one wave
 // per SIMD with G = 2.
-template <typename E, int D, int GK, int G>
-__global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 128 ? 1 : 2)) void solve_kernel(TauArgs a) {
+// A = Packed<TauArgs>: packed sequences with grouped heads; everything but
+// the place of the workgroup's rows is the same.
+template <typename E, int D, int GK, int G, typename A>
+__global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 128 ? 1 : 2)) void solve_kernel(A a) {
+  constexpr bool PK = is_packed<A>::value;
   using TL = PadTile<E, D>;
   using M = Mma<E>;
   constexpr int KS = D / M::KW;
@@ -85,7 +89,11 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
   __shared__ uint32_t bits[SV_WAVES * BW];
 
   const int lane = lane_id(), w = wave_id();
-  const int n = a.n, T = a.T;
+  const int tile = a.tile0 + (int)blockIdx.x;
+  [[maybe_unused]] Place at;
+  if constexpr (PK)
+    if (!packed_place(a.pk, tile, a.pk.heads, false, at)) return;
+  const int n = PK ? at.n : a.n, T = PK ? at.T : a.T;
   const int nqt = (n + ROWS - 1) / ROWS;
   const int TW = (T + 31) / 32;
   const float c = a.c, g = a.gamma;
@@ -104,7 +112,6 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
   //  - singles of a later fill (CandEntry, 8 bytes), up to `scap` per list
   //    over the whole slot.
   const int kshift = n > LIST_MAX_SEQLEN ? 6 : 0;
-  const int tile = a.tile0 + (int)blockIdx.x;
   char* const slot = a.cand && (int)blockIdx.x < a.slots
                          ? static_cast<char*>(a.cand) + (size_t)blockIdx.x * (solve_slot_bytes(a.cap) / 2 * G)
                          : nullptr;
@@ -113,9 +120,17 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
   char* const sslot = cache ? kslot + (size_t)a.cap * G * SV_NT * 2 : nullptr;
   char* const bslot = cache ? sslot + (size_t)a.cap * G * SV_NT * 4 : nullptr;
   const int scap = a.cap * (int)(SOLVE_QUAD_BYTES + SOLVE_SINGLE_BYTES) / (int)sizeof(CandEntry);
-  const int bh = tile % a.BH;
-  int qt = tile / a.BH;
-  if (a.causal) qt = nqt - 1 - qt;  // longest rows first
+  const int bh = PK ? at.head : tile % a.BH;
+  int qt = PK ? at.tile : tile / a.BH;
+  if (!PK && a.causal) qt = nqt - 1 - qt;  // longest rows first
+  const size_t row0 = PK ? at.row0 : (size_t)bh * n;  // of the head in tau, and its tables
+  const size_t blk0 = PK ? at.blk0 : (size_t)bh * T;
+  int width = T, ldq = D, ldk = D;
+  if constexpr (PK) {
+    width = a.pk.width;
+    ldq = a.pk.q.row;
+    ldk = a.pk.k.row;
+  }
   const int q0 = qt * ROWS + 32 * G * w;  // first row of this wave
   const int qb = q0 / BLK;                 // its query block
   const int qbl = G == 2 ? w : w >> 1;     // that block's mask words in `bits`
@@ -129,19 +144,26 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
     row_ok[gq] = qi[gq] < n;
     ni[gq] = a.causal ? qi[gq] + 1 : n;
   }
-  const E* Q = static_cast<const E*>(a.q) + (size_t)bh * n * D;
-  const E* K = static_cast<const E*>(a.k) + (size_t)bh * n * D;
+  const E* Q = static_cast<const E*>(a.q);
+  const E* K = static_cast<const E*>(a.k);
+  if constexpr (PK) {
+    Q += (int64_t)at.start * ldq + bh * a.pk.q.head;
+    K += (int64_t)at.start * ldk + bh / a.pk.group * a.pk.k.head;
+  } else {
+    Q += (size_t)bh * n * D;
+    K += (size_t)bh * n * D;
+  }
   const int wg_last = min(n, (qt + 1) * ROWS) - 1;
   const int nkb = a.causal ? wg_last / BLK + 1 : T;
 
-  TileDma<TL, D, SV_NT> dma;
-  dma.init();
+  TileDma<TL, D, SV_NT, PK> dma;
+  dma.init(ldk);
 
   typename M::frag qf[G][KS];
 #pragma unroll
   for (int gq = 0; gq < G; ++gq)
 #pragma unroll
-    for (int kk = 0; kk < KS; ++kk) qf[gq][kk] = load_row_frag_global<E, D>(Q, qi[gq], n, kk);
+    for (int kk = 0; kk < KS; ++kk) qf[gq][kk] = load_row_frag_global<E, D>(Q, qi[gq], n, kk, ldq);
 
   for (int x = lane; x < TW; x += 64) bits[qbl * BW + x] = 0;
 
@@ -632,7 +654,9 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
   // scores pass than at the bound of the first stream alone.
   const int first = W < nkb ? W : 0;
   [[maybe_unused]] int seen = 0;  // key blocks searched for the lists
-  const bool more = sizeof(E) == 2 && g <= 2.f && T >= REFINE_MORE_BLOCKS && a.BH * nqt <= SV_G1_BELOW * 2 / G;
+  int tiles = a.BH * nqt;
+  if constexpr (PK) tiles = a.pk.heads * ((const ci32*)a.pk.header->count)[a.pk.size];
+  const bool more = sizeof(E) == 2 && g <= 2.f && T >= REFINE_MORE_BLOCKS && tiles <= SV_G1_BELOW * 2 / G;
   auto nth = [&](int kb) { return kb >= first ? kb - first : kb - first + nkb; };  // its place in the stream
   stream_from(first, [&](int kb, const E* kt) {
     // once the lists have overflowed, the first stream's blocks need nothing
@@ -1009,7 +1033,7 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
     const bool stop = __syncthreads_and(conv) || it >= a.max_iter;
     evals = it + 1;
     if (stop && !cached) break;
-    if (sizeof(E) == 2 && stop && a.lists) {
+    if (!PK && sizeof(E) == 2 && stop && a.lists) {
 #pragma unroll
       for (int gq = 0; gq < G; ++gq) support += mc[gq];
 #pragma unroll
@@ -1062,13 +1086,13 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
   // (nor where the support is more than any use takes: B8 H12 n1024 d64 c =
   // 0.5, 460 against 408 us; not for fp32, whose limits are wide, and which at
   // d = 128 would pass 256 registers and run one wave per SIMD)
-  if constexpr (sizeof(E) == 2) {
+  if constexpr (!PK && sizeof(E) == 2) {
     if (lane == 0) atomicAdd(&ssum[qbl], support);
     __syncthreads();
     support = __builtin_amdgcn_readfirstlane(ssum[qbl]);
     listable &= support <= list_few(T) || support <= LIST_MOST * 33 / 32 * (a.causal ? qb + 1 : T);
   }
-  ListBlock* const lb = a.lists && listable && qb < T ? a.lists + ((size_t)bh * T + qb) : nullptr;
+  ListBlock* const lb = !PK && a.lists && listable && qb < T ? a.lists + ((size_t)bh * T + qb) : nullptr;
   int lc[G] = {};
   auto list_id = [&](int gq) { return 64 * (lane >> 5) + (q0 - qb * BLK) + 32 * gq + (lane & 31); };
   auto emit = [&](int gq, float zp, int key) {
@@ -1135,7 +1159,7 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
     auto z64 = [&](int gq, float sv, int jv) -> double {
       const float raw = fmaf(c, sv, -tau[gq]);
       if (!(raw > -band[gq])) return -1.0;
-      return exact_x<D>(Qf + (size_t)qi[gq] * D, Kf + (size_t)jv * D, a.c64) - t64[gq];
+      return exact_x<D>(Qf + (size_t)qi[gq] * ldq, Kf + (size_t)jv * ldk, a.c64) - t64[gq];
     };
     // With compacted lists (and whole keys in them) the fp64 scores are taken
     // once and kept where the quads were: at B2 H4 n1025 d64 causal, alpha
@@ -1153,8 +1177,8 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
       for (int gq = 0; gq < G; ++gq)
         for (int e = 0; e < ns[gq]; ++e) {
           const float raw = fmaf(c, ld_single(e, gq, true), -tau[gq]);
-          *x64_at(e, gq) = raw > -band[gq] ? exact_x<D>(Qf + (size_t)qi[gq] * D,
-                                                        Kf + (size_t)ld_block(e, gq, true) * D, a.c64)
+          *x64_at(e, gq) = raw > -band[gq] ? exact_x<D>(Qf + (size_t)qi[gq] * ldq,
+                                                        Kf + (size_t)ld_block(e, gq, true) * ldk, a.c64)
                                            : -1e300;  // below the band: outside the support
         }
     }
@@ -1190,8 +1214,8 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
       for (int gq = 0; gq < G; ++gq)
         if (row_ok[gq]) {
           const float th = (float)t64[gq];
-          a.tau[(size_t)bh * n + qi[gq]] = th;
-          a.tau_lo[(size_t)bh * n + qi[gq]] = (float)(t64[gq] - (double)th);
+          a.tau[row0 + qi[gq]] = th;
+          a.tau_lo[row0 + qi[gq]] = (float)(t64[gq] - (double)th);
         }
     }
     for (int x = lane; x < TW; x += 64) bits[qbl * BW + x] = 0;
@@ -1214,8 +1238,8 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
 #pragma unroll
       for (int gq = 0; gq < G; ++gq)
         if (row_ok[gq]) {
-          a.tau[(size_t)bh * n + qi[gq]] = tau[gq];
-          if (std::is_same<E, float>::value) a.tau_lo[(size_t)bh * n + qi[gq]] = 0.f;
+          a.tau[row0 + qi[gq]] = tau[gq];
+          if (std::is_same<E, float>::value) a.tau_lo[row0 + qi[gq]] = 0.f;
         }
     }
     if (cached) {
@@ -1243,7 +1267,7 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
 #pragma unroll
     for (int gq = 0; gq < G; ++gq) {
       lb->count[list_id(gq)] = (uint8_t)min(lc[gq], LIST_CAP);
-      if (lane < 32 && row_ok[gq]) lb->tau[list_id(gq)] = a.tau[(size_t)bh * n + qi[gq]];
+      if (lane < 32 && row_ok[gq]) lb->tau[list_id(gq)] = a.tau[row0 + qi[gq]];
       total += lc[gq] > LIST_CAP ? LIST_ENTRIES + 1 : lc[gq];
     }
 #pragma unroll
@@ -1258,20 +1282,20 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
   // a ballot and a prefix count per 64 key blocks.
   // (The no-mask mode takes neither.)
   const bool tables = a.mask != nullptr;
-  int32_t* const row = a.q_index + ((size_t)bh * T + qb) * T;
+  int32_t* const row = a.q_index + (blk0 + qb) * width;
   int listed = 0;
   for (int k0 = 0; k0 < T; k0 += 64) {
     const int kb = k0 + lane;
     const bool b = kb < T && ((bits[qbl * BW + (kb >> 5)] >> (kb & 31)) & 1u);
-    if (tables && kb < T) a.mask[((size_t)bh * T + qb) * T + kb] = b ? 1 : 0;
+    if (tables && kb < T) a.mask[(blk0 + qb) * width + kb] = b ? 1 : 0;
     const unsigned long long m = __ballot(b);
     if (tables && b) row[listed + __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u))] = kb;
     listed += __popcll(m);
   }
-  if (tables && lane == 0) a.q_count[(size_t)bh * T + qb] = listed;
-  if (a.lists && lane == 0)
+  if (tables && lane == 0) a.q_count[blk0 + qb] = listed;
+  if (!PK && a.lists && lane == 0)
     a.use[(size_t)bh * T + qb] = cached ? list_use(lsum[qbl], listed, T, sizeof(E) == 4) : LIST_NONE;
-  if (a.stats && lane == 0) {
+  if (!PK && a.stats && lane == 0) {
     a.stats[(size_t)bh * T + qb] = passes;
     a.stats[((size_t)a.BH + bh) * T + qb] = evals;
   }
@@ -1297,10 +1321,10 @@ hipError_t launch_tiles(K kernel, TauArgs a, int rows, int threads, hipStream_t 
 
 template <typename E, int D, int G>
 hipError_t launch_solve_g(TauArgs a, hipStream_t s) {
-  auto kernel = solve_kernel<E, D, 0, G>;
-  if (a.gk == 1) kernel = solve_kernel<E, D, 1, G>;
-  if (a.gk == 2) kernel = solve_kernel<E, D, 2, G>;
-  if (a.gk == 4) kernel = solve_kernel<E, D, 4, G>;
+  auto kernel = solve_kernel<E, D, 0, G, TauArgs>;
+  if (a.gk == 1) kernel = solve_kernel<E, D, 1, G, TauArgs>;
+  if (a.gk == 2) kernel = solve_kernel<E, D, 2, G, TauArgs>;
+  if (a.gk == 4) kernel = solve_kernel<E, D, 4, G, TauArgs>;
   // a slot of the two-group form holds the lists of two one-group tiles
   if (G == 1) a.slots *= 2;
   return launch_tiles(kernel, a, SV_ROWS / 2 * G, SV_NT, s);
@@ -1320,6 +1344,38 @@ hipError_t launch_solve_d(const TauArgs& a, hipStream_t s) {
   const int64_t tiles = (int64_t)a.BH * ((a.n + SV_ROWS - 1) / SV_ROWS);
   if (tiles < SV_G1_BELOW || (D <= 64 && a.n <= SV_G1_MAX_N)) return launch_solve_g<E, D, 1>(a, s);
   return launch_solve_g<E, D, 2>(a, s);
+}
+
+// Packed sequences: as launch_tiles, over the most tiles that the sequences
+// can have.
+template <typename E, int D, int G>
+hipError_t launch_solve_packed_g(Packed<TauArgs> a, int tiles, hipStream_t s) {
+  using A = Packed<TauArgs>;
+  auto kernel = solve_kernel<E, D, 0, G, A>;
+  if (a.gk == 1) kernel = solve_kernel<E, D, 1, G, A>;
+  if (a.gk == 2) kernel = solve_kernel<E, D, 2, G, A>;
+  if (a.gk == 4) kernel = solve_kernel<E, D, 4, G, A>;
+  if (G == 1) a.slots *= 2;
+  const int per = a.cand && a.slots > 0 && a.slots < tiles ? a.slots : tiles;
+  for (int t0 = 0; t0 < tiles; t0 += per) {
+    a.tile0 = t0;
+    const hipError_t e = launch_kernel(kernel, dim3((unsigned)(tiles - t0 < per ? tiles - t0 : per)),
+                                       dim3(SV_NT), s, a);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+// The two forms as in launch_solve_d, by the most tiles.
+template <typename E, int D>
+hipError_t launch_solve_packed(Packed<TauArgs> a, hipStream_t s) {
+  PackedArgs& pk = a.pk;
+  const int tiles = pk.heads * packed_tiles(pk.tokens, pk.seq_count, 2);
+  const bool one = tiles < SV_G1_BELOW || (D <= 64 && pk.width * BLK <= SV_G1_MAX_N);
+  pk.size = one ? 1 : 2;
+  pk.tiles = pk.lists[pk.size];
+  if (one) return launch_solve_packed_g<E, D, 1>(a, pk.heads * packed_tiles(pk.tokens, pk.seq_count, 1), s);
+  return launch_solve_packed_g<E, D, 2>(a, tiles, s);
 }
 
 }  // namespace
@@ -1352,13 +1408,26 @@ static bool small_solver(const TauArgs& a, int dtype, int head_dim) {
   return head_dim == 64 || a.n <= 256 || blocks <= 512;
 }
 
+hipError_t launch_tau_packed(const Packed<TauArgs>& a, int dtype, int head_dim, hipStream_t s) {
+  if (dtype == 0) return head_dim == 64 ? launch_tau_packed_bf16_64(a, s) : launch_tau_packed_bf16_128(a, s);
+  return head_dim == 64 ? launch_tau_packed_f32_64(a, s) : launch_tau_packed_f32_128(a, s);
+}
+
 hipError_t launch_tau(const TauArgs& a, int dtype, int head_dim, hipStream_t s) {
   if (small_solver(a, dtype, head_dim)) return launch_tau_small(a, dtype, head_dim, s);
   if (dtype == 0) return head_dim == 64 ? launch_tau_bf16_64(a, s) : launch_tau_bf16_128(a, s);
   return head_dim == 64 ? launch_tau_f32_64(a, s) : launch_tau_f32_128(a, s);
 }
+#elif EA_TAU_PART == 5
+hipError_t launch_tau_packed_bf16_64(const Packed<TauArgs>& a, hipStream_t s) { return launch_solve_packed<__bf16, 64>(a, s); }
+#elif EA_TAU_PART == 6
+hipError_t launch_tau_packed_bf16_128(const Packed<TauArgs>& a, hipStream_t s) { return launch_solve_packed<__bf16, 128>(a, s); }
+#elif EA_TAU_PART == 7
+hipError_t launch_tau_packed_f32_64(const Packed<TauArgs>& a, hipStream_t s) { return launch_solve_packed<float, 64>(a, s); }
+#elif EA_TAU_PART == 8
+hipError_t launch_tau_packed_f32_128(const Packed<TauArgs>& a, hipStream_t s) { return launch_solve_packed<float, 128>(a, s); }
 #else
-#error "EA_TAU_PART must be 0 .. 4"
+#error "EA_TAU_PART must be 0 .. 8"
 #endif
 
 }  // namespace ea
