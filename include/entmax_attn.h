@@ -379,11 +379,13 @@ typedef struct {
   int32_t head_dim, dtype;         /* as ea_shape */
 } ea_packed_shape;
 
-/* Bytes of a plan, of the residuals that the forward writes and the backward
- * reads (params->need_bwd; without it, scratch of the forward), and of the
- * workspaces (the forward's is optional, as entmax_attn_fwd's). */
+/* Bytes of the residuals that the forward writes and the backward reads
+ * (params->need_bwd; without it, scratch of the forward), of the workspaces
+ * (the forward's is optional, as entmax_attn_fwd's), and of the element lists
+ * (optional, as in entmax_attn_fwd_lists, and as much a residual as the
+ * others; 0 where max_seqlen is above 65536). */
 typedef struct {
-  size_t residuals, ws_fwd, ws_bwd;
+  size_t residuals, ws_fwd, ws_bwd, lists;
 } ea_packed_sizes;
 typedef struct {
   ea_strides q, k, v, o;
@@ -395,7 +397,8 @@ ea_status entmax_packed_plan(int32_t tokens, int32_t seqs, int32_t max_seqlen, i
 ea_status entmax_packed_sizes(const ea_packed_shape* shape, const ea_params* params, ea_packed_sizes* out);
 
 /*
- * Forward and backward.  plan: of the same tokens, seqs and max_seqlen (its
+ * Forward and backward.  lists: sizes.lists bytes, or NULL; a backward takes
+ * those of its forward, or NULL.  plan: of the same tokens, seqs and max_seqlen (its
  * causal only orders the work).  Every buffer 16-byte aligned.  dout has the
  * strides strides->o.  dq [tokens, heads, d], dk and dv [tokens, kv_heads, d]
  * are contiguous and of the inputs' dtype (each rounded once, from fp32 sums).
@@ -406,12 +409,13 @@ ea_status entmax_packed_sizes(const ea_packed_shape* shape, const ea_params* par
 ea_status entmax_packed_fwd(const ea_packed_shape* shape, const ea_params* params, const void* plan,
                             const void* q, const void* k, const void* v, void* o,
                             const ea_packed_strides* strides, int32_t zero_rest, void* residuals,
-                            size_t residual_bytes, void* workspace, size_t ws_bytes, void* stream);
+                            size_t residual_bytes, void* lists, size_t lists_bytes, void* workspace,
+                            size_t ws_bytes, void* stream);
 ea_status entmax_packed_bwd(const ea_packed_shape* shape, const ea_params* params, const void* plan,
                             const void* q, const void* k, const void* v, const void* dout,
                             const ea_packed_strides* strides, int32_t zero_rest, const void* residuals,
-                            size_t residual_bytes, void* dq, void* dk, void* dv, void* workspace,
-                            size_t ws_bytes, void* stream);
+                            size_t residual_bytes, const void* lists, size_t lists_bytes, void* dq, void* dk,
+                            void* dv, void* workspace, size_t ws_bytes, void* stream);
 
 /*
  * One new token per request: o[b, h] = sum_j p_j v_j over the `prefix` keys

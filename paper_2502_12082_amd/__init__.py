@@ -772,7 +772,7 @@ class PackedShape(ctypes.Structure):
 
 
 class PackedSizes(ctypes.Structure):
-    _fields_ = [(f, ctypes.c_size_t) for f in ("residuals", "ws_fwd", "ws_bwd")]
+    _fields_ = [(f, ctypes.c_size_t) for f in ("residuals", "ws_fwd", "ws_bwd", "lists")]
 
 
 class PackedStrides(ctypes.Structure):
@@ -800,9 +800,9 @@ for _name, _args in (
         ("entmax_packed_plan", [_i32, _i32, _i32, _i32, _v, _v, _sz, _v]),
         ("entmax_packed_sizes", [_P(PackedShape), _P(Params), _P(PackedSizes)]),
         ("entmax_packed_fwd", [_P(PackedShape), _P(Params), _v, _v, _v, _v, _v, _P(PackedStrides), _i32,
-                               _v, _sz, _v, _sz, _v]),
+                               _v, _sz, _v, _sz, _v, _sz, _v]),
         ("entmax_packed_bwd", [_P(PackedShape), _P(Params), _v, _v, _v, _v, _v, _P(PackedStrides), _i32,
-                               _v, _sz, _v, _v, _v, _v, _sz, _v]),
+                               _v, _sz, _v, _sz, _v, _v, _v, _v, _sz, _v]),
         ("entmax_prefix_decode_workspace", [_P(DecodeShape), _P(_sz)]),
         ("entmax_prefix_decode", [_P(DecodeShape), _P(Params), _P(DecodeStrides), _v, _v, _v, _v, _v, _v,
                                   _v, _v, _sz, _v])):
@@ -1046,11 +1046,21 @@ def packed_plan(cu_seqlens, tokens, max_seqlen=None, causal=True) -> PackedPlan:
 
 class PackedResiduals:
     """What packed_forward leaves for packed_backward: thresholds, O^(2) and the
-    block tables in one device buffer, and the plan."""
+    block tables in one device buffer, the element lists (see Residuals) or
+    None, and the plan."""
 
-    def __init__(self, shape: PackedShape, params: Params, plan: PackedPlan, sizes: PackedSizes, device):
+    def __init__(self, shape: PackedShape, params: Params, plan: PackedPlan, sizes: PackedSizes, device,
+                 lists: bool = True):
         self.shape, self.params, self.plan, self.sizes = shape, params, plan, sizes
         self.buffer = torch.empty(sizes.residuals, dtype=torch.uint8, device=device)
+        # (as for Residuals: short sequences are not listed)
+        short = shape.max_seqlen <= (LISTS_FROM if shape.dtype == EA_BF16 else LISTS_FROM // 4)
+        nbytes = 0 if short or not lists else sizes.lists
+        self._share = _claim(self.buffer.device, nbytes) if nbytes else None
+        self.lists = _bytes_or_none(nbytes, device) if self._share else None
+
+    def lists_ptr(self):
+        return (None, 0) if self.lists is None else (self.lists.data_ptr(), self.lists.numel())
 
 
 def _packed_shape(q, k, v, plan):
@@ -1079,7 +1089,7 @@ def _packed_strides(q, k, v, o):
 
 
 def packed_forward(q, k, v, plan: PackedPlan, alpha=1.5, scale=None, need_bwd=True, max_iter=None, tol=None,
-                   out=None, workspace=None):
+                   out=None, workspace=None, lists=True):
     """(O, residuals) of alpha-entmax attention within each sequence of the plan
     (causal if the plan is): q [tokens, heads, d], k and v [tokens, kv_heads, d],
     bf16 or fp32, any strides with a contiguous last dimension; query head h
@@ -1088,7 +1098,8 @@ def packed_forward(q, k, v, plan: PackedPlan, alpha=1.5, scale=None, need_bwd=Tr
     Rows of no sequence (before cu_seqlens[0], behind the last) are 0 in an O
     that the call makes and left as they are in `out`.  need_bwd=False gives
     residuals that packed_backward does not take.  tol: default 1e-5, for fp32
-    1e-6.  workspace: as for forward (sizes.ws_fwd bytes of the residuals)."""
+    1e-6.  workspace: as for forward (sizes.ws_fwd bytes of the residuals).
+    lists: whether the residuals hold element lists (see Residuals)."""
     shape = _packed_shape(q, k, v, plan)
     if tol is None and shape.dtype == EA_F32:
         tol = 1e-6  # (Sum p is off by up to tol, which the fp32 outputs show)
@@ -1108,7 +1119,7 @@ def packed_forward(q, k, v, plan: PackedPlan, alpha=1.5, scale=None, need_bwd=Tr
     with _on_device(q.device):
         if made:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        res = PackedResiduals(shape, params, plan, sizes, q.device)
+        res = PackedResiduals(shape, params, plan, sizes, q.device, lists)
         if workspace is None:
             workspace = torch.empty(max(sizes.ws_fwd, 16), dtype=torch.uint8, device=q.device)
         ws, ws_bytes = (None, 0) if workspace is False else (workspace.data_ptr(),
@@ -1116,7 +1127,7 @@ def packed_forward(q, k, v, plan: PackedPlan, alpha=1.5, scale=None, need_bwd=Tr
         _check(_lib.entmax_packed_fwd(
             ctypes.byref(shape), ctypes.byref(params), plan.buffer.data_ptr(), q.data_ptr(), k.data_ptr(),
             v.data_ptr(), out.data_ptr(), _packed_strides(q, k, v, out), int(made), res.buffer.data_ptr(),
-            res.buffer.numel(), ws, ws_bytes, _stream_handle(q.device)), "entmax_packed_fwd")
+            res.buffer.numel(), *res.lists_ptr(), ws, ws_bytes, _stream_handle(q.device)), "entmax_packed_fwd")
     return out, res
 
 
@@ -1161,7 +1172,7 @@ def packed_backward(q, k, v, dout, res: PackedResiduals, dq=None, dk=None, dv=No
         _check(_lib.entmax_packed_bwd(
             ctypes.byref(shape), ctypes.byref(res.params), res.plan.buffer.data_ptr(), q.data_ptr(),
             k.data_ptr(), v.data_ptr(), dout.data_ptr(), _packed_strides(q, k, v, dout), int(made),
-            res.buffer.data_ptr(), res.buffer.numel(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+            res.buffer.data_ptr(), res.buffer.numel(), *res.lists_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
             workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_handle(q.device)),
             "entmax_packed_bwd")
     return dq, dk, dv

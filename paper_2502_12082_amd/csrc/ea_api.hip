@@ -790,6 +790,23 @@ ea_status check_packed(const ea_packed_shape* s, const ea_params* p) {
   return EA_OK;
 }
 
+size_t packed_lists_bytes(const ea_packed_shape* s) {
+  if (s->max_seqlen > LIST_MAX_SEQLEN) return 0;
+  const size_t blocks = (size_t)s->heads * packed_tiles(s->tokens, s->seqs, 0);
+  return up256(blocks * sizeof(ListBlock)) + blocks * 4;
+}
+int32_t* packed_lists_use(const ea_packed_shape* s, const void* lists) {
+  const size_t blocks = (size_t)s->heads * packed_tiles(s->tokens, s->seqs, 0);
+  return reinterpret_cast<int32_t*>(static_cast<char*>(const_cast<void*>(lists)) + up256(blocks * sizeof(ListBlock)));
+}
+ea_status check_packed_lists(const ea_packed_shape* s, const void* lists, size_t bytes) {
+  if (!lists) return EA_OK;
+  const size_t need = packed_lists_bytes(s);
+  if (need == 0) return EA_ERR_UNSUPPORTED;
+  if (!aligned(lists, 16)) return EA_ERR_INVALID_ARG;
+  return bytes < need ? EA_ERR_WORKSPACE : EA_OK;
+}
+
 int packed_parts(const ea_packed_shape* s) {
   return dkdv_packed_parts(s->tokens, s->seqs, s->heads, s->kv_heads, s->dtype, s->head_dim);
 }
@@ -884,17 +901,19 @@ ea_status entmax_packed_sizes(const ea_packed_shape* shape, const ea_params* par
   out->residuals = residual_parts(shape, params, nullptr, &r);
   out->ws_fwd = packed_ws_fwd(shape);
   out->ws_bwd = packed_ws_bwd(shape);
+  out->lists = packed_lists_bytes(shape);
   return EA_OK;
 }
 
 ea_status entmax_packed_fwd(const ea_packed_shape* shape, const ea_params* params, const void* plan, const void* q,
                             const void* k, const void* v, void* o, const ea_packed_strides* strides,
-                            int32_t zero_rest, void* residuals, size_t residual_bytes, void* workspace,
-                            size_t ws_bytes, void* stream) {
+                            int32_t zero_rest, void* residuals, size_t residual_bytes, void* lists,
+                            size_t lists_bytes, void* workspace, size_t ws_bytes, void* stream) {
   PackedResiduals r;
   ea_status st = prep_packed(shape, params, plan, q, k, v, o, strides, residuals, residual_bytes, &r);
   if (st != EA_OK) return st;
   if (workspace && !aligned(workspace, 16)) return EA_ERR_INVALID_ARG;
+  if ((st = check_packed_lists(shape, lists, lists_bytes)) != EA_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const PackedArgs pk = packed_args(shape, plan, strides, zero_rest);
   const int64_t most = (int64_t)shape->heads * packed_tiles(shape->tokens, shape->seqs, 2);
@@ -921,6 +940,10 @@ ea_status entmax_packed_fwd(const ea_packed_shape* shape, const ea_params* param
   ta.gk = gamma_kind(params->alpha);
   ta.c64 = c64_of(params);
   ta.g64 = g64_of(params);
+  if (lists) {
+    ta.lists = static_cast<ListBlock*>(lists);
+    ta.use = packed_lists_use(shape, lists);
+  }
   if ((st = from_hip(launch_tau_packed(ta, shape->dtype, shape->head_dim, s))) != EA_OK) return st;
   Packed<FwdArgs> fa{};
   fa.pk = pk;
@@ -942,19 +965,23 @@ ea_status entmax_packed_fwd(const ea_packed_shape* shape, const ea_params* param
   fa.gk = ta.gk;
   fa.c64 = ta.c64;
   fa.g64 = ta.g64;
+  fa.lists = ta.lists;
+  fa.use = ta.use;
   return from_hip(launch_fwd_packed(fa, shape->dtype, shape->head_dim, params->need_bwd != 0, s));
 }
 
 ea_status entmax_packed_bwd(const ea_packed_shape* shape, const ea_params* params, const void* plan, const void* q,
                             const void* k, const void* v, const void* dout, const ea_packed_strides* strides,
-                            int32_t zero_rest, const void* residuals, size_t residual_bytes, void* dq, void* dk,
-                            void* dv, void* workspace, size_t ws_bytes, void* stream) {
+                            int32_t zero_rest, const void* residuals, size_t residual_bytes, const void* lists,
+                            size_t lists_bytes, void* dq, void* dk, void* dv, void* workspace, size_t ws_bytes,
+                            void* stream) {
   PackedResiduals r;
   ea_status st = prep_packed(shape, params, plan, q, k, v, dout, strides, residuals, residual_bytes, &r);
   if (st != EA_OK) return st;
   if (!params->need_bwd || !tensor_ok(dq) || !tensor_ok(dk) || !tensor_ok(dv) || !tensor_ok(workspace))
     return EA_ERR_INVALID_ARG;
   if (ws_bytes < packed_ws_bwd(shape)) return EA_ERR_WORKSPACE;
+  if ((st = check_packed_lists(shape, lists, lists_bytes)) != EA_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(stream);
   Packed<DeltaArgs> da{};
   da.pk = packed_args(shape, plan, strides, zero_rest);
@@ -991,6 +1018,10 @@ ea_status entmax_packed_bwd(const ea_packed_shape* shape, const ea_params* param
   ba.gk = gamma_kind(params->alpha);
   ba.c64 = c64_of(params);
   ba.g64 = g64_of(params);
+  if (lists) {
+    ba.lists = static_cast<const ListBlock*>(lists);
+    ba.buckets.used = packed_lists_use(shape, lists);
+  }
   if ((st = from_hip(launch_bwd_dkdv_packed(ba, shape->dtype, shape->head_dim, s))) != EA_OK) return st;
   return from_hip(launch_bwd_dq_packed(ba, shape->dtype, shape->head_dim, s));
 }

@@ -1480,24 +1480,23 @@ constexpr int DQ_NT = 256;
 // against 0.252 ms on B1 H8 n16384 causal).
 // dQ of a query block from its element lists (see gather_fwd): dP = <dO_i,
 // V_j> summed over a group's lanes, then dQ_i += dS K_j in registers.  Per
-// entry this reads one row of V and one of K from L2.
-template <typename E, int D, int GK>
-__device__ __forceinline__ void gather_dq(const BwdArgs& a, const ListBlock& lb, int bh, int qb) {
+// entry this reads one row of V and one of K from L2.  The operands are the
+// head's, as in gather_fwd; dQ, of type Out, has rows ldq elements apart.
+template <typename E, int D, int GK, bool STRIDED, typename Out>
+__device__ __forceinline__ void gather_dq(float gamma, float scale, const ListBlock& lb, const E* K, int ldk, const E* V,
+                                          int ldv, const E* dO, int ldo, const float* delta, Out* dQ0, int ldq, int n,
+                                          int qb) {
   using R = RowGroup<E, D>;
   constexpr int VPL = R::VPL, LPR = R::LPR, BATCH = 8;
   const int lane = lane_id(), w = wave_id(), sub = lane % LPR;
-  const int n = a.n;
-  const size_t head = (size_t)bh * n * D;
-  const E* K = static_cast<const E*>(a.k) + head;
-  const E* V = static_cast<const E*>(a.v) + head;
-  const E* dO = static_cast<const E*>(a.dout) + head;
+  auto load = [&](const E* base, uint32_t row, int ld) { return STRIDED ? R::load(base, row, ld) : R::load(base, row); };
   for (int r0 = w * R::GROUPS; r0 < BLK; r0 += 4 * R::GROUPS) {
     const int row = r0 + lane / LPR, i = qb * BLK + row;
     const int c0 = lb.count[row], cnt = c0 + lb.count[64 + row];
     const uint32_t ir = (uint32_t)min(i, n - 1);
-    const float del = a.delta[(size_t)bh * n + ir];
+    const float del = delta[ir];
     float go[VPL], acc[VPL] = {};
-    R::unpack(R::load(dO, ir), go);
+    R::unpack(load(dO, ir, ldo), go);
     for (int base = 0; __ballot(base < cnt) != 0ull; base += LPR) {
       float z = 0.f;
       int key = 0;
@@ -1514,8 +1513,8 @@ __device__ __forceinline__ void gather_dq(const BwdArgs& a, const ListBlock& lb,
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
           const uint32_t j = (uint32_t)R::from(key, u0 + u);
-          vw[u] = R::load(V, j);
-          kw[u] = R::load(K, j);
+          vw[u] = load(V, j, ldv);
+          kw[u] = load(K, j, ldk);
         }
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
@@ -1524,7 +1523,7 @@ __device__ __forceinline__ void gather_dq(const BwdArgs& a, const ListBlock& lb,
 #pragma unroll
           for (int d = 0; d < VPL; ++d) dp = fmaf(go[d], x[d], dp);
           dp = R::sum(dp);
-          Gamma<GK>::pu(R::from(z, u0 + u), a.gamma, p, ue);
+          Gamma<GK>::pu(R::from(z, u0 + u), gamma, p, ue);
           // (nothing from the repeated entries past the end, whatever dP is)
           const float ds = ue > 0.f ? ue * (dp - del) : 0.f;
           R::unpack(kw[u], x);
@@ -1534,14 +1533,13 @@ __device__ __forceinline__ void gather_dq(const BwdArgs& a, const ListBlock& lb,
       }
     }
     if (i >= n) continue;
-    float* dQ = a.dq + head + (size_t)i * D + sub * VPL;
+    Out* dQ = dQ0 + (size_t)i * ldq + sub * VPL;
+    Out o[VPL];
 #pragma unroll
-    for (int d = 0; d < VPL; d += 4) {
-      f32x4 o;
+    for (int d = 0; d < VPL; ++d) o[d] = (Out)(cnt > 0 ? scale * acc[d] : 0.f);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = cnt > 0 ? a.scale * acc[d + e] : 0.f;
-      *reinterpret_cast<f32x4*>(dQ + d) = o;
-    }
+    for (int d = 0; d < VPL; d += 16 / (int)sizeof(Out))
+      *reinterpret_cast<u32x4*>(dQ + d) = *reinterpret_cast<const u32x4*>(o + d);
   }
 }
 
@@ -1573,10 +1571,6 @@ __global__ __launch_bounds__(DQ_NT, 2) void dq_kernel(A a) {
   if constexpr (!PK) {
     if (a.lists) head_major(blockIdx.x, a.BH, T, bh, qb, head_group<E, D>(n, 2));
     if (a.causal) qb = T - 1 - qb;  // longest lists first
-    if (a.lists && (a.buckets.used[(size_t)bh * T + qb] & LISTED)) {
-      gather_dq<E, D, GK>(a, a.lists[(size_t)bh * T + qb], bh, qb);
-      return;
-    }
   }
   const int q0 = qb * BLK + 32 * qh;
   const int i = q0 + (lane & 31);
@@ -1606,6 +1600,17 @@ __global__ __launch_bounds__(DQ_NT, 2) void dq_kernel(A a) {
     Kg += head;
     Vg += head;
     dOg += head;
+  }
+  // (the packed form's `used` is the forward's `use`: its residuals belong to one forward)
+  if (a.lists && (a.buckets.used[blk] & (PK ? (int)LIST_DQ : LISTED))) {
+    if constexpr (PK)
+      gather_dq<E, D, GK, true>(a.gamma, a.scale, a.lists[blk], Kg, ldk, Vg, ldv, dOg, ldo, a.delta + row0,
+                                reinterpret_cast<E*>(a.dq) + ((int64_t)at.start * a.pk.heads + bh) * D,
+                                a.pk.heads * D, n, qb);
+    else
+      gather_dq<E, D, GK, false>(a.gamma, a.scale, a.lists[blk], Kg, D, Vg, D, dOg, D, a.delta + row0, a.dq + head, D, n,
+                                 qb);
+    return;
   }
   const float tau = i < n ? a.tau[row0 + i] : 0.f;
   const float del = i < n ? a.delta[row0 + i] : 0.f;

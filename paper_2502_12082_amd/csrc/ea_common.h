@@ -504,6 +504,11 @@ struct RowGroup {
   static constexpr int LPR = D / VPL;              // lanes per row: 8, 16 or 32
   static constexpr int GROUPS = 64 / LPR;          // rows per wave
 
+  // (rows `ld` elements apart)
+  __device__ __forceinline__ static u32x4 load(const E* base, uint32_t row, int ld) {
+    const char* const p = reinterpret_cast<const char*>(base) + (size_t)row * (uint32_t)(ld * (int)sizeof(E));
+    return *reinterpret_cast<const u32x4*>(p + (uint32_t)(lane_id() % LPR) * 16u);
+  }
   __device__ __forceinline__ static u32x4 load(const E* base, uint32_t row) {
     const uint32_t off = row * (uint32_t)(D * sizeof(E)) + (uint32_t)(lane_id() % LPR) * 16u;
     return *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(base) + off);

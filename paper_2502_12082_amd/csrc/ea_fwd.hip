@@ -65,15 +65,14 @@ __device__ void column_table(const FwdArgs& a, size_t blk0, int j, int T, int wi
 // O (and O2) of a query block from its element lists: RowGroup::GROUPS rows
 // of a wave at once, each group of lanes adding up p V_j (and u V_j) over its
 // row's entries in registers.  Per entry this reads one row of V from L2 and
-// takes about D / 8 VALU operations in place of the block products.
-template <typename E, int D, int GK, bool TRAIN>
-__device__ __forceinline__ void gather_fwd(const FwdArgs& a, const ListBlock& lb, int bh, int qb) {
+// takes about D / 8 VALU operations in place of the block products.  V, O and
+// O2 are the head's, rows of V and O ldv and ldo elements apart (STRIDED) or D.
+template <typename E, int D, int GK, bool TRAIN, bool STRIDED>
+__device__ __forceinline__ void gather_fwd(float gamma, const ListBlock& lb, const E* V, int ldv, E* O0, int ldo,
+                                           float* O20, int n, int qb) {
   using R = RowGroup<E, D>;
   constexpr int VPL = R::VPL, LPR = R::LPR, BATCH = LPR < 16 ? LPR : 16;
   const int lane = lane_id(), w = wave_id(), sub = lane % LPR;
-  const int n = a.n;
-  const size_t head = (size_t)bh * n * D;
-  const E* V = static_cast<const E*>(a.v) + head;
   // the lengths of all the rows' lists first, 16 bits a row: one wait for
   // them instead of one a row
   constexpr int STEP = 4 * R::GROUPS;
@@ -106,12 +105,15 @@ __device__ __forceinline__ void gather_fwd(const FwdArgs& a, const ListBlock& lb
         if (u0 > 0 && __ballot(base + u0 < cnt) == 0ull) break;
         u32x4 v[BATCH];
 #pragma unroll
-        for (int u = 0; u < BATCH; ++u) v[u] = R::load(V, (uint32_t)R::from(key, u0 + u));
+        for (int u = 0; u < BATCH; ++u) {
+          const uint32_t j = (uint32_t)R::from(key, u0 + u);
+          v[u] = STRIDED ? R::load(V, j, ldv) : R::load(V, j);
+        }
 #pragma unroll
         for (int u = 0; u < BATCH; ++u) {
           float x[VPL], p, ue;
           R::unpack(v[u], x);
-          Gamma<GK>::pu(R::from(z, u0 + u), a.gamma, p, ue);
+          Gamma<GK>::pu(R::from(z, u0 + u), gamma, p, ue);
           usum += ue;
 #pragma unroll
           for (int d = 0; d < VPL; ++d) {
@@ -122,15 +124,14 @@ __device__ __forceinline__ void gather_fwd(const FwdArgs& a, const ListBlock& lb
       }
     }
     if (i >= n) continue;
-    const size_t off = head + (size_t)i * D + sub * VPL;
-    E* O = static_cast<E*>(a.o) + off;
+    E* O = O0 + (size_t)i * (STRIDED ? ldo : D) + sub * VPL;
     const bool any = cnt > 0;  // (a row without entries read row 0 of V)
     E ov[VPL];
 #pragma unroll
     for (int d = 0; d < VPL; ++d) ov[d] = (E)(any ? o[d] : 0.f);
     *reinterpret_cast<u32x4*>(O) = *reinterpret_cast<const u32x4*>(ov);
     if constexpr (TRAIN) {
-      float* O2 = a.o2 + off;
+      float* O2 = O20 + (size_t)i * D + sub * VPL;
 #pragma unroll
       for (int d = 0; d < VPL; d += 4) {
         f32x4 t;
@@ -201,10 +202,6 @@ __global__ __launch_bounds__(FWD_NT, !TRAIN && D == 64 && sizeof(E) == 2 ? 4 : 2
   if constexpr (!PK) {
     if (a.lists) head_major(blockIdx.x, a.BH, T, bh, qb, head_group<E, D>(n, 1));
     if (a.causal) qb = T - 1 - qb;  // longest lists first
-    if (a.lists && (((const ci32*)a.use)[(size_t)bh * T + qb] & LIST_FWD)) {
-      gather_fwd<E, D, GK, TRAIN>(a, a.lists[(size_t)bh * T + qb], bh, qb);
-      return;
-    }
   }
   const size_t row0 = PK ? at.row0 : (size_t)bh * n;
   const size_t blk = (PK ? at.blk0 : (size_t)bh * T) + qb;
@@ -234,6 +231,10 @@ __global__ __launch_bounds__(FWD_NT, !TRAIN && D == 64 && sizeof(E) == 2 ? 4 : 2
     K += head;
     V += head;
     O += head;
+  }
+  if (a.lists && (((const ci32*)a.use)[blk] & LIST_FWD)) {
+    gather_fwd<E, D, GK, TRAIN, PK>(a.gamma, a.lists[blk], V, ldv, O, ldo, a.o2 + head, n, qb);
+    return;
   }
   const float tau = i < n ? a.tau[row0 + i] : 0.f;
   const float c = a.c, g = a.gamma;

@@ -74,8 +74,9 @@ static_assert(SV_ROWS == 64 * SV_WAVES, "one 64-row query block per wave (G = 2)
 // per SIMD with G = 2.
 // A = Packed<TauArgs>: packed sequences with grouped heads; everything but
 // the place of the workgroup's rows is the same.
+// Solves tile `tile` with the cache slot `slot_index`.
 template <typename E, int D, int GK, int G, typename A>
-__global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 128 ? 1 : 2)) void solve_kernel(A a) {
+__device__ __forceinline__ void solve_tile(const A& a, const int tile, const int slot_index) {
   constexpr bool PK = is_packed<A>::value;
   using TL = PadTile<E, D>;
   using M = Mma<E>;
@@ -89,7 +90,6 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
   __shared__ uint32_t bits[SV_WAVES * BW];
 
   const int lane = lane_id(), w = wave_id();
-  const int tile = a.tile0 + (int)blockIdx.x;
   [[maybe_unused]] Place at;
   if constexpr (PK)
     if (!packed_place(a.pk, tile, a.pk.heads, false, at)) return;
@@ -98,8 +98,8 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
   const int TW = (T + 31) / 32;
   const float c = a.c, g = a.gamma;
   const bool newton_bound = g >= 1.f;  // f convex: Newton steps bound the root from below
-  // Tile a.tile0 + blockIdx.x, and this workgroup's cache slot, or none.  A
-  // launch covers at most one tile per slot (see launch_tiles).  List
+  // This workgroup's cache slot, or none.  A launch has at most one workgroup
+  // per slot (see launch_tiles).  List
   // (thread t, group gq) holds entry e at index (G e + gq) * SV_NT + t of
   // each array of the slot.  The lists come in three forms:
   //  - quads, as pass 0 collects them: a quad array (16 bytes per entry)
@@ -112,8 +112,8 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
   //  - singles of a later fill (CandEntry, 8 bytes), up to `scap` per list
   //    over the whole slot.
   const int kshift = n > LIST_MAX_SEQLEN ? 6 : 0;
-  char* const slot = a.cand && (int)blockIdx.x < a.slots
-                         ? static_cast<char*>(a.cand) + (size_t)blockIdx.x * (solve_slot_bytes(a.cap) / 2 * G)
+  char* const slot = a.cand && slot_index < a.slots
+                         ? static_cast<char*>(a.cand) + (size_t)slot_index * (solve_slot_bytes(a.cap) / 2 * G)
                          : nullptr;
   const bool cache = slot != nullptr;
   char* const kslot = cache ? slot + (size_t)a.cap * G * SV_NT * 16 : nullptr;
@@ -1033,7 +1033,7 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
     const bool stop = __syncthreads_and(conv) || it >= a.max_iter;
     evals = it + 1;
     if (stop && !cached) break;
-    if (!PK && sizeof(E) == 2 && stop && a.lists) {
+    if (sizeof(E) == 2 && stop && a.lists) {
 #pragma unroll
       for (int gq = 0; gq < G; ++gq) support += mc[gq];
 #pragma unroll
@@ -1086,13 +1086,13 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
   // (nor where the support is more than any use takes: B8 H12 n1024 d64 c =
   // 0.5, 460 against 408 us; not for fp32, whose limits are wide, and which at
   // d = 128 would pass 256 registers and run one wave per SIMD)
-  if constexpr (!PK && sizeof(E) == 2) {
+  if constexpr (sizeof(E) == 2) {
     if (lane == 0) atomicAdd(&ssum[qbl], support);
     __syncthreads();
     support = __builtin_amdgcn_readfirstlane(ssum[qbl]);
     listable &= support <= list_few(T) || support <= LIST_MOST * 33 / 32 * (a.causal ? qb + 1 : T);
   }
-  ListBlock* const lb = !PK && a.lists && listable && qb < T ? a.lists + ((size_t)bh * T + qb) : nullptr;
+  ListBlock* const lb = a.lists && listable && qb < T ? a.lists + (blk0 + qb) : nullptr;
   int lc[G] = {};
   auto list_id = [&](int gq) { return 64 * (lane >> 5) + (q0 - qb * BLK) + 32 * gq + (lane & 31); };
   auto emit = [&](int gq, float zp, int key) {
@@ -1293,11 +1293,34 @@ __global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 1
     listed += __popcll(m);
   }
   if (tables && lane == 0) a.q_count[blk0 + qb] = listed;
-  if (!PK && a.lists && lane == 0)
-    a.use[(size_t)bh * T + qb] = cached ? list_use(lsum[qbl], listed, T, sizeof(E) == 4) : LIST_NONE;
+  if (a.lists && lane == 0)
+    a.use[blk0 + qb] = cached ? list_use(lsum[qbl], listed, T, sizeof(E) == 4) : LIST_NONE;
   if (!PK && a.stats && lane == 0) {
     a.stats[(size_t)bh * T + qb] = passes;
     a.stats[((size_t)a.BH + bh) * T + qb] = evals;
+  }
+}
+
+// Tile a.tile0 + blockIdx.x.  The packed form's workgroups stay and take one
+// tile after another instead: the tiles of sequences of many lengths, in
+// launches of one per slot, would leave most of the device idle at the end of
+// each launch (32 heads of eight sequences of 130 to 4096 tokens, d = 128: five
+// launches, 1000 us, against one of 640).  Tiles come longest first, so in
+// every other round the workgroups take them in the opposite order, eight at a
+// time (a workgroup stays on its XCD and with it its head's keys): those that
+// had the longest of one round have the shortest of the next.
+template <typename E, int D, int GK, int G, typename A>
+__global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 128 ? 1 : 2)) void solve_kernel(A a) {
+  if constexpr (is_packed<A>::value) {
+    const int tiles = a.pk.heads * ((const ci32*)a.pk.header->count)[a.pk.size];
+    const int wg = blockIdx.x, wgs = gridDim.x, b = wg & 7, back = (wgs / 8 - 1 - (wg >> 3)) * 8 + b;
+    for (int t0 = 0, round = 0; t0 < tiles; t0 += wgs, ++round) {
+      const int tile = t0 + (wgs % 8 == 0 && (round & 1) ? back : wg);
+      if (tile < tiles) solve_tile<E, D, GK, G>(a, tile, wg);
+      __syncthreads();  // the tile's shared memory has been read
+    }
+  } else {
+    solve_tile<E, D, GK, G>(a, a.tile0 + (int)blockIdx.x, (int)blockIdx.x);
   }
 }
 
@@ -1346,8 +1369,9 @@ hipError_t launch_solve_d(const TauArgs& a, hipStream_t s) {
   return launch_solve_g<E, D, 2>(a, s);
 }
 
-// Packed sequences: as launch_tiles, over the most tiles that the sequences
-// can have.
+// Packed sequences: as many workgroups as the device holds at a time (256
+// compute units; waves per SIMD as the kernel is built for), and no more than
+// there are slots, or tiles.
 template <typename E, int D, int G>
 hipError_t launch_solve_packed_g(Packed<TauArgs> a, int tiles, hipStream_t s) {
   using A = Packed<TauArgs>;
@@ -1356,14 +1380,9 @@ hipError_t launch_solve_packed_g(Packed<TauArgs> a, int tiles, hipStream_t s) {
   if (a.gk == 2) kernel = solve_kernel<E, D, 2, G, A>;
   if (a.gk == 4) kernel = solve_kernel<E, D, 4, G, A>;
   if (G == 1) a.slots *= 2;
-  const int per = a.cand && a.slots > 0 && a.slots < tiles ? a.slots : tiles;
-  for (int t0 = 0; t0 < tiles; t0 += per) {
-    a.tile0 = t0;
-    const hipError_t e = launch_kernel(kernel, dim3((unsigned)(tiles - t0 < per ? tiles - t0 : per)),
-                                       dim3(SV_NT), s, a);
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  int wgs = 256 * (G == 1 ? SV_OCC1 : sizeof(E) == 4 && D == 128 ? 1 : 2);
+  if (a.cand && a.slots < wgs) wgs = a.slots;
+  return launch_kernel(kernel, dim3((unsigned)(tiles < wgs ? tiles : wgs)), dim3(SV_NT), s, a);
 }
 
 // The two forms as in launch_solve_d, by the most tiles.

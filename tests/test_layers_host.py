@@ -193,7 +193,7 @@ def test_packed_abi():
     st = ea.PackedStrides(*[ea.Strides(512, 64)] * 4)
     assert sizes(good) == ea.EA_OK
     call = lambda plan_, res_bytes, strides: lib.entmax_packed_fwd(
-        ctypes.byref(s), ctypes.byref(p), plan_, 4096, 4096, 4096, 4096, strides, 0, 4096, res_bytes, None, 0, None)
+        ctypes.byref(s), ctypes.byref(p), plan_, 4096, 4096, 4096, 4096, strides, 0, 4096, res_bytes, None, 0, None, 0, None)
     assert call(None, z.residuals, st) == ea.EA_ERR_INVALID_ARG
     assert call(4096, z.residuals - 1, st) == ea.EA_ERR_WORKSPACE
     assert call(4096, z.residuals, ea.PackedStrides(*[ea.Strides(511, 64)] * 4)) == ea.EA_ERR_INVALID_ARG
