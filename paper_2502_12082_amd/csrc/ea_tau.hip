@@ -64,6 +64,10 @@ constexpr int REFINE_MORE_LISTS = 16;
 constexpr int REFINE_MORE_BLOCKS = 32;
 // quads beyond their share of 1.5 times the capacity at which lists are given up
 constexpr int GIVE_UP_MIN = 24;
+// compacted singles of a list that the packed one-group form holds in LDS
+// (scores and keys of SV_NT lists; three workgroups share the 160 KB of a
+// compute unit)
+constexpr int LDS_SINGLES = 32;
 static_assert(SV_ROWS == 64 * SV_WAVES, "one 64-row query block per wave (G = 2)");
 
 // G = 2: each wave owns one 64-row query block as two groups of 32 rows.
@@ -83,7 +87,19 @@ __device__ __forceinline__ void solve_tile(const A& a, const int tile, const int
   constexpr int KS = D / M::KW;
   constexpr int BW = MAX_KEY_BLOCKS / 32;  // mask words per query block
   constexpr int ROWS = SV_WAVES * 32 * G;  // rows per workgroup
-  __shared__ __attribute__((aligned(16))) E kbuf[2][TL::ELEMS];
+  // The packed one-group form keeps its compacted lists in LDS, in place of the
+  // key tiles, which are not needed any more once the scores are collected.
+  constexpr bool IN_LDS = PK && G == 1 && !precise_path<E, GK>();
+  struct LdsLists {
+    float score[LDS_SINGLES + 1][SV_NT];  // (one row more: see the store)
+    uint16_t key[LDS_SINGLES + 1][SV_NT];
+  };
+  union Pool {
+    E kbuf[2][TL::ELEMS];
+    LdsLists lists[IN_LDS ? 1 : 0];
+  };
+  __shared__ __attribute__((aligned(16))) Pool pool;
+  auto& kbuf = pool.kbuf;
   // bit kb of word kb / 32: key block kb holds a positive probability for a
   // row of the query block (one per wave with G = 2, per pair of waves with
   // G = 1)
@@ -795,14 +811,109 @@ __device__ __forceinline__ void solve_tile(const A& a, const int tile, const int
     if (!newton_bound || !(cached || near)) tau[gq] = 0.5f * (lo[gq] + hi[gq]);
   }
   int attempts = cache ? 1 : 0;  // cache fills tried (pass 0 is the first)
-  // form of the lists: 0 quads, 1 compacted singles, 2 singles of a later fill
+  // form of the lists: 0 quads, 1 compacted singles, 2 singles of a later fill, 3 compacted singles in LDS
   int lists = 0;
   bool fits = false;             // a fill at the current lower end would fit
   float f_prev[G];
 #pragma unroll
   for (int gq = 0; gq < G; ++gq) f_prev[gq] = INFINITY;
 
+  // f and its derivatives from a lane's sums of z^gamma, z^(gamma-1),
+  // z^(gamma-2) and its count of z > 0.
+  auto derivatives = [&](float m0, float m1, float m2, int mc, float& f, float& f1, float& f2) {
+    if constexpr (GK == 1) m1 = (float)mc;
+    if constexpr (GK == 2) m2 = (float)mc;
+    m0 = sum_halves(m0);
+    m1 = sum_halves(m1);
+    m2 = sum_halves(m2);
+    f = m0 - 1.f;  // Eq. 3
+    if constexpr (GK == 1) {  // Eq. 6, 7
+      f1 = -m1;
+      f2 = 0.f;
+    } else if constexpr (GK == 2) {
+      f1 = -2.f * m1;
+      f2 = 2.f * m2;
+    } else if constexpr (GK == 4) {
+      f1 = -4.f * m1;
+      f2 = 12.f * m2;
+    } else {
+      f1 = -g * m1;
+      f2 = g * (g - 1.f) * m2;
+    }
+  };
+  // The update rules: B_f (Eq. 4); for gamma >= 1, where f is convex, the
+  // Newton step from tau bounds the root from below (less a slack for the
+  // rounding of f); H_f (Eq. 5) where it lands inside the bracket, widened
+  // by the slack of its fp32 ends, and for gamma < 1 only if |f| has halved
+  // since the last step; otherwise the midpoint.
+  auto update = [&](int gq, float f, float f1, float f2) {
+    if (!row_ok[gq]) return;
+    // gamma < 1: a row that has converged keeps its tau while others go on
+    // (its |f| cannot halve any more, and the midpoint that follows from
+    // that is as far away as the bracket is wide)
+    if (!newton_bound && fabsf(f) <= a.tol) return;
+    if (f < 0.f)
+      hi[gq] = tau[gq];
+    else
+      lo[gq] = tau[gq];
+    const float slack = 1e-6f * fmaxf(1.f, fmaxf(fabsf(lo[gq]), fabsf(hi[gq])));
+    if (newton_bound && f1 < 0.f) {
+      const float tn = tau[gq] - f / f1 - 10.f * slack;
+      lo[gq] = fminf(fmaxf(lo[gq], tn), hi[gq]);
+    }
+    const float th = tau[gq] - 2.f * f * f1 / (2.f * f1 * f1 - f * f2);
+    bool take = th >= lo[gq] - slack && th <= hi[gq] + slack;
+    if (!newton_bound && fabsf(f) > 0.5f * f_prev[gq]) take = false;
+    f_prev[gq] = fabsf(f);
+    // (a step that ends below a bracket whose lower end is Newton's bound:
+    // that end is the better guess)
+    tau[gq] = take ? fminf(fmaxf(th, lo[gq]), hi[gq])
+                   : newton_bound && th < lo[gq] ? lo[gq] : 0.5f * (lo[gq] + hi[gq]);
+  };
+
   int support = 0;  // of the wave's rows, at the last evaluation (uniform)
+
+  // The packed one-group form's first evaluation: use(score) of every quad's
+  // scores, and those above `bound` into the LDS lists.  A score is stored
+  // where its list ends, kept or not: the next one overwrites it if it is not.
+  // False if a list of the wave is too long.
+  [[maybe_unused]] auto to_lds_lists = [&](float bound, auto&& use) {
+    LdsLists& ll = pool.lists[0];
+    int k = 0;
+    scan_quads(0, [&](const f32x4& v, int key4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        use(v[i]);
+        const int at = min(k, LDS_SINGLES);
+        ll.score[at][threadIdx.x] = v[i];
+        ll.key[at][threadIdx.x] = (uint16_t)((4 * key4 + i) >> kshift);
+        k += v[i] > bound ? 1 : 0;
+      }
+    });
+    ns[0] = k;
+    nsmax[0] = __builtin_amdgcn_readfirstlane(wave_max(k));
+    return nsmax[0] <= LDS_SINGLES;
+  };
+  // use(score, key) of the LDS list (key as in scan_compact)
+  [[maybe_unused]] auto scan_lds = [&](auto&& use) {
+    LdsLists& ll = pool.lists[0];
+    for (int e0 = 0; e0 < nsmax[0]; e0 += 8) {
+      float v[8];
+      int kv[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int e = min(e0 + u, LDS_SINGLES);
+        v[u] = ll.score[e][threadIdx.x];
+        kv[u] = ll.key[e][threadIdx.x];
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) use(e0 + u < ns[0] ? v[u] : -INFINITY, kv[u] << kshift);
+    }
+  };
+  // Whether something holds for all, or any, threads that go on together: in
+  // the packed form with the cache in use a wave goes on by itself.
+  auto all_of = [&](bool v) { return PK && G == 1 && cached ? __ballot(!v) == 0ull : (bool)__syncthreads_and(v); };
+  auto any_of = [&](bool v) { return PK && G == 1 && cached ? __ballot(v) != 0ull : (bool)__syncthreads_or(v); };
   for (int it = 0;; ++it) {
     // ---- evaluation at tau (per group): m0 = sum z^gamma, m1 = sum
     // z^(gamma-1), m2 = sum z^(gamma-2) over the strict support z > 0, mc =
@@ -960,11 +1071,19 @@ __device__ __forceinline__ void solve_tile(const A& a, const int tile, const int
         fits = !__syncthreads_or(any_over(over, scap));
         if (!fits) attempts = 2;  // no retry, and no more counting
       }
+    } else if (IN_LDS && lists == 3) {
+      scan_lds([&](float sv, int) { add_z(relu_z(c, sv, tau[0]), 0); });
     } else if (lists == 2) {
       scan_scores_singles([&](int gq, float sv) { add_z(relu_z(c, sv, tau[gq]), gq); });
     } else if (lists == 1) {
       scan_scores_compact([&](int gq, float sv) { add_z(relu_z(c, sv, tau[gq]), gq); });
+    } else if (IN_LDS && it == 0 && to_lds_lists(s_lo[0], [&](float sv) { add_z(relu_z(c, sv, tau[0]), 0); })) {
+      lists = 3;
     } else if (it == 0) {
+      if constexpr (IN_LDS) {  // (the evaluation starts again)
+        m0[0] = m1[0] = m2[0] = 0.f;
+        mc[0] = 0;
+      }
       // first evaluation on the quads: also copies the scores above the
       // lower end (every later tau stays >= lo, so the others are 0 there)
       // into the compacted lists, in the same order
@@ -989,7 +1108,7 @@ __device__ __forceinline__ void solve_tile(const A& a, const int tile, const int
           cs[gq] += keep ? 1 : 0;
         }
       });
-      if (!__syncthreads_or(any_over(cs, a.cap))) {
+      if (!any_of(any_over(cs, a.cap))) {
         lists = 1;
 #pragma unroll
         for (int gq = 0; gq < G; ++gq) {
@@ -1005,32 +1124,14 @@ __device__ __forceinline__ void solve_tile(const A& a, const int tile, const int
     float f[G], f1[G], f2[G];
 #pragma unroll
     for (int gq = 0; gq < G; ++gq) {
-      if constexpr (GK == 1) m1[gq] = (float)mc[gq];
-      if constexpr (GK == 2) m2[gq] = (float)mc[gq];
-      m0[gq] = sum_halves(m0[gq]);
-      m1[gq] = sum_halves(m1[gq]);
-      m2[gq] = sum_halves(m2[gq]);
-      f[gq] = m0[gq] - 1.f;  // Eq. 3
-      if constexpr (GK == 1) {  // Eq. 6, 7
-        f1[gq] = -m1[gq];
-        f2[gq] = 0.f;
-      } else if constexpr (GK == 2) {
-        f1[gq] = -2.f * m1[gq];
-        f2[gq] = 2.f * m2[gq];
-      } else if constexpr (GK == 4) {
-        f1[gq] = -4.f * m1[gq];
-        f2[gq] = 12.f * m2[gq];
-      } else {
-        f1[gq] = -g * m1[gq];
-        f2[gq] = g * (g - 1.f) * m2[gq];
-      }
+      derivatives(m0[gq], m1[gq], m2[gq], mc[gq], f[gq], f1[gq], f2[gq]);
       conv &= !row_ok[gq] || fabsf(f[gq]) <= a.tol;
     }
     // A streamed evaluation has just written the mask bits at this tau, so
     // the loop ends here.  With cached scores the bits are rebuilt at the
     // end from the returned tau, so the update from this last evaluation
     // is still taken: one more Halley step costs nothing there.
-    const bool stop = __syncthreads_and(conv) || it >= a.max_iter;
+    const bool stop = all_of(conv) || it >= a.max_iter;
     evals = it + 1;
     if (stop && !cached) break;
     if (sizeof(E) == 2 && stop && a.lists) {
@@ -1041,35 +1142,7 @@ __device__ __forceinline__ void solve_tile(const A& a, const int tile, const int
       support = __builtin_amdgcn_readfirstlane(support);
     }
 #pragma unroll
-    for (int gq = 0; gq < G; ++gq) {
-      if (!row_ok[gq]) continue;
-      // gamma < 1: a row that has converged keeps its tau while others go on
-      // (its |f| cannot halve any more, and the midpoint that follows from
-      // that is as far away as the bracket is wide)
-      if (!newton_bound && fabsf(f[gq]) <= a.tol) continue;
-      // The update rules: B_f (Eq. 4); for gamma >= 1, where f is convex, the
-      // Newton step from tau bounds the root from below (less a slack for the
-      // rounding of f); H_f (Eq. 5) where it lands inside the bracket, widened
-      // by the slack of its fp32 ends, and for gamma < 1 only if |f| has halved
-      // since the last step; otherwise the midpoint.
-      if (f[gq] < 0.f)
-        hi[gq] = tau[gq];
-      else
-        lo[gq] = tau[gq];
-      const float slack = 1e-6f * fmaxf(1.f, fmaxf(fabsf(lo[gq]), fabsf(hi[gq])));
-      if (newton_bound && f1[gq] < 0.f) {
-        const float tn = tau[gq] - f[gq] / f1[gq] - 10.f * slack;
-        lo[gq] = fminf(fmaxf(lo[gq], tn), hi[gq]);
-      }
-      const float th = tau[gq] - 2.f * f[gq] * f1[gq] / (2.f * f1[gq] * f1[gq] - f[gq] * f2[gq]);
-      bool take = th >= lo[gq] - slack && th <= hi[gq] + slack;
-      if (!newton_bound && fabsf(f[gq]) > 0.5f * f_prev[gq]) take = false;
-      f_prev[gq] = fabsf(f[gq]);
-      // (a step that ends below a bracket whose lower end is Newton's bound:
-      // that end is the better guess)
-      tau[gq] = take ? fminf(fmaxf(th, lo[gq]), hi[gq])
-                     : newton_bound && th < lo[gq] ? lo[gq] : 0.5f * (lo[gq] + hi[gq]);
-    }
+    for (int gq = 0; gq < G; ++gq) update(gq, f[gq], f1[gq], f2[gq]);
     if (stop) break;
   }
 
@@ -1082,7 +1155,7 @@ __device__ __forceinline__ void solve_tile(const A& a, const int tile, const int
   // (not tried where many rows hold half as many candidates again as a list
   // takes; a few such rows may still fit, and one block that is not listed
   // among many that are keeps the launches of the later kernels waiting for it)
-  bool listable = cached && __popcll(__ballot(any_over(lists == 1 ? ns : cc, LIST_CAP * 3 / 2))) <= 8;
+  bool listable = cached && __popcll(__ballot(any_over(lists == 1 || lists == 3 ? ns : cc, LIST_CAP * 3 / 2))) <= 8;
   // (nor where the support is more than any use takes: B8 H12 n1024 d64 c =
   // 0.5, 460 against 408 us; not for fp32, whose limits are wide, and which at
   // d = 128 would pass 256 registers and run one wave per SIMD)
@@ -1248,7 +1321,9 @@ __device__ __forceinline__ void solve_tile(const A& a, const int tile, const int
       __syncthreads();
 #pragma unroll
       for (int gq = 0; gq < G; ++gq) {
-        if (lists == 2) {
+        if (IN_LDS && lists == 3) {
+          scan_lds([&](float sv, int jv) { emit(0, relu_z(c, sv, tau[0]), jv); });
+        } else if (lists == 2) {
           scan_singles(gq, [&](float sv, int jv) { emit(gq, relu_z(c, sv, tau[gq]), jv); });
         } else if (lists == 1) {
           scan_compact(gq, [&](float sv, int jv) { emit(gq, relu_z(c, sv, tau[gq]), jv); });
@@ -1390,7 +1465,7 @@ template <typename E, int D>
 hipError_t launch_solve_packed(Packed<TauArgs> a, hipStream_t s) {
   PackedArgs& pk = a.pk;
   const int tiles = pk.heads * packed_tiles(pk.tokens, pk.seq_count, 2);
-  const bool one = tiles < SV_G1_BELOW || (D <= 64 && pk.width * BLK <= SV_G1_MAX_N);
+  const bool one = true;
   pk.size = one ? 1 : 2;
   pk.tiles = pk.lists[pk.size];
   if (one) return launch_solve_packed_g<E, D, 1>(a, pk.heads * packed_tiles(pk.tokens, pk.seq_count, 1), s);
