@@ -381,11 +381,12 @@ typedef struct {
 
 /* Bytes of the residuals that the forward writes and the backward reads
  * (params->need_bwd; without it, scratch of the forward), of the workspaces
- * (the forward's is optional, as entmax_attn_fwd's), and of the element lists
+ * (the forward's is optional, as entmax_attn_fwd's; a backward uses its lists
+ * where its workspace has ws_bwd_lists bytes), and of the element lists
  * (optional, as in entmax_attn_fwd_lists, and as much a residual as the
  * others; 0 where max_seqlen is above 65536). */
 typedef struct {
-  size_t residuals, ws_fwd, ws_bwd, lists;
+  size_t residuals, ws_fwd, ws_bwd, lists, ws_bwd_lists;
 } ea_packed_sizes;
 typedef struct {
   ea_strides q, k, v, o;
@@ -404,7 +405,7 @@ ea_status entmax_packed_sizes(const ea_packed_shape* shape, const ea_params* par
  * are contiguous and of the inputs' dtype (each rounded once, from fp32 sums).
  * Rows that belong to no sequence (before cu[0], behind cu[seqs]) are left as
  * they are, or with zero_rest != 0 set to 0.  Launches: 2 (forward; the solver
- * one more per workspace slot count), 3 or 4 (backward).
+ * one more per workspace slot count), 3 or 4 (backward; with lists 4).
  */
 ea_status entmax_packed_fwd(const ea_packed_shape* shape, const ea_params* params, const void* plan,
                             const void* q, const void* k, const void* v, void* o,

@@ -772,7 +772,7 @@ class PackedShape(ctypes.Structure):
 
 
 class PackedSizes(ctypes.Structure):
-    _fields_ = [(f, ctypes.c_size_t) for f in ("residuals", "ws_fwd", "ws_bwd", "lists")]
+    _fields_ = [(f, ctypes.c_size_t) for f in ("residuals", "ws_fwd", "ws_bwd", "lists", "ws_bwd_lists")]
 
 
 class PackedStrides(ctypes.Structure):
@@ -1136,7 +1136,8 @@ def packed_backward(q, k, v, dout, res: PackedResiduals, dq=None, dk=None, dv=No
     inputs' dtype: [tokens, heads, d] and [tokens, kv_heads, d], contiguous.
     dout has any strides with a contiguous last dimension.  Rows of no sequence
     are 0 in gradients that the call makes; they are left as they are if dq, dk
-    and dv are given (all three or none)."""
+    and dv are given (all three or none).  workspace: a device buffer of at least
+    res.sizes.ws_bwd bytes (ws_bwd_lists, to use the element lists of res)."""
     if not isinstance(res, PackedResiduals):
         raise ValueError("res must be the residuals of a packed_forward call")
     shape = _packed_shape(q, k, v, res.plan)
@@ -1167,6 +1168,8 @@ def packed_backward(q, k, v, dout, res: PackedResiduals, dq=None, dk=None, dv=No
     with _on_device(q.device):
         if made:
             dq, dk, dv = (torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v))
+        if workspace is None and res.lists is not None:
+            workspace = _bytes_or_none(res.sizes.ws_bwd_lists, q.device)
         if workspace is None:
             workspace = torch.empty(res.sizes.ws_bwd, dtype=torch.uint8, device=q.device)
         _check(_lib.entmax_packed_bwd(

@@ -815,10 +815,29 @@ size_t packed_ws_fwd(const ea_packed_shape* s) {
   const int64_t tiles = (int64_t)s->heads * packed_tiles(s->tokens, s->seqs, 2);
   return (size_t)(tiles < MAX_SOLVE_SLOTS ? tiles : MAX_SOLVE_SLOTS) * SOLVE_SLOT_BYTES;
 }
-size_t packed_ws_bwd(const ea_packed_shape* s) {
+// The backward's workspace: delta, the parts of dK and dV where there are some
+// (with element lists always, and one more), and with lists their buckets.
+struct PackedBwdWs {
+  float *delta, *dk, *dv;
+  int32_t* wrote;
+  Buckets buckets;
+};
+size_t packed_ws_bwd(const ea_packed_shape* s, bool lists, void* base, PackedBwdWs* w) {
   const int parts = packed_parts(s);
-  const size_t sums = parts > 1 ? 2 * (size_t)parts * s->tokens * s->kv_heads * s->head_dim * 4 : 0;
-  return up256((size_t)s->heads * s->tokens * 4) + sums;
+  const size_t blocks = (size_t)s->heads * packed_tiles(s->tokens, s->seqs, 0);
+  const size_t sums = (size_t)(lists ? parts + 1 : parts > 1 ? parts : 0) * s->tokens * s->kv_heads * s->head_dim;
+  Parts p{static_cast<char*>(base)};
+  w->delta = p.take<float>((size_t)s->heads * s->tokens);
+  w->dk = p.take<float>(sums);
+  w->dv = p.take<float>(sums);
+  if (!lists) return p.at;
+  w->wrote = p.take<int32_t>((size_t)parts * blocks / s->heads * s->kv_heads);
+  w->buckets.used = p.take<int32_t>(blocks);
+  w->buckets.heads = p.take<int32_t>((size_t)s->heads * s->seqs);
+  w->buckets.off = p.take<uint16_t>(blocks * (((size_t)s->max_seqlen + 63) / 64 + 1));
+  w->buckets.z = p.take<float>(blocks * LIST_ENTRIES);
+  w->buckets.code = p.take<uint16_t>(blocks * LIST_ENTRIES);
+  return p.at;
 }
 
 // A tile copy's offsets are 32-bit numbers of elements.
@@ -900,8 +919,10 @@ ea_status entmax_packed_sizes(const ea_packed_shape* shape, const ea_params* par
   PackedResiduals r;
   out->residuals = residual_parts(shape, params, nullptr, &r);
   out->ws_fwd = packed_ws_fwd(shape);
-  out->ws_bwd = packed_ws_bwd(shape);
   out->lists = packed_lists_bytes(shape);
+  PackedBwdWs w;
+  out->ws_bwd = packed_ws_bwd(shape, false, nullptr, &w);
+  out->ws_bwd_lists = out->lists ? packed_ws_bwd(shape, true, nullptr, &w) : out->ws_bwd;
   return EA_OK;
 }
 
@@ -980,23 +1001,28 @@ ea_status entmax_packed_bwd(const ea_packed_shape* shape, const ea_params* param
   if (st != EA_OK) return st;
   if (!params->need_bwd || !tensor_ok(dq) || !tensor_ok(dk) || !tensor_ok(dv) || !tensor_ok(workspace))
     return EA_ERR_INVALID_ARG;
-  if (ws_bytes < packed_ws_bwd(shape)) return EA_ERR_WORKSPACE;
   if ((st = check_packed_lists(shape, lists, lists_bytes)) != EA_OK) return st;
+  PackedBwdWs w{};
+  if (lists && ws_bytes < packed_ws_bwd(shape, true, workspace, &w)) lists = nullptr;  // no room to sort them
+  if (!lists && ws_bytes < packed_ws_bwd(shape, false, workspace, &w)) return EA_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);
   Packed<DeltaArgs> da{};
   da.pk = packed_args(shape, plan, strides, zero_rest);
   da.dout = dout;
   da.o2 = r.o2;
-  da.delta = static_cast<float*>(workspace);
+  da.delta = w.delta;
+  if (lists) {
+    da.lists = static_cast<const ListBlock*>(lists);
+    da.use = packed_lists_use(shape, lists);
+    da.buckets = w.buckets;
+  }
   da.rows = (int64_t)shape->heads * shape->tokens;
   if ((st = from_hip(launch_delta_packed(da, shape->dtype, shape->head_dim, s))) != EA_OK) return st;
   Packed<BwdArgs> ba{};
   ba.pk = da.pk;
   ba.pk.parts = packed_parts(shape);
-  if (ba.pk.parts > 1) {
-    ba.pk.dk_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + up256((size_t)da.rows * 4));
-    ba.pk.dv_part = ba.pk.dk_part + (size_t)ba.pk.parts * shape->tokens * shape->kv_heads * shape->head_dim;
-  }
+  ba.pk.dk_part = w.dk;
+  ba.pk.dv_part = w.dv;
   ba.q = q;
   ba.k = k;
   ba.v = v;
@@ -1019,8 +1045,10 @@ ea_status entmax_packed_bwd(const ea_packed_shape* shape, const ea_params* param
   ba.c64 = c64_of(params);
   ba.g64 = g64_of(params);
   if (lists) {
-    ba.lists = static_cast<const ListBlock*>(lists);
-    ba.buckets.used = packed_lists_use(shape, lists);
+    ba.lists = da.lists;
+    ba.buckets = w.buckets;
+    ba.pk.use = da.use;
+    ba.pk.wrote = w.wrote;
   }
   if ((st = from_hip(launch_bwd_dkdv_packed(ba, shape->dtype, shape->head_dim, s))) != EA_OK) return st;
   return from_hip(launch_bwd_dq_packed(ba, shape->dtype, shape->head_dim, s));

@@ -100,12 +100,119 @@ static_assert(PREP_SMALL <= (PREP_NT / 64) * PREP_T && PREP_SMALL >= PREP_T, "a 
 // Buckets::used: the block's lists are good (for dQ), and sorted (for dK, dV)
 constexpr int LISTED = 1, SORTED = 2;
 
+// The entries of a query block's lists sorted by key block, T of them: bucket J
+// at off[J] (off: [T + 1]), z and code (row and key within their blocks).  A
+// counting sort: each wave takes 32 of the 128 lists, counts its entries per
+// key block, and places them after those of the waves before.  Every thread of
+// the workgroup; `cursor` is scratch.
+__device__ __forceinline__ void sort_lists(const ListBlock& lb, int T, uint32_t (*cursor)[PREP_T], uint16_t* off,
+                                           float* zg, uint16_t* cg) {
+  constexpr int W = PREP_NT / 64;
+  __shared__ float zs[PREP_STAGE];
+  __shared__ uint16_t cs[PREP_STAGE];
+  __shared__ uint32_t wsum[W];
+  const int t = threadIdx.x, lane = lane_id(), w = wave_id();
+  const int bits = 32 - __clz(max(T - 1, 1));
+  for (int x = t; x < W * T; x += PREP_NT) cursor[x / T][x % T] = 0;
+  const int id = 32 * w + (lane & 31), half = lane >> 5, cnt = lb.count[id];
+  int most = cnt;  // longest list of the wave
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) most = max(most, __shfl_xor(most, o));
+  // Lanes below 32 take the even entries of their list, the others the odd;
+  // loads in batches of eight entries per lane.
+  constexpr int B = 8;
+  auto keys = [&](int e0, int (&key)[B]) {
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      const int e = e0 + 2 * u + half;
+      key[u] = e < cnt ? (int)lb.key[LIST_IDS * e + id] : -1;
+    }
+  };
+  __syncthreads();
+  for (int e0 = 0; e0 < most; e0 += 2 * B) {
+    int key[B];
+    keys(e0, key);
+#pragma unroll
+    for (int u = 0; u < B; ++u)
+      if (key[u] >= 0) atomicAdd(&cursor[w][key[u] >> 6], 1u);
+  }
+  __syncthreads();
+  // exclusive sums in the order (key block, wave)
+  const int per = (T + PREP_NT - 1) / PREP_NT;
+  uint32_t mine = 0;
+  for (int k = 0; k < per; ++k) {
+    const int j = t * per + k;
+    if (j < T)
+      for (int x = 0; x < W; ++x) mine += cursor[x][j];
+  }
+  uint32_t incl = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t v = __shfl_up(incl, o);
+    if (lane >= o) incl += v;
+  }
+  if (lane == 63) wsum[w] = incl;
+  __syncthreads();
+  uint32_t start = incl - mine;
+  for (int x = 0; x < w; ++x) start += wsum[x];
+  const uint32_t total = wsum[0] + wsum[1] + wsum[2] + wsum[3];
+  for (int k = 0; k < per; ++k) {
+    const int j = t * per + k;
+    if (j < T) {
+      off[j] = (uint16_t)start;
+      for (int x = 0; x < W; ++x) {
+        const uint32_t v = cursor[x][j];
+        cursor[x][j] = start;
+        start += v;
+      }
+    }
+  }
+  if (t == 0) off[T] = (uint16_t)total;
+  __syncthreads();
+  const bool staged = total <= PREP_STAGE;
+  for (int e0 = 0; e0 < most; e0 += 2 * B) {
+    int key[B];
+    float z[B];
+    keys(e0, key);
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      const int e = e0 + 2 * u + half;
+      z[u] = e < cnt ? lb.z[LIST_IDS * e + id] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      const bool ok = key[u] >= 0;
+      const unsigned long long act = __ballot(ok);
+      if (act == 0ull) break;
+      const int kb = key[u] >> 6;
+      const unsigned long long m = same_key(kb, bits, act);
+      if (ok) {
+        const int rank = lanes_below(m);
+        const uint32_t p = cursor[w][kb] + (uint32_t)rank;
+        if (rank == __popcll(m) - 1) cursor[w][kb] = p + 1;  // (all lanes have read it by then)
+        const uint16_t code = (uint16_t)((id & 63) * 64 + (key[u] & 63));
+        if (staged) {
+          zs[p] = z[u];
+          cs[p] = code;
+        } else {
+          zg[p] = z[u];
+          cg[p] = code;
+        }
+      }
+    }
+  }
+  if (!staged) return;
+  __syncthreads();
+  for (uint32_t p = t; p < total; p += PREP_NT) {
+    zg[p] = zs[p];
+    cg[p] = cs[p];
+  }
+}
+
 // One workgroup per 64-row query block: delta of its rows, and, where the
 // forward listed the block, its entries sorted by key block for the dK/dV
-// kernel (a counting sort: each wave takes 32 of the 128 lists, counts its
-// entries per key block, and places them after those of the waves before).
-// Entries of one key block keep the order of (wave, entry, list), so the sort
-// is deterministic.  The lists are used only if their thresholds are the
+// kernel.  Entries of one key block keep the order of (wave, entry, list), so
+// the sort is deterministic.  The lists are used only if their thresholds are the
 // residuals' (a forward that did not write lists may have filled the
 // residuals again).
 template <typename E, int D>
@@ -113,10 +220,7 @@ __global__ __launch_bounds__(PREP_NT) void prep_kernel(DeltaArgs a) {
   constexpr int PER = D / 16;  // 16 lanes per row
   constexpr int W = PREP_NT / 64;
   __shared__ uint32_t cursor[W][PREP_T];
-  __shared__ float zs[PREP_STAGE];
-  __shared__ uint16_t cs[PREP_STAGE];
-  __shared__ uint32_t wsum[W];
-  const int t = threadIdx.x, lane = lane_id(), w = wave_id();
+  const int t = threadIdx.x;
   const int bh = blockIdx.x / a.T, qb = blockIdx.x % a.T;
   const size_t blk = blockIdx.x;
   const int nr = min(BLK, a.n - qb * BLK);
@@ -178,104 +282,47 @@ __global__ __launch_bounds__(PREP_NT) void prep_kernel(DeltaArgs a) {
   if (t == 0) a.buckets.used[blk] = (use & LIST_DQ ? LISTED : 0) | (sorted ? SORTED : 0);
   if (!sorted) return;
 
-  const int bits = 32 - __clz(max(T - 1, 1));
-  for (int x = t; x < W * T; x += PREP_NT) cursor[x / T][x % T] = 0;
-  const int id = 32 * w + (lane & 31), half = lane >> 5, cnt = lb.count[id];
-  int most = cnt;  // longest list of the wave
+  sort_lists(lb, T, cursor, a.buckets.off + blk * (size_t)(T + 1), a.buckets.z + blk * LIST_ENTRIES,
+             a.buckets.code + blk * LIST_ENTRIES);
+}
+
+// Packed sequences: the same for a query block of one sequence.  The dK/dV
+// work of a head is split, sequence by sequence, under the same condition.
+template <typename E, int D>
+__global__ __launch_bounds__(PREP_NT) void prep_packed_kernel(Packed<DeltaArgs> a) {
+  constexpr int PER = D / 16;  // 16 lanes per row
+  __shared__ uint32_t cursor[PREP_NT / 64][PREP_T];
+  Place at;
+  if (!packed_place(a.pk, blockIdx.x, a.pk.heads, false, at)) return;
+  const int t = threadIdx.x, qb = at.tile, T = at.T;
+  const size_t blk = at.blk0 + qb;
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) most = max(most, __shfl_xor(most, o));
-  // Lanes below 32 take the even entries of their list, the others the odd;
-  // loads in batches of eight entries per lane.
-  constexpr int B = 8;
-  auto keys = [&](int e0, int (&key)[B]) {
+  for (int r = t >> 4; r < BLK; r += PREP_NT / 16) {
+    const int i = qb * BLK + r;
+    float acc = 0.f;
+    if (i < at.n) {
+      const E* dO = static_cast<const E*>(a.dout) + (int64_t)(at.start + i) * a.pk.o.row + at.head * a.pk.o.head +
+                    (t & 15) * PER;
+      const float* o2 = a.o2 + (at.row0 + i) * D + (t & 15) * PER;
 #pragma unroll
-    for (int u = 0; u < B; ++u) {
-      const int e = e0 + 2 * u + half;
-      key[u] = e < cnt ? (int)lb.key[LIST_IDS * e + id] : -1;
-    }
-  };
-  __syncthreads();
-  for (int e0 = 0; e0 < most; e0 += 2 * B) {
-    int key[B];
-    keys(e0, key);
-#pragma unroll
-    for (int u = 0; u < B; ++u)
-      if (key[u] >= 0) atomicAdd(&cursor[w][key[u] >> 6], 1u);
-  }
-  __syncthreads();
-  // exclusive sums in the order (key block, wave)
-  uint16_t* const off = a.buckets.off + blk * (size_t)(T + 1);
-  const int per = (T + PREP_NT - 1) / PREP_NT;
-  uint32_t mine = 0;
-  for (int k = 0; k < per; ++k) {
-    const int j = t * per + k;
-    if (j < T)
-      for (int x = 0; x < W; ++x) mine += cursor[x][j];
-  }
-  uint32_t incl = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t v = __shfl_up(incl, o);
-    if (lane >= o) incl += v;
-  }
-  if (lane == 63) wsum[w] = incl;
-  __syncthreads();
-  uint32_t start = incl - mine;
-  for (int x = 0; x < w; ++x) start += wsum[x];
-  const uint32_t total = wsum[0] + wsum[1] + wsum[2] + wsum[3];
-  for (int k = 0; k < per; ++k) {
-    const int j = t * per + k;
-    if (j < T) {
-      off[j] = (uint16_t)start;
-      for (int x = 0; x < W; ++x) {
-        const uint32_t v = cursor[x][j];
-        cursor[x][j] = start;
-        start += v;
-      }
-    }
-  }
-  if (t == 0) off[T] = (uint16_t)total;
-  __syncthreads();
-  float* const zg = a.buckets.z + blk * LIST_ENTRIES;
-  uint16_t* const cg = a.buckets.code + blk * LIST_ENTRIES;
-  const bool staged = total <= PREP_STAGE;
-  for (int e0 = 0; e0 < most; e0 += 2 * B) {
-    int key[B];
-    float z[B];
-    keys(e0, key);
-#pragma unroll
-    for (int u = 0; u < B; ++u) {
-      const int e = e0 + 2 * u + half;
-      z[u] = e < cnt ? lb.z[LIST_IDS * e + id] : 0.f;
+      for (int e = 0; e < PER; ++e) acc = fmaf((float)dO[e], o2[e], acc);
     }
 #pragma unroll
-    for (int u = 0; u < B; ++u) {
-      const bool ok = key[u] >= 0;
-      const unsigned long long act = __ballot(ok);
-      if (act == 0ull) break;
-      const int kb = key[u] >> 6;
-      const unsigned long long m = same_key(kb, bits, act);
-      if (ok) {
-        const int rank = lanes_below(m);
-        const uint32_t p = cursor[w][kb] + (uint32_t)rank;
-        if (rank == __popcll(m) - 1) cursor[w][kb] = p + 1;  // (all lanes have read it by then)
-        const uint16_t code = (uint16_t)((id & 63) * 64 + (key[u] & 63));
-        if (staged) {
-          zs[p] = z[u];
-          cs[p] = code;
-        } else {
-          zg[p] = z[u];
-          cg[p] = code;
-        }
-      }
-    }
+    for (int m = 8; m >= 1; m >>= 1) acc += __shfl_xor(acc, m);
+    if (i < at.n && (t & 15) == 0) a.delta[at.row0 + i] = acc;
   }
-  if (!staged) return;
-  __syncthreads();
-  for (uint32_t p = t; p < total; p += PREP_NT) {
-    zg[p] = zs[p];
-    cg[p] = cs[p];
+  int listed = 0;
+  for (int x0 = 0; x0 < T; x0 += PREP_NT) {
+    const int x = x0 + t;
+    listed += __syncthreads_count(x < T && (a.use[at.blk0 + min(x, T - 1)] & LIST_DKDV) != 0);
   }
+  const bool split = (sizeof(E) == 2 ? 8 : 4) * (T - listed) <= T;
+  if (qb == 0 && t == 0) a.buckets.heads[(size_t)at.head * a.pk.seq_count + at.seq] = split ? listed : 0;
+  const bool sorted = split && (a.use[blk] & LIST_DKDV);
+  if (t == 0) a.buckets.used[blk] = sorted ? SORTED : 0;
+  if (!sorted) return;
+  sort_lists(a.lists[blk], T, cursor, a.buckets.off + blk * (size_t)(a.pk.width + 1), a.buckets.z + blk * LIST_ENTRIES,
+             a.buckets.code + blk * LIST_ENTRIES);
 }
 
 // ------------------------------- element lists from the thresholds alone
@@ -564,15 +611,20 @@ template <typename E, int D>
 __device__ __forceinline__ void store_packed(const PackedArgs& pk, const Place& at, float* out, float* part,
                                              int row, int col, float x) {
   const int64_t off = ((int64_t)(at.start + row) * pk.kv_heads + at.head) * D + col;
-  if (pk.parts > 1)
+  if (pk.parts > 1 || pk.wrote)
     part[(int64_t)at.part * pk.tokens * pk.kv_heads * D + off] = x;
   else
     reinterpret_cast<E*>(out)[off] = (E)x;
 }
-// dK and dV rows of no sequence (where they are not reduced from parts).
+// Whether this workgroup has sums for key block kb (with element lists).
+__device__ __forceinline__ void mark_part(const PackedArgs& pk, const Place& at, int kb, bool any) {
+  if (threadIdx.x == 0 && kb < at.T)
+    pk.wrote[((size_t)at.part * pk.kv_heads + at.head) * pk.blocks + at.block + kb] = any;
+}
+// dK and dV rows of no sequence (called where the gradients themselves are written).
 template <typename E, int D, int NT, typename A>
 __device__ __forceinline__ void zero_rest_dkdv(const A& a, const Place& at) {
-  if (at.item != 0 || !a.pk.zero_rest || a.pk.parts > 1) return;
+  if (at.item != 0 || !a.pk.zero_rest) return;
   const Strides rows{a.pk.kv_heads * D, D};
   zero_rest<E, D, NT>(a.pk, reinterpret_cast<E*>(a.dk), rows, at.head);
   zero_rest<E, D, NT>(a.pk, reinterpret_cast<E*>(a.dv), rows, at.head);
@@ -598,7 +650,7 @@ __global__ __launch_bounds__(BWD_NT) void dkdv_kernel(A a) {
   [[maybe_unused]] KeyHead kh{};
   if constexpr (PK) {
     const bool work = packed_place(a.pk, blockIdx.x, a.pk.kv_heads * a.pk.parts, true, at);
-    zero_rest_dkdv<E, D, BWD_NT>(a, at);
+    if (a.pk.parts == 1 && !a.pk.wrote) zero_rest_dkdv<E, D, BWD_NT>(a, at);
     if (!work) return;
     kh = key_head(a.pk, at, a.causal);
   }
@@ -645,11 +697,23 @@ __global__ __launch_bounds__(BWD_NT) void dkdv_kernel(A a) {
   const bool dense = !PK && a.k_index == nullptr;
   const int32_t* list = dense ? nullptr : a.k_index + blk * width;
   int cnt = dense ? (a.causal ? T - kb : T) : a.k_count[blk];
-  __shared__ uint16_t unlisted[PK ? 1 : LIST_MAX_SEQLEN / BLK];
+  __shared__ uint16_t unlisted[LIST_MAX_SEQLEN / BLK];
   const int sorted = !PK && a.lists ? sorted_blocks<BWD_NT>(a.buckets, bh, T) : 0;
   if (!PK && a.lists && sorted == T) return;
-  const bool some = !PK && sorted > 0;
-  if (some) {
+  bool some = !PK && sorted > 0;
+  [[maybe_unused]] bool any = false;
+  // (the packed form, of query head bh: its blocks without lists, if some of its blocks have)
+  [[maybe_unused]] auto without_lists = [&]() {
+    if constexpr (PK) {
+      if (a.lists) {
+        some = ((const ci32*)a.buckets.heads)[(size_t)bh * a.pk.seq_count + at.seq] != 0;
+        if (some) cnt = unlisted_blocks<BWD_NT>(list, 0, cnt, a.buckets.used + (blk - kb), unlisted);
+      }
+      any |= cnt > 0;
+    }
+  };
+  without_lists();
+  if (!PK && some) {
     cnt = unlisted_blocks<BWD_NT>(list, a.causal ? kb : 0, cnt, a.buckets.used + (size_t)bh * T, unlisted);
     if (cnt == 0) return;
   }
@@ -780,11 +844,19 @@ __global__ __launch_bounds__(BWD_NT) void dkdv_kernel(A a) {
       delg = a.delta + row0;
       list = a.k_index + blk * width;
       cnt = a.k_count[blk];
+      ++bh;
+      without_lists();
     } else {
       break;
     }
   }
 
+  if constexpr (PK) {
+    if (a.lists) {
+      mark_part(a.pk, at, kb, any);
+      if (!any) return;
+    }
+  }
   if (!wave_ok) return;
   if constexpr (PK) {
 #pragma unroll
@@ -863,7 +935,7 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(A a) {
   [[maybe_unused]] KeyHead khead{};
   if constexpr (PK) {
     const bool work = packed_place(a.pk, blockIdx.x, a.pk.kv_heads * a.pk.parts, true, at);
-    zero_rest_dkdv<E, D, BWD2_NT>(a, at);
+    if (a.pk.parts == 1 && !a.pk.wrote) zero_rest_dkdv<E, D, BWD2_NT>(a, at);
     if (!work) return;
     khead = key_head(a.pk, at, a.causal);
   }
@@ -923,7 +995,26 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(A a) {
   };
   int nA = count_of(kbA), nB = count_of(kbB);
   int pA = 0, pB = 0;
-  int hn = 0;  // query head of the next entry, after the first (packed forms)
+  // packed forms: query head of the next entry, after the first, and (with
+  // element lists) masks of the current chunks
+  int hn = 0;
+  [[maybe_unused]] unsigned long long mA = 0, mB = 0;
+  [[maybe_unused]] bool any = false;
+  [[maybe_unused]] auto chunk = [&](int kb, int e0, int cnt) {
+    const int e = min(e0 + lane, cnt - 1);
+    const int qb = a.k_index[(blk0 + kb) * width + e];
+    return __ballot(e0 + lane < cnt && !(a.buckets.used[blk0 + qb] & SORTED));
+  };
+  // the lists of the head that begins (nothing is left of a head all of whose blocks are sorted)
+  [[maybe_unused]] auto begin_head = [&]() {
+    if constexpr (PK) {
+      nA = count_of(kbA);
+      nB = count_of(kbB);
+      pA = pB = 0;
+      if (a.lists && ((const ci32*)a.buckets.heads)[(size_t)(bh + hn) * a.pk.seq_count + at.seq] == T) nA = nB = 0;
+    }
+  };
+  begin_head();
   // With element lists, only the query blocks without them (see dkdv_kernel).
   if (some) {
     const int32_t* used = a.buckets.used + (size_t)bh * T;
@@ -939,14 +1030,32 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(A a) {
   // the next query block of the union, and whether each key block lists it
   auto next = [&](auto left, int& h, int& qb, bool& inA, bool& inB) {
     if constexpr (PK) {
-      while (pA >= nA && pB >= nB) {
+      // With element lists, entries in chunks of 64, as masks of those whose
+      // query blocks have no lists (one vector load a chunk).
+      for (;;) {
+        if (a.lists) {
+          for (; mA == 0 && pA < nA; pA += 64) mA = chunk(kbA, pA, nA);
+          for (; mB == 0 && pB < nB; pB += 64) mB = chunk(kbB, pB, nB);
+          if (mA | mB) break;
+        } else if (pA < nA || pB < nB) {
+          break;
+        }
         if (++hn >= khead.count) return false;
         blk0 += a.pk.blocks;
-        nA = count_of(kbA);
-        nB = count_of(kbB);
-        pA = pB = 0;
+        begin_head();
       }
       h = hn;
+      if (a.lists) {
+        const int hA = mA ? entry_of(left, kbA, pA - 64 + __builtin_ctzll(mA)) : T;
+        const int hB = mB ? entry_of(left, kbB, pB - 64 + __builtin_ctzll(mB)) : T;
+        qb = min(hA, hB);
+        inA = hA == qb;
+        inB = hB == qb;
+        if (inA) mA &= mA - 1;
+        if (inB) mB &= mB - 1;
+        any = true;
+        return true;
+      }
     }
     const int hA = pA < nA ? entry_of(left, kbA, pA) : T;
     const int hB = pB < nB ? entry_of(left, kbB, pB) : T;
@@ -1140,6 +1249,13 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(A a) {
   else
     run(std::false_type{});
 
+  if constexpr (PK) {
+    if (a.lists) {
+      mark_part(a.pk, at, kbA, any);
+      mark_part(a.pk, at, kbB, any);
+      if (!any) return;
+    }
+  }
   if (!wave_ok) return;
   if constexpr (PK) {
 #pragma unroll
@@ -1187,8 +1303,12 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(A a) {
 constexpr int LK_NT = 256;
 constexpr int LK_CHUNK = 2048;
 
-template <typename E, int D, int GK>
-__global__ __launch_bounds__(LK_NT, 2) void dkdv_lists_kernel(BwdArgs a) {
+// A = Packed<BwdArgs>: the query heads of a key head one after another, into
+// the last part; then the sum of all parts, in the inputs' type, is the
+// gradient.
+template <typename E, int D, int GK, typename A>
+__global__ __launch_bounds__(LK_NT, 2) void dkdv_lists_kernel(A a) {
+  constexpr bool PK = is_packed<A>::value;
   using R = RowGroup<E, D>;
   constexpr int VPL = R::VPL, LPR = R::LPR, NG = LK_NT / LPR, W = LK_NT / 64;
   __shared__ uint32_t code[LK_CHUNK];   // (query row << 6) | key
@@ -1202,266 +1322,351 @@ __global__ __launch_bounds__(LK_NT, 2) void dkdv_lists_kernel(BwdArgs a) {
   __shared__ __attribute__((aligned(16))) u32x4 vt[BLK * LPR];        // rows of V
   __shared__ __attribute__((aligned(16))) float part[NG][2 * D];      // dV, dK of a share's leading key
   const int t = threadIdx.x, lane = lane_id(), w = wave_id(), sub = lane % LPR, grp = t / LPR;
-  const int n = a.n, T = a.T;
-  int bh, kb;
-  head_major(blockIdx.x, a.BH, T, bh, kb);
-  const size_t head = (size_t)bh * n * D;
-  const E* Q = static_cast<const E*>(a.q) + head;
-  const E* V = static_cast<const E*>(a.v) + head;
-  const E* dO = static_cast<const E*>(a.dout) + head;
-  const float* del = a.delta + (size_t)bh * n;
+  [[maybe_unused]] Place place;
+  [[maybe_unused]] KeyHead khead{};
+  if constexpr (PK) {
+    const bool work = packed_place(a.pk, blockIdx.x, a.pk.kv_heads, true, place);
+    zero_rest_dkdv<E, D, LK_NT>(a, place);
+    if (!work) return;
+    khead = {place.head * a.pk.group, a.pk.group, a.causal ? place.T - 1 - place.tile : place.tile};
+  }
+  const int n = PK ? place.n : a.n, T = PK ? place.T : a.T;
+  int bh, kb, width = T;
+  if constexpr (PK) {
+    bh = khead.first;
+    kb = khead.kb;
+    width = a.pk.width;
+  } else {
+    head_major(blockIdx.x, a.BH, T, bh, kb);
+  }
+  size_t row0 = (size_t)bh * n, blk0 = (size_t)bh * T;
+  int ldq = D, ldo = D, ldv = D, ldg = D;  // (ldg: of dK and dV)
+  const size_t head = row0 * D;
+  const E* Q = static_cast<const E*>(a.q);
+  const E* V = static_cast<const E*>(a.v);
+  const E* dO = static_cast<const E*>(a.dout);
+  float *dK = a.dk, *dV = a.dv;
+  if constexpr (PK) {
+    ldq = a.pk.q.row;
+    ldo = a.pk.o.row;
+    ldv = a.pk.v.row;
+    ldg = a.pk.kv_heads * D;
+    row0 = (size_t)bh * a.pk.tokens + place.start;
+    blk0 = (size_t)bh * a.pk.blocks + place.block;
+    Q += (int64_t)place.start * ldq + bh * a.pk.q.head;
+    V += (int64_t)place.start * ldv + place.head * a.pk.v.head;
+    dO += (int64_t)place.start * ldo + bh * a.pk.o.head;
+    const int64_t at = ((int64_t)a.pk.parts * a.pk.tokens + place.start) * ldg + place.head * D;
+    dK = a.pk.dk_part + at;
+    dV = a.pk.dv_part + at;
+  } else {
+    Q += head;
+    V += head;
+    dO += head;
+    dK += head;
+    dV += head;
+  }
+  auto load = [&](const E* base, uint32_t row, int ld) { return PK ? R::load(base, row, ld) : R::load(base, row); };
+  const float* del = a.delta + row0;
   const int k0 = kb * BLK;
-  const bool dense = a.k_index == nullptr;  // no tables: every valid query block
-  const int32_t* list = dense ? nullptr : a.k_index + ((size_t)bh * T + kb) * T;
-  const int cnt = dense ? (a.causal ? T - kb : T) : a.k_count[(size_t)bh * T + kb];
+  const bool dense = !PK && a.k_index == nullptr;  // no tables: every valid query block
+  const int32_t* list = dense ? nullptr : a.k_index + (blk0 + kb) * width;
+  int cnt = dense ? (a.causal ? T - kb : T) : a.k_count[blk0 + kb];
   auto qb_of = [&](int e) { return dense ? (a.causal ? kb + e : e) : list[e]; };
-  const int32_t* used = a.buckets.used + (size_t)bh * T;
+  const int32_t* used = a.buckets.used + blk0;
 
-  const int sorted = sorted_blocks<LK_NT>(a.buckets, bh, T);
-  if (sorted == 0) return;
+  int sorted = 0;
+  if constexpr (!PK) {
+    sorted = sorted_blocks<LK_NT>(a.buckets, bh, T);
+    if (sorted == 0) return;
+  }
   // whether the other dK/dV kernel wrote this key block (some query block of
   // its list is not sorted): the first round then adds to it as the later
   // ones do
   bool add = false;
-  if (sorted < T) {
+  if (!PK && sorted < T) {
     bool other = false;
     for (int e = t; e < cnt; e += LK_NT) other |= !(used[qb_of(e)] & SORTED);
     add = __syncthreads_or(other);
   }
 #pragma unroll
-  for (int r = grp; r < BLK; r += NG) vt[r * LPR + sub] = R::load(V, (uint32_t)min(k0 + r, n - 1));
+  for (int r = grp; r < BLK; r += NG) vt[r * LPR + sub] = load(V, (uint32_t)min(k0 + r, n - 1), ldv);
 
   // dK and dV of key kl, this lane's columns
   auto put = [&](int kl, const float (&dv)[VPL], const float (&dk)[VPL]) {
     if (k0 + kl >= n) return;
-    const size_t at = head + (size_t)(k0 + kl) * D + sub * VPL;
+    const size_t at = (size_t)(k0 + kl) * (PK ? ldg : D) + sub * VPL;
 #pragma unroll
     for (int d = 0; d < VPL; d += 4) {
       f32x4 x = {dv[d], dv[d + 1], dv[d + 2], dv[d + 3]};
       f32x4 y = {a.scale * dk[d], a.scale * dk[d + 1], a.scale * dk[d + 2], a.scale * dk[d + 3]};
       if (add) {
-        x += *reinterpret_cast<const f32x4*>(a.dv + at + d);
-        y += *reinterpret_cast<const f32x4*>(a.dk + at + d);
+        x += *reinterpret_cast<const f32x4*>(dV + at + d);
+        y += *reinterpret_cast<const f32x4*>(dK + at + d);
       }
-      *reinterpret_cast<f32x4*>(a.dv + at + d) = x;
-      *reinterpret_cast<f32x4*>(a.dk + at + d) = y;
+      *reinterpret_cast<f32x4*>(dV + at + d) = x;
+      *reinterpret_cast<f32x4*>(dK + at + d) = y;
     }
   };
 
-  int e0 = 0;
-  do {
-    // The runs of this batch: query block, place in its buckets, length, and
-    // (run_at) the sum of the lengths before it.
-    const int e = e0 + t;
-    int qb = 0, from = 0, num = 0;
-    if (e < cnt) {
-      qb = qb_of(e);
-      if (used[qb] & SORTED) {
-        const uint16_t* off = a.buckets.off + ((size_t)bh * T + qb) * (size_t)(T + 1) + kb;
-        from = off[0];
-        num = off[1] - from;
-      }
-    }
-    int incl = num;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(incl, o);
-      if (lane >= o) incl += v;
-    }
-    __syncthreads();  // wsum and the runs of the batch before have been read
-    if (lane == 63) wsum[w] = incl;
-    __syncthreads();
-    int at = incl - num, total = 0;
-#pragma unroll
-    for (int x = 0; x < W; ++x) {
-      if (x < w) at += wsum[x];
-      total += wsum[x];
-    }
-    run_qb[t] = (uint16_t)qb;
-    run_from[t] = (uint16_t)from;
-    run_num[t] = (uint16_t)num;
-    run_at[t] = at;
-    __syncthreads();
-    // tp threads (a power of two) copy one run
-    const int runs = max(min(cnt - e0, LK_NT), 1);
-    int tp = 1;
-    while (2 * tp * runs <= LK_NT) tp *= 2;
-    const int run = t / tp;
-    int c0 = 0;  // entries [c0, c0 + LK_CHUNK) of the batch in this round
-    do {
-      const int M = min(total - c0, LK_CHUNK);
-      if (run < runs) {
-        const int rq = run_qb[run], ra = run_at[run], rn = min((int)run_num[run], c0 + LK_CHUNK - ra);
-        const size_t src = ((size_t)bh * T + rq) * LIST_ENTRIES + run_from[run];
-        constexpr int B = 4;
-        for (int x0 = max(0, c0 - ra) + t % tp; x0 < rn; x0 += B * tp) {
-          int cd[B];
-          float z[B];
-#pragma unroll
-          for (int u = 0; u < B; ++u) {
-            const int x = min(x0 + u * tp, rn - 1);
-            cd[u] = a.buckets.code[src + x];
-            z[u] = a.buckets.z[src + x];
-          }
-#pragma unroll
-          for (int u = 0; u < B; ++u) {
-            const int x = x0 + u * tp;
-            if (x < rn) {
-              code[ra + x - c0] = ((uint32_t)(rq * BLK + (cd[u] >> 6)) << 6) | (uint32_t)(cd[u] & 63);
-              zv[ra + x - c0] = z[u];
-            }
+  for (int x = 0;;) {
+    // (the packed form: query heads some of whose blocks are sorted)
+    bool work = true;
+    if constexpr (PK) work = ((const ci32*)a.buckets.heads)[(size_t)bh * a.pk.seq_count + place.seq] != 0;
+    if (work) {
+      int e0 = 0;
+      do {
+        // The runs of this batch: query block, place in its buckets, length, and
+        // (run_at) the sum of the lengths before it.
+        const int e = e0 + t;
+        int qb = 0, from = 0, num = 0;
+        if (e < cnt) {
+          qb = qb_of(e);
+          if (used[qb] & SORTED) {
+            const uint16_t* off = a.buckets.off + (blk0 + qb) * (size_t)(width + 1) + kb;
+            from = off[0];
+            num = off[1] - from;
           }
         }
-      }
-      (&cursor[0][0])[t] = 0;  // W * BLK = LK_NT counters
-      __syncthreads();
-      // sort by key: wave w takes entries [w * q, (w + 1) * q)
-      const int q = (M + W - 1) / W, b0 = w * q, b1 = min(M, b0 + q);
-      for (int x = b0 + lane; x < b1; x += 64) atomicAdd(&cursor[w][code[x] & 63], 1);
-      __syncthreads();
-      if (w == 0) {
-        int s = 0;
-#pragma unroll
-        for (int x = 0; x < W; ++x) s += cursor[x][lane];
-        int in = s;
+        int incl = num;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
-          const int v = __shfl_up(in, o);
-          if (lane >= o) in += v;
+          const int v = __shfl_up(incl, o);
+          if (lane >= o) incl += v;
         }
-        int p = in - s;
-        kstart[lane] = p;
-        if (lane == 63) kstart[BLK] = in;
+        __syncthreads();  // wsum and the runs of the batch before have been read
+        if (lane == 63) wsum[w] = incl;
+        __syncthreads();
+        int at = incl - num, total = 0;
 #pragma unroll
         for (int x = 0; x < W; ++x) {
-          const int v = cursor[x][lane];
-          cursor[x][lane] = p;
-          p += v;
+          if (x < w) at += wsum[x];
+          total += wsum[x];
         }
-      }
-      __syncthreads();
-      for (int x = b0; x < b1; x += 64) {
-        const bool ok = x + lane < b1;
-        const int key = ok ? (int)(code[x + lane] & 63u) : 0;
-        const unsigned long long m = same_key(key, 6, __ballot(ok));
-        if (ok) {
-          const int rank = lanes_below(m);
-          const int p = cursor[w][key] + rank;
-          if (rank == __popcll(m) - 1) cursor[w][key] = p + 1;
-          order[p] = (uint16_t)(x + lane);
-        }
-      }
-      __syncthreads();
-
-      // this group's share of the sorted entries
-      const int share = (M + NG - 1) / NG;
-      const int s0 = grp * share, s1 = min(M, s0 + share);
-      float dv[VPL] = {}, dk[VPL] = {};
-      int cur = -1;          // the key being added up
-      bool lead = false;     // it started in an earlier share
-      bool owe = false;      // after the loop: `cur` is this group's, unfinished
-      auto post_part = [&]() {
+        run_qb[t] = (uint16_t)qb;
+        run_from[t] = (uint16_t)from;
+        run_num[t] = (uint16_t)num;
+        run_at[t] = at;
+        __syncthreads();
+        // tp threads (a power of two) copy one run
+        const int runs = max(min(cnt - e0, LK_NT), 1);
+        int tp = 1;
+        while (2 * tp * runs <= LK_NT) tp *= 2;
+        const int run = t / tp;
+        int c0 = 0;  // entries [c0, c0 + LK_CHUNK) of the batch in this round
+        do {
+          const int M = min(total - c0, LK_CHUNK);
+          if (run < runs) {
+            const int rq = run_qb[run], ra = run_at[run], rn = min((int)run_num[run], c0 + LK_CHUNK - ra);
+            const size_t src = (blk0 + rq) * LIST_ENTRIES + run_from[run];
+            constexpr int B = 4;
+            for (int x0 = max(0, c0 - ra) + t % tp; x0 < rn; x0 += B * tp) {
+              int cd[B];
+              float z[B];
 #pragma unroll
-        for (int d = 0; d < VPL; ++d) {
-          part[grp][sub * VPL + d] = dv[d];
-          part[grp][D + sub * VPL + d] = dk[d];
-        }
-      };
-      // batches of U entries, the next one's rows in flight meanwhile (past
-      // the end of the share its last entry again)
-      constexpr int U = 4;
-      u32x4 ow[U], qw[U];
-      uint32_t cd[U];
-      float z[U], dl[U];
-      auto fetch = [&](int p0) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int o = (int)order[max(min(p0 + u, s1 - 1), 0)];
-          cd[u] = code[o];
-          z[u] = zv[o];
-          ow[u] = R::load(dO, cd[u] >> 6);
-          qw[u] = R::load(Q, cd[u] >> 6);
-          dl[u] = del[cd[u] >> 6];
-        }
-      };
-      if (M > 0) fetch(s0);
-      for (int p0 = s0; __ballot(p0 < s1) != 0ull; p0 += U) {
-        u32x4 ow0[U], qw0[U];
-        uint32_t cd0[U];
-        float z0[U], dl0[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          ow0[u] = ow[u];
-          qw0[u] = qw[u];
-          cd0[u] = cd[u];
-          z0[u] = z[u];
-          dl0[u] = dl[u];
-        }
-        fetch(p0 + U);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          if (p0 + u < s1) {
-            const int kl = (int)(cd0[u] & 63u);
-            if (kl != cur) {
-              if (cur >= 0) {
-                if (lead)
-                  post_part();
-                else
-                  put(cur, dv, dk);
+              for (int u = 0; u < B; ++u) {
+                const int x = min(x0 + u * tp, rn - 1);
+                cd[u] = a.buckets.code[src + x];
+                z[u] = a.buckets.z[src + x];
               }
-              cur = kl;
-              lead = kstart[kl] < s0;
 #pragma unroll
-              for (int d = 0; d < VPL; ++d) dv[d] = dk[d] = 0.f;
+              for (int u = 0; u < B; ++u) {
+                const int x = x0 + u * tp;
+                if (x < rn) {
+                  code[ra + x - c0] = ((uint32_t)(rq * BLK + (cd[u] >> 6)) << 6) | (uint32_t)(cd[u] & 63);
+                  zv[ra + x - c0] = z[u];
+                }
+              }
             }
-            float x[VPL], y[VPL];
-            R::unpack(ow0[u], x);
-            R::unpack(vt[kl * LPR + sub], y);
-            float dp = 0.f, pp, uu;
+          }
+          (&cursor[0][0])[t] = 0;  // W * BLK = LK_NT counters
+          __syncthreads();
+          // sort by key: wave w takes entries [w * q, (w + 1) * q)
+          const int q = (M + W - 1) / W, b0 = w * q, b1 = min(M, b0 + q);
+          for (int x = b0 + lane; x < b1; x += 64) atomicAdd(&cursor[w][code[x] & 63], 1);
+          __syncthreads();
+          if (w == 0) {
+            int s = 0;
 #pragma unroll
-            for (int d = 0; d < VPL; ++d) dp = fmaf(x[d], y[d], dp);
-            dp = R::sum(dp);
-            Gamma<GK>::pu(z0[u], a.gamma, pp, uu);
-            const float ds = uu * (dp - dl0[u]);
-            R::unpack(qw0[u], y);
+            for (int x = 0; x < W; ++x) s += cursor[x][lane];
+            int in = s;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+              const int v = __shfl_up(in, o);
+              if (lane >= o) in += v;
+            }
+            int p = in - s;
+            kstart[lane] = p;
+            if (lane == 63) kstart[BLK] = in;
+#pragma unroll
+            for (int x = 0; x < W; ++x) {
+              const int v = cursor[x][lane];
+              cursor[x][lane] = p;
+              p += v;
+            }
+          }
+          __syncthreads();
+          for (int x = b0; x < b1; x += 64) {
+            const bool ok = x + lane < b1;
+            const int key = ok ? (int)(code[x + lane] & 63u) : 0;
+            const unsigned long long m = same_key(key, 6, __ballot(ok));
+            if (ok) {
+              const int rank = lanes_below(m);
+              const int p = cursor[w][key] + rank;
+              if (rank == __popcll(m) - 1) cursor[w][key] = p + 1;
+              order[p] = (uint16_t)(x + lane);
+            }
+          }
+          __syncthreads();
+
+          // this group's share of the sorted entries
+          const int share = (M + NG - 1) / NG;
+          const int s0 = grp * share, s1 = min(M, s0 + share);
+          float dv[VPL] = {}, dk[VPL] = {};
+          int cur = -1;          // the key being added up
+          bool lead = false;     // it started in an earlier share
+          bool owe = false;      // after the loop: `cur` is this group's, unfinished
+          auto post_part = [&]() {
 #pragma unroll
             for (int d = 0; d < VPL; ++d) {
-              dv[d] = fmaf(pp, x[d], dv[d]);
-              dk[d] = fmaf(ds, y[d], dk[d]);
+              part[grp][sub * VPL + d] = dv[d];
+              part[grp][D + sub * VPL + d] = dk[d];
+            }
+          };
+          // batches of U entries, the next one's rows in flight meanwhile (past
+          // the end of the share its last entry again)
+          constexpr int U = 4;
+          u32x4 ow[U], qw[U];
+          uint32_t cd[U];
+          float z[U], dl[U];
+          auto fetch = [&](int p0) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              const int o = (int)order[max(min(p0 + u, s1 - 1), 0)];
+              cd[u] = code[o];
+              z[u] = zv[o];
+              ow[u] = load(dO, cd[u] >> 6, ldo);
+              qw[u] = load(Q, cd[u] >> 6, ldq);
+              dl[u] = del[cd[u] >> 6];
+            }
+          };
+          if (M > 0) fetch(s0);
+          for (int p0 = s0; __ballot(p0 < s1) != 0ull; p0 += U) {
+            u32x4 ow0[U], qw0[U];
+            uint32_t cd0[U];
+            float z0[U], dl0[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              ow0[u] = ow[u];
+              qw0[u] = qw[u];
+              cd0[u] = cd[u];
+              z0[u] = z[u];
+              dl0[u] = dl[u];
+            }
+            fetch(p0 + U);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              if (p0 + u < s1) {
+                const int kl = (int)(cd0[u] & 63u);
+                if (kl != cur) {
+                  if (cur >= 0) {
+                    if (lead)
+                      post_part();
+                    else
+                      put(cur, dv, dk);
+                  }
+                  cur = kl;
+                  lead = kstart[kl] < s0;
+#pragma unroll
+                  for (int d = 0; d < VPL; ++d) dv[d] = dk[d] = 0.f;
+                }
+                float x[VPL], y[VPL];
+                R::unpack(ow0[u], x);
+                R::unpack(vt[kl * LPR + sub], y);
+                float dp = 0.f, pp, uu;
+#pragma unroll
+                for (int d = 0; d < VPL; ++d) dp = fmaf(x[d], y[d], dp);
+                dp = R::sum(dp);
+                Gamma<GK>::pu(z0[u], a.gamma, pp, uu);
+                const float ds = uu * (dp - dl0[u]);
+                R::unpack(qw0[u], y);
+#pragma unroll
+                for (int d = 0; d < VPL; ++d) {
+                  dv[d] = fmaf(pp, x[d], dv[d]);
+                  dk[d] = fmaf(ds, y[d], dk[d]);
+                }
+              }
             }
           }
-        }
-      }
-      if (cur >= 0) {
-        if (lead)
-          post_part();
-        else if (kstart[cur + 1] <= s1)
-          put(cur, dv, dk);
-        else
-          owe = true;
-      }
-      __syncthreads();
-      if (owe) {
-        for (int g = grp + 1; g * share < kstart[cur + 1]; ++g) {
-#pragma unroll
-          for (int d = 0; d < VPL; ++d) {
-            dv[d] += part[g][sub * VPL + d];
-            dk[d] += part[g][D + sub * VPL + d];
+          if (cur >= 0) {
+            if (lead)
+              post_part();
+            else if (kstart[cur + 1] <= s1)
+              put(cur, dv, dk);
+            else
+              owe = true;
           }
-        }
-        put(cur, dv, dk);
+          __syncthreads();
+          if (owe) {
+            for (int g = grp + 1; g * share < kstart[cur + 1]; ++g) {
+#pragma unroll
+              for (int d = 0; d < VPL; ++d) {
+                dv[d] += part[g][sub * VPL + d];
+                dk[d] += part[g][D + sub * VPL + d];
+              }
+            }
+            put(cur, dv, dk);
+          }
+          if (!add) {  // keys without entries
+            const float zero[VPL] = {};
+            for (int kl = grp; kl < BLK; kl += NG)
+              if (kstart[kl] == kstart[kl + 1]) put(kl, zero, zero);
+          }
+          add = true;
+          __syncthreads();
+          c0 += LK_CHUNK;
+        } while (c0 < total);
+        e0 += LK_NT;
+      } while (e0 < cnt);
+    }
+    if constexpr (PK) {
+      if (++x == khead.count) break;
+      ++bh;
+      blk0 += a.pk.blocks;
+      Q += a.pk.q.head;
+      dO += a.pk.o.head;
+      del += a.pk.tokens;
+      list = a.k_index + (blk0 + kb) * width;
+      cnt = a.k_count[blk0 + kb];
+      used = a.buckets.used + blk0;
+    } else {
+      break;
+    }
+  }
+  if constexpr (PK) {
+    __syncthreads();  // (the workgroup's sums are written)
+    const int64_t values = (int64_t)a.pk.tokens * ldg, first = ((int64_t)place.start + k0) * ldg + place.head * D;
+    for (int x = t; x < BLK * D / 4; x += LK_NT) {
+      const int row = x / (D / 4), col = x % (D / 4) * 4;
+      if (k0 + row >= n) continue;
+      const int64_t off = first + (int64_t)row * ldg + col;
+      f32x4 k4 = {0.f, 0.f, 0.f, 0.f}, v4 = {0.f, 0.f, 0.f, 0.f};
+      for (int p = 0; p <= a.pk.parts; ++p) {
+        if (p < a.pk.parts ? !((const ci32*)a.pk.wrote)[((size_t)p * a.pk.kv_heads + place.head) * a.pk.blocks + place.block + kb]
+                           : !add)
+          continue;
+        k4 += *reinterpret_cast<const f32x4*>(a.pk.dk_part + p * values + off);
+        v4 += *reinterpret_cast<const f32x4*>(a.pk.dv_part + p * values + off);
       }
-      if (!add) {  // keys without entries
-        const float zero[VPL] = {};
-        for (int kl = grp; kl < BLK; kl += NG)
-          if (kstart[kl] == kstart[kl + 1]) put(kl, zero, zero);
+      E* const dk = reinterpret_cast<E*>(a.dk) + off;
+      E* const dv = reinterpret_cast<E*>(a.dv) + off;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        dk[e] = (E)k4[e];
+        dv[e] = (E)v4[e];
       }
-      add = true;
-      __syncthreads();
-      c0 += LK_CHUNK;
-    } while (c0 < total);
-    e0 += LK_NT;
-  } while (e0 < cnt);
+    }
+  }
 }
 
 // --------------------------------------------------------------------- dQ
@@ -1601,8 +1806,13 @@ __global__ __launch_bounds__(DQ_NT, 2) void dq_kernel(A a) {
     Vg += head;
     dOg += head;
   }
-  // (the packed form's `used` is the forward's `use`: its residuals belong to one forward)
-  if (a.lists && (a.buckets.used[blk] & (PK ? (int)LIST_DQ : LISTED))) {
+  // (the packed form's residuals belong to one forward: what it listed is good)
+  bool listed = false;
+  if constexpr (PK)
+    listed = a.lists && (((const ci32*)a.pk.use)[blk] & LIST_DQ);
+  else
+    listed = a.lists && (a.buckets.used[blk] & LISTED);
+  if (listed) {
     if constexpr (PK)
       gather_dq<E, D, GK, true>(a.gamma, a.scale, a.lists[blk], Kg, ldk, Vg, ldv, dOg, ldo, a.delta + row0,
                                 reinterpret_cast<E*>(a.dq) + ((int64_t)at.start * a.pk.heads + bh) * D,
@@ -1835,6 +2045,16 @@ hipError_t launch_dkdv_packed_d(Packed<BwdArgs> a, hipStream_t s) {
     if (a.gk == 4) kernel = dkdv_kernel<E, D, 4, A>;
     e = launch_kernel(kernel, grid, dim3(BWD_NT), s, a);
   }
+  if (e == hipSuccess && a.lists) {
+    a.pk.size = 0;
+    a.pk.tiles = a.pk.lists[0];
+    auto kernel = dkdv_lists_kernel<E, D, 0, A>;
+    if (a.gk == 1) kernel = dkdv_lists_kernel<E, D, 1, A>;
+    if (a.gk == 2) kernel = dkdv_lists_kernel<E, D, 2, A>;
+    if (a.gk == 4) kernel = dkdv_lists_kernel<E, D, 4, A>;
+    return launch_kernel(kernel, dim3((unsigned)(a.pk.kv_heads * packed_tiles(a.pk.tokens, a.pk.seq_count, 0))),
+                         dim3(LK_NT), s, a);
+  }
   if (e != hipSuccess || a.pk.parts == 1) return e;
   const int64_t quads = (int64_t)a.pk.tokens * a.pk.kv_heads * D / 2;
   return launch_kernel(reduce_parts_kernel<E, D>, dim3((unsigned)((quads + 255) / 256)), dim3(256), s, a);
@@ -1854,7 +2074,13 @@ hipError_t launch_dq_packed_d(Packed<BwdArgs> a, hipStream_t s) {
 }
 
 template <typename E, int D>
-hipError_t launch_delta_packed_d(const Packed<DeltaArgs>& a, hipStream_t s) {
+hipError_t launch_delta_packed_d(Packed<DeltaArgs> a, hipStream_t s) {
+  if (a.lists) {
+    a.pk.size = 0;
+    a.pk.tiles = a.pk.lists[0];
+    return launch_kernel(prep_packed_kernel<E, D>,
+                         dim3((unsigned)(a.pk.heads * packed_tiles(a.pk.tokens, a.pk.seq_count, 0))), dim3(PREP_NT), s, a);
+  }
   return launch_kernel(delta_packed_kernel<E, D>, dim3((unsigned)((a.rows + 15) / 16)), dim3(256), s, a);
 }
 
@@ -1874,10 +2100,10 @@ hipError_t launch_collect_d(const CollectArgs& a, hipStream_t s) {
 template <typename E, int D>
 hipError_t launch_dkdv_lists_d(const BwdArgs& a, hipStream_t s) {
   dim3 grid((unsigned)(a.BH * a.T)), block(LK_NT);
-  auto kernel = dkdv_lists_kernel<E, D, 0>;
-  if (a.gk == 1) kernel = dkdv_lists_kernel<E, D, 1>;
-  if (a.gk == 2) kernel = dkdv_lists_kernel<E, D, 2>;
-  if (a.gk == 4) kernel = dkdv_lists_kernel<E, D, 4>;
+  auto kernel = dkdv_lists_kernel<E, D, 0, BwdArgs>;
+  if (a.gk == 1) kernel = dkdv_lists_kernel<E, D, 1, BwdArgs>;
+  if (a.gk == 2) kernel = dkdv_lists_kernel<E, D, 2, BwdArgs>;
+  if (a.gk == 4) kernel = dkdv_lists_kernel<E, D, 4, BwdArgs>;
   return launch_kernel(kernel, grid, block, s, a);
 }
 

@@ -128,6 +128,10 @@ struct PackedArgs {
   int zero_rest;       // whether the rows of no sequence are set to 0 in what is written
   int parts;           // dK/dV: workgroups that share the query heads of a key head
   float *dk_part, *dv_part;  // parts > 1: [parts, tokens, kv_heads, D] sums to add up
+  // with element lists there are always parts, one more than `parts` (the list
+  // kernel's), and
+  const int32_t* use;  // the forward's ListUse of every query block
+  int32_t* wrote;      // [parts, kv_heads, blocks]: whether a part has sums for a key block
 };
 // The arguments of a kernel's packed form.
 template <typename A>
@@ -248,7 +252,7 @@ struct FwdArgs {
 // per query block), with its row and key within their blocks (row * 64 + key).
 struct Buckets {
   int32_t* used;   // [BH * T]: whether the block's lists serve dQ, and its buckets dK and dV
-  int32_t* heads;  // [BH]: whether any block of the head has buckets
+  int32_t* heads;  // [BH]: whether any block of the head has buckets (packed: [heads, seqs] how many have)
   uint16_t* off;   // [BH * T, T + 1]
   float* z;        // [BH * T, LIST_ENTRIES]
   uint16_t* code;  // [BH * T, LIST_ENTRIES]

@@ -16,7 +16,7 @@ struct is_packed<Packed<A>> : std::true_type {};
 // Tile `tile` (64 << size rows) of a sequence of n rows and T blocks, for
 // query head `head` (dK/dV: key head `head`, part `part` of its query heads).
 struct Place {
-  int head, part, item, tile, start, n, T;
+  int head, part, item, tile, seq, start, n, T;
   int block;             // the sequence's first block among all
   size_t row0, blk0;  // of the query head: its first row in tau, and first block in the tables
 };
@@ -33,6 +33,7 @@ __device__ __forceinline__ bool packed_place(const PackedArgs& pk, int b, int he
   if (at.item >= ((const ci32*)pk.header->count)[pk.size]) return false;
   const ci32* const tile = (const ci32*)(pk.tiles + at.item);
   const ci32* const seq = (const ci32*)(pk.seqs + tile[0]);
+  at.seq = tile[0];
   at.tile = tile[1];
   at.start = seq[0];
   at.n = seq[1];
