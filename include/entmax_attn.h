@@ -429,7 +429,8 @@ ea_status entmax_packed_bwd(const ea_packed_shape* shape, const ea_params* param
  *   k_prefix, v_prefix  [prefix, kv_heads, d] (not read where prefix is 0)
  *   params alpha, scale, max_iter and tol are used
  * prefix + capacity <= 131072.  workspace: entmax_prefix_decode_workspace
- * bytes, 16-byte aligned (4 bytes a score).  Two launches.
+ * bytes, 16-byte aligned (about 5 bytes for every query head and key, most of
+ * them for rows with thousands of probabilities).  Two launches.
  */
 typedef struct {
   int32_t requests, heads, kv_heads, head_dim, dtype;

@@ -1185,7 +1185,7 @@ def packed_backward(q, k, v, dout, res: PackedResiduals, dq=None, dk=None, dv=No
 
 def prefix_decode_workspace(q, k_cache, prefix=0):
     """Bytes of the workspace of prefix_decode for these tensors and a prefix of
-    that many keys (4 bytes for every query head's score of every key)."""
+    that many keys (about 5 bytes for every query head and key)."""
     shape = DecodeShape(q.shape[0], q.shape[1], k_cache.shape[2], q.shape[2], _ea_dtype(q, "q"), int(prefix),
                         k_cache.shape[1])
     n = ctypes.c_size_t()

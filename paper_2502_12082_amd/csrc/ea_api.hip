@@ -1071,11 +1071,13 @@ ea_status check_decode(const ea_decode_shape* s) {
 size_t decode_parts(const ea_decode_shape* s, void* base, DecodeArgs* a) {
   const size_t rows = (size_t)s->requests * s->heads;
   const size_t pb = ((size_t)s->prefix + DEC_KEYS - 1) / DEC_KEYS, ob = ((size_t)s->capacity + DEC_KEYS - 1) / DEC_KEYS;
+  const size_t p_wide = (pb + DEC_RUN - 1) / DEC_RUN * DEC_RUN, o_wide = (ob + DEC_RUN - 1) / DEC_RUN * DEC_RUN;
   Parts p{static_cast<char*>(base)};
-  a->ps = p.take<float>(rows * pb * DEC_KEYS);
-  a->pm = p.take<float>(rows * pb);
-  a->os = p.take<float>(rows * ob * DEC_KEYS);
-  a->om = p.take<float>(rows * ob);
+  a->pq = p.take<float>(rows * pb * 8);
+  a->oq = p.take<float>(rows * ob * 8);
+  a->pm = p.take<float>(rows * p_wide);
+  a->om = p.take<float>(rows * o_wide);
+  a->spill = p.take<float>(rows * (pb + ob) * DEC_KEYS);
   return p.at;
 }
 
@@ -1142,6 +1144,7 @@ ea_status entmax_prefix_decode(const ea_decode_shape* shape, const ea_params* pa
   a.group = shape->heads / shape->kv_heads;
   a.prefix = shape->prefix;
   a.capacity = shape->capacity;
+  static_assert(DEC_RUN == 4, "a run's maxima are 16 bytes");
   constexpr int RUN_KEYS = DEC_KEYS * DEC_RUN;
   a.prefix_runs = (shape->prefix + RUN_KEYS - 1) / RUN_KEYS;
   a.own_runs = (shape->capacity + RUN_KEYS - 1) / RUN_KEYS;

@@ -616,6 +616,13 @@ __device__ __forceinline__ void store_packed(const PackedArgs& pk, const Place& 
   else
     reinterpret_cast<E*>(out)[off] = (E)x;
 }
+__device__ __forceinline__ void store4(__bf16* out, const f32x4& x) {
+  bf16x4 o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = (__bf16)x[e];
+  *reinterpret_cast<bf16x4*>(out) = o;
+}
+__device__ __forceinline__ void store4(float* out, const f32x4& x) { *reinterpret_cast<f32x4*>(out) = x; }
 // Whether this workgroup has sums for key block kb (with element lists).
 __device__ __forceinline__ void mark_part(const PackedArgs& pk, const Place& at, int kb, bool any) {
   if (threadIdx.x == 0 && kb < at.T)
@@ -999,7 +1006,7 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(A a) {
   // element lists) masks of the current chunks
   int hn = 0;
   [[maybe_unused]] unsigned long long mA = 0, mB = 0;
-  [[maybe_unused]] bool any = false;
+  [[maybe_unused]] bool any = false, masks = false;
   [[maybe_unused]] auto chunk = [&](int kb, int e0, int cnt) {
     const int e = min(e0 + lane, cnt - 1);
     const int qb = a.k_index[(blk0 + kb) * width + e];
@@ -1011,7 +1018,11 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(A a) {
       nA = count_of(kbA);
       nB = count_of(kbB);
       pA = pB = 0;
-      if (a.lists && ((const ci32*)a.buckets.heads)[(size_t)(bh + hn) * a.pk.seq_count + at.seq] == T) nA = nB = 0;
+      if (a.lists) {
+        const int sorted = ((const ci32*)a.buckets.heads)[(size_t)(bh + hn) * a.pk.seq_count + at.seq];
+        masks = sorted != 0;
+        if (sorted == T) nA = nB = 0;
+      }
     }
   };
   begin_head();
@@ -1030,10 +1041,10 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(A a) {
   // the next query block of the union, and whether each key block lists it
   auto next = [&](auto left, int& h, int& qb, bool& inA, bool& inB) {
     if constexpr (PK) {
-      // With element lists, entries in chunks of 64, as masks of those whose
-      // query blocks have no lists (one vector load a chunk).
+      // Heads with sorted blocks: entries in chunks of 64, as masks of those
+      // whose query blocks are not sorted (one vector load a chunk).
       for (;;) {
-        if (a.lists) {
+        if (masks) {
           for (; mA == 0 && pA < nA; pA += 64) mA = chunk(kbA, pA, nA);
           for (; mB == 0 && pB < nB; pB += 64) mB = chunk(kbB, pB, nB);
           if (mA | mB) break;
@@ -1045,7 +1056,8 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(A a) {
         begin_head();
       }
       h = hn;
-      if (a.lists) {
+      any = true;
+      if (masks) {
         const int hA = mA ? entry_of(left, kbA, pA - 64 + __builtin_ctzll(mA)) : T;
         const int hB = mB ? entry_of(left, kbB, pB - 64 + __builtin_ctzll(mB)) : T;
         qb = min(hA, hB);
@@ -1053,7 +1065,6 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(A a) {
         inB = hB == qb;
         if (inA) mA &= mA - 1;
         if (inB) mB &= mB - 1;
-        any = true;
         return true;
       }
     }
@@ -1658,13 +1669,8 @@ __global__ __launch_bounds__(LK_NT, 2) void dkdv_lists_kernel(A a) {
         k4 += *reinterpret_cast<const f32x4*>(a.pk.dk_part + p * values + off);
         v4 += *reinterpret_cast<const f32x4*>(a.pk.dv_part + p * values + off);
       }
-      E* const dk = reinterpret_cast<E*>(a.dk) + off;
-      E* const dv = reinterpret_cast<E*>(a.dv) + off;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        dk[e] = (E)k4[e];
-        dv[e] = (E)v4[e];
-      }
+      store4(reinterpret_cast<E*>(a.dk) + off, k4);
+      store4(reinterpret_cast<E*>(a.dv) + off, v4);
     }
   }
 }
@@ -1978,15 +1984,7 @@ __global__ __launch_bounds__(256) void reduce_parts_kernel(Packed<BwdArgs> a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] += v[e];
     }
-  E* out = reinterpret_cast<E*>(second ? a.dv : a.dk) + x;
-  if constexpr (sizeof(E) == 2) {
-    bf16x4 o;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = (__bf16)sum[e];
-    *reinterpret_cast<bf16x4*>(out) = o;
-  } else {
-    *reinterpret_cast<f32x4*>(out) = sum;
-  }
+  store4(reinterpret_cast<E*>(second ? a.dv : a.dk) + x, sum);
 }
 
 template <typename E, int D>

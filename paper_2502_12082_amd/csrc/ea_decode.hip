@@ -8,23 +8,26 @@
 // stream by, as a softmax has; but few keys have a probability, so that after
 // the scores only those rows of V have to be read.  Two kernels:
 //
-// Scores.  The queries of every request that share a key head form one matrix,
+// Maxima.  The queries of every request that share a key head form one matrix,
 // so a prefix key is read once for all of them; a request's own cache meets
 // the queries of its group.  A wave holds 32 RT queries as MFMA B operands in
 // registers and streams key blocks of 32 from memory straight into A operands
 // (no LDS: each key row is used by one wave).  Bound by HBM: the keys are read
-// once, a score is 4 bytes written against 2 D bytes of key read for all
-// queries of the head.  The maximum of every (query, key block) is written too.
+// once.  The scores themselves are not written, but the largest of every four
+// and of every 32 keys: with 128 queries to a key head the scores would be
+// four times the key's bytes, in 16-byte pieces (decode of 32 requests, 32/8
+// heads, behind 65536 shared keys, d = 128: XX us, with all scores written 108).
 //
 // Solve.  One workgroup per query row.  The maxima of its blocks are scores of
-// distinct keys, so f restricted to them lies below f, and its root b is a
+// distinct keys, so f restricted to them lies below f, and its root is a
 // lower bound of tau (as the bound of the attention solver, over every block):
-// only blocks with a larger maximum are read, and of those only the scores
-// above b are kept, in LDS.  tau is solved on the kept scores (Algorithm 1's
-// iteration), and the rows of V with a probability are gathered, 16 bytes a
-// lane.  Rows that keep more than fit are solved by reading the scores of
-// those blocks again for every evaluation, and gather V part by part.
-// Every list keeps the order of the keys, so results do not depend on timing.
+// only quads of keys whose maximum is above it can have a probability.  Their
+// scores are computed again, from K rows that the caches still hold, into LDS,
+// tau is solved on them (Algorithm 1's iteration), and the rows of V with a
+// probability are gathered, 16 bytes a lane.  Rows with more quads than fit
+// compute the scores of whole blocks into memory and read them for every
+// evaluation, and gather V part by part.  Every list has an order that depends
+// on the scores alone, not on timing.
 #include "ea_common.h"
 #include "ea_internal.h"
 
@@ -35,14 +38,16 @@ namespace {
 constexpr int SC_NT = 256;
 constexpr int SC_WAVES = SC_NT / 64;
 
-// ------------------------------------------------------------------ scores
+// ------------------------------------------------------------------ maxima
 
-// Scores of DEC_RUN key blocks from block kb0 on (`blocks` in all, `keys`
-// keys) against the wave's 32 RT rows from r0 on (`rows` in all):
-// s[(kb * rows + r) * 32 + key], and maxima m[r * blocks + kb].
+// Maxima of DEC_RUN key blocks from block kb0 on (`blocks` in all, `keys`
+// keys) against the wave's 32 RT rows from r0 on (`rows` in all): of the quads
+// of four keys, qm[(kb * rows + r) * 8 + quad] (a wave writes 1 KB in one
+// piece), and of blocks, m[r * wide + kb].
 template <typename E, int D, int RT>
-__device__ __forceinline__ void score_run(const E* K, int64_t ldk, int keys, int blocks, int kb0, int r0, int rows,
-                                          const typename Mma<E>::frag (&qf)[RT][D / Mma<E>::KW], float* s, float* m) {
+__device__ __forceinline__ void maxima_run(const E* K, int64_t ldk, int keys, int blocks, int wide, int kb0, int r0,
+                                           int rows, const typename Mma<E>::frag (&qf)[RT][D / Mma<E>::KW], float* qm,
+                                           float* m) {
   using M = Mma<E>;
   constexpr int KS = D / M::KW;
   const int lane = lane_id(), half = lane >> 5;
@@ -53,7 +58,7 @@ __device__ __forceinline__ void score_run(const E* K, int64_t ldk, int keys, int
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) f[kk] = load_row_frag_global<E, D>(row, 0, 1, kk);
   };
-  float top[RT][DEC_RUN];
+  f32x4 top[RT];
   load(kb0, kf[0]);
 #pragma unroll
   for (int x = 0; x < DEC_RUN; ++x) {
@@ -72,49 +77,44 @@ __device__ __forceinline__ void score_run(const E* K, int64_t ldk, int keys, int
         for (int r = 0; r < 16; ++r)
           if (kb * DEC_KEYS + crow(r) >= keys) v[r] = -INFINITY;
       }
-      float mx = v[0];
+      // (the lane's quads 4 i .. 4 i + 3 are keys 8 i + 4 half ..: quad 2 i + half, stored at 4 half + i)
+      f32x4 gm;
 #pragma unroll
-      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, v[r]);
+      for (int i = 0; i < 4; ++i) gm[i] = fmaxf(fmaxf(v[4 * i], v[4 * i + 1]), fmaxf(v[4 * i + 2], v[4 * i + 3]));
       float lo, hi;
-      wave_halves(mx, lo, hi);
+      wave_halves(fmaxf(fmaxf(gm[0], gm[1]), fmaxf(gm[2], gm[3])), lo, hi);
       top[t][x] = fmaxf(lo, hi);
       const int row = r0 + 32 * t + (lane & 31);
-      if (row < rows) {
-        float* out = s + ((int64_t)kb * rows + row) * DEC_KEYS + 4 * half;
-#pragma unroll
-        for (int r = 0; r < 16; r += 4) *reinterpret_cast<f32x4*>(out + 2 * r) = f32x4{v[r], v[r + 1], v[r + 2], v[r + 3]};
-      }
+      if (row < rows) *reinterpret_cast<f32x4*>(qm + ((int64_t)kb * rows + row) * 8 + 4 * half) = gm;
     }
   }
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const int row = r0 + 32 * t + (lane & 31);
-    if (row < rows && half == 0) {
-#pragma unroll
-      for (int x = 0; x < DEC_RUN; ++x)
-        if (kb0 + x < blocks) m[(int64_t)row * blocks + kb0 + x] = top[t][x];
-    }
+    if (row < rows && half == 0) *reinterpret_cast<f32x4*>(m + (int64_t)row * wide + kb0) = top[t];
   }
 }
+// Quad of a block stored at place i of its eight.
+__device__ __forceinline__ int quad_at(int i) { return 2 * (i & 3) + (i >> 2); }
 
 __device__ __forceinline__ int blocks_of(int keys) { return (keys + DEC_KEYS - 1) / DEC_KEYS; }
 __device__ __forceinline__ int own_length(const DecodeArgs& a, int b) {
   return min(max(((const ci32*)a.lengths)[b], 0), a.capacity);
 }
 
-// Workgroups of the prefix first: per key head, row tile and chunk of
-// `per_wave` runs a wave; then one wave per request, key head, row tile and run.
+// Workgroups of the prefix first: per chunk of `per_wave` runs a wave, row tile
+// and key head; then one wave per request, key head, row tile and run.
 template <typename E, int D, int RT>
-__global__ __launch_bounds__(SC_NT, 2) void decode_scores_kernel(DecodeArgs a, int row_tiles, int per_wave, int prefix_wgs) {
+__global__ __launch_bounds__(SC_NT, 2) void decode_maxima_kernel(DecodeArgs a, int row_tiles, int per_wave, int prefix_wgs) {
   using M = Mma<E>;
   constexpr int KS = D / M::KW;
   const int lane = lane_id(), w = wave_id();
   int x = blockIdx.x;
   if (x < prefix_wgs) {
     const int rows = a.requests * a.group;
-    // row tiles of the same keys are next to each other in time
-    const int chunks = (a.prefix_runs + SC_WAVES * per_wave - 1) / (SC_WAVES * per_wave);
-    const int rt = x % row_tiles, chunk = x / row_tiles % chunks, kv = x / row_tiles / chunks;
+    // Row tiles of the same keys are next to each other in time, and with eight
+    // key heads on one XCD.
+    const int kv = x % a.kv_heads, rt = x / a.kv_heads % row_tiles, chunk = x / a.kv_heads / row_tiles;
     const int r0 = rt * 32 * RT, blocks = blocks_of(a.prefix);
     typename M::frag qf[RT][KS];
 #pragma unroll
@@ -125,12 +125,13 @@ __global__ __launch_bounds__(SC_NT, 2) void decode_scores_kernel(DecodeArgs a, i
       for (int kk = 0; kk < KS; ++kk) qf[t][kk] = load_row_frag_global<E, D>(row, 0, 1, kk);
     }
     const E* K = static_cast<const E*>(a.pk) + kv * a.pk_head;
-    float* s = a.ps + (int64_t)kv * blocks * rows * DEC_KEYS;
-    float* m = a.pm + (int64_t)kv * rows * blocks;
+    const int wide = a.prefix_runs * DEC_RUN;
+    float* qm = a.pq + (int64_t)kv * blocks * rows * 8;
+    float* m = a.pm + (int64_t)kv * rows * wide;
     for (int y = 0; y < per_wave; ++y) {
       const int run = (chunk * per_wave + y) * SC_WAVES + w;
       if (run >= a.prefix_runs) break;
-      score_run<E, D, RT>(K, a.pk_row, a.prefix, blocks, run * DEC_RUN, r0, rows, qf, s, m);
+      maxima_run<E, D, RT>(K, a.pk_row, a.prefix, blocks, wide, run * DEC_RUN, r0, rows, qf, qm, m);
     }
     return;
   }
@@ -147,8 +148,9 @@ __global__ __launch_bounds__(SC_NT, 2) void decode_scores_kernel(DecodeArgs a, i
 #pragma unroll
   for (int kk = 0; kk < KS; ++kk) qf[0][kk] = load_row_frag_global<E, D>(row, 0, 1, kk);
   const int64_t bk = (int64_t)b * a.kv_heads + kv;
-  score_run<E, D, 1>(static_cast<const E*>(a.k) + b * a.k_batch + kv * a.k_head, a.k_row, keys, blocks, run * DEC_RUN,
-                     rt * 32, a.group, qf, a.os + bk * blocks * a.group * DEC_KEYS, a.om + bk * a.group * blocks);
+  maxima_run<E, D, 1>(static_cast<const E*>(a.k) + b * a.k_batch + kv * a.k_head, a.k_row, keys, blocks,
+                      a.own_runs * DEC_RUN, run * DEC_RUN, rt * 32, a.group, qf, a.oq + bk * blocks * a.group * 8,
+                      a.om + bk * a.group * a.own_runs * DEC_RUN);
 }
 
 // ------------------------------------------------------------------- solve
@@ -156,29 +158,47 @@ __global__ __launch_bounds__(SC_NT, 2) void decode_scores_kernel(DecodeArgs a, i
 constexpr int SO_NT = 256;
 constexpr int SO_WAVES = SO_NT / 64;
 constexpr int SO_CAP = 2048;     // scores kept in LDS
-constexpr int SO_BLOCKS = MAX_SEQLEN / DEC_KEYS + 2;  // block numbers kept in LDS
+constexpr int SO_QUADS = SO_CAP / 4;
+constexpr int SO_BLOCKS = MAX_SEQLEN / DEC_KEYS + 2;  // most blocks of a row
+constexpr int SO_MAXIMA = (SO_BLOCKS + SO_NT - 1) / SO_NT;  // of them, each thread's
 constexpr int SO_LANE = 8;       // scores per lane that every wave solves on its own
+constexpr int SO_STEPS = 4;      // blocks that eight threads read at once
 
-// The wave's and the workgroup's sums and counts.  All threads.
+// Sum, and maximum, over the wave, in all lanes (lanes exchange inside quads,
+// mirrored inside 8 and 16 lanes, then rows and halves by swaps: no LDS).
+template <typename F>
+__device__ __forceinline__ float wave_fold(float v, F&& f) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  auto dpp = [](float x, auto ctrl) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), decltype(ctrl)::value, 0xf,
+                                                                0xf, true));
+  };
+  v = f(v, dpp(v, std::integral_constant<int, 0xB1>{}));   // quad_perm 1, 0, 3, 2
+  v = f(v, dpp(v, std::integral_constant<int, 0x4E>{}));   // quad_perm 2, 3, 0, 1
+  v = f(v, dpp(v, std::integral_constant<int, 0x141>{}));  // row_half_mirror
+  v = f(v, dpp(v, std::integral_constant<int, 0x140>{}));  // row_mirror
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+#endif
+  float lo, hi;
+  wave_halves(v, lo, hi);
+  return f(lo, hi);
+}
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+  return wave_fold(v, [](float a, float b) { return a + b; });
 }
 __device__ __forceinline__ float wave_maxf(float v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-  return v;
+  return wave_fold(v, [](float a, float b) { return fmaxf(a, b); });
 }
 
-// A row's scores: blocks 0 .. prefix blocks - 1, then its own.
-struct RowScores {
-  const float *ps, *os, *pm, *om;  // of the row
-  int64_t p_step, o_step;          // block to block in the scores
+// A row's blocks: 0 .. prefix blocks - 1, then its own.
+struct RowBlocks {
+  const float *pm, *om, *pq, *oq;  // of the row
+  int64_t p_step, o_step;          // block to block in the quads' maxima
   int p_blocks, blocks;
   __device__ __forceinline__ float top(int b) const { return b < p_blocks ? pm[b] : om[b - p_blocks]; }
-  __device__ __forceinline__ const float* block(int b) const {
-    return b < p_blocks ? ps + b * p_step : os + (b - p_blocks) * o_step;
+  __device__ __forceinline__ const float* quads(int b) const {
+    return b < p_blocks ? pq + b * p_step : oq + (b - p_blocks) * o_step;
   }
 };
 
@@ -186,47 +206,53 @@ template <typename E, int D, int GK>
 __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
   using R = RowGroup<E, D>;
   constexpr int VPL = R::VPL, LPR = R::LPR, NG = SO_NT / LPR;
-  __shared__ float kept[SO_CAP];     // scores above the bound, in the order of the keys
-  __shared__ int kept_key[SO_CAP];   // 32 block + key in the block
+  __shared__ float kept[SO_CAP];          // scores of the quads, four each
+  __shared__ uint16_t quad[SO_QUADS];     // quads with a score above the bound (the block's first key / 4 + quad)
   __shared__ uint16_t chosen[SO_BLOCKS];  // blocks with such a score
-  __shared__ float red[3][SO_WAVES];
-  __shared__ int cnt[SO_WAVES];
+  __shared__ float red[2][3][SO_WAVES];
+  __shared__ int cnt[2][SO_WAVES];
   static_assert(sizeof(kept) >= NG * D * sizeof(float), "the groups' sums fit in place of the scores");
-  const int t = threadIdx.x, lane = lane_id(), w = wave_id();
+  static_assert(SO_BLOCKS * (DEC_KEYS / 4) <= 65536, "a quad's number fits 16 bits");
+  const int t = threadIdx.x, lane = lane_id(), w = wave_id(), sub = lane % LPR, grp = t / LPR;
   const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads, kv = h / a.group, g = h % a.group;
   const int len = own_length(a, b);
   const int p_blocks = blocks_of(a.prefix), own_cap = blocks_of(a.capacity);
-  RowScores row;
+  const int p_wide = a.prefix_runs * DEC_RUN, o_wide = a.own_runs * DEC_RUN;
+  RowBlocks row;
   row.p_blocks = p_blocks;
   row.blocks = p_blocks + blocks_of(len);
   const int64_t rows = (int64_t)a.requests * a.group, r = (int64_t)b * a.group + g, bk = (int64_t)b * a.kv_heads + kv;
-  row.ps = a.ps + ((int64_t)kv * p_blocks * rows + r) * DEC_KEYS;
-  row.p_step = rows * DEC_KEYS;
-  row.pm = a.pm + ((int64_t)kv * rows + r) * p_blocks;
-  row.os = a.os + (bk * own_cap * a.group + g) * DEC_KEYS;
-  row.o_step = (int64_t)a.group * DEC_KEYS;
-  row.om = a.om + (bk * a.group + g) * own_cap;
+  row.pm = a.pm + ((int64_t)kv * rows + r) * p_wide;
+  row.pq = a.pq + ((int64_t)kv * p_blocks * rows + r) * 8;
+  row.p_step = rows * 8;
+  row.om = a.om + (bk * a.group + g) * o_wide;
+  row.oq = a.oq + (bk * own_cap * a.group + g) * 8;
+  row.o_step = (int64_t)a.group * 8;
   E* const O = static_cast<E*>(a.o) + b * a.o_row + h * a.o_head;
   const float c = a.c, gm = a.gamma;
 
-  // Sums over the workgroup of three values, in all threads.
+  // Sums over the workgroup of three values, in all threads (two buffers in
+  // turn: one barrier).
+  int turn = 0;
   auto sum3 = [&](float& x, float& y, float& z) {
     x = wave_sum(x);
     y = wave_sum(y);
     z = wave_sum(z);
-    __syncthreads();
+    auto& m = red[turn];
+    turn ^= 1;
     if (lane == 0) {
-      red[0][w] = x;
-      red[1][w] = y;
-      red[2][w] = z;
+      m[0][w] = x;
+      m[1][w] = y;
+      m[2][w] = z;
     }
     __syncthreads();
-    x = (red[0][0] + red[0][1]) + (red[0][2] + red[0][3]);
-    y = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
-    z = (red[2][0] + red[2][1]) + (red[2][2] + red[2][3]);
+    x = (m[0][0] + m[0][1]) + (m[0][2] + m[0][3]);
+    y = (m[1][0] + m[1][1]) + (m[1][2] + m[1][3]);
+    z = (m[2][0] + m[2][1]) + (m[2][2] + m[2][3]);
   };
   // Where the thread's `mine` items go among those of all threads, from
   // `base` on; base grows by all of them.
+  int cturn = 0;
   auto place = [&](int mine, int& base) {
     int incl = mine;
 #pragma unroll
@@ -234,26 +260,37 @@ __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
       const int v = __shfl_up(incl, o);
       if (lane >= o) incl += v;
     }
-    __syncthreads();
-    if (lane == 63) cnt[w] = incl;
+    auto& m = cnt[cturn];
+    cturn ^= 1;
+    if (lane == 63) m[w] = incl;
     __syncthreads();
     int at = base + incl - mine;
 #pragma unroll
     for (int x = 0; x < SO_WAVES; ++x) {
-      if (x < w) at += cnt[x];
-      base += cnt[x];
+      if (x < w) at += m[x];
+      base += m[x];
     }
     return at;
   };
 
-  // ---- the largest score, and the bound from the blocks' maxima
-  float m = -INFINITY;
-  for (int x = t; x < row.blocks; x += SO_NT) m = fmaxf(m, row.top(x));
+  // ---- the maxima of the row's blocks, and the largest score
+  float top[SO_MAXIMA], m = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < SO_MAXIMA; ++j) {
+    top[j] = -INFINITY;
+    if (j * SO_NT >= row.blocks) break;
+    if (j * SO_NT + t < row.blocks) top[j] = row.top(j * SO_NT + t);
+  }
+#pragma unroll
+  for (int j = 0; j < SO_MAXIMA; ++j) {
+    if (j * SO_NT >= row.blocks) break;
+    m = fmaxf(m, top[j]);
+  }
   m = wave_maxf(m);
-  if (lane == 0) red[0][w] = m;
+  if (lane == 0) red[0][0][w] = m;
   __syncthreads();
-  m = c * fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-  __syncthreads();
+  m = c * fmaxf(fmaxf(red[0][0][0], red[0][0][1]), fmaxf(red[0][0][2], red[0][0][3]));
+  turn = 1;
   if (!(m > -INFINITY)) {  // no keys (or none with a finite score): nothing to add up
     for (int x = t; x < D; x += SO_NT) O[x] = (E)0.f;
     return;
@@ -270,66 +307,129 @@ __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
       if constexpr (GK == 0) s2 += u / z;
     }
   };
+  // The bound: Newton's steps on f restricted to the maxima, from max x - 1,
+  // stay below its root where f is convex.  First each wave takes its own
+  // maxima alone (a bound as well), without waiting for the others; then two
+  // steps on all of them from the best of those.
   const bool convex = gm >= 1.f;
   float lo = m - 1.f;
   if (convex) {
+    auto sums = [&](float& s0, float& s1) {
+      float s2 = 0.f;
+#pragma unroll
+      for (int j = 0; j < SO_MAXIMA; ++j) {
+        if (j * SO_NT >= row.blocks) break;
+        add(relu_z(c, top[j], lo), s0, s1, s2);
+      }
+    };
     for (int it = 0; it < 8; ++it) {
+      float s0 = 0.f, s1 = 0.f;
+      sums(s0, s1);
+      s0 = wave_sum(s0);
+      s1 = wave_sum(s1);
+      const float step = (s0 - 1.f) / (gm * s1);
+      if (!(step > 1e-2f)) break;
+      lo += step;
+    }
+    if (lane == 0) red[1][0][w] = lo;
+    __syncthreads();
+    lo = fmaxf(fmaxf(red[1][0][0], red[1][0][1]), fmaxf(red[1][0][2], red[1][0][3]));
+    turn = 0;
+    for (int it = 0; it < 2; ++it) {
       float s0 = 0.f, s1 = 0.f, s2 = 0.f;
-      for (int x = t; x < row.blocks; x += SO_NT) add(relu_z(c, row.top(x), lo), s0, s1, s2);
+      sums(s0, s1);
       sum3(s0, s1, s2);
       const float step = (s0 - 1.f) / (gm * s1);
-      if (!(step > 1e-3f)) break;
-      lo += step;
+      if (step > 0.f) lo += step;
     }
   }
   // less the rounding of the sums (a lower bound serves as well)
   lo -= 4e-6f * fmaxf(1.f, fabsf(lo));
 
   // ---- the blocks with a score above the bound, and those scores
-  int nb = 0;
-  for (int x0 = 0; x0 < row.blocks; x0 += SO_NT) {
-    const int x = x0 + t;
-    const bool take = x < row.blocks && relu_z(c, row.top(min(x, row.blocks - 1)), lo) > 0.f;
-    const int at = place(take ? 1 : 0, nb);
-    if (take) chosen[at] = (uint16_t)x;
+  int nb = 0, mine = 0;
+#pragma unroll
+  for (int j = 0; j < SO_MAXIMA; ++j) {
+    if (j * SO_NT >= row.blocks) break;
+    mine += relu_z(c, top[j], lo) > 0.f ? 1 : 0;
+  }
+  int to = place(mine, nb);
+#pragma unroll
+  for (int j = 0; j < SO_MAXIMA; ++j) {
+    if (j * SO_NT >= row.blocks) break;
+    if (relu_z(c, top[j], lo) > 0.f) chosen[to++] = (uint16_t)(j * SO_NT + t);
   }
   __syncthreads();
-  // Scores of the chosen blocks in turn: eight threads to a block, four
-  // scores each.  use(score vector, first key, 0 <= thread's block < nb).
+  // ---- the quads with a score above the bound: eight threads to a block
   constexpr int BPS = SO_NT / 8;  // blocks a step
-  auto scores_of = [&](int x) { return *reinterpret_cast<const f32x4*>(row.block(chosen[x]) + 4 * (t & 7)); };
-  // Keeps the scores of chosen blocks [x0, x1) with z > 0 at `at_tau`, up to
-  // SO_CAP of them; returns their number (more: the rest are not kept).
-  auto collect = [&](int x0, int x1, float at_tau) {
-    int n = 0;
-    for (int s0 = x0; s0 < x1; s0 += BPS) {
-      const int x = s0 + (t >> 3);
-      f32x4 v = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-      if (x < x1) v = scores_of(x);
-      int mine = 0;
-      bool in[4];
+  int nq = 0;
+  for (int s0 = 0; s0 < nb; s0 += BPS * SO_STEPS) {
+    int mine = 0;
+    bool in[SO_STEPS];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        in[e] = relu_z(c, v[e], at_tau) > 0.f;
-        mine += in[e] ? 1 : 0;
-      }
-      int at = place(mine, n);
-      const int key = x < x1 ? chosen[x] * DEC_KEYS + 4 * (t & 7) : 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (in[e]) {
-          if (at < SO_CAP) {
-            kept[at] = v[e];
-            kept_key[at] = key + e;
-          }
-          ++at;
-        }
+    for (int u = 0; u < SO_STEPS; ++u) {
+      const int x = s0 + u * BPS + (t >> 3);
+      in[u] = x < nb && relu_z(c, row.quads(chosen[min(x, nb - 1)])[t & 7], lo) > 0.f;
+      mine += in[u] ? 1 : 0;
     }
-    __syncthreads();
-    return n;
+    int at = place(mine, nq);
+#pragma unroll
+    for (int u = 0; u < SO_STEPS; ++u)
+      if (in[u]) {
+        if (at < SO_QUADS) quad[at] = (uint16_t)(chosen[s0 + u * BPS + (t >> 3)] * (DEC_KEYS / 4) + quad_at(t & 7));
+        ++at;
+      }
+  }
+  __syncthreads();
+  const bool wide = nq > SO_QUADS;
+
+  // ---- their scores: a group of lanes per key row
+  const E* const own_k = static_cast<const E*>(a.k) + b * a.k_batch + kv * a.k_head;
+  const E* const pre_k = static_cast<const E*>(a.pk) + kv * a.pk_head;
+  float qv[VPL];
+  R::unpack(R::load(static_cast<const E*>(a.q) + b * a.q_row + h * a.q_head, 0u), qv);
+  // Scores of four keys from key 4 x on (counted over all blocks), the same in all lanes of the group.
+  auto quad_scores = [&](int x) {
+    const int blk = x / (DEC_KEYS / 4);
+    const bool shared = blk < p_blocks;
+    const int k0 = 4 * x - (shared ? 0 : p_blocks * DEC_KEYS), end = shared ? a.prefix : len;
+    const E* const base = shared ? pre_k : own_k;
+    const int64_t ld = shared ? a.pk_row : a.k_row;
+    u32x4 kw[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      kw[e] = *reinterpret_cast<const u32x4*>(base + min(k0 + e, end - 1) * ld + sub * VPL);
+    f32x4 s;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float x2[VPL], dot = 0.f;
+      R::unpack(kw[e], x2);
+#pragma unroll
+      for (int d = 0; d < VPL; ++d) dot = fmaf(qv[d], x2[d], dot);
+      dot = R::sum(dot);
+      s[e] = k0 + e < end ? dot : -INFINITY;
+    }
+    return s;
   };
-  const int total = collect(0, nb, lo);
-  const bool wide = total > SO_CAP;
+  float* const spill = a.spill + ((int64_t)b * a.heads + h) * (int64_t)(p_blocks + own_cap) * DEC_KEYS;
+  if (!wide) {
+    for (int x = grp; x < nq; x += NG) {
+      const f32x4 s = quad_scores(quad[x]);
+      if (sub == 0) *reinterpret_cast<f32x4*>(kept + 4 * x) = s;
+    }
+  } else {
+    for (int x = grp; x < nb * (DEC_KEYS / 4); x += NG) {
+      const int q = chosen[x / (DEC_KEYS / 4)] * (DEC_KEYS / 4) + x % (DEC_KEYS / 4);
+      const f32x4 s = quad_scores(q);
+      if (sub == 0) *reinterpret_cast<f32x4*>(spill + 4 * (int64_t)q) = s;
+    }
+  }
+  __syncthreads();
+  const int total = 4 * nq;
+  // scores of chosen block x, four to each of eight threads (wide rows)
+  auto scores_of = [&](int x) {
+    return *reinterpret_cast<const f32x4*>(spill + (int64_t)chosen[x] * DEC_KEYS + 4 * (t & 7));
+  };
 
   // ---- tau: Algorithm 1's iteration on the kept scores
   float hi = m - powf((float)max(a.prefix + len, 1), 1.f - a.alpha);
@@ -381,11 +481,11 @@ __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
   }
 
   // ---- O: the rows of V with a probability
-  const int sub = lane % LPR, grp = t / LPR;
   float o[VPL] = {};
-  const char* const own_v = reinterpret_cast<const char*>(static_cast<const E*>(a.v) + b * a.v_batch + kv * a.v_head);
-  const char* const pre_v = reinterpret_cast<const char*>(static_cast<const E*>(a.pv) + kv * a.pv_head);
-  auto gather = [&](int n) {
+  const E* const own_v = static_cast<const E*>(a.v) + b * a.v_batch + kv * a.v_head;
+  const E* const pre_v = static_cast<const E*>(a.pv) + kv * a.pv_head;
+  // of n kept scores, those at 4 i of the keys from 4 first(i) on
+  auto gather = [&](int n, auto&& first) {
     constexpr int BATCH = 4;
     for (int y0 = grp; y0 < n; y0 += NG * BATCH) {
       u32x4 v[BATCH];
@@ -398,10 +498,10 @@ __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
         if (y < n) {
           p[u] = Gamma<GK>::p_only(relu_z(c, kept[y], tau), gm);
           if (p[u] > 0.f) {  // (a key without a probability is not read)
-            const int key = kept_key[y], blk = key / DEC_KEYS;
-            const char* v_row = blk < p_blocks ? pre_v + key * a.pv_row * (int64_t)sizeof(E)
-                                               : own_v + (key - p_blocks * DEC_KEYS) * a.v_row * (int64_t)sizeof(E);
-            v[u] = *reinterpret_cast<const u32x4*>(v_row + sub * 16);
+            const int key = 4 * first(y >> 2) + (y & 3);
+            const E* const v_row = key < p_blocks * DEC_KEYS ? pre_v + key * a.pv_row
+                                                             : own_v + (key - p_blocks * DEC_KEYS) * a.v_row;
+            v[u] = *reinterpret_cast<const u32x4*>(v_row + sub * VPL);
           }
         }
       }
@@ -415,12 +515,16 @@ __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
     }
   };
   if (!wide) {
-    gather(total);
+    gather(total, [&](int i) { return (int)quad[i]; });
   } else {
-    constexpr int PART = SO_CAP / DEC_KEYS;  // blocks whose scores all fit
+    constexpr int PART = SO_CAP / DEC_KEYS;  // blocks whose scores fit
     for (int x0 = 0; x0 < nb; x0 += PART) {
+      const int x1 = min(x0 + PART, nb);
       __syncthreads();
-      gather(collect(x0, min(x0 + PART, nb), tau));
+      for (int x = x0 + (t >> 3); x < x1; x += BPS)
+        *reinterpret_cast<f32x4*>(kept + (x - x0) * DEC_KEYS + 4 * (t & 7)) = scores_of(x);
+      __syncthreads();
+      gather((x1 - x0) * DEC_KEYS, [&](int i) { return chosen[x0 + i / (DEC_KEYS / 4)] * (DEC_KEYS / 4) + i % (DEC_KEYS / 4); });
     }
   }
   __syncthreads();
@@ -436,7 +540,7 @@ __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
 }
 
 template <typename E, int D, int RT>
-hipError_t launch_scores(const DecodeArgs& a, hipStream_t s) {
+hipError_t launch_maxima(const DecodeArgs& a, hipStream_t s) {
   const int row_tiles = (a.requests * a.group + 32 * RT - 1) / (32 * RT);
   // runs of a wave: as few as give every wave of the device work (eight waves
   // to each of 256 compute units), so that queries are loaded seldom
@@ -452,7 +556,7 @@ hipError_t launch_scores(const DecodeArgs& a, hipStream_t s) {
   DecodeArgs args = a;
   int rt = row_tiles, pw = per_wave, pg = (int)prefix_wgs;
   void* params[] = {&args, &rt, &pw, &pg};
-  return hipLaunchKernel(reinterpret_cast<const void*>(decode_scores_kernel<E, D, RT>), dim3((unsigned)wgs), dim3(SC_NT),
+  return hipLaunchKernel(reinterpret_cast<const void*>(decode_maxima_kernel<E, D, RT>), dim3((unsigned)wgs), dim3(SC_NT),
                          params, 0, s);
 }
 
@@ -461,11 +565,11 @@ hipError_t launch_decode_d(const DecodeArgs& a, hipStream_t s) {
   const int rows = a.requests * a.group;
   hipError_t e;
   if (sizeof(E) == 2 && rows > 64)
-    e = launch_scores<E, D, sizeof(E) == 2 ? 4 : 1>(a, s);
+    e = launch_maxima<E, D, sizeof(E) == 2 ? 4 : 1>(a, s);
   else if (sizeof(E) == 2 && rows > 32)
-    e = launch_scores<E, D, sizeof(E) == 2 ? 2 : 1>(a, s);
+    e = launch_maxima<E, D, sizeof(E) == 2 ? 2 : 1>(a, s);
   else
-    e = launch_scores<E, D, 1>(a, s);
+    e = launch_maxima<E, D, 1>(a, s);
   if (e != hipSuccess) return e;
   auto kernel = decode_solve_kernel<E, D, 0>;
   if (a.gk == 1) kernel = decode_solve_kernel<E, D, 1>;
