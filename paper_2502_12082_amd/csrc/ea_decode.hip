@@ -15,8 +15,8 @@
 // (no LDS: each key row is used by one wave).  Bound by HBM: the keys are read
 // once.  The scores themselves are not written, but the largest of every four
 // and of every 32 keys: with 128 queries to a key head the scores would be
-// four times the key's bytes, in 16-byte pieces (decode of 32 requests, 32/8
-// heads, behind 65536 shared keys, d = 128: XX us, with all scores written 108).
+// four times the key's bytes, in 16-byte pieces (32 requests, 32/8 heads, behind
+// 65536 shared keys, d = 128: 43 us, with all scores written 108).
 //
 // Solve.  One workgroup per query row.  The maxima of its blocks are scores of
 // distinct keys, so f restricted to them lies below f, and its root is a
@@ -155,14 +155,12 @@ __global__ __launch_bounds__(SC_NT, 2) void decode_maxima_kernel(DecodeArgs a, i
 
 // ------------------------------------------------------------------- solve
 
-constexpr int SO_NT = 256;
-constexpr int SO_WAVES = SO_NT / 64;
 constexpr int SO_CAP = 2048;     // scores kept in LDS
 constexpr int SO_QUADS = SO_CAP / 4;
 constexpr int SO_BLOCKS = MAX_SEQLEN / DEC_KEYS + 2;  // most blocks of a row
-constexpr int SO_MAXIMA = (SO_BLOCKS + SO_NT - 1) / SO_NT;  // of them, each thread's
-constexpr int SO_LANE = 8;       // scores per lane that every wave solves on its own
+constexpr int SO_LANE = 8;       // scores per lane that a wave solves on its own
 constexpr int SO_STEPS = 4;      // blocks that eight threads read at once
+constexpr int SO_MAXIMA = 16;    // blocks' maxima that a thread holds in registers
 
 // Sum, and maximum, over the wave, in all lanes (lanes exchange inside quads,
 // mirrored inside 8 and 16 lanes, then rows and halves by swaps: no LDS).
@@ -202,10 +200,12 @@ struct RowBlocks {
   }
 };
 
-template <typename E, int D, int GK>
-__global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
+// NT = 64: one wave per row, which waits for no other and repeats no other's
+// arithmetic.  NT = 256: four, for few or long rows (see launch_decode_d).
+template <typename E, int D, int GK, int NT>
+__global__ __launch_bounds__(NT) void decode_solve_kernel(DecodeArgs a) {
   using R = RowGroup<E, D>;
-  constexpr int VPL = R::VPL, LPR = R::LPR, NG = SO_NT / LPR;
+  constexpr int VPL = R::VPL, LPR = R::LPR, NG = NT / LPR, SO_NT = NT, SO_WAVES = NT / 64;
   __shared__ float kept[SO_CAP];          // scores of the quads, four each
   __shared__ uint16_t quad[SO_QUADS];     // quads with a score above the bound (the block's first key / 4 + quad)
   __shared__ uint16_t chosen[SO_BLOCKS];  // blocks with such a score
@@ -214,7 +214,10 @@ __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
   static_assert(sizeof(kept) >= NG * D * sizeof(float), "the groups' sums fit in place of the scores");
   static_assert(SO_BLOCKS * (DEC_KEYS / 4) <= 65536, "a quad's number fits 16 bits");
   const int t = threadIdx.x, lane = lane_id(), w = wave_id(), sub = lane % LPR, grp = t / LPR;
-  const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads, kv = h / a.group, g = h % a.group;
+  // (heads of one key head are kv_heads apart: with eight key heads they meet on
+  // one XCD, whose L2 then has to hold the rows of that head alone)
+  const int b = blockIdx.x / a.heads, y = blockIdx.x % a.heads, kv = y % a.kv_heads, g = y / a.kv_heads;
+  const int h = kv * a.group + g;
   const int len = own_length(a, b);
   const int p_blocks = blocks_of(a.prefix), own_cap = blocks_of(a.capacity);
   const int p_wide = a.prefix_runs * DEC_RUN, o_wide = a.own_runs * DEC_RUN;
@@ -238,6 +241,7 @@ __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
     x = wave_sum(x);
     y = wave_sum(y);
     z = wave_sum(z);
+    if constexpr (SO_WAVES == 1) return;
     auto& m = red[turn];
     turn ^= 1;
     if (lane == 0) {
@@ -246,9 +250,25 @@ __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
       m[2][w] = z;
     }
     __syncthreads();
-    x = (m[0][0] + m[0][1]) + (m[0][2] + m[0][3]);
-    y = (m[1][0] + m[1][1]) + (m[1][2] + m[1][3]);
-    z = (m[2][0] + m[2][1]) + (m[2][2] + m[2][3]);
+    x = y = z = 0.f;
+#pragma unroll
+    for (int i = 0; i < SO_WAVES; ++i) {
+      x += m[0][i];
+      y += m[1][i];
+      z += m[2][i];
+    }
+  };
+  // The largest of a wave-uniform value over the workgroup.
+  auto max_waves = [&](float x) {
+    if constexpr (SO_WAVES > 1) {
+      auto& m = red[turn];
+      turn ^= 1;
+      if (lane == 0) m[0][w] = x;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < SO_WAVES; ++i) x = fmaxf(x, m[0][i]);
+    }
+    return x;
   };
   // Where the thread's `mine` items go among those of all threads, from
   // `base` on; base grows by all of them.
@@ -259,6 +279,11 @@ __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
     for (int o = 1; o < 64; o <<= 1) {
       const int v = __shfl_up(incl, o);
       if (lane >= o) incl += v;
+    }
+    if constexpr (SO_WAVES == 1) {
+      const int at = base + incl - mine;
+      base += __builtin_amdgcn_readlane(incl, 63);
+      return at;
     }
     auto& m = cnt[cturn];
     cturn ^= 1;
@@ -278,19 +303,21 @@ __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
 #pragma unroll
   for (int j = 0; j < SO_MAXIMA; ++j) {
     top[j] = -INFINITY;
-    if (j * SO_NT >= row.blocks) break;
-    if (j * SO_NT + t < row.blocks) top[j] = row.top(j * SO_NT + t);
+    if (j * NT >= row.blocks) break;
+    if (j * NT + t < row.blocks) top[j] = row.top(j * NT + t);
   }
+  // use(maximum, block) of the thread's blocks; those of longer rows are read again
+  auto each_top = [&](auto&& use) {
 #pragma unroll
-  for (int j = 0; j < SO_MAXIMA; ++j) {
-    if (j * SO_NT >= row.blocks) break;
-    m = fmaxf(m, top[j]);
-  }
-  m = wave_maxf(m);
-  if (lane == 0) red[0][0][w] = m;
-  __syncthreads();
-  m = c * fmaxf(fmaxf(red[0][0][0], red[0][0][1]), fmaxf(red[0][0][2], red[0][0][3]));
-  turn = 1;
+    for (int j = 0; j < SO_MAXIMA; ++j) {
+      if (j * NT >= row.blocks) break;
+      use(top[j], j * NT + t);
+    }
+#pragma unroll 4
+    for (int x = SO_MAXIMA * NT + t; x < row.blocks; x += NT) use(row.top(x), x);
+  };
+  each_top([&](float v, int) { m = fmaxf(m, v); });
+  m = c * max_waves(wave_maxf(m));
   if (!(m > -INFINITY)) {  // no keys (or none with a finite score): nothing to add up
     for (int x = t; x < D; x += SO_NT) O[x] = (E)0.f;
     return;
@@ -309,37 +336,30 @@ __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
   };
   // The bound: Newton's steps on f restricted to the maxima, from max x - 1,
   // stay below its root where f is convex.  First each wave takes its own
-  // maxima alone (a bound as well), without waiting for the others; then two
-  // steps on all of them from the best of those.
+  // maxima alone (a bound as well), without waiting for the others; then a
+  // step on all of them from the best of those.
   const bool convex = gm >= 1.f;
   float lo = m - 1.f;
   if (convex) {
     auto sums = [&](float& s0, float& s1) {
       float s2 = 0.f;
-#pragma unroll
-      for (int j = 0; j < SO_MAXIMA; ++j) {
-        if (j * SO_NT >= row.blocks) break;
-        add(relu_z(c, top[j], lo), s0, s1, s2);
-      }
+      each_top([&](float v, int) { add(relu_z(c, v, lo), s0, s1, s2); });
     };
     for (int it = 0; it < 8; ++it) {
       float s0 = 0.f, s1 = 0.f;
       sums(s0, s1);
       s0 = wave_sum(s0);
       s1 = wave_sum(s1);
-      const float step = (s0 - 1.f) / (gm * s1);
+      const float step = (s0 - 1.f) * __builtin_amdgcn_rcpf(gm * s1);
       if (!(step > 1e-2f)) break;
       lo += step;
     }
-    if (lane == 0) red[1][0][w] = lo;
-    __syncthreads();
-    lo = fmaxf(fmaxf(red[1][0][0], red[1][0][1]), fmaxf(red[1][0][2], red[1][0][3]));
-    turn = 0;
-    for (int it = 0; it < 2; ++it) {
+    if constexpr (SO_WAVES > 1) {
+      lo = max_waves(lo);
       float s0 = 0.f, s1 = 0.f, s2 = 0.f;
       sums(s0, s1);
       sum3(s0, s1, s2);
-      const float step = (s0 - 1.f) / (gm * s1);
+      const float step = (s0 - 1.f) * __builtin_amdgcn_rcpf(gm * s1);
       if (step > 0.f) lo += step;
     }
   }
@@ -348,34 +368,29 @@ __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
 
   // ---- the blocks with a score above the bound, and those scores
   int nb = 0, mine = 0;
-#pragma unroll
-  for (int j = 0; j < SO_MAXIMA; ++j) {
-    if (j * SO_NT >= row.blocks) break;
-    mine += relu_z(c, top[j], lo) > 0.f ? 1 : 0;
-  }
+  each_top([&](float v, int) { mine += relu_z(c, v, lo) > 0.f ? 1 : 0; });
   int to = place(mine, nb);
-#pragma unroll
-  for (int j = 0; j < SO_MAXIMA; ++j) {
-    if (j * SO_NT >= row.blocks) break;
-    if (relu_z(c, top[j], lo) > 0.f) chosen[to++] = (uint16_t)(j * SO_NT + t);
-  }
+  each_top([&](float v, int x) {
+    if (relu_z(c, v, lo) > 0.f) chosen[to++] = (uint16_t)x;
+  });
   __syncthreads();
   // ---- the quads with a score above the bound: eight threads to a block
   constexpr int BPS = SO_NT / 8;  // blocks a step
   int nq = 0;
   for (int s0 = 0; s0 < nb; s0 += BPS * SO_STEPS) {
-    int mine = 0;
-    bool in[SO_STEPS];
+    float q[SO_STEPS];
 #pragma unroll
     for (int u = 0; u < SO_STEPS; ++u) {
       const int x = s0 + u * BPS + (t >> 3);
-      in[u] = x < nb && relu_z(c, row.quads(chosen[min(x, nb - 1)])[t & 7], lo) > 0.f;
-      mine += in[u] ? 1 : 0;
+      q[u] = x < nb ? row.quads(chosen[x])[t & 7] : -INFINITY;
     }
+    int mine = 0;
+#pragma unroll
+    for (int u = 0; u < SO_STEPS; ++u) mine += relu_z(c, q[u], lo) > 0.f ? 1 : 0;
     int at = place(mine, nq);
 #pragma unroll
     for (int u = 0; u < SO_STEPS; ++u)
-      if (in[u]) {
+      if (relu_z(c, q[u], lo) > 0.f) {
         if (at < SO_QUADS) quad[at] = (uint16_t)(chosen[s0 + u * BPS + (t >> 3)] * (DEC_KEYS / 4) + quad_at(t & 7));
         ++at;
       }
@@ -388,42 +403,51 @@ __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
   const E* const pre_k = static_cast<const E*>(a.pk) + kv * a.pk_head;
   float qv[VPL];
   R::unpack(R::load(static_cast<const E*>(a.q) + b * a.q_row + h * a.q_head, 0u), qv);
-  // Scores of four keys from key 4 x on (counted over all blocks), the same in all lanes of the group.
-  auto quad_scores = [&](int x) {
-    const int blk = x / (DEC_KEYS / 4);
-    const bool shared = blk < p_blocks;
-    const int k0 = 4 * x - (shared ? 0 : p_blocks * DEC_KEYS), end = shared ? a.prefix : len;
-    const E* const base = shared ? pre_k : own_k;
-    const int64_t ld = shared ? a.pk_row : a.k_row;
-    u32x4 kw[4];
+  // store(i, scores) of the quads number(i), i < n (four keys each, from key 4
+  // number(i) on, counted over all blocks): two at a time, by the first lane of a group.
+  auto quad_scores = [&](int n, auto&& number, auto&& store) {
+    for (int x0 = grp; x0 < n; x0 += 2 * NG) {
+      u32x4 kw[2][4];
+      int left[2];  // keys from the quad's first to the end
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      kw[e] = *reinterpret_cast<const u32x4*>(base + min(k0 + e, end - 1) * ld + sub * VPL);
-    f32x4 s;
+      for (int u = 0; u < 2; ++u) {
+        const int q = number(min(x0 + u * NG, n - 1));
+        const bool shared = q < p_blocks * (DEC_KEYS / 4);
+        const int k0 = 4 * q - (shared ? 0 : p_blocks * DEC_KEYS);
+        left[u] = (shared ? a.prefix : len) - k0;
+        const E* const base = (shared ? pre_k : own_k) + sub * VPL;
+        const int64_t ld = shared ? a.pk_row : a.k_row;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float x2[VPL], dot = 0.f;
-      R::unpack(kw[e], x2);
+        for (int e = 0; e < 4; ++e)
+          kw[u][e] = *reinterpret_cast<const u32x4*>(base + (k0 + min(e, left[u] - 1)) * ld);
+      }
 #pragma unroll
-      for (int d = 0; d < VPL; ++d) dot = fmaf(qv[d], x2[d], dot);
-      dot = R::sum(dot);
-      s[e] = k0 + e < end ? dot : -INFINITY;
+      for (int u = 0; u < 2; ++u) {
+        f32x4 s;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float x2[VPL], dot = 0.f;
+          R::unpack(kw[u][e], x2);
+#pragma unroll
+          for (int d = 0; d < VPL; ++d) dot = fmaf(qv[d], x2[d], dot);
+          dot = R::sum(dot);
+          s[e] = e < left[u] ? dot : -INFINITY;
+        }
+        if (sub == 0 && x0 + u * NG < n) store(x0 + u * NG, s);
+      }
     }
-    return s;
   };
   float* const spill = a.spill + ((int64_t)b * a.heads + h) * (int64_t)(p_blocks + own_cap) * DEC_KEYS;
-  if (!wide) {
-    for (int x = grp; x < nq; x += NG) {
-      const f32x4 s = quad_scores(quad[x]);
-      if (sub == 0) *reinterpret_cast<f32x4*>(kept + 4 * x) = s;
-    }
-  } else {
-    for (int x = grp; x < nb * (DEC_KEYS / 4); x += NG) {
-      const int q = chosen[x / (DEC_KEYS / 4)] * (DEC_KEYS / 4) + x % (DEC_KEYS / 4);
-      const f32x4 s = quad_scores(q);
-      if (sub == 0) *reinterpret_cast<f32x4*>(spill + 4 * (int64_t)q) = s;
-    }
-  }
+  if (!wide)
+    quad_scores(nq, [&](int i) { return (int)quad[i]; },
+                [&](int i, const f32x4& s) { *reinterpret_cast<f32x4*>(kept + 4 * i) = s; });
+  else
+    quad_scores(nb * (DEC_KEYS / 4),
+                [&](int i) { return chosen[i / (DEC_KEYS / 4)] * (DEC_KEYS / 4) + i % (DEC_KEYS / 4); },
+                [&](int i, const f32x4& s) {
+                  *reinterpret_cast<f32x4*>(spill + (int64_t)chosen[i / (DEC_KEYS / 4)] * DEC_KEYS +
+                                            4 * (i % (DEC_KEYS / 4))) = s;
+                });
   __syncthreads();
   const int total = 4 * nq;
   // scores of chosen block x, four to each of eight threads (wide rows)
@@ -445,7 +469,10 @@ __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
     float s0 = 0.f, s1 = 0.f, s2 = 0.f;
     if (alone) {
 #pragma unroll
-      for (int e = 0; e < SO_LANE; ++e) add(relu_z(c, x[e], tau), s0, s1, s2);
+      for (int e = 0; e < SO_LANE; ++e) {
+        if (64 * e >= total) break;
+        add(relu_z(c, x[e], tau), s0, s1, s2);
+      }
       s0 = wave_sum(s0);
       s1 = wave_sum(s1);
       s2 = wave_sum(s2);
@@ -486,7 +513,7 @@ __global__ __launch_bounds__(SO_NT) void decode_solve_kernel(DecodeArgs a) {
   const E* const pre_v = static_cast<const E*>(a.pv) + kv * a.pv_head;
   // of n kept scores, those at 4 i of the keys from 4 first(i) on
   auto gather = [&](int n, auto&& first) {
-    constexpr int BATCH = 4;
+    constexpr int BATCH = 8;
     for (int y0 = grp; y0 < n; y0 += NG * BATCH) {
       u32x4 v[BATCH];
       float p[BATCH];
@@ -560,6 +587,15 @@ hipError_t launch_maxima(const DecodeArgs& a, hipStream_t s) {
                          params, 0, s);
 }
 
+template <typename E, int D, int NT>
+hipError_t launch_solve(const DecodeArgs& a, hipStream_t s) {
+  auto kernel = decode_solve_kernel<E, D, 0, NT>;
+  if (a.gk == 1) kernel = decode_solve_kernel<E, D, 1, NT>;
+  if (a.gk == 2) kernel = decode_solve_kernel<E, D, 2, NT>;
+  if (a.gk == 4) kernel = decode_solve_kernel<E, D, 4, NT>;
+  return launch_kernel(kernel, dim3((unsigned)(a.requests * a.heads)), dim3(NT), s, a);
+}
+
 template <typename E, int D>
 hipError_t launch_decode_d(const DecodeArgs& a, hipStream_t s) {
   const int rows = a.requests * a.group;
@@ -571,11 +607,11 @@ hipError_t launch_decode_d(const DecodeArgs& a, hipStream_t s) {
   else
     e = launch_maxima<E, D, 1>(a, s);
   if (e != hipSuccess) return e;
-  auto kernel = decode_solve_kernel<E, D, 0>;
-  if (a.gk == 1) kernel = decode_solve_kernel<E, D, 1>;
-  if (a.gk == 2) kernel = decode_solve_kernel<E, D, 2>;
-  if (a.gk == 4) kernel = decode_solve_kernel<E, D, 4>;
-  return launch_kernel(kernel, dim3((unsigned)(a.requests * a.heads)), dim3(SO_NT), s, a);
+  // Rows for two waves on every compute unit have one each, few or long ones
+  // four: 2048 rows of 260 to 288 blocks 31 us against 37, 1024 rows of 2050
+  // blocks 33 against 23 (a wave then holds half of its maxima in registers).
+  const bool one = a.requests * a.heads >= 512 && a.prefix_runs + a.own_runs <= SO_MAXIMA * 64 / 2 / DEC_RUN;
+  return one ? launch_solve<E, D, 64>(a, s) : launch_solve<E, D, 256>(a, s);
 }
 
 }  // namespace

@@ -133,9 +133,13 @@ __device__ __forceinline__ void angles(const RotaryArgs& a, int token, float2* t
     for (int x = 0; x + 1 < ROT_MAX_AXES; ++x) axis += x + 1 < a.axes && p >= a.axis_end[x] ? 1 : 0;
     const double turns = (double)a.positions[(size_t)axis * a.position_stride + token] *
                          ((double)a.freqs[p] * 0.15915494309189535);
+    // the nearest quarter turn apart, so that fp32 holds the rest with an error
+    // of 2^-28 turns at most
+    const double quarters = rint(4.0 * turns);
+    const int q = (int)(quarters - 4.0 * floor(0.25 * quarters));
     float s, c;
-    sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
-    table[p] = make_float2(c, s);
+    sincospif(2.f * (float)(turns - 0.25 * quarters), &s, &c);
+    table[p] = q == 0 ? make_float2(c, s) : q == 1 ? make_float2(-s, c) : q == 2 ? make_float2(-c, -s) : make_float2(s, -c);
   }
 }
 
@@ -309,19 +313,33 @@ __global__ __launch_bounds__(ROT_NT) void rotary_bwd_kernel(RotaryArgs a) {
 }
 
 // dw from the workgroups' partials: 16 values per workgroup, each the sum of
-// 16 threads' sums over every 16th partial.
-constexpr int DW_NT = 256;
+// 64 threads' sums over every 64th partial (at most 16 loads each, all in
+// flight at once: 1024 partials of 2 x 128 values in XX us, with a quarter of
+// the threads 20).
+constexpr int DW_NT = 1024;
+constexpr int DW_ROWS = DW_NT / 16;
 __global__ __launch_bounds__(DW_NT) void rotary_dw_kernel(RotaryArgs a) {
-  __shared__ float part[16][17];
+  __shared__ float part[DW_ROWS][17];
   const int c = threadIdx.x & 15, r = threadIdx.x >> 4, width = 2 * a.d, col = blockIdx.x * 16 + c;
-  float s = 0.f;
-  for (int x = r; x < a.partial_count; x += 16) s += a.partials[(size_t)x * width + col];
+  static_assert(ROT_MAX_PARTIALS <= 16 * DW_ROWS, "sixteen loads a thread");
+  float s = 0.f, v[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int x = r + i * DW_ROWS;
+    v[i] = x < a.partial_count ? a.partials[(size_t)x * width + col] : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s += v[i];
   part[r][c] = s;
   __syncthreads();
+#pragma unroll
+  for (int half = DW_ROWS / 2; half >= 1; half /= 2) {
+    if (r < half) part[r][c] += part[r + half][c];
+    __syncthreads();
+  }
   if (r == 0) {
-    for (int x = 1; x < 16; ++x) s += part[x][c];
     float* out = col < a.d ? a.dq_weight : a.dk_weight;
-    if (out) out[col < a.d ? col : col - a.d] = s;
+    if (out) out[col < a.d ? col : col - a.d] = part[0][c];
   }
 }
 
