@@ -25,6 +25,7 @@ and one decoding step, for requests that share a prefix:
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import threading
 
@@ -824,7 +825,7 @@ def _strided(t, name, shape, dtype, device, written=False):
     bytes; a tensor to be written must not hold an element twice."""
     if not isinstance(t, torch.Tensor):
         raise ValueError("%s must be a torch tensor" % name)
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
     if t.dtype != dtype:
         raise ValueError("%s has dtype %s, expected %s" % (name, t.dtype, dtype))
@@ -833,11 +834,15 @@ def _strided(t, name, shape, dtype, device, written=False):
     if t.numel() == 0:
         return
     vec = 16 // t.element_size()
+    if t.is_contiguous() and shape[-1] % vec == 0 and t.data_ptr() % 16 == 0:
+        return
     if t.stride(-1) != 1:
         raise ValueError("%s must be contiguous in its last dimension" % name)
-    # (the stride of a dimension of one element is never used)
-    used = [s for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n > 1]
-    if t.data_ptr() % 16 or any(s % vec for s in used):
+    bad = t.data_ptr() % 16
+    for n, step in zip(t.shape, t.stride()[:-1]):  # (the stride of a dimension of one element is never used)
+        if n > 1 and step % vec:
+            bad = 1
+    if bad:
         raise ValueError("%s: rows must start at multiples of 16 bytes" % name)
     if written:
         # each dimension steps over all of the smaller ones
@@ -852,8 +857,16 @@ def _stride(t, dim):
     return t.stride(dim) if t.shape[dim] > 1 else 0
 
 
+# Argument structures are built once for each set of sizes that a program uses:
+# a call at the sizes of a decoding step is a few microseconds of host time,
+# and each structure one or two.  They are never written to afterwards.
+@functools.lru_cache(maxsize=1024)
+def _strides_of(row, head):
+    return Strides(row, head)
+
+
 def _row_head(t, row=0, head=1):
-    return Strides(_stride(t, row), _stride(t, head))
+    return _strides_of(_stride(t, row), _stride(t, head))
 
 
 def _ptr(t):
@@ -871,20 +884,21 @@ def _overlap(a, b):
     return a0 < b1 and b0 < a1
 
 
-class _on_device:
-    """Makes a device current for a call where it is not (a launch goes to a
-    stream of the current device)."""
-
-    def __init__(self, device):
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-
+class _SameDevice:
     def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
+        pass
 
     def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+        pass
+
+
+_same_device = _SameDevice()
+
+
+def _on_device(device):
+    """Makes a device current for a call where it is not (a launch goes to a
+    stream of the current device)."""
+    return _same_device if device.index == torch._C._cuda_getDevice() else torch.cuda.device(device)
 
 
 # ------------------------------------------------------ norm and rotation
@@ -899,35 +913,43 @@ def _check_rotary(q, k, positions, freqs, q_weight, k_weight, sections, eps, int
     hk, dev = k.shape[1], q.device
     _strided(q, "q", q.shape, q.dtype, dev)
     _strided(k, "k", (tokens, hk, d), q.dtype, dev)
-    if not isinstance(freqs, torch.Tensor) or freqs.dim() != 1:
-        raise ValueError("freqs must be a [rot_dim / 2] tensor")
-    _need(freqs, "freqs", freqs.shape, torch.float32, dev)
+    if not isinstance(freqs, torch.Tensor) or freqs.dim() != 1 or not freqs.is_contiguous():
+        raise ValueError("freqs must be a contiguous [rot_dim / 2] tensor")
+    if freqs.dtype != torch.float32 or freqs.device != dev:
+        raise ValueError("freqs has dtype %s on %s, expected float32 on %s" % (freqs.dtype, freqs.device, dev))
     pairs = freqs.shape[0]
     sections = (pairs,) if sections is None else tuple(int(s) for s in sections)
     if not 1 <= len(sections) <= 4 or min(sections) < 0 or sum(sections) != pairs:
         raise ValueError("sections must be 1 to 4 numbers of pairs that add up to len(freqs) = %d" % pairs)
     if 2 * pairs > d or pairs % 8:
         raise ValueError("freqs must hold a multiple of 8 pairs, at most half of head_dim")
-    shape = (len(sections), tokens)
-    if not isinstance(positions, torch.Tensor) or tuple(positions.shape) not in ((shape,) if len(sections) > 1
-                                                                                 else (shape, (tokens,))):
-        raise ValueError("positions must be a %s tensor" % (list(shape),))
+    axes = len(sections)
+    if not isinstance(positions, torch.Tensor) or not (
+            positions.shape == (axes, tokens) or (axes == 1 and positions.shape == (tokens,))):
+        raise ValueError("positions must be a %s tensor" % ([axes, tokens],))
     if positions.dtype != torch.int32 or positions.device != dev:
         raise ValueError("positions must be int32 and on %s" % dev)
     if tokens > 1 and positions.stride(-1) != 1:
         raise ValueError("positions must be contiguous in its last dimension")
-    weights = [(n, w) for n, w in (("q_weight", q_weight), ("k_weight", k_weight)) if w is not None]
     wt = q.dtype
-    for name, w in weights:
-        wt = weights[0][1].dtype if isinstance(weights[0][1], torch.Tensor) else None
+    given = [(n, w) for n, w in (("q_weight", q_weight), ("k_weight", k_weight)) if w is not None]
+    if given:
+        wt = given[0][1].dtype if isinstance(given[0][1], torch.Tensor) else None
         if wt not in (q.dtype, torch.float32):
             raise ValueError("weights must have the dtype of q, or be float32")
-        _need(w, name, (d,), wt, dev)
-        if w.data_ptr() % 16:
-            raise ValueError("%s must start at a multiple of 16 bytes" % name)
-    r = Rotary(tokens, hq, hk, d, dt, EA_F32 if wt == torch.float32 else EA_BF16, 2 * pairs,
-               int(bool(interleaved)), len(sections), (ctypes.c_int32 * 4)(*sections), float(eps))
+        for name, w in given:
+            _need(w, name, (d,), wt, dev)
+            if w.data_ptr() % 16:
+                raise ValueError("%s must start at a multiple of 16 bytes" % name)
+    r = _rotary_of(tokens, hq, hk, d, dt, EA_F32 if wt == torch.float32 else EA_BF16, 2 * pairs, bool(interleaved),
+                   sections, float(eps))
     return r, positions.stride(0) if positions.dim() == 2 else 0
+
+
+@functools.lru_cache(maxsize=256)
+def _rotary_of(tokens, hq, hk, d, dt, weight_dt, rot, interleaved, sections, eps):
+    return Rotary(tokens, hq, hk, d, dt, weight_dt, rot, int(interleaved), len(sections),
+                  (ctypes.c_int32 * 4)(*sections), eps)
 
 
 def norm_rotary(q, k, positions, freqs, q_weight=None, k_weight=None, sections=None, eps=1e-6,
@@ -943,18 +965,22 @@ def norm_rotary(q, k, positions, freqs, q_weight=None, k_weight=None, sections=N
     gives the number of consecutive pairs that each axis rotates.
     q_out, k_out: tensors to write, which may be q and k themselves."""
     r, pos_stride = _check_rotary(q, k, positions, freqs, q_weight, k_weight, sections, eps, interleaved)
-    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
-    k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
     for name, out, like in (("q_out", q_out, q), ("k_out", k_out, k)):
+        if out is None:
+            continue
         _strided(out, name, like.shape, like.dtype, like.device, written=True)
         for other_name, t in (("q", q), ("k", k)):
             if _overlap(out, t) and not (t is like and out.data_ptr() == t.data_ptr() and out.stride() == t.stride()):
                 if not _apart(out, t):
                     raise ValueError("%s overlaps %s" % (name, other_name))
+    if q_out is not None and k_out is not None and _overlap(q_out, k_out) and not _apart(q_out, k_out):
+        raise ValueError("q_out overlaps k_out")
     _on_gpu(q.device)
     with _on_device(q.device):
+        q_out = q.new_empty(q.shape) if q_out is None else q_out
+        k_out = k.new_empty(k.shape) if k_out is None else k_out
         _check(_lib.entmax_norm_rotary(
-            ctypes.byref(r), q.data_ptr(), _row_head(q), k.data_ptr(), _row_head(k), positions.data_ptr(),
+            r, q.data_ptr(), _row_head(q), k.data_ptr(), _row_head(k), positions.data_ptr(),
             pos_stride, freqs.data_ptr(), _ptr(q_weight), _ptr(k_weight), q_out.data_ptr(), _row_head(q_out),
             k_out.data_ptr(), _row_head(k_out), _stream_handle(q.device)), "entmax_norm_rotary")
     return q_out, k_out
@@ -983,16 +1009,15 @@ def norm_rotary_backward(dq_out, dk_out, q, k, positions, freqs, q_weight=None, 
     _strided(dk_out, "dk_out", k.shape, q.dtype, q.device)
     _on_gpu(q.device)
     with _on_device(q.device):
-        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        dk = torch.empty(k.shape, dtype=k.dtype, device=q.device)
+        dq, dk = q.new_empty(q.shape), k.new_empty(k.shape)
         make = torch.empty if q.shape[0] else torch.zeros
         dwq, dwk = (None if w is None else make(q.shape[-1], dtype=torch.float32, device=q.device)
                     for w in (q_weight, k_weight))
         n = ctypes.c_size_t()
-        _check(_lib.entmax_norm_rotary_workspace(ctypes.byref(r), ctypes.byref(n)), "entmax_norm_rotary_workspace")
+        _check(_lib.entmax_norm_rotary_workspace(r, ctypes.byref(n)), "entmax_norm_rotary_workspace")
         ws = torch.empty(max(n.value, 16), dtype=torch.uint8, device=q.device)
         _check(_lib.entmax_norm_rotary_bwd(
-            ctypes.byref(r), dq_out.data_ptr(), _row_head(dq_out), dk_out.data_ptr(), _row_head(dk_out),
+            r, dq_out.data_ptr(), _row_head(dq_out), dk_out.data_ptr(), _row_head(dk_out),
             q.data_ptr(), _row_head(q), k.data_ptr(), _row_head(k), positions.data_ptr(), pos_stride,
             freqs.data_ptr(), _ptr(q_weight), _ptr(k_weight), dq.data_ptr(), dk.data_ptr(), _ptr(dwq),
             _ptr(dwk), ws.data_ptr(), ws.numel(), _stream_handle(q.device)), "entmax_norm_rotary_bwd")
@@ -1081,11 +1106,31 @@ def _packed_shape(q, k, v, plan):
     _strided(q, "q", q.shape, q.dtype, q.device)
     _strided(k, "k", (tokens, hk, d), q.dtype, q.device)
     _strided(v, "v", (tokens, hk, d), q.dtype, q.device)
-    return PackedShape(tokens, plan.seqs, plan.max_seqlen, hq, hk, d, dt)
+    return _packed_shape_of(tokens, plan.seqs, plan.max_seqlen, hq, hk, d, dt)
 
 
-def _packed_strides(q, k, v, o):
-    return PackedStrides(_row_head(q), _row_head(k), _row_head(v), _row_head(o))
+@functools.lru_cache(maxsize=256)
+def _packed_shape_of(*sizes):
+    return PackedShape(*sizes)
+
+
+def _packed_strides(*tensors):
+    return _packed_strides_of(*[s for t in tensors for s in (_stride(t, 0), _stride(t, 1))])
+
+
+@functools.lru_cache(maxsize=1024)
+def _packed_strides_of(*s):
+    return PackedStrides(*[Strides(s[i], s[i + 1]) for i in range(0, 8, 2)])
+
+
+@functools.lru_cache(maxsize=256)
+def _packed_params(alpha, scale, causal, need_bwd, max_iter, tol, head_dim, *shape):
+    """(Params, PackedSizes) of a call."""
+    params = make_params(alpha, scale, causal, need_bwd, max_iter, tol, head_dim=head_dim)
+    sizes = PackedSizes()
+    _check(_lib.entmax_packed_sizes(_packed_shape_of(*shape), ctypes.byref(params), ctypes.byref(sizes)),
+           "entmax_packed_sizes")
+    return params, sizes
 
 
 def packed_forward(q, k, v, plan: PackedPlan, alpha=1.5, scale=None, need_bwd=True, max_iter=None, tol=None,
@@ -1103,10 +1148,9 @@ def packed_forward(q, k, v, plan: PackedPlan, alpha=1.5, scale=None, need_bwd=Tr
     shape = _packed_shape(q, k, v, plan)
     if tol is None and shape.dtype == EA_F32:
         tol = 1e-6  # (Sum p is off by up to tol, which the fp32 outputs show)
-    params = make_params(alpha, scale, plan.causal, need_bwd, max_iter, tol, head_dim=q.shape[-1])
-    sizes = PackedSizes()
-    _check(_lib.entmax_packed_sizes(ctypes.byref(shape), ctypes.byref(params), ctypes.byref(sizes)),
-           "entmax_packed_sizes")
+    params, sizes = _packed_params(alpha, scale, plan.causal, bool(need_bwd), max_iter, tol, q.shape[-1],
+                                   shape.tokens, shape.seqs, shape.max_seqlen, shape.heads, shape.kv_heads,
+                                   shape.head_dim, shape.dtype)
     made = out is None
     if not made:
         _strided(out, "out", q.shape, q.dtype, q.device, written=True)
@@ -1118,14 +1162,14 @@ def packed_forward(q, k, v, plan: PackedPlan, alpha=1.5, scale=None, need_bwd=Tr
     _on_gpu(q.device)
     with _on_device(q.device):
         if made:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = q.new_empty(q.shape)
         res = PackedResiduals(shape, params, plan, sizes, q.device, lists)
         if workspace is None:
             workspace = torch.empty(max(sizes.ws_fwd, 16), dtype=torch.uint8, device=q.device)
         ws, ws_bytes = (None, 0) if workspace is False else (workspace.data_ptr(),
                                                             workspace.numel() * workspace.element_size())
         _check(_lib.entmax_packed_fwd(
-            ctypes.byref(shape), ctypes.byref(params), plan.buffer.data_ptr(), q.data_ptr(), k.data_ptr(),
+            shape, params, plan.buffer.data_ptr(), q.data_ptr(), k.data_ptr(),
             v.data_ptr(), out.data_ptr(), _packed_strides(q, k, v, out), int(made), res.buffer.data_ptr(),
             res.buffer.numel(), *res.lists_ptr(), ws, ws_bytes, _stream_handle(q.device)), "entmax_packed_fwd")
     return out, res
@@ -1167,13 +1211,13 @@ def packed_backward(q, k, v, dout, res: PackedResiduals, dq=None, dk=None, dv=No
     _on_gpu(q.device)
     with _on_device(q.device):
         if made:
-            dq, dk, dv = (torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v))
+            dq, dk, dv = (t.new_empty(t.shape) for t in (q, k, v))
         if workspace is None and res.lists is not None:
             workspace = _bytes_or_none(res.sizes.ws_bwd_lists, q.device)
         if workspace is None:
             workspace = torch.empty(res.sizes.ws_bwd, dtype=torch.uint8, device=q.device)
         _check(_lib.entmax_packed_bwd(
-            ctypes.byref(shape), ctypes.byref(res.params), res.plan.buffer.data_ptr(), q.data_ptr(),
+            shape, res.params, res.plan.buffer.data_ptr(), q.data_ptr(),
             k.data_ptr(), v.data_ptr(), dout.data_ptr(), _packed_strides(q, k, v, dout), int(made),
             res.buffer.data_ptr(), res.buffer.numel(), *res.lists_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
             workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_handle(q.device)),
@@ -1186,12 +1230,22 @@ def packed_backward(q, k, v, dout, res: PackedResiduals, dq=None, dk=None, dv=No
 def prefix_decode_workspace(q, k_cache, prefix=0):
     """Bytes of the workspace of prefix_decode for these tensors and a prefix of
     that many keys (about 5 bytes for every query head and key)."""
-    shape = DecodeShape(q.shape[0], q.shape[1], k_cache.shape[2], q.shape[2], _ea_dtype(q, "q"), int(prefix),
-                        k_cache.shape[1])
-    n = ctypes.c_size_t()
-    _check(_lib.entmax_prefix_decode_workspace(ctypes.byref(shape), ctypes.byref(n)),
-           "entmax_prefix_decode_workspace")
-    return n.value
+    return _decode_of(1.5, None, None, None, q.shape[0], q.shape[1], k_cache.shape[2], q.shape[2],
+                      _ea_dtype(q, "q"), int(prefix), k_cache.shape[1])[2]
+
+
+@functools.lru_cache(maxsize=256)
+def _decode_of(alpha, scale, max_iter, tol, *sizes):
+    """(DecodeShape, Params, bytes of the workspace) of a call."""
+    shape, n = DecodeShape(*sizes), ctypes.c_size_t()
+    params = make_params(alpha, scale, False, False, max_iter, tol, head_dim=shape.head_dim)
+    _check(_lib.entmax_prefix_decode_workspace(shape, ctypes.byref(n)), "entmax_prefix_decode_workspace")
+    return shape, params, n.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _decode_strides_of(*s):
+    return DecodeStrides(*[Strides(s[i], s[i + 1]) for i in range(0, 12, 2)], s[12], s[13])
 
 
 def prefix_decode(q, k_cache, v_cache, lengths, k_prefix=None, v_prefix=None, alpha=1.5, scale=None,
@@ -1234,25 +1288,22 @@ def prefix_decode(q, k_cache, v_cache, lengths, k_prefix=None, v_prefix=None, al
                         ("v_prefix", v_prefix)):
             if t is not None and _overlap(out, t):
                 raise ValueError("out overlaps %s" % name)
-    params = make_params(alpha, scale, False, False, max_iter, 1e-6 if tol is None else tol, head_dim=d)
-    shape = DecodeShape(B, hq, hk, d, dt, P, cap)
-    n = ctypes.c_size_t()
-    _check(_lib.entmax_prefix_decode_workspace(ctypes.byref(shape), ctypes.byref(n)),
-           "entmax_prefix_decode_workspace")
+    shape, params, nbytes = _decode_of(alpha, scale, max_iter, 1e-6 if tol is None else tol, B, hq, hk, d, dt, P, cap)
     if workspace is not None:
-        _check_bytes(workspace, "workspace", n.value, dev)
+        _check_bytes(workspace, "workspace", nbytes, dev)
     _on_gpu(dev)
-    none = Strides(0, 0)
     with _on_device(dev):
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+            out = q.new_empty(q.shape)
         if workspace is None:
-            workspace = torch.empty(max(n.value, 16), dtype=torch.uint8, device=dev)
-        strides = DecodeStrides(_row_head(q), _row_head(out), _row_head(k_cache, 1, 2), _row_head(v_cache, 1, 2),
-                                none if P == 0 else _row_head(k_prefix), none if P == 0 else _row_head(v_prefix),
-                                _stride(k_cache, 0), _stride(v_cache, 0))
+            workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=dev)
+        kp, vp = (q, q) if P == 0 else (k_prefix, v_prefix)  # (without a prefix, not read)
+        strides = _decode_strides_of(
+            _stride(q, 0), _stride(q, 1), _stride(out, 0), _stride(out, 1), _stride(k_cache, 1), _stride(k_cache, 2),
+            _stride(v_cache, 1), _stride(v_cache, 2), _stride(kp, 0), _stride(kp, 1), _stride(vp, 0), _stride(vp, 1),
+            _stride(k_cache, 0), _stride(v_cache, 0))
         _check(_lib.entmax_prefix_decode(
-            ctypes.byref(shape), ctypes.byref(params), strides, q.data_ptr(), k_cache.data_ptr(),
+            shape, params, strides, q.data_ptr(), k_cache.data_ptr(),
             v_cache.data_ptr(), lengths.data_ptr(), _ptr(k_prefix), _ptr(v_prefix), out.data_ptr(),
             workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_handle(dev)),
             "entmax_prefix_decode")
