@@ -404,8 +404,8 @@ ea_status entmax_packed_sizes(const ea_packed_shape* shape, const ea_params* par
  * strides strides->o.  dq [tokens, heads, d], dk and dv [tokens, kv_heads, d]
  * are contiguous and of the inputs' dtype (each rounded once, from fp32 sums).
  * Rows that belong to no sequence (before cu[0], behind cu[seqs]) are left as
- * they are, or with zero_rest != 0 set to 0.  Launches: 2 (forward; the solver
- * one more per workspace slot count), 3 or 4 (backward; with lists 4).
+ * they are, or with zero_rest != 0 set to 0.  Launches: 2 (forward), 3 or 4
+ * (backward).
  */
 ea_status entmax_packed_fwd(const ea_packed_shape* shape, const ea_params* params, const void* plan,
                             const void* q, const void* k, const void* v, void* o,

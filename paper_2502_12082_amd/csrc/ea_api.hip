@@ -752,7 +752,7 @@ size_t plan_parts(int32_t tokens, int32_t seqs, void* base, PlanArgs* a) {
   Parts p{static_cast<char*>(base)};
   a->header = p.take<PackedHeader>(1);
   a->seqs = p.take<PackedSeq>((size_t)seqs);
-  for (int z = 0; z < 3; ++z) a->tiles[z] = p.take<PackedTile>((size_t)packed_tiles(tokens, seqs, z));
+  for (int z = 0; z < 2; ++z) a->tiles[z] = p.take<PackedTile>((size_t)packed_tiles(tokens, seqs, z));
   return p.at;
 }
 
@@ -811,9 +811,11 @@ int packed_parts(const ea_packed_shape* s) {
   return dkdv_packed_parts(s->tokens, s->seqs, s->heads, s->kv_heads, s->dtype, s->head_dim);
 }
 
-size_t packed_ws_fwd(const ea_packed_shape* s) {
-  const int64_t tiles = (int64_t)s->heads * packed_tiles(s->tokens, s->seqs, 2);
-  return (size_t)(tiles < MAX_SOLVE_SLOTS ? tiles : MAX_SOLVE_SLOTS) * SOLVE_SLOT_BYTES;
+// The solver's workgroups of 128 rows use half a slot each, and no more of them
+// run at a time than PACKED_SOLVERS.
+int64_t packed_slots(const ea_packed_shape* s) {
+  const int64_t tiles = (int64_t)s->heads * packed_tiles(s->tokens, s->seqs, 1);
+  return ((tiles < PACKED_SOLVERS ? tiles : PACKED_SOLVERS) + 1) / 2;
 }
 // The backward's workspace: delta, the parts of dK and dV where there are some
 // (with element lists always, and one more), and with lists their buckets.
@@ -854,7 +856,7 @@ PackedArgs packed_args(const ea_packed_shape* s, const void* plan, const ea_pack
   PackedArgs a{};
   a.header = parts.header;
   a.seqs = parts.seqs;
-  for (int z = 0; z < 3; ++z) a.lists[z] = parts.tiles[z];
+  for (int z = 0; z < 2; ++z) a.lists[z] = parts.tiles[z];
   a.seq_count = s->seqs;
   a.heads = s->heads;
   a.kv_heads = s->kv_heads;
@@ -918,7 +920,7 @@ ea_status entmax_packed_sizes(const ea_packed_shape* shape, const ea_params* par
   if (!out) return EA_ERR_INVALID_ARG;
   PackedResiduals r;
   out->residuals = residual_parts(shape, params, nullptr, &r);
-  out->ws_fwd = packed_ws_fwd(shape);
+  out->ws_fwd = (size_t)packed_slots(shape) * SOLVE_SLOT_BYTES;
   out->lists = packed_lists_bytes(shape);
   PackedBwdWs w;
   out->ws_bwd = packed_ws_bwd(shape, false, nullptr, &w);
@@ -937,7 +939,7 @@ ea_status entmax_packed_fwd(const ea_packed_shape* shape, const ea_params* param
   if ((st = check_packed_lists(shape, lists, lists_bytes)) != EA_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const PackedArgs pk = packed_args(shape, plan, strides, zero_rest);
-  const int64_t most = (int64_t)shape->heads * packed_tiles(shape->tokens, shape->seqs, 2);
+  const int64_t most = packed_slots(shape);
   int64_t slots = workspace ? (int64_t)(ws_bytes / SOLVE_SLOT_BYTES) : 0;
   if (slots > most) slots = most;
   Packed<TauArgs> ta{};

@@ -95,8 +95,8 @@ __host__ __device__ inline int list_use(int entries, int blocks, int T, bool f32
 #endif
 
 // Packed sequences: rows [start, start + len) of [tokens, heads, D] tensors,
-// `group` query heads to a key head.  The sequences' tiles of 64, 128 and 256
-// rows are listed by plan_kernel (ea_packed.hip), those with the most keys
+// `group` query heads to a key head.  The sequences' tiles of 64 and 128 rows
+// are listed by plan_kernel (ea_packed.hip), those with the most keys
 // first; a launch takes one workgroup per head and possible tile (the host
 // does not know their number), and those beyond the list return.  Tables and
 // statistics are per query head: tau of head h and token t at h tokens + t,
@@ -113,14 +113,13 @@ struct PackedTile {
   int32_t seq, tile;
 };
 struct PackedHeader {
-  int32_t count[3];    // tiles of 64, 128 and 256 rows
+  int32_t count[2];    // tiles of 64 and 128 rows
   int32_t begin, end;  // the rows that belong to sequences
-  int32_t unused[3];
 };
 struct PackedArgs {
   const PackedHeader* header;
   const PackedSeq* seqs;
-  const PackedTile* lists[3];  // of 64, 128 and 256 rows
+  const PackedTile* lists[2];  // of 64 and 128 rows
   const PackedTile* tiles;     // those of this launch, 64 << size rows
   int size, seq_count;
   int heads, kv_heads, group, tokens, blocks, width;
@@ -139,6 +138,9 @@ struct Packed : A {
   PackedArgs pk;
 };
 
+// Workgroups of the packed solver that run at a time: three on each of 256
+// compute units.
+constexpr int PACKED_SOLVERS = 768;
 // The most tiles of 64 << size rows that `seqs` sequences of `tokens` rows in
 // all can have.
 constexpr int packed_tiles(int tokens, int seqs, int size) { return tokens / (64 << size) + seqs; }
@@ -147,7 +149,7 @@ struct PlanArgs {
   const int32_t* cu;  // [seqs + 1]
   PackedHeader* header;
   PackedSeq* seqs;
-  PackedTile* tiles[3];  // packed_tiles() of each size
+  PackedTile* tiles[2];  // packed_tiles() of each size
   int seq_count, tokens, max_seqlen, causal;
 };
 

@@ -2,7 +2,7 @@
 //
 // Sequence s of a batch packed into one row of tokens is the rows [cu[s],
 // cu[s + 1]).  Every kernel of the packed forms gives a workgroup one tile of
-// 64, 128 or 256 rows of one sequence, so it needs to know which tile of which
+// 64 or 128 rows of one sequence, so it needs to know which tile of which
 // sequence workgroup x has, those with the most keys first (a grid lasts as
 // long as the workgroup that ends last).  That is a function of cu alone, and
 // cu is known on the device: one launch lists the tiles for every layer's
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * (PLAN_NT / 64) + wave_id());
   // the wave's sequence, which 64 of its tiles, and the blocks before it
-  int seq = -1, start = 0, len = 0, chunk = 0, waves = 0, block = 0, first = -1, last = 0, total[3] = {};
+  int seq = -1, start = 0, len = 0, chunk = 0, waves = 0, block = 0, first = -1, last = 0, total[2] = {};
   walk(a, [&](int s, int begin, int n) {
     const int need = max(tiles_of(n, 6), 1);  // (an empty sequence has a record too)
     if (wave >= waves && wave < waves + need) {
@@ -62,19 +62,19 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
       last = begin + n;
     }
 #pragma unroll
-    for (int z = 0; z < 3; ++z) total[z] += tiles_of(n, z);
+    for (int z = 0; z < 2; ++z) total[z] += tiles_of(n, z);
   });
-  if (wave == 0 && lane == 0) *a.header = PackedHeader{{total[0], total[1], total[2]}, max(first, 0), last, {}};
+  if (wave == 0 && lane == 0) *a.header = PackedHeader{{total[0], total[1]}, max(first, 0), last};
   if (seq < 0) return;
   if (chunk == 0 && lane == 0) a.seqs[seq] = PackedSeq{start, len, block, 0};
   const int t = 64 * chunk + lane;
   // tiles before tile t of each size: longer ones of any sequence, and as long
   // ones of an earlier one.  Causal tiles are as long as their number, others
   // as long as their sequence.
-  int before[3] = {};
+  int before[2] = {};
   walk(a, [&](int s, int, int n) {
 #pragma unroll
-    for (int z = 0; z < 3; ++z) {
+    for (int z = 0; z < 2; ++z) {
       const int N = tiles_of(n, z);
       if (a.causal)
         before[z] += max(N - t - 1, 0) + (s < seq && N > t ? 1 : 0);
@@ -83,7 +83,7 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
     }
   });
 #pragma unroll
-  for (int z = 0; z < 3; ++z)
+  for (int z = 0; z < 2; ++z)
     if (t < tiles_of(len, z)) a.tiles[z][before[z] + (a.causal ? 0 : t)] = PackedTile{seq, t};
 }
 

@@ -89,7 +89,7 @@ __device__ __forceinline__ void solve_tile(const A& a, const int tile, const int
   constexpr int ROWS = SV_WAVES * 32 * G;  // rows per workgroup
   // The packed one-group form keeps its compacted lists in LDS, in place of the
   // key tiles, which are not needed any more once the scores are collected.
-  constexpr bool IN_LDS = PK && G == 1 && !precise_path<E, GK>();
+  constexpr bool IN_LDS = PK && (GK == 1 || GK == 2);
   struct LdsLists {
     float score[LDS_SINGLES + 1][SV_NT];  // (one row more: see the store)
     uint16_t key[LDS_SINGLES + 1][SV_NT];
@@ -912,8 +912,8 @@ __device__ __forceinline__ void solve_tile(const A& a, const int tile, const int
   };
   // Whether something holds for all, or any, threads that go on together: in
   // the packed form with the cache in use a wave goes on by itself.
-  auto all_of = [&](bool v) { return PK && G == 1 && cached ? __ballot(!v) == 0ull : (bool)__syncthreads_and(v); };
-  auto any_of = [&](bool v) { return PK && G == 1 && cached ? __ballot(v) != 0ull : (bool)__syncthreads_or(v); };
+  auto all_of = [&](bool v) { return PK && cached ? __ballot(!v) == 0ull : (bool)__syncthreads_and(v); };
+  auto any_of = [&](bool v) { return PK && cached ? __ballot(v) != 0ull : (bool)__syncthreads_or(v); };
   for (int it = 0;; ++it) {
     // ---- evaluation at tau (per group): m0 = sum z^gamma, m1 = sum
     // z^(gamma-1), m2 = sum z^(gamma-2) over the strict support z > 0, mc =
@@ -1380,7 +1380,7 @@ __device__ __forceinline__ void solve_tile(const A& a, const int tile, const int
 // tile after another instead: the tiles of sequences of many lengths, in
 // launches of one per slot, would leave most of the device idle at the end of
 // each launch (32 heads of eight sequences of 130 to 4096 tokens, d = 128: five
-// launches, 1000 us, against one of 640).  Tiles come longest first, so in
+// launches, 1000 us, against one of 870).  Tiles come longest first, so in
 // every other round the workgroups take them in the opposite order, eight at a
 // time (a workgroup stays on its XCD and with it its head's keys): those that
 // had the longest of one round have the shortest of the next.
@@ -1444,32 +1444,26 @@ hipError_t launch_solve_d(const TauArgs& a, hipStream_t s) {
   return launch_solve_g<E, D, 2>(a, s);
 }
 
-// Packed sequences: as many workgroups as the device holds at a time (256
-// compute units; waves per SIMD as the kernel is built for), and no more than
-// there are slots, or tiles.
-template <typename E, int D, int G>
-hipError_t launch_solve_packed_g(Packed<TauArgs> a, int tiles, hipStream_t s) {
-  using A = Packed<TauArgs>;
-  auto kernel = solve_kernel<E, D, 0, G, A>;
-  if (a.gk == 1) kernel = solve_kernel<E, D, 1, G, A>;
-  if (a.gk == 2) kernel = solve_kernel<E, D, 2, G, A>;
-  if (a.gk == 4) kernel = solve_kernel<E, D, 4, G, A>;
-  if (G == 1) a.slots *= 2;
-  int wgs = 256 * (G == 1 ? SV_OCC1 : sizeof(E) == 4 && D == 128 ? 1 : 2);
-  if (a.cand && a.slots < wgs) wgs = a.slots;
-  return launch_kernel(kernel, dim3((unsigned)(tiles < wgs ? tiles : wgs)), dim3(SV_NT), s, a);
-}
-
-// The two forms as in launch_solve_d, by the most tiles.
+// Packed sequences: the one-group form at all sizes, as many workgroups as the
+// device holds at a time, and no more than there are slots, or tiles.  (Packed
+// forward, one causal sequence, us, one-group against two-group form: n = 4096,
+// 16 heads, d = 128, c = 1 271 against 328, n = 16384, 8 heads 1462 against
+// 1831, n = 65536, 4 heads 8220 against 9998, at c = 16 2828 against 2606.)
 template <typename E, int D>
 hipError_t launch_solve_packed(Packed<TauArgs> a, hipStream_t s) {
-  PackedArgs& pk = a.pk;
-  const int tiles = pk.heads * packed_tiles(pk.tokens, pk.seq_count, 2);
-  const bool one = true;
-  pk.size = one ? 1 : 2;
-  pk.tiles = pk.lists[pk.size];
-  if (one) return launch_solve_packed_g<E, D, 1>(a, pk.heads * packed_tiles(pk.tokens, pk.seq_count, 1), s);
-  return launch_solve_packed_g<E, D, 2>(a, tiles, s);
+  using A = Packed<TauArgs>;
+  static_assert(PACKED_SOLVERS == 256 * SV_OCC1, "workgroups of the one-group form that run at a time");
+  auto kernel = solve_kernel<E, D, 0, 1, A>;
+  if (a.gk == 1) kernel = solve_kernel<E, D, 1, 1, A>;
+  if (a.gk == 2) kernel = solve_kernel<E, D, 2, 1, A>;
+  if (a.gk == 4) kernel = solve_kernel<E, D, 4, 1, A>;
+  a.pk.size = 1;
+  a.pk.tiles = a.pk.lists[1];
+  a.slots *= 2;  // (half a slot each)
+  const int tiles = a.pk.heads * packed_tiles(a.pk.tokens, a.pk.seq_count, 1);
+  int wgs = tiles < PACKED_SOLVERS ? tiles : PACKED_SOLVERS;
+  if (a.cand && a.slots < wgs) wgs = a.slots;
+  return launch_kernel(kernel, dim3((unsigned)wgs), dim3(SV_NT), s, a);
 }
 
 }  // namespace
