@@ -1657,20 +1657,30 @@ __global__ __launch_bounds__(LK_NT, 2) void dkdv_lists_kernel(A a) {
   if constexpr (PK) {
     __syncthreads();  // (the workgroup's sums are written)
     const int64_t values = (int64_t)a.pk.tokens * ldg, first = ((int64_t)place.start + k0) * ldg + place.head * D;
-    for (int x = t; x < BLK * D / 4; x += LK_NT) {
-      const int row = x / (D / 4), col = x % (D / 4) * 4;
-      if (k0 + row >= n) continue;
-      const int64_t off = first + (int64_t)row * ldg + col;
-      f32x4 k4 = {0.f, 0.f, 0.f, 0.f}, v4 = {0.f, 0.f, 0.f, 0.f};
-      for (int p = 0; p <= a.pk.parts; ++p) {
-        if (p < a.pk.parts ? !((const ci32*)a.pk.wrote)[((size_t)p * a.pk.kv_heads + place.head) * a.pk.blocks + place.block + kb]
-                           : !add)
-          continue;
-        k4 += *reinterpret_cast<const f32x4*>(a.pk.dk_part + p * values + off);
-        v4 += *reinterpret_cast<const f32x4*>(a.pk.dv_part + p * values + off);
+    // (every value of a part is in flight at once)
+    constexpr int PER = BLK * D / 4 / LK_NT;
+    f32x4 k4[PER], v4[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) k4[i] = v4[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int row = t / (D / 4), col = t % (D / 4) * 4;
+    constexpr int STEP = LK_NT / (D / 4);  // rows
+    for (int p = 0; p <= a.pk.parts; ++p) {
+      if (p < a.pk.parts ? !((const ci32*)a.pk.wrote)[((size_t)p * a.pk.kv_heads + place.head) * a.pk.blocks + place.block + kb]
+                         : !add)
+        continue;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int64_t off = p * values + first + (int64_t)min(row + i * STEP, n - 1 - k0) * ldg + col;
+        k4[i] += *reinterpret_cast<const f32x4*>(a.pk.dk_part + off);
+        v4[i] += *reinterpret_cast<const f32x4*>(a.pk.dv_part + off);
       }
-      store4(reinterpret_cast<E*>(a.dk) + off, k4);
-      store4(reinterpret_cast<E*>(a.dv) + off, v4);
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (k0 + row + i * STEP >= n) break;
+      const int64_t off = first + (int64_t)(row + i * STEP) * ldg + col;
+      store4(reinterpret_cast<E*>(a.dk) + off, k4[i]);
+      store4(reinterpret_cast<E*>(a.dv) + off, v4[i]);
     }
   }
 }
