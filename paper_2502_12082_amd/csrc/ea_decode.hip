@@ -155,9 +155,8 @@ __global__ __launch_bounds__(SC_NT, 2) void decode_maxima_kernel(DecodeArgs a, i
 
 // ------------------------------------------------------------------- solve
 
-constexpr int SO_CAP = 2048;     // scores kept in LDS
-constexpr int SO_QUADS = SO_CAP / 4;
-constexpr int SO_BLOCKS = MAX_SEQLEN / DEC_KEYS + 2;  // most blocks of a row
+constexpr int SO_LONGEST = MAX_SEQLEN / DEC_KEYS + 2;  // most blocks of a row
+constexpr int SO_SHORT = 512;    // and of one that a single wave takes
 constexpr int SO_LANE = 8;       // scores per lane that a wave solves on its own
 constexpr int SO_STEPS = 4;      // blocks that eight threads read at once
 constexpr int SO_MAXIMA = 16;    // blocks' maxima that a thread holds in registers
@@ -206,13 +205,16 @@ template <typename E, int D, int GK, int NT>
 __global__ __launch_bounds__(NT) void decode_solve_kernel(DecodeArgs a) {
   using R = RowGroup<E, D>;
   constexpr int VPL = R::VPL, LPR = R::LPR, NG = NT / LPR, SO_NT = NT, SO_WAVES = NT / 64;
+  constexpr int SO_CAP = NT == 64 ? 1024 : 2048;  // scores kept in LDS
+  constexpr int SO_QUADS = SO_CAP / 4;
+  constexpr int SO_BLOCKS = NT == 64 ? SO_SHORT : SO_LONGEST;
   __shared__ float kept[SO_CAP];          // scores of the quads, four each
   __shared__ uint16_t quad[SO_QUADS];     // quads with a score above the bound (the block's first key / 4 + quad)
   __shared__ uint16_t chosen[SO_BLOCKS];  // blocks with such a score
   __shared__ float red[2][3][SO_WAVES];
   __shared__ int cnt[2][SO_WAVES];
   static_assert(sizeof(kept) >= NG * D * sizeof(float), "the groups' sums fit in place of the scores");
-  static_assert(SO_BLOCKS * (DEC_KEYS / 4) <= 65536, "a quad's number fits 16 bits");
+  static_assert(SO_LONGEST * (DEC_KEYS / 4) <= 65536, "a quad's number fits 16 bits");
   const int t = threadIdx.x, lane = lane_id(), w = wave_id(), sub = lane % LPR, grp = t / LPR;
   // (heads of one key head are kv_heads apart: with eight key heads they meet on
   // one XCD, whose L2 then has to hold the rows of that head alone)
@@ -404,13 +406,14 @@ __global__ __launch_bounds__(NT) void decode_solve_kernel(DecodeArgs a) {
   float qv[VPL];
   R::unpack(R::load(static_cast<const E*>(a.q) + b * a.q_row + h * a.q_head, 0u), qv);
   // store(i, scores) of the quads number(i), i < n (four keys each, from key 4
-  // number(i) on, counted over all blocks): two at a time, by the first lane of a group.
+  // number(i) on, counted over all blocks), by the first lane of a group; QB at a time.
+  constexpr int QB = NT == 64 ? 4 : 2;
   auto quad_scores = [&](int n, auto&& number, auto&& store) {
-    for (int x0 = grp; x0 < n; x0 += 2 * NG) {
-      u32x4 kw[2][4];
-      int left[2];  // keys from the quad's first to the end
+    for (int x0 = grp; x0 < n; x0 += QB * NG) {
+      u32x4 kw[QB][4];
+      int left[QB];  // keys from the quad's first to the end
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < QB; ++u) {
         const int q = number(min(x0 + u * NG, n - 1));
         const bool shared = q < p_blocks * (DEC_KEYS / 4);
         const int k0 = 4 * q - (shared ? 0 : p_blocks * DEC_KEYS);
@@ -422,7 +425,7 @@ __global__ __launch_bounds__(NT) void decode_solve_kernel(DecodeArgs a) {
           kw[u][e] = *reinterpret_cast<const u32x4*>(base + (k0 + min(e, left[u] - 1)) * ld);
       }
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < QB; ++u) {
         f32x4 s;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -511,29 +514,38 @@ __global__ __launch_bounds__(NT) void decode_solve_kernel(DecodeArgs a) {
   float o[VPL] = {};
   const E* const own_v = static_cast<const E*>(a.v) + b * a.v_batch + kv * a.v_head;
   const E* const pre_v = static_cast<const E*>(a.pv) + kv * a.pv_head;
-  // of n kept scores, those at 4 i of the keys from 4 first(i) on
+  // Of n kept scores, those at 4 i of the keys from 4 first(i) on: those with a
+  // probability move to the front (a score is not overwritten before every
+  // thread has read its own), p in place of the score, and their rows of V are
+  // added up.
+  __shared__ uint16_t from[SO_CAP];
   auto gather = [&](int n, auto&& first) {
+    int np = 0;
+    for (int y0 = 0; y0 < n; y0 += NT) {
+      const float p = y0 + t < n ? Gamma<GK>::p_only(relu_z(c, kept[y0 + t], tau), gm) : 0.f;
+      const int at = place(p > 0.f ? 1 : 0, np);
+      if (p > 0.f) {
+        kept[at] = p;
+        from[at] = (uint16_t)(y0 + t);
+      }
+    }
+    __syncthreads();
     constexpr int BATCH = 8;
-    for (int y0 = grp; y0 < n; y0 += NG * BATCH) {
+    for (int y0 = grp; y0 < np; y0 += NG * BATCH) {
       u32x4 v[BATCH];
       float p[BATCH];
 #pragma unroll
       for (int u = 0; u < BATCH; ++u) {
-        const int y = y0 + u * NG;
-        p[u] = 0.f;
-        v[u] = u32x4{0, 0, 0, 0};
-        if (y < n) {
-          p[u] = Gamma<GK>::p_only(relu_z(c, kept[y], tau), gm);
-          if (p[u] > 0.f) {  // (a key without a probability is not read)
-            const int key = 4 * first(y >> 2) + (y & 3);
-            const E* const v_row = key < p_blocks * DEC_KEYS ? pre_v + key * a.pv_row
-                                                             : own_v + (key - p_blocks * DEC_KEYS) * a.v_row;
-            v[u] = *reinterpret_cast<const u32x4*>(v_row + sub * VPL);
-          }
-        }
+        const int y = min(y0 + u * NG, np - 1), i = from[y];
+        p[u] = y0 + u * NG < np ? kept[y] : 0.f;
+        const int key = 4 * first(i >> 2) + (i & 3);
+        const E* const v_row = key < p_blocks * DEC_KEYS ? pre_v + key * a.pv_row
+                                                         : own_v + (key - p_blocks * DEC_KEYS) * a.v_row;
+        v[u] = *reinterpret_cast<const u32x4*>(v_row + sub * VPL);
       }
 #pragma unroll
       for (int u = 0; u < BATCH; ++u) {
+        if (y0 + u * NG >= np) break;  // (the last row again, whatever it holds)
         float e[VPL];
         R::unpack(v[u], e);
 #pragma unroll
@@ -609,8 +621,8 @@ hipError_t launch_decode_d(const DecodeArgs& a, hipStream_t s) {
   if (e != hipSuccess) return e;
   // Rows for two waves on every compute unit have one each, few or long ones
   // four: 2048 rows of 260 to 288 blocks 31 us against 37, 1024 rows of 2050
-  // blocks 33 against 23 (a wave then holds half of its maxima in registers).
-  const bool one = a.requests * a.heads >= 512 && a.prefix_runs + a.own_runs <= SO_MAXIMA * 64 / 2 / DEC_RUN;
+  // blocks 33 against 23.
+  const bool one = a.requests * a.heads >= 512 && a.prefix_runs + a.own_runs <= SO_SHORT / DEC_RUN;
   return one ? launch_solve<E, D, 64>(a, s) : launch_solve<E, D, 256>(a, s);
 }
 

@@ -62,6 +62,16 @@ def test_supports(ea, c, alpha):
     compare(run(ea, x, alpha, max_iter=40), x, alpha, "c%g a%g" % (c, alpha), c)
 
 
+@pytest.mark.parametrize("c", [0.0, 0.3, 1.0, 8.0])
+@pytest.mark.parametrize("d,dtype", [(128, BF), (64, F32)])
+def test_many_rows(ea, c, d, dtype):
+    """Rows enough for a wave each: every key in the support, many, few."""
+    g = torch.Generator().manual_seed(10)
+    lengths = torch.randint(0, 90, (40,), generator=g).tolist()
+    x = make(lengths, 1500, 90, 16, 2, d, dtype, c=c, seed=11)
+    compare(run(ea, x), x, 1.5, "c%g d%d" % (c, d), c)
+
+
 def test_long_prefix(ea):
     x = make([100, 0, 50], 100000, 100, 4, 2, 128, BF, c=1.0, seed=2)
     compare(run(ea, x), x, 1.5, "long")
