@@ -865,6 +865,12 @@ def _strides_of(row, head):
     return Strides(row, head)
 
 
+def _numbers(alpha, scale, max_iter, tol):
+    """A call's parameters as plain numbers, whatever holds them."""
+    return (float(alpha), None if scale is None else float(scale), None if max_iter is None else int(max_iter),
+            None if tol is None else float(tol))
+
+
 def _row_head(t, row=0, head=1):
     return _strides_of(_stride(t, row), _stride(t, head))
 
@@ -1133,7 +1139,7 @@ def _packed_strides_of(*s):
 
 
 @functools.lru_cache(maxsize=256)
-def _packed_params(alpha, scale, causal, need_bwd, max_iter, tol, head_dim, *shape):
+def _packed_params(alpha, scale, max_iter, tol, causal, need_bwd, head_dim, *shape):
     """(Params, PackedSizes) of a call."""
     params = make_params(alpha, scale, causal, need_bwd, max_iter, tol, head_dim=head_dim)
     sizes = PackedSizes()
@@ -1157,7 +1163,7 @@ def packed_forward(q, k, v, plan: PackedPlan, alpha=1.5, scale=None, need_bwd=Tr
     shape = _packed_shape(q, k, v, plan)
     if tol is None and shape.dtype == EA_F32:
         tol = 1e-6  # (Sum p is off by up to tol, which the fp32 outputs show)
-    params, sizes = _packed_params(alpha, scale, plan.causal, bool(need_bwd), max_iter, tol, q.shape[-1],
+    params, sizes = _packed_params(*_numbers(alpha, scale, max_iter, tol), plan.causal, bool(need_bwd), q.shape[-1],
                                    shape.tokens, shape.seqs, shape.max_seqlen, shape.heads, shape.kv_heads,
                                    shape.head_dim, shape.dtype)
     made = out is None
@@ -1297,7 +1303,8 @@ def prefix_decode(q, k_cache, v_cache, lengths, k_prefix=None, v_prefix=None, al
                         ("v_prefix", v_prefix)):
             if t is not None and _overlap(out, t):
                 raise ValueError("out overlaps %s" % name)
-    shape, params, nbytes = _decode_of(alpha, scale, max_iter, 1e-6 if tol is None else tol, B, hq, hk, d, dt, P, cap)
+    shape, params, nbytes = _decode_of(*_numbers(alpha, scale, max_iter, 1e-6 if tol is None else tol), B, hq, hk, d,
+                                       dt, P, cap)
     if workspace is not None:
         _check_bytes(workspace, "workspace", nbytes, dev)
     _on_gpu(dev)

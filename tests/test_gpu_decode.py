@@ -85,6 +85,39 @@ def test_lengths_outside(ea):
     assert torch.equal(run(ea, x), want)
 
 
+def test_far_rows(ea):
+    """A cache whose offsets pass 32 bits, in elements and bytes."""
+    B, cap, hk, d = 66, 65536, 8, 64
+    g = torch.Generator().manual_seed(12)
+    x = make([0] * B, 0, 1, 16, hk, d, BF, seed=12)
+    x["k"], x["v"] = (torch.zeros(B, cap, hk, d, dtype=BF, device="cuda") for _ in range(2))
+    x["lengths"][0], x["lengths"][B - 1] = 100, cap
+    for b, n in ((0, 100), (B - 1, cap)):
+        for name in ("k", "v"):
+            x[name][b, :n] = torch.randn(n, hk, d, generator=g).to(BF).cuda()
+    got = run(ea, x)
+    last = {n: (t[B - 1:] if t is not None else None) for n, t in x.items()}
+    first = {n: (t[:1] if t is not None else None) for n, t in x.items()}
+    compare(got[B - 1:], last, 1.5, "last")
+    compare(got[:1], first, 1.5, "first")
+    assert not got[1:B - 1].any()
+
+
+def test_no_requests(ea):
+    x = make([], 5, 3, 2, 1, 64, BF)
+    assert run(ea, x).shape == (0, 2, 64)
+
+
+def test_parameters_in_tensors(ea):
+    """A call takes what its parameters hold when it is made."""
+    x = make([300, 41], 20, 4, 2, 1, 64, BF, c=2.0, seed=13)
+    alpha, scale = torch.tensor(1.25), torch.tensor(0.1)
+    for a, s in ((1.25, 0.1), (2.0, 0.3)):
+        alpha.fill_(a), scale.fill_(s)
+        got = run(ea, x, alpha, scale=scale)
+        assert torch.equal(got, run(ea, x, float(alpha), scale=float(scale)))
+
+
 def test_equal_scores(ea):
     """Ties: every key the same, so that each has probability 1 / n."""
     x = make([100, 40], 60, 100, 2, 1, 64, BF, seed=4)

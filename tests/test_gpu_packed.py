@@ -304,3 +304,34 @@ def test_two_streams(ea):
     torch.cuda.synchronize()
     for x, y in zip(got, want):
         assert all(torch.equal(a, b) for a, b in zip(x, y))
+
+
+def test_longest_sequences(ea):
+    """More keys than 16 bits number, against the batched path."""
+    n, d = 70001, 64
+    q, k, v, _, cud = make([0, n], n, 2, 1, d, BF, c=4.0, seed=15)
+    o, res = ea.packed_forward(q, k, v, ea.packed_plan(cud, n), alpha=1.5, need_bwd=False)
+    assert res.lists is None
+    batched = lambda t: t.transpose(0, 1)[None].contiguous()
+    kk, vv = (t.repeat_interleave(2, 1) for t in (k, v))
+    want, _ = ea.forward(batched(q), batched(kk), batched(vv), alpha=1.5, causal=True, need_bwd=False)
+    want = want[0].transpose(0, 1).double().cpu()
+    check("long", o, want, 1e-3, 2.0 ** -8 * want.abs())
+
+
+def test_far_rows(ea):
+    """Rows so far apart that their offsets pass 32 bits, in elements and bytes."""
+    tokens, hq, hk, d, width = 20000, 2, 1, 64, 120000
+    cu = [0, 15000, tokens]
+    q, k, v, do, cud = make(cu, tokens, hq, hk, d, BF, c=4.0, seed=16)
+    plan = ea.packed_plan(cud, tokens)
+    want = run(ea, q, k, v, do, plan, 1.5)
+    wide = torch.empty(tokens, width, dtype=BF, device="cuda")
+    parts, at = [], 0
+    for t in (q, k, v, do):
+        part = wide[:, at:at + t.shape[1] * d].view(t.shape)
+        part.copy_(t)
+        parts.append(part)
+        at += 30000
+    got = run(ea, *parts, plan, 1.5)
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
