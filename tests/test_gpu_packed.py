@@ -322,7 +322,7 @@ def test_longest_sequences(ea):
 def test_far_rows(ea):
     """Rows so far apart that their offsets pass 32 bits, in elements and bytes."""
     tokens, hq, hk, d, width = 20000, 2, 1, 64, 120000
-    cu = [0, 15000, tokens]
+    cu = [0, 19000, tokens]
     q, k, v, do, cud = make(cu, tokens, hq, hk, d, BF, c=4.0, seed=16)
     plan = ea.packed_plan(cud, tokens)
     want = run(ea, q, k, v, do, plan, 1.5)
