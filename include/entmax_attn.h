@@ -403,6 +403,7 @@ ea_status entmax_packed_sizes(const ea_packed_shape* shape, const ea_params* par
  * causal only orders the work).  Every buffer 16-byte aligned.  dout has the
  * strides strides->o.  dq [tokens, heads, d], dk and dv [tokens, kv_heads, d]
  * are contiguous and of the inputs' dtype (each rounded once, from fp32 sums).
+ * Rows of q, k, v, o and dout are at most 2^24 elements apart.
  * Rows that belong to no sequence (before cu[0], behind cu[seqs]) are left as
  * they are, or with zero_rest != 0 set to 0.  Launches: 2 (forward), 3 or 4
  * (backward).
@@ -428,8 +429,9 @@ ea_status entmax_packed_bwd(const ea_packed_shape* shape, const ea_params* param
  *   k, v   [requests, capacity, kv_heads, d]
  *   k_prefix, v_prefix  [prefix, kv_heads, d] (not read where prefix is 0)
  *   params alpha, scale, max_iter and tol are used
- * prefix + capacity <= 131072.  workspace: entmax_prefix_decode_workspace
- * bytes, 16-byte aligned (about 5 bytes for every query head and key, most of
+ * prefix + capacity <= 131072; rows of k and k_prefix are at most 2^24 elements
+ * apart.  workspace: entmax_prefix_decode_workspace
+ * bytes, 16-byte aligned (about 4.4 bytes for every query head and key, most of
  * them for rows with thousands of probabilities).  Two launches.
  */
 typedef struct {

@@ -871,6 +871,12 @@ def _numbers(alpha, scale, max_iter, tol):
             None if tol is None else float(tol))
 
 
+def _near(rows):
+    """Raises ValueError where rows are further apart than a tile's offsets reach."""
+    if max(rows) > 1 << 24:
+        raise ValueError("rows are %d elements apart, at most 2^24 are possible" % max(rows))
+
+
 def _row_head(t, row=0, head=1):
     return _strides_of(_stride(t, row), _stride(t, head))
 
@@ -1135,6 +1141,7 @@ def _packed_strides(*tensors):
 
 @functools.lru_cache(maxsize=1024)
 def _packed_strides_of(*s):
+    _near(s[::2])
     return PackedStrides(*[Strides(s[i], s[i + 1]) for i in range(0, 8, 2)])
 
 
@@ -1244,7 +1251,7 @@ def packed_backward(q, k, v, dout, res: PackedResiduals, dq=None, dk=None, dv=No
 
 def prefix_decode_workspace(q, k_cache, prefix=0):
     """Bytes of the workspace of prefix_decode for these tensors and a prefix of
-    that many keys (about 5 bytes for every query head and key)."""
+    that many keys (about 4.4 bytes for every query head and key)."""
     return _decode_of(1.5, None, None, None, q.shape[0], q.shape[1], k_cache.shape[2], q.shape[2],
                       _ea_dtype(q, "q"), int(prefix), k_cache.shape[1])[2]
 
@@ -1260,6 +1267,7 @@ def _decode_of(alpha, scale, max_iter, tol, *sizes):
 
 @functools.lru_cache(maxsize=1024)
 def _decode_strides_of(*s):
+    _near((s[4], s[8]))  # (of the keys)
     return DecodeStrides(*[Strides(s[i], s[i + 1]) for i in range(0, 12, 2)], s[12], s[13])
 
 

@@ -1075,8 +1075,8 @@ size_t decode_parts(const ea_decode_shape* s, void* base, DecodeArgs* a) {
   const size_t pb = ((size_t)s->prefix + DEC_KEYS - 1) / DEC_KEYS, ob = ((size_t)s->capacity + DEC_KEYS - 1) / DEC_KEYS;
   const size_t p_wide = (pb + DEC_RUN - 1) / DEC_RUN * DEC_RUN, o_wide = (ob + DEC_RUN - 1) / DEC_RUN * DEC_RUN;
   Parts p{static_cast<char*>(base)};
-  a->pq = p.take<float>(rows * pb * 8);
-  a->oq = p.take<float>(rows * ob * 8);
+  a->pq = p.take<uint8_t>(rows * p_wide * (DEC_KEYS / 4));
+  a->oq = p.take<uint8_t>(rows * o_wide * (DEC_KEYS / 4));
   a->pm = p.take<float>(rows * p_wide);
   a->om = p.take<float>(rows * o_wide);
   a->spill = p.take<float>(rows * (pb + ob) * DEC_KEYS);
@@ -1107,6 +1107,10 @@ ea_status entmax_prefix_decode(const ea_decode_shape* shape, const ea_params* pa
   const int64_t vec = 16 / (int64_t)es;
   if (!st || !strides_ok(&st->q, es) || !strides_ok(&st->o, es)) return EA_ERR_INVALID_ARG;
   if (!tensor_ok(q) || !tensor_ok(o) || !small_ok(lengths)) return EA_ERR_INVALID_ARG;
+  // (a block's offsets are 32-bit numbers)
+  constexpr int64_t MAX_KEY_ROW = 1 << 24;
+  if (shape->capacity && st->k.row > MAX_KEY_ROW) return EA_ERR_INVALID_ARG;
+  if (shape->prefix && st->k_prefix.row > MAX_KEY_ROW) return EA_ERR_INVALID_ARG;
   if (shape->capacity) {
     if (!tensor_ok(k) || !tensor_ok(v) || !strides_ok(&st->k, es) || !strides_ok(&st->v, es)) return EA_ERR_INVALID_ARG;
     for (int64_t x : {st->k_request, st->v_request})

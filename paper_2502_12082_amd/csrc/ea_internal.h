@@ -189,12 +189,13 @@ struct DecodeArgs {
   const int32_t* lengths;  // [requests], clamped to 0 .. capacity
   int requests, heads, kv_heads, group, prefix, capacity;
   int prefix_runs, own_runs;  // per key head, and per request and key head
-  // workspace: maxima of the scores of every row's quads of four keys
-  // [kv_heads, prefix blocks, requests * group, 8] and [requests, kv_heads, own
-  // blocks, group, 8], of its blocks (in rows of whole runs) [kv_heads,
-  // requests * group, prefix_runs * DEC_RUN] and [requests, kv_heads, group,
-  // own_runs * DEC_RUN], and room for its scores [requests, heads, blocks, 32]
-  float *pq, *oq, *pm, *om, *spill;
+  // workspace: of every row's quads of four keys a byte each (see maxima_run)
+  // [kv_heads, prefix_runs, requests * group, 32] and [requests, kv_heads,
+  // own_runs, group, 32], the maxima of its blocks [kv_heads, requests * group,
+  // prefix_runs * DEC_RUN] and [requests, kv_heads, group, own_runs * DEC_RUN],
+  // and room for its scores [requests, heads, blocks, 32]
+  uint8_t *pq, *oq;
+  float *pm, *om, *spill;
   float c, alpha, gamma, tol;
   int max_iter, gk;
 };

@@ -240,3 +240,25 @@ def test_prefix_decode_abi(at, value, code):
     assert n.value >= 3 * 4 * 107 * 4
     good[at] = value
     assert ea._lib.entmax_prefix_decode_workspace(ctypes.byref(ea.DecodeShape(*good)), ctypes.byref(n)) == code
+
+
+def test_rows_too_far_apart():
+    """A tile's offsets are 32-bit numbers: refused by the binding, and by the C entry points."""
+    far = (1 << 24) + 8
+    for i in range(4):
+        rows = [64] * 8
+        rows[2 * i] = far
+        with pytest.raises(ValueError, match="apart"):
+            ea._packed_strides_of(*rows)
+    for i in (4, 8):
+        rows = [64] * 14
+        rows[i] = far
+        with pytest.raises(ValueError, match="apart"):
+            ea._decode_strides_of(*rows)
+    shape = ea.DecodeShape(1, 1, 1, 64, ea.EA_BF16, 64, 64)
+    params = ea.make_params(1.5, None, False, False, None, 1e-6, head_dim=64)
+    near, far = ea.Strides(64, 64), ea.Strides(far, 64)
+    for k, kp in ((far, near), (near, far)):
+        strides = ea.DecodeStrides(near, near, k, near, kp, near, 4096, 4096)
+        assert ea._lib.entmax_prefix_decode(shape, params, strides, 4096, 4096, 4096, 4096, 4096, 4096, 4096, 4096,
+                                            1 << 20, None) == ea.EA_ERR_INVALID_ARG
