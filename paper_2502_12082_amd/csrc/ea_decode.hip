@@ -688,7 +688,7 @@ hipError_t launch_decode_d(const DecodeArgs& a, hipStream_t s) {
     e = launch_maxima<E, D, 1>(a, s);
   if (e != hipSuccess) return e;
   // Rows for two waves on every compute unit have one each, few or long ones
-  // four: 2048 rows of 260 to 288 blocks 31 us against 37, 1024 rows of 2050
+  // four: 2048 rows of 260 to 288 blocks 25 us against 35, 1024 rows of 2050
   // blocks 33 against 23.
   const bool one = a.requests * a.heads >= 512 && a.prefix_runs + a.own_runs <= SO_SHORT / DEC_RUN;
   return one ? launch_solve<E, D, 64>(a, s) : launch_solve<E, D, 256>(a, s);

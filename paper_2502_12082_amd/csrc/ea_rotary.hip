@@ -11,7 +11,8 @@
 //   dx = r (g - xh mean(g xh)),  dw = sum over tokens and heads of dy xh
 //
 // Both are bound by HBM: the forward reads and writes every value once, the
-// backward reads two and writes one.  Layout: a lane holds two chunks of eight
+// backward reads two and writes one (32768 tokens, 16/8 heads, d = 128, bf16:
+// 76 us, 5.3 TB/s, and 133 us, 4.6 TB/s; a copy of 1 GiB 5.2).  Layout: a lane holds two chunks of eight
 // values that contain whole pairs, D / 16 lanes hold a row, a wave takes 64 /
 // (D / 16) heads of one token at a time.  A token's angles are taken once, one
 // pair per lane, and shared through LDS by all of its heads: positions reach
@@ -314,7 +315,7 @@ __global__ __launch_bounds__(ROT_NT) void rotary_bwd_kernel(RotaryArgs a) {
 
 // dw from the workgroups' partials: 16 values per workgroup, each the sum of
 // 64 threads' sums over every 64th partial (at most 16 loads each, all in
-// flight at once: 1024 partials of 2 x 128 values in 4 us, with a quarter of
+// flight at once: 1024 partials of 2 x 128 values in 5 us, with a quarter of
 // the threads 20).
 constexpr int DW_NT = 1024;
 constexpr int DW_ROWS = DW_NT / 16;
