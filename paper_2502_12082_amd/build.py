@@ -31,7 +31,7 @@ CFLAGS = [
     "-I", os.path.join(ROOT, "include"),
 ]
 # Files compiled in several parts, in parallel: (macro, number of parts).
-PARTS = {"ea_tau.hip": ("EA_TAU_PART", 9)}
+PARTS = {"ea_tau.hip": ("EA_TAU_PART", 9), "ea_small.hip": ("EA_SMALL_PART", 2)}
 
 
 def _units():

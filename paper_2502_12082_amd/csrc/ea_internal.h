@@ -345,6 +345,7 @@ hipError_t launch_tau(const TauArgs& a, int dtype, int head_dim, hipStream_t s);
 // general alpha (no candidate cache, no K passes beyond the first).
 constexpr int SMALL_MAX_N = 1024;
 hipError_t launch_tau_small(const TauArgs& a, int dtype, int head_dim, hipStream_t s);
+hipError_t launch_tau_small_packed(Packed<TauArgs> a, int dtype, int head_dim, hipStream_t s);
 hipError_t launch_tau_bf16_64(const TauArgs& a, hipStream_t s);
 hipError_t launch_tau_bf16_128(const TauArgs& a, hipStream_t s);
 hipError_t launch_tau_f32_64(const TauArgs& a, hipStream_t s);

@@ -18,6 +18,7 @@
 
 #include "ea_common.h"
 #include "ea_internal.h"
+#include "ea_packed.h"
 
 namespace ea {
 
@@ -42,8 +43,10 @@ __device__ __forceinline__ f32x4 step_operands(const f32x4& v) {
 #endif
 }
 
-template <typename E, int D, int GK, int KT>
-__global__ __launch_bounds__(SM_NT, KT <= 4 ? 4 : 2) void solve_small_kernel(TauArgs a) {
+// A = Packed<TauArgs>: packed sequences, rows and tables of the workgroup's place.
+template <typename E, int D, int GK, int KT, typename A>
+__global__ __launch_bounds__(SM_NT, KT <= 4 ? 4 : 2) void solve_small_kernel(A a) {
+  constexpr bool PK = is_packed<A>::value;
   using M = Mma<E>;
   constexpr int KS = D / M::KW;
   __shared__ float list[SM_LIST + 1][SM_NT];  // the last row takes dropped stores
@@ -53,14 +56,31 @@ __global__ __launch_bounds__(SM_NT, KT <= 4 ? 4 : 2) void solve_small_kernel(Tau
   __shared__ int over, entries;
 
   const int t = threadIdx.x, lane = lane_id(), w = wave_id(), rg = w & 1, kg = w >> 1, half = lane >> 5;
-  const int n = a.n, T = a.T;
-  const int bh = blockIdx.x % a.BH, qb = blockIdx.x / a.BH;
+  [[maybe_unused]] Place at;
+  if constexpr (PK) {
+    if (!packed_place(a.pk, blockIdx.x, a.pk.heads, false, at)) return;
+  }
+  const int n = PK ? at.n : a.n, T = PK ? at.T : a.T;
+  const int bh = PK ? at.head : blockIdx.x % a.BH, qb = PK ? at.tile : blockIdx.x / a.BH;
+  const size_t row0 = PK ? at.row0 : (size_t)bh * n;             // of the head in tau,
+  const size_t blk = (PK ? at.blk0 : (size_t)bh * T) + qb;  // and the block in the tables
+  int width = T, ldq = D, ldk = D;
   const int q0 = qb * BLK + 32 * rg, i = q0 + (lane & 31), row = 32 * rg + (lane & 31);
   const bool row_ok = i < n;
   const float c = a.c, g = a.gamma;
   const bool newton_bound = g >= 1.f;
-  const E* Q = static_cast<const E*>(a.q) + (size_t)bh * n * D;
-  const E* K = static_cast<const E*>(a.k) + (size_t)bh * n * D;
+  const E* Q = static_cast<const E*>(a.q);
+  const E* K = static_cast<const E*>(a.k);
+  if constexpr (PK) {
+    width = a.pk.width;
+    ldq = a.pk.q.row;
+    ldk = a.pk.k.row;
+    Q += (int64_t)at.start * ldq + bh * a.pk.q.head;
+    K += (int64_t)at.start * ldk + bh / a.pk.group * a.pk.k.head;
+  } else {
+    Q += row0 * D;
+    K += row0 * D;
+  }
   const int keys = a.causal ? min(n, q0 + 32) : n;  // keys any row of the wave sees
   if (t == 0) {
     bits = 0;
@@ -73,7 +93,7 @@ __global__ __launch_bounds__(SM_NT, KT <= 4 ? 4 : 2) void solve_small_kernel(Tau
   if constexpr (sizeof(E) == 2) {
     typename M::frag qf[KS];
 #pragma unroll
-    for (int kk = 0; kk < KS; ++kk) qf[kk] = load_row_frag_global<E, D>(Q, i, n, kk);
+    for (int kk = 0; kk < KS; ++kk) qf[kk] = load_row_frag_global<E, D>(Q, i, n, kk, ldq);
 #pragma unroll
     for (int k = 0; k < KT; ++k) {
       s[k] = zero16();
@@ -81,14 +101,14 @@ __global__ __launch_bounds__(SM_NT, KT <= 4 ? 4 : 2) void solve_small_kernel(Tau
       if (j0 < keys && q0 < n) {
 #pragma unroll
         for (int kk = 0; kk < KS; ++kk)
-          s[k] = M::mma(load_row_frag_global<E, D>(K, min(j0 + (lane & 31), n - 1), n, kk), qf[kk], s[k]);
+          s[k] = M::mma(load_row_frag_global<E, D>(K, min(j0 + (lane & 31), n - 1), n, kk, ldk), qf[kk], s[k]);
       }
     }
   } else {
     // fp32: 16-byte loads, then four operands (Q's in the first tile, so that
     // its keys are on the way meanwhile; a wave without that tile has no other)
     f32x4 qf[D / 8];
-    const float* qr = reinterpret_cast<const float*>(Q) + (size_t)min(i, n - 1) * D + 4 * half;
+    const float* qr = reinterpret_cast<const float*>(Q) + (size_t)min(i, n - 1) * ldq + 4 * half;
 #pragma unroll
     for (int m = 0; m < D / 8; ++m) qf[m] = *reinterpret_cast<const f32x4*>(qr + 8 * m);
 #pragma unroll
@@ -96,7 +116,7 @@ __global__ __launch_bounds__(SM_NT, KT <= 4 ? 4 : 2) void solve_small_kernel(Tau
       s[k] = zero16();
       const int j0 = 32 * (kg + SM_KG * k);
       if (j0 < keys && q0 < n) {
-        const float* kr = reinterpret_cast<const float*>(K) + (size_t)min(j0 + (lane & 31), n - 1) * D + 4 * half;
+        const float* kr = reinterpret_cast<const float*>(K) + (size_t)min(j0 + (lane & 31), n - 1) * ldk + 4 * half;
 #pragma unroll
         for (int m = 0; m < D / 8; ++m) {
           const f32x4 kf = step_operands(*reinterpret_cast<const f32x4*>(kr + 8 * m));
@@ -301,8 +321,8 @@ __global__ __launch_bounds__(SM_NT, KT <= 4 ? 4 : 2) void solve_small_kernel(Tau
   }
 
   if (row_ok && half == 0 && kg == 0) {
-    a.tau[(size_t)bh * n + i] = tau;
-    if (std::is_same<E, float>::value) a.tau_lo[(size_t)bh * n + i] = 0.f;
+    a.tau[row0 + i] = tau;
+    if (std::is_same<E, float>::value) a.tau_lo[row0 + i] = 0.f;
   }
 
   // ---- mask bits, and the element lists: the lists of a row's two halves
@@ -333,7 +353,7 @@ __global__ __launch_bounds__(SM_NT, KT <= 4 ? 4 : 2) void solve_small_kernel(Tau
   __syncthreads();
   const uint32_t mask = bits;
   const int blocks = __popc(mask);
-  ListBlock* const lb = a.lists ? a.lists + ((size_t)bh * T + qb) : nullptr;
+  ListBlock* const lb = a.lists ? a.lists + blk : nullptr;
   const int use = list_use(entries, blocks, T, sizeof(E) == 4);
   bool fit = listed && use != LIST_NONE;
   int base = 0, all = 0;
@@ -371,46 +391,64 @@ __global__ __launch_bounds__(SM_NT, KT <= 4 ? 4 : 2) void solve_small_kernel(Tau
         if (half == 0 && row_ok) lb->tau[row] = tau;
       }
     }
-    if (t == 0) a.use[(size_t)bh * T + qb] = fit ? use : LIST_NONE;
+    if (t == 0) a.use[blk] = fit ? use : LIST_NONE;
   }
   if (w != 0) return;
   // mask row and row table (at most 16 key blocks)
   const bool b = lane < T && (mask >> lane & 1u), tables = a.mask != nullptr;
-  if (tables && lane < T) a.mask[((size_t)bh * T + qb) * T + lane] = b ? 1 : 0;
+  if (tables && lane < T) a.mask[blk * width + lane] = b ? 1 : 0;
   const unsigned long long m = __ballot(b);
-  if (tables && b) a.q_index[((size_t)bh * T + qb) * T + __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u)] = lane;
+  if (tables && b) a.q_index[blk * width + __builtin_amdgcn_mbcnt_lo((unsigned)m, 0u)] = lane;
   if (lane == 0) {
-    if (tables) a.q_count[(size_t)bh * T + qb] = blocks;
-    if (a.stats) {
-      a.stats[(size_t)bh * T + qb] = 1;
+    if (tables) a.q_count[blk] = blocks;
+    if (!PK && a.stats) {
+      a.stats[blk] = 1;
       a.stats[((size_t)a.BH + bh) * T + qb] = evals;
     }
   }
 }
 
-template <typename E, int D, int GK>
-hipError_t launch_small_g(const TauArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)(a.BH * a.T)), block(SM_NT);
-  if (a.n <= 256) return launch_kernel(solve_small_kernel<E, D, GK, 2>, grid, block, s, a);
-  if (a.n <= 512) return launch_kernel(solve_small_kernel<E, D, GK, 4>, grid, block, s, a);
-  return launch_kernel(solve_small_kernel<E, D, GK, 8>, grid, block, s, a);
+// (workgroups, and the longest sequence)
+template <typename E, int D, int GK, typename A>
+hipError_t launch_small_g(const A& a, int wgs, int n, hipStream_t s) {
+  const dim3 grid((unsigned)wgs), block(SM_NT);
+  if (n <= 256) return launch_kernel(solve_small_kernel<E, D, GK, 2, A>, grid, block, s, a);
+  if (n <= 512) return launch_kernel(solve_small_kernel<E, D, GK, 4, A>, grid, block, s, a);
+  return launch_kernel(solve_small_kernel<E, D, GK, 8, A>, grid, block, s, a);
 }
 
-template <typename E, int D>
-hipError_t launch_small_d(const TauArgs& a, hipStream_t s) {
-  if (a.gk == 1) return launch_small_g<E, D, 1>(a, s);
-  if (a.gk == 2) return launch_small_g<E, D, 2>(a, s);
-  if (a.gk == 4) return launch_small_g<E, D, 4>(a, s);
-  if constexpr (sizeof(E) == 2) return launch_small_g<E, D, 0>(a, s);
+template <typename E, int D, typename A>
+hipError_t launch_small_d(const A& a, int wgs, int n, hipStream_t s) {
+  if (a.gk == 1) return launch_small_g<E, D, 1>(a, wgs, n, s);
+  if (a.gk == 2) return launch_small_g<E, D, 2>(a, wgs, n, s);
+  if (a.gk == 4) return launch_small_g<E, D, 4>(a, wgs, n, s);
+  if constexpr (sizeof(E) == 2) return launch_small_g<E, D, 0>(a, wgs, n, s);
   return hipErrorInvalidValue;  // (fp32 inputs with a general alpha: solve_kernel)
+}
+
+template <typename A>
+hipError_t launch_small(const A& a, int wgs, int n, int dtype, int head_dim, hipStream_t s) {
+  if (dtype == 0)
+    return head_dim == 64 ? launch_small_d<__bf16, 64>(a, wgs, n, s) : launch_small_d<__bf16, 128>(a, wgs, n, s);
+  return head_dim == 64 ? launch_small_d<float, 64>(a, wgs, n, s) : launch_small_d<float, 128>(a, wgs, n, s);
 }
 
 }  // namespace
 
+// Compiled twice (EA_SMALL_PART, see build.py): the batched and the packed form.
+#if EA_SMALL_PART == 0
 hipError_t launch_tau_small(const TauArgs& a, int dtype, int head_dim, hipStream_t s) {
-  if (dtype == 0)
-    return head_dim == 64 ? launch_small_d<__bf16, 64>(a, s) : launch_small_d<__bf16, 128>(a, s);
-  return head_dim == 64 ? launch_small_d<float, 64>(a, s) : launch_small_d<float, 128>(a, s);
+  return launch_small(a, a.BH * a.T, a.n, dtype, head_dim, s);
 }
+#elif EA_SMALL_PART == 1
+hipError_t launch_tau_small_packed(Packed<TauArgs> a, int dtype, int head_dim, hipStream_t s) {
+  a.pk.size = 0;
+  a.pk.tiles = a.pk.lists[0];
+  const int wgs = a.pk.heads * packed_tiles(a.pk.tokens, a.pk.seq_count, 0);
+  return launch_small(a, wgs, 64 * a.pk.width, dtype, head_dim, s);
+}
+#else
+#error "EA_SMALL_PART must be 0 or 1"
+#endif
 
 }  // namespace ea

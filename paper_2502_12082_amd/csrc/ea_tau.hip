@@ -1496,7 +1496,24 @@ static bool small_solver(const TauArgs& a, int dtype, int head_dim) {
   return head_dim == 64 || a.n <= 256 || blocks <= 512;
 }
 
+// Packed sequences, none longer than `width` blocks.  As above, but what it
+// saves against workgroups that stay is less on large grids of bf16 d = 64 rows
+// with few scores above the bound.  Forward, causal, in us, solve_kernel against
+// it at c = 1, and at c = 4: 16/4 heads, d = 64, 3 sequences of up to 256 38
+// against 25, 32 against 24; 32 of 256 84 against 76, 70 against 72; 4 of 512 (8
+// heads) 52 against 31, 44 against 30; 16 of 512 117 against 104, 85 against 100;
+// 64 of 512 409 against 371, 299 against 362.  fp32, 64 of 512 831 against 664,
+// 659 against 575; 2 of up to 1000 149 against 62, 106 against 62.
+static bool small_packed(const Packed<TauArgs>& a, int dtype, int head_dim) {
+  const int n = 64 * a.pk.width;
+  if (n > SMALL_MAX_N || (dtype == 1 && a.gk == 0)) return false;
+  const int64_t blocks = (int64_t)a.pk.heads * packed_tiles(a.pk.tokens, a.pk.seq_count, 0);
+  if (n > 512) return blocks <= 384;
+  return n <= 256 || (head_dim == 64 && dtype == 1) || blocks <= (head_dim == 64 ? 1024 : 512);
+}
+
 hipError_t launch_tau_packed(const Packed<TauArgs>& a, int dtype, int head_dim, hipStream_t s) {
+  if (small_packed(a, dtype, head_dim)) return launch_tau_small_packed(a, dtype, head_dim, s);
   if (dtype == 0) return head_dim == 64 ? launch_tau_packed_bf16_64(a, s) : launch_tau_packed_bf16_128(a, s);
   return head_dim == 64 ? launch_tau_packed_f32_64(a, s) : launch_tau_packed_f32_128(a, s);
 }

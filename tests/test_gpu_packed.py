@@ -246,6 +246,22 @@ def test_element_lists(ea, d, dtype, alpha, c, causal):
     compare((o,) + ea.packed_backward(q, k, v, do, res), q, k, v, do, cu, alpha, causal, "none", c)
 
 
+@pytest.mark.parametrize("d,dtype,alpha,c", [(64, BF, 1.5, 3.0), (128, BF, 1.25, 6.0), (64, F32, 2.0, 2.0),
+                                             (128, F32, 1.5, 3.0)])
+@pytest.mark.parametrize("cu", [[0, 700, 710, 1000], [0, 256, 330, 587], [0, 255, 256, 300]])
+def test_short_sequences(ea, cu, d, dtype, alpha, c):
+    """Sequences of up to 1024, 512 and 256 keys in strided rows, listed where they are long enough."""
+    n = max(b - a for a, b in zip(cu, cu[1:]))
+    q, k, v, do, cud = make(cu, cu[-1], 4, 2, d, dtype, c=c, seed=17)
+    wide = torch.cat([q, k, v], 1)
+    q, k, v = wide[:, :4], wide[:, 4:6], wide[:, 6:]
+    for causal in (True, False):
+        plan = ea.packed_plan(cud, cu[-1], max_seqlen=n, causal=causal)
+        got = run(ea, q, k, v, do, plan, alpha)
+        compare(got, q, k, v, do, cu, alpha, causal, "short %d d%d a%g" % (n, d, alpha), c)
+        assert torch.equal(got[0], ea.packed_forward(q, k, v, plan, alpha=alpha, workspace=False)[0])
+
+
 def test_differences(ea):
     """Gradients against central differences of the fp32 forward.  Its 25600
     outputs are off by some 3e-7 each: 5e-5 on either end of the difference, so
