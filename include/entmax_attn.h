@@ -331,7 +331,7 @@ typedef struct {
  * rot_dim: a multiple of 16, 0 (norm alone) to d.  tokens may be 0.  One launch.
  */
 typedef struct {
-  int32_t tokens, heads, kv_heads, head_dim; /* head_dim in {64, 128} */
+  int32_t tokens, heads, kv_heads, head_dim; /* tokens <= 2^25, head_dim in {64, 128} */
   int32_t dtype, weight_dtype;               /* ea_dtype */
   int32_t rot_dim, interleaved;
   int32_t axes, sections[4];                 /* 1..4 axes; sections add up to rot_dim / 2 */
@@ -373,7 +373,7 @@ ea_status entmax_norm_rotary_bwd(const ea_rotary* r, const void* dq_out, const e
  * rows of the outputs are unspecified).
  */
 typedef struct {
-  int32_t tokens, seqs;            /* tokens >= 1, seqs >= 1 */
+  int32_t tokens, seqs;            /* tokens >= 1, seqs >= 1; heads * (tokens / 64 + seqs) < 2^22 */
   int32_t max_seqlen;              /* 1..131072: no sequence is longer */
   int32_t heads, kv_heads;         /* heads a multiple of kv_heads */
   int32_t head_dim, dtype;         /* as ea_shape */
@@ -429,7 +429,7 @@ ea_status entmax_packed_bwd(const ea_packed_shape* shape, const ea_params* param
  *   k, v   [requests, capacity, kv_heads, d]
  *   k_prefix, v_prefix  [prefix, kv_heads, d] (not read where prefix is 0)
  *   params alpha, scale, max_iter and tol are used
- * prefix + capacity <= 131072; rows of k and k_prefix are at most 2^24 elements
+ * prefix + capacity <= 131072, requests * heads < 2^23; rows of k and k_prefix are at most 2^24 elements
  * apart.  workspace: entmax_prefix_decode_workspace
  * bytes, 16-byte aligned (about 4.4 bytes for every query head and key, most of
  * them for rows with thousands of probabilities).  Two launches.

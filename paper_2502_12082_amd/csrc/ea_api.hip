@@ -642,8 +642,8 @@ ea_status check_rotary(const ea_rotary* r) {
     pairs += r->sections[a];
   }
   if (2 * pairs != r->rot_dim) return EA_ERR_INVALID_ARG;
-  // heads and waves of a launch are 32-bit numbers
-  if ((int64_t)r->heads + r->kv_heads > (1 << 20) || (int64_t)r->tokens > INT32_MAX / 2) return EA_ERR_UNSUPPORTED;
+  // a launch has fewer than 2^32 threads, 64 of them to a token
+  if ((int64_t)r->heads + r->kv_heads > (1 << 20) || r->tokens > (1 << 25)) return EA_ERR_UNSUPPORTED;
   return EA_OK;
 }
 
@@ -785,8 +785,8 @@ ea_status check_packed(const ea_packed_shape* s, const ea_params* p) {
   if (!dtype_ok(s->dtype) || (s->head_dim != 64 && s->head_dim != 128)) return EA_ERR_UNSUPPORTED;
   if (s->max_seqlen > MAX_SEQLEN) return EA_ERR_UNSUPPORTED;
   if ((st = check_params(p)) != EA_OK) return st;
-  // grids and row numbers over all heads are 32-bit numbers
-  if ((int64_t)s->heads * packed_tiles(s->tokens, s->seqs, 0) > INT32_MAX / 2) return EA_ERR_UNSUPPORTED;
+  // a launch has fewer than 2^32 threads: up to 512 to a tile, 16 to a row
+  if ((int64_t)s->heads * packed_tiles(s->tokens, s->seqs, 0) >= (1 << 22)) return EA_ERR_UNSUPPORTED;
   return EA_OK;
 }
 
@@ -1066,7 +1066,7 @@ ea_status check_decode(const ea_decode_shape* s) {
   if (s->prefix < 0 || s->capacity < 0) return EA_ERR_INVALID_ARG;
   if (!dtype_ok(s->dtype) || (s->head_dim != 64 && s->head_dim != 128)) return EA_ERR_UNSUPPORTED;
   if ((int64_t)s->prefix + s->capacity > MAX_SEQLEN) return EA_ERR_UNSUPPORTED;
-  if ((int64_t)s->requests * s->heads > INT32_MAX / 2) return EA_ERR_UNSUPPORTED;
+  if ((int64_t)s->requests * s->heads >= (1 << 23)) return EA_ERR_UNSUPPORTED;  // (256 threads a row, fewer than 2^32)
   return EA_OK;
 }
 

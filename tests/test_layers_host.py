@@ -262,3 +262,21 @@ def test_rows_too_far_apart():
         strides = ea.DecodeStrides(near, near, k, near, kp, near, 4096, 4096)
         assert ea._lib.entmax_prefix_decode(shape, params, strides, 4096, 4096, 4096, 4096, 4096, 4096, 4096, 4096,
                                             1 << 20, None) == ea.EA_ERR_INVALID_ARG
+
+
+def test_grids_of_one_launch():
+    """What a launch cannot hold is refused by the sizes, before any launch."""
+    lib, n, sizes = ea._lib, ctypes.c_size_t(), ea.PackedSizes()
+    params = ea.make_params(1.5, None, True, True, None, None, head_dim=64)
+    size = lambda tokens, heads: lib.entmax_packed_sizes(ea.PackedShape(tokens, 1, 1000, heads, 1, 64, ea.EA_BF16),
+                                                        ctypes.byref(params), ctypes.byref(sizes))
+    assert size(64 * (2 ** 20 - 2), 4) == ea.EA_OK
+    assert size(64 * (2 ** 20 - 1), 4) == ea.EA_ERR_UNSUPPORTED
+    rows = lambda requests: lib.entmax_prefix_decode_workspace(
+        ea.DecodeShape(requests, 8, 1, 64, ea.EA_BF16, 64, 64), ctypes.byref(n))
+    assert rows(2 ** 20 - 1) == ea.EA_OK
+    assert rows(2 ** 20) == ea.EA_ERR_UNSUPPORTED
+    tokens = lambda t: lib.entmax_norm_rotary_workspace(
+        ea.Rotary(t, 1, 1, 64, ea.EA_BF16, ea.EA_BF16, 64, 0, 1, (ctypes.c_int32 * 4)(32), 1e-6), ctypes.byref(n))
+    assert tokens(2 ** 25) == ea.EA_OK
+    assert tokens(2 ** 25 + 1) == ea.EA_ERR_UNSUPPORTED
