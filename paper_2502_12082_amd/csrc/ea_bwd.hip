@@ -13,9 +13,14 @@
 // the lookup tables as in App. A.5).  `scale` appears because the entmax
 // input is scale * Q K^T; no alpha factor survives the chain rule.
 //
-// Precision: S and dP are bf16 x bf16 products accumulated in fp32; P is
-// rounded to bf16 for P^T dO; dS is fed to the MFMA as a two-term bf16 split
-// (hi + lo) so dK and dQ keep ~16 mantissa bits of dS; outputs are fp32.
+// Precision: S and dP are bf16 x bf16 products accumulated in fp32; dS is fed to
+// the MFMA as a two-term bf16 split (hi + lo) so dK and dQ keep ~16 mantissa
+// bits of dS; outputs are fp32.  P is rounded to bf16 for P^T dO in the batched
+// forms, whose dV is fp32, and split in two like dS in the packed forms: their
+// dV is rounded once, to the inputs' type, and a P of 8 bits showed beside that
+// (sequences of 444 to 3000 rows, 16/4 heads, d = 128: 2.3e-3 relative in the
+// 2-norm against 1.7e-3 of the rounding alone), and not in query blocks with
+// element lists, which keep fp32 P.
 //
 // gfx950 layout: 32 resident rows per wave in registers (K and V rows for
 // dK/dV; Q and dO rows for dQ); the other side's 64-row tiles are copied by
@@ -791,12 +796,18 @@ __global__ __launch_bounds__(BWD_NT) void dkdv_kernel(A a) {
     }
 #pragma unroll
     for (int t = 0; t < PS; ++t) {
-      const typename M::frag pa = M::pack(p, t);
-      typename M::frag dh, dl;
+      typename M::frag pa, dh, dl;
+      [[maybe_unused]] typename M::frag pl;
+      if constexpr (PK)
+        M::pack_split(p, t, pa, pl);
+      else
+        pa = M::pack(p, t);
       M::pack_split(dsv, t, dh, dl);
 #pragma unroll
       for (int nt = 0; nt < NTD; ++nt) {
-        dv[nt] = M::mma(pa, lds_perm_frag<E, D>(dt, 32 * nt, 32 * qh, t), dv[nt]);
+        const typename M::frag ob_ = lds_perm_frag<E, D>(dt, 32 * nt, 32 * qh, t);
+        dv[nt] = M::mma(pa, ob_, dv[nt]);
+        if constexpr (PK && !M::exact_operands) dv[nt] = M::mma(pl, ob_, dv[nt]);
         const typename M::frag qb_ = lds_perm_frag<E, D>(qt, 32 * nt, 32 * qh, t);
         dk[nt] = M::mma(dh, qb_, dk[nt]);
         if constexpr (!M::exact_operands) dk[nt] = M::mma(dl, qb_, dk[nt]);
@@ -910,6 +921,10 @@ __global__ __launch_bounds__(BWD_NT) void dkdv_kernel(A a) {
 // the waves of a key block that does not list the staged query block only
 // keep the barriers.
 //
+// The packed form takes P in two terms as well.  A second array of operands
+// would not fit beside the three stages (160 KB in all, and 1.5 KB of tau and
+// delta), so the second term travels as the eight bits that follow the first.
+//
 // The Q and dO tiles (with their tau and delta) go through three LDS stages,
 // so each copy has two steps to land, and the barriers wait only for LDS
 // traffic: a plain workgroup barrier would also wait for the copies in
@@ -935,6 +950,9 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(A a) {
   __shared__ __attribute__((aligned(16))) float del_s[3][BLK];
   // operands posted by each wave: [wave][P, dS hi, dS lo][step][lane]
   __shared__ __attribute__((aligned(16))) u32x4 post[BWD2_NT / 64][3][PS][64];
+  // packed forms: the second term of P, eight bits a value: [wave][lane]
+  __shared__ __attribute__((aligned(16))) u32x4 post_low[PK ? BWD2_NT / 64 : 1][PK ? 64 : 1];
+  static_assert(PS == 2, "the low bits of a lane's operands are 16 bytes");
 
   const int lane = lane_id(), w = wave_id();
   const int kh = (w >> 1) & 1, ch = w & 1;
@@ -1094,8 +1112,10 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(A a) {
 
   // S = Q K^T, dP = dO V^T of query half qh (rows = queries) for this wave's
   // keys; masked sub-tiles set invalid scores to -inf (then P = dS = 0).
+  // P of the packed forms is rounded to 24 bits: its upper 16 are the bf16 operand
+  // pa, the next eight its byte of `low` (see split_low).
   auto operands = [&](const E* qt, const E* dt, const float* ts, const float* ds_, int qh,
-                      bool masked, int i0, F* pa, F* dh, F* dl) {
+                      bool masked, int i0, F* pa, F* dh, F* dl, u32x4& low) {
     f32x16 s = zero16(), dp = zero16();
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
@@ -1126,18 +1146,47 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(A a) {
     }
 #pragma unroll
     for (int t = 0; t < PS; ++t) {
-      pa[t] = M::pack(p, t);
+      if constexpr (PK) {
+        u32x4 hw;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {  // (P is 0 to 1: no sign, no overflow)
+          const uint32_t x = __float_as_uint(p[8 * t + 2 * e]) + 0x80u, y = __float_as_uint(p[8 * t + 2 * e + 1]) + 0x80u;
+          hw[e] = x >> 16 | (y & 0xFFFF0000u);
+          const uint32_t two = (x >> 8 & 0xFFu) | (y & 0xFF00u);
+          low[2 * t + (e >> 1)] = e & 1 ? low[2 * t + (e >> 1)] | two << 16 : two;
+        }
+        pa[t] = __builtin_bit_cast(F, hw);
+      } else {
+        pa[t] = M::pack(p, t);
+      }
       M::pack_split(dsv, t, dh[t], dl[t]);
     }
   };
+  // The second term of P, exact in bf16: its bits behind the first 16.
+  auto split_low = [&](const F& pa, const u32x4& low, int t) {
+    const u32x4 hw = __builtin_bit_cast(u32x4, pa);
+    u32x4 lw;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t two = low[2 * t + (e >> 1)] >> (16 * (e & 1)), x = hw[e] << 16, y = hw[e] & 0xFFFF0000u;
+      const float lx = __uint_as_float(x | (two & 0xFFu) << 8) - __uint_as_float(x);
+      const float ly = __uint_as_float(y | (two & 0xFF00u)) - __uint_as_float(y);
+      lw[e] = __float_as_uint(lx) >> 16 | (__float_as_uint(ly) & 0xFFFF0000u);
+    }
+    return __builtin_bit_cast(F, lw);
+  };
   // dV += P^T dO and dK += dS^T Q over query half qh, this wave's columns
-  auto accum = [&](const E* qt, const E* dt, int qh, const F* pa, const F* dh, const F* dl) {
+  auto accum = [&](const E* qt, const E* dt, int qh, const F* pa, const F* dh, const F* dl, const u32x4& low) {
 #pragma unroll
     for (int t = 0; t < PS; ++t) {
+      [[maybe_unused]] F pl;
+      if constexpr (PK) pl = split_low(pa[t], low, t);
 #pragma unroll
       for (int nt = 0; nt < NTH; ++nt) {
         const int col0 = 32 * (ch * NTH + nt);
-        dv[nt] = M::mma(pa[t], lds_perm_frag<E, D>(dt, col0, 32 * qh, t), dv[nt]);
+        const F ob_ = lds_perm_frag<E, D>(dt, col0, 32 * qh, t);
+        dv[nt] = M::mma(pa[t], ob_, dv[nt]);
+        if constexpr (PK) dv[nt] = M::mma(pl, ob_, dv[nt]);
         const F qb_ = lds_perm_frag<E, D>(qt, col0, 32 * qh, t);
         dk[nt] = M::mma(dh[t], qb_, dk[nt]);
         dk[nt] = M::mma(dl[t], qb_, dk[nt]);
@@ -1190,16 +1239,18 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(A a) {
   };
   // S, dP, P, dS of query half ch (kept for this wave, posted for its partner)
   F pa[PS], dh[PS], dl[PS];
+  u32x4 low = {};
   auto phase1 = [&](int qb, int b, int tb) {
     const int i0 = qb * BLK + 32 * ch;
     if (!half_valid(i0)) return;
-    operands(qbuf[b], dobuf[b], tau_s[tb], del_s[tb], ch, half_masked(i0), i0, pa, dh, dl);
+    operands(qbuf[b], dobuf[b], tau_s[tb], del_s[tb], ch, half_masked(i0), i0, pa, dh, dl, low);
 #pragma unroll
     for (int t = 0; t < PS; ++t) {
       post[w][0][t][lane] = __builtin_bit_cast(u32x4, pa[t]);
       post[w][1][t][lane] = __builtin_bit_cast(u32x4, dh[t]);
       post[w][2][t][lane] = __builtin_bit_cast(u32x4, dl[t]);
     }
+    if constexpr (PK) post_low[w][lane] = low;
   };
   // both query halves into this wave's columns: the partner's half first
   auto phase2 = [&](int qb, int b) {
@@ -1211,9 +1262,11 @@ __global__ __launch_bounds__(BWD2_NT, 2) void dkdv2_kernel(A a) {
         xh[t] = __builtin_bit_cast(F, post[w ^ 1][1][t][lane]);
         xl[t] = __builtin_bit_cast(F, post[w ^ 1][2][t][lane]);
       }
-      accum(qbuf[b], dobuf[b], ch ^ 1, xa, xh, xl);
+      u32x4 xlow = {};
+      if constexpr (PK) xlow = post_low[w ^ 1][lane];
+      accum(qbuf[b], dobuf[b], ch ^ 1, xa, xh, xl, xlow);
     }
-    if (half_valid(qb * BLK + 32 * ch)) accum(qbuf[b], dobuf[b], ch, pa, dh, dl);
+    if (half_valid(qb * BLK + 32 * ch)) accum(qbuf[b], dobuf[b], ch, pa, dh, dl, low);
   };
 
   // `left`: only the query blocks left in `unlisted`, a loop of its own, so
