@@ -369,8 +369,8 @@ ea_status entmax_norm_rotary_bwd(const ea_rotary* r, const void* dq_out, const e
  * entmax_packed_plan lists the sequences' tiles, for every call on the same
  * cu, from the device's cu in one launch; the host does not wait.  A range of
  * cu that is empty holds no rows; one that is negative, overlaps an earlier
- * one, ends behind `tokens` or is longer than max_seqlen is not computed (its
- * rows of the outputs are unspecified).
+ * one, ends behind `tokens` or is longer than max_seqlen is left out (see
+ * zero_rest).
  */
 typedef struct {
   int32_t tokens, seqs;            /* tokens >= 1, seqs >= 1; heads * (tokens / 64 + seqs) < 2^22 */
@@ -405,7 +405,9 @@ ea_status entmax_packed_sizes(const ea_packed_shape* shape, const ea_params* par
  * are contiguous and of the inputs' dtype (each rounded once, from fp32 sums).
  * Rows of q, k, v, o and dout are at most 2^24 elements apart.
  * Rows that belong to no sequence (before cu[0], behind cu[seqs]) are left as
- * they are, or with zero_rest != 0 set to 0.  Launches: 2 (forward), 3 or 4
+ * they are, or with zero_rest != 0 set to 0; those of sequences that are left
+ * out are NaN then (without: O's are left as they are, the gradients' are
+ * unspecified).  Launches: 2 (forward), 3 or 4
  * (backward).
  */
 ea_status entmax_packed_fwd(const ea_packed_shape* shape, const ea_params* params, const void* plan,

@@ -1058,7 +1058,8 @@ def packed_plan(cu_seqlens, tokens, max_seqlen=None, causal=True) -> PackedPlan:
     launch; the host does not wait for cu_seqlens.  max_seqlen: no sequence is
     longer (default: tokens); the residuals' tables grow with it.  A sequence
     that is longer, reaches outside the tensors or overlaps an earlier one is
-    not computed: its rows of the outputs are unspecified."""
+    left out: its rows are NaN in outputs that a call makes, and in given ones
+    stay (O) or are unspecified (gradients)."""
     if not isinstance(cu_seqlens, torch.Tensor) or cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 2:
         raise ValueError("cu_seqlens must be a [seqs + 1] tensor of at least one sequence")
     _need(cu_seqlens, "cu_seqlens", cu_seqlens.shape, torch.int32)

@@ -1835,8 +1835,15 @@ __global__ __launch_bounds__(DQ_NT, 2) void dq_kernel(A a) {
   [[maybe_unused]] Place at;
   if constexpr (PK) {
     const bool work = packed_place(a.pk, blockIdx.x, a.pk.heads, false, at);
-    if (at.item == 0 && a.pk.zero_rest)
-      zero_rest<E, D, DQ_NT>(a.pk, reinterpret_cast<E*>(a.dq), Strides{a.pk.heads * D, D}, at.head);
+    if (a.pk.zero_rest) {
+      const Strides rows{a.pk.heads * D, D}, kv_rows{a.pk.kv_heads * D, D};
+      if (at.item == 0) zero_rest<E, D, DQ_NT>(a.pk, reinterpret_cast<E*>(a.dq), rows, at.head);
+      left_out<E, D, DQ_NT>(a.pk, at, work, reinterpret_cast<E*>(a.dq), rows, at.head);
+      if (at.head < a.pk.kv_heads) {  // (dK and dV too: this launch is the last)
+        left_out<E, D, DQ_NT>(a.pk, at, work, reinterpret_cast<E*>(a.dk), kv_rows, at.head);
+        left_out<E, D, DQ_NT>(a.pk, at, work, reinterpret_cast<E*>(a.dv), kv_rows, at.head);
+      }
+    }
     if (!work) return;
   }
   const int n = PK ? at.n : a.n, T = PK ? at.T : a.T;

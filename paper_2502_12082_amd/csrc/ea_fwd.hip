@@ -174,7 +174,10 @@ __global__ __launch_bounds__(FWD_NT, !TRAIN && D == 64 && sizeof(E) == 2 ? 4 : 2
       return;
     }
     const bool work = packed_place(a.pk, blockIdx.x, a.pk.heads, false, at);
-    if (at.item == 0 && a.pk.zero_rest) zero_rest<E, D, FWD_NT>(a.pk, static_cast<E*>(a.o), a.pk.o, at.head);
+    if (a.pk.zero_rest) {
+      if (at.item == 0) zero_rest<E, D, FWD_NT>(a.pk, static_cast<E*>(a.o), a.pk.o, at.head);
+      left_out<E, D, FWD_NT>(a.pk, at, work, static_cast<E*>(a.o), a.pk.o, at.head);
+    }
     if (!work) return;
   } else {
     const int nqb = a.BH * a.T;

@@ -107,14 +107,16 @@ struct Strides {
   int64_t head;  // and from head to head
 };
 struct PackedSeq {
-  int32_t start, len, block, unused;  // block: its first query block
+  int32_t start, len, block;  // block: its first query block
+  int32_t gap;                // rows right before it that a sequence which is left out holds
 };
 struct PackedTile {
   int32_t seq, tile;
 };
 struct PackedHeader {
   int32_t count[2];    // tiles of 64 and 128 rows
-  int32_t begin, end;  // the rows that belong to sequences
+  int32_t begin, end;  // the rows that belong to sequences,
+  int32_t last;        // of those that are computed up to here
 };
 struct PackedArgs {
   const PackedHeader* header;
@@ -124,7 +126,8 @@ struct PackedArgs {
   int size, seq_count;
   int heads, kv_heads, group, tokens, blocks, width;
   Strides q, k, v, o;  // (o: also of its gradient)
-  int zero_rest;       // whether the rows of no sequence are set to 0 in what is written
+  int zero_rest;       // whether in what is written the rows of no sequence are set to 0, and
+                       // those of sequences that are left out to NaN
   int parts;           // dK/dV: workgroups that share the query heads of a key head
   float *dk_part, *dv_part;  // parts > 1: [parts, tokens, kv_heads, D] sums to add up
   // with element lists there are always parts, one more than `parts` (the list

@@ -18,6 +18,7 @@ struct is_packed<Packed<A>> : std::true_type {};
 struct Place {
   int head, part, item, tile, seq, start, n, T;
   int block;             // the sequence's first block among all
+  int gap;               // rows before it of a sequence that is left out
   size_t row0, blk0;  // of the query head: its first row in tau, and first block in the tables
 };
 
@@ -40,20 +41,35 @@ __device__ __forceinline__ bool packed_place(const PackedArgs& pk, int b, int he
   at.T = (at.n + BLK - 1) / BLK;
   at.row0 = (size_t)at.head * pk.tokens + at.start;
   at.block = seq[2];
+  at.gap = seq[3];
   at.blk0 = (size_t)at.head * pk.blocks + at.block;
   return at.n > 0;
 }
 
-// Sets the rows of `head` that belong to no sequence to 0 (every thread of a
+// Sets rows [r0, r1) of `head` to the 32-bit word `word` (every thread of a
 // workgroup of NT).  D values of type E, 16-byte aligned rows.
 template <typename E, int D, int NT>
-__device__ void zero_rest(const PackedArgs& pk, E* base, const Strides& st, int head) {
+__device__ __forceinline__ void fill_rows(E* base, const Strides& st, int head, int r0, int r1, uint32_t word) {
   constexpr int VEC = 16 / (int)sizeof(E), CPR = D / VEC;
-  const int begin = pk.header->begin, rest = begin + pk.tokens - pk.header->end;
-  for (int64_t x = threadIdx.x; x < (int64_t)rest * CPR; x += NT) {
-    const int r = (int)(x / CPR), row = r < begin ? r : r - begin + pk.header->end;
-    *reinterpret_cast<u32x4*>(base + (int64_t)row * st.row + head * st.head + (x % CPR) * VEC) = u32x4{0, 0, 0, 0};
-  }
+  for (int64_t x = threadIdx.x; x < (int64_t)(r1 - r0) * CPR; x += NT)
+    *reinterpret_cast<u32x4*>(base + (r0 + x / CPR) * st.row + head * st.head + (x % CPR) * VEC) =
+        u32x4{word, word, word, word};
+}
+// Sets the rows of `head` that belong to no sequence to 0.
+template <typename E, int D, int NT>
+__device__ void zero_rest(const PackedArgs& pk, E* base, const Strides& st, int head) {
+  fill_rows<E, D, NT>(base, st, head, 0, pk.header->begin, 0u);
+  fill_rows<E, D, NT>(base, st, head, pk.header->end, pk.tokens, 0u);
+}
+// The rows of `head` that belong to sequences which are left out: NaN, since
+// whoever gave such a sequence should see it.  By the workgroups of item 0 (the
+// rows behind the last sequence that is computed; `work`: whether it has one)
+// and of every sequence's tile 0 (those before it).
+template <typename E, int D, int NT>
+__device__ void left_out(const PackedArgs& pk, const Place& at, bool work, E* base, const Strides& st, int head) {
+  constexpr uint32_t NAN_WORD = sizeof(E) == 2 ? 0x7FC07FC0u : 0x7FC00000u;
+  if (at.item == 0) fill_rows<E, D, NT>(base, st, head, pk.header->last, pk.header->end, NAN_WORD);
+  if (work && at.tile == 0) fill_rows<E, D, NT>(base, st, head, at.start - at.gap, at.start, NAN_WORD);
 }
 
 }  // namespace ea

@@ -45,8 +45,11 @@ __device__ __forceinline__ int tiles_of(int rows, int size) { return (rows + (64
 __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(blockIdx.x * (PLAN_NT / 64) + wave_id());
-  // the wave's sequence, which 64 of its tiles, and the blocks before it
-  int seq = -1, start = 0, len = 0, chunk = 0, waves = 0, block = 0, first = -1, last = 0, total[2] = {};
+  // the wave's sequence, which 64 of its tiles, the blocks before it, and the
+  // rows between it and the sequence before (or cu[0])
+  int seq = -1, start = 0, len = 0, chunk = 0, waves = 0, block = 0, gap = 0, total[2] = {};
+  const int cu0 = min(max(((const ci32*)a.cu)[0], 0), a.tokens);
+  int first = cu0, last = cu0;
   walk(a, [&](int s, int begin, int n) {
     const int need = max(tiles_of(n, 6), 1);  // (an empty sequence has a record too)
     if (wave >= waves && wave < waves + need) {
@@ -55,18 +58,22 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
       len = n;
       chunk = wave - waves;
       block = total[0];
+      gap = n ? max(begin - last, 0) : 0;
     }
     waves += need;
     if (n) {
-      if (first < 0) first = begin;
+      first = min(first, begin);
       last = begin + n;
     }
 #pragma unroll
     for (int z = 0; z < 2; ++z) total[z] += tiles_of(n, z);
   });
-  if (wave == 0 && lane == 0) *a.header = PackedHeader{{total[0], total[1]}, max(first, 0), last};
+  if (wave == 0 && lane == 0) {
+    const int end = max(last, min(((const ci32*)a.cu)[a.seq_count], a.tokens));
+    *a.header = PackedHeader{{total[0], total[1]}, first, end, last};
+  }
   if (seq < 0) return;
-  if (chunk == 0 && lane == 0) a.seqs[seq] = PackedSeq{start, len, block, 0};
+  if (chunk == 0 && lane == 0) a.seqs[seq] = PackedSeq{start, len, block, gap};
   const int t = 64 * chunk + lane;
   // tiles before tile t of each size: longer ones of any sequence, and as long
   // ones of an earlier one.  Causal tiles are as long as their number, others

@@ -1,12 +1,13 @@
-"""Packed attention where its paths meet: the precision of dV by products."""
+"""Packed attention where its paths meet: the precision of dV by products, and
+sequences that are left out."""
 import pytest
 
 torch = pytest.importorskip("torch")
 from layer_util import check, packed64  # noqa: E402
-from test_gpu_packed import ea, make  # noqa: E402,F401
+from test_gpu_packed import ea, make, run  # noqa: E402,F401
 
 pytestmark = pytest.mark.gpu
-BF = torch.bfloat16
+BF, F32 = torch.bfloat16, torch.float32
 
 
 @pytest.mark.parametrize("d,hq,hk", [(64, 4, 2), (128, 4, 1)])
@@ -24,3 +25,41 @@ def test_dv_holds_p_in_two_terms(ea, d, hq, hk, lists):
     dv = ea.packed_backward(q, k, v, do, res)[2]
     _, _, _, want, dv_abs = packed64(q, k, v, cu, 1.5, d ** -0.5, True, do)
     check("dv d%d lists %s" % (d, lists), dv, want, 1e-4, dv_abs * 2.0 ** -15)
+
+
+@pytest.mark.parametrize("hq,hk,d,dtype", [(4, 2, 64, BF), (4, 1, 128, BF), (2, 2, 128, BF), (4, 2, 64, F32)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_sequences_that_are_left_out(ea, hq, hk, d, dtype, causal):
+    """Too long, backwards, overlapping or outside: NaN in tensors that the
+    calls make, the rows of no sequence 0, the others as by themselves."""
+    tokens = 400
+    q, k, v, do, _ = make([0, 1], tokens, hq, hk, d, dtype, seed=22)
+    for cu, fine in (([5, 40, 120, 190, 390], [(5, 40), (120, 190)]),    # the second and the last are too long
+                     ([0, 100, 130, 390, 400], [(100, 130), (390, 400)]),  # the first is, and the third
+                     ([3, 60, 30, 90, 380], [(3, 60)]),                    # backwards, then over rows of the first
+                     ([10, 200, 399], []),                                 # none is left
+                     ([0, 50, 500, 80, 120], [(0, 50), (80, 120)])):       # one ends outside
+        cud = torch.tensor(cu, dtype=torch.int32, device="cuda")
+        plan = ea.packed_plan(cud, tokens, max_seqlen=70, causal=causal)
+        got = run(ea, q, k, v, do, plan, 1.5)
+        left = torch.ones(tokens, dtype=torch.bool, device="cuda")
+        for a, b in fine:
+            alone = torch.tensor([0, b - a], dtype=torch.int32, device="cuda")
+            want = run(ea, *(t[a:b] for t in (q, k, v, do)), ea.packed_plan(alone, b - a, causal=causal), 1.5)
+            left[a:b] = False
+            for x, y in zip(got, want):  # (alone in other parts: sums in another order)
+                check("%s %d" % (cu, a), x[a:b], y.double().cpu(), 1e-4, 2.0 ** -7 * y.double().cpu().abs())
+        inside = torch.zeros_like(left)
+        inside[cu[0]:cu[-1]] = True
+        for x in got:
+            assert torch.isnan(x[left & inside]).all(), cu
+            assert not x[left & ~inside].any(), cu
+        # given tensors keep their rows of no sequence, and those of the others in O
+        out = torch.full_like(q, 3.0)
+        grads = [torch.full_like(t, 5.0) for t in (q, k, v)]
+        _, res = ea.packed_forward(q, k, v, plan, alpha=1.5, out=out)
+        ea.packed_backward(q, k, v, do, res, *grads)
+        assert (out[left] == 3.0).all()
+        for x, y in zip([out] + grads, got):
+            assert torch.equal(x[~left], y[~left])
+            assert (x[left & ~inside] == (3.0 if x is out else 5.0)).all()
