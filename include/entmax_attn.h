@@ -373,7 +373,7 @@ ea_status entmax_norm_rotary_bwd(const ea_rotary* r, const void* dq_out, const e
  * zero_rest).
  */
 typedef struct {
-  int32_t tokens, seqs;            /* tokens >= 1, seqs >= 1; heads * (tokens / 64 + seqs) < 2^22 */
+  int32_t tokens, seqs;            /* tokens >= 1, seqs 1..65536; heads * (tokens / 64 + seqs) < 2^22 */
   int32_t max_seqlen;              /* 1..131072: no sequence is longer */
   int32_t heads, kv_heads;         /* heads a multiple of kv_heads */
   int32_t head_dim, dtype;         /* as ea_shape */

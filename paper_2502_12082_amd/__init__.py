@@ -1054,7 +1054,7 @@ class PackedPlan:
 
 def packed_plan(cu_seqlens, tokens, max_seqlen=None, causal=True) -> PackedPlan:
     """Lists the tiles of the sequences cu_seqlens[s] .. cu_seqlens[s + 1] (int32
-    [seqs + 1] on the device, ascending) of tensors with `tokens` rows.  One
+    [seqs + 1] on the device, ascending; up to 65536 sequences) of tensors with `tokens` rows.  One
     launch; the host does not wait for cu_seqlens.  max_seqlen: no sequence is
     longer (default: tokens); the residuals' tables grow with it.  A sequence
     that is longer, reaches outside the tensors or overlaps an earlier one is

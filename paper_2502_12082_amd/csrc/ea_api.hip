@@ -744,6 +744,7 @@ namespace {
 
 ea_status check_plan(int32_t tokens, int32_t seqs) {
   if (tokens < 1 || seqs < 1) return EA_ERR_INVALID_ARG;
+  if (seqs > MAX_SEQS) return EA_ERR_UNSUPPORTED;
   // tiles and rows are 32-bit numbers
   return (int64_t)tokens / 64 + seqs > (1 << 26) ? EA_ERR_UNSUPPORTED : EA_OK;
 }

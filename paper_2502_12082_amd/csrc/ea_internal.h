@@ -148,6 +148,9 @@ constexpr int PACKED_SOLVERS = 768;
 // all can have.
 constexpr int packed_tiles(int tokens, int seqs, int size) { return tokens / (64 << size) + seqs; }
 
+// The most sequences of a plan (see plan_kernel).
+constexpr int MAX_SEQS = 1 << 16;
+
 struct PlanArgs {
   const int32_t* cu;  // [seqs + 1]
   PackedHeader* header;

@@ -1,9 +1,9 @@
-"""Packed attention where its paths meet: the precision of dV by products, and
-sequences that are left out."""
+"""Packed attention where its paths meet: the precision of dV by products,
+sequences that are left out, many sequences."""
 import pytest
 
 torch = pytest.importorskip("torch")
-from layer_util import check, packed64  # noqa: E402
+from layer_util import HALF_STEP, check, packed64  # noqa: E402
 from test_gpu_packed import ea, make, run  # noqa: E402,F401
 
 pytestmark = pytest.mark.gpu
@@ -63,3 +63,26 @@ def test_sequences_that_are_left_out(ea, hq, hk, d, dtype, causal):
         for x, y in zip([out] + grads, got):
             assert torch.equal(x[~left], y[~left])
             assert (x[left & ~inside] == (3.0 if x is out else 5.0)).all()
+
+
+def test_thousands_of_sequences(ea):
+    """Every row in the place that its sequence gives it, at 20000 sequences: with
+    one key a sequence's rows are V itself, so every sequence is checked."""
+    g = torch.Generator().manual_seed(25)
+    lens = torch.randint(0, 4, (20000,), generator=g)
+    lens[[7, 9999, 19999]] = torch.tensor([300, 65, 128])
+    cu = torch.cat([torch.zeros(1, dtype=torch.int64), lens.cumsum(0)])
+    tokens = int(cu[-1])
+    q, k, v, do, _ = make([0, 1], tokens, 2, 1, 64, BF, c=2.0, seed=26)
+    plan = ea.packed_plan(cu.int().cuda(), tokens, max_seqlen=300)
+    got = run(ea, q, k, v, do, plan, 1.5)
+    first = cu[:-1][lens > 0].cuda()  # causal: a first row sees itself alone
+    assert torch.equal(got[0][first], v[first].expand(-1, 2, -1))
+    for s in [7, 9999, 19999] + list(range(0, 20000, 997)):
+        a, b = int(cu[s]), int(cu[s + 1])
+        if a == b:
+            continue
+        want = packed64(q[a:b], k[a:b], v[a:b], [0, b - a], 1.5, 0.125, True, do[a:b])
+        for name, x, y in zip(("o", "dq", "dk"), got, want):
+            check("%d %s" % (s, name), x[a:b], y, 4e-3)
+        check("%d dv" % s, got[3][a:b], want[3], 1e-3, want[4] * HALF_STEP[BF])
