@@ -813,10 +813,11 @@ int packed_parts(const ea_packed_shape* s) {
 }
 
 // The solver's workgroups of 128 rows use half a slot each, and no more of them
-// run at a time than PACKED_SOLVERS.
-int64_t packed_slots(const ea_packed_shape* s) {
+// run at a time than packed_solvers().
+int64_t packed_slots(const ea_packed_shape* s, const ea_params* p) {
   const int64_t tiles = (int64_t)s->heads * packed_tiles(s->tokens, s->seqs, 1);
-  return ((tiles < PACKED_SOLVERS ? tiles : PACKED_SOLVERS) + 1) / 2;
+  const int64_t most = packed_solvers(s->dtype == EA_F32, s->head_dim, gamma_kind(p->alpha));
+  return ((tiles < most ? tiles : most) + 1) / 2;
 }
 // The backward's workspace: delta, the parts of dK and dV where there are some
 // (with element lists always, and one more), and with lists their buckets.
@@ -921,7 +922,7 @@ ea_status entmax_packed_sizes(const ea_packed_shape* shape, const ea_params* par
   if (!out) return EA_ERR_INVALID_ARG;
   PackedResiduals r;
   out->residuals = residual_parts(shape, params, nullptr, &r);
-  out->ws_fwd = (size_t)packed_slots(shape) * SOLVE_SLOT_BYTES;
+  out->ws_fwd = (size_t)packed_slots(shape, params) * SOLVE_SLOT_BYTES;
   out->lists = packed_lists_bytes(shape);
   PackedBwdWs w;
   out->ws_bwd = packed_ws_bwd(shape, false, nullptr, &w);
@@ -940,7 +941,7 @@ ea_status entmax_packed_fwd(const ea_packed_shape* shape, const ea_params* param
   if ((st = check_packed_lists(shape, lists, lists_bytes)) != EA_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const PackedArgs pk = packed_args(shape, plan, strides, zero_rest);
-  const int64_t most = packed_slots(shape);
+  const int64_t most = packed_slots(shape, params);
   int64_t slots = workspace ? (int64_t)(ws_bytes / SOLVE_SLOT_BYTES) : 0;
   if (slots > most) slots = most;
   Packed<TauArgs> ta{};

@@ -142,8 +142,13 @@ struct Packed : A {
 };
 
 // Workgroups of the packed solver that run at a time: three on each of 256
-// compute units.
-constexpr int PACKED_SOLVERS = 768;
+// compute units; with fp32 inputs at d = 128, whose key tiles take 68 KB and
+// whose queries 128 registers, two, and for a general alpha (gk = 0), which
+// refines tau in fp64 in as many registers again, one.
+constexpr int packed_solver_occupancy(bool f32, int head_dim, int gk) {
+  return !f32 || head_dim != 128 ? 3 : gk != 0 ? 2 : 1;
+}
+constexpr int packed_solvers(bool f32, int head_dim, int gk) { return 256 * packed_solver_occupancy(f32, head_dim, gk); }
 // The most tiles of 64 << size rows that `seqs` sequences of `tokens` rows in
 // all can have.
 constexpr int packed_tiles(int tokens, int seqs, int size) { return tokens / (64 << size) + seqs; }

@@ -99,6 +99,8 @@ __device__ __forceinline__ void solve_tile(const A& a, const int tile, const int
     LdsLists lists[IN_LDS ? 1 : 0];
   };
   __shared__ __attribute__((aligned(16))) Pool pool;
+  static_assert(!PK || (sizeof(Pool) + 2048) * packed_solver_occupancy(sizeof(E) == 4, D, GK) <= 160 * 1024,
+                "the packed solver's workgroups share a compute unit's LDS");
   auto& kbuf = pool.kbuf;
   // bit kb of word kb / 32: key block kb holds a positive probability for a
   // row of the query block (one per wave with G = 2, per pair of waves with
@@ -1376,6 +1378,17 @@ __device__ __forceinline__ void solve_tile(const A& a, const int tile, const int
   }
 }
 
+// Waves per SIMD that an instance is compiled for.  (The packed fp32 d = 128
+// form takes 271 registers if three are asked for, which LDS does not allow,
+// and then runs one, 768 workgroups in three lots.  Forward, causal, us, so and
+// now: 32/8 heads, 4096 rows, c = 1 1318 and 1121; 16/4 heads, four sequences of
+// 2048, c = 2 676 and 584; 12/4 heads, 8192 rows, c = 4 1300 and 1108.)
+template <typename E, int D, int GK, int G, typename A>
+constexpr int solve_waves() {
+  if (is_packed<A>::value) return packed_solver_occupancy(sizeof(E) == 4, D, GK);
+  return G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 128 ? 1 : 2);
+}
+
 // Tile a.tile0 + blockIdx.x.  The packed form's workgroups stay and take one
 // tile after another instead: the tiles of sequences of many lengths, in
 // launches of one per slot, would leave most of the device idle at the end of
@@ -1385,7 +1398,7 @@ __device__ __forceinline__ void solve_tile(const A& a, const int tile, const int
 // time (a workgroup stays on its XCD and with it its head's keys): those that
 // had the longest of one round have the shortest of the next.
 template <typename E, int D, int GK, int G, typename A>
-__global__ __launch_bounds__(SV_NT, G == 1 ? SV_OCC1 : (sizeof(E) == 4 && D == 128 ? 1 : 2)) void solve_kernel(A a) {
+__global__ __launch_bounds__(SV_NT, (solve_waves<E, D, GK, G, A>())) void solve_kernel(A a) {
   if constexpr (is_packed<A>::value) {
     const int tiles = a.pk.heads * ((const ci32*)a.pk.header->count)[a.pk.size];
     const int wg = blockIdx.x, wgs = gridDim.x, b = wg & 7, back = (wgs / 8 - 1 - (wg >> 3)) * 8 + b;
@@ -1452,7 +1465,6 @@ hipError_t launch_solve_d(const TauArgs& a, hipStream_t s) {
 template <typename E, int D>
 hipError_t launch_solve_packed(Packed<TauArgs> a, hipStream_t s) {
   using A = Packed<TauArgs>;
-  static_assert(PACKED_SOLVERS == 256 * SV_OCC1, "workgroups of the one-group form that run at a time");
   auto kernel = solve_kernel<E, D, 0, 1, A>;
   if (a.gk == 1) kernel = solve_kernel<E, D, 1, 1, A>;
   if (a.gk == 2) kernel = solve_kernel<E, D, 2, 1, A>;
@@ -1461,7 +1473,8 @@ hipError_t launch_solve_packed(Packed<TauArgs> a, hipStream_t s) {
   a.pk.tiles = a.pk.lists[1];
   a.slots *= 2;  // (half a slot each)
   const int tiles = a.pk.heads * packed_tiles(a.pk.tokens, a.pk.seq_count, 1);
-  int wgs = tiles < PACKED_SOLVERS ? tiles : PACKED_SOLVERS;
+  const int most = packed_solvers(sizeof(E) == 4, D, a.gk);
+  int wgs = tiles < most ? tiles : most;
   if (a.cand && a.slots < wgs) wgs = a.slots;
   return launch_kernel(kernel, dim3((unsigned)wgs), dim3(SV_NT), s, a);
 }

@@ -1,5 +1,5 @@
 """Packed attention where its paths meet: the precision of dV by products,
-sequences that are left out, many sequences."""
+sequences that are left out, many sequences, more tiles than workgroups."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -86,3 +86,17 @@ def test_thousands_of_sequences(ea):
         for name, x, y in zip(("o", "dq", "dk"), got, want):
             check("%d %s" % (s, name), x[a:b], y, 4e-3)
         check("%d dv" % s, got[3][a:b], want[3], 1e-3, want[4] * HALF_STEP[BF])
+
+
+@pytest.mark.parametrize("alpha", [1.5, 1.7])
+def test_more_tiles_than_workgroups(ea, alpha):
+    """fp32 at d = 128, whose solver runs fewer workgroups at a time than there
+    are tiles here (640), against the batched path: both solve to 1e-6 and are
+    off by 2^-24 sqrt(d + n) |x| beside that."""
+    B, n, hq, hk, d = 2, 2048, 20, 5, 128
+    cu = [0, n, 2 * n]
+    q, k, v, _, cud = make(cu, B * n, hq, hk, d, F32, c=2.0, seed=27)
+    o, _ = ea.packed_forward(q, k, v, ea.packed_plan(cud, B * n, max_seqlen=n), alpha=alpha, need_bwd=False)
+    batched = lambda t, rep: t.view(B, n, -1, d).transpose(1, 2).repeat_interleave(rep, 1).contiguous()
+    want, _ = ea.forward(batched(q, 1), batched(k, 4), batched(v, 4), alpha=alpha, causal=True, need_bwd=False, tol=1e-6)
+    check("a%g" % alpha, o, want.transpose(1, 2).reshape(B * n, hq, d).double().cpu(), 1e-4)

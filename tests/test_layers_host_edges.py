@@ -7,6 +7,23 @@ torch = pytest.importorskip("torch")
 ea = pytest.importorskip("paper_2502_12082_amd", reason="HIP library not built")
 
 
+SLOT = 1179648  # bytes of one cache slot of the solver
+
+
+def test_solvers_that_run_at_a_time():
+    """The packed solver's workgroups are those that run at a time: three on each
+    of 256 compute units; fp32 at d = 128 two (68 KB of key tiles each), with a
+    general alpha one (428 registers).  They take half a cache slot each."""
+    z = ea.PackedSizes()
+    for d, dtype, alpha, groups in ((64, ea.EA_BF16, 1.5, 768), (128, ea.EA_BF16, 1.7, 768), (64, ea.EA_F32, 1.7, 768),
+                                    (128, ea.EA_F32, 1.5, 512), (128, ea.EA_F32, 1.25, 512), (128, ea.EA_F32, 2.0, 512),
+                                    (128, ea.EA_F32, 1.7, 256)):
+        params = ea.make_params(alpha, None, True, True, None, None, head_dim=64)
+        shape = ea.PackedShape(65536, 1, 65536, 8, 8, d, dtype)
+        assert ea._lib.entmax_packed_sizes(shape, ctypes.byref(params), ctypes.byref(z)) == ea.EA_OK
+        assert z.ws_fwd == groups // 2 * SLOT, (d, dtype, alpha)
+
+
 def test_sequences_of_a_plan():
     """plan_kernel's work grows with the square of the sequences: more than 2^16
     are refused before any launch."""
