@@ -430,7 +430,10 @@ ea_status entmax_packed_bwd(const ea_packed_shape* shape, const ea_params* param
  *   q, o   [requests, heads, d], row strides from request to request
  *   k, v   [requests, capacity, kv_heads, d]
  *   k_prefix, v_prefix  [prefix, kv_heads, d] (not read where prefix is 0)
- *   params alpha, scale, max_iter and tol are used
+ *   params alpha, scale, max_iter and tol are used; alpha > 2 converges slowly
+ *          at worst and wants a max_iter of 40 or more
+ * fp32 inputs with alpha > 2: scores near the edge of the support are taken in
+ * 64 bits, and tau is finished in 64 bits.
  * prefix + capacity <= 131072, requests * heads < 2^23; rows of k and k_prefix are at most 2^24 elements
  * apart.  workspace: entmax_prefix_decode_workspace
  * bytes, 16-byte aligned (about 4.4 bytes for every query head and key, most of

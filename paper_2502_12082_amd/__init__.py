@@ -1281,7 +1281,8 @@ def prefix_decode(q, k_cache, v_cache, lengths, k_prefix=None, v_prefix=None, al
     [requests, capacity, kv_heads, d].  bf16 or fp32, any strides with a
     contiguous last dimension.  A request without any key has O = 0.
 
-    tol: default 1e-6.  workspace: a device buffer of prefix_decode_workspace
+    tol: default 1e-6.  max_iter: 12 updates by default; alpha > 2 wants 40 or
+    more.  workspace: a device buffer of prefix_decode_workspace
     bytes, to keep from call to call (one call at a time)."""
     if not isinstance(q, torch.Tensor) or q.dim() != 3:
         raise ValueError("q must be a [requests, heads, head_dim] tensor")

@@ -1162,6 +1162,8 @@ ea_status entmax_prefix_decode(const ea_decode_shape* shape, const ea_params* pa
   a.tol = params->tol;
   a.max_iter = params->max_iter;
   a.gk = gamma_kind(params->alpha);
+  a.c64 = c64_of(params);
+  a.g64 = g64_of(params);
   return from_hip(launch_decode(a, shape->dtype, shape->head_dim, static_cast<hipStream_t>(stream)));
 }
 

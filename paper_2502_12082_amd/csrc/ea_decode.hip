@@ -29,6 +29,14 @@
 // compute the scores of whole blocks into memory and read them for every
 // evaluation, and gather V part by part.  Every list has an order that depends
 // on the scores alone, not on timing.
+//
+// fp32 inputs with alpha > 2: p = z^gamma, gamma < 1, has no bounded slope at z
+// = 0, where an fp32 score off by 1e-6 has p off by 1e-3 (alpha 3).  As in
+// attention (ea_common.h), scores within PRECISE_BAND max(1, |tau|) of the edge are
+// taken in fp64 there, and tau is finished in fp64; few keys are that near (keys
+// put at the edge, alpha 3, queries 20 times as large: O off by 7e-3 without and
+// under 5e-5 with; 8 requests, 32/8 heads, 32768 shared keys, alpha 2.5 84 and 94
+// us).  For 1 < alpha <= 2 the slope is at most gamma, and fp32 serves.
 #include "ea_common.h"
 #include "ea_internal.h"
 
@@ -578,11 +586,80 @@ __global__ __launch_bounds__(NT) void decode_solve_kernel(DecodeArgs a) {
     if (stop) break;
   }
 
+  // ---- fp32 inputs, alpha > 2: tau in fp64 (see the top of this file)
+  [[maybe_unused]] double t64 = tau;
+  [[maybe_unused]] const float band = PRECISE_BAND * fmaxf(1.f, fabsf(tau));
+  const bool precise = precise_path<E, GK>() && !convex;
+  // z of a kept score (-inf or NaN: none), -1 for one below the band
+  [[maybe_unused]] auto z64 = [&](float score, int key) -> double {
+    const float raw = fmaf(c, score, -tau);
+    if (!(raw > -band)) return -1.0;
+    if (raw >= band) return a.c64 * (double)score - t64;
+    const E* const k_row = key < p_blocks * DEC_KEYS ? pre_k + key * a.pk_row : own_k + (key - p_blocks * DEC_KEYS) * a.k_row;
+    const E* const q_row = static_cast<const E*>(a.q) + b * a.q_row + h * a.q_head;
+    return exact_x<D>(reinterpret_cast<const float*>(q_row), reinterpret_cast<const float*>(k_row), a.c64) - t64;
+  };
+  [[maybe_unused]] auto z_of = [&](float score, int key) { return (float)fmin(fmax(z64(score, key), 0.0), 1.0); };
+  if constexpr (precise_path<E, GK>()) {
+    if (precise) {
+      __shared__ double red64[2][2][SO_WAVES];
+      const float wider = 1e-5f * fmaxf(1.f, fmaxf(fabsf(low), fabsf(hi)));
+      double below = (double)low - wider, above = (double)hi + wider, f_last = INFINITY;
+      // Newton's steps inside a bracket, its middle where they leave it or do
+      // not halve |f| (f has a kink at every score); the ends meet after 40
+      for (int it = 0; it < 40; ++it) {
+        double s0 = 0.0, s1 = 0.0;
+        auto add64 = [&](double z) {
+          if (z > 0.0) {
+            const double u = pow(z, a.g64 - 1.0);
+            s0 = fma(u, z, s0);
+            s1 += u;
+          }
+        };
+        if (!wide) {
+          for (int y = t; y < total; y += SO_NT) add64(z64(kept[y], 4 * quad[y >> 2] + (y & 3)));
+        } else {
+          for (int y = t >> 3; y < nb; y += BPS) {
+            const f32x4 v = scores_of(y);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) add64(z64(v[e], chosen[y] * DEC_KEYS + 4 * (t & 7) + e));
+          }
+        }
+#pragma unroll
+        for (int x2 = 32; x2 >= 1; x2 >>= 1) {
+          s0 += __shfl_xor(s0, x2);
+          s1 += __shfl_xor(s1, x2);
+        }
+        auto& m64 = red64[it & 1];
+        if (lane == 0) {
+          m64[0][w] = s0;
+          m64[1][w] = s1;
+        }
+        __syncthreads();
+        s0 = s1 = 0.0;
+#pragma unroll
+        for (int x2 = 0; x2 < SO_WAVES; ++x2) {
+          s0 += m64[0][x2];
+          s1 += m64[1][x2];
+        }
+        const double f = s0 - 1.0;
+        if (fabs(f) <= 1e-9) break;
+        if (f < 0.0)
+          above = t64;
+        else
+          below = t64;
+        const double tn = t64 + f / (a.g64 * s1);
+        t64 = tn > below && tn < above && fabs(f) <= 0.5 * f_last ? tn : 0.5 * (below + above);
+        f_last = fabs(f);
+      }
+    }
+  }
+
   // ---- O: the rows of V with a probability
   float o[VPL] = {};
   const E* const own_v = static_cast<const E*>(a.v) + b * a.v_batch + kv * a.v_head;
   const E* const pre_v = static_cast<const E*>(a.pv) + kv * a.pv_head;
-  // Of n kept scores, those at 4 i of the keys from 4 first(i) on: those with a
+  // Of n kept scores (or, if precise, z), those at 4 i of the keys from 4 first(i) on: those with a
   // probability move to the front (a score is not overwritten before every
   // thread has read its own), p in place of the score, and their rows of V are
   // added up.
@@ -590,7 +667,8 @@ __global__ __launch_bounds__(NT) void decode_solve_kernel(DecodeArgs a) {
   auto gather = [&](int n, auto&& first) {
     int np = 0;
     for (int y0 = 0; y0 < n; y0 += NT) {
-      const float p = y0 + t < n ? Gamma<GK>::p_only(relu_z(c, kept[y0 + t], tau), gm) : 0.f;
+      const float z = y0 + t < n ? (precise ? kept[y0 + t] : relu_z(c, kept[y0 + t], tau)) : 0.f;
+      const float p = Gamma<GK>::p_only(z, gm);
       const int at = place(p > 0.f ? 1 : 0, np);
       if (p > 0.f) {
         kept[at] = p;
@@ -622,14 +700,23 @@ __global__ __launch_bounds__(NT) void decode_solve_kernel(DecodeArgs a) {
     }
   };
   if (!wide) {
+    if constexpr (precise_path<E, GK>())
+      if (precise)
+        for (int y = t; y < total; y += SO_NT) kept[y] = z_of(kept[y], 4 * quad[y >> 2] + (y & 3));
     gather(total, [&](int i) { return (int)quad[i]; });
   } else {
     constexpr int PART = SO_CAP / DEC_KEYS;  // blocks whose scores fit
     for (int x0 = 0; x0 < nb; x0 += PART) {
       const int x1 = min(x0 + PART, nb);
       __syncthreads();
-      for (int x = x0 + (t >> 3); x < x1; x += BPS)
-        *reinterpret_cast<f32x4*>(kept + (x - x0) * DEC_KEYS + 4 * (t & 7)) = scores_of(x);
+      for (int x = x0 + (t >> 3); x < x1; x += BPS) {
+        f32x4 v = scores_of(x);
+        if constexpr (precise_path<E, GK>())
+          if (precise)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = z_of(v[e], chosen[x] * DEC_KEYS + 4 * (t & 7) + e);
+        *reinterpret_cast<f32x4*>(kept + (x - x0) * DEC_KEYS + 4 * (t & 7)) = v;
+      }
       __syncthreads();
       gather((x1 - x0) * DEC_KEYS, [&](int i) { return chosen[x0 + i / (DEC_KEYS / 4)] * (DEC_KEYS / 4) + i % (DEC_KEYS / 4); });
     }

@@ -209,6 +209,7 @@ struct DecodeArgs {
   float *pm, *om, *spill;
   float c, alpha, gamma, tol;
   int max_iter, gk;
+  double c64, g64;  // c and gamma (fp32 inputs, alpha > 2)
 };
 
 struct TauArgs {
