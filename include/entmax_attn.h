@@ -434,7 +434,9 @@ ea_status entmax_packed_bwd(const ea_packed_shape* shape, const ea_params* param
  *          at worst and wants a max_iter of 40 or more
  * fp32 inputs with alpha > 2: scores near the edge of the support are taken in
  * 64 bits, and tau is finished in 64 bits.
- * prefix + capacity <= 131072, requests * heads < 2^23; rows of k and k_prefix are at most 2^24 elements
+ * prefix + capacity <= 131072, requests * heads < 2^23, and kv_heads times the
+ * runs of 128 keys of every request's cache (and those of the prefix, once for
+ * 32 rows at most) < 2^26; rows of k and k_prefix are at most 2^24 elements
  * apart.  workspace: entmax_prefix_decode_workspace
  * bytes, 16-byte aligned (about 4.4 bytes for every query head and key, most of
  * them for rows with thousands of probabilities).  Two launches.

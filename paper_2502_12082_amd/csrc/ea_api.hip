@@ -1062,13 +1062,31 @@ ea_status entmax_packed_bwd(const ea_packed_shape* shape, const ea_params* param
 
 namespace {
 
+// The sizes of a call.
+DecodeArgs decode_sizes(const ea_decode_shape* s) {
+  DecodeArgs a{};
+  a.requests = s->requests;
+  a.heads = s->heads;
+  a.kv_heads = s->kv_heads;
+  a.group = s->heads / s->kv_heads;
+  a.prefix = s->prefix;
+  a.capacity = s->capacity;
+  static_assert(DEC_RUN == 4, "a run's maxima are 16 bytes");
+  constexpr int RUN_KEYS = DEC_KEYS * DEC_RUN;
+  a.prefix_runs = (s->prefix + RUN_KEYS - 1) / RUN_KEYS;
+  a.own_runs = (s->capacity + RUN_KEYS - 1) / RUN_KEYS;
+  return a;
+}
+
 ea_status check_decode(const ea_decode_shape* s) {
   if (!s) return EA_ERR_INVALID_ARG;
   if (s->requests < 0 || s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads != 0) return EA_ERR_INVALID_ARG;
   if (s->prefix < 0 || s->capacity < 0) return EA_ERR_INVALID_ARG;
   if (!dtype_ok(s->dtype) || (s->head_dim != 64 && s->head_dim != 128)) return EA_ERR_UNSUPPORTED;
   if ((int64_t)s->prefix + s->capacity > MAX_SEQLEN) return EA_ERR_UNSUPPORTED;
-  if ((int64_t)s->requests * s->heads >= (1 << 23)) return EA_ERR_UNSUPPORTED;  // (256 threads a row, fewer than 2^32)
+  // a launch has fewer than 2^32 threads: 256 to a row, 64 to a workgroup over keys
+  if ((int64_t)s->requests * s->heads >= (1 << 23)) return EA_ERR_UNSUPPORTED;
+  if (decode_maxima_wgs(decode_sizes(s), s->dtype) >= (1 << 26)) return EA_ERR_UNSUPPORTED;
   return EA_OK;
 }
 
@@ -1121,7 +1139,7 @@ ea_status entmax_prefix_decode(const ea_decode_shape* shape, const ea_params* pa
   if (shape->prefix && (!tensor_ok(k_prefix) || !tensor_ok(v_prefix) || !strides_ok(&st->k_prefix, es) ||
                         !strides_ok(&st->v_prefix, es)))
     return EA_ERR_INVALID_ARG;
-  DecodeArgs a{};
+  DecodeArgs a = decode_sizes(shape);
   const size_t need = decode_parts(shape, workspace, &a);
   if (need && !tensor_ok(workspace)) return EA_ERR_INVALID_ARG;
   if (ws_bytes < need) return EA_ERR_WORKSPACE;
@@ -1146,16 +1164,6 @@ ea_status entmax_prefix_decode(const ea_decode_shape* shape, const ea_params* pa
   a.pv_row = st->v_prefix.row;
   a.pv_head = st->v_prefix.head;
   a.lengths = lengths;
-  a.requests = shape->requests;
-  a.heads = shape->heads;
-  a.kv_heads = shape->kv_heads;
-  a.group = shape->heads / shape->kv_heads;
-  a.prefix = shape->prefix;
-  a.capacity = shape->capacity;
-  static_assert(DEC_RUN == 4, "a run's maxima are 16 bytes");
-  constexpr int RUN_KEYS = DEC_KEYS * DEC_RUN;
-  a.prefix_runs = (shape->prefix + RUN_KEYS - 1) / RUN_KEYS;
-  a.own_runs = (shape->capacity + RUN_KEYS - 1) / RUN_KEYS;
   a.c = (params->alpha - 1.0f) * params->scale;
   a.alpha = params->alpha;
   a.gamma = 1.0f / (params->alpha - 1.0f);

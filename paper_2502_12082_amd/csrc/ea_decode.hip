@@ -733,25 +733,38 @@ __global__ __launch_bounds__(NT) void decode_solve_kernel(DecodeArgs a) {
   }
 }
 
-template <typename E, int D, int RT>
-hipError_t launch_maxima(const DecodeArgs& a, hipStream_t s) {
-  const int row_tiles = (a.requests * a.group + 32 * RT - 1) / (32 * RT);
+// Rows of 32 that a wave of the prefix holds.  (64 rows to a wave, with registers
+// for two waves more than with 128: 49 us against 45 for 640 rows, 16 requests of
+// 40/1 heads behind 65536 keys.)
+int row_tile(bool f32, int rows) { return !f32 && rows > 32 ? 2 : 1; }
+
+struct MaximaGrid {
+  int row_tiles, per_wave;
+  int64_t prefix_wgs, wgs;
+};
+MaximaGrid maxima_grid(const DecodeArgs& a, bool f32) {
+  const int rows = a.requests * a.group, tile = 32 * row_tile(f32, rows);
+  MaximaGrid g;
+  g.row_tiles = (int)(((int64_t)rows + tile - 1) / tile);
   // runs of a wave: as few as give every wave of the device work (eight waves
   // to each of 256 compute units), so that queries are loaded seldom
-  int64_t waves = (int64_t)a.kv_heads * row_tiles * a.prefix_runs;
-  int per_wave = (int)(waves / 2048);
-  per_wave = per_wave < 1 ? 1 : per_wave > 8 ? 8 : per_wave;
-  const int chunks = (a.prefix_runs + per_wave - 1) / per_wave;
-  const int64_t prefix_wgs = a.prefix ? (int64_t)a.kv_heads * row_tiles * chunks : 0;
-  const int64_t own = (int64_t)a.requests * a.kv_heads * ((a.group + 31) / 32) * a.own_runs;
-  const int64_t wgs = prefix_wgs + own;
-  if (wgs == 0) return hipSuccess;
-  if (wgs > INT32_MAX) return hipErrorInvalidConfiguration;
+  const int64_t each = (int64_t)a.kv_heads * g.row_tiles * a.prefix_runs / 2048;
+  g.per_wave = each < 1 ? 1 : each > 8 ? 8 : (int)each;
+  const int chunks = (a.prefix_runs + g.per_wave - 1) / g.per_wave;
+  g.prefix_wgs = (int64_t)a.kv_heads * g.row_tiles * chunks;
+  g.wgs = g.prefix_wgs + (int64_t)a.requests * a.kv_heads * ((a.group + 31) / 32) * a.own_runs;
+  return g;
+}
+
+template <typename E, int D, int RT>
+hipError_t launch_maxima(const DecodeArgs& a, hipStream_t s) {
+  MaximaGrid g = maxima_grid(a, sizeof(E) == 4);
+  if (g.wgs == 0) return hipSuccess;
   DecodeArgs args = a;
-  int rt = row_tiles, pw = per_wave, pg = (int)prefix_wgs;
-  void* params[] = {&args, &rt, &pw, &pg};
-  return hipLaunchKernel(reinterpret_cast<const void*>(decode_maxima_kernel<E, D, RT>), dim3((unsigned)wgs), dim3(SC_NT),
-                         params, 0, s);
+  int pg = (int)g.prefix_wgs;
+  void* params[] = {&args, &g.row_tiles, &g.per_wave, &pg};
+  return hipLaunchKernel(reinterpret_cast<const void*>(decode_maxima_kernel<E, D, RT>), dim3((unsigned)g.wgs),
+                         dim3(SC_NT), params, 0, s);
 }
 
 template <typename E, int D, int NT>
@@ -765,11 +778,8 @@ hipError_t launch_solve(const DecodeArgs& a, hipStream_t s) {
 
 template <typename E, int D>
 hipError_t launch_decode_d(const DecodeArgs& a, hipStream_t s) {
-  const int rows = a.requests * a.group;
   hipError_t e;
-  // (64 rows to a wave, with registers for two waves more than with 128: 49 us
-  // against 45 for 640 rows, 16 requests of 40/1 heads behind 65536 keys.)
-  if (sizeof(E) == 2 && rows > 32)
+  if (row_tile(sizeof(E) == 4, a.requests * a.group) == 2)
     e = launch_maxima<E, D, sizeof(E) == 2 ? 2 : 1>(a, s);
   else
     e = launch_maxima<E, D, 1>(a, s);
@@ -782,6 +792,8 @@ hipError_t launch_decode_d(const DecodeArgs& a, hipStream_t s) {
 }
 
 }  // namespace
+
+int64_t decode_maxima_wgs(const DecodeArgs& a, int dtype) { return maxima_grid(a, dtype != 0).wgs; }
 
 hipError_t launch_decode(const DecodeArgs& a, int dtype, int head_dim, hipStream_t s) {
   if (dtype == 0) return head_dim == 64 ? launch_decode_d<__bf16, 64>(a, s) : launch_decode_d<__bf16, 128>(a, s);

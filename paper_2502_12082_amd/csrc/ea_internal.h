@@ -384,6 +384,8 @@ hipError_t launch_bwd_dkdv_packed(const Packed<BwdArgs>& a, int dtype, int head_
 hipError_t launch_bwd_dq_packed(const Packed<BwdArgs>& a, int dtype, int head_dim, hipStream_t s);
 // Workgroups that share the query heads of a key head in launch_bwd_dkdv_packed.
 int dkdv_packed_parts(int tokens, int seqs, int heads, int kv_heads, int dtype, int head_dim);
+// Workgroups of decoding's first kernel, 64 threads each (from the sizes of `a`).
+int64_t decode_maxima_wgs(const DecodeArgs& a, int dtype);
 hipError_t launch_decode(const DecodeArgs& a, int dtype, int head_dim, hipStream_t s);
 int rotary_partials(int tokens);
 hipError_t launch_rotary_fwd(const RotaryArgs& a, int dtype, hipStream_t s);

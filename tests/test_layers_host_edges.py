@@ -34,3 +34,18 @@ def test_sequences_of_a_plan():
     size = lambda seqs: ea._lib.entmax_packed_sizes(ea.PackedShape(1000, seqs, 100, 1, 1, 64, ea.EA_BF16),
                                                     ctypes.byref(params), ctypes.byref(z))
     assert size(1 << 16) == ea.EA_OK and size((1 << 16) + 1) == ea.EA_ERR_UNSUPPORTED
+
+
+def test_decoding_grid_of_one_launch():
+    """Workgroups over keys that one launch cannot hold (2^26 of 64 threads) are
+    refused by the sizes: 8 x 1024 for every request's own cache, and those of
+    the prefix with them."""
+    n = ctypes.c_size_t()
+    size = lambda *s: ea._lib.entmax_prefix_decode_workspace(ea.DecodeShape(*s), ctypes.byref(n))
+    assert size(8191, 8, 8, 64, ea.EA_BF16, 0, 131072) == ea.EA_OK
+    assert size(8192, 8, 8, 64, ea.EA_BF16, 0, 131072) == ea.EA_ERR_UNSUPPORTED
+    # 8199 x 8 x 1023 = 2^26 - 8248; 257 tiles of 32 rows, 8 key heads, one run: 2056 more; in 64 rows 1032
+    assert size(8199, 8, 8, 64, ea.EA_F32, 128, 130944) == ea.EA_OK
+    # 8200 x 8 x 1023 = 2^26 - 64
+    assert size(8200, 8, 8, 64, ea.EA_F32, 0, 130944) == ea.EA_OK
+    assert size(8200, 8, 8, 64, ea.EA_F32, 128, 130944) == ea.EA_ERR_UNSUPPORTED
