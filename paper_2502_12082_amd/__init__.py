@@ -1323,10 +1323,11 @@ def prefix_decode(q, k_cache, v_cache, lengths, k_prefix=None, v_prefix=None, al
             out = q.new_empty(q.shape)
         if workspace is None:
             workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=dev)
-        kp, vp = (q, q) if P == 0 else (k_prefix, v_prefix)  # (without a prefix, not read)
         strides = _decode_strides_of(
             _stride(q, 0), _stride(q, 1), _stride(out, 0), _stride(out, 1), _stride(k_cache, 1), _stride(k_cache, 2),
-            _stride(v_cache, 1), _stride(v_cache, 2), _stride(kp, 0), _stride(kp, 1), _stride(vp, 0), _stride(vp, 1),
+            _stride(v_cache, 1), _stride(v_cache, 2),
+            *((0, 0, 0, 0) if P == 0 else (_stride(k_prefix, 0), _stride(k_prefix, 1), _stride(v_prefix, 0),
+                                           _stride(v_prefix, 1))),
             _stride(k_cache, 0), _stride(v_cache, 0))
         _check(_lib.entmax_prefix_decode(
             shape, params, strides, q.data_ptr(), k_cache.data_ptr(),

@@ -1,4 +1,5 @@
-"""prefix_decode: fp32 keys at the edge of the support."""
+"""prefix_decode: fp32 keys at the edge of the support, strides of a prefix that is
+not there."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -6,7 +7,7 @@ from layer_util import check, decode64  # noqa: E402
 from test_gpu_decode import compare, ea, make, run  # noqa: E402,F401
 
 pytestmark = pytest.mark.gpu
-F32 = torch.float32
+BF, F32 = torch.bfloat16, torch.float32
 
 
 @pytest.mark.parametrize("alpha", [1.25, 1.7, 2.5, 3.0])
@@ -62,3 +63,13 @@ def test_fp32_keys_at_the_edge_of_many_rows(ea):
     edge_keys(x, 3.0, 0.125)
     want = decode64(x["q"], x["k"], x["v"], lengths, None, None, 3.0, 0.125)
     check("many", run(ea, x, 3.0, max_iter=64), want, 5e-5)
+
+
+def test_no_prefix_takes_no_strides(ea):
+    """Without a prefix a query's strides stand for nothing but the query's."""
+    x = make([9, 5], 0, 9, 2, 1, 64, BF, seed=36)
+    want = run(ea, x)
+    far = torch.empty(2, (1 << 24) + 64, dtype=BF, device="cuda")
+    q = far[:, :128].view(2, 2, 64)
+    q.copy_(x["q"])
+    assert torch.equal(run(ea, dict(x, q=q)), want)
