@@ -348,7 +348,8 @@ ea_status entmax_norm_rotary(const ea_rotary* r, const void* q, const ea_strides
  * dq, dk (of `dtype`, [tokens, heads, d] contiguous) with respect to q and k,
  * and dq_weight, dk_weight (fp32 [d], or NULL).  dq and dk may be dq_out and
  * dk_out where those are contiguous.  workspace: entmax_norm_rotary_workspace
- * bytes, 16-byte aligned.  Sums are taken in a fixed order.  Two launches.
+ * bytes, 16-byte aligned.  Sums are taken in a fixed order, and are 0 without
+ * tokens.  Two launches.
  */
 ea_status entmax_norm_rotary_workspace(const ea_rotary* r, size_t* bytes);
 ea_status entmax_norm_rotary_bwd(const ea_rotary* r, const void* dq_out, const ea_strides* dq_out_strides,

@@ -1022,8 +1022,7 @@ def norm_rotary_backward(dq_out, dk_out, q, k, positions, freqs, q_weight=None, 
     _on_gpu(q.device)
     with _on_device(q.device):
         dq, dk = q.new_empty(q.shape), k.new_empty(k.shape)
-        make = torch.empty if q.shape[0] else torch.zeros
-        dwq, dwk = (None if w is None else make(q.shape[-1], dtype=torch.float32, device=q.device)
+        dwq, dwk = (None if w is None else torch.empty(q.shape[-1], dtype=torch.float32, device=q.device)
                     for w in (q_weight, k_weight))
         n = ctypes.c_size_t()
         _check(_lib.entmax_norm_rotary_workspace(r, ctypes.byref(n)), "entmax_norm_rotary_workspace")

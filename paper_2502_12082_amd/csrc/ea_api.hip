@@ -716,14 +716,21 @@ ea_status entmax_norm_rotary_bwd(const ea_rotary* r, const void* dq_out, const e
                                  float* dq_weight, float* dk_weight, void* workspace, size_t ws_bytes,
                                  void* stream) {
   ea_status st = check_rotary(r);
-  if (st != EA_OK || r->tokens == 0) return st;
-  RotaryArgs a;
+  if (st != EA_OK) return st;
+  if (!aligned(dq_weight, 4) || !aligned(dk_weight, 4)) return EA_ERR_INVALID_ARG;
+  RotaryArgs a{};
+  if (r->tokens == 0) {  // (the sums of no terms)
+    a.d = r->head_dim;
+    a.dq_weight = dq_weight;
+    a.dk_weight = dk_weight;
+    return from_hip(launch_rotary_bwd(a, r->dtype, static_cast<hipStream_t>(stream)));
+  }
   st = prep_rotary(r, q, q_strides, k, k_strides, positions, position_stride, freqs, q_weight, k_weight, &a);
   if (st != EA_OK) return st;
   const size_t es = size_of(r->dtype);
   if (!tensor_ok(dq_out) || !tensor_ok(dk_out) || !strides_ok(dq_out_strides, es) || !strides_ok(dk_out_strides, es))
     return EA_ERR_INVALID_ARG;
-  if (!tensor_ok(dq) || !tensor_ok(dk) || !aligned(dq_weight, 4) || !aligned(dk_weight, 4)) return EA_ERR_INVALID_ARG;
+  if (!tensor_ok(dq) || !tensor_ok(dk)) return EA_ERR_INVALID_ARG;
   if (!tensor_ok(workspace)) return EA_ERR_INVALID_ARG;
   if (ws_bytes < rotary_ws(r)) return EA_ERR_WORKSPACE;
   const int64_t d = r->head_dim;

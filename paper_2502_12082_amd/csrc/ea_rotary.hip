@@ -359,8 +359,11 @@ hipError_t launch_fwd_d(RotaryArgs a, hipStream_t s) {
 
 template <typename E, int D>
 hipError_t launch_bwd_d(const RotaryArgs& a, hipStream_t s) {
-  const hipError_t e = launch_kernel(rotary_bwd_kernel<E, D>, dim3((unsigned)a.partial_count), dim3(ROT_NT), s, a);
-  if (e != hipSuccess || !(a.dq_weight || a.dk_weight)) return e;
+  if (a.partial_count > 0) {
+    const hipError_t e = launch_kernel(rotary_bwd_kernel<E, D>, dim3((unsigned)a.partial_count), dim3(ROT_NT), s, a);
+    if (e != hipSuccess) return e;
+  }
+  if (!(a.dq_weight || a.dk_weight)) return hipSuccess;
   return launch_kernel(rotary_dw_kernel, dim3(2 * D / 16), dim3(DW_NT), s, a);
 }
 
