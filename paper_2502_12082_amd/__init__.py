@@ -859,7 +859,8 @@ def _stride(t, dim):
 
 # Argument structures are built once for each set of sizes that a program uses:
 # a call at the sizes of a decoding step is a few microseconds of host time,
-# and each structure one or two.  They are never written to afterwards.
+# and each structure one or two.  They are never written to afterwards, and
+# no object that a caller gets holds one.
 @functools.lru_cache(maxsize=1024)
 def _strides_of(row, head):
     return Strides(row, head)
@@ -1096,7 +1097,9 @@ class PackedResiduals:
 
     def __init__(self, shape: PackedShape, params: Params, plan: PackedPlan, sizes: PackedSizes, device,
                  lists: bool = True):
-        self.shape, self.params, self.plan, self.sizes = shape, params, plan, sizes
+        # (copies: the calls' structures are kept for later calls, see above)
+        self.shape, self.params, self.sizes = (type(x).from_buffer_copy(x) for x in (shape, params, sizes))
+        self.plan = plan
         self.buffer = torch.empty(sizes.residuals, dtype=torch.uint8, device=device)
         # (as for Residuals, short sequences are not listed; fp32 products take longer)
         least = PACKED_LISTS_FROM if params.need_bwd else LISTS_FROM

@@ -49,3 +49,22 @@ def test_decoding_grid_of_one_launch():
     # 8200 x 8 x 1023 = 2^26 - 64
     assert size(8200, 8, 8, 64, ea.EA_F32, 0, 130944) == ea.EA_OK
     assert size(8200, 8, 8, 64, ea.EA_F32, 128, 130944) == ea.EA_ERR_UNSUPPORTED
+
+
+def test_residuals_own_their_structures():
+    """What one call's residuals hold is no other call's: the structures that the
+    binding keeps for a set of sizes are not handed out."""
+    plan = ea.PackedPlan(torch.zeros(4096, dtype=torch.uint8), 10, 2, 10, True)
+    t = [torch.zeros(10, h, 64, dtype=torch.bfloat16) for h in (4, 2, 2)]
+    key = (1.5, None, None, None, True, True, 64, 10, 2, 10, 4, 2, 64, ea.EA_BF16)
+
+    def make():
+        params, sizes = ea._packed_params(*key)
+        return ea.PackedResiduals(ea._packed_shape(*t, plan), params, plan, sizes, "cpu")
+
+    first = make()
+    scale, nbytes = first.params.scale, first.sizes.ws_bwd
+    first.params.scale, first.sizes.ws_bwd, first.shape.tokens = 7.0, 1, 3
+    second = make()
+    assert second.params.scale == scale and second.sizes.ws_bwd == nbytes and second.shape.tokens == 10
+    assert ea._packed_shape(*t, plan).tokens == 10
