@@ -20,8 +20,10 @@
  *
  * Errors: arguments are checked before anything is launched; on failure
  * nothing is written and a non-zero ea_status is returned.  NaN/Inf inside
- * the tensors is not checked and propagates.  No C++ exception crosses this
- * interface.  All functions are reentrant.
+ * the tensors is not checked: in v and dout it propagates to what uses it, a
+ * score that is NaN has probability 0, and a query whose largest score is not
+ * finite (NaN or infinite itself, or against such a key) has o = 0, as if it had
+ * no keys.  No C++ exception crosses this interface.  All functions are reentrant.
  */
 #ifndef ENTMAX_ATTN_H
 #define ENTMAX_ATTN_H
@@ -431,7 +433,7 @@ ea_status entmax_packed_bwd(const ea_packed_shape* shape, const ea_params* param
  *   q, o   [requests, heads, d], row strides from request to request
  *   k, v   [requests, capacity, kv_heads, d]
  *   k_prefix, v_prefix  [prefix, kv_heads, d] (not read where prefix is 0)
- *   params alpha, scale, max_iter and tol are used; alpha > 2 converges slowly
+ *   params alpha, scale, max_iter and tol are used (causal and need_bwd are not); alpha > 2 converges slowly
  *          at worst and wants a max_iter of 40 or more
  * fp32 inputs with alpha > 2: scores near the edge of the support are taken in
  * 64 bits, and tau is finished in 64 bits.

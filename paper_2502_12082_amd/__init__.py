@@ -1168,7 +1168,7 @@ def packed_forward(q, k, v, plan: PackedPlan, alpha=1.5, scale=None, need_bwd=Tr
     Rows of no sequence (before cu_seqlens[0], behind the last) are 0 in an O
     that the call makes and left as they are in `out`.  need_bwd=False gives
     residuals that packed_backward does not take.  tol: default 1e-5, for fp32
-    1e-6.  workspace: as for forward (sizes.ws_fwd bytes of the residuals).
+    1e-6.  max_iter: 12 updates by default; alpha > 2 wants 40 or more.  workspace: as for forward (sizes.ws_fwd bytes of the residuals).
     lists: whether the residuals hold element lists (see Residuals)."""
     shape = _packed_shape(q, k, v, plan)
     if tol is None and shape.dtype == EA_F32:
@@ -1281,7 +1281,8 @@ def prefix_decode(q, k_cache, v_cache, lengths, k_prefix=None, v_prefix=None, al
     prefix), which all requests share, and to the first lengths[b] keys (int32
     on the device, taken as 0 .. capacity) of its own k_cache, v_cache
     [requests, capacity, kv_heads, d].  bf16 or fp32, any strides with a
-    contiguous last dimension.  A request without any key has O = 0.
+    contiguous last dimension.  A request without any key has O = 0, and so has
+    a query whose largest score is not finite.
 
     tol: default 1e-6.  max_iter: 12 updates by default; alpha > 2 wants 40 or
     more.  workspace: a device buffer of prefix_decode_workspace

@@ -1,10 +1,10 @@
 """prefix_decode: fp32 keys at the edge of the support, strides of a prefix that is
-not there."""
+not there, waves of several runs, scores that are not finite."""
 import pytest
 
 torch = pytest.importorskip("torch")
 from layer_util import check, decode64  # noqa: E402
-from test_gpu_decode import compare, ea, make, run  # noqa: E402,F401
+from test_gpu_decode import ATOL, compare, ea, make, run  # noqa: E402,F401
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
@@ -73,3 +73,33 @@ def test_no_prefix_takes_no_strides(ea):
     q = far[:, :128].view(2, 2, 64)
     q.copy_(x["q"])
     assert torch.equal(run(ea, dict(x, q=q)), want)
+
+
+@pytest.mark.parametrize("prefix,requests,d,dtype", [(33001, 20, 64, BF), (100001, 20, 64, BF), (33001, 12, 128, F32)])
+def test_several_runs_to_a_wave(ea, prefix, requests, d, dtype):
+    """Prefixes whose waves take 2 (33001) and 6 runs, the last ones fewer, of
+    two row tiles; some rows of the first, middle and last request and key head."""
+    x = make([b % 5 for b in range(requests)], prefix, 5, 32, 8, d, dtype, seed=35)
+    got = run(ea, x)
+    for b, h in ((0, 0), (0, 31), (requests // 2, 13), (requests - 1, 5), (requests - 1, 31)):
+        one = lambda t, dim: t.narrow(dim, h // 4, 1)
+        want = decode64(x["q"][b:b + 1, h:h + 1], one(x["k"], 2)[b:b + 1], one(x["v"], 2)[b:b + 1],
+                        x["lengths"][b:b + 1].tolist(), one(x["pk"], 1), one(x["pv"], 1), 1.5, d ** -0.5)
+        check("%d %d" % (b, h), got[b:b + 1, h:h + 1], want, ATOL[dtype])
+
+
+@pytest.mark.parametrize("prefix,own", [(0, 30), (200, 700), (5000, 10)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("dtype,alpha", [(BF, 1.5), (BF, 2.5), (F32, 3.0)])
+def test_scores_that_are_not_finite(ea, prefix, own, bad, dtype, alpha):
+    """A query that is not finite, in one element (scores of +-inf, or NaN) or in
+    all (NaN): its row of O is 0, as in attention, and the others are unchanged."""
+    x = make([own, own - 3], prefix, own, 4, 2, 64, dtype, seed=37)
+    want = run(ea, x, alpha, max_iter=40)
+    x["q"] = x["q"].clone()
+    x["q"][1, 2] = bad
+    x["q"][0, 1, 5] = bad
+    got = run(ea, x, alpha, max_iter=40)
+    assert not got[1, 2].any() and not got[0, 1].any()
+    got[1, 2], got[0, 1] = want[1, 2], want[0, 1]
+    assert torch.equal(got, want)

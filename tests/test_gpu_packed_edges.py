@@ -1,5 +1,6 @@
 """Packed attention where its paths meet: the precision of dV by products,
-sequences that are left out, many sequences, more tiles than workgroups."""
+sequences that are left out, many sequences, more tiles than workgroups,
+dense query blocks among listed ones, scores that are not finite."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -100,3 +101,45 @@ def test_more_tiles_than_workgroups(ea, alpha):
     batched = lambda t, rep: t.view(B, n, -1, d).transpose(1, 2).repeat_interleave(rep, 1).contiguous()
     want, _ = ea.forward(batched(q, 1), batched(k, 4), batched(v, 4), alpha=alpha, causal=True, need_bwd=False, tol=1e-6)
     check("a%g" % alpha, o, want.transpose(1, 2).reshape(B * n, hq, d).double().cpu(), 1e-4)
+
+
+def test_dense_blocks_among_listed(ea):
+    """A key head that visits more than 64 query blocks, a few of them (under an
+    eighth) not listed, against the same without lists."""
+    n, d, hq, hk = 5000, 128, 4, 2
+    q, k, v, do, cud = make([0, n], n, hq, hk, d, BF, c=4.0, seed=23)
+    for h, blocks in ((0, (3, 40, 66, 70)), (1, ()), (2, (65,)), (3, (10, 77))):
+        for b in blocks:
+            q[64 * b:64 * b + 64, h] *= 0.02
+    plan = ea.packed_plan(cud, n)
+    o, res = ea.packed_forward(q, k, v, plan, alpha=1.5)
+    blocks = n // 64 + 1
+    use = res.lists[-4 * hq * blocks:].view(torch.int32).view(hq, blocks)[:, :(n + 63) // 64]
+    missing = ((use & 4) == 0).sum(1)
+    print("blocks not listed for dK and dV, of %d: %s" % (use.shape[1], missing.tolist()), flush=True)
+    assert (8 * missing <= use.shape[1]).all() and missing[0] >= 4 and missing[2] >= 1
+    got = (o,) + ea.packed_backward(q, k, v, do, res)
+    o, res = ea.packed_forward(q, k, v, plan, alpha=1.5, lists=False)
+    want = (o,) + ea.packed_backward(q, k, v, do, res)
+    for name, x, y in zip(("o", "dq", "dk", "dv"), got, want):
+        # (half a step each, and gradients of scores four times as large: see test_gpu_packed)
+        y = y.double().cpu()
+        check(name, x, y, 1e-3 * 16, 2.0 ** -8 * y.abs())
+
+
+@pytest.mark.parametrize("d,dtype", [(64, BF), (128, BF), (64, F32)])
+@pytest.mark.parametrize("n", [60, 700, 1300])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_scores_that_are_not_finite(ea, n, bad, d, dtype):
+    """A query that is not finite, in one element (scores of +-inf, or NaN) or in
+    all (NaN): its row of O is 0, the others are unchanged."""
+    q, k, v, _, cud = make([0, n], n, 2, 1, d, dtype, seed=24)
+    plan = ea.packed_plan(cud, n)
+    want = ea.packed_forward(q, k, v, plan, alpha=1.5, need_bwd=False)[0]
+    q = q.clone()
+    q[n // 2, 1] = bad
+    q[n // 3, 0, 5] = bad
+    got = ea.packed_forward(q, k, v, plan, alpha=1.5, need_bwd=False)[0]
+    assert not got[n // 2, 1].any() and not got[n // 3, 0].any()
+    got[n // 2, 1], got[n // 3, 0] = want[n // 2, 1], want[n // 3, 0]
+    check("n%d %s" % (n, bad), got, want.double().cpu(), 1e-4, 2.0 ** -8 * want.double().cpu().abs())
