@@ -322,7 +322,8 @@ typedef struct {
  * y_2i+1)); the values behind rot_dim are y.  phi = position * freqs[i], the
  * position being that of axis a for the sections[a] pairs that follow those of
  * the axes before it (one axis: the token's position; three: time, height and
- * width).  Angles are exact for every int32 position (reduced in fp64).
+ * width).  Positions are any int32; an angle is off by 2^-51 of itself and
+ * 2^-25 radians at most (reduced in fp64: 1e-6 radians at 2^31 times 1).
  *   q, k       [tokens, heads, d] and [tokens, kv_heads, d] of `dtype`, any
  *              strides (for instance parts of a fused projection's rows)
  *   q_out, k_out  (written); may be q and k themselves, and otherwise must not

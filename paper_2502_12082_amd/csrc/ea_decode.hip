@@ -68,11 +68,11 @@ struct KeyRing {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) off[i] = TL::src_off(64 * i + lane_id(), ld) * (uint32_t)sizeof(E);
   }
-  // Copies block kb of `keys` rows to place x (rows past the end repeat the last
-  // one; their scores become -inf).
+  // Copies block kb of `keys` rows to place x (rows past the end become 0; their
+  // scores are set to -inf).
   __device__ __forceinline__ void copy(const E* K, int keys, int kb, int x) const {
 #if defined(__HIP_DEVICE_COMPILE__)
-    // (a buffer of the rows that there are: the others read as 0)
+    // (a buffer of the rows that there are)
     kb = __builtin_amdgcn_readfirstlane(kb);
     const int rows = __builtin_amdgcn_readfirstlane(min(keys - kb * DEC_KEYS, DEC_KEYS));
     const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<E*>(K + (int64_t)kb * DEC_KEYS * ld), (short)0,

@@ -200,7 +200,7 @@ struct DecodeArgs {
   const int32_t* lengths;  // [requests], clamped to 0 .. capacity
   int requests, heads, kv_heads, group, prefix, capacity;
   int prefix_runs, own_runs;  // per key head, and per request and key head
-  // workspace: of every row's quads of four keys a byte each (see maxima_run)
+  // workspace: of every row's quads of four keys a byte each (see maxima_runs)
   // [kv_heads, prefix_runs, requests * group, 32] and [requests, kv_heads,
   // own_runs, group, 32], the maxima of its blocks [kv_heads, requests * group,
   // prefix_runs * DEC_RUN] and [requests, kv_heads, group, own_runs * DEC_RUN],
@@ -371,7 +371,7 @@ hipError_t launch_bwd_dkdv_lists(const BwdArgs& a, int dtype, int head_dim, hipS
 // (a sample of the density, then the lists of heads that look sparse)
 hipError_t launch_collect(const CollectArgs& a, int dtype, int head_dim, hipStream_t s);
 hipError_t launch_bwd_dq(const BwdArgs& a, int dtype, int head_dim, hipStream_t s);
-// The packed forms (no lists; T and n of the arguments are not used).
+// The packed forms (T and n of the arguments are not used).
 hipError_t launch_plan(const PlanArgs& a, hipStream_t s);
 hipError_t launch_tau_packed(const Packed<TauArgs>& a, int dtype, int head_dim, hipStream_t s);
 hipError_t launch_tau_packed_bf16_64(const Packed<TauArgs>& a, hipStream_t s);
