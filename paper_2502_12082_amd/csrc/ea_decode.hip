@@ -785,8 +785,13 @@ hipError_t launch_decode_d(const DecodeArgs& a, hipStream_t s) {
     e = launch_maxima<E, D, 1>(a, s);
   if (e != hipSuccess) return e;
   // Rows for two waves on every compute unit have one each, few or long ones
-  // four: 2048 rows of 260 to 288 blocks 25 us against 35, 1024 rows of 2050
-  // blocks 33 against 23.
+  // four.  A call in a graph, us, one wave against four, rows of 16 blocks (no
+  // prefix), 136 and 480 (16/4 heads, d = 128): c = 1, 256 rows 18, 22, 28 against
+  // 16, 17, 22; 512 20, 25, 34 against 19, 20, 28; 1024 24, 27, 43 against 25, 26,
+  // 40; 2048 33, 32, 61 against 42, 41, 69.  c = 4, where fewer quads are left:
+  // 256 17, 19, 23 against 19, 19, 22; 512 19, 19, 29 against 20, 21, 29; 1024 22,
+  // 21, 36 against 26, 26, 39.  Longer: solve alone, 1024 rows of 2050 blocks 33
+  // against 23.
   const bool one = a.requests * a.heads >= 512 && a.prefix_runs + a.own_runs <= SO_SHORT / DEC_RUN;
   return one ? launch_solve<E, D, 64>(a, s) : launch_solve<E, D, 256>(a, s);
 }
