@@ -15,7 +15,7 @@
 // walk's step is 64 sequences, one to a lane, the next ones on their way
 // meanwhile; the work still grows with the square of the sequences, so their
 // number is bounded (MAX_SEQS).  A call on 700, 4096, 16384 and 65536 sequences
-// of one row takes 16, 84, 820 and 11300 us (one sequence at a step, by scalar
+// of one row takes 15, 83, 840 and 11900 us (one sequence at a step, by scalar
 // loads: 204, 3030, 42800 and 661000).
 #include "ea_common.h"
 #include "ea_internal.h"
@@ -26,10 +26,19 @@ namespace {
 
 constexpr int PLAN_NT = 256;
 
+// Sum over the wave, in all lanes.
 __device__ __forceinline__ int wave_sum(int v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
+#if defined(__HIP_DEVICE_COMPILE__)
+  // (inside quads, mirrored inside 8 and 16 lanes, then over the four rows)
+  v += __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, true);
+  return __builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16) + __builtin_amdgcn_readlane(v, 32) +
+         __builtin_amdgcn_readlane(v, 48);
+#else
   return v;
+#endif
 }
 
 // The sequences in turn, 64 at a time, each with its rows: none where cu does
@@ -146,7 +155,6 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
     for (int z = 0; z < 2; ++z)
 #pragma unroll
       for (int k = 0; k < FEW; ++k) {
-        if (k >= mine) break;
         const int sum = wave_sum(count[z][k]);
         if (lane == k) before[z] = sum;
       }
