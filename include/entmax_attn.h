@@ -331,7 +331,9 @@ typedef struct {
  *   positions  int32 [axes, tokens], rows `position_stride` elements apart
  *   freqs      fp32 [rot_dim / 2], radians per position
  *   q_weight, k_weight  [d] of weight_dtype (that of q, or fp32), or NULL: 1
- * rot_dim: a multiple of 16, 0 (norm alone) to d.  tokens may be 0.  One launch.
+ * rot_dim: a multiple of 16, 0 (norm alone) to d.  tokens may be 0.  A row that
+ * holds a value that is not finite has no defined result (nor has its weight's
+ * gradient in the backward); other rows are not affected.  One launch.
  */
 typedef struct {
   int32_t tokens, heads, kv_heads, head_dim; /* tokens <= 2^25, head_dim in {64, 128} */
