@@ -10,8 +10,8 @@ is the number of its four bits (sign, and 0, 0.5, 1, 1.5, 2, 3, 4 or 6) times 2^
 s being the scale byte of its 32 values; s = 255 stands for NaN.  The scale is the
 smallest power of two, 2^-125 or more, that leaves the largest of the 32 magnitudes at
 most 7 (6 and 7 are as far apart as half a step of the next numbers would be);
-values are rounded to the nearest number, ties to the even code, and magnitudes
-under 2^-126 count as 0.  A table gives the pages of each row (a request, or a beam).
+values are rounded to the nearest number, ties to the even code.  A table gives the
+pages of each row (a request, or a beam).
 
 ops
     append   cache_append of new tokens' keys and values, and cache_read of the
@@ -227,8 +227,7 @@ def work(case):
 
 def _pack(x):
     """(codes [..., d / 2], scales [..., d / 32]) of values [..., d], bytes."""
-    x = x.float()
-    x = torch.where(x.abs() < 2.0 ** -126, x * 0.0, x).unflatten(-1, (-1, 32))
+    x = x.float().unflatten(-1, (-1, 32))
     bits = x.abs().amax(-1).view(torch.int32)  # (a NaN's are the largest)
     power = bits >> 23
     scale = (power - 2 + ((bits & 0x7FFFFF) > 0x600000).int()).clamp_min(2)
@@ -507,7 +506,6 @@ def _values64(tiles, d):
 def _rounded64(x):
     """What values stand for after they went to 4 bits and back."""
     x = x.double().unflatten(-1, (-1, 32))
-    x = torch.where(x.abs() < 2.0 ** -126, 0.0, x)
     # scales one by one from the smallest up to where the largest magnitude fits
     top = x.abs().amax(-1, keepdim=True)
     scale = torch.full_like(top, 2.0 ** -125)
