@@ -8,8 +8,8 @@ tokens, each 16 rows of d / 2 bytes (value 2 i of a token in the low half of byt
 i, value 2 i + 1 in the high half) and then 16 rows of d / 32 scale bytes.  A value
 is the number of its four bits (sign, and 0, 0.5, 1, 1.5, 2, 3, 4 or 6) times 2^(s - 127),
 s being the scale byte of its 32 values; s = 255 stands for NaN.  The scale is the
-smallest power of two, 2^-125 or more, that leaves the largest of the 32 magnitudes at
-most 7 (6 and 7 are as far apart as half a step of the next numbers would be);
+smallest power of two from 2^-125 to 2^125 that leaves the largest of the 32 magnitudes at
+most 7 (2^125 where none does; 6 and 7 are as far apart as half a step of the next numbers would be);
 values are rounded to the nearest number, ties to the even code.  A table gives the
 pages of each row (a request, or a beam).
 
@@ -230,7 +230,7 @@ def _pack(x):
     x = x.float().unflatten(-1, (-1, 32))
     bits = x.abs().amax(-1).view(torch.int32)  # (a NaN's are the largest)
     power = bits >> 23
-    scale = (power - 2 + ((bits & 0x7FFFFF) > 0x600000).int()).clamp_min(2)
+    scale = (power - 2 + ((bits & 0x7FFFFF) > 0x600000).int()).clamp(2, 252)
     scale = torch.where(power == 255, 255, scale)
     y = x * ((254 - scale).clamp_min(0) << 23).view(torch.float32).unsqueeze(-1)
     m = y.abs()
@@ -510,7 +510,7 @@ def _rounded64(x):
     top = x.abs().amax(-1, keepdim=True)
     scale = torch.full_like(top, 2.0 ** -125)
     for _ in range(260):
-        small = top > 7.0 * scale
+        small = (top > 7.0 * scale) & (scale < 2.0 ** 125)
         if not small.any():
             break
         scale = torch.where(small, 2.0 * scale, scale)
