@@ -462,6 +462,111 @@ ea_status entmax_prefix_decode(const ea_decode_shape* shape, const ea_params* pa
                                const void* v_prefix, void* o, void* workspace, size_t ws_bytes,
                                void* stream);
 
+/*
+ * A cache of keys and values in pages and in 4 bits: `pages` pages of page_size
+ * tokens (a power of two, 16 to 1024) of every key head; bytes
+ *   [pages][kv_heads][2: keys, values][page_size / 16 tiles][17 head_dim / 2]
+ * of which a tile holds 16 tokens: 16 rows of head_dim / 2 bytes, value 2 i of a
+ * token in the low and 2 i + 1 in the high half of byte i, then 16 rows of head_dim / 32
+ * scale bytes, one for every 32 values.  The low three bits of a code c stand for 0,
+ * 0.5, 1, 1.5, 2, 3, 4 or 6, bit 3 is the sign, and the value is that times
+ * 2^(s - 127), s being its scale byte; s = 255: NaN (0 and 1 are never written).
+ * Several layers are one such cache after another.  A pool holds fewer than 2^31
+ * tokens.  cache: 16-byte aligned.
+ *
+ * A table names the pages of each row (a request, a beam): entry p of row r holds
+ * tokens p page_size .. of it.  Entries that are not a page's number are none.  All
+ * of these numbers are on the device, and none of them leads outside the buffers.
+ */
+typedef struct {
+  int32_t pages, page_size, kv_heads, head_dim; /* head_dim in {64, 128} */
+} ea_cache;
+typedef struct {
+  const int32_t* pages; /* [rows, width], rows `stride` elements apart */
+  int32_t rows, width;  /* width * page_size <= 131072 */
+  int64_t stride;
+} ea_page_table;
+ea_status entmax_cache_page_bytes(const ea_cache* c, size_t* bytes);
+
+/*
+ * Append: token i of k and v ([tokens, kv_heads, head_dim] of `dtype`, any
+ * strides) becomes token positions[i] of the table's row rows[i] (int32 on the
+ * device).  Each 32 values get the smallest scale 2^e, -125 <= e <= 125, that
+ * leaves the largest magnitude at most 7 (e = 125 where none does), and are
+ * rounded to the nearest number, ties to the even code, magnitudes above 6 to 6;
+ * 32 values of which one is not finite become NaN.  A token whose row, position
+ * or page there is not is left out.  Two tokens of one call that have the same
+ * place leave either's bytes in any part of it.  Nothing else is written.
+ * Read: the same rows' values (exact in both types), 0 where there is no page.
+ * tokens may be 0.  One launch each.
+ */
+ea_status entmax_cache_append(const ea_cache* c, void* cache, const ea_page_table* table, int32_t tokens,
+                              int32_t dtype, const int32_t* rows, const int32_t* positions, const void* k,
+                              const ea_strides* k_strides, const void* v, const ea_strides* v_strides,
+                              void* stream);
+ea_status entmax_cache_read(const ea_cache* c, const void* cache, const ea_page_table* table, int32_t tokens,
+                            int32_t dtype, const int32_t* rows, const int32_t* positions, void* k,
+                            const ea_strides* k_strides, void* v, const ea_strides* v_strides, void* stream);
+
+/*
+ * Update of a table for the next step.  Row r of the new table goes on from
+ * row parents[r] of the table (none where that is no row), whose first
+ * lengths[parents[r]] tokens it has, and gains counts[r] tokens (loses its last
+ * -counts[r], where negative), for which it gets pages.  Rows may share pages:
+ * where a row is about to write to a page that others hold as well, it gets a
+ * copy (of all rows that hold the page and are about to write to it, the lowest
+ * keeps it if no other holds it).  Pages that no row of the new table keeps are
+ * free, and are given out lowest first, row by row: for the copy, then for the
+ * pages behind.  A row gets all of its pages or none: missing[r] is 0, or the
+ * pages that it needed where those up to it needed more than are free, or -1 where its
+ * tokens do not fit the table's width; such a row keeps its tokens and gains none.
+ *   lengths        [table rows], taken as 0 .. width * page_size
+ *   parents, counts, lengths_out, missing  [rows_out], and table_out
+ *                  [rows_out, width], rows out_stride apart; entries behind a row's
+ *                  pages are -1.  They overlap neither each other nor the inputs.
+ *   layers         pages are copied in all of them
+ * Compaction: pages in use (in the first entries of a row, as many as hold
+ * its length) from number `used` on, their count, move to the free ones below, in
+ * order; table_out [table rows, width] names the new places, and used is 1 number.
+ * workspace: entmax_cache_workspace bytes for as many rows (rows_out), 16-byte aligned.
+ * rows_out may be 0.  Three launches each.
+ */
+ea_status entmax_cache_workspace(const ea_cache* c, int32_t rows, size_t* bytes);
+ea_status entmax_cache_update(const ea_cache* c, int32_t layers, void* cache, const ea_page_table* table,
+                              const int32_t* lengths, int32_t rows_out, const int32_t* parents,
+                              const int32_t* counts, int32_t* table_out, int64_t out_stride,
+                              int32_t* lengths_out, int32_t* missing, void* workspace, size_t ws_bytes,
+                              void* stream);
+ea_status entmax_cache_compact(const ea_cache* c, int32_t layers, void* cache, const ea_page_table* table,
+                               const int32_t* lengths, int32_t* table_out, int64_t out_stride, int32_t* used,
+                               void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * One query per row of q over such a cache: o[i, h] = sum_j p_j v_j over the first
+ * lengths[i] tokens (taken as 0 .. longest) of the table's row rows[i] (rows NULL:
+ * row i).  Tokens without a page have no key; a query without keys, or whose
+ * largest score is not finite, has o = 0.  A key with a NaN scale has no
+ * probability, a value with one makes what it is used in NaN.
+ *   q, o   [queries, heads, head_dim] of `dtype`, any strides; o does not overlap q
+ *   params alpha (at most 2), scale, max_iter and tol are used
+ * q enters the scores within 2^-19 (bf16) or 2^-29 (fp32) of the largest magnitude of
+ * its 32 values.  alpha > 2 is not supported: p has no bounded slope at the edge
+ * of the support there.
+ * queries * heads < 2^23; kv_heads times the regions of 1024 keys of every
+ * query < 2^24.  workspace: entmax_paged_decode_workspace bytes, 16-byte aligned
+ * (8 bytes for every query head and key of `longest`, of which few are used).
+ * Two launches.
+ */
+typedef struct {
+  int32_t queries, heads, dtype;
+  int32_t longest; /* 0..131072: no query has more keys */
+} ea_paged_shape;
+ea_status entmax_paged_decode_workspace(const ea_paged_shape* shape, const ea_cache* c, size_t* bytes);
+ea_status entmax_paged_decode(const ea_paged_shape* shape, const ea_params* params, const ea_cache* c,
+                              const void* cache, const ea_page_table* table, const void* q,
+                              const ea_strides* q_strides, const int32_t* lengths, const int32_t* rows, void* o,
+                              const ea_strides* o_strides, void* workspace, size_t ws_bytes, void* stream);
+
 /* Static, human-readable name of a status code. */
 const char* entmax_attn_status_string(ea_status s);
 

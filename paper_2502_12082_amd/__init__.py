@@ -21,6 +21,13 @@ heads ([tokens, heads, d] tensors, such as parts of a fused projection's rows):
 and one decoding step, for requests that share a prefix:
 
     o = ea.prefix_decode(q, k_cache, v_cache, lengths, k_prefix, v_prefix)
+
+or with keys and values in pages and in 4 bits, for all layers of a step:
+
+    cache = ea.paged_cache(pages, page_size, kv_heads, head_dim, layers)
+    table, lengths, missing = ea.cache_update(cache, table, lengths, parents, counts)
+    ea.cache_append(cache[layer], k, v, rows, positions, table)
+    o = ea.paged_decode(q, cache[layer], table, lengths)
 """
 from __future__ import annotations
 
@@ -55,7 +62,9 @@ SYMBOLS = ("entmax_attn_default_params", "entmax_attn_sizes", "entmax_attn_fwd",
            "entmax_attn_bwd_lists_workspace", "entmax_norm_rotary", "entmax_norm_rotary_workspace",
            "entmax_norm_rotary_bwd", "entmax_packed_plan_bytes", "entmax_packed_plan",
            "entmax_packed_sizes", "entmax_packed_fwd", "entmax_packed_bwd",
-           "entmax_prefix_decode_workspace", "entmax_prefix_decode")
+           "entmax_prefix_decode_workspace", "entmax_prefix_decode", "entmax_cache_page_bytes",
+           "entmax_cache_append", "entmax_cache_read", "entmax_cache_workspace", "entmax_cache_update",
+           "entmax_cache_compact", "entmax_paged_decode_workspace", "entmax_paged_decode")
 EA_ALL_STAGES = -1
 MAX_SEQLEN = 131072  # the longest sequence of every attention call
 NOALLOC_MAX_ROWS = 1048576  # EA_NOALLOC_MAX_ROWS of include/entmax_attn.h
@@ -1342,4 +1351,339 @@ def prefix_decode(q, k_cache, v_cache, lengths, k_prefix=None, v_prefix=None, al
             v_cache.data_ptr(), lengths.data_ptr(), _ptr(k_prefix), _ptr(v_prefix), out.data_ptr(),
             workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_handle(dev)),
             "entmax_prefix_decode")
+    return out
+
+
+# ------------------------------------------- a cache in pages and in 4 bits
+#
+# A layer's cache is a uint8 tensor [pages, kv_heads, 2, page_size / 16, 17 head_dim / 2]
+# (the layout of its bytes: include/entmax_attn.h), a model's one [layers, ...] of
+# those; a table of pages is an int32 tensor [rows, width].
+
+class Cache(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("pages", "page_size", "kv_heads", "head_dim")]
+
+
+class PageTable(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("rows", ctypes.c_int32), ("width", ctypes.c_int32),
+                ("stride", ctypes.c_int64)]
+
+
+class PagedShape(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("queries", "heads", "dtype", "longest")]
+
+
+for _name, _args in (
+        ("entmax_cache_page_bytes", [_P(Cache), _P(_sz)]),
+        ("entmax_cache_append", [_P(Cache), _v, _P(PageTable), _i32, _i32, _v, _v, _v, _P(Strides), _v, _P(Strides),
+                                 _v]),
+        ("entmax_cache_read", [_P(Cache), _v, _P(PageTable), _i32, _i32, _v, _v, _v, _P(Strides), _v, _P(Strides), _v]),
+        ("entmax_cache_workspace", [_P(Cache), _i32, _P(_sz)]),
+        ("entmax_cache_update", [_P(Cache), _i32, _v, _P(PageTable), _v, _i32, _v, _v, _v, _i64, _v, _v, _v, _sz, _v]),
+        ("entmax_cache_compact", [_P(Cache), _i32, _v, _P(PageTable), _v, _v, _i64, _v, _v, _sz, _v]),
+        ("entmax_paged_decode_workspace", [_P(PagedShape), _P(Cache), _P(_sz)]),
+        ("entmax_paged_decode", [_P(PagedShape), _P(Params), _P(Cache), _v, _P(PageTable), _v, _P(Strides), _v, _v, _v,
+                                 _P(Strides), _v, _sz, _v])):
+    getattr(_lib, _name).argtypes = _args
+    getattr(_lib, _name).restype = ctypes.c_int
+
+
+@functools.lru_cache(maxsize=256)
+def _cache_of(shape):
+    """The Cache of a layer's tensor of this shape."""
+    if len(shape) != 5 or shape[2] != 2 or shape[4] not in (544, 1088):
+        raise ValueError("a layer's cache is a [pages, kv_heads, 2, page_size / 16, 17 head_dim / 2] tensor, not %s" %
+                         (shape,))
+    c, n = Cache(shape[0], 16 * shape[3], shape[1], shape[4] * 2 // 17), ctypes.c_size_t()
+    _check(_lib.entmax_cache_page_bytes(c, ctypes.byref(n)), "entmax_cache_page_bytes")
+    return c
+
+
+def paged_cache(pages, page_size, kv_heads, head_dim, layers=None, device="cuda"):
+    """A cache of `pages` pages of page_size tokens (a power of two, 16 to 1024), each
+    of kv_heads heads of 64 or 128 dimensions: a uint8 tensor of one layer, or with
+    layers=n [n, ...] of as many, filled with zeros.  A token takes 17 head_dim / 16
+    bytes of every key head."""
+    if page_size % 16 or head_dim not in (64, 128):
+        raise ValueError("page_size must be a multiple of 16, and head_dim 64 or 128")
+    shape = (pages, kv_heads, 2, page_size // 16, 17 * head_dim // 2)
+    _cache_of(shape)
+    return torch.zeros(shape if layers is None else (layers,) + shape, dtype=torch.uint8, device=device)
+
+
+def _layer(cache):
+    if not isinstance(cache, torch.Tensor) or cache.dtype != torch.uint8:
+        raise ValueError("cache must be a uint8 tensor")
+    c = _cache_of(cache.shape)
+    if not cache.is_contiguous():
+        raise ValueError("cache must be contiguous")
+    if cache.data_ptr() % 16:
+        raise ValueError("cache must start at a multiple of 16 bytes")
+    return c
+
+
+def _layers(cache):
+    """(Cache, layers) of a model's or one layer's cache."""
+    if isinstance(cache, torch.Tensor) and cache.dim() == 6:
+        if cache.shape[0] < 1:
+            raise ValueError("cache has no layers")
+        if not cache.is_contiguous():
+            raise ValueError("cache must be contiguous")
+        return _layer(cache[0]), cache.shape[0]
+    return _layer(cache), 1
+
+
+def _table(table, c, device, name="table"):
+    if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.dtype != torch.int32:
+        raise ValueError("%s must be an int32 [rows, width] tensor" % name)
+    rows, width = table.shape
+    if rows < 1 or width < 1:
+        raise ValueError("%s has no entries" % name)
+    if table.device != device:
+        raise ValueError("%s is on %s, expected %s" % (name, table.device, device))
+    if width > 1 and table.stride(1) != 1:
+        raise ValueError("%s must be contiguous in its last dimension" % name)
+    if width * c.page_size > MAX_SEQLEN:
+        raise ValueError("%s holds %d tokens a row, at most %d are possible" % (name, width * c.page_size, MAX_SEQLEN))
+    return PageTable(table.data_ptr(), rows, width, _stride(table, 0))
+
+
+def _places(cache, rows, positions, table):
+    c = _layer(cache)
+    t = _table(table, c, cache.device)
+    if not isinstance(rows, torch.Tensor) or rows.dim() != 1:
+        raise ValueError("rows must be a [tokens] tensor")
+    _need(rows, "rows", rows.shape, torch.int32, cache.device)
+    _need(positions, "positions", rows.shape, torch.int32, cache.device)
+    return c, t
+
+
+def cache_append(cache, k, v, rows, positions, table):
+    """Writes keys and values k, v [tokens, kv_heads, head_dim] (bf16 or fp32, any strides
+    with a contiguous last dimension) into a layer's cache, rounded to 4 bits: token
+    i becomes token positions[i] of the table's row rows[i] (int32 on the device).
+    Tokens without a place (a negative position, no such row, no page) are left
+    out.  Two tokens of one call must not have the same place, and rows that share
+    a page must not write to it (cache_update gives them pages of their own)."""
+    c, t = _places(cache, rows, positions, table)
+    shape = (rows.shape[0], c.kv_heads, c.head_dim)
+    if not isinstance(k, torch.Tensor):
+        raise ValueError("k must be a torch tensor")
+    dt, dev = _ea_dtype(k, "k"), cache.device
+    _strided(k, "k", shape, k.dtype, dev)
+    _strided(v, "v", shape, k.dtype, dev)
+    _on_gpu(dev)
+    with _on_device(dev):
+        _check(_lib.entmax_cache_append(c, cache.data_ptr(), t, shape[0], dt, rows.data_ptr(), positions.data_ptr(),
+                                        k.data_ptr(), _row_head(k), v.data_ptr(), _row_head(v), _stream_handle(dev)),
+               "entmax_cache_append")
+
+
+def cache_read(cache, rows, positions, table, dtype=torch.bfloat16, k_out=None, v_out=None):
+    """(k, v) [tokens, kv_heads, head_dim]: the values that a layer's cache holds for the
+    tokens positions[i] of the table's rows rows[i], 0 where there is no page.
+    dtype: bfloat16 or float32, exact in both.  k_out, v_out: tensors to write."""
+    c, t = _places(cache, rows, positions, table)
+    shape, dev = (rows.shape[0], c.kv_heads, c.head_dim), cache.device
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("dtype must be bfloat16 or float32, not %s" % dtype)
+    for name, out in (("k_out", k_out), ("v_out", v_out)):
+        if out is not None:
+            _strided(out, name, shape, dtype, dev, written=True)
+    if k_out is not None and v_out is not None and _overlap(k_out, v_out) and not _apart(k_out, v_out):
+        raise ValueError("k_out overlaps v_out")
+    _on_gpu(dev)
+    with _on_device(dev):
+        k_out = torch.empty(shape, dtype=dtype, device=dev) if k_out is None else k_out
+        v_out = torch.empty(shape, dtype=dtype, device=dev) if v_out is None else v_out
+        _check(_lib.entmax_cache_read(c, cache.data_ptr(), t, shape[0], EA_BF16 if dtype == torch.bfloat16 else EA_F32,
+                                      rows.data_ptr(), positions.data_ptr(), k_out.data_ptr(), _row_head(k_out),
+                                      v_out.data_ptr(), _row_head(v_out), _stream_handle(dev)), "entmax_cache_read")
+    return k_out, v_out
+
+
+@functools.lru_cache(maxsize=256)
+def _cache_workspace(c_shape, rows):
+    n = ctypes.c_size_t()
+    _check(_lib.entmax_cache_workspace(_cache_of(c_shape), rows, ctypes.byref(n)), "entmax_cache_workspace")
+    return n.value
+
+
+def cache_workspace(cache, rows):
+    """Bytes of the workspace of cache_update for that many new rows, or of
+    cache_compact for a table of as many."""
+    _layers(cache)
+    return _cache_workspace(cache.shape[-5:], int(rows))
+
+
+def _written(outs, inputs):
+    """Raises ValueError where one of outs (name, tensor) overlaps another or an input."""
+    for n, (name, out) in enumerate(outs):
+        for other_name, other in outs[n + 1:] + inputs:
+            if _overlap(out, other):
+                raise ValueError("%s overlaps %s" % (name, other_name))
+
+
+def cache_update(cache, table, lengths, parents, counts, table_out=None, lengths_out=None, missing_out=None,
+                 workspace=None):
+    """(table_out, lengths_out, missing_out): the table of the next step.  Its row r
+    goes on from row parents[r] of the table, of lengths[parents[r]] tokens (from none,
+    where that is no row), and gains counts[r] tokens (loses its last ones, where
+    negative), for which it gets pages; all are int32 tensors on the device.
+
+    Rows may go on from the same row: they share its pages, and where a row is
+    about to write to a page that others hold as well, it gets a copy in every
+    layer (cache: a model's, or one layer's).  Pages that no new row holds are free;
+    they are given out lowest first, row by row.  A row gets all of its pages or none:
+    missing_out[r] is 0, or the pages that it needed where there were not enough, or -1
+    where its tokens do not fit the table; such a row keeps its tokens and gains none.
+    Entries behind a row's pages are -1.
+
+    table_out [rows, width], lengths_out, missing_out [rows]: tensors to write, which
+    are not those that the call reads.  workspace: cache_workspace bytes, to keep
+    from call to call (one call at a time)."""
+    c, layers = _layers(cache)
+    dev = cache.device
+    t = _table(table, c, dev)
+    _need(lengths, "lengths", (t.rows,), torch.int32, dev)
+    if not isinstance(parents, torch.Tensor) or parents.dim() != 1:
+        raise ValueError("parents must be a [rows] tensor")
+    rows = parents.shape[0]
+    _need(parents, "parents", (rows,), torch.int32, dev)
+    _need(counts, "counts", (rows,), torch.int32, dev)
+    if table_out is not None or lengths_out is not None or missing_out is not None:
+        if table_out is None or lengths_out is None or missing_out is None:
+            raise ValueError("table_out, lengths_out and missing_out must be given together")
+        if rows:
+            _table(table_out, c, dev, "table_out")
+        if table_out.shape != (rows, t.width):
+            raise ValueError("table_out has shape %s, expected %s" % (tuple(table_out.shape), (rows, t.width)))
+        if rows > 1 and table_out.stride(0) < t.width:
+            raise ValueError("table_out has elements that share memory")
+        _need(lengths_out, "lengths_out", (rows,), torch.int32, dev)
+        _need(missing_out, "missing_out", (rows,), torch.int32, dev)
+        _written([("table_out", table_out), ("lengths_out", lengths_out), ("missing_out", missing_out)],
+                 [("table", table), ("lengths", lengths), ("parents", parents), ("counts", counts)])
+    nbytes = _cache_workspace(cache.shape[-5:], rows)
+    if workspace is not None:
+        _check_bytes(workspace, "workspace", nbytes, dev)
+    _on_gpu(dev)
+    with _on_device(dev):
+        if table_out is None:
+            table_out, lengths_out = torch.empty((rows, t.width), dtype=torch.int32, device=dev), torch.empty_like(parents)
+            missing_out = torch.empty_like(parents)
+        if workspace is None:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        _check(_lib.entmax_cache_update(
+            c, layers, cache.data_ptr(), t, lengths.data_ptr(), rows, parents.data_ptr(), counts.data_ptr(),
+            table_out.data_ptr(), max(_stride(table_out, 0), t.width), lengths_out.data_ptr(), missing_out.data_ptr(),
+            workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_handle(dev)),
+            "entmax_cache_update")
+    return table_out, lengths_out, missing_out
+
+
+def cache_compact(cache, table, lengths, table_out=None, used_out=None, workspace=None):
+    """(table_out, used_out): the table, its rows of lengths[r] tokens, after all pages in
+    use have moved to the lowest numbers, in every layer; used_out (int32 [1]) is their
+    count, so that pages from there on are free.  Pages that are below it already
+    stay.  table_out, used_out: tensors to write, which are not the call's inputs."""
+    c, layers = _layers(cache)
+    dev = cache.device
+    t = _table(table, c, dev)
+    _need(lengths, "lengths", (t.rows,), torch.int32, dev)
+    if (table_out is None) != (used_out is None):
+        raise ValueError("table_out and used_out must be given together")
+    if table_out is not None:
+        _table(table_out, c, dev, "table_out")
+        if table_out.shape != table.shape:
+            raise ValueError("table_out has shape %s, expected %s" % (tuple(table_out.shape), tuple(table.shape)))
+        if t.rows > 1 and table_out.stride(0) < t.width:
+            raise ValueError("table_out has elements that share memory")
+        _need(used_out, "used_out", (1,), torch.int32, dev)
+        _written([("table_out", table_out), ("used_out", used_out)], [("table", table), ("lengths", lengths)])
+    nbytes = _cache_workspace(cache.shape[-5:], t.rows)
+    if workspace is not None:
+        _check_bytes(workspace, "workspace", nbytes, dev)
+    _on_gpu(dev)
+    with _on_device(dev):
+        if table_out is None:
+            table_out = torch.empty((t.rows, t.width), dtype=torch.int32, device=dev)
+            used_out = torch.empty(1, dtype=torch.int32, device=dev)
+        if workspace is None:
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        _check(_lib.entmax_cache_compact(
+            c, layers, cache.data_ptr(), t, lengths.data_ptr(), table_out.data_ptr(),
+            max(_stride(table_out, 0), t.width), used_out.data_ptr(), workspace.data_ptr(),
+            workspace.numel() * workspace.element_size(), _stream_handle(dev)), "entmax_cache_compact")
+    return table_out, used_out
+
+
+@functools.lru_cache(maxsize=256)
+def _paged_of(alpha, scale, max_iter, tol, c_shape, *sizes):
+    """(PagedShape, Params, bytes of the workspace) of a call."""
+    c, shape, n = _cache_of(c_shape), PagedShape(*sizes), ctypes.c_size_t()
+    params = make_params(alpha, scale, False, False, max_iter, tol, head_dim=c.head_dim)
+    _check(_lib.entmax_paged_decode_workspace(shape, c, ctypes.byref(n)), "entmax_paged_decode_workspace")
+    return shape, params, n.value
+
+
+def _longest(table, c, max_length):
+    most = table.shape[1] * c.page_size
+    return most if max_length is None else min(most, max(0, int(max_length)))
+
+
+def paged_decode_workspace(q, cache, table, max_length=None):
+    """Bytes of the workspace of paged_decode for these tensors (8 bytes for every query
+    head and key that the table, or max_length, allows; few of them are written)."""
+    c = _layer(cache)
+    return _paged_of(1.5, None, None, None, cache.shape, q.shape[0], q.shape[1], _ea_dtype(q, "q"),
+                     _longest(table, c, max_length))[2]
+
+
+def paged_decode(q, cache, table, lengths, rows=None, alpha=1.5, scale=None, max_iter=None, tol=None, out=None,
+                 workspace=None, max_length=None):
+    """O [queries, heads, head_dim] of q [queries, heads, head_dim] (bf16 or fp32, any strides
+    with a contiguous last dimension): query i attends to the first lengths[i] tokens
+    (int32 on the device) of the table's row rows[i] (None: row i) in a layer's
+    cache.  Several queries may have the same row, with lengths of their own (the
+    last tokens of a draft).  A query without any key has O = 0, and so has one
+    whose largest score is not finite.  1 < alpha <= 2.
+
+    max_length: no query has more keys (default: what the table holds; grids and
+    workspace grow with it).  tol: default 1e-6.  workspace: a device buffer of
+    paged_decode_workspace bytes, to keep from call to call (one call at a time)."""
+    c = _layer(cache)
+    dev = cache.device
+    t = _table(table, c, dev)
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be a [queries, heads, head_dim] tensor")
+    dt = _ea_dtype(q, "q")
+    n, heads, d = q.shape
+    if d != c.head_dim:
+        raise ValueError("q has head_dim %d, the cache %d" % (d, c.head_dim))
+    if heads < 1 or heads % c.kv_heads:
+        raise ValueError("q's %d heads must be a multiple of the cache's %d" % (heads, c.kv_heads))
+    _strided(q, "q", q.shape, q.dtype, dev)
+    _need(lengths, "lengths", (n,), torch.int32, dev)
+    if rows is not None:
+        _need(rows, "rows", (n,), torch.int32, dev)
+    elif n > t.rows:
+        raise ValueError("q has %d queries, the table %d rows: give rows" % (n, t.rows))
+    if out is not None:
+        _strided(out, "out", q.shape, q.dtype, dev, written=True)
+        _written([("out", out)], [("q", q)])
+    shape, params, nbytes = _paged_of(*_numbers(alpha, scale, max_iter, 1e-6 if tol is None else tol), cache.shape, n,
+                                      heads, dt, _longest(table, c, max_length))
+    if workspace is not None:
+        _check_bytes(workspace, "workspace", nbytes, dev)
+    _on_gpu(dev)
+    with _on_device(dev):
+        if out is None:
+            out = q.new_empty(q.shape)
+        if workspace is None:
+            workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=dev)
+        _check(_lib.entmax_paged_decode(
+            shape, params, c, cache.data_ptr(), t, q.data_ptr(), _row_head(q), lengths.data_ptr(), _ptr(rows),
+            out.data_ptr(), _row_head(out), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+            _stream_handle(dev)), "entmax_paged_decode")
     return out

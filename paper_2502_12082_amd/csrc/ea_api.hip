@@ -1182,6 +1182,228 @@ ea_status entmax_prefix_decode(const ea_decode_shape* shape, const ea_params* pa
   return from_hip(launch_decode(a, shape->dtype, shape->head_dim, static_cast<hipStream_t>(stream)));
 }
 
+// ------------------------------------------------ a cache in pages and 4 bits
+
+namespace {
+
+ea_status check_cache(const ea_cache* c, PageDims* out) {
+  if (!c || c->pages < 1 || c->page_size < 1 || c->kv_heads < 1) return EA_ERR_INVALID_ARG;
+  if (c->head_dim != 64 && c->head_dim != 128) return EA_ERR_UNSUPPORTED;
+  if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return EA_ERR_UNSUPPORTED;
+  if (c->kv_heads > 1 << 16) return EA_ERR_UNSUPPORTED;
+  int shift = 4;
+  while (1 << shift < c->page_size) ++shift;
+  // (a token's place in the pool is a 32-bit number)
+  if ((int64_t)c->pages << shift > INT32_MAX) return EA_ERR_UNSUPPORTED;
+  *out = PageDims{c->pages, shift, c->kv_heads, c->head_dim};
+  return EA_OK;
+}
+
+ea_status check_table(const ea_page_table* t, const PageDims& c, PageTable* out) {
+  if (!t || t->rows < 1 || t->width < 1 || t->stride < 0 || t->stride > MAX_STRIDE) return EA_ERR_INVALID_ARG;
+  if (!small_ok(t->pages)) return EA_ERR_INVALID_ARG;
+  if ((int64_t)t->width << c.shift > MAX_SEQLEN || t->rows > 1 << 20) return EA_ERR_UNSUPPORTED;
+  *out = PageTable{t->pages, t->rows, t->width, t->stride};
+  return EA_OK;
+}
+
+ea_status cache_rows(const ea_cache* c, const void* cache, const ea_page_table* table, int32_t tokens, int32_t dtype,
+                     const int32_t* rows, const int32_t* positions, const void* k, const ea_strides* ks,
+                     const void* v, const ea_strides* vs, bool append, void* stream) {
+  CacheRowsArgs a{};
+  ea_status st = check_cache(c, &a.c);
+  if (st != EA_OK || (st = check_table(table, a.c, &a.t)) != EA_OK) return st;
+  if (!dtype_ok(dtype)) return EA_ERR_UNSUPPORTED;
+  if (tokens < 0) return EA_ERR_INVALID_ARG;
+  // a launch has fewer than 2^32 threads: at least 16 tokens to 256 of them
+  if ((int64_t)tokens * c->kv_heads >= (int64_t)1 << 27) return EA_ERR_UNSUPPORTED;
+  if (tokens == 0) return EA_OK;
+  const size_t es = size_of(dtype);
+  if (!strides_ok(ks, es) || !strides_ok(vs, es)) return EA_ERR_INVALID_ARG;
+  if (!tensor_ok(cache) || !tensor_ok(k) || !tensor_ok(v) || !small_ok(rows) || !small_ok(positions))
+    return EA_ERR_INVALID_ARG;
+  a.cache = static_cast<uint8_t*>(const_cast<void*>(cache));
+  a.k = const_cast<void*>(k);
+  a.v = const_cast<void*>(v);
+  a.k_row = ks->row;
+  a.k_head = ks->head;
+  a.v_row = vs->row;
+  a.v_head = vs->head;
+  a.rows = rows;
+  a.positions = positions;
+  a.tokens = tokens;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  return from_hip(append ? launch_cache_append(a, dtype, s) : launch_cache_read(a, dtype, s));
+}
+
+size_t update_parts(const PageDims& c, int rows, void* base, CacheUpdateArgs* a) {
+  const size_t pairs = rows > c.pages ? rows : c.pages;
+  Parts p{static_cast<char*>(base)};
+  a->marks = p.take<int32_t>(UPDATE_MARKS);
+  a->holders = p.take<int32_t>(c.pages);
+  a->writers = p.take<int32_t>(c.pages);
+  a->lowest = p.take<int32_t>(c.pages);
+  a->free_list = p.take<int32_t>(c.pages);
+  a->before = p.take<int32_t>(rows);
+  a->source = p.take<int32_t>(pairs);
+  a->target = p.take<int32_t>(pairs);
+  return p.at;
+}
+
+// The arguments that an update and a compaction have in common.
+ea_status table_args(const ea_cache* c, int32_t layers, void* cache, const ea_page_table* table,
+                     const int32_t* lengths, int32_t rows, int32_t* table_out, int64_t out_stride, void* workspace,
+                     size_t ws_bytes, CacheUpdateArgs* a) {
+  ea_status st = check_cache(c, &a->c);
+  if (st != EA_OK || (st = check_table(table, a->c, &a->t)) != EA_OK) return st;
+  if (layers < 1 || rows < 0 || out_stride < table->width || out_stride > MAX_STRIDE) return EA_ERR_INVALID_ARG;
+  if (layers > 1 << 16 || rows > 1 << 20) return EA_ERR_UNSUPPORTED;
+  if (!tensor_ok(cache) || !small_ok(lengths) || (rows && !small_ok(table_out))) return EA_ERR_INVALID_ARG;
+  if (!tensor_ok(workspace)) return EA_ERR_INVALID_ARG;
+  if (ws_bytes < update_parts(a->c, rows, workspace, a)) return EA_ERR_WORKSPACE;
+  a->layers = layers;
+  a->cache = static_cast<uint8_t*>(cache);
+  a->lengths = lengths;
+  a->table_out = table_out;
+  a->out_stride = out_stride;
+  a->rows_out = rows;
+  return EA_OK;
+}
+
+ea_status check_paged(const ea_paged_shape* s, const ea_cache* c, PagedArgs* a) {
+  if (!s) return EA_ERR_INVALID_ARG;
+  const ea_status st = check_cache(c, &a->c);
+  if (st != EA_OK) return st;
+  if (s->queries < 0 || s->heads < 1 || s->heads % c->kv_heads != 0 || s->longest < 0) return EA_ERR_INVALID_ARG;
+  if (!dtype_ok(s->dtype) || s->longest > MAX_SEQLEN) return EA_ERR_UNSUPPORTED;
+  // a launch has fewer than 2^32 threads: 256 to a workgroup
+  if ((int64_t)s->queries * s->heads >= 1 << 23) return EA_ERR_UNSUPPORTED;
+  a->queries = s->queries;
+  a->heads = s->heads;
+  a->group = s->heads / c->kv_heads;
+  a->longest = s->longest;
+  a->regions = (s->longest + PAGED_REGION - 1) / PAGED_REGION;
+  if (paged_score_wgs(*a) >= 1 << 24) return EA_ERR_UNSUPPORTED;
+  return EA_OK;
+}
+
+size_t paged_parts(void* base, PagedArgs* a) {
+  const size_t lists = (size_t)a->queries * a->heads * a->regions;
+  Parts p{static_cast<char*>(base)};
+  a->top = p.take<float>(lists);
+  a->listed = p.take<int32_t>(lists);
+  a->list = p.take<u32x2_t>(lists * PAGED_REGION);
+  return p.at;
+}
+
+}  // namespace
+
+ea_status entmax_cache_page_bytes(const ea_cache* c, size_t* bytes) {
+  PageDims d;
+  const ea_status st = check_cache(c, &d);
+  if (st != EA_OK) return st;
+  if (!bytes) return EA_ERR_INVALID_ARG;
+  *bytes = (size_t)page_bytes(d);
+  return EA_OK;
+}
+
+ea_status entmax_cache_append(const ea_cache* c, void* cache, const ea_page_table* table, int32_t tokens,
+                              int32_t dtype, const int32_t* rows, const int32_t* positions, const void* k,
+                              const ea_strides* ks, const void* v, const ea_strides* vs, void* stream) {
+  return cache_rows(c, cache, table, tokens, dtype, rows, positions, k, ks, v, vs, true, stream);
+}
+
+ea_status entmax_cache_read(const ea_cache* c, const void* cache, const ea_page_table* table, int32_t tokens,
+                            int32_t dtype, const int32_t* rows, const int32_t* positions, void* k,
+                            const ea_strides* ks, void* v, const ea_strides* vs, void* stream) {
+  return cache_rows(c, cache, table, tokens, dtype, rows, positions, k, ks, v, vs, false, stream);
+}
+
+ea_status entmax_cache_workspace(const ea_cache* c, int32_t rows, size_t* bytes) {
+  PageDims d;
+  const ea_status st = check_cache(c, &d);
+  if (st != EA_OK) return st;
+  if (rows < 0 || !bytes) return EA_ERR_INVALID_ARG;
+  if (rows > 1 << 20) return EA_ERR_UNSUPPORTED;
+  CacheUpdateArgs a{};
+  *bytes = update_parts(d, rows, nullptr, &a);
+  return EA_OK;
+}
+
+ea_status entmax_cache_update(const ea_cache* c, int32_t layers, void* cache, const ea_page_table* table,
+                              const int32_t* lengths, int32_t rows_out, const int32_t* parents, const int32_t* counts,
+                              int32_t* table_out, int64_t out_stride, int32_t* lengths_out, int32_t* missing,
+                              void* workspace, size_t ws_bytes, void* stream) {
+  CacheUpdateArgs a{};
+  const ea_status st =
+      table_args(c, layers, cache, table, lengths, rows_out, table_out, out_stride, workspace, ws_bytes, &a);
+  if (st != EA_OK) return st;
+  if (rows_out == 0) return EA_OK;
+  if (!small_ok(parents) || !small_ok(counts) || !small_ok(lengths_out) || !small_ok(missing))
+    return EA_ERR_INVALID_ARG;
+  a.parents = parents;
+  a.counts = counts;
+  a.lengths_out = lengths_out;
+  a.missing = missing;
+  return from_hip(launch_cache_update(a, static_cast<hipStream_t>(stream)));
+}
+
+ea_status entmax_cache_compact(const ea_cache* c, int32_t layers, void* cache, const ea_page_table* table,
+                               const int32_t* lengths, int32_t* table_out, int64_t out_stride, int32_t* used,
+                               void* workspace, size_t ws_bytes, void* stream) {
+  CacheUpdateArgs a{};
+  const ea_status st = table_args(c, layers, cache, table, lengths, table ? table->rows : 0, table_out, out_stride,
+                                  workspace, ws_bytes, &a);
+  if (st != EA_OK) return st;
+  if (!small_ok(used)) return EA_ERR_INVALID_ARG;
+  a.missing = used;
+  return from_hip(launch_cache_compact(a, static_cast<hipStream_t>(stream)));
+}
+
+ea_status entmax_paged_decode_workspace(const ea_paged_shape* shape, const ea_cache* c, size_t* bytes) {
+  PagedArgs a{};
+  const ea_status st = check_paged(shape, c, &a);
+  if (st != EA_OK) return st;
+  if (!bytes) return EA_ERR_INVALID_ARG;
+  *bytes = paged_parts(nullptr, &a);
+  return EA_OK;
+}
+
+ea_status entmax_paged_decode(const ea_paged_shape* shape, const ea_params* params, const ea_cache* c,
+                              const void* cache, const ea_page_table* table, const void* q, const ea_strides* qs,
+                              const int32_t* lengths, const int32_t* rows, void* o, const ea_strides* os,
+                              void* workspace, size_t ws_bytes, void* stream) {
+  PagedArgs a{};
+  ea_status st = check_paged(shape, c, &a);
+  if (st != EA_OK || (st = check_table(table, a.c, &a.t)) != EA_OK) return st;
+  if (!params) return EA_ERR_INVALID_ARG;
+  if ((st = check_params(params)) != EA_OK) return st;
+  if (params->alpha > 2.0f) return EA_ERR_UNSUPPORTED;
+  if (shape->queries == 0) return EA_OK;
+  const size_t es = size_of(shape->dtype);
+  if (!strides_ok(qs, es) || !strides_ok(os, es) || !tensor_ok(q) || !tensor_ok(o)) return EA_ERR_INVALID_ARG;
+  if (!tensor_ok(cache) || !small_ok(lengths) || (rows && !small_ok(rows))) return EA_ERR_INVALID_ARG;
+  const size_t need = paged_parts(workspace, &a);
+  if (need && !tensor_ok(workspace)) return EA_ERR_INVALID_ARG;
+  if (ws_bytes < need) return EA_ERR_WORKSPACE;
+  a.cache = static_cast<const uint8_t*>(cache);
+  a.q = q;
+  a.o = o;
+  a.q_row = qs->row;
+  a.q_head = qs->head;
+  a.o_row = os->row;
+  a.o_head = os->head;
+  a.lengths = lengths;
+  a.rows = rows;
+  a.scale_c = (params->alpha - 1.0f) * params->scale;
+  a.alpha = params->alpha;
+  a.gamma = 1.0f / (params->alpha - 1.0f);
+  a.tol = params->tol;
+  a.max_iter = params->max_iter;
+  a.gk = gamma_kind(params->alpha);
+  return from_hip(launch_paged_decode(a, shape->dtype, static_cast<hipStream_t>(stream)));
+}
+
 const char* entmax_attn_status_string(ea_status s) {
   switch (s) {
     case EA_OK: return "ok";

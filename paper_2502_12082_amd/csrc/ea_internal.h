@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "ea_pages.h"
+
 namespace ea {
 
 // Largest sequence length the kernels accept (the solver keeps one byte per
@@ -212,6 +214,61 @@ struct DecodeArgs {
   double c64, g64;  // c and gamma (fp32 inputs, alpha > 2)
 };
 
+// Rows of a paged 4-bit cache (ea_pages.h): token i is token positions[i] of the
+// table's row rows[i]; one without a page is left out (read: 0).
+struct CacheRowsArgs {
+  PageDims c;
+  PageTable t;
+  uint8_t* cache;
+  void *k, *v;  // [tokens, kv_heads, D]: read by an append, written by a read
+  int64_t k_row, k_head, v_row, v_head;
+  const int32_t *rows, *positions;
+  int tokens;
+};
+
+// Page tables of the rows that go on (update), or of the same rows with their
+// pages moved to the lowest places (compaction).
+struct CacheUpdateArgs {
+  PageDims c;
+  PageTable t;
+  int layers;
+  uint8_t* cache;
+  const int32_t *lengths, *parents, *counts;  // (a compaction has lengths alone)
+  int32_t* table_out;
+  int64_t out_stride;
+  int rows_out;
+  int32_t *lengths_out, *missing;  // [rows_out]; of a compaction `missing` is one number, the pages in use
+  // workspace: [pages] rows that hold each page, rows about to write to it, the
+  // lowest of those, and free pages (compaction: holders, -, where each page goes, free
+  // pages), [rows_out] pages needed before each row, and [copies] page pairs; marks
+  int32_t *holders, *writers, *lowest, *free_list, *before, *source, *target, *marks;
+};
+// marks: workgroups that have arrived, copies to make
+constexpr int UPDATE_MARKS = 2;
+
+// One query per row of q over the pages of a row of the table.  Keys are taken in
+// regions of PAGED_REGION.
+constexpr int PAGED_REGION = 1024;
+typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
+struct PagedArgs {
+  PageDims c;
+  PageTable t;
+  const uint8_t* cache;
+  const void* q;
+  void* o;
+  int64_t q_row, q_head, o_row, o_head;
+  const int32_t* lengths;  // [queries], clamped to 0 .. longest
+  const int32_t* rows;     // [queries], or null: row i of query i
+  int queries, heads, group, longest, regions;
+  // workspace, of every row (query and head) and region of keys: its largest
+  // score, how many of its scores are listed, and those with their keys
+  float* top;       // [queries, heads, regions]
+  int32_t* listed;  // [queries, heads, regions]
+  u32x2_t* list;    // [queries, heads, regions, PAGED_REGION]
+  float scale_c, alpha, gamma, tol;  // scale_c: (alpha - 1) scale
+  int max_iter, gk;
+};
+
 struct TauArgs {
   const void* q;
   const void* k;
@@ -387,6 +444,13 @@ int dkdv_packed_parts(int tokens, int seqs, int heads, int kv_heads, int dtype, 
 // Workgroups of decoding's first kernel, 64 threads each (from the sizes of `a`).
 int64_t decode_maxima_wgs(const DecodeArgs& a, int dtype);
 hipError_t launch_decode(const DecodeArgs& a, int dtype, int head_dim, hipStream_t s);
+// Workgroups of paged decoding's first kernel, 256 threads each.
+int64_t paged_score_wgs(const PagedArgs& a);
+hipError_t launch_paged_decode(const PagedArgs& a, int dtype, hipStream_t s);
+hipError_t launch_cache_append(const CacheRowsArgs& a, int dtype, hipStream_t s);
+hipError_t launch_cache_read(const CacheRowsArgs& a, int dtype, hipStream_t s);
+hipError_t launch_cache_update(const CacheUpdateArgs& a, hipStream_t s);
+hipError_t launch_cache_compact(const CacheUpdateArgs& a, hipStream_t s);
 int rotary_partials(int tokens);
 hipError_t launch_rotary_fwd(const RotaryArgs& a, int dtype, hipStream_t s);
 hipError_t launch_rotary_bwd(const RotaryArgs& a, int dtype, hipStream_t s);

@@ -1,0 +1,604 @@
+// ea_paged.hip -- alpha-entmax attention of single tokens over a cache in pages
+// and in 4 bits (ea_pages.h), 1 < alpha <= 2.
+//
+// For head h of query i, with keys k_j of its row of the table:
+//   x_j = (alpha - 1) scale <q, k_j>,  tau: sum_j [x_j - tau]_+^gamma = 1,
+//   o = sum_j [x_j - tau]_+^gamma v_j.
+// Two kernels:
+//
+// Scores.  <q, k> comes from the matrix cores' product of 8-bit and 4-bit
+// operands with a scale for every 32 values: K's codes and scales are its operands
+// as they lie in the cache.  Its 8-bit operand has four significant bits, and it
+// keeps products of 8 values 13 bits below the largest of them (measured; 23 bits
+// between such groups), so q is taken apart into digits: of a block of 32 values with
+// the largest magnitude in [8, 16) units, digit 0 is the nearest whole number
+// of units, digit 1 that of 32nds of what is left, and so on, each a whole number of at
+// most 16.  A product of a digit and a code has 8 bits, and the sums of a
+// block are exact.  Four digits are within 2^-19 of the largest magnitude (bf16),
+// six within 2^-29 (fp32).  Only scores that can matter are written: those within 1
+// (of x) of the largest of their region of keys, as tau is at least max x - 1.
+//
+// Solve.  One workgroup per query row.  The largest scores of its regions are scores
+// of distinct keys, so f restricted to them lies below f and its root is a lower
+// bound of tau; the listed scores above it go to LDS, tau is solved on them
+// (Algorithm 1's iteration), and the rows of V with a probability are gathered.
+// Rows with more scores than fit read their lists for every evaluation.  Lists have an
+// order that depends on the scores alone, and sums one that depends on the lists.
+#include "ea_common.h"
+#include "ea_internal.h"
+
+namespace ea {
+
+namespace {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// v and its neighbours in other lanes of 16, by the VALU alone.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __uint_as_float(
+      (uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+#else
+  return v;
+#endif
+}
+constexpr int QUAD_1032 = 0xB1, QUAD_2301 = 0x4E, HALF_MIRROR = 0x141, MIRROR = 0x140;
+template <typename F>
+__device__ __forceinline__ float fold8(float v, F&& f) {
+  v = f(v, dpp<QUAD_1032>(v));
+  v = f(v, dpp<QUAD_2301>(v));
+  return f(v, dpp<HALF_MIRROR>(v));
+}
+template <typename F>
+__device__ __forceinline__ float fold16(float v, F&& f) {
+  v = fold8(v, f);
+  return f(v, dpp<MIRROR>(v));
+}
+template <typename F>
+__device__ __forceinline__ float fold64(float v, F&& f) {
+  v = fold16(v, f);
+#if defined(__HIP_DEVICE_COMPILE__)
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+#endif
+  float lo, hi;
+  wave_halves(v, lo, hi);
+  return f(lo, hi);
+}
+__device__ __forceinline__ float addf(float a, float b) { return a + b; }
+__device__ __forceinline__ float maxf(float a, float b) { return fmaxf(a, b); }
+
+__device__ __forceinline__ int query_length(const PagedArgs& a, int i) {
+  return min(max(((const ci32*)a.lengths)[i], 0), a.longest);
+}
+__device__ __forceinline__ int query_row(const PagedArgs& a, int i) {
+  return a.rows ? ((const ci32*)a.rows)[i] : i;
+}
+
+// ------------------------------------------------------------------ scores
+
+constexpr int PS_NT = 256, PS_WAVES = 4;
+constexpr int PS_KEYS = PAGED_REGION / PS_WAVES;  // of a wave
+constexpr int PS_TILES = PS_KEYS / PAGE_TILE;
+constexpr int PS_CHUNK = 4;  // tiles that are left out together where a row ends before them
+constexpr int PS_HEADS = 16;  // query heads of a workgroup, the rows of a product
+
+template <typename E>
+constexpr int digits() {
+  return sizeof(E) == 2 ? 4 : 6;
+}
+
+// The rows of a product that heads have: a lane holds four rows of it, and a group of
+// up to four heads fills one of them in every lane.
+__device__ __forceinline__ int row_of_head(int j) { return (j & 3) * 4 + (j >> 2); }
+
+// R4: registers of a tile's scores, heads 4 at a time.
+template <typename E, int D, int R4>
+__global__ __launch_bounds__(PS_NT) void paged_scores_kernel(PagedArgs a, int head_tiles) {
+  constexpr int T = digits<E>(), NM = T * D / 128;  // products of a tile
+  constexpr int SB = D / 32;
+  __shared__ __attribute__((aligned(16))) uint8_t dig[T][PS_HEADS][D];
+  __shared__ uint8_t unit[T][PS_HEADS][SB];
+  __shared__ float wave_top[PS_WAVES][PS_HEADS];
+  __shared__ int wave_count[PS_WAVES][PS_HEADS];
+  const int t = threadIdx.x, lane = lane_id(), w = wave_id(), col = lane & 15, g = lane >> 4;
+  int x = blockIdx.x;
+  const int kv = x % a.c.kv_heads;
+  x /= a.c.kv_heads;
+  const int ht = x % head_tiles;
+  x /= head_tiles;
+  const int region = x % a.regions, i = x / a.regions;
+  const int len = query_length(a, i), first = region * PAGED_REGION;
+  if (first >= len) return;
+  const int heads = min(PS_HEADS, a.group - ht * PS_HEADS), h0 = kv * a.group + ht * PS_HEADS;
+
+  // ---- the wave's tiles: their pages, then all of their loads
+  const int k0 = first + w * PS_KEYS, row = query_row(a, i);
+  const int ids = col < PS_TILES && k0 + col * PAGE_TILE < len ? page_of(a.c, a.t, row, k0 + col * PAGE_TILE) : -1;
+  i32x4 kf[PS_TILES];
+  int ks[PS_TILES];
+#pragma unroll
+  for (int c = 0; c < PS_TILES; c += PS_CHUNK) {
+    if (k0 + c * PAGE_TILE >= len) break;
+#pragma unroll
+    for (int u = c; u < c + PS_CHUNK; ++u) {
+      // (a tile without a page reads the first one's, and its scores are dropped)
+      const int page = max(__builtin_amdgcn_readlane(ids, u), 0);
+      const uint8_t* const tile = a.cache + tile_at(a.c, page, kv, false, k0 + u * PAGE_TILE);
+      const int part = D == 128 ? g : g & 1;
+      kf[u] = *reinterpret_cast<const i32x4*>(tile + (uint32_t)(col * (D / 2) + part * 16));
+      ks[u] = tile[(uint32_t)(PAGE_TILE * (D / 2) + col * SB + part)];
+    }
+  }
+
+  // ---- the digits of the queries
+  for (int c = t; c < heads * (D / 4); c += PS_NT) {
+    const int j = c / (D / 4), at = c % (D / 4) * 4;
+    const E* const p = static_cast<const E*>(a.q) + i * a.q_row + (h0 + j) * a.q_head + at;
+    float y[4];
+    if constexpr (sizeof(E) == 2) {
+      const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        y[2 * e] = __uint_as_float(v[e] << 16);
+        y[2 * e + 1] = __uint_as_float(v[e] & 0xFFFF0000u);
+      }
+    } else {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = v[e];
+    }
+    // (non-negative floats compare as integers do; NaN is the largest)
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m = max(m, __float_as_uint(y[e]) & 0x7FFFFFFFu);
+    m = __float_as_uint(fold8(__uint_as_float(m), [](float p, float q) {
+      return __uint_as_float(max(__float_as_uint(p), __float_as_uint(q)));
+    }));
+    const int e0 = (int)(m >> 23);  // units of 2^(e0 - 127 - 3)
+    const bool finite = e0 != 255;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = finite ? ldexpf(y[e], 130 - e0) : 0.f;
+    const int r = row_of_head(j);
+#pragma unroll
+    for (int d = 0; d < T; ++d) {
+      float n[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        n[e] = rintf(y[e]);
+        y[e] = (y[e] - n[e]) * 32.f;
+      }
+      int word = 0;
+#if defined(__HIP_DEVICE_COMPILE__)
+      word = __builtin_amdgcn_cvt_pk_fp8_f32(n[0], n[1], word, false);
+      word = __builtin_amdgcn_cvt_pk_fp8_f32(n[2], n[3], word, true);
+#endif
+      const int scale = e0 - 3 - 5 * d;  // (digits under 2^-127 are dropped)
+      *reinterpret_cast<int*>(&dig[d][r][at]) = scale < 0 ? 0 : word;
+      if ((c & 7) == 0) unit[d][r][at / 32] = finite ? (uint8_t)max(scale, 0) : 255;
+    }
+  }
+  __syncthreads();
+  // A operands: of 128 values a lane holds 16 g .. and 64 + 16 g .., and the scale
+  // of block g; at D = 64 two digits are one operand, K's row twice the other
+  i32x8 qf[NM];
+  int qs[NM];
+#pragma unroll
+  for (int m = 0; m < NM; ++m) {
+    const i32x4 lo = *reinterpret_cast<const i32x4*>(D == 128 ? &dig[m][col][16 * g] : &dig[2 * m][col][16 * g]);
+    const i32x4 hi = *reinterpret_cast<const i32x4*>(D == 128 ? &dig[m][col][64 % D + 16 * g] : &dig[(2 * m + 1) % T][col][16 * g]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      qf[m][e] = lo[e];
+      qf[m][4 + e] = hi[e];
+    }
+    qs[m] = D == 128 ? unit[m][col][g % SB] : unit[(2 * m + (g >> 1)) % T][col][g & 1];
+  }
+
+  // ---- scores of head g + 4 r and the tile's key `col`
+  float s[PS_TILES][R4];
+#pragma unroll
+  for (int u = 0; u < PS_TILES; ++u)
+#pragma unroll
+    for (int r = 0; r < R4; ++r) s[u][r] = -INFINITY;
+  float top[R4];
+#pragma unroll
+  for (int r = 0; r < R4; ++r) top[r] = -INFINITY;
+#pragma unroll
+  for (int c = 0; c < PS_TILES; c += PS_CHUNK) {
+    if (k0 + c * PAGE_TILE >= len) break;
+#pragma unroll
+    for (int u = c; u < c + PS_CHUNK; ++u) {
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#if defined(__HIP_DEVICE_COMPILE__)
+      const i32x8 k = {kf[u][0], kf[u][1], kf[u][2], kf[u][3], 0, 0, 0, 0};
+#pragma unroll
+      for (int m = NM - 1; m >= 0; --m)  // (the smallest first)
+        v = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(qf[m], k, v, 0, 4, 0, qs[m], 0, ks[u]);
+#endif
+      const bool ok = k0 + u * PAGE_TILE + col < len && __builtin_amdgcn_readlane(ids, u) >= 0;
+#pragma unroll
+      for (int r = 0; r < R4; ++r) {
+        s[u][r] = ok ? v[r] : -INFINITY;
+        top[r] = fmaxf(top[r], s[u][r]);  // (a NaN is left out)
+      }
+    }
+  }
+
+  // ---- the region's largest, and what is within 1 / c of it
+#pragma unroll
+  for (int r = 0; r < R4; ++r) {
+    top[r] = fold16(top[r], maxf);
+    if (col == 0) wave_top[w][g + 4 * r] = top[r];
+  }
+  __syncthreads();
+  const float reach = 1.0001f / a.scale_c;
+  float bound[R4];
+  int count[R4];
+#pragma unroll
+  for (int r = 0; r < R4; ++r) {
+    const int j = g + 4 * r;
+    top[r] = fmaxf(fmaxf(wave_top[0][j], wave_top[1][j]), fmaxf(wave_top[2][j], wave_top[3][j]));
+    bound[r] = j < heads ? top[r] - reach : INFINITY;
+    count[r] = 0;
+  }
+  auto among = [&](bool keep) { return (uint32_t)(__ballot(keep) >> (16 * g)) & 0xFFFFu; };
+#pragma unroll
+  for (int u = 0; u < PS_TILES; ++u)
+#pragma unroll
+    for (int r = 0; r < R4; ++r) count[r] += __popc(among(s[u][r] > bound[r]));
+#pragma unroll
+  for (int r = 0; r < R4; ++r)
+    if (col == 0) wave_count[w][g + 4 * r] = count[r];
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < R4; ++r) {
+    const int j = g + 4 * r;
+    if (j >= heads) continue;
+    const int64_t list = ((int64_t)i * a.heads + h0 + j) * a.regions + region;
+    int to = 0, all = 0;
+#pragma unroll
+    for (int y = 0; y < PS_WAVES; ++y) {
+      to += y < w ? wave_count[y][j] : 0;
+      all += wave_count[y][j];
+    }
+    if (w == 0 && col == 0) {
+      a.top[list] = top[r];
+      a.listed[list] = all;
+    }
+    count[r] = to;
+  }
+#pragma unroll
+  for (int u = 0; u < PS_TILES; ++u) {
+    if (k0 + u * PAGE_TILE >= len) break;
+    const int at = k0 + u * PAGE_TILE;
+    // where the key lies in the pool
+    const uint32_t slot = ((uint32_t)__builtin_amdgcn_readlane(ids, u) << a.c.shift) +
+                          (uint32_t)(at & ((1 << a.c.shift) - 1)) + col;
+#pragma unroll
+    for (int r = 0; r < R4; ++r) {
+      const bool keep = s[u][r] > bound[r];
+      const uint32_t m = among(keep);
+      if (keep) {
+        const int64_t list = ((int64_t)i * a.heads + h0 + g + 4 * r) * a.regions + region;
+        u32x2_t entry = {__float_as_uint(s[u][r]), slot};
+        a.list[list * PAGED_REGION + count[r] + __popc(m & ((1u << col) - 1))] = entry;
+      }
+      count[r] += __popc(m);
+    }
+  }
+}
+
+// ------------------------------------------------------------------- solve
+
+constexpr int MAX_REGIONS = MAX_SEQLEN / PAGED_REGION;
+constexpr int PV_VALS = 16;   // values of V that a lane takes of a row
+constexpr int PV_BATCH = 4;   // rows of V of a lane in flight
+
+template <typename E, int D, int GK, int NT>
+__global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
+  constexpr int WAVES = NT / 64, CAP = NT == 256 ? 512 : 256;  // scores that a wave keeps
+  constexpr int LPK = D / PV_VALS, KPW = 64 / LPK;
+  constexpr int ALONE = 8;  // scores per lane that every wave solves by itself
+  static_assert(WAVES * CAP * 8 >= WAVES * D * 4, "the waves' sums fit in place of the scores");
+  __shared__ __attribute__((aligned(16))) u32x2_t kept[WAVES][CAP];
+  __shared__ float red[2][3][WAVES];
+  __shared__ int counts[WAVES];
+  const int t = threadIdx.x, lane = lane_id(), w = wave_id();
+  // (heads of one key head are kv_heads apart: with eight of them, on one XCD)
+  const int i = blockIdx.x / a.heads, y = blockIdx.x % a.heads;
+  const int kv = y % a.c.kv_heads, h = kv * a.group + y / a.c.kv_heads;
+  const int len = query_length(a, i), regions = (len + PAGED_REGION - 1) / PAGED_REGION;
+  const int64_t row = ((int64_t)i * a.heads + h) * a.regions;
+  E* const O = static_cast<E*>(a.o) + i * a.o_row + h * a.o_head;
+  const float c = a.scale_c, gm = a.gamma;
+
+  // ---- the regions' largest scores: in every wave
+  float top[MAX_REGIONS / 64], m = -INFINITY;
+#pragma unroll
+  for (int e = 0; e < MAX_REGIONS / 64; ++e) {
+    top[e] = 64 * e + lane < regions ? a.top[row + 64 * e + lane] : -INFINITY;
+    m = fmaxf(m, top[e]);
+  }
+  m = c * fold64(m, maxf);
+  if (!(m > -INFINITY && m < INFINITY)) {  // no keys, or none with a finite score
+    for (int d = t; d < D; d += NT) O[d] = (E)0.f;
+    return;
+  }
+  // z^gamma, z^(gamma-1), z^(gamma-2) summed over z > 0
+  auto add = [&](float z, float& s0, float& s1, float& s2) {
+    if (z > 0.f) {
+      float p, u;
+      Gamma<GK>::pu(z, gm, p, u);
+      s0 += p;
+      s1 += u;
+      if constexpr (GK == 2) s2 += 1.f;
+      if constexpr (GK == 4) s2 += z * z;
+      if constexpr (GK == 0) s2 += u / z;
+    }
+  };
+  float lo = m - 1.f;
+  for (int it = 0; it < 8; ++it) {
+    float s0 = 0.f, s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int e = 0; e < MAX_REGIONS / 64; ++e) add(relu_z(c, top[e], lo), s0, s1, s2);
+    s0 = fold64(s0, addf);
+    s1 = fold64(s1, addf);
+    const float step = (s0 - 1.f) * __builtin_amdgcn_rcpf(gm * s1);
+    if (!(step > 1e-3f)) break;
+    lo += step;
+  }
+  lo -= 4e-6f * fmaxf(1.f, fabsf(lo));  // (the sums' rounding)
+
+  // ---- the listed scores above the bound.  With fewer regions than waves several waves
+  // share a region's list, 64 entries at a time in turn.
+  const int parts = regions >= WAVES ? 1 : WAVES / regions;
+  // use(entry) of the wave's entries, 64 at a time; keep(entries of this step) first
+  auto each = [&](auto&& use) {
+    for (int x = w; x < regions * parts; x += WAVES) {
+      const int region = x / parts;
+      float best = top[0];
+      if constexpr (MAX_REGIONS > 64) best = region < 64 ? top[0] : top[1];
+      best = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(best), region & 63));
+      if (!(relu_z(c, best, lo) > 0.f)) continue;
+      const int n = a.listed[row + region];
+      const u32x2_t* const list = a.list + (row + region) * PAGED_REGION;
+      for (int e0 = 64 * (x % parts); e0 < n; e0 += 64 * parts) {
+        u32x2_t v = {0xFF800000u, 0};  // (-inf)
+        if (e0 + lane < n) v = list[e0 + lane];
+        use(v);
+      }
+    }
+  };
+  int mine = 0;  // the wave's count
+  const uint64_t before = (1ull << lane) - 1;
+  each([&](const u32x2_t& v) {
+    const bool keep = relu_z(c, __uint_as_float(v[0]), lo) > 0.f;
+    const uint64_t k = __ballot(keep);
+    const int to = mine + __popcll(k & before);
+    if (keep && to < CAP) kept[w][to] = v;
+    mine += __popcll(k);
+  });
+  if (lane == 0) counts[w] = mine;
+  __syncthreads();
+  int total = 0;
+  bool wide = false;
+#pragma unroll
+  for (int x = 0; x < WAVES; ++x) {
+    total += counts[x];
+    wide |= counts[x] > CAP;
+  }
+
+  // ---- tau: Algorithm 1's iteration on them
+  int turn = 0;
+  auto sum3 = [&](float& s0, float& s1, float& s2) {
+    s0 = fold64(s0, addf);
+    s1 = fold64(s1, addf);
+    s2 = fold64(s2, addf);
+    auto& r = red[turn];
+    turn ^= 1;
+    if (lane == 0) {
+      r[0][w] = s0;
+      r[1][w] = s1;
+      r[2][w] = s2;
+    }
+    __syncthreads();
+    s0 = s1 = s2 = 0.f;
+#pragma unroll
+    for (int x = 0; x < WAVES; ++x) {
+      s0 += r[0][x];
+      s1 += r[1][x];
+      s2 += r[2][x];
+    }
+  };
+  const bool alone = !wide && total <= 64 * ALONE;
+  float own[ALONE];
+  if (alone) {
+#pragma unroll
+    for (int e = 0; e < ALONE; ++e) {
+      own[e] = -INFINITY;
+      int at = 64 * e + lane, x = 0;
+      if (at < total) {
+        while (at >= counts[x]) at -= counts[x++];
+        own[e] = __uint_as_float(kept[x][at][0]);
+      }
+    }
+    __syncthreads();  // (a wave that is done writes to its list)
+  }
+  float hi = m - powf((float)len, 1.f - a.alpha);
+  float low = fminf(lo, hi), tau = low;
+  for (int it = 0;; ++it) {
+    float s0 = 0.f, s1 = 0.f, s2 = 0.f;
+    if (alone) {
+#pragma unroll
+      for (int e = 0; e < ALONE; ++e) {
+        if (64 * e >= total) break;
+        add(relu_z(c, own[e], tau), s0, s1, s2);
+      }
+      s0 = fold64(s0, addf);
+      s1 = fold64(s1, addf);
+      s2 = fold64(s2, addf);
+    } else if (!wide) {
+      for (int e = lane; e < mine; e += 64) add(relu_z(c, __uint_as_float(kept[w][e][0]), tau), s0, s1, s2);
+      sum3(s0, s1, s2);
+    } else {
+      each([&](const u32x2_t& v) { add(relu_z(c, __uint_as_float(v[0]), tau), s0, s1, s2); });
+      sum3(s0, s1, s2);
+    }
+    const float f = s0 - 1.f;
+    const bool stop = fabsf(f) <= a.tol || it >= a.max_iter;
+    // B_f, Newton's bound, H_f: the update rules of the attention solver
+    const float f1 = -gm * s1, f2 = gm * (gm - 1.f) * s2;
+    if (f < 0.f)
+      hi = tau;
+    else
+      low = tau;
+    const float slack = 1e-6f * fmaxf(1.f, fmaxf(fabsf(low), fabsf(hi)));
+    if (f1 < 0.f) low = fminf(fmaxf(low, tau - f / f1 - 10.f * slack), hi);
+    const float th = tau - 2.f * f * f1 / (2.f * f1 * f1 - f * f2);
+    const bool take = th >= low - slack && th <= hi + slack;
+    // (the update from the last evaluation is taken too)
+    tau = take ? fminf(fmaxf(th, low), hi) : th < low ? low : 0.5f * (low + hi);
+    if (stop) break;
+  }
+
+  // ---- O: the rows of V with a probability.  LPK lanes to a row, each 16 values of
+  // it (half a block).
+  float o[PV_VALS] = {};
+  const int sub = lane % LPK, grp = lane / LPK;
+  const uint8_t* const V = a.cache + tile_at(a.c, 0, kv, true, 0);
+  const int64_t page_step = page_bytes(a.c);
+  const int mask = (1 << a.c.shift) - 1;
+  // of the wave's first n kept entries, scores, those with p > 0, p in place of the score
+  auto gather = [&](int n) {
+    int np = 0;
+    for (int e0 = 0; e0 < n; e0 += 64) {
+      u32x2_t v = {0xFF800000u, 0};
+      if (e0 + lane < n) v = kept[w][e0 + lane];
+      const float p = Gamma<GK>::p_only(relu_z(c, __uint_as_float(v[0]), tau), gm);
+      const uint64_t k = __ballot(p > 0.f);
+      if (p > 0.f) {
+        v[0] = __float_as_uint(p);
+        kept[w][np + __popcll(k & before)] = v;
+      }
+      np += __popcll(k);
+    }
+    for (int e0 = 0; e0 < np; e0 += KPW * PV_BATCH) {
+      u32x2 codes[PV_BATCH];
+      float p[PV_BATCH];
+      uint32_t scale[PV_BATCH];
+#pragma unroll
+      for (int u = 0; u < PV_BATCH; ++u) {
+        const int e = e0 + u * KPW + grp;
+        const u32x2_t v = kept[w][min(e, np - 1)];
+        p[u] = __uint_as_float(v[0]);
+        const int at = (int)(v[1] & (uint32_t)mask);
+        const uint8_t* const tile = V + (int64_t)(v[1] >> a.c.shift) * page_step + (at >> 4) * tile_bytes(D);
+        codes[u] = *reinterpret_cast<const u32x2*>(tile + (at & 15) * (D / 2) + 8 * sub);
+        scale[u] = tile[PAGE_TILE * (D / 2) + (at & 15) * (D / 32) + sub / 2];
+      }
+#pragma unroll
+      for (int u = 0; u < PV_BATCH; ++u) {
+        if (e0 + u * KPW >= np) break;
+        // (a row again in the place of none: whatever it holds is not used)
+#if defined(__HIP_DEVICE_COMPILE__)
+        const float ps = e0 + u * KPW + grp >= np ? 0.f
+                         : scale[u] == 255        ? __builtin_nanf("")
+                                                  : p[u] * __uint_as_float(scale[u] << 23);
+        auto two = [&](int at, auto v) {
+          o[at] = fmaf(ps, v[0], o[at]);
+          o[at + 1] = fmaf(ps, v[1], o[at + 1]);
+        };
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          two(8 * x, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u][x], 1.f, 0));
+          two(8 * x + 2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u][x], 1.f, 1));
+          two(8 * x + 4, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u][x], 1.f, 2));
+          two(8 * x + 6, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u][x], 1.f, 3));
+        }
+#endif
+      }
+    }
+  };
+  if (!wide) {
+    gather(mine);
+  } else {
+    int n = 0;  // (the wave's list is filled and emptied in turn)
+    each([&](const u32x2_t& v) {
+      if (n + 64 > CAP) {
+        gather(n);
+        n = 0;
+      }
+      const bool keep = relu_z(c, __uint_as_float(v[0]), tau) > 0.f;
+      const uint64_t k = __ballot(keep);
+      if (keep) kept[w][n + __popcll(k & before)] = v;
+      n += __popcll(k);
+    });
+    gather(n);
+  }
+  __syncthreads();
+  // sums over the rows of a wave, then over the waves, in place of the scores
+  float(&sums)[WAVES][D] = reinterpret_cast<float(&)[WAVES][D]>(kept);
+#pragma unroll
+  for (int d = 0; d < PV_VALS; ++d) {
+#pragma unroll
+    for (int x = LPK; x < 64; x <<= 1) o[d] += __shfl_xor(o[d], x);
+    if (grp == 0) sums[w][sub * PV_VALS + d] = o[d];
+  }
+  __syncthreads();
+  for (int d = t; d < D; d += NT) {
+    float sum = 0.f;
+#pragma unroll
+    for (int x = 0; x < WAVES; ++x) sum += sums[x][d];
+    O[d] = (E)sum;
+  }
+}
+
+int head_tiles(const PagedArgs& a) { return (a.group + PS_HEADS - 1) / PS_HEADS; }
+
+template <typename E, int D>
+hipError_t launch_scores(const PagedArgs& a, hipStream_t s) {
+  const int r4 = a.group >= 16 ? 4 : (a.group + 3) / 4;
+  void (*kernel)(PagedArgs, int) = paged_scores_kernel<E, D, 1>;
+  if (r4 == 2) kernel = paged_scores_kernel<E, D, 2>;
+  if (r4 == 3) kernel = paged_scores_kernel<E, D, 3>;
+  if (r4 == 4) kernel = paged_scores_kernel<E, D, 4>;
+  PagedArgs args = a;
+  int tiles = head_tiles(a);
+  void* params[] = {&args, &tiles};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)paged_score_wgs(a)), dim3(PS_NT), params,
+                         0, s);
+}
+
+template <typename E, int D, int NT>
+hipError_t launch_solve(const PagedArgs& a, hipStream_t s) {
+  auto kernel = paged_solve_kernel<E, D, 0, NT>;
+  if (a.gk == 1) kernel = paged_solve_kernel<E, D, 1, NT>;
+  if (a.gk == 2) kernel = paged_solve_kernel<E, D, 2, NT>;
+  if (a.gk == 4) kernel = paged_solve_kernel<E, D, 4, NT>;
+  return launch_kernel(kernel, dim3((unsigned)(a.queries * a.heads)), dim3(NT), s, a);
+}
+
+template <typename E, int D>
+hipError_t launch_paged(const PagedArgs& a, hipStream_t s) {
+  if (a.regions) {
+    const hipError_t e = launch_scores<E, D>(a, s);
+    if (e != hipSuccess) return e;
+  }
+  return launch_solve<E, D, 256>(a, s);
+}
+
+}  // namespace
+
+int64_t paged_score_wgs(const PagedArgs& a) {
+  return (int64_t)a.queries * a.regions * head_tiles(a) * a.c.kv_heads;
+}
+
+hipError_t launch_paged_decode(const PagedArgs& a, int dtype, hipStream_t s) {
+  if (dtype == 0) return a.c.head_dim == 64 ? launch_paged<__bf16, 64>(a, s) : launch_paged<__bf16, 128>(a, s);
+  return a.c.head_dim == 64 ? launch_paged<float, 64>(a, s) : launch_paged<float, 128>(a, s);
+}
+
+}  // namespace ea

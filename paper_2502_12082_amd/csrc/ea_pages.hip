@@ -1,0 +1,455 @@
+// ea_pages.hip -- a cache of keys and values in pages and in 4 bits: rows go in
+// and come back (append, read), and page tables go from step to step (update,
+// compaction) with the pages that have to be copied.
+//
+// Blocks of 32 values share the scale 2^e, the smallest that leaves the largest
+// magnitude at most 7: with a = max |x| = m 2^E, 1 <= m < 2, that is e = E - 2, or
+// E - 1 where m > 1.75; x / 2^e is rounded to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4
+// and 6, ties to the even code (v_cvt_scalef32_pk_fp4, which takes the scale).  e is
+// -125 at least and 125 at most, so that every number there is is a normal fp32 one.
+#include "ea_common.h"
+#include "ea_internal.h"
+
+namespace ea {
+
+namespace {
+
+// ------------------------------------------------------------ rows in, rows out
+
+// A thread takes 8 values of one token's key and value head: 16 (bf16) or 32
+// bytes, 4 bytes of codes.  LPR lanes are a row; a wave's rows are tokens in order,
+// whose rows of codes lie in one piece.  Bound by HBM where tokens are many.
+constexpr int CR_NT = 256, CR_VALS = 8;
+template <typename E>
+struct Vals {
+  float x[CR_VALS];
+  __device__ __forceinline__ void load(const E* p) {
+    if constexpr (sizeof(E) == 2) {
+      const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+      }
+    } else {
+      const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[i] = a[i];
+        x[4 + i] = b[i];
+      }
+    }
+  }
+  // (a code's number times a power of two has two significant bits: no rounding in bf16)
+  __device__ __forceinline__ void store(E* p) const {
+    if constexpr (sizeof(E) == 2) {
+      u32x4 w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        w[i] = __float_as_uint(x[2 * i]) >> 16 | (__float_as_uint(x[2 * i + 1]) & 0xFFFF0000u);
+      *reinterpret_cast<u32x4*>(p) = w;
+    } else {
+      f32x4 a, b;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        a[i] = x[i];
+        b[i] = x[4 + i];
+      }
+      reinterpret_cast<f32x4*>(p)[0] = a;
+      reinterpret_cast<f32x4*>(p)[1] = b;
+    }
+  }
+};
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_of(uint32_t v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+#else
+  return v;
+#endif
+}
+
+// Scale byte of the block of 32 values whose four lanes call this, 255 where one
+// of them is not finite.  (Magnitudes compare as the integers that their bits are.)
+__device__ __forceinline__ uint32_t scale_of(const float (&x)[CR_VALS]) {
+  uint32_t a = 0;
+#pragma unroll
+  for (int i = 0; i < CR_VALS; ++i) a = max(a, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+  a = max(a, dpp_of<0xB1>(a));  // quad_perm 1, 0, 3, 2
+  a = max(a, dpp_of<0x4E>(a));  // quad_perm 2, 3, 0, 1
+  const int e = (int)(a >> 23);
+  return e == 255 ? 255u : (uint32_t)min(max(e - 2 + ((a & 0x7FFFFFu) > 0x600000u ? 1 : 0), 2), 252);
+}
+
+__device__ __forceinline__ uint32_t codes_of(const float (&x)[CR_VALS], uint32_t scale) {
+  uint32_t w = 0;
+#if defined(__HIP_DEVICE_COMPILE__)
+  if (scale == 255) return 0;
+  const float s = __uint_as_float(scale << 23);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], s, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], s, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], s, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], s, 3);
+#endif
+  return w;
+}
+__device__ __forceinline__ void values_of(uint32_t w, uint32_t scale, float (&x)[CR_VALS]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const float s = scale == 255 ? __builtin_nanf("") : __uint_as_float(scale << 23);
+  auto pair = [&](int at, auto v) {
+    x[at] = v[0] * s;
+    x[at + 1] = v[1] * s;
+  };
+  pair(0, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 0));
+  pair(2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 1));
+  pair(4, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 2));
+  pair(6, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.f, 3));
+#endif
+}
+
+// Rows that a thread takes one after another, all loads first.
+constexpr int CR_ROWS = 2;
+
+template <typename E, int D, bool APPEND>
+__global__ __launch_bounds__(CR_NT) void cache_rows_kernel(CacheRowsArgs a, int token_tiles) {
+  constexpr int LPR = D / CR_VALS, STEP = CR_NT / LPR;
+  const int sub = threadIdx.x % LPR, head = blockIdx.x / token_tiles;
+  const int t0 = blockIdx.x % token_tiles * (STEP * CR_ROWS) + threadIdx.x / LPR;
+  E* const K = static_cast<E*>(a.k) + head * a.k_head + sub * CR_VALS;
+  E* const V = static_cast<E*>(a.v) + head * a.v_head + sub * CR_VALS;
+  int32_t at[CR_ROWS], page[CR_ROWS];
+#pragma unroll
+  for (int u = 0; u < CR_ROWS; ++u) {
+    const int t = t0 + u * STEP;
+    at[u] = t < a.tokens ? a.positions[t] : -1;
+    page[u] = t < a.tokens ? page_of(a.c, a.t, a.rows[t], at[u]) : -1;
+  }
+  if constexpr (APPEND) {
+    Vals<E> k[CR_ROWS], v[CR_ROWS];
+#pragma unroll
+    for (int u = 0; u < CR_ROWS; ++u) {
+      const int64_t t = min(t0 + u * STEP, a.tokens - 1);
+      k[u].load(K + t * a.k_row);
+      v[u].load(V + t * a.v_row);
+    }
+#pragma unroll
+    for (int u = 0; u < CR_ROWS; ++u) {
+      const uint32_t ks = scale_of(k[u].x), vs = scale_of(v[u].x);
+      if (page[u] < 0) continue;
+      const int r = at[u] & (PAGE_TILE - 1);
+      uint8_t* const kt = a.cache + tile_at(a.c, page[u], head, false, at[u]);
+      uint8_t* const vt = kt + part_bytes(a.c);
+      const int to = r * (D / 2) + 4 * sub;
+      *reinterpret_cast<uint32_t*>(kt + to) = codes_of(k[u].x, ks);
+      *reinterpret_cast<uint32_t*>(vt + to) = codes_of(v[u].x, vs);
+      if (sub % 4 == 0) {
+        const int st = PAGE_TILE * (D / 2) + r * (D / 32) + sub / 4;
+        kt[st] = (uint8_t)ks;
+        vt[st] = (uint8_t)vs;
+      }
+    }
+  } else {
+    uint32_t k[CR_ROWS], v[CR_ROWS], ks[CR_ROWS], vs[CR_ROWS];
+#pragma unroll
+    for (int u = 0; u < CR_ROWS; ++u) {
+      // (a row without a page reads the first one, and writes 0)
+      const int r = at[u] & (PAGE_TILE - 1);
+      const uint8_t* const kt = a.cache + tile_at(a.c, max(page[u], 0), head, false, at[u]);
+      const uint8_t* const vt = kt + part_bytes(a.c);
+      const int from = r * (D / 2) + 4 * sub, st = PAGE_TILE * (D / 2) + r * (D / 32) + sub / 4;
+      k[u] = *reinterpret_cast<const uint32_t*>(kt + from);
+      v[u] = *reinterpret_cast<const uint32_t*>(vt + from);
+      ks[u] = kt[st];
+      vs[u] = vt[st];
+    }
+#pragma unroll
+    for (int u = 0; u < CR_ROWS; ++u) {
+      const int64_t t = t0 + u * STEP;
+      if (t >= a.tokens) continue;
+      if (page[u] < 0) k[u] = v[u] = ks[u] = vs[u] = 0;
+      Vals<E> x;
+      values_of(k[u], ks[u], x.x);
+      x.store(K + t * a.k_row);
+      values_of(v[u], vs[u], x.x);
+      x.store(V + t * a.v_row);
+    }
+  }
+}
+
+template <bool APPEND>
+hipError_t launch_rows(const CacheRowsArgs& a, int dtype, hipStream_t s) {
+  void (*kernel)(CacheRowsArgs, int) =
+      a.c.head_dim == 64 ? (dtype == 0 ? cache_rows_kernel<__bf16, 64, APPEND> : cache_rows_kernel<float, 64, APPEND>)
+                         : (dtype == 0 ? cache_rows_kernel<__bf16, 128, APPEND> : cache_rows_kernel<float, 128, APPEND>);
+  const int step = CR_NT / (a.c.head_dim / CR_VALS) * CR_ROWS;
+  int tiles = (a.tokens + step - 1) / step;
+  CacheRowsArgs args = a;
+  void* params[] = {&args, &tiles};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)(tiles * a.c.kv_heads)), dim3(CR_NT),
+                         params, 0, s);
+}
+
+// ------------------------------------------------------------------ tables
+
+constexpr int UP_NT = 1024, UP_WAVES = UP_NT / 64;
+
+// Sums of `mine` over the threads before this one, from `base` on; base grows by
+// all of them.  Counts stop at 2^30 (no pool has as many pages).
+__device__ __forceinline__ int count_up(int a, int b) { return min(a + b, 1 << 30); }
+__device__ __forceinline__ int place_of(int mine, int& base, int (&sums)[2][UP_WAVES], int& turn) {
+  const int lane = lane_id(), w = wave_id();
+  int incl = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(incl, o);
+    if (lane >= o) incl = count_up(incl, v);
+  }
+  int excl = __shfl_up(incl, 1);
+  if (lane == 0) excl = 0;
+  auto& m = sums[turn];
+  turn ^= 1;
+  if (lane == 63) m[w] = incl;
+  __syncthreads();
+  int at = base;
+#pragma unroll
+  for (int x = 0; x < UP_WAVES; ++x) {
+    if (x < w) at = count_up(at, m[x]);
+    base = count_up(base, m[x]);
+  }
+  return count_up(at, excl);
+}
+
+// Whether this workgroup is the last of the launch to come here; what the others
+// wrote before can be read then.
+__device__ __forceinline__ bool last_to_arrive(int32_t* arrived) {
+  __shared__ int last;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) last = atomicAdd(arrived, 1) == (int)gridDim.x - 1;
+  __syncthreads();
+  if (last) __threadfence();
+  return last != 0;
+}
+
+__global__ __launch_bounds__(256) void clear_kernel(CacheUpdateArgs a) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < UPDATE_MARKS) a.marks[i] = 0;
+  if (i >= a.c.pages) return;
+  a.holders[i] = 0;
+  if (a.parents) {
+    a.writers[i] = 0;
+    a.lowest[i] = INT32_MAX;
+  }
+}
+
+__device__ __forceinline__ int row_length(const CacheUpdateArgs& a, int row) {
+  return row < 0 || row >= a.t.rows ? 0 : a.lengths[row];
+}
+__device__ __forceinline__ RowPlan plan_of(const CacheUpdateArgs& a, int r) {
+  return plan_row(row_length(a, a.parents[r]), a.counts[r], a.t.width, a.c.shift);
+}
+// The page that a row which `writes` has in part filled, or -1.
+__device__ __forceinline__ int last_page(const CacheUpdateArgs& a, int r, const RowPlan& p) {
+  return p.writes ? page_of(a.c, a.t, a.parents[r], p.old) : -1;
+}
+__device__ __forceinline__ bool row_copies(const CacheUpdateArgs& a, int r, int last) {
+  return last >= 0 && copies(a.holders[last], a.writers[last], a.lowest[last], r);
+}
+
+// A workgroup per row: the entries that stay, and who holds what.  The last one
+// then finds the pages that rows need among those that no row holds.
+__global__ __launch_bounds__(UP_NT) void update_tables_kernel(CacheUpdateArgs a) {
+  __shared__ int sums[2][UP_WAVES];
+  const int t = threadIdx.x, lane = lane_id(), w = wave_id();
+  {
+    const int r = blockIdx.x, parent = a.parents[r];
+    const RowPlan p = plan_of(a, r);
+    int32_t* const out = a.table_out + r * a.out_stride;
+    const int32_t* const in = a.t.ids + (p.old ? parent : 0) * a.t.stride;
+    for (int i = t; i < a.t.width; i += UP_NT) {
+      int id = -1;
+      if (i < p.kept) {
+        id = in[i];
+        if (id >= 0 && id < a.c.pages) atomicAdd(a.holders + id, 1);
+      }
+      out[i] = id;
+    }
+    if (t == 0) {
+      const int last = last_page(a, r, p);
+      if (last >= 0) {
+        atomicAdd(a.writers + last, 1);
+        atomicMin(a.lowest + last, r);
+      }
+    }
+  }
+  if (!last_to_arrive(a.marks)) return;
+  // ---- pages needed before each row
+  int turn = 0, needed = 0;
+  for (int r0 = 0; r0 < a.rows_out; r0 += UP_NT) {
+    const int r = r0 + t;
+    int need = 0;
+    if (r < a.rows_out) {
+      const RowPlan p = plan_of(a, r);
+      need = p.grown + (row_copies(a, r, last_page(a, r, p)) ? 1 : 0);
+    }
+    const int at = place_of(need, needed, sums, turn);
+    if (r < a.rows_out) a.before[r] = at;
+  }
+  // ---- as many free pages, the lowest first
+  const int want = min(needed, a.c.pages);
+  int found = 0;
+  for (int p0 = 0; p0 < a.c.pages && found < want; p0 += 4 * UP_NT) {
+    int32_t h[4];
+    int mine = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int p = p0 + 4 * t + e;
+      h[e] = p < a.c.pages ? a.holders[p] : 1;
+      mine += h[e] == 0 ? 1 : 0;
+    }
+    int at = place_of(mine, found, sums, turn);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (h[e] == 0) a.free_list[at++] = p0 + 4 * t + e;
+  }
+  __syncthreads();
+  // ---- to the rows that can have all of theirs, a wave to a row
+  for (int r = w; r < a.rows_out; r += UP_WAVES) {
+    const RowPlan p = plan_of(a, r);
+    const int last = last_page(a, r, p), copy = row_copies(a, r, last) ? 1 : 0;
+    const int need = p.grown + copy, at = a.before[r];
+    const bool done = need == 0 || count_up(at, need) <= found;
+    int32_t* const out = a.table_out + r * a.out_stride;
+    if (done)
+      for (int i = lane; i < p.grown; i += 64) out[p.kept + i] = a.free_list[at + copy + i];
+    if (lane == 0) {
+      const int to = done && copy ? a.free_list[at] : -1;
+      if (to >= 0) out[p.old >> a.c.shift] = to;
+      a.source[r] = last;
+      a.target[r] = to;
+      a.lengths_out[r] = done ? p.wanted : p.old;
+      a.missing[r] = !p.fits ? -1 : done ? 0 : need;
+    }
+  }
+}
+
+// Rows' pages are marked; the last workgroup pairs those in use behind the first
+// `used` with the free ones among these.
+__global__ __launch_bounds__(UP_NT) void compact_plan_kernel(CacheUpdateArgs a) {
+  __shared__ int sums[2][UP_WAVES];
+  const int t = threadIdx.x;
+  {
+    const int r = blockIdx.x;
+    const RowPlan p = plan_row(row_length(a, r), 0, a.t.width, a.c.shift);
+    const int32_t* const in = a.t.ids + r * a.t.stride;
+    for (int i = t; i < p.kept; i += UP_NT) {
+      const int id = in[i];
+      if (id >= 0 && id < a.c.pages) atomicOr(a.holders + id, 1);
+    }
+  }
+  if (!last_to_arrive(a.marks)) return;
+  int turn = 0, used = 0;
+  for (int p0 = 0; p0 < a.c.pages; p0 += 4 * UP_NT) {
+    int mine = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int p = p0 + 4 * t + e;
+      mine += p < a.c.pages && a.holders[p] ? 1 : 0;
+    }
+    place_of(mine, used, sums, turn);
+  }
+  // free pages below `used`, then pages in use from there on: as many
+  int holes = 0, moves = 0;
+  for (int p0 = 0; p0 < a.c.pages; p0 += UP_NT) {
+    const int p = p0 + t;
+    const bool in_use = p < a.c.pages && a.holders[p] != 0;
+    const bool hole = p < used && !in_use, move = p >= used && in_use;
+    const int h = place_of(hole ? 1 : 0, holes, sums, turn), m = place_of(move ? 1 : 0, moves, sums, turn);
+    if (hole) a.target[h] = p;
+    if (move) a.source[m] = p;
+  }
+  __syncthreads();
+  for (int p = t; p < a.c.pages; p += UP_NT) a.lowest[p] = p;
+  __syncthreads();
+  for (int m = t; m < moves; m += UP_NT) a.lowest[a.source[m]] = a.target[m];
+  if (t == 0) {
+    a.marks[1] = moves;
+    a.missing[0] = used;
+  }
+}
+
+constexpr int CP_NT = 256, CP_LOADS = 4, CP_CHUNK = CP_NT * CP_LOADS * 16;
+
+// Copies page source[i] to page target[i] (none where that is negative) of every
+// layer, i < `pairs` (COMPACT: as many as were found; then the tables too).
+template <bool COMPACT>
+__global__ __launch_bounds__(CP_NT) void copy_pages_kernel(CacheUpdateArgs a, int chunks) {
+  const int t = threadIdx.x;
+  const int64_t bytes = page_bytes(a.c), layer = bytes * a.c.pages;
+  const int pairs = COMPACT ? a.marks[1] : a.rows_out;
+  const int64_t items = (int64_t)pairs * a.layers * chunks;
+  for (int64_t x = blockIdx.x; x < items; x += gridDim.x) {
+    const int chunk = (int)(x % chunks), l = (int)(x / chunks % a.layers), i = (int)(x / chunks / a.layers);
+    const int to = a.target[i];
+    if (to < 0) continue;
+    const uint8_t* const from = a.cache + l * layer + a.source[i] * bytes;
+    uint8_t* const dst = a.cache + l * layer + to * bytes;
+    const int64_t at = (int64_t)chunk * CP_CHUNK + 16 * t;
+    u32x4 v[CP_LOADS];
+#pragma unroll
+    for (int u = 0; u < CP_LOADS; ++u)
+      if (at + u * CP_NT * 16 < bytes) v[u] = *reinterpret_cast<const u32x4*>(from + at + u * CP_NT * 16);
+#pragma unroll
+    for (int u = 0; u < CP_LOADS; ++u)
+      if (at + u * CP_NT * 16 < bytes) *reinterpret_cast<u32x4*>(dst + at + u * CP_NT * 16) = v[u];
+  }
+  if constexpr (COMPACT) {
+    for (int r = blockIdx.x; r < a.t.rows; r += gridDim.x) {
+      const int kept = plan_row(row_length(a, r), 0, a.t.width, a.c.shift).kept;
+      for (int i = t; i < a.t.width; i += CP_NT) {
+        int id = -1;
+        if (i < kept) {
+          id = a.t.ids[r * a.t.stride + i];
+          if (id >= 0 && id < a.c.pages) id = a.lowest[id];
+        }
+        a.table_out[r * a.out_stride + i] = id;
+      }
+    }
+  }
+}
+
+template <bool COMPACT>
+hipError_t launch_copies(const CacheUpdateArgs& a, int64_t pairs, hipStream_t s) {
+  int chunks = (int)((page_bytes(a.c) + CP_CHUNK - 1) / CP_CHUNK);
+  int64_t wgs = pairs * a.layers * chunks;
+  if (COMPACT && wgs < a.t.rows) wgs = a.t.rows;
+  if (wgs > 4096) wgs = 4096;
+  CacheUpdateArgs args = a;
+  void* params[] = {&args, &chunks};
+  return hipLaunchKernel(reinterpret_cast<const void*>(copy_pages_kernel<COMPACT>), dim3((unsigned)wgs), dim3(CP_NT),
+                         params, 0, s);
+}
+
+hipError_t launch_clear(const CacheUpdateArgs& a, hipStream_t s) {
+  return launch_kernel(clear_kernel, dim3((unsigned)((a.c.pages + 255) / 256)), dim3(256), s, a);
+}
+
+}  // namespace
+
+hipError_t launch_cache_append(const CacheRowsArgs& a, int dtype, hipStream_t s) { return launch_rows<true>(a, dtype, s); }
+hipError_t launch_cache_read(const CacheRowsArgs& a, int dtype, hipStream_t s) { return launch_rows<false>(a, dtype, s); }
+
+hipError_t launch_cache_update(const CacheUpdateArgs& a, hipStream_t s) {
+  hipError_t e = launch_clear(a, s);
+  if (e == hipSuccess) e = launch_kernel(update_tables_kernel, dim3((unsigned)a.rows_out), dim3(UP_NT), s, a);
+  return e == hipSuccess ? launch_copies<false>(a, a.rows_out, s) : e;
+}
+
+hipError_t launch_cache_compact(const CacheUpdateArgs& a, hipStream_t s) {
+  hipError_t e = launch_clear(a, s);
+  if (e == hipSuccess) e = launch_kernel(compact_plan_kernel, dim3((unsigned)a.t.rows), dim3(UP_NT), s, a);
+  return e == hipSuccess ? launch_copies<true>(a, a.c.pages / 2 + 1, s) : e;
+}
+
+}  // namespace ea

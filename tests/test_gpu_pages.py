@@ -1,0 +1,303 @@
+"""A cache in pages and in 4 bits on the GPU: rows in and out, and its tables."""
+import random
+
+import pytest
+
+torch = pytest.importorskip("torch")
+from tests import pages_util as pu  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+ea = None
+I32, BF, F32 = torch.int32, torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def library():
+    global ea
+    import paper_2502_12082_amd
+    ea = paper_2502_12082_amd
+
+
+def rows_of(n, hk, d, dtype, seed):
+    """Keys and values with what rounding can meet: magnitudes from 2^-126 to 2^127,
+    ties, zeros, subnormals, blocks at the borders of scales, not finite ones."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(2, n, hk, d, generator=g, dtype=torch.float64)
+    x = x * torch.exp2(torch.randint(-6, 6, (2, n, hk, d // 32), generator=g).double()).repeat_interleave(32, -1)
+    blocks = x.unflatten(-1, (-1, 32)).flatten(0, -2)
+    ties = torch.tensor([7.0, 5.0, -5.0, 0.25, -0.25, 0.75, 1.25, 1.75, 2.5, 3.5, -0.0, 6.5, 4.5, 1e-3])
+    for i in range(blocks.shape[0]):
+        kind = i % 11
+        if kind == 1:
+            blocks[i, :14] = ties
+            blocks[i, 14:] = 0.0
+            blocks[i] *= 2.0 ** ((i * 37) % 240 - 120)
+        if kind == 3:
+            blocks[i] *= 2.0 ** -127 / 3
+        if kind == 5:
+            blocks[i] = 0.0
+        if kind == 7:
+            blocks[i, 3] = 7.03125 * 2.0 ** (i % 9)
+        if kind == 9 and i % 2:
+            blocks[i, i % 32] = (float("inf"), float("-inf"), float("nan"))[i % 3]
+        if kind == 10:
+            blocks[i, 0] = 3.2e38
+    return x.to(dtype)
+
+
+def same(got, want):
+    got, want = got.double().cpu(), want.double()
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(torch.nan_to_num(got, 0.0), torch.nan_to_num(want, 0.0))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n,hk,d,page", [(1, 1, 64, 16), (2, 8, 128, 16), (37, 3, 64, 32), (65, 2, 128, 64), (130, 1, 128, 256),
+                                         (33, 5, 128, 1024), (300, 4, 64, 16)])
+def test_append_and_read(n, hk, d, page, dtype):
+    rng = random.Random(n * 7 + page)
+    lengths = [max(1, n // 3), n, 5]
+    table, pages = pu.shuffled_table(lengths, page, 3, n)
+    table[0, 0] = pages  # (row 0 loses its first page: its tokens there have no place)
+    places = [(r, p) for r, m in enumerate(lengths) for p in range(m)]
+    places = rng.sample(places, min(n, len(places)))
+    places += [(0, -1), (-1, 0), (3, 0), (1, page * table.shape[1]), (2 ** 31 - 1, 2 ** 31 - 1), (-2 ** 31, 3), (1, -2 ** 31)]
+    rng.shuffle(places)
+    rows, positions = (torch.tensor(v, dtype=I32) for v in zip(*places))
+    x = rows_of(len(places), hk, d, dtype, n + page)
+    # parts of one projection's rows
+    fused = torch.zeros(len(places), 4, hk, d, dtype=dtype)
+    fused[:, 1], fused[:, 2] = x[0], x[1]
+    fused = fused.cuda()
+    cache = torch.full((pages, hk, 2, page // 16, 17 * d // 2), 0xA5, dtype=torch.uint8)
+    got = cache.cuda()
+    ea.cache_append(got, fused[:, 1], fused[:, 2], rows.cuda(), positions.cuda(), table.cuda())
+    code, scale = pu.pack(x)
+    held = []
+    for i, (r, p) in enumerate(places):
+        ok = 0 <= r < 3 and 0 <= p < page * table.shape[1] and 0 <= int(table[r, p // page]) < pages
+        held.append(ok)
+        for h in range(hk if ok else 0):
+            for w in (0, 1):
+                pu.put(cache, int(table[r, p // page]), p % page, h, w, code[w, i, h], scale[w, i, h])
+    # (codes under a NaN scale say nothing)
+    same(pu.values(got), pu.values(cache))
+    bad = (scale == 255).any()
+    if not bad:
+        assert torch.equal(got.cpu(), cache)
+    want = pu.unpack(code, scale) * torch.tensor(held).view(1, -1, 1, 1)
+    want = torch.where(torch.tensor(held).view(1, -1, 1, 1), pu.unpack(code, scale), 0.0)
+    for out in (BF, F32):
+        k, v = ea.cache_read(got, rows.cuda(), positions.cuda(), table.cuda(), dtype=out)
+        assert k.dtype == out
+        same(k, want[0])
+        same(v, want[1])
+    # into parts of wider rows, the rest of which stays
+    wide = torch.full((len(places), 3, hk, d), 7.0, dtype=dtype, device="cuda")
+    ea.cache_read(got, rows.cuda(), positions.cuda(), table.cuda(), dtype=dtype, k_out=wide[:, 2], v_out=wide[:, 0])
+    same(wide[:, 2], want[0])
+    same(wide[:, 0], want[1])
+    assert (wide[:, 1] == 7).all()
+
+
+def test_no_tokens():
+    cache = torch.zeros(2, 1, 2, 1, 544, dtype=torch.uint8, device="cuda")
+    none, table = torch.zeros(0, dtype=I32, device="cuda"), torch.zeros(1, 2, dtype=I32, device="cuda")
+    x = torch.zeros(0, 1, 64, dtype=BF, device="cuda")
+    ea.cache_append(cache, x, x, none, none, table)
+    assert ea.cache_read(cache, none, none, table)[0].shape == (0, 1, 64)
+    out = ea.cache_update(cache, table, torch.zeros(1, dtype=I32, device="cuda"), none, none)
+    assert out[0].shape == (0, 2) and out[1].shape == (0,)
+
+
+def test_behind_32_bits():
+    """A pool of more than 2^32 bytes, and rows more than 2^31 elements into k."""
+    hk, d, page = 8, 128, 1024
+    pages = (5 << 30) // (page * hk * 136)
+    cache = torch.zeros(pages, hk, 2, page // 16, 1088, dtype=torch.uint8, device="cuda")
+    assert cache.numel() > 1 << 32
+    table = torch.tensor([[pages - 1, 0], [pages - 2, 1]], dtype=I32, device="cuda")
+    rows = torch.tensor([0, 0, 1, 1], dtype=I32, device="cuda")
+    positions = torch.tensor([1023, 1024, 500, 2047], dtype=I32, device="cuda")
+    x = torch.randn(2, 4, hk, d, dtype=F32).to(BF)
+    far = torch.zeros(4, 1 << 30, dtype=BF, device="cuda")
+    k, v = far[:, :hk * d].view(4, hk, d), far[:, hk * d:2 * hk * d].view(4, hk, d)
+    k.copy_(x[0])
+    v.copy_(x[1])
+    ea.cache_append(cache, k, v, rows, positions, table)
+    want = pu.unpack(*pu.pack(x))
+    got = ea.cache_read(cache, rows, positions, table)
+    same(got[0], want[0])
+    same(got[1], want[1])
+    copy = ea.cache_read(cache, rows, positions, table, k_out=k, v_out=v)
+    same(copy[0], want[0])
+    same(copy[1], want[1])
+    held = pu.values(cache[pages - 1:])[0, 1023]
+    assert torch.equal(held[:, 0], want[0, 0])
+
+
+# ------------------------------------------------------------------ tables
+
+def table_case(seed):
+    rng = random.Random(seed)
+    page, width = rng.choice([16, 32, 128]), rng.choice([1, 2, 7, 40, 70])
+    rows = rng.choice([1, 2, 5, 33, 150])
+    lengths = [min(width * page, rng.choice([0, 1, page, page + 1, width * page, width * page - 1, rng.randrange(width * page + 1)]))
+               for _ in range(rows)]
+    need = sum(-(-n // page) for n in lengths)
+    pages = max(1, need + rng.choice([0, 0, 1, 3, rows, 3 * rows]))
+    ids = list(range(pages))
+    rng.shuffle(ids)
+    table, at = [], 0
+    for r, n in enumerate(lengths):
+        m = -(-n // page)
+        if r and rng.random() < 0.4:  # shares a prefix with an earlier row
+            o = rng.randrange(r)
+            both = min(m, -(-lengths[o] // page), rng.randrange(width + 1))
+            row = table[o][:both] + ids[at:at + m - both]
+            at += m - both
+        else:
+            row = ids[at:at + m]
+            at += m
+        table.append(row + [-1] * (width - m))
+    out_rows = rng.choice([1, rows, rows + 3, 2 * rows])
+    parents = [rng.choice([rng.randrange(rows), min(r, rows - 1), rng.randrange(rows), -1]) for r in range(out_rows)]
+    if rng.random() < 0.3:
+        parents = [rng.randrange(rows) if rng.random() < 0.5 else parents[0] for _ in parents]
+    counts = [rng.choice([0, 1, 1, 1, -1, -page, rng.randrange(-50, 200)]) for _ in range(out_rows)]
+    return page, pages, table, lengths, parents, counts
+
+
+def apply_copies(cache, copies):
+    want = cache.clone()
+    for source, to in copies:
+        want[:, to] = cache[:, source]
+    return want
+
+
+def ints(v):
+    return torch.tensor(v, dtype=I32, device="cuda")
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_update(seed):
+    page, pages, table, lengths, parents, counts = table_case(seed)
+    if seed % 6 == 5:  # entries, lengths and parents that say nothing
+        table[0][0] = pages
+        table[-1][-1] = -2 ** 31
+        lengths[-1] = 2 ** 31 - 1
+        lengths[0] = -5 if seed % 12 == 5 else lengths[0]
+        parents[0] = 2 ** 31 - 1
+        parents[-1] = -2 ** 31
+        counts[-1] = 2 ** 31 - 1 if seed % 12 == 5 else -2 ** 31
+    hk, d, layers = seed % 3 + 1, 64 if seed % 2 else 128, seed % 4 + 1
+    g = torch.Generator().manual_seed(seed)
+    cache = torch.randint(0, 256, (layers, pages, hk, 2, page // 16, 17 * d // 2), generator=g).to(torch.uint8)
+    got = cache.cuda()
+    t, l, m, copies = pu.update_by_hand(table, lengths, parents, counts, page, pages)
+    new = ea.cache_update(got, ints(table), ints(lengths), ints(parents), ints(counts))
+    assert new[0].tolist() == t
+    assert new[1].tolist() == l
+    assert new[2].tolist() == m
+    assert torch.equal(got.cpu(), apply_copies(cache, copies))
+    # the same again (copies go to pages that were free), into given tensors, parts of wider ones
+    wide = torch.full((len(parents), len(t[0]) + 3), 77, dtype=I32, device="cuda")
+    other = [torch.empty(len(parents), dtype=I32, device="cuda") for _ in range(2)]
+    ws = torch.full((ea.cache_workspace(got, len(parents)),), 0xEE, dtype=torch.uint8, device="cuda")
+    table_in = torch.full((len(table), len(table[0]) + 5), 1, dtype=I32, device="cuda")
+    table_in[:, 2:-3] = ints(table)
+    ea.cache_update(got if layers > 1 else got[0], table_in[:, 2:-3], ints(lengths), ints(parents), ints(counts),
+                    wide[:, 1:-2], *other, workspace=ws)
+    assert wide[:, 1:-2].tolist() == t and other[0].tolist() == l and other[1].tolist() == m
+    assert (wide[:, 0] == 77).all() and (wide[:, -2:] == 77).all()
+    assert torch.equal(got.cpu(), apply_copies(cache, copies))
+
+
+def test_update_copies_only_what_is_written():
+    """Rows that share a page in part filled: idle rows, and rows cut back into it."""
+    page, table = 16, [[0, 1], [0, 1], [0, 1], [0, 2]]
+    cases = [
+        # all go on: the lowest keeps page 1
+        ([20, 20, 20, 20], [0, 1, 2, 3], [1, 1, 1, 1], [[0, 1], [0, 3], [0, 4], [0, 2]]),
+        # one waits: the others get copies
+        ([20, 20, 20, 20], [0, 1, 2, 3], [0, 1, 1, 1], [[0, 1], [0, 3], [0, 4], [0, 2]]),
+        # a row cut back into page 0, which all hold, goes on there
+        ([10, 20, 20, 20], [0, 1, 2, 3], [1, 0, 0, 0], [[3, -1], [0, 1], [0, 1], [0, 2]]),
+        # cut back only: nothing is written, nothing copied
+        ([20, 20, 20, 20], [0, 1, 2, 3], [-10, 0, 0, 0], [[0, -1], [0, 1], [0, 1], [0, 2]]),
+        # both children of one row write: one copy, to the page that is free
+        ([20, 20, 20, 20], [3, 3], [1, 1], [[0, 2], [0, 1]]),
+    ]
+    for lengths, parents, counts, want in cases:
+        cache = torch.arange(5, dtype=torch.uint8).view(1, 5, 1, 1, 1, 1).expand(1, 5, 1, 2, 1, 544).contiguous().cuda()
+        new, _, missing = ea.cache_update(cache, ints(table), ints(lengths), ints(parents), ints(counts))
+        assert missing.tolist() == [0] * len(parents)
+        assert new.tolist() == want
+        byte = cache[0, :, 0, 0, 0, 0].tolist()
+        for row, parent in zip(want, parents):
+            for a, b in zip(row, table[parent]):
+                assert a < 0 or byte[a] == b
+
+
+def test_update_of_a_long_pool():
+    """Free pages found behind many used ones, more rows than threads, a long growth."""
+    page, pages, rows, width = 16, 20000, 1500, 4096
+    table = torch.full((rows, width), -1, dtype=I32)
+    ids = torch.randperm(pages, generator=torch.Generator().manual_seed(1))
+    lengths = [1 + (7 * r) % 300 for r in range(rows)]
+    at = 0
+    for r, n in enumerate(lengths):
+        m = -(-n // page)
+        table[r, :m] = ids[at:at + m].int()
+        at += m
+    parents = [(r * 11) % rows for r in range(rows)]
+    counts = [1 + r % 3 for r in range(rows)]
+    counts[700] = 65536 - 300  # (4000 pages)
+    counts[701] = 65537
+    cache = torch.randint(0, 256, (1, pages, 1, 2, 1, 544), dtype=torch.uint8)
+    got = cache.cuda()
+    t, l, m, copies = pu.update_by_hand(table.tolist(), lengths, parents, counts, page, pages)
+    assert -1 in m and len(copies) == 0
+    new = ea.cache_update(got, table.cuda(), ints(lengths), ints(parents), ints(counts))
+    assert new[0].tolist() == t and new[1].tolist() == l and new[2].tolist() == m
+    assert torch.equal(got.cpu(), cache)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_compact(seed):
+    page, pages, table, lengths, _, _ = table_case(seed + 100)
+    pages += seed % 4 * 40  # (holes)
+    rng = random.Random(seed)
+    to = list(range(pages))
+    rng.shuffle(to)
+    table = [[to[p] if p >= 0 else p for p in row] for row in table]
+    if seed % 6 == 5:
+        table[0][0], lengths[-1] = pages + 3, 2 ** 31 - 1
+        table[-1] = [p if p >= 0 else -7 for p in table[-1]]
+    layers, hk, d = seed % 3 + 1, 2, 64 if seed % 2 else 128
+    cache = torch.randint(0, 256, (layers, pages, hk, 2, page // 16, 17 * d // 2),
+                          generator=torch.Generator().manual_seed(seed)).to(torch.uint8)
+    t, used, moves = pu.compact_by_hand(table, lengths, page, pages)
+    for _ in range(2):  # (sources are not written: again the same)
+        got = cache.cuda()
+        new, count = ea.cache_compact(got, ints(table), ints(lengths))
+        assert count.tolist() == [used] and new.tolist() == t
+        assert torch.equal(got.cpu(), apply_copies(cache, moves))
+    out = torch.empty_like(new), torch.empty_like(count)
+    ea.cache_compact(got, ints(table), ints(lengths), *out)
+    assert out[0].tolist() == t and out[1].tolist() == [used]
+    # what is compact stays
+    again, count = ea.cache_compact(got, new, ints(lengths))
+    assert again.tolist() == t and count.tolist() == [used]
+
+
+def test_compact_of_a_long_pool():
+    pages, width = 9000, 600
+    ids = torch.randperm(pages, generator=torch.Generator().manual_seed(2))[:8 * 600].view(8, 600).int()
+    lengths = [16 * 600 - 100 * r for r in range(8)]
+    cache = torch.randint(0, 256, (2, pages, 1, 2, 1, 544), dtype=torch.uint8)
+    t, used, moves = pu.compact_by_hand(ids.tolist(), lengths, 16, pages)
+    got = cache.cuda()
+    new, count = ea.cache_compact(got, ids.cuda(), ints(lengths))
+    assert count.tolist() == [used] and new.tolist() == t and len(moves) > 1000
+    assert torch.equal(got.cpu(), apply_copies(cache, moves))
