@@ -482,9 +482,8 @@ typedef struct {
   int32_t pages, page_size, kv_heads, head_dim; /* head_dim in {64, 128} */
 } ea_cache;
 typedef struct {
-  const int32_t* pages; /* [rows, width], rows `stride` elements apart */
-  int32_t rows, width;  /* width * page_size <= 131072 */
-  int64_t stride;
+  int32_t rows, width; /* int32 [rows, width], rows `stride` elements apart; */
+  int64_t stride;      /* width * page_size <= 131072 */
 } ea_page_table;
 ea_status entmax_cache_page_bytes(const ea_cache* c, size_t* bytes);
 
@@ -500,12 +499,12 @@ ea_status entmax_cache_page_bytes(const ea_cache* c, size_t* bytes);
  * Read: the same rows' values (exact in both types), 0 where there is no page.
  * tokens may be 0.  One launch each.
  */
-ea_status entmax_cache_append(const ea_cache* c, void* cache, const ea_page_table* table, int32_t tokens,
-                              int32_t dtype, const int32_t* rows, const int32_t* positions, const void* k,
+ea_status entmax_cache_append(const ea_cache* c, void* cache, const ea_page_table* t,
+                              const int32_t* table, int32_t tokens, int32_t dtype, const int32_t* rows, const int32_t* positions, const void* k,
                               const ea_strides* k_strides, const void* v, const ea_strides* v_strides,
                               void* stream);
-ea_status entmax_cache_read(const ea_cache* c, const void* cache, const ea_page_table* table, int32_t tokens,
-                            int32_t dtype, const int32_t* rows, const int32_t* positions, void* k,
+ea_status entmax_cache_read(const ea_cache* c, const void* cache, const ea_page_table* t,
+                            const int32_t* table, int32_t tokens, int32_t dtype, const int32_t* rows, const int32_t* positions, void* k,
                             const ea_strides* k_strides, void* v, const ea_strides* v_strides, void* stream);
 
 /*
@@ -529,16 +528,17 @@ ea_status entmax_cache_read(const ea_cache* c, const void* cache, const ea_page_
  * its length) from number `used` on, their count, move to the free ones below, in
  * order; table_out [table rows, width] names the new places, and used is 1 number.
  * workspace: entmax_cache_workspace bytes for as many rows (rows_out), 16-byte aligned.
- * rows_out may be 0.  Three launches each.
+ * rows_out may be 0.  Two launches each, or four: with more than 1024 rows, 2^18
+ * entries or 2^17 pages.
  */
 ea_status entmax_cache_workspace(const ea_cache* c, int32_t rows, size_t* bytes);
-ea_status entmax_cache_update(const ea_cache* c, int32_t layers, void* cache, const ea_page_table* table,
-                              const int32_t* lengths, int32_t rows_out, const int32_t* parents,
+ea_status entmax_cache_update(const ea_cache* c, int32_t layers, void* cache, const ea_page_table* t,
+                              const int32_t* table, const int32_t* lengths, int32_t rows_out, const int32_t* parents,
                               const int32_t* counts, int32_t* table_out, int64_t out_stride,
                               int32_t* lengths_out, int32_t* missing, void* workspace, size_t ws_bytes,
                               void* stream);
-ea_status entmax_cache_compact(const ea_cache* c, int32_t layers, void* cache, const ea_page_table* table,
-                               const int32_t* lengths, int32_t* table_out, int64_t out_stride, int32_t* used,
+ea_status entmax_cache_compact(const ea_cache* c, int32_t layers, void* cache, const ea_page_table* t,
+                               const int32_t* table, const int32_t* lengths, int32_t* table_out, int64_t out_stride, int32_t* used,
                                void* workspace, size_t ws_bytes, void* stream);
 
 /*
@@ -563,7 +563,7 @@ typedef struct {
 } ea_paged_shape;
 ea_status entmax_paged_decode_workspace(const ea_paged_shape* shape, const ea_cache* c, size_t* bytes);
 ea_status entmax_paged_decode(const ea_paged_shape* shape, const ea_params* params, const ea_cache* c,
-                              const void* cache, const ea_page_table* table, const void* q,
+                              const void* cache, const ea_page_table* t, const int32_t* table, const void* q,
                               const ea_strides* q_strides, const int32_t* lengths, const int32_t* rows, void* o,
                               const ea_strides* o_strides, void* workspace, size_t ws_bytes, void* stream);
 

@@ -1365,8 +1365,7 @@ class Cache(ctypes.Structure):
 
 
 class PageTable(ctypes.Structure):
-    _fields_ = [("pages", ctypes.c_void_p), ("rows", ctypes.c_int32), ("width", ctypes.c_int32),
-                ("stride", ctypes.c_int64)]
+    _fields_ = [("rows", ctypes.c_int32), ("width", ctypes.c_int32), ("stride", ctypes.c_int64)]
 
 
 class PagedShape(ctypes.Structure):
@@ -1375,17 +1374,33 @@ class PagedShape(ctypes.Structure):
 
 for _name, _args in (
         ("entmax_cache_page_bytes", [_P(Cache), _P(_sz)]),
-        ("entmax_cache_append", [_P(Cache), _v, _P(PageTable), _i32, _i32, _v, _v, _v, _P(Strides), _v, _P(Strides),
+        ("entmax_cache_append", [_P(Cache), _v, _P(PageTable), _v, _i32, _i32, _v, _v, _v, _P(Strides), _v, _P(Strides),
                                  _v]),
-        ("entmax_cache_read", [_P(Cache), _v, _P(PageTable), _i32, _i32, _v, _v, _v, _P(Strides), _v, _P(Strides), _v]),
+        ("entmax_cache_read", [_P(Cache), _v, _P(PageTable), _v, _i32, _i32, _v, _v, _v, _P(Strides), _v, _P(Strides),
+                               _v]),
         ("entmax_cache_workspace", [_P(Cache), _i32, _P(_sz)]),
-        ("entmax_cache_update", [_P(Cache), _i32, _v, _P(PageTable), _v, _i32, _v, _v, _v, _i64, _v, _v, _v, _sz, _v]),
-        ("entmax_cache_compact", [_P(Cache), _i32, _v, _P(PageTable), _v, _v, _i64, _v, _v, _sz, _v]),
+        ("entmax_cache_update", [_P(Cache), _i32, _v, _P(PageTable), _v, _v, _i32, _v, _v, _v, _i64, _v, _v, _v, _sz,
+                                 _v]),
+        ("entmax_cache_compact", [_P(Cache), _i32, _v, _P(PageTable), _v, _v, _v, _i64, _v, _v, _sz, _v]),
         ("entmax_paged_decode_workspace", [_P(PagedShape), _P(Cache), _P(_sz)]),
-        ("entmax_paged_decode", [_P(PagedShape), _P(Params), _P(Cache), _v, _P(PageTable), _v, _P(Strides), _v, _v, _v,
-                                 _P(Strides), _v, _sz, _v])):
+        ("entmax_paged_decode", [_P(PagedShape), _P(Params), _P(Cache), _v, _P(PageTable), _v, _v, _P(Strides), _v, _v,
+                                 _v, _P(Strides), _v, _sz, _v])):
     getattr(_lib, _name).argtypes = _args
     getattr(_lib, _name).restype = ctypes.c_int
+
+# What a call's checks gave for tensors of these shapes, strides, types and devices: at
+# the sizes of a decoding step the checks take longer than the kernels (an append of 64
+# tokens 13 us of host time with them, 8 without).  Nothing here depends on
+# what a tensor holds or where it lies; addresses are checked at each call.
+_checked = {}
+
+
+def _remember(key, value):
+    if key is not None:
+        if len(_checked) >= 1024:
+            _checked.clear()
+        _checked[key] = value
+    return value
 
 
 @functools.lru_cache(maxsize=256)
@@ -1445,10 +1460,15 @@ def _table(table, c, device, name="table"):
         raise ValueError("%s must be contiguous in its last dimension" % name)
     if width * c.page_size > MAX_SEQLEN:
         raise ValueError("%s holds %d tokens a row, at most %d are possible" % (name, width * c.page_size, MAX_SEQLEN))
-    return PageTable(table.data_ptr(), rows, width, _stride(table, 0))
+    return _page_table_of(rows, width, _stride(table, 0))
 
 
-def _places(cache, rows, positions, table):
+@functools.lru_cache(maxsize=256)
+def _page_table_of(rows, width, stride):
+    return PageTable(rows, width, stride)
+
+
+def _check_places(cache, rows, positions, table):
     c = _layer(cache)
     t = _table(table, c, cache.device)
     if not isinstance(rows, torch.Tensor) or rows.dim() != 1:
@@ -1458,6 +1478,18 @@ def _places(cache, rows, positions, table):
     return c, t
 
 
+def _check_append(cache, k, v, rows, positions, table):
+    c, t = _check_places(cache, rows, positions, table)
+    shape = (rows.shape[0], c.kv_heads, c.head_dim)
+    if not isinstance(k, torch.Tensor):
+        raise ValueError("k must be a torch tensor")
+    dt = _ea_dtype(k, "k")
+    _strided(k, "k", shape, k.dtype, cache.device)
+    _strided(v, "v", shape, k.dtype, cache.device)
+    _on_gpu(cache.device)
+    return c, t, shape[0], dt, _row_head(k), _row_head(v)
+
+
 def cache_append(cache, k, v, rows, positions, table):
     """Writes keys and values k, v [tokens, kv_heads, head_dim] (bf16 or fp32, any strides
     with a contiguous last dimension) into a layer's cache, rounded to 4 bits: token
@@ -1465,40 +1497,66 @@ def cache_append(cache, k, v, rows, positions, table):
     Tokens without a place (a negative position, no such row, no page) are left
     out.  Two tokens of one call must not have the same place, and rows that share
     a page must not write to it (cache_update gives them pages of their own)."""
-    c, t = _places(cache, rows, positions, table)
-    shape = (rows.shape[0], c.kv_heads, c.head_dim)
-    if not isinstance(k, torch.Tensor):
-        raise ValueError("k must be a torch tensor")
-    dt, dev = _ea_dtype(k, "k"), cache.device
-    _strided(k, "k", shape, k.dtype, dev)
-    _strided(v, "v", shape, k.dtype, dev)
-    _on_gpu(dev)
+    try:
+        dev = cache.device
+        key = ("append", dev, cache.shape, cache.stride(), cache.dtype, k.shape, k.stride(), k.dtype, k.device, v.shape,
+               v.stride(), v.dtype, v.device, rows.shape, rows.stride(), rows.dtype, rows.device, positions.shape,
+               positions.stride(), positions.dtype, positions.device, table.shape, table.stride(), table.dtype,
+               table.device)
+        args = None if (cache.data_ptr() | k.data_ptr() | v.data_ptr()) & 15 else _checked.get(key)
+    except (AttributeError, TypeError):
+        key = args = None
+    c, t, tokens, dt, ks, vs = args or _remember(key, _check_append(cache, k, v, rows, positions, table))
     with _on_device(dev):
-        _check(_lib.entmax_cache_append(c, cache.data_ptr(), t, shape[0], dt, rows.data_ptr(), positions.data_ptr(),
-                                        k.data_ptr(), _row_head(k), v.data_ptr(), _row_head(v), _stream_handle(dev)),
+        _check(_lib.entmax_cache_append(c, cache.data_ptr(), t, table.data_ptr(), tokens, dt, rows.data_ptr(),
+                                        positions.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs, _stream_handle(dev)),
                "entmax_cache_append")
 
 
-def cache_read(cache, rows, positions, table, dtype=torch.bfloat16, k_out=None, v_out=None):
-    """(k, v) [tokens, kv_heads, head_dim]: the values that a layer's cache holds for the
-    tokens positions[i] of the table's rows rows[i], 0 where there is no page.
-    dtype: bfloat16 or float32, exact in both.  k_out, v_out: tensors to write."""
-    c, t = _places(cache, rows, positions, table)
+def _check_read(cache, rows, positions, table, dtype, k_out, v_out):
+    c, t = _check_places(cache, rows, positions, table)
     shape, dev = (rows.shape[0], c.kv_heads, c.head_dim), cache.device
     if dtype not in (torch.bfloat16, torch.float32):
         raise ValueError("dtype must be bfloat16 or float32, not %s" % dtype)
     for name, out in (("k_out", k_out), ("v_out", v_out)):
         if out is not None:
             _strided(out, name, shape, dtype, dev, written=True)
+            for other_name, other in (("cache", cache), ("table", table), ("rows", rows), ("positions", positions)):
+                if _overlap(out, other):
+                    raise ValueError("%s overlaps %s" % (name, other_name))
     if k_out is not None and v_out is not None and _overlap(k_out, v_out) and not _apart(k_out, v_out):
         raise ValueError("k_out overlaps v_out")
     _on_gpu(dev)
+    return c, t, shape, EA_BF16 if dtype == torch.bfloat16 else EA_F32, _strides_of(c.kv_heads * c.head_dim, c.head_dim)
+
+
+def cache_read(cache, rows, positions, table, dtype=torch.bfloat16, k_out=None, v_out=None):
+    """(k, v) [tokens, kv_heads, head_dim]: the values that a layer's cache holds for the
+    tokens positions[i] of the table's rows rows[i], 0 where there is no page.
+    dtype: bfloat16 or float32, exact in both.  k_out, v_out: tensors to write."""
+    try:
+        dev = cache.device
+        key = ("read", dev, dtype, cache.shape, cache.stride(), cache.dtype, rows.shape, rows.stride(), rows.dtype,
+               rows.device, positions.shape, positions.stride(), positions.dtype, positions.device, table.shape,
+               table.stride(), table.dtype, table.device)
+        # (tensors to write are checked each time: whether they overlap is where they lie)
+        args = None if k_out is not None or v_out is not None or cache.data_ptr() & 15 else _checked.get(key)
+    except (AttributeError, TypeError):
+        key = args = None
+    c, t, shape, dt, strides = args or _remember(key, _check_read(cache, rows, positions, table, dtype, k_out, v_out))
     with _on_device(dev):
-        k_out = torch.empty(shape, dtype=dtype, device=dev) if k_out is None else k_out
-        v_out = torch.empty(shape, dtype=dtype, device=dev) if v_out is None else v_out
-        _check(_lib.entmax_cache_read(c, cache.data_ptr(), t, shape[0], EA_BF16 if dtype == torch.bfloat16 else EA_F32,
-                                      rows.data_ptr(), positions.data_ptr(), k_out.data_ptr(), _row_head(k_out),
-                                      v_out.data_ptr(), _row_head(v_out), _stream_handle(dev)), "entmax_cache_read")
+        ks = vs = strides
+        if k_out is None:
+            k_out = torch.empty(shape, dtype=dtype, device=dev)
+        else:
+            ks = _row_head(k_out)
+        if v_out is None:
+            v_out = torch.empty(shape, dtype=dtype, device=dev)
+        else:
+            vs = _row_head(v_out)
+        _check(_lib.entmax_cache_read(c, cache.data_ptr(), t, table.data_ptr(), shape[0], dt, rows.data_ptr(),
+                                      positions.data_ptr(), k_out.data_ptr(), ks, v_out.data_ptr(), vs,
+                                      _stream_handle(dev)), "entmax_cache_read")
     return k_out, v_out
 
 
@@ -1524,6 +1582,40 @@ def _written(outs, inputs):
                 raise ValueError("%s overlaps %s" % (name, other_name))
 
 
+def _check_table_out(table_out, rows, c, t, dev):
+    if not isinstance(table_out, torch.Tensor) or table_out.shape != (rows, t.width):
+        raise ValueError("table_out must be a %s tensor" % ([rows, t.width],))
+    if rows:
+        _table(table_out, c, dev, "table_out")
+    if rows > 1 and table_out.stride(0) < t.width:
+        raise ValueError("table_out has elements that share memory")
+
+
+def _check_update(cache, table, lengths, parents, counts, table_out, lengths_out, missing_out, workspace):
+    c, layers = _layers(cache)
+    dev = cache.device
+    t = _table(table, c, dev)
+    _need(lengths, "lengths", (t.rows,), torch.int32, dev)
+    if not isinstance(parents, torch.Tensor) or parents.dim() != 1:
+        raise ValueError("parents must be a [rows] tensor")
+    rows = parents.shape[0]
+    _need(parents, "parents", (rows,), torch.int32, dev)
+    _need(counts, "counts", (rows,), torch.int32, dev)
+    if table_out is not None or lengths_out is not None or missing_out is not None:
+        if table_out is None or lengths_out is None or missing_out is None:
+            raise ValueError("table_out, lengths_out and missing_out must be given together")
+        _check_table_out(table_out, rows, c, t, dev)
+        _need(lengths_out, "lengths_out", (rows,), torch.int32, dev)
+        _need(missing_out, "missing_out", (rows,), torch.int32, dev)
+        _written([("table_out", table_out), ("lengths_out", lengths_out), ("missing_out", missing_out)],
+                 [("table", table), ("lengths", lengths), ("parents", parents), ("counts", counts), ("cache", cache)])
+    nbytes = _cache_workspace(cache.shape[-5:], rows)
+    if workspace is not None:
+        _check_bytes(workspace, "workspace", nbytes, dev)
+    _on_gpu(dev)
+    return c, layers, t, rows, nbytes
+
+
 def cache_update(cache, table, lengths, parents, counts, table_out=None, lengths_out=None, missing_out=None,
                  workspace=None):
     """(table_out, lengths_out, missing_out): the table of the next step.  Its row r
@@ -1542,51 +1634,34 @@ def cache_update(cache, table, lengths, parents, counts, table_out=None, lengths
     table_out [rows, width], lengths_out, missing_out [rows]: tensors to write, which
     are not those that the call reads.  workspace: cache_workspace bytes, to keep
     from call to call (one call at a time)."""
-    c, layers = _layers(cache)
-    dev = cache.device
-    t = _table(table, c, dev)
-    _need(lengths, "lengths", (t.rows,), torch.int32, dev)
-    if not isinstance(parents, torch.Tensor) or parents.dim() != 1:
-        raise ValueError("parents must be a [rows] tensor")
-    rows = parents.shape[0]
-    _need(parents, "parents", (rows,), torch.int32, dev)
-    _need(counts, "counts", (rows,), torch.int32, dev)
-    if table_out is not None or lengths_out is not None or missing_out is not None:
-        if table_out is None or lengths_out is None or missing_out is None:
-            raise ValueError("table_out, lengths_out and missing_out must be given together")
-        if rows:
-            _table(table_out, c, dev, "table_out")
-        if table_out.shape != (rows, t.width):
-            raise ValueError("table_out has shape %s, expected %s" % (tuple(table_out.shape), (rows, t.width)))
-        if rows > 1 and table_out.stride(0) < t.width:
-            raise ValueError("table_out has elements that share memory")
-        _need(lengths_out, "lengths_out", (rows,), torch.int32, dev)
-        _need(missing_out, "missing_out", (rows,), torch.int32, dev)
-        _written([("table_out", table_out), ("lengths_out", lengths_out), ("missing_out", missing_out)],
-                 [("table", table), ("lengths", lengths), ("parents", parents), ("counts", counts)])
-    nbytes = _cache_workspace(cache.shape[-5:], rows)
-    if workspace is not None:
-        _check_bytes(workspace, "workspace", nbytes, dev)
-    _on_gpu(dev)
+    given = table_out is not None or lengths_out is not None or missing_out is not None or workspace is not None
+    try:
+        dev = cache.device
+        key = ("update", dev, cache.shape, cache.stride(), cache.dtype, table.shape, table.stride(), table.dtype,
+               table.device, lengths.shape, lengths.stride(), lengths.dtype, lengths.device, parents.shape,
+               parents.stride(), parents.dtype, parents.device, counts.shape, counts.stride(), counts.dtype,
+               counts.device)
+        args = None if given or cache.data_ptr() & 15 else _checked.get(key)
+    except (AttributeError, TypeError):
+        key = args = None
+    c, layers, t, rows, nbytes = args or _remember(key, _check_update(
+        cache, table, lengths, parents, counts, table_out, lengths_out, missing_out, workspace))
     with _on_device(dev):
         if table_out is None:
-            table_out, lengths_out = torch.empty((rows, t.width), dtype=torch.int32, device=dev), torch.empty_like(parents)
-            missing_out = torch.empty_like(parents)
+            table_out = torch.empty((rows, t.width), dtype=torch.int32, device=dev)
+            lengths_out, missing_out = torch.empty_like(parents), torch.empty_like(parents)
         if workspace is None:
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        else:
+            nbytes = workspace.numel() * workspace.element_size()
         _check(_lib.entmax_cache_update(
-            c, layers, cache.data_ptr(), t, lengths.data_ptr(), rows, parents.data_ptr(), counts.data_ptr(),
-            table_out.data_ptr(), max(_stride(table_out, 0), t.width), lengths_out.data_ptr(), missing_out.data_ptr(),
-            workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_handle(dev)),
-            "entmax_cache_update")
+            c, layers, cache.data_ptr(), t, table.data_ptr(), lengths.data_ptr(), rows, parents.data_ptr(),
+            counts.data_ptr(), table_out.data_ptr(), max(_stride(table_out, 0), t.width), lengths_out.data_ptr(),
+            missing_out.data_ptr(), workspace.data_ptr(), nbytes, _stream_handle(dev)), "entmax_cache_update")
     return table_out, lengths_out, missing_out
 
 
-def cache_compact(cache, table, lengths, table_out=None, used_out=None, workspace=None):
-    """(table_out, used_out): the table, its rows of lengths[r] tokens, after all pages in
-    use have moved to the lowest numbers, in every layer; used_out (int32 [1]) is their
-    count, so that pages from there on are free.  Pages that are below it already
-    stay.  table_out, used_out: tensors to write, which are not the call's inputs."""
+def _check_compact(cache, table, lengths, table_out, used_out, workspace):
     c, layers = _layers(cache)
     dev = cache.device
     t = _table(table, c, dev)
@@ -1594,27 +1669,43 @@ def cache_compact(cache, table, lengths, table_out=None, used_out=None, workspac
     if (table_out is None) != (used_out is None):
         raise ValueError("table_out and used_out must be given together")
     if table_out is not None:
-        _table(table_out, c, dev, "table_out")
-        if table_out.shape != table.shape:
-            raise ValueError("table_out has shape %s, expected %s" % (tuple(table_out.shape), tuple(table.shape)))
-        if t.rows > 1 and table_out.stride(0) < t.width:
-            raise ValueError("table_out has elements that share memory")
+        _check_table_out(table_out, t.rows, c, t, dev)
         _need(used_out, "used_out", (1,), torch.int32, dev)
-        _written([("table_out", table_out), ("used_out", used_out)], [("table", table), ("lengths", lengths)])
+        _written([("table_out", table_out), ("used_out", used_out)],
+                 [("table", table), ("lengths", lengths), ("cache", cache)])
     nbytes = _cache_workspace(cache.shape[-5:], t.rows)
     if workspace is not None:
         _check_bytes(workspace, "workspace", nbytes, dev)
     _on_gpu(dev)
+    return c, layers, t, nbytes
+
+
+def cache_compact(cache, table, lengths, table_out=None, used_out=None, workspace=None):
+    """(table_out, used_out): the table, its rows of lengths[r] tokens, after all pages in
+    use have moved to the lowest numbers, in every layer; used_out (int32 [1]) is their
+    count, so that pages from there on are free.  Pages that are below it already
+    stay.  table_out, used_out: tensors to write, which are not the call's inputs."""
+    given = table_out is not None or used_out is not None or workspace is not None
+    try:
+        dev = cache.device
+        key = ("compact", dev, cache.shape, cache.stride(), cache.dtype, table.shape, table.stride(), table.dtype,
+               table.device, lengths.shape, lengths.stride(), lengths.dtype, lengths.device)
+        args = None if given or cache.data_ptr() & 15 else _checked.get(key)
+    except (AttributeError, TypeError):
+        key = args = None
+    c, layers, t, nbytes = args or _remember(key, _check_compact(cache, table, lengths, table_out, used_out, workspace))
     with _on_device(dev):
         if table_out is None:
             table_out = torch.empty((t.rows, t.width), dtype=torch.int32, device=dev)
             used_out = torch.empty(1, dtype=torch.int32, device=dev)
         if workspace is None:
             workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        else:
+            nbytes = workspace.numel() * workspace.element_size()
         _check(_lib.entmax_cache_compact(
-            c, layers, cache.data_ptr(), t, lengths.data_ptr(), table_out.data_ptr(),
-            max(_stride(table_out, 0), t.width), used_out.data_ptr(), workspace.data_ptr(),
-            workspace.numel() * workspace.element_size(), _stream_handle(dev)), "entmax_cache_compact")
+            c, layers, cache.data_ptr(), t, table.data_ptr(), lengths.data_ptr(), table_out.data_ptr(),
+            max(_stride(table_out, 0), t.width), used_out.data_ptr(), workspace.data_ptr(), nbytes,
+            _stream_handle(dev)), "entmax_cache_compact")
     return table_out, used_out
 
 
@@ -1640,18 +1731,7 @@ def paged_decode_workspace(q, cache, table, max_length=None):
                      _longest(table, c, max_length))[2]
 
 
-def paged_decode(q, cache, table, lengths, rows=None, alpha=1.5, scale=None, max_iter=None, tol=None, out=None,
-                 workspace=None, max_length=None):
-    """O [queries, heads, head_dim] of q [queries, heads, head_dim] (bf16 or fp32, any strides
-    with a contiguous last dimension): query i attends to the first lengths[i] tokens
-    (int32 on the device) of the table's row rows[i] (None: row i) in a layer's
-    cache.  Several queries may have the same row, with lengths of their own (the
-    last tokens of a draft).  A query without any key has O = 0, and so has one
-    whose largest score is not finite.  1 < alpha <= 2.
-
-    max_length: no query has more keys (default: what the table holds; grids and
-    workspace grow with it).  tol: default 1e-6.  workspace: a device buffer of
-    paged_decode_workspace bytes, to keep from call to call (one call at a time)."""
+def _check_paged(q, cache, table, lengths, rows, numbers, max_length, out, workspace):
     c = _layer(cache)
     dev = cache.device
     t = _table(table, c, dev)
@@ -1671,19 +1751,50 @@ def paged_decode(q, cache, table, lengths, rows=None, alpha=1.5, scale=None, max
         raise ValueError("q has %d queries, the table %d rows: give rows" % (n, t.rows))
     if out is not None:
         _strided(out, "out", q.shape, q.dtype, dev, written=True)
-        _written([("out", out)], [("q", q)])
-    shape, params, nbytes = _paged_of(*_numbers(alpha, scale, max_iter, 1e-6 if tol is None else tol), cache.shape, n,
-                                      heads, dt, _longest(table, c, max_length))
+        _written([("out", out)], [("q", q), ("cache", cache), ("table", table), ("lengths", lengths)] +
+                 ([] if rows is None else [("rows", rows)]))
+    shape, params, nbytes = _paged_of(*numbers, cache.shape, n, heads, dt, _longest(table, c, max_length))
     if workspace is not None:
         _check_bytes(workspace, "workspace", nbytes, dev)
     _on_gpu(dev)
+    return shape, params, c, t, _row_head(q), _strides_of(heads * d, d), max(nbytes, 16)
+
+
+def paged_decode(q, cache, table, lengths, rows=None, alpha=1.5, scale=None, max_iter=None, tol=None, out=None,
+                 workspace=None, max_length=None):
+    """O [queries, heads, head_dim] of q [queries, heads, head_dim] (bf16 or fp32, any strides
+    with a contiguous last dimension): query i attends to the first lengths[i] tokens
+    (int32 on the device) of the table's row rows[i] (None: row i) in a layer's
+    cache.  Several queries may have the same row, with lengths of their own (the
+    last tokens of a draft).  A query without any key has O = 0, and so has one
+    whose largest score is not finite.  1 < alpha <= 2.
+
+    max_length: no query has more keys (default: what the table holds; grids and
+    workspace grow with it).  tol: default 1e-6.  workspace: a device buffer of
+    paged_decode_workspace bytes, to keep from call to call (one call at a time)."""
+    numbers = _numbers(alpha, scale, max_iter, 1e-6 if tol is None else tol)
+    max_length = None if max_length is None else int(max_length)
+    try:
+        dev = cache.device
+        key = ("paged", dev, numbers, max_length, cache.shape, cache.stride(), cache.dtype, q.shape, q.stride(), q.dtype,
+               q.device, table.shape, table.stride(), table.dtype, table.device, lengths.shape, lengths.stride(),
+               lengths.dtype, lengths.device, rows is not None and (rows.shape, rows.stride(), rows.dtype, rows.device))
+        args = (None if out is not None or workspace is not None or (cache.data_ptr() | q.data_ptr()) & 15
+                else _checked.get(key))
+    except (AttributeError, TypeError):
+        key = args = None
+    shape, params, c, t, qs, os_, nbytes = args or _remember(key, _check_paged(
+        q, cache, table, lengths, rows, numbers, max_length, out, workspace))
     with _on_device(dev):
         if out is None:
-            out = q.new_empty(q.shape)
+            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        else:
+            os_ = _row_head(out)
         if workspace is None:
-            workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=dev)
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        else:
+            nbytes = workspace.numel() * workspace.element_size()
         _check(_lib.entmax_paged_decode(
-            shape, params, c, cache.data_ptr(), t, q.data_ptr(), _row_head(q), lengths.data_ptr(), _ptr(rows),
-            out.data_ptr(), _row_head(out), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-            _stream_handle(dev)), "entmax_paged_decode")
+            shape, params, c, cache.data_ptr(), t, table.data_ptr(), q.data_ptr(), qs, lengths.data_ptr(), _ptr(rows),
+            out.data_ptr(), os_, workspace.data_ptr(), nbytes, _stream_handle(dev)), "entmax_paged_decode")
     return out

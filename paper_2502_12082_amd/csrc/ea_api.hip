@@ -1199,20 +1199,20 @@ ea_status check_cache(const ea_cache* c, PageDims* out) {
   return EA_OK;
 }
 
-ea_status check_table(const ea_page_table* t, const PageDims& c, PageTable* out) {
+ea_status check_table(const ea_page_table* t, const int32_t* ids, const PageDims& c, PageTable* out) {
   if (!t || t->rows < 1 || t->width < 1 || t->stride < 0 || t->stride > MAX_STRIDE) return EA_ERR_INVALID_ARG;
-  if (!small_ok(t->pages)) return EA_ERR_INVALID_ARG;
+  if (!small_ok(ids)) return EA_ERR_INVALID_ARG;
   if ((int64_t)t->width << c.shift > MAX_SEQLEN || t->rows > 1 << 20) return EA_ERR_UNSUPPORTED;
-  *out = PageTable{t->pages, t->rows, t->width, t->stride};
+  *out = PageTable{ids, t->rows, t->width, t->stride};
   return EA_OK;
 }
 
-ea_status cache_rows(const ea_cache* c, const void* cache, const ea_page_table* table, int32_t tokens, int32_t dtype,
-                     const int32_t* rows, const int32_t* positions, const void* k, const ea_strides* ks,
+ea_status cache_rows(const ea_cache* c, const void* cache, const ea_page_table* t, const int32_t* table, int32_t tokens,
+                     int32_t dtype, const int32_t* rows, const int32_t* positions, const void* k, const ea_strides* ks,
                      const void* v, const ea_strides* vs, bool append, void* stream) {
   CacheRowsArgs a{};
   ea_status st = check_cache(c, &a.c);
-  if (st != EA_OK || (st = check_table(table, a.c, &a.t)) != EA_OK) return st;
+  if (st != EA_OK || (st = check_table(t, table, a.c, &a.t)) != EA_OK) return st;
   if (!dtype_ok(dtype)) return EA_ERR_UNSUPPORTED;
   if (tokens < 0) return EA_ERR_INVALID_ARG;
   // a launch has fewer than 2^32 threads: at least 16 tokens to 256 of them
@@ -1251,12 +1251,12 @@ size_t update_parts(const PageDims& c, int rows, void* base, CacheUpdateArgs* a)
 }
 
 // The arguments that an update and a compaction have in common.
-ea_status table_args(const ea_cache* c, int32_t layers, void* cache, const ea_page_table* table,
-                     const int32_t* lengths, int32_t rows, int32_t* table_out, int64_t out_stride, void* workspace,
+ea_status table_args(const ea_cache* c, int32_t layers, void* cache, const ea_page_table* t,
+                     const int32_t* table, const int32_t* lengths, int32_t rows, int32_t* table_out, int64_t out_stride, void* workspace,
                      size_t ws_bytes, CacheUpdateArgs* a) {
   ea_status st = check_cache(c, &a->c);
-  if (st != EA_OK || (st = check_table(table, a->c, &a->t)) != EA_OK) return st;
-  if (layers < 1 || rows < 0 || out_stride < table->width || out_stride > MAX_STRIDE) return EA_ERR_INVALID_ARG;
+  if (st != EA_OK || (st = check_table(t, table, a->c, &a->t)) != EA_OK) return st;
+  if (layers < 1 || rows < 0 || out_stride < t->width || out_stride > MAX_STRIDE) return EA_ERR_INVALID_ARG;
   if (layers > 1 << 16 || rows > 1 << 20) return EA_ERR_UNSUPPORTED;
   if (!tensor_ok(cache) || !small_ok(lengths) || (rows && !small_ok(table_out))) return EA_ERR_INVALID_ARG;
   if (!tensor_ok(workspace)) return EA_ERR_INVALID_ARG;
@@ -1307,16 +1307,16 @@ ea_status entmax_cache_page_bytes(const ea_cache* c, size_t* bytes) {
   return EA_OK;
 }
 
-ea_status entmax_cache_append(const ea_cache* c, void* cache, const ea_page_table* table, int32_t tokens,
-                              int32_t dtype, const int32_t* rows, const int32_t* positions, const void* k,
-                              const ea_strides* ks, const void* v, const ea_strides* vs, void* stream) {
-  return cache_rows(c, cache, table, tokens, dtype, rows, positions, k, ks, v, vs, true, stream);
+ea_status entmax_cache_append(const ea_cache* c, void* cache, const ea_page_table* t,
+                              const int32_t* table, int32_t tokens, int32_t dtype, const int32_t* rows,
+                              const int32_t* positions, const void* k, const ea_strides* ks, const void* v, const ea_strides* vs, void* stream) {
+  return cache_rows(c, cache, t, table, tokens, dtype, rows, positions, k, ks, v, vs, true, stream);
 }
 
-ea_status entmax_cache_read(const ea_cache* c, const void* cache, const ea_page_table* table, int32_t tokens,
-                            int32_t dtype, const int32_t* rows, const int32_t* positions, void* k,
-                            const ea_strides* ks, void* v, const ea_strides* vs, void* stream) {
-  return cache_rows(c, cache, table, tokens, dtype, rows, positions, k, ks, v, vs, false, stream);
+ea_status entmax_cache_read(const ea_cache* c, const void* cache, const ea_page_table* t,
+                            const int32_t* table, int32_t tokens, int32_t dtype, const int32_t* rows,
+                            const int32_t* positions, void* k, const ea_strides* ks, void* v, const ea_strides* vs, void* stream) {
+  return cache_rows(c, cache, t, table, tokens, dtype, rows, positions, k, ks, v, vs, false, stream);
 }
 
 ea_status entmax_cache_workspace(const ea_cache* c, int32_t rows, size_t* bytes) {
@@ -1330,13 +1330,13 @@ ea_status entmax_cache_workspace(const ea_cache* c, int32_t rows, size_t* bytes)
   return EA_OK;
 }
 
-ea_status entmax_cache_update(const ea_cache* c, int32_t layers, void* cache, const ea_page_table* table,
-                              const int32_t* lengths, int32_t rows_out, const int32_t* parents, const int32_t* counts,
+ea_status entmax_cache_update(const ea_cache* c, int32_t layers, void* cache, const ea_page_table* t,
+                              const int32_t* table, const int32_t* lengths, int32_t rows_out, const int32_t* parents, const int32_t* counts,
                               int32_t* table_out, int64_t out_stride, int32_t* lengths_out, int32_t* missing,
                               void* workspace, size_t ws_bytes, void* stream) {
   CacheUpdateArgs a{};
   const ea_status st =
-      table_args(c, layers, cache, table, lengths, rows_out, table_out, out_stride, workspace, ws_bytes, &a);
+      table_args(c, layers, cache, t, table, lengths, rows_out, table_out, out_stride, workspace, ws_bytes, &a);
   if (st != EA_OK) return st;
   if (rows_out == 0) return EA_OK;
   if (!small_ok(parents) || !small_ok(counts) || !small_ok(lengths_out) || !small_ok(missing))
@@ -1348,11 +1348,11 @@ ea_status entmax_cache_update(const ea_cache* c, int32_t layers, void* cache, co
   return from_hip(launch_cache_update(a, static_cast<hipStream_t>(stream)));
 }
 
-ea_status entmax_cache_compact(const ea_cache* c, int32_t layers, void* cache, const ea_page_table* table,
-                               const int32_t* lengths, int32_t* table_out, int64_t out_stride, int32_t* used,
+ea_status entmax_cache_compact(const ea_cache* c, int32_t layers, void* cache, const ea_page_table* t,
+                               const int32_t* table, const int32_t* lengths, int32_t* table_out, int64_t out_stride, int32_t* used,
                                void* workspace, size_t ws_bytes, void* stream) {
   CacheUpdateArgs a{};
-  const ea_status st = table_args(c, layers, cache, table, lengths, table ? table->rows : 0, table_out, out_stride,
+  const ea_status st = table_args(c, layers, cache, t, table, lengths, t ? t->rows : 0, table_out, out_stride,
                                   workspace, ws_bytes, &a);
   if (st != EA_OK) return st;
   if (!small_ok(used)) return EA_ERR_INVALID_ARG;
@@ -1370,12 +1370,12 @@ ea_status entmax_paged_decode_workspace(const ea_paged_shape* shape, const ea_ca
 }
 
 ea_status entmax_paged_decode(const ea_paged_shape* shape, const ea_params* params, const ea_cache* c,
-                              const void* cache, const ea_page_table* table, const void* q, const ea_strides* qs,
-                              const int32_t* lengths, const int32_t* rows, void* o, const ea_strides* os,
+                              const void* cache, const ea_page_table* t, const int32_t* table, const void* q,
+                              const ea_strides* qs, const int32_t* lengths, const int32_t* rows, void* o, const ea_strides* os,
                               void* workspace, size_t ws_bytes, void* stream) {
   PagedArgs a{};
   ea_status st = check_paged(shape, c, &a);
-  if (st != EA_OK || (st = check_table(table, a.c, &a.t)) != EA_OK) return st;
+  if (st != EA_OK || (st = check_table(t, table, a.c, &a.t)) != EA_OK) return st;
   if (!params) return EA_ERR_INVALID_ARG;
   if ((st = check_params(params)) != EA_OK) return st;
   if (params->alpha > 2.0f) return EA_ERR_UNSUPPORTED;

@@ -239,12 +239,12 @@ struct CacheUpdateArgs {
   int rows_out;
   int32_t *lengths_out, *missing;  // [rows_out]; of a compaction `missing` is one number, the pages in use
   // workspace: [pages] rows that hold each page, rows about to write to it, the
-  // lowest of those, and free pages (compaction: holders, -, where each page goes, free
-  // pages), [rows_out] pages needed before each row, and [copies] page pairs; marks
+  // lowest of those, and free pages (compaction: a bit for each page in use, -, where pages
+  // go, -), [rows_out] pages needed before each row, [copies] page pairs, and the
+  // number of copies of a compaction
   int32_t *holders, *writers, *lowest, *free_list, *before, *source, *target, *marks;
 };
-// marks: workgroups that have arrived, copies to make
-constexpr int UPDATE_MARKS = 2;
+constexpr int UPDATE_MARKS = 1;
 
 // One query per row of q over the pages of a row of the table.  Keys are taken in
 // regions of PAGED_REGION.

@@ -220,29 +220,6 @@ __device__ __forceinline__ int place_of(int mine, int& base, int (&sums)[2][UP_W
   return count_up(at, excl);
 }
 
-// Whether this workgroup is the last of the launch to come here; what the others
-// wrote before can be read then.
-__device__ __forceinline__ bool last_to_arrive(int32_t* arrived) {
-  __shared__ int last;
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x == 0) last = atomicAdd(arrived, 1) == (int)gridDim.x - 1;
-  __syncthreads();
-  if (last) __threadfence();
-  return last != 0;
-}
-
-__global__ __launch_bounds__(256) void clear_kernel(CacheUpdateArgs a) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i < UPDATE_MARKS) a.marks[i] = 0;
-  if (i >= a.c.pages) return;
-  a.holders[i] = 0;
-  if (a.parents) {
-    a.writers[i] = 0;
-    a.lowest[i] = INT32_MAX;
-  }
-}
-
 __device__ __forceinline__ int row_length(const CacheUpdateArgs& a, int row) {
   return row < 0 || row >= a.t.rows ? 0 : a.lengths[row];
 }
@@ -253,50 +230,247 @@ __device__ __forceinline__ RowPlan plan_of(const CacheUpdateArgs& a, int r) {
 __device__ __forceinline__ int last_page(const CacheUpdateArgs& a, int r, const RowPlan& p) {
   return p.writes ? page_of(a.c, a.t, a.parents[r], p.old) : -1;
 }
-__device__ __forceinline__ bool row_copies(const CacheUpdateArgs& a, int r, int last) {
-  return last >= 0 && copies(a.holders[last], a.writers[last], a.lowest[last], r);
+__device__ __forceinline__ RowPlan kept_of(const CacheUpdateArgs& a, int r) {
+  return plan_row(row_length(a, r), 0, a.t.width, a.c.shift);
 }
 
-// A workgroup per row: the entries that stay, and who holds what.  The last one
-// then finds the pages that rows need among those that no row holds.
-__global__ __launch_bounds__(UP_NT) void update_tables_kernel(CacheUpdateArgs a) {
-  __shared__ int sums[2][UP_WAVES];
-  const int t = threadIdx.x, lane = lane_id(), w = wave_id();
-  {
-    const int r = blockIdx.x, parent = a.parents[r];
-    const RowPlan p = plan_of(a, r);
-    int32_t* const out = a.table_out + r * a.out_stride;
-    const int32_t* const in = a.t.ids + (p.old ? parent : 0) * a.t.stride;
-    for (int i = t; i < a.t.width; i += UP_NT) {
-      int id = -1;
-      if (i < p.kept) {
-        id = in[i];
-        if (id >= 0 && id < a.c.pages) atomicAdd(a.holders + id, 1);
-      }
-      out[i] = id;
+// Small tables (small_tables): one workgroup plans, with a bit in LDS for every page
+// that is held, and counts of the pages that rows are about to write to in a hash
+// table.  It is bound by its chain of loads and barriers: a row's parent, its length, its
+// entries.
+constexpr int PL_ROWS = UP_NT, PL_WORDS = 4096, PL_SLOTS = 2 * PL_ROWS;
+constexpr int PL_BATCH = 8, PL_LOADS = 2;  // rows of a wave, and entries of a lane of each, in flight
+
+struct PageSet {
+  uint32_t* word;  // a bit for each page
+  int pages;
+  __device__ __forceinline__ int words() const { return (pages + 31) / 32; }
+  __device__ __forceinline__ void clear() const {
+    for (int i = threadIdx.x; i < words(); i += UP_NT) word[i] = 0;
+  }
+  // pages [32 i, 32 i + 32) that are in the set
+  __device__ __forceinline__ uint32_t held(int i) const { return i < words() ? word[i] : 0; }
+  __device__ __forceinline__ uint32_t free(int i) const {
+    return i >= words() ? 0 : ~word[i] & (32 * i + 32 > pages ? (1u << (pages & 31)) - 1 : ~0u);
+  }
+};
+
+// use(page) of the entries [0, kept[r]) that name pages of the table's rows from[r].
+template <typename F>
+__device__ __forceinline__ void each_held(const CacheUpdateArgs& a, const int* from, const int* kept, int rows, F&& use) {
+  const int lane = lane_id();
+  for (int r0 = wave_id(); r0 < rows; r0 += PL_BATCH * UP_WAVES) {
+    int n[PL_BATCH], most = 0;
+    const int32_t* in[PL_BATCH];
+#pragma unroll
+    for (int j = 0; j < PL_BATCH; ++j) {
+      const int r = r0 + j * UP_WAVES;
+      n[j] = r < rows ? kept[r] : 0;
+      in[j] = a.t.ids + (n[j] ? from[r] : 0) * a.t.stride;
+      most = max(most, n[j]);
     }
-    if (t == 0) {
-      const int last = last_page(a, r, p);
-      if (last >= 0) {
-        atomicAdd(a.writers + last, 1);
-        atomicMin(a.lowest + last, r);
-      }
+    for (int e0 = lane; e0 < most; e0 += 64 * PL_LOADS) {
+      int id[PL_BATCH][PL_LOADS];
+#pragma unroll
+      for (int j = 0; j < PL_BATCH; ++j)
+#pragma unroll
+        for (int u = 0; u < PL_LOADS; ++u) id[j][u] = e0 + 64 * u < n[j] ? in[j][e0 + 64 * u] : -1;
+#pragma unroll
+      for (int j = 0; j < PL_BATCH; ++j)
+#pragma unroll
+        for (int u = 0; u < PL_LOADS; ++u)
+          if (id[j][u] >= 0 && id[j][u] < a.c.pages) use(id[j][u]);
     }
   }
-  if (!last_to_arrive(a.marks)) return;
+}
+
+// Workgroup 0 plans; workgroup 1 + r writes those entries of row r that need no plan.
+__global__ __launch_bounds__(UP_NT) void update_small_kernel(CacheUpdateArgs a) {
+  __shared__ uint32_t held_words[PL_WORDS];
+  __shared__ int key[PL_SLOTS], holders[PL_SLOTS], writers[PL_SLOTS], lowest[PL_SLOTS];
+  __shared__ int from[PL_ROWS], kept[PL_ROWS], before[PL_ROWS + 1];
+  __shared__ int sums[2][UP_WAVES];
+  const int t = threadIdx.x;
+  if (blockIdx.x) {
+    const int r = blockIdx.x - 1;
+    const RowPlan p = plan_of(a, r);
+    int32_t* const out = a.table_out + r * a.out_stride;
+    const int32_t* const in = a.t.ids + (p.old ? a.parents[r] : 0) * a.t.stride;
+    const int open = p.writes ? p.old >> a.c.shift : -1;
+    for (int i = t; i < a.t.width; i += UP_NT)
+      if (i != open && (i < p.kept || i >= p.kept + p.grown)) out[i] = i < p.kept ? in[i] : -1;
+    return;
+  }
+  const PageSet held{held_words, a.c.pages};
+  held.clear();
+  for (int i = t; i < PL_SLOTS; i += UP_NT) {
+    key[i] = -1;
+    holders[i] = writers[i] = 0;
+    lowest[i] = INT32_MAX;
+  }
+  __syncthreads();
+  RowPlan p{};
+  int last = -1, slot = 0;
+  if (t < a.rows_out) {
+    p = plan_of(a, t);
+    from[t] = a.parents[t];
+    kept[t] = p.kept;
+    last = last_page(a, t, p);
+  }
+  auto first = [](int page) { return (int)((uint32_t)page * 0x9E3779B1u >> 21); };
+  static_assert(PL_SLOTS == 1 << 11, "a hash is 11 bits");
+  if (last >= 0) {
+    for (slot = first(last);; slot = (slot + 1) % PL_SLOTS) {  // (at most half of the slots are taken)
+      const int was = atomicCAS(&key[slot], -1, last);
+      if (was == -1 || was == last) break;
+    }
+    atomicAdd(&writers[slot], 1);
+    atomicMin(&lowest[slot], t);
+  }
+  __syncthreads();
+  each_held(a, from, kept, a.rows_out, [&](int id) {
+    atomicOr(&held_words[id >> 5], 1u << (id & 31));
+    for (int s = first(id); key[s] != -1; s = (s + 1) % PL_SLOTS)
+      if (key[s] == id) {
+        atomicAdd(&holders[s], 1);
+        break;
+      }
+  });
+  __syncthreads();
   // ---- pages needed before each row
+  int turn = 0, needed = 0;
+  const int copy = last >= 0 && copies(holders[slot], writers[slot], lowest[slot], t) ? 1 : 0;
+  const int need = t < a.rows_out ? p.grown + copy : 0;
+  const int at = place_of(need, needed, sums, turn);
+  before[t] = at;
+  kept[t] = p.kept | copy << 30;
+  if (t == 0) before[PL_ROWS] = needed;
+  // ---- as many free pages, the lowest first
+  int found = 0;
+  for (int w0 = 0; w0 < held.words() && found < needed; w0 += UP_NT) {
+    uint32_t bits = held.free(w0 + t);
+    int to = place_of(__popc(bits), found, sums, turn);
+    for (; bits && to < needed; bits &= bits - 1) a.free_list[to++] = 32 * (w0 + t) + __ffs(bits) - 1;
+  }
+  __syncthreads();
+  // ---- to the rows that can have all of theirs
+  if (t < a.rows_out) {
+    const bool done = need == 0 || at + need <= found;
+    const int to = done && copy ? a.free_list[at] : -1;
+    // (the entry that the row is about to write to; an entry that names no page stays)
+    if (p.writes) {
+      const int e = p.old >> a.c.shift;
+      a.table_out[t * a.out_stride + e] = to >= 0 ? to : a.t.ids[from[t] * a.t.stride + e];
+    }
+    a.source[t] = last;
+    a.target[t] = to;
+    a.lengths_out[t] = done ? p.wanted : p.old;
+    a.missing[t] = !p.fits ? -1 : done ? 0 : need;
+  }
+  for (int k = t; k < needed; k += UP_NT) {
+    int lo = 0, hi = PL_ROWS;  // before[lo] <= k < before[hi]: the row that needs page k
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      (before[mid] <= k ? lo : hi) = mid;
+    }
+    const int i = k - before[lo] - (kept[lo] >> 30);
+    if (i >= 0)
+      a.table_out[lo * a.out_stride + (kept[lo] & 0x3FFFFFFF) + i] = before[lo + 1] <= found ? a.free_list[k] : -1;
+  }
+}
+
+// Pages in use are marked; those behind the first `used` are paired with the free
+// ones among these.
+__device__ __forceinline__ void pair_pages(const CacheUpdateArgs& a, const PageSet& held, int (&sums)[2][UP_WAVES]) {
+  const int t = threadIdx.x;
+  int turn = 0, used = 0;
+  for (int w0 = 0; w0 < held.words(); w0 += UP_NT) place_of(__popc(held.held(w0 + t)), used, sums, turn);
+  // free pages below `used`, and pages in use from there on: as many
+  int holes = 0, moves = 0;
+  for (int w0 = 0; w0 < held.words(); w0 += UP_NT) {
+    const int first = 32 * (w0 + t);
+    const uint32_t below = used <= first ? 0u : used >= first + 32 ? ~0u : (1u << (used - first)) - 1;
+    uint32_t hole = held.free(w0 + t) & below, move = held.held(w0 + t) & ~below;
+    int h = place_of(__popc(hole), holes, sums, turn), m = place_of(__popc(move), moves, sums, turn);
+    for (; hole; hole &= hole - 1) a.target[h++] = first + __ffs(hole) - 1;
+    for (; move; move &= move - 1) a.source[m++] = first + __ffs(move) - 1;
+  }
+  __syncthreads();
+  for (int m = t; m < moves; m += UP_NT) a.lowest[a.source[m]] = a.target[m];
+  if (t == 0) {
+    a.marks[0] = moves;
+    a.missing[0] = used;
+  }
+}
+
+__global__ __launch_bounds__(UP_NT) void compact_small_kernel(CacheUpdateArgs a) {
+  __shared__ uint32_t held_words[PL_WORDS];
+  __shared__ int from[PL_ROWS], kept[PL_ROWS];
+  __shared__ int sums[2][UP_WAVES];
+  const int t = threadIdx.x;
+  const PageSet held{held_words, a.c.pages};
+  held.clear();
+  if (t < a.t.rows) {
+    from[t] = t;
+    kept[t] = kept_of(a, t).kept;
+  }
+  __syncthreads();
+  each_held(a, from, kept, a.t.rows, [&](int id) { atomicOr(&held_words[id >> 5], 1u << (id & 31)); });
+  __syncthreads();
+  pair_pages(a, held, sums);
+}
+
+// Any tables: counts of every page in memory, by a workgroup per row, and then one
+// workgroup that plans.
+__global__ __launch_bounds__(256) void clear_kernel(CacheUpdateArgs a) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= a.c.pages) return;
+  a.holders[i] = 0;
+  if (a.parents) {
+    a.writers[i] = 0;
+    a.lowest[i] = INT32_MAX;
+  }
+}
+
+__global__ __launch_bounds__(256) void update_rows_kernel(CacheUpdateArgs a) {
+  const int t = threadIdx.x, r = blockIdx.x;
+  const RowPlan p = plan_of(a, r);
+  int32_t* const out = a.table_out + r * a.out_stride;
+  const int32_t* const in = a.t.ids + (p.old ? a.parents[r] : 0) * a.t.stride;
+  for (int i = t; i < a.t.width; i += 256) {
+    int id = -1;
+    if (i < p.kept) {
+      id = in[i];
+      if (id >= 0 && id < a.c.pages) atomicAdd(a.holders + id, 1);
+    }
+    out[i] = id;
+  }
+  if (t == 0) {
+    const int last = last_page(a, r, p);
+    if (last >= 0) {
+      atomicAdd(a.writers + last, 1);
+      atomicMin(a.lowest + last, r);
+    }
+  }
+}
+
+__global__ __launch_bounds__(UP_NT) void update_plan_kernel(CacheUpdateArgs a) {
+  __shared__ int sums[2][UP_WAVES];
+  const int t = threadIdx.x, lane = lane_id(), w = wave_id();
+  auto row_copies = [&](int r, int last) {
+    return last >= 0 && copies(a.holders[last], a.writers[last], a.lowest[last], r);
+  };
   int turn = 0, needed = 0;
   for (int r0 = 0; r0 < a.rows_out; r0 += UP_NT) {
     const int r = r0 + t;
     int need = 0;
     if (r < a.rows_out) {
       const RowPlan p = plan_of(a, r);
-      need = p.grown + (row_copies(a, r, last_page(a, r, p)) ? 1 : 0);
+      need = p.grown + (row_copies(r, last_page(a, r, p)) ? 1 : 0);
     }
     const int at = place_of(need, needed, sums, turn);
     if (r < a.rows_out) a.before[r] = at;
   }
-  // ---- as many free pages, the lowest first
   const int want = min(needed, a.c.pages);
   int found = 0;
   for (int p0 = 0; p0 < a.c.pages && found < want; p0 += 4 * UP_NT) {
@@ -314,10 +488,10 @@ __global__ __launch_bounds__(UP_NT) void update_tables_kernel(CacheUpdateArgs a)
       if (h[e] == 0) a.free_list[at++] = p0 + 4 * t + e;
   }
   __syncthreads();
-  // ---- to the rows that can have all of theirs, a wave to a row
+  // (a wave to a row)
   for (int r = w; r < a.rows_out; r += UP_WAVES) {
     const RowPlan p = plan_of(a, r);
-    const int last = last_page(a, r, p), copy = row_copies(a, r, last) ? 1 : 0;
+    const int last = last_page(a, r, p), copy = row_copies(r, last) ? 1 : 0;
     const int need = p.grown + copy, at = a.before[r];
     const bool done = need == 0 || count_up(at, need) <= found;
     int32_t* const out = a.table_out + r * a.out_stride;
@@ -334,49 +508,17 @@ __global__ __launch_bounds__(UP_NT) void update_tables_kernel(CacheUpdateArgs a)
   }
 }
 
-// Rows' pages are marked; the last workgroup pairs those in use behind the first
-// `used` with the free ones among these.
+__global__ __launch_bounds__(256) void compact_rows_kernel(CacheUpdateArgs a) {
+  const int r = blockIdx.x, kept = kept_of(a, r).kept;
+  const int32_t* const in = a.t.ids + r * a.t.stride;
+  for (int i = threadIdx.x; i < kept; i += 256) {
+    const int id = in[i];
+    if (id >= 0 && id < a.c.pages) atomicOr(reinterpret_cast<uint32_t*>(a.holders) + (id >> 5), 1u << (id & 31));
+  }
+}
 __global__ __launch_bounds__(UP_NT) void compact_plan_kernel(CacheUpdateArgs a) {
   __shared__ int sums[2][UP_WAVES];
-  const int t = threadIdx.x;
-  {
-    const int r = blockIdx.x;
-    const RowPlan p = plan_row(row_length(a, r), 0, a.t.width, a.c.shift);
-    const int32_t* const in = a.t.ids + r * a.t.stride;
-    for (int i = t; i < p.kept; i += UP_NT) {
-      const int id = in[i];
-      if (id >= 0 && id < a.c.pages) atomicOr(a.holders + id, 1);
-    }
-  }
-  if (!last_to_arrive(a.marks)) return;
-  int turn = 0, used = 0;
-  for (int p0 = 0; p0 < a.c.pages; p0 += 4 * UP_NT) {
-    int mine = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int p = p0 + 4 * t + e;
-      mine += p < a.c.pages && a.holders[p] ? 1 : 0;
-    }
-    place_of(mine, used, sums, turn);
-  }
-  // free pages below `used`, then pages in use from there on: as many
-  int holes = 0, moves = 0;
-  for (int p0 = 0; p0 < a.c.pages; p0 += UP_NT) {
-    const int p = p0 + t;
-    const bool in_use = p < a.c.pages && a.holders[p] != 0;
-    const bool hole = p < used && !in_use, move = p >= used && in_use;
-    const int h = place_of(hole ? 1 : 0, holes, sums, turn), m = place_of(move ? 1 : 0, moves, sums, turn);
-    if (hole) a.target[h] = p;
-    if (move) a.source[m] = p;
-  }
-  __syncthreads();
-  for (int p = t; p < a.c.pages; p += UP_NT) a.lowest[p] = p;
-  __syncthreads();
-  for (int m = t; m < moves; m += UP_NT) a.lowest[a.source[m]] = a.target[m];
-  if (t == 0) {
-    a.marks[1] = moves;
-    a.missing[0] = used;
-  }
+  pair_pages(a, PageSet{reinterpret_cast<uint32_t*>(a.holders), a.c.pages}, sums);
 }
 
 constexpr int CP_NT = 256, CP_LOADS = 4, CP_CHUNK = CP_NT * CP_LOADS * 16;
@@ -387,7 +529,7 @@ template <bool COMPACT>
 __global__ __launch_bounds__(CP_NT) void copy_pages_kernel(CacheUpdateArgs a, int chunks) {
   const int t = threadIdx.x;
   const int64_t bytes = page_bytes(a.c), layer = bytes * a.c.pages;
-  const int pairs = COMPACT ? a.marks[1] : a.rows_out;
+  const int pairs = COMPACT ? a.marks[0] : a.rows_out;
   const int64_t items = (int64_t)pairs * a.layers * chunks;
   for (int64_t x = blockIdx.x; x < items; x += gridDim.x) {
     const int chunk = (int)(x % chunks), l = (int)(x / chunks % a.layers), i = (int)(x / chunks / a.layers);
@@ -406,12 +548,12 @@ __global__ __launch_bounds__(CP_NT) void copy_pages_kernel(CacheUpdateArgs a, in
   }
   if constexpr (COMPACT) {
     for (int r = blockIdx.x; r < a.t.rows; r += gridDim.x) {
-      const int kept = plan_row(row_length(a, r), 0, a.t.width, a.c.shift).kept;
+      const int kept = kept_of(a, r).kept, used = a.missing[0];
       for (int i = t; i < a.t.width; i += CP_NT) {
         int id = -1;
         if (i < kept) {
           id = a.t.ids[r * a.t.stride + i];
-          if (id >= 0 && id < a.c.pages) id = a.lowest[id];
+          if (id >= used && id < a.c.pages) id = a.lowest[id];
         }
         a.table_out[r * a.out_stride + i] = id;
       }
@@ -435,20 +577,37 @@ hipError_t launch_clear(const CacheUpdateArgs& a, hipStream_t s) {
   return launch_kernel(clear_kernel, dim3((unsigned)((a.c.pages + 255) / 256)), dim3(256), s, a);
 }
 
+// Tables that one workgroup plans.
+bool small_tables(const CacheUpdateArgs& a, int rows) {
+  return rows <= PL_ROWS && a.c.pages <= 32 * PL_WORDS && (int64_t)rows * a.t.width <= 1 << 18;
+}
+
 }  // namespace
 
 hipError_t launch_cache_append(const CacheRowsArgs& a, int dtype, hipStream_t s) { return launch_rows<true>(a, dtype, s); }
 hipError_t launch_cache_read(const CacheRowsArgs& a, int dtype, hipStream_t s) { return launch_rows<false>(a, dtype, s); }
 
 hipError_t launch_cache_update(const CacheUpdateArgs& a, hipStream_t s) {
-  hipError_t e = launch_clear(a, s);
-  if (e == hipSuccess) e = launch_kernel(update_tables_kernel, dim3((unsigned)a.rows_out), dim3(UP_NT), s, a);
+  hipError_t e;
+  if (small_tables(a, a.rows_out)) {
+    e = launch_kernel(update_small_kernel, dim3((unsigned)a.rows_out + 1), dim3(UP_NT), s, a);
+  } else {
+    e = launch_clear(a, s);
+    if (e == hipSuccess) e = launch_kernel(update_rows_kernel, dim3((unsigned)a.rows_out), dim3(256), s, a);
+    if (e == hipSuccess) e = launch_kernel(update_plan_kernel, dim3(1), dim3(UP_NT), s, a);
+  }
   return e == hipSuccess ? launch_copies<false>(a, a.rows_out, s) : e;
 }
 
 hipError_t launch_cache_compact(const CacheUpdateArgs& a, hipStream_t s) {
-  hipError_t e = launch_clear(a, s);
-  if (e == hipSuccess) e = launch_kernel(compact_plan_kernel, dim3((unsigned)a.t.rows), dim3(UP_NT), s, a);
+  hipError_t e;
+  if (small_tables(a, a.t.rows)) {
+    e = launch_kernel(compact_small_kernel, dim3(1), dim3(UP_NT), s, a);
+  } else {
+    e = launch_clear(a, s);
+    if (e == hipSuccess) e = launch_kernel(compact_rows_kernel, dim3((unsigned)a.t.rows), dim3(256), s, a);
+    if (e == hipSuccess) e = launch_kernel(compact_plan_kernel, dim3(1), dim3(UP_NT), s, a);
+  }
   return e == hipSuccess ? launch_copies<true>(a, a.c.pages / 2 + 1, s) : e;
 }
 

@@ -123,7 +123,8 @@ def compact_by_hand(table, lengths, page, pages):
     width = len(table[0])
     rows = [row[:-(-min(max(n, 0), width * page) // page)] for row, n in zip(table, lengths)]
     used = sorted({p for row in rows for p in row if 0 <= p < pages})
-    holes = [p for p in range(len(used)) if p not in set(used)]
+    held = set(used)
+    holes = [p for p in range(len(used)) if p not in held]
     moves = list(zip([p for p in used if p >= len(used)], holes))
     to = dict(moves)
     return [[to.get(p, p) for p in row] + [-1] * (width - len(row)) for row in rows], len(used), moves

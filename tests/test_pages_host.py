@@ -192,7 +192,7 @@ def test_update_refuses():
     for change, word in (
             (dict(lengths=ints(5)), "lengths"), (dict(parents=torch.zeros(3, dtype=torch.int64)), "parents"),
             (dict(counts=ints(1)), "counts"), (dict(table_out=t), "together"),
-            (dict(out, table_out=torch.zeros(3, 5, dtype=I32)), "shape"), (dict(out, lengths_out=ints(1)), "lengths_out"),
+            (dict(out, table_out=torch.zeros(3, 5, dtype=I32)), "table_out must be"), (dict(out, lengths_out=ints(1)), "lengths_out"),
             (dict(out, missing_out=i), "overlaps"), (dict(out, table=t, lengths=i.clone()), "overlaps table"),
             (dict(out, parents=i), "overlaps parents"), (dict(out, table_out=t[:1].expand(3, 4)), "memory"),
             (dict(out, table=wide[:, :4], lengths=i.clone(), table_out=wide[:, 4:]), "overlaps|GPU"),
@@ -208,7 +208,7 @@ def test_compact_refuses():
     for change, word in ((dict(lengths=ints(5)), "lengths"), (dict(table_out=t), "together"),
                          (dict(table_out=t, used_out=ints(1, 2)), "used_out"),
                          (dict(table_out=a["table"], used_out=ints(1)), "overlaps"),
-                         (dict(table_out=t[:1], used_out=ints(1)), "shape"), (dict(), "GPU")):
+                         (dict(table_out=t[:1], used_out=ints(1)), "table_out must be"), (dict(), "GPU")):
         with pytest.raises(ValueError, match=word):
             ea.cache_compact(**dict(a, **change))
 
@@ -244,8 +244,8 @@ def test_decode_refuses(change, word):
 ADDRESS = 1 << 20  # (of nothing: these calls end before they look)
 
 
-def c_table(width=4, rows=2, stride=4, pages=ADDRESS):
-    return ea.PageTable(pages, rows, width, stride)
+def c_table(width=4, rows=2, stride=4):
+    return ea.PageTable(rows, width, stride)
 
 
 @pytest.mark.parametrize("c,code", [
@@ -260,7 +260,7 @@ def test_cache_abi(c, code):
     assert ea._lib.entmax_cache_workspace(c, 1, ctypes.byref(n)) == code
     assert ea._lib.entmax_paged_decode_workspace(ea.PagedShape(1, 2, 0, 8), c, ctypes.byref(n)) == code
     s = ea.Strides(128, 64)
-    assert ea._lib.entmax_cache_append(c, ADDRESS, c_table(), 1, 0, ADDRESS, ADDRESS, ADDRESS, s, ADDRESS, s, None) == code
+    assert ea._lib.entmax_cache_append(c, ADDRESS, c_table(), ADDRESS, 1, 0, ADDRESS, ADDRESS, ADDRESS, s, ADDRESS, s, None) == code
 
 
 OK_CACHE = ea.Cache(4, 16, 2, 64)
@@ -268,8 +268,8 @@ OK_CACHE = ea.Cache(4, 16, 2, 64)
 
 @pytest.mark.parametrize("change,code", [
     (dict(table=c_table(width=0)), ea.EA_ERR_INVALID_ARG), (dict(table=c_table(rows=0)), ea.EA_ERR_INVALID_ARG),
-    (dict(table=c_table(stride=-4)), ea.EA_ERR_INVALID_ARG), (dict(table=c_table(pages=None)), ea.EA_ERR_INVALID_ARG),
-    (dict(table=c_table(pages=ADDRESS + 2)), ea.EA_ERR_INVALID_ARG),
+    (dict(table=c_table(stride=-4)), ea.EA_ERR_INVALID_ARG), (dict(ids=None), ea.EA_ERR_INVALID_ARG),
+    (dict(ids=ADDRESS + 2), ea.EA_ERR_INVALID_ARG),
     (dict(table=c_table(width=8193, stride=8193)), ea.EA_ERR_UNSUPPORTED),
     (dict(tokens=-1), ea.EA_ERR_INVALID_ARG), (dict(tokens=1 << 26), ea.EA_ERR_UNSUPPORTED),
     (dict(dtype=2), ea.EA_ERR_UNSUPPORTED), (dict(k=ADDRESS + 8), ea.EA_ERR_INVALID_ARG), (dict(v=None), ea.EA_ERR_INVALID_ARG),
@@ -277,7 +277,7 @@ OK_CACHE = ea.Cache(4, 16, 2, 64)
     (dict(cache=None), ea.EA_ERR_INVALID_ARG), (dict(ks=ea.Strides(127, 64)), ea.EA_ERR_INVALID_ARG),
     (dict(tokens=0), ea.EA_OK)])
 def test_rows_abi(change, code):
-    a = dict(cache=ADDRESS, table=c_table(), tokens=1, dtype=0, rows=ADDRESS, positions=ADDRESS, k=ADDRESS,
+    a = dict(cache=ADDRESS, table=c_table(), ids=ADDRESS, tokens=1, dtype=0, rows=ADDRESS, positions=ADDRESS, k=ADDRESS,
              ks=ea.Strides(128, 64), v=ADDRESS, vs=ea.Strides(128, 64))
     a.update(change)
     for f in (ea._lib.entmax_cache_append, ea._lib.entmax_cache_read):
@@ -292,7 +292,7 @@ def test_rows_abi(change, code):
     (dict(lengths_out=None), ea.EA_ERR_INVALID_ARG), (dict(missing=None), ea.EA_ERR_INVALID_ARG),
     (dict(workspace=None), ea.EA_ERR_INVALID_ARG), (dict(nbytes=64), ea.EA_ERR_WORKSPACE), (dict(rows=0), ea.EA_OK)])
 def test_update_abi(change, code):
-    a = dict(layers=1, cache=ADDRESS, table=c_table(), lengths=ADDRESS, rows=3, parents=ADDRESS, counts=ADDRESS,
+    a = dict(layers=1, cache=ADDRESS, table=c_table(), ids=ADDRESS, lengths=ADDRESS, rows=3, parents=ADDRESS, counts=ADDRESS,
              table_out=ADDRESS, out_stride=4, lengths_out=ADDRESS, missing=ADDRESS, workspace=ADDRESS, nbytes=1 << 20)
     a.update(change)
     assert ea._lib.entmax_cache_update(OK_CACHE, *a.values(), None) == code
@@ -309,7 +309,7 @@ def test_update_abi(change, code):
     (dict(o=ADDRESS + 4), ea.EA_ERR_INVALID_ARG), (dict(workspace=None), ea.EA_ERR_INVALID_ARG),
     (dict(nbytes=1000), ea.EA_ERR_WORKSPACE), (dict(shape=ea.PagedShape(0, 4, 0, 64)), ea.EA_OK)])
 def test_decode_abi(change, code):
-    a = dict(shape=ea.PagedShape(2, 4, 0, 64), alpha=1.5, cache=ADDRESS, table=c_table(), q=ADDRESS, qs=ea.Strides(256, 64),
+    a = dict(shape=ea.PagedShape(2, 4, 0, 64), alpha=1.5, cache=ADDRESS, table=c_table(), ids=ADDRESS, q=ADDRESS, qs=ea.Strides(256, 64),
              lengths=ADDRESS, rows=None, o=ADDRESS, os=ea.Strides(256, 64), workspace=ADDRESS, nbytes=1 << 24)
     a.update(change)
     p = ea.make_params(a.pop("alpha"))
