@@ -1290,8 +1290,7 @@ ea_status check_paged(const ea_paged_shape* s, const ea_cache* c, PagedArgs* a) 
 size_t paged_parts(void* base, PagedArgs* a) {
   const size_t lists = (size_t)a->queries * a->heads * a->regions;
   Parts p{static_cast<char*>(base)};
-  a->top = p.take<float>(lists);
-  a->listed = p.take<int32_t>(lists);
+  a->tops = p.take<u32x4_t>(lists);
   a->list = p.take<u32x2_t>(lists * PAGED_REGION);
   return p.at;
 }

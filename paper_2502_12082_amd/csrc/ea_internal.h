@@ -250,6 +250,7 @@ constexpr int UPDATE_MARKS = 1;
 // regions of PAGED_REGION.
 constexpr int PAGED_REGION = 1024;
 typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 struct PagedArgs {
   PageDims c;
   PageTable t;
@@ -261,10 +262,10 @@ struct PagedArgs {
   const int32_t* rows;     // [queries], or null: row i of query i
   int queries, heads, group, longest, regions;
   // workspace, of every row (query and head) and region of keys: its largest
-  // score, how many of its scores are listed, and those with their keys
-  float* top;       // [queries, heads, regions]
-  int32_t* listed;  // [queries, heads, regions]
-  u32x2_t* list;    // [queries, heads, regions, PAGED_REGION]
+  // score, its bound of tau, how many of its scores are listed (and 0), and those with
+  // their places in the pool
+  u32x4_t* tops;  // [queries, heads, regions]
+  u32x2_t* list;  // [queries, heads, regions, PAGED_REGION]
   float scale_c, alpha, gamma, tol;  // scale_c: (alpha - 1) scale
   int max_iter, gk;
 };

@@ -15,12 +15,14 @@
 // of units, digit 1 that of 32nds of what is left, and so on, each a whole number of at
 // most 16.  A product of a digit and a code has 8 bits, and the sums of a
 // block are exact.  Four digits are within 2^-19 of the largest magnitude (bf16),
-// six within 2^-29 (fp32).  Only scores that can matter are written: those within 1
-// (of x) of the largest of their region of keys, as tau is at least max x - 1.
+// six within 2^-29 (fp32).  Only scores that can matter are written: the largest scores of
+// a region's lanes are scores of distinct keys, so f restricted to them lies below f,
+// and its root is a lower bound of tau.  (Those within 1 of the largest, as
+// tau is at least max x - 1, were ten times as many: 64 requests of up to 9216 keys,
+// 32/8 heads, d = 128, 45 us against 33.)
 //
-// Solve.  One workgroup per query row.  The largest scores of its regions are scores
-// of distinct keys, so f restricted to them lies below f and its root is a lower
-// bound of tau; the listed scores above it go to LDS, tau is solved on them
+// Solve.  One workgroup per query row.  The regions' bounds, and in the same way the
+// largest scores of its regions, bound tau from below; the listed scores above that go to LDS, tau is solved on them
 // (Algorithm 1's iteration), and the rows of V with a probability are gathered.
 // Rows with more scores than fit read their lists for every evaluation.  Lists have an
 // order that depends on the scores alone, and sums one that depends on the lists.
@@ -84,6 +86,7 @@ constexpr int PS_KEYS = PAGED_REGION / PS_WAVES;  // of a wave
 constexpr int PS_TILES = PS_KEYS / PAGE_TILE;
 constexpr int PS_CHUNK = 4;  // tiles that are left out together where a row ends before them
 constexpr int PS_HEADS = 16;  // query heads of a workgroup, the rows of a product
+constexpr int PS_STEPS = 6;   // Newton's steps of a region's bound
 
 template <typename E>
 constexpr int digits() {
@@ -94,6 +97,38 @@ constexpr int digits() {
 // up to four heads fills one of them in every lane.
 __device__ __forceinline__ int row_of_head(int j) { return (j & 3) * 4 + (j >> 2); }
 
+template <int CTRL>
+__device__ __forceinline__ int dpp_int(int v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true);
+#else
+  return v;
+#endif
+}
+
+// A lower bound of tau: the root of f restricted to the scores v of 16 lanes, `top`
+// the largest of them, by Newton's steps from c top - 1 on, which stay below it.  It is
+// less by the sums' rounding, and NaN where the largest is not finite.
+template <int GK>
+__device__ __forceinline__ float region_bound(const float (&v)[PS_WAVES], float top, float c, float gamma) {
+  float lo = c * top - 1.f;
+#pragma unroll 1
+  for (int it = 0; it < PS_STEPS; ++it) {
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int y = 0; y < PS_WAVES; ++y) {
+      float p, u;
+      Gamma<GK>::pu(relu_z(c, v[y], lo), gamma, p, u);
+      s0 += p;
+      s1 += u;
+    }
+    s0 = fold16(s0, addf);
+    s1 = fold16(s1, addf);
+    lo += fmaxf((s0 - 1.f) * __builtin_amdgcn_rcpf(gamma * s1), 0.f);
+  }
+  return lo - 4e-6f * fmaxf(1.f, fabsf(lo));
+}
+
 // R4: registers of a tile's scores, heads 4 at a time.
 template <typename E, int D, int R4>
 __global__ __launch_bounds__(PS_NT) void paged_scores_kernel(PagedArgs a, int head_tiles) {
@@ -101,7 +136,7 @@ __global__ __launch_bounds__(PS_NT) void paged_scores_kernel(PagedArgs a, int he
   constexpr int SB = D / 32;
   __shared__ __attribute__((aligned(16))) uint8_t dig[T][PS_HEADS][D];
   __shared__ uint8_t unit[T][PS_HEADS][SB];
-  __shared__ float wave_top[PS_WAVES][PS_HEADS];
+  __shared__ float lane_top[PS_WAVES][PS_HEADS][16];
   __shared__ int wave_count[PS_WAVES][PS_HEADS];
   const int t = threadIdx.x, lane = lane_id(), w = wave_id(), col = lane & 15, g = lane >> 4;
   int x = blockIdx.x;
@@ -128,7 +163,7 @@ __global__ __launch_bounds__(PS_NT) void paged_scores_kernel(PagedArgs a, int he
       const int page = max(__builtin_amdgcn_readlane(ids, u), 0);
       const uint8_t* const tile = a.cache + tile_at(a.c, page, kv, false, k0 + u * PAGE_TILE);
       const int part = D == 128 ? g : g & 1;
-      kf[u] = *reinterpret_cast<const i32x4*>(tile + (uint32_t)(col * (D / 2) + part * 16));
+      kf[u] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(tile + (uint32_t)(col * (D / 2) + part * 16)));
       ks[u] = tile[(uint32_t)(PAGE_TILE * (D / 2) + col * SB + part)];
     }
   }
@@ -227,67 +262,62 @@ __global__ __launch_bounds__(PS_NT) void paged_scores_kernel(PagedArgs a, int he
     }
   }
 
-  // ---- the region's largest, and what is within 1 / c of it
+  // ---- a lower bound of tau from the largest scores of the lanes, which are scores of
+  // 64 keys of the region: Newton's steps on f restricted to them, from max x - 1
 #pragma unroll
-  for (int r = 0; r < R4; ++r) {
-    top[r] = fold16(top[r], maxf);
-    if (col == 0) wave_top[w][g + 4 * r] = top[r];
-  }
+  for (int r = 0; r < R4; ++r) lane_top[w][g + 4 * r][col] = top[r];
   __syncthreads();
-  const float reach = 1.0001f / a.scale_c;
+  const float c = a.scale_c;
   float bound[R4];
-  int count[R4];
+  int mine[R4], to[R4];  // the lane's scores above it, one bit each, and where they go in the wave's
 #pragma unroll
   for (int r = 0; r < R4; ++r) {
-    const int j = g + 4 * r;
-    top[r] = fmaxf(fmaxf(wave_top[0][j], wave_top[1][j]), fmaxf(wave_top[2][j], wave_top[3][j]));
-    bound[r] = j < heads ? top[r] - reach : INFINITY;
-    count[r] = 0;
+    float v[PS_WAVES];
+#pragma unroll
+    for (int y = 0; y < PS_WAVES; ++y) v[y] = lane_top[y][g + 4 * r][col];
+    top[r] = fold16(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), maxf);
+    const float lo = a.gk == 1   ? region_bound<1>(v, top[r], c, a.gamma)
+                     : a.gk == 2 ? region_bound<2>(v, top[r], c, a.gamma)
+                     : a.gk == 4 ? region_bound<4>(v, top[r], c, a.gamma)
+                                 : region_bound<0>(v, top[r], c, a.gamma);
+    bound[r] = g + 4 * r < heads ? lo : INFINITY;
+    mine[r] = 0;
+#pragma unroll
+    for (int u = 0; u < PS_TILES; ++u) mine[r] |= relu_z(c, s[u][r], bound[r]) > 0.f ? 1 << u : 0;
+    // (sums over the lanes of 16 up to each)
+    const int n = __popc(mine[r]);
+    int incl = n;
+    incl += dpp_int<0x111>(incl);  // row_shr 1, 2, 4, 8
+    incl += dpp_int<0x112>(incl);
+    incl += dpp_int<0x114>(incl);
+    incl += dpp_int<0x118>(incl);
+    to[r] = incl - n;
+    if (col == 15) wave_count[w][g + 4 * r] = incl;
   }
-  auto among = [&](bool keep) { return (uint32_t)(__ballot(keep) >> (16 * g)) & 0xFFFFu; };
-#pragma unroll
-  for (int u = 0; u < PS_TILES; ++u)
-#pragma unroll
-    for (int r = 0; r < R4; ++r) count[r] += __popc(among(s[u][r] > bound[r]));
-#pragma unroll
-  for (int r = 0; r < R4; ++r)
-    if (col == 0) wave_count[w][g + 4 * r] = count[r];
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < R4; ++r) {
     const int j = g + 4 * r;
-    if (j >= heads) continue;
-    const int64_t list = ((int64_t)i * a.heads + h0 + j) * a.regions + region;
-    int to = 0, all = 0;
+    const int64_t list = ((int64_t)i * a.heads + h0 + min(j, heads - 1)) * a.regions + region;
+    int all = 0;
 #pragma unroll
     for (int y = 0; y < PS_WAVES; ++y) {
-      to += y < w ? wave_count[y][j] : 0;
-      all += wave_count[y][j];
+      const int n = wave_count[y][j];
+      to[r] += y < w ? n : 0;
+      all += n;
     }
-    if (w == 0 && col == 0) {
-      a.top[list] = top[r];
-      a.listed[list] = all;
-    }
-    count[r] = to;
-  }
+    if (w == 0 && col == 0 && j < heads)
+      a.tops[list] = u32x4_t{__float_as_uint(top[r]), __float_as_uint(bound[r]), (uint32_t)all, 0};
+    u32x2_t* at = a.list + list * PAGED_REGION + to[r];
 #pragma unroll
-  for (int u = 0; u < PS_TILES; ++u) {
-    if (k0 + u * PAGE_TILE >= len) break;
-    const int at = k0 + u * PAGE_TILE;
-    // where the key lies in the pool
-    const uint32_t slot = ((uint32_t)__builtin_amdgcn_readlane(ids, u) << a.c.shift) +
-                          (uint32_t)(at & ((1 << a.c.shift) - 1)) + col;
-#pragma unroll
-    for (int r = 0; r < R4; ++r) {
-      const bool keep = s[u][r] > bound[r];
-      const uint32_t m = among(keep);
-      if (keep) {
-        const int64_t list = ((int64_t)i * a.heads + h0 + g + 4 * r) * a.regions + region;
-        u32x2_t entry = {__float_as_uint(s[u][r]), slot};
-        a.list[list * PAGED_REGION + count[r] + __popc(m & ((1u << col) - 1))] = entry;
+    for (int u = 0; u < PS_TILES; ++u)
+      if (mine[r] & 1 << u) {
+        // (where the key lies in the pool)
+        const int key = k0 + u * PAGE_TILE;
+        const uint32_t slot = ((uint32_t)__builtin_amdgcn_readlane(ids, u) << a.c.shift) +
+                              (uint32_t)(key & ((1 << a.c.shift) - 1)) + col;
+        *at++ = u32x2_t{__float_as_uint(s[u][r]), slot};
       }
-      count[r] += __popc(m);
-    }
   }
 }
 
@@ -310,17 +340,28 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
   // (heads of one key head are kv_heads apart: with eight of them, on one XCD)
   const int i = blockIdx.x / a.heads, y = blockIdx.x % a.heads;
   const int kv = y % a.c.kv_heads, h = kv * a.group + y / a.c.kv_heads;
-  const int len = query_length(a, i), regions = (len + PAGED_REGION - 1) / PAGED_REGION;
   const int64_t row = ((int64_t)i * a.heads + h) * a.regions;
   E* const O = static_cast<E*>(a.o) + i * a.o_row + h * a.o_head;
   const float c = a.scale_c, gm = a.gamma;
 
   // ---- the regions' largest scores: in every wave
-  float top[MAX_REGIONS / 64], m = -INFINITY;
+  // (read before the length has come: those behind it are not looked at)
+  float top[MAX_REGIONS / 64], m = -INFINITY, lo = -INFINITY;
+  int listed[MAX_REGIONS / 64];
+  u32x4_t found[MAX_REGIONS / 64];
 #pragma unroll
   for (int e = 0; e < MAX_REGIONS / 64; ++e) {
-    top[e] = 64 * e + lane < regions ? a.top[row + 64 * e + lane] : -INFINITY;
+    found[e] = u32x4_t{0, 0, 0, 0};
+    if (64 * e + lane < a.regions) found[e] = a.tops[row + 64 * e + lane];
+  }
+  const int len = query_length(a, i), regions = (len + PAGED_REGION - 1) / PAGED_REGION;
+#pragma unroll
+  for (int e = 0; e < MAX_REGIONS / 64; ++e) {
+    const bool there = 64 * e + lane < regions;
+    top[e] = there ? __uint_as_float(found[e][0]) : -INFINITY;
+    listed[e] = (int)found[e][2];
     m = fmaxf(m, top[e]);
+    if (there) lo = fmaxf(lo, __uint_as_float(found[e][1]));  // (the best of the regions' bounds)
   }
   m = c * fold64(m, maxf);
   if (!(m > -INFINITY && m < INFINITY)) {  // no keys, or none with a finite score
@@ -339,7 +380,7 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
       if constexpr (GK == 0) s2 += u / z;
     }
   };
-  float lo = m - 1.f;
+  lo = fmaxf(fold64(lo, maxf), m - 1.f);
   for (int it = 0; it < 8; ++it) {
     float s0 = 0.f, s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -347,10 +388,13 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
     s0 = fold64(s0, addf);
     s1 = fold64(s1, addf);
     const float step = (s0 - 1.f) * __builtin_amdgcn_rcpf(gm * s1);
-    if (!(step > 1e-3f)) break;
+    if (!(step > 1e-3f)) break;  // (no key is above it where s1 is 0)
     lo += step;
+    if (it == 7 || !(step > 1e-2f)) {
+      lo -= 4e-6f * fmaxf(1.f, fabsf(lo));  // (the sums' rounding)
+      break;
+    }
   }
-  lo -= 4e-6f * fmaxf(1.f, fabsf(lo));  // (the sums' rounding)
 
   // ---- the listed scores above the bound.  With fewer regions than waves several waves
   // share a region's list, 64 entries at a time in turn.
@@ -359,11 +403,10 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
   auto each = [&](auto&& use) {
     for (int x = w; x < regions * parts; x += WAVES) {
       const int region = x / parts;
-      float best = top[0];
-      if constexpr (MAX_REGIONS > 64) best = region < 64 ? top[0] : top[1];
-      best = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(best), region & 63));
-      if (!(relu_z(c, best, lo) > 0.f)) continue;
-      const int n = a.listed[row + region];
+      static_assert(MAX_REGIONS == 128, "two for each lane");
+      const float best = region < 64 ? top[0] : top[1];
+      if (!(relu_z(c, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(best), region & 63)), lo) > 0.f)) continue;
+      const int n = __builtin_amdgcn_readlane(region < 64 ? listed[0] : listed[1], region & 63);
       const u32x2_t* const list = a.list + (row + region) * PAGED_REGION;
       for (int e0 = 64 * (x % parts); e0 < n; e0 += 64 * parts) {
         u32x2_t v = {0xFF800000u, 0};  // (-inf)
