@@ -4,7 +4,7 @@
 // For head h of query i, with keys k_j of its row of the table:
 //   x_j = (alpha - 1) scale <q, k_j>,  tau: sum_j [x_j - tau]_+^gamma = 1,
 //   o = sum_j [x_j - tau]_+^gamma v_j.
-// Two kernels:
+// Two kernels, or for short rows one that does both:
 //
 // Scores.  <q, k> comes from the matrix cores' product of 8-bit and 4-bit
 // operands with a scale for every 32 values: K's codes and scales are its operands
@@ -47,6 +47,7 @@ __device__ __forceinline__ float dpp(float v) {
 #endif
 }
 constexpr int QUAD_1032 = 0xB1, QUAD_2301 = 0x4E, HALF_MIRROR = 0x141, MIRROR = 0x140;
+constexpr int ROW_ROR_4 = 0x124, ROW_ROR_8 = 0x128;
 template <typename F>
 __device__ __forceinline__ float fold8(float v, F&& f) {
   v = f(v, dpp<QUAD_1032>(v));
@@ -58,9 +59,9 @@ __device__ __forceinline__ float fold16(float v, F&& f) {
   v = fold8(v, f);
   return f(v, dpp<MIRROR>(v));
 }
+// over the four lanes that are 16 apart
 template <typename F>
-__device__ __forceinline__ float fold64(float v, F&& f) {
-  v = fold16(v, f);
+__device__ __forceinline__ float fold_rows(float v, F&& f) {
 #if defined(__HIP_DEVICE_COMPILE__)
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
@@ -68,6 +69,10 @@ __device__ __forceinline__ float fold64(float v, F&& f) {
   float lo, hi;
   wave_halves(v, lo, hi);
   return f(lo, hi);
+}
+template <typename F>
+__device__ __forceinline__ float fold64(float v, F&& f) {
+  return fold_rows(fold16(v, f), f);
 }
 __device__ __forceinline__ float addf(float a, float b) { return a + b; }
 __device__ __forceinline__ float maxf(float a, float b) { return fmaxf(a, b); }
@@ -114,7 +119,7 @@ __device__ __forceinline__ int dpp_int(int v) {
 // the largest of them, by Newton's steps from c top - 1 on, which stay below it.  It is
 // less by the sums' rounding, and NaN where the largest is not finite.
 template <int GK>
-__device__ __forceinline__ float region_bound(const float (&v)[PS_WAVES], float top, float c, float gamma) {
+__device__ __forceinline__ float region_bound_of(const float (&v)[PS_WAVES], float top, float c, float gamma) {
   float lo = c * top - 1.f;
 #pragma unroll 1
   for (int it = 0; it < PS_STEPS; ++it) {
@@ -132,17 +137,187 @@ __device__ __forceinline__ float region_bound(const float (&v)[PS_WAVES], float 
   }
   return lo - 4e-6f * fmaxf(1.f, fabsf(lo));
 }
+__device__ __forceinline__ float region_bound(const PagedArgs& a, const float (&v)[PS_WAVES], float top) {
+  switch (a.gk) {
+    case 1: return region_bound_of<1>(v, top, a.scale_c, a.gamma);
+    case 2: return region_bound_of<2>(v, top, a.scale_c, a.gamma);
+    case 4: return region_bound_of<4>(v, top, a.scale_c, a.gamma);
+  }
+  return region_bound_of<0>(v, top, a.scale_c, a.gamma);
+}
 
-// R4: registers of a tile's scores, heads 4 at a time.
+// Queries in digits: `heads` of them from head h0 of query i on.
+template <typename E, int D>
+struct Digits {
+  static constexpr int T = digits<E>();
+  uint8_t digit[T][PS_HEADS][D];
+  uint8_t unit[T][PS_HEADS][D / 32];
+
+  template <int NT>
+  __device__ __forceinline__ void take(const PagedArgs& a, int i, int h0, int heads) {
+    for (int c = threadIdx.x; c < heads * (D / 4); c += NT) {
+      const int j = c / (D / 4), at = c % (D / 4) * 4;
+      const E* const p = static_cast<const E*>(a.q) + i * a.q_row + (h0 + j) * a.q_head + at;
+      float y[4];
+      if constexpr (sizeof(E) == 2) {
+        const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          y[2 * e] = __uint_as_float(v[e] << 16);
+          y[2 * e + 1] = __uint_as_float(v[e] & 0xFFFF0000u);
+        }
+      } else {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = v[e];
+      }
+      // (non-negative floats compare as integers do; NaN is the largest)
+      uint32_t m = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m = max(m, __float_as_uint(y[e]) & 0x7FFFFFFFu);
+      m = __float_as_uint(fold8(__uint_as_float(m), [](float p, float q) {
+        return __uint_as_float(max(__float_as_uint(p), __float_as_uint(q)));
+      }));
+      const int e0 = (int)(m >> 23);  // units of 2^(e0 - 127 - 3)
+      const bool finite = e0 != 255;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = finite ? ldexpf(y[e], 130 - e0) : 0.f;
+      const int r = row_of_head(j);
+#pragma unroll
+      for (int d = 0; d < T; ++d) {
+        float n[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          n[e] = rintf(y[e]);
+          y[e] = (y[e] - n[e]) * 32.f;
+        }
+        int word = 0;
+#if defined(__HIP_DEVICE_COMPILE__)
+        word = __builtin_amdgcn_cvt_pk_fp8_f32(n[0], n[1], word, false);
+        word = __builtin_amdgcn_cvt_pk_fp8_f32(n[2], n[3], word, true);
+#endif
+        const int scale = e0 - 3 - 5 * d;  // (digits under 2^-127 are dropped)
+        *reinterpret_cast<int*>(&digit[d][r][at]) = scale < 0 ? 0 : word;
+        if ((c & 7) == 0) unit[d][r][at / 32] = finite ? (uint8_t)max(scale, 0) : 255;
+      }
+    }
+  }
+};
+
+// A wave's TILES tiles of keys, tile u from key k0 + u step on, against up to 16 heads:
+// R4 registers of scores to a tile, heads 4 at a time.
+template <typename E, int D, int R4, int TILES>
+struct WaveKeys {
+  static constexpr int T = digits<E>(), NM = T * D / 128;  // products of a tile
+  static constexpr int SB = D / 32, AHEAD = TILES < PS_AHEAD ? TILES : PS_AHEAD;
+  static_assert(TILES <= 16 && TILES % PS_CHUNK == 0, "a lane of 16 for each tile's page");
+  const PagedArgs& a;
+  const int kv, k0, step, len, col, g;
+  int ids;  // page of tile `col`, -1 where there is none
+  i32x4 kf[AHEAD];
+  int ks[AHEAD];
+
+  __device__ __forceinline__ WaveKeys(const PagedArgs& args, int i, int kv_head, int first, int apart, int length)
+      : a(args), kv(kv_head), k0(first), step(apart), len(length), col(lane_id() & 15), g(lane_id() >> 4) {
+    const int key = k0 + col * step;
+    ids = col < TILES && key < len ? page_of(a.c, a.t, query_row(a, i), key) : -1;
+#pragma unroll
+    for (int c = 0; c < AHEAD; c += PS_CHUNK) load(c);
+  }
+  __device__ __forceinline__ void load(int c) {  // chunk c of the tiles
+    if (k0 + c * step >= len) return;
+#pragma unroll
+    for (int u = c; u < c + PS_CHUNK; ++u) {
+      // (a tile without a page reads the first one's, and its scores are dropped)
+      const int page = max(__builtin_amdgcn_readlane(ids, u), 0);
+      const uint8_t* const tile = a.cache + tile_at(a.c, page, kv, false, k0 + u * step);
+      const int part = D == 128 ? g : g & 1;
+      kf[u % AHEAD] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(tile + (uint32_t)(col * (D / 2) + part * 16)));
+      ks[u % AHEAD] = tile[(uint32_t)(PAGE_TILE * (D / 2) + col * SB + part)];
+    }
+  }
+  // s: of head g + 4 r and the tiles' key `col` (-inf: none); top: the lane's largest
+  __device__ __forceinline__ void scores(const Digits<E, D>& q, float (&s)[TILES][R4], float (&top)[R4]) {
+    // A operands: of 128 values a lane holds 16 g .. and 64 + 16 g .., and the scale
+    // of block g; at D = 64 two digits are one operand, K's row twice the other
+    i32x8 qf[NM];
+    int qs[NM];
+#pragma unroll
+    for (int m = 0; m < NM; ++m) {
+      const i32x4 lo = *reinterpret_cast<const i32x4*>(D == 128 ? &q.digit[m][col][16 * g] : &q.digit[2 * m][col][16 * g]);
+      const i32x4 hi = *reinterpret_cast<const i32x4*>(D == 128 ? &q.digit[m][col][64 % D + 16 * g]
+                                                                : &q.digit[(2 * m + 1) % T][col][16 * g]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        qf[m][e] = lo[e];
+        qf[m][4 + e] = hi[e];
+      }
+      qs[m] = D == 128 ? q.unit[m][col][g % SB] : q.unit[(2 * m + (g >> 1)) % T][col][g & 1];
+    }
+#pragma unroll
+    for (int u = 0; u < TILES; ++u)
+#pragma unroll
+      for (int r = 0; r < R4; ++r) s[u][r] = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < R4; ++r) top[r] = -INFINITY;
+#pragma unroll
+    for (int c = 0; c < TILES; c += PS_CHUNK) {
+      if (k0 + c * step >= len) break;
+#pragma unroll
+      for (int u = c; u < c + PS_CHUNK; ++u) {
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#if defined(__HIP_DEVICE_COMPILE__)
+        const i32x4 kw = kf[u % AHEAD];
+        const i32x8 k = {kw[0], kw[1], kw[2], kw[3], 0, 0, 0, 0};
+#pragma unroll
+        for (int m = NM - 1; m >= 0; --m)  // (the smallest first)
+          v = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(qf[m], k, v, 0, 4, 0, qs[m], 0, ks[u % AHEAD]);
+#endif
+        const bool ok = k0 + u * step + col < len && __builtin_amdgcn_readlane(ids, u) >= 0;
+#pragma unroll
+        for (int r = 0; r < R4; ++r) {
+          s[u][r] = ok ? v[r] : -INFINITY;
+          top[r] = fmaxf(top[r], s[u][r]);  // (a NaN is left out)
+        }
+      }
+      if (c + AHEAD < TILES) load(c + AHEAD);
+    }
+  }
+  // where the lane's key of tile u lies in the pool
+  __device__ __forceinline__ uint32_t slot(int u) const {
+    return ((uint32_t)__builtin_amdgcn_readlane(ids, u) << a.c.shift) +
+           (uint32_t)((k0 + u * step) & ((1 << a.c.shift) - 1)) + col;
+  }
+  // The lane's scores above `bound`, a bit for each tile; where they go among those of the
+  // 16 lanes of its row, and how many these have (in the last of them).
+  __device__ __forceinline__ static int above(const float (&s)[TILES][R4], int r, float c, float bound, int& to, int& all) {
+    int mine = 0;
+#pragma unroll
+    for (int u = 0; u < TILES; ++u) mine |= relu_z(c, s[u][r], bound) > 0.f ? 1 << u : 0;
+    const int n = __popc(mine);
+    all = n;
+    all += dpp_int<0x111>(all);  // row_shr 1, 2, 4, 8: sums over the lanes up to each
+    all += dpp_int<0x112>(all);
+    all += dpp_int<0x114>(all);
+    all += dpp_int<0x118>(all);
+    to = all - n;
+    return mine;
+  }
+  __device__ __forceinline__ void write(const float (&s)[TILES][R4], int r, int mine, u32x2_t* at) const {
+#pragma unroll
+    for (int u = 0; u < TILES; ++u)
+      if (mine & 1 << u) *at++ = u32x2_t{__float_as_uint(s[u][r]), slot(u)};
+  }
+};
+
+// A workgroup per region of keys, query, key head and 16 of its query heads.
 template <typename E, int D, int R4>
 __global__ __launch_bounds__(PS_NT) void paged_scores_kernel(PagedArgs a, int head_tiles) {
-  constexpr int T = digits<E>(), NM = T * D / 128;  // products of a tile
-  constexpr int SB = D / 32;
-  __shared__ __attribute__((aligned(16))) uint8_t dig[T][PS_HEADS][D];
-  __shared__ uint8_t unit[T][PS_HEADS][SB];
+  using W = WaveKeys<E, D, R4, PS_TILES>;
+  __shared__ __attribute__((aligned(16))) Digits<E, D> q;
   __shared__ float lane_top[PS_WAVES][PS_HEADS][16];
   __shared__ int wave_count[PS_WAVES][PS_HEADS];
-  const int t = threadIdx.x, lane = lane_id(), w = wave_id(), col = lane & 15, g = lane >> 4;
+  const int lane = lane_id(), w = wave_id(), col = lane & 15, g = lane >> 4;
   int x = blockIdx.x;
   const int kv = x % a.c.kv_heads;
   x /= a.c.kv_heads;
@@ -152,155 +327,30 @@ __global__ __launch_bounds__(PS_NT) void paged_scores_kernel(PagedArgs a, int he
   const int len = query_length(a, i), first = region * PAGED_REGION;
   if (first >= len) return;
   const int heads = min(PS_HEADS, a.group - ht * PS_HEADS), h0 = kv * a.group + ht * PS_HEADS;
-
-  // ---- the wave's tiles: their pages, then their loads
-  const int k0 = first + w * PS_KEYS, row = query_row(a, i);
-  const int ids = col < PS_TILES && k0 + col * PAGE_TILE < len ? page_of(a.c, a.t, row, k0 + col * PAGE_TILE) : -1;
-  i32x4 kf[PS_AHEAD];
-  int ks[PS_AHEAD];
-  // chunk c of the wave's tiles
-  auto load = [&](int c) {
-    if (k0 + c * PAGE_TILE >= len) return;
-#pragma unroll
-    for (int u = c; u < c + PS_CHUNK; ++u) {
-      // (a tile without a page reads the first one's, and its scores are dropped)
-      const int page = max(__builtin_amdgcn_readlane(ids, u), 0);
-      const uint8_t* const tile = a.cache + tile_at(a.c, page, kv, false, k0 + u * PAGE_TILE);
-      const int part = D == 128 ? g : g & 1;
-      kf[u % PS_AHEAD] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(tile + (uint32_t)(col * (D / 2) + part * 16)));
-      ks[u % PS_AHEAD] = tile[(uint32_t)(PAGE_TILE * (D / 2) + col * SB + part)];
-    }
-  };
-#pragma unroll
-  for (int c = 0; c < PS_AHEAD; c += PS_CHUNK) load(c);
-
-  // ---- the digits of the queries
-  for (int c = t; c < heads * (D / 4); c += PS_NT) {
-    const int j = c / (D / 4), at = c % (D / 4) * 4;
-    const E* const p = static_cast<const E*>(a.q) + i * a.q_row + (h0 + j) * a.q_head + at;
-    float y[4];
-    if constexpr (sizeof(E) == 2) {
-      const u32x2 v = *reinterpret_cast<const u32x2*>(p);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        y[2 * e] = __uint_as_float(v[e] << 16);
-        y[2 * e + 1] = __uint_as_float(v[e] & 0xFFFF0000u);
-      }
-    } else {
-      const f32x4 v = *reinterpret_cast<const f32x4*>(p);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = v[e];
-    }
-    // (non-negative floats compare as integers do; NaN is the largest)
-    uint32_t m = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) m = max(m, __float_as_uint(y[e]) & 0x7FFFFFFFu);
-    m = __float_as_uint(fold8(__uint_as_float(m), [](float p, float q) {
-      return __uint_as_float(max(__float_as_uint(p), __float_as_uint(q)));
-    }));
-    const int e0 = (int)(m >> 23);  // units of 2^(e0 - 127 - 3)
-    const bool finite = e0 != 255;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = finite ? ldexpf(y[e], 130 - e0) : 0.f;
-    const int r = row_of_head(j);
-#pragma unroll
-    for (int d = 0; d < T; ++d) {
-      float n[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        n[e] = rintf(y[e]);
-        y[e] = (y[e] - n[e]) * 32.f;
-      }
-      int word = 0;
-#if defined(__HIP_DEVICE_COMPILE__)
-      word = __builtin_amdgcn_cvt_pk_fp8_f32(n[0], n[1], word, false);
-      word = __builtin_amdgcn_cvt_pk_fp8_f32(n[2], n[3], word, true);
-#endif
-      const int scale = e0 - 3 - 5 * d;  // (digits under 2^-127 are dropped)
-      *reinterpret_cast<int*>(&dig[d][r][at]) = scale < 0 ? 0 : word;
-      if ((c & 7) == 0) unit[d][r][at / 32] = finite ? (uint8_t)max(scale, 0) : 255;
-    }
-  }
+  W keys(a, i, kv, first + w * PS_KEYS, PAGE_TILE, len);
+  q.template take<PS_NT>(a, i, h0, heads);
   __syncthreads();
-  // A operands: of 128 values a lane holds 16 g .. and 64 + 16 g .., and the scale
-  // of block g; at D = 64 two digits are one operand, K's row twice the other
-  i32x8 qf[NM];
-  int qs[NM];
-#pragma unroll
-  for (int m = 0; m < NM; ++m) {
-    const i32x4 lo = *reinterpret_cast<const i32x4*>(D == 128 ? &dig[m][col][16 * g] : &dig[2 * m][col][16 * g]);
-    const i32x4 hi = *reinterpret_cast<const i32x4*>(D == 128 ? &dig[m][col][64 % D + 16 * g] : &dig[(2 * m + 1) % T][col][16 * g]);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      qf[m][e] = lo[e];
-      qf[m][4 + e] = hi[e];
-    }
-    qs[m] = D == 128 ? unit[m][col][g % SB] : unit[(2 * m + (g >> 1)) % T][col][g & 1];
-  }
-
-  // ---- scores of head g + 4 r and the tile's key `col`
-  float s[PS_TILES][R4];
-#pragma unroll
-  for (int u = 0; u < PS_TILES; ++u)
-#pragma unroll
-    for (int r = 0; r < R4; ++r) s[u][r] = -INFINITY;
-  float top[R4];
-#pragma unroll
-  for (int r = 0; r < R4; ++r) top[r] = -INFINITY;
-#pragma unroll
-  for (int c = 0; c < PS_TILES; c += PS_CHUNK) {
-    if (k0 + c * PAGE_TILE >= len) break;
-#pragma unroll
-    for (int u = c; u < c + PS_CHUNK; ++u) {
-      f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#if defined(__HIP_DEVICE_COMPILE__)
-      const i32x4 kw = kf[u % PS_AHEAD];
-      const i32x8 k = {kw[0], kw[1], kw[2], kw[3], 0, 0, 0, 0};
-#pragma unroll
-      for (int m = NM - 1; m >= 0; --m)  // (the smallest first)
-        v = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(qf[m], k, v, 0, 4, 0, qs[m], 0, ks[u % PS_AHEAD]);
-#endif
-      const bool ok = k0 + u * PAGE_TILE + col < len && __builtin_amdgcn_readlane(ids, u) >= 0;
-#pragma unroll
-      for (int r = 0; r < R4; ++r) {
-        s[u][r] = ok ? v[r] : -INFINITY;
-        top[r] = fmaxf(top[r], s[u][r]);  // (a NaN is left out)
-      }
-    }
-    if (c + PS_AHEAD < PS_TILES) load(c + PS_AHEAD);
-  }
-
+  float s[PS_TILES][R4], top[R4];
+  keys.scores(q, s, top);
   // ---- a lower bound of tau from the largest scores of the lanes, which are scores of
-  // 64 keys of the region: Newton's steps on f restricted to them, from max x - 1
+  // 64 keys of the region, and what is above it
 #pragma unroll
   for (int r = 0; r < R4; ++r) lane_top[w][g + 4 * r][col] = top[r];
   __syncthreads();
-  const float c = a.scale_c;
+  // (every wave by itself: with a barrier more instead the longest rows took 33.6 us, 32.5 so)
   float bound[R4];
-  int mine[R4], to[R4];  // the lane's scores above it, one bit each, and where they go in the wave's
+  int mine[R4], to[R4];
 #pragma unroll
   for (int r = 0; r < R4; ++r) {
     float v[PS_WAVES];
 #pragma unroll
     for (int y = 0; y < PS_WAVES; ++y) v[y] = lane_top[y][g + 4 * r][col];
     top[r] = fold16(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), maxf);
-    const float lo = a.gk == 1   ? region_bound<1>(v, top[r], c, a.gamma)
-                     : a.gk == 2 ? region_bound<2>(v, top[r], c, a.gamma)
-                     : a.gk == 4 ? region_bound<4>(v, top[r], c, a.gamma)
-                                 : region_bound<0>(v, top[r], c, a.gamma);
+    const float lo = region_bound(a, v, top[r]);
     bound[r] = g + 4 * r < heads ? lo : INFINITY;
-    mine[r] = 0;
-#pragma unroll
-    for (int u = 0; u < PS_TILES; ++u) mine[r] |= relu_z(c, s[u][r], bound[r]) > 0.f ? 1 << u : 0;
-    // (sums over the lanes of 16 up to each)
-    const int n = __popc(mine[r]);
-    int incl = n;
-    incl += dpp_int<0x111>(incl);  // row_shr 1, 2, 4, 8
-    incl += dpp_int<0x112>(incl);
-    incl += dpp_int<0x114>(incl);
-    incl += dpp_int<0x118>(incl);
-    to[r] = incl - n;
-    if (col == 15) wave_count[w][g + 4 * r] = incl;
+    int all;
+    mine[r] = W::above(s, r, a.scale_c, bound[r], to[r], all);
+    if (col == 15) wave_count[w][g + 4 * r] = all;
   }
   __syncthreads();
 #pragma unroll
@@ -316,16 +366,7 @@ __global__ __launch_bounds__(PS_NT) void paged_scores_kernel(PagedArgs a, int he
     }
     if (w == 0 && col == 0 && j < heads)
       a.tops[list] = u32x4_t{__float_as_uint(top[r]), __float_as_uint(bound[r]), (uint32_t)all, 0};
-    u32x2_t* at = a.list + list * PAGED_REGION + to[r];
-#pragma unroll
-    for (int u = 0; u < PS_TILES; ++u)
-      if (mine[r] & 1 << u) {
-        // (where the key lies in the pool)
-        const int key = k0 + u * PAGE_TILE;
-        const uint32_t slot = ((uint32_t)__builtin_amdgcn_readlane(ids, u) << a.c.shift) +
-                              (uint32_t)(key & ((1 << a.c.shift) - 1)) + col;
-        *at++ = u32x2_t{__float_as_uint(s[u][r]), slot};
-      }
+    keys.write(s, r, mine[r], a.list + list * PAGED_REGION + to[r]);
   }
 }
 
@@ -335,10 +376,138 @@ constexpr int MAX_REGIONS = MAX_SEQLEN / PAGED_REGION;
 constexpr int PV_VALS = 16;   // values of V that a lane takes of a row
 constexpr int PV_BATCH = 4;   // rows of V of a lane in flight
 
+// z^gamma, z^(gamma-1), z^(gamma-2) summed over z > 0
+template <int GK>
+__device__ __forceinline__ void add_z(float z, float gamma, float& s0, float& s1, float& s2) {
+  if (z > 0.f) {
+    float p, u;
+    Gamma<GK>::pu(z, gamma, p, u);
+    s0 += p;
+    s1 += u;
+    if constexpr (GK == 2) s2 += 1.f;
+    if constexpr (GK == 4) s2 += z * z;
+    if constexpr (GK == 0) s2 += u / z;
+  }
+}
+
+// tau of a row of `len` keys from its bound lo on, m the largest x: Algorithm 1's
+// iteration.  sums(tau, s0, s1, s2): of all of the row's scores.
+template <typename F>
+__device__ __forceinline__ float solve_tau(const PagedArgs& a, float lo, float m, int len, F&& sums) {
+  const float gm = a.gamma;
+  float hi = m - exp2f((1.f - a.alpha) * __log2f((float)len));
+  float low = fminf(lo, hi), tau = low;
+  for (int it = 0;; ++it) {
+    float s0 = 0.f, s1 = 0.f, s2 = 0.f;
+    sums(tau, s0, s1, s2);
+    const float f = s0 - 1.f;
+    const bool stop = fabsf(f) <= a.tol || it >= a.max_iter;
+    // B_f, Newton's bound, H_f: the update rules of the attention solver
+    const float f1 = -gm * s1, f2 = gm * (gm - 1.f) * s2;
+    if (f < 0.f)
+      hi = tau;
+    else
+      low = tau;
+    const float slack = 1e-6f * fmaxf(1.f, fmaxf(fabsf(low), fabsf(hi)));
+    if (f1 < 0.f) low = fminf(fmaxf(low, tau - f * __builtin_amdgcn_rcpf(f1) - 10.f * slack), hi);
+    const float th = tau - 2.f * f * f1 * __builtin_amdgcn_rcpf(2.f * f1 * f1 - f * f2);
+    const bool take = th >= low - slack && th <= hi + slack;
+    // (the update from the last evaluation is taken too)
+    tau = take ? fminf(fmaxf(th, low), hi) : th < low ? low : 0.5f * (low + hi);
+    if (stop) return tau;
+  }
+}
+
+// The sum of rows of V times their probabilities: LPK lanes to a row, each 16 values of it
+// (half a block).
+template <int D>
+struct RowSum {
+  static constexpr int LPK = D / PV_VALS, KPW = 64 / LPK;  // lanes of a row, rows of a wave
+  float o[PV_VALS];
+  const uint8_t* V;  // the values of the key head in page 0
+  int64_t page_step;
+  int shift, sub, grp;
+
+  __device__ __forceinline__ RowSum(const PagedArgs& a, int kv)
+      : o{}, V(a.cache + tile_at(a.c, 0, kv, true, 0)), page_step(page_bytes(a.c)), shift(a.c.shift),
+        sub(lane_id() % LPK), grp(lane_id() / LPK) {}
+  // Adds entries (p, place in the pool) list[first], list[first + 1] .. KPW at a time, and then those
+  // `step` behind, up to n.
+  __device__ __forceinline__ void add(const u32x2_t* list, int first, int step, int n) {
+    for (int e0 = first; e0 < n; e0 += step * PV_BATCH) {
+      u32x2 codes[PV_BATCH];
+      float p[PV_BATCH];
+      uint32_t scale[PV_BATCH];
+#pragma unroll
+      for (int u = 0; u < PV_BATCH; ++u) {
+        const u32x2_t v = list[min(e0 + u * step + grp, n - 1)];
+        p[u] = __uint_as_float(v[0]);
+        const int at = (int)(v[1] & ((1u << shift) - 1));
+        const uint8_t* const tile = V + (int64_t)(v[1] >> shift) * page_step + (at >> 4) * tile_bytes(D);
+        codes[u] = *reinterpret_cast<const u32x2*>(tile + (at & 15) * (D / 2) + 8 * sub);
+        scale[u] = tile[PAGE_TILE * (D / 2) + (at & 15) * (D / 32) + sub / 2];
+      }
+#pragma unroll
+      for (int u = 0; u < PV_BATCH; ++u) {
+        if (e0 + u * step >= n) break;
+        // (a row again in the place of none: whatever it holds is not used)
+#if defined(__HIP_DEVICE_COMPILE__)
+        const float ps = e0 + u * step + grp >= n ? 0.f
+                         : scale[u] == 255        ? __builtin_nanf("")
+                                                  : p[u] * __uint_as_float(scale[u] << 23);
+        auto two = [&](int at, auto v) {
+          o[at] = fmaf(ps, v[0], o[at]);
+          o[at + 1] = fmaf(ps, v[1], o[at + 1]);
+        };
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          two(8 * x, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u][x], 1.f, 0));
+          two(8 * x + 2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u][x], 1.f, 1));
+          two(8 * x + 4, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u][x], 1.f, 2));
+          two(8 * x + 6, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u][x], 1.f, 3));
+        }
+#endif
+      }
+    }
+  }
+  // the wave's sums
+  __device__ __forceinline__ void store(float (&sums)[D]) {
+#pragma unroll
+    for (int d = 0; d < PV_VALS; ++d) {
+      // (lanes rotate inside 16, then rows and halves swap: no LDS)
+      if constexpr (LPK == 4) o[d] += dpp<ROW_ROR_4>(o[d]);
+      o[d] = fold_rows(o[d] + dpp<ROW_ROR_8>(o[d]), addf);
+    }
+    if (grp == 0)
+#pragma unroll
+      for (int d = 0; d < PV_VALS; d += 4)
+        *reinterpret_cast<f32x4*>(&sums[sub * PV_VALS + d]) = f32x4{o[d], o[d + 1], o[d + 2], o[d + 3]};
+  }
+};
+
+// Of n entries with scores, those with a probability move to the front, p in place of the
+// score (a wave; no entry is overwritten before it has been read).  Their number.
+template <int GK>
+__device__ __forceinline__ int keep_probable(const PagedArgs& a, u32x2_t* list, int n, float tau) {
+  const int lane = lane_id();
+  int np = 0;
+  for (int e0 = 0; e0 < n; e0 += 64) {
+    u32x2_t v = {0xFF800000u, 0};
+    if (e0 + lane < n) v = list[e0 + lane];
+    const float p = Gamma<GK>::p_only(relu_z(a.scale_c, __uint_as_float(v[0]), tau), a.gamma);
+    const uint64_t k = __ballot(p > 0.f);
+    if (p > 0.f) {
+      v[0] = __float_as_uint(p);
+      list[np + __popcll(k & ((1ull << lane) - 1))] = v;
+    }
+    np += __popcll(k);
+  }
+  return np;
+}
+
 template <typename E, int D, int GK, int NT>
 __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
   constexpr int WAVES = NT / 64, CAP = NT == 64 ? 1024 : 512;  // scores that a wave keeps
-  constexpr int LPK = D / PV_VALS, KPW = 64 / LPK;
   constexpr int ALONE = 8;  // scores per lane that every wave solves by itself
   constexpr int LOADS = 4;
   static_assert(WAVES * CAP * 8 >= WAVES * D * 4, "the waves' sums fit in place of the scores");
@@ -377,23 +546,11 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
     for (int d = t; d < D; d += NT) O[d] = (E)0.f;
     return;
   }
-  // z^gamma, z^(gamma-1), z^(gamma-2) summed over z > 0
-  auto add = [&](float z, float& s0, float& s1, float& s2) {
-    if (z > 0.f) {
-      float p, u;
-      Gamma<GK>::pu(z, gm, p, u);
-      s0 += p;
-      s1 += u;
-      if constexpr (GK == 2) s2 += 1.f;
-      if constexpr (GK == 4) s2 += z * z;
-      if constexpr (GK == 0) s2 += u / z;
-    }
-  };
   lo = fmaxf(fold64(lo, maxf), m - 1.f);
   for (int it = 0; it < 8; ++it) {
     float s0 = 0.f, s1 = 0.f, s2 = 0.f;
 #pragma unroll
-    for (int e = 0; e < MAX_REGIONS / 64; ++e) add(relu_z(c, top[e], lo), s0, s1, s2);
+    for (int e = 0; e < MAX_REGIONS / 64; ++e) add_z<GK>(relu_z(c, top[e], lo), gm, s0, s1, s2);
     s0 = fold64(s0, addf);
     s1 = fold64(s1, addf);
     const float step = (s0 - 1.f) * __builtin_amdgcn_rcpf(gm * s1);
@@ -504,101 +661,28 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
     }
     __syncthreads();  // (a wave that is done writes to its list)
   }
-  float hi = m - powf((float)len, 1.f - a.alpha);
-  float low = fminf(lo, hi), tau = low;
-  for (int it = 0;; ++it) {
-    float s0 = 0.f, s1 = 0.f, s2 = 0.f;
+  const float tau = solve_tau(a, lo, m, len, [&](float tau, float& s0, float& s1, float& s2) {
     if (alone) {
 #pragma unroll
       for (int e = 0; e < ALONE; ++e) {
         if (64 * e >= total) break;
-        add(relu_z(c, own[e], tau), s0, s1, s2);
+        add_z<GK>(relu_z(c, own[e], tau), gm, s0, s1, s2);
       }
       s0 = fold64(s0, addf);
       s1 = fold64(s1, addf);
       s2 = fold64(s2, addf);
     } else if (!wide) {
-      for (int e = lane; e < mine; e += 64) add(relu_z(c, __uint_as_float(kept[w][e][0]), tau), s0, s1, s2);
+      for (int e = lane; e < mine; e += 64) add_z<GK>(relu_z(c, __uint_as_float(kept[w][e][0]), tau), gm, s0, s1, s2);
       sum3(s0, s1, s2);
     } else {
-      each([&](const u32x2_t& v) { add(relu_z(c, __uint_as_float(v[0]), tau), s0, s1, s2); });
+      each([&](const u32x2_t& v) { add_z<GK>(relu_z(c, __uint_as_float(v[0]), tau), gm, s0, s1, s2); });
       sum3(s0, s1, s2);
     }
-    const float f = s0 - 1.f;
-    const bool stop = fabsf(f) <= a.tol || it >= a.max_iter;
-    // B_f, Newton's bound, H_f: the update rules of the attention solver
-    const float f1 = -gm * s1, f2 = gm * (gm - 1.f) * s2;
-    if (f < 0.f)
-      hi = tau;
-    else
-      low = tau;
-    const float slack = 1e-6f * fmaxf(1.f, fmaxf(fabsf(low), fabsf(hi)));
-    if (f1 < 0.f) low = fminf(fmaxf(low, tau - f / f1 - 10.f * slack), hi);
-    const float th = tau - 2.f * f * f1 / (2.f * f1 * f1 - f * f2);
-    const bool take = th >= low - slack && th <= hi + slack;
-    // (the update from the last evaluation is taken too)
-    tau = take ? fminf(fmaxf(th, low), hi) : th < low ? low : 0.5f * (low + hi);
-    if (stop) break;
-  }
+  });
 
-  // ---- O: the rows of V with a probability.  LPK lanes to a row, each 16 values of
-  // it (half a block).
-  float o[PV_VALS] = {};
-  const int sub = lane % LPK, grp = lane / LPK;
-  const uint8_t* const V = a.cache + tile_at(a.c, 0, kv, true, 0);
-  const int64_t page_step = page_bytes(a.c);
-  const int mask = (1 << a.c.shift) - 1;
-  // of the wave's first n kept entries, scores, those with p > 0, p in place of the score
-  auto gather = [&](int n) {
-    int np = 0;
-    for (int e0 = 0; e0 < n; e0 += 64) {
-      u32x2_t v = {0xFF800000u, 0};
-      if (e0 + lane < n) v = kept[w][e0 + lane];
-      const float p = Gamma<GK>::p_only(relu_z(c, __uint_as_float(v[0]), tau), gm);
-      const uint64_t k = __ballot(p > 0.f);
-      if (p > 0.f) {
-        v[0] = __float_as_uint(p);
-        kept[w][np + __popcll(k & before)] = v;
-      }
-      np += __popcll(k);
-    }
-    for (int e0 = 0; e0 < np; e0 += KPW * PV_BATCH) {
-      u32x2 codes[PV_BATCH];
-      float p[PV_BATCH];
-      uint32_t scale[PV_BATCH];
-#pragma unroll
-      for (int u = 0; u < PV_BATCH; ++u) {
-        const int e = e0 + u * KPW + grp;
-        const u32x2_t v = kept[w][min(e, np - 1)];
-        p[u] = __uint_as_float(v[0]);
-        const int at = (int)(v[1] & (uint32_t)mask);
-        const uint8_t* const tile = V + (int64_t)(v[1] >> a.c.shift) * page_step + (at >> 4) * tile_bytes(D);
-        codes[u] = *reinterpret_cast<const u32x2*>(tile + (at & 15) * (D / 2) + 8 * sub);
-        scale[u] = tile[PAGE_TILE * (D / 2) + (at & 15) * (D / 32) + sub / 2];
-      }
-#pragma unroll
-      for (int u = 0; u < PV_BATCH; ++u) {
-        if (e0 + u * KPW >= np) break;
-        // (a row again in the place of none: whatever it holds is not used)
-#if defined(__HIP_DEVICE_COMPILE__)
-        const float ps = e0 + u * KPW + grp >= np ? 0.f
-                         : scale[u] == 255        ? __builtin_nanf("")
-                                                  : p[u] * __uint_as_float(scale[u] << 23);
-        auto two = [&](int at, auto v) {
-          o[at] = fmaf(ps, v[0], o[at]);
-          o[at + 1] = fmaf(ps, v[1], o[at + 1]);
-        };
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          two(8 * x, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u][x], 1.f, 0));
-          two(8 * x + 2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u][x], 1.f, 1));
-          two(8 * x + 4, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u][x], 1.f, 2));
-          two(8 * x + 6, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[u][x], 1.f, 3));
-        }
-#endif
-      }
-    }
-  };
+  // ---- O: the rows of V with a probability
+  RowSum<D> o(a, kv);
+  auto gather = [&](int n) { o.add(kept[w], 0, RowSum<D>::KPW, keep_probable<GK>(a, kept[w], n, tau)); };
   if (!wide) {
     gather(mine);
   } else {
@@ -618,12 +702,7 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
   __syncthreads();
   // sums over the rows of a wave, then over the waves, in place of the scores
   float(&sums)[WAVES][D] = reinterpret_cast<float(&)[WAVES][D]>(kept);
-#pragma unroll
-  for (int d = 0; d < PV_VALS; ++d) {
-#pragma unroll
-    for (int x = LPK; x < 64; x <<= 1) o[d] += __shfl_xor(o[d], x);
-    if (grp == 0) sums[w][sub * PV_VALS + d] = o[d];
-  }
+  o.store(sums[w]);
   __syncthreads();
   for (int d = t; d < D; d += NT) {
     float sum = 0.f;
@@ -633,20 +712,191 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
   }
 }
 
+// ------------------------------------------------------------- short rows
+
+// Both steps in one workgroup per query, key head and 16 of its query heads, for rows of
+// which 16 waves hold all scores at once: no lists in memory (but those of rows with
+// more scores above the bound than fit), and one launch.
+constexpr int SH_NT = 1024, SH_WAVES = SH_NT / 64;
+// Tiles of a wave, which with R4 registers of scores each leave it its 128 registers.  (16
+// of four heads fit too, but from 2048 keys on one compute unit's loads take longer than a
+// second launch: one request of 4096 keys, 16/4 heads, d = 128, 16.3 us against 14.9.)
+constexpr int sh_tiles(int r4) { return r4 <= 2 ? 8 : 4; }
+constexpr int SH_LIST = 1024;  // entries of the heads of one register of scores
+
+// tau of one head from its n listed scores, by one wave; then the list holds those with a
+// probability, and their number comes back.
+template <int GK>
+__device__ __forceinline__ int solve_short(const PagedArgs& a, u32x2_t* list, int n, float lo, float m, int len) {
+  constexpr int ALONE = 8;
+  const int lane = lane_id();
+  float own[ALONE];
+#pragma unroll
+  for (int e = 0; e < ALONE; ++e) own[e] = 64 * e + lane < n ? __uint_as_float(list[64 * e + lane][0]) : -INFINITY;
+  const float tau = solve_tau(a, lo, m, len, [&](float tau, float& s0, float& s1, float& s2) {
+#pragma unroll
+    for (int e = 0; e < ALONE; ++e) {
+      if (64 * e >= n) break;
+      add_z<GK>(relu_z(a.scale_c, own[e], tau), a.gamma, s0, s1, s2);
+    }
+    for (int e = 64 * ALONE + lane; e < n; e += 64)
+      add_z<GK>(relu_z(a.scale_c, __uint_as_float(list[e][0]), tau), a.gamma, s0, s1, s2);
+    s0 = fold64(s0, addf);
+    s1 = fold64(s1, addf);
+    s2 = fold64(s2, addf);
+  });
+  return keep_probable<GK>(a, list, n, tau);
+}
+
+template <typename E, int D, int R4>
+__global__ __launch_bounds__(SH_NT) void paged_short_kernel(PagedArgs a, int head_tiles) {
+  constexpr int TILES = sh_tiles(R4), HEADS = 4 * R4, CAP = SH_LIST / R4;
+  constexpr int WPH = R4 == 1 ? 4 : R4 == 2 ? 2 : 1;  // waves that add up one head's rows of V
+  using W = WaveKeys<E, D, R4, TILES>;
+  __shared__ __attribute__((aligned(16))) Digits<E, D> q;
+  __shared__ float lane_top[SH_WAVES][HEADS][16];
+  __shared__ int wave_count[SH_WAVES][HEADS];
+  __shared__ u32x2_t lists[HEADS][CAP];
+  __shared__ float head_top[HEADS], head_bound[HEADS];
+  __shared__ int head_count[HEADS];
+  static_assert(sizeof(q) >= SH_WAVES * D * sizeof(float), "the waves' sums fit in place of the digits");
+  const int t = threadIdx.x, lane = lane_id(), w = wave_id(), col = lane & 15, g = lane >> 4;
+  int x = blockIdx.x;
+  const int kv = x % a.c.kv_heads;
+  x /= a.c.kv_heads;
+  const int ht = x % head_tiles, i = x / head_tiles;
+  const int len = query_length(a, i);
+  const int heads = min(PS_HEADS, a.group - ht * PS_HEADS), h0 = kv * a.group + ht * PS_HEADS;
+  // (a wave's tiles are 16 apart, so that a few tiles are of as many waves)
+  W keys(a, i, kv, w * PAGE_TILE, SH_WAVES * PAGE_TILE, len);
+  q.template take<SH_NT>(a, i, h0, heads);
+  __syncthreads();
+  float s[TILES][R4], top[R4];
+  keys.scores(q, s, top);
+#pragma unroll
+  for (int r = 0; r < R4; ++r) lane_top[w][g + 4 * r][col] = top[r];
+  __syncthreads();
+  // (a wave to each register of heads: the others would repeat its arithmetic)
+  if (w < R4) {
+    const int j = g + 4 * w;
+    float v[PS_WAVES];
+#pragma unroll
+    for (int y = 0; y < PS_WAVES; ++y) {
+      v[y] = lane_top[y][j][col];
+#pragma unroll
+      for (int z = PS_WAVES; z < SH_WAVES; z += PS_WAVES) v[y] = fmaxf(v[y], lane_top[y + z][j][col]);
+    }
+    const float m = fold16(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), maxf);
+    const float lo = region_bound(a, v, m);
+    if (col == 0) {
+      head_top[j] = m;
+      head_bound[j] = j < heads ? lo : INFINITY;
+    }
+  }
+  __syncthreads();
+  int mine[R4], to[R4];
+#pragma unroll
+  for (int r = 0; r < R4; ++r) {
+    int all;
+    mine[r] = W::above(s, r, a.scale_c, head_bound[g + 4 * r], to[r], all);
+    if (col == 15) wave_count[w][g + 4 * r] = all;
+  }
+  __syncthreads();
+  bool fits = true;
+#pragma unroll
+  for (int r = 0; r < R4; ++r) {
+    const int n = wave_count[col][g + 4 * r];  // (of wave `col`)
+    auto sum16 = [](int v) {  // (counts are exact in fp32)
+      return (int)fold16((float)v, addf);
+    };
+    to[r] += sum16(col < w ? n : 0);
+    const int all = sum16(n);
+    fits = fits && all <= CAP;
+    if (w == 0 && col == 0) head_count[g + 4 * r] = all;
+  }
+  fits = __all(fits);  // (every wave sees all heads)
+  // entry 0 of head j's list
+  auto list_of = [&](int j) -> u32x2_t* {
+    return fits ? lists[j] : a.list + ((int64_t)i * a.heads + h0 + j) * a.regions * PAGED_REGION;
+  };
+#pragma unroll
+  for (int r = 0; r < R4; ++r) keys.write(s, r, mine[r], list_of(min(g + 4 * r, heads - 1)) + to[r]);
+  __syncthreads();
+  // ---- a wave to a head: tau, and the keys with a probability
+  if (w < heads) {
+    const float m = a.scale_c * head_top[w], lo = fmaxf(head_bound[w], m - 1.f);
+    int n = 0;
+    if (m > -INFINITY && m < INFINITY) {  // (else no keys, or none with a finite score)
+      const int all = __builtin_amdgcn_readfirstlane(head_count[w]);
+      u32x2_t* const list = list_of(w);
+      switch (a.gk) {
+        case 1: n = solve_short<1>(a, list, all, lo, m, len); break;
+        case 2: n = solve_short<2>(a, list, all, lo, m, len); break;
+        case 4: n = solve_short<4>(a, list, all, lo, m, len); break;
+        default: n = solve_short<0>(a, list, all, lo, m, len);
+      }
+    }
+    if (lane == 0) head_count[w] = n;
+  }
+  __syncthreads();
+  // ---- their rows of V
+  float(&sums)[SH_WAVES][D] = reinterpret_cast<float(&)[SH_WAVES][D]>(q);
+  const int j = w / WPH;
+  if (j < heads) {
+    RowSum<D> o(a, kv);
+    constexpr int KPW = RowSum<D>::KPW;
+    o.add(list_of(j), w % WPH * KPW, WPH * KPW, __builtin_amdgcn_readfirstlane(head_count[j]));
+    o.store(sums[w]);
+  }
+  __syncthreads();
+  for (int e = t; e < heads * D; e += SH_NT) {
+    const int h = e / D, d = e % D;
+    float sum = 0.f;
+#pragma unroll
+    for (int y = 0; y < WPH; ++y) sum += sums[h * WPH + y][d];
+    static_cast<E*>(a.o)[i * a.o_row + (h0 + h) * a.o_head + d] = (E)sum;
+  }
+}
+
 int head_tiles(const PagedArgs& a) { return (a.group + PS_HEADS - 1) / PS_HEADS; }
+
+int head_registers(const PagedArgs& a) { return a.group >= PS_HEADS ? 4 : (a.group + 3) / 4; }
+
+hipError_t launch_heads(void (*kernel)(PagedArgs, int), int64_t wgs, int threads, const PagedArgs& a, hipStream_t s) {
+  PagedArgs args = a;
+  int tiles = head_tiles(a);
+  void* params[] = {&args, &tiles};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)wgs), dim3(threads), params, 0, s);
+}
 
 template <typename E, int D>
 hipError_t launch_scores(const PagedArgs& a, hipStream_t s) {
-  const int r4 = a.group >= 16 ? 4 : (a.group + 3) / 4;
+  const int r4 = head_registers(a);
   void (*kernel)(PagedArgs, int) = paged_scores_kernel<E, D, 1>;
   if (r4 == 2) kernel = paged_scores_kernel<E, D, 2>;
   if (r4 == 3) kernel = paged_scores_kernel<E, D, 3>;
   if (r4 == 4) kernel = paged_scores_kernel<E, D, 4>;
-  PagedArgs args = a;
-  int tiles = head_tiles(a);
-  void* params[] = {&args, &tiles};
-  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)paged_score_wgs(a)), dim3(PS_NT), params,
-                         0, s);
+  return launch_heads(kernel, paged_score_wgs(a), PS_NT, a, s);
+}
+
+int64_t short_wgs(const PagedArgs& a) { return (int64_t)a.queries * head_tiles(a) * a.c.kv_heads; }
+
+// Rows that one workgroup each takes, where every one has a compute unit: us in a graph,
+// against the two kernels, 32/8 heads, d = 128, 1, 16 and 64 requests (8, 128 and 512
+// workgroups) of up to 128 keys 9.9, 10.1, 18.4 against 11.4, 12.3, 12.8, of up to
+// 1000 11.0, 11.9, 21.8 against 13.4, 15.8, 17.2.
+bool short_rows(const PagedArgs& a) {
+  return a.longest <= SH_WAVES * PAGE_TILE * sh_tiles(head_registers(a)) && short_wgs(a) <= 256;
+}
+
+template <typename E, int D>
+hipError_t launch_short(const PagedArgs& a, hipStream_t s) {
+  const int r4 = head_registers(a);
+  void (*kernel)(PagedArgs, int) = paged_short_kernel<E, D, 1>;
+  if (r4 == 2) kernel = paged_short_kernel<E, D, 2>;
+  if (r4 == 3) kernel = paged_short_kernel<E, D, 3>;
+  if (r4 == 4) kernel = paged_short_kernel<E, D, 4>;
+  return launch_heads(kernel, short_wgs(a), SH_NT, a, s);
 }
 
 template <typename E, int D, int NT>
@@ -660,6 +910,7 @@ hipError_t launch_solve(const PagedArgs& a, hipStream_t s) {
 
 template <typename E, int D>
 hipError_t launch_paged(const PagedArgs& a, hipStream_t s) {
+  if (short_rows(a)) return launch_short<E, D>(a, s);
   if (a.regions) {
     const hipError_t e = launch_scores<E, D>(a, s);
     if (e != hipSuccess) return e;
