@@ -505,15 +505,24 @@ __device__ __forceinline__ int keep_probable(const PagedArgs& a, u32x2_t* list, 
   return np;
 }
 
+constexpr int SO_LANE = 8;              // scores per lane of a wave that solves a row alone
+constexpr int SO_FEW = 64 * SO_LANE;
+constexpr int SO_OWN = 16;              // scores per thread of a workgroup that solves one
+constexpr int SO_BUFFER = 128;          // entries on their way to a wave's gather
+
+// Rows with few scores above the bound are solved by the first wave alone, without
+// barriers; the others help it with the rows of V (share), or end, where there are rows
+// for every wave of the device.  Rows with more are solved by all of them: each thread
+// keeps SO_OWN scores, and reads the others of its own for every evaluation.
 template <typename E, int D, int GK, int NT>
-__global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
-  constexpr int WAVES = NT / 64, CAP = NT == 64 ? 1024 : 512;  // scores that a wave keeps
-  constexpr int ALONE = 8;  // scores per lane that every wave solves by itself
-  constexpr int LOADS = 4;
-  static_assert(WAVES * CAP * 8 >= WAVES * D * 4, "the waves' sums fit in place of the scores");
-  __shared__ __attribute__((aligned(16))) u32x2_t kept[WAVES][CAP];
+__global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a, int share) {
+  constexpr int WAVES = NT / 64, KPW = RowSum<D>::KPW;
+  static_assert(WAVES * SO_BUFFER >= SO_FEW, "a wave's scores fit in the place of all buffers");
+  __shared__ u32x2_t buffer[WAVES][SO_BUFFER];
+  __shared__ __attribute__((aligned(16))) float sums[WAVES][D];
   __shared__ float red[2][3][WAVES];
-  __shared__ int counts[WAVES], starts[WAVES][MAX_REGIONS + 1];
+  __shared__ int starts[MAX_REGIONS + 1], row_count;
+  __shared__ float row_top, row_bound;
   const int t = threadIdx.x, lane = lane_id(), w = wave_id();
   // (heads of one key head are kv_heads apart: with eight of them, on one XCD)
   const int i = blockIdx.x / a.heads, y = blockIdx.x % a.heads;
@@ -522,186 +531,170 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
   E* const O = static_cast<E*>(a.o) + i * a.o_row + h * a.o_head;
   const float c = a.scale_c, gm = a.gamma;
 
-  // ---- the regions' largest scores: in every wave
-  // (read before the length has come: those behind it are not looked at)
-  float top[MAX_REGIONS / 64], m = -INFINITY, lo = -INFINITY;
-  int listed[MAX_REGIONS / 64];
-  u32x4_t found[MAX_REGIONS / 64];
+  // ---- the regions' largest scores and bounds, and from them a bound of the row; where each
+  // region's listed scores start among all that are looked at (none, where its largest is
+  // below the bound)
+  if (w == 0) {
+    // (read before the length has come: regions behind it are not looked at)
+    float top[MAX_REGIONS / 64], m = -INFINITY, lo = -INFINITY;
+    u32x4_t found[MAX_REGIONS / 64];
 #pragma unroll
-  for (int e = 0; e < MAX_REGIONS / 64; ++e) {
-    found[e] = u32x4_t{0, 0, 0, 0};
-    if (64 * e + lane < a.regions) found[e] = a.tops[row + 64 * e + lane];
-  }
-  const int len = query_length(a, i), regions = (len + PAGED_REGION - 1) / PAGED_REGION;
-#pragma unroll
-  for (int e = 0; e < MAX_REGIONS / 64; ++e) {
-    const bool there = 64 * e + lane < regions;
-    top[e] = there ? __uint_as_float(found[e][0]) : -INFINITY;
-    listed[e] = (int)found[e][2];
-    m = fmaxf(m, top[e]);
-    if (there) lo = fmaxf(lo, __uint_as_float(found[e][1]));  // (the best of the regions' bounds)
-  }
-  m = c * fold64(m, maxf);
-  if (!(m > -INFINITY && m < INFINITY)) {  // no keys, or none with a finite score
-    for (int d = t; d < D; d += NT) O[d] = (E)0.f;
-    return;
-  }
-  lo = fmaxf(fold64(lo, maxf), m - 1.f);
-  for (int it = 0; it < 8; ++it) {
-    float s0 = 0.f, s1 = 0.f, s2 = 0.f;
-#pragma unroll
-    for (int e = 0; e < MAX_REGIONS / 64; ++e) add_z<GK>(relu_z(c, top[e], lo), gm, s0, s1, s2);
-    s0 = fold64(s0, addf);
-    s1 = fold64(s1, addf);
-    const float step = (s0 - 1.f) * __builtin_amdgcn_rcpf(gm * s1);
-    if (!(step > 1e-3f)) break;  // (no key is above it where s1 is 0)
-    lo += step;
-    if (it == 7 || !(step > 1e-2f)) {
-      lo -= 4e-6f * fmaxf(1.f, fabsf(lo));  // (the sums' rounding)
-      break;
+    for (int e = 0; e < MAX_REGIONS / 64; ++e) {
+      found[e] = u32x4_t{0, 0, 0, 0};
+      if (64 * e + lane < a.regions) found[e] = a.tops[row + 64 * e + lane];
     }
-  }
-
-  // ---- the listed scores above the bound: those of all regions in one order, 64 of them to
-  // a wave in turn, LOADS of these on their way at once.  starts: of each region's
-  // (none, where its largest is below the bound)
-  {
+    const int regions = (query_length(a, i) + PAGED_REGION - 1) / PAGED_REGION;
+#pragma unroll
+    for (int e = 0; e < MAX_REGIONS / 64; ++e) {
+      const bool there = 64 * e + lane < regions;
+      top[e] = there ? __uint_as_float(found[e][0]) : -INFINITY;
+      m = fmaxf(m, top[e]);
+      if (there) lo = fmaxf(lo, __uint_as_float(found[e][1]));  // (the best of the regions' bounds)
+    }
+    m = c * fold64(m, maxf);
+    lo = fmaxf(fold64(lo, maxf), m - 1.f);
+    const bool any = m > -INFINITY && m < INFINITY;
+    for (int it = 0; any && it < 8; ++it) {
+      float s0 = 0.f, s1 = 0.f, s2 = 0.f;
+#pragma unroll
+      for (int e = 0; e < MAX_REGIONS / 64; ++e) add_z<GK>(relu_z(c, top[e], lo), gm, s0, s1, s2);
+      s0 = fold64(s0, addf);
+      s1 = fold64(s1, addf);
+      const float step = (s0 - 1.f) * __builtin_amdgcn_rcpf(gm * s1);
+      if (!(step > 1e-3f)) break;  // (no key is above it where s1 is 0)
+      lo += step;
+      if (it == 7 || !(step > 1e-2f)) {
+        lo -= 4e-6f * fmaxf(1.f, fabsf(lo));  // (the sums' rounding)
+        break;
+      }
+    }
     int base = 0;
 #pragma unroll
     for (int e = 0; e < MAX_REGIONS / 64; ++e) {
-      const int n = relu_z(c, top[e], lo) > 0.f ? listed[e] : 0;
+      const int n = any && relu_z(c, top[e], lo) > 0.f ? (int)found[e][2] : 0;
       int incl = n;
 #pragma unroll
       for (int x = 1; x < 64; x <<= 1) {
         const int v = __shfl_up(incl, x);
         if (lane >= x) incl += v;
       }
-      starts[w][64 * e + lane] = base + incl - n;
+      starts[64 * e + lane] = base + incl - n;
       base += __builtin_amdgcn_readlane(incl, 63);
     }
-    if (lane == 0) starts[w][MAX_REGIONS] = base;
-  }
-  const int entries = __builtin_amdgcn_readfirstlane(starts[w][MAX_REGIONS]);
-  // use(entry) of the wave's entries, one in each lane
-  auto each = [&](auto&& use) {
-    for (int e0 = 64 * w; e0 < entries; e0 += 64 * WAVES * LOADS) {
-      u32x2_t v[LOADS];
-#pragma unroll
-      for (int u = 0; u < LOADS; ++u) {
-        const int e = e0 + u * 64 * WAVES + lane;
-        v[u] = u32x2_t{0xFF800000u, 0};  // (-inf)
-        if (e < entries) {
-          int x = 0;  // the last region that starts at or before e
-#pragma unroll
-          for (int step = MAX_REGIONS / 2; step; step >>= 1)
-            if (starts[w][x + step] <= e) x += step;
-          v[u] = a.list[(row + x) * PAGED_REGION + (e - starts[w][x])];
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < LOADS; ++u) {
-        if (e0 + u * 64 * WAVES >= entries) break;
-        use(v[u]);
-      }
-    }
-  };
-  int mine = 0;  // the wave's count
-  const uint64_t before = (1ull << lane) - 1;
-  each([&](const u32x2_t& v) {
-    const bool keep = relu_z(c, __uint_as_float(v[0]), lo) > 0.f;
-    const uint64_t k = __ballot(keep);
-    const int to = mine + __popcll(k & before);
-    if (keep && to < CAP) kept[w][to] = v;
-    mine += __popcll(k);
-  });
-  if (lane == 0) counts[w] = mine;
-  __syncthreads();
-  int total = 0;
-  bool wide = false;
-#pragma unroll
-  for (int x = 0; x < WAVES; ++x) {
-    total += counts[x];
-    wide |= counts[x] > CAP;
-  }
-
-  // ---- tau: Algorithm 1's iteration on them
-  int turn = 0;
-  auto sum3 = [&](float& s0, float& s1, float& s2) {
-    s0 = fold64(s0, addf);
-    s1 = fold64(s1, addf);
-    s2 = fold64(s2, addf);
-    if constexpr (WAVES == 1) return;
-    auto& r = red[turn];
-    turn ^= 1;
     if (lane == 0) {
-      r[0][w] = s0;
-      r[1][w] = s1;
-      r[2][w] = s2;
+      starts[MAX_REGIONS] = base;
+      row_top = m;
+      row_bound = lo;
     }
-    __syncthreads();
-    s0 = s1 = s2 = 0.f;
+  }
+  __syncthreads();
+  const int entries = __builtin_amdgcn_readfirstlane(starts[MAX_REGIONS]);
+  if (entries == 0) {  // no keys, or none with a finite score
+    for (int d = t; d < D; d += NT) O[d] = (E)0.f;
+    return;
+  }
+  const float m = row_top, lo = row_bound;
+  const int len = query_length(a, i);
+  auto entry = [&](int e) {  // number e of them
+    int x = 0;  // the last region that starts at or before it
 #pragma unroll
-    for (int x = 0; x < WAVES; ++x) {
-      s0 += r[0][x];
-      s1 += r[1][x];
-      s2 += r[2][x];
-    }
+    for (int step = MAX_REGIONS / 2; step; step >>= 1)
+      if (starts[x + step] <= e) x += step;
+    return a.list + (row + x) * PAGED_REGION + (e - starts[x]);
   };
-  const bool alone = !wide && total <= 64 * ALONE;
-  float own[ALONE];
-  if (alone) {
+  RowSum<D> o(a, kv);
+
+  if (entries <= SO_FEW) {
+    u32x2_t* const kept = buffer[0];
+    if (w == 0) {
+      float own[SO_LANE];
+      u32x2_t v[SO_LANE];
 #pragma unroll
-    for (int e = 0; e < ALONE; ++e) {
-      own[e] = -INFINITY;
-      int at = 64 * e + lane, x = 0;
-      if (at < total) {
-        while (at >= counts[x]) at -= counts[x++];
-        own[e] = __uint_as_float(kept[x][at][0]);
+      for (int e = 0; e < SO_LANE; ++e) {
+        v[e] = u32x2_t{0xFF800000u, 0};  // (-inf)
+        if (64 * e + lane < entries) v[e] = *entry(64 * e + lane);
+      }
+#pragma unroll
+      for (int e = 0; e < SO_LANE; ++e) {
+        own[e] = __uint_as_float(v[e][0]);
+        if (64 * e + lane < entries) kept[64 * e + lane] = v[e];
+      }
+      const float tau = solve_tau(a, lo, m, len, [&](float tau, float& s0, float& s1, float& s2) {
+#pragma unroll
+        for (int e = 0; e < SO_LANE; ++e) {
+          if (64 * e >= entries) break;
+          add_z<GK>(relu_z(c, own[e], tau), gm, s0, s1, s2);
+        }
+        s0 = fold64(s0, addf);
+        s1 = fold64(s1, addf);
+        s2 = fold64(s2, addf);
+      });
+      const int n = keep_probable<GK>(a, kept, entries, tau);
+      if (!share) {
+        o.add(kept, 0, KPW, n);
+        o.store(sums[0]);
+        for (int d = lane; d < D; d += 64) O[d] = (E)sums[0][d];
+      } else if (lane == 0) {
+        row_count = n;
       }
     }
-    __syncthreads();  // (a wave that is done writes to its list)
-  }
-  const float tau = solve_tau(a, lo, m, len, [&](float tau, float& s0, float& s1, float& s2) {
-    if (alone) {
+    if (!share) return;
+    __syncthreads();
+    o.add(kept, w * KPW, WAVES * KPW, __builtin_amdgcn_readfirstlane(row_count));
+  } else {
+    // a thread's entries are t, t + NT ..
+    float own[SO_OWN];
 #pragma unroll
-      for (int e = 0; e < ALONE; ++e) {
-        if (64 * e >= total) break;
+    for (int e = 0; e < SO_OWN; ++e) own[e] = e * NT + t < entries ? __uint_as_float((*entry(e * NT + t))[0]) : -INFINITY;
+    int turn = 0;
+    const float tau = solve_tau(a, lo, m, len, [&](float tau, float& s0, float& s1, float& s2) {
+#pragma unroll
+      for (int e = 0; e < SO_OWN; ++e) {
+        if (e * NT >= entries) break;
         add_z<GK>(relu_z(c, own[e], tau), gm, s0, s1, s2);
       }
+#pragma unroll 4
+      for (int e = SO_OWN * NT + t; e < entries; e += NT)
+        add_z<GK>(relu_z(c, __uint_as_float((*entry(e))[0]), tau), gm, s0, s1, s2);
       s0 = fold64(s0, addf);
       s1 = fold64(s1, addf);
       s2 = fold64(s2, addf);
-    } else if (!wide) {
-      for (int e = lane; e < mine; e += 64) add_z<GK>(relu_z(c, __uint_as_float(kept[w][e][0]), tau), gm, s0, s1, s2);
-      sum3(s0, s1, s2);
-    } else {
-      each([&](const u32x2_t& v) { add_z<GK>(relu_z(c, __uint_as_float(v[0]), tau), gm, s0, s1, s2); });
-      sum3(s0, s1, s2);
-    }
-  });
-
-  // ---- O: the rows of V with a probability
-  RowSum<D> o(a, kv);
-  auto gather = [&](int n) { o.add(kept[w], 0, RowSum<D>::KPW, keep_probable<GK>(a, kept[w], n, tau)); };
-  if (!wide) {
-    gather(mine);
-  } else {
-    int n = 0;  // (the wave's list is filled and emptied in turn)
-    each([&](const u32x2_t& v) {
-      if (n + 64 > CAP) {
-        gather(n);
+      // (two buffers in turn: one barrier)
+      auto& r = red[turn];
+      turn ^= 1;
+      if (lane == 0) {
+        r[0][w] = s0;
+        r[1][w] = s1;
+        r[2][w] = s2;
+      }
+      __syncthreads();
+      s0 = s1 = s2 = 0.f;
+#pragma unroll
+      for (int x = 0; x < WAVES; ++x) {
+        s0 += r[0][x];
+        s1 += r[1][x];
+        s2 += r[2][x];
+      }
+    });
+    // those with a probability go through the wave's buffer
+    int n = 0;
+    const uint64_t before = (1ull << lane) - 1;
+#pragma unroll 4
+    for (int e0 = 64 * w; e0 < entries; e0 += NT) {
+      u32x2_t v = {0xFF800000u, 0};
+      if (e0 + lane < entries) v = *entry(e0 + lane);
+      const float p = Gamma<GK>::p_only(relu_z(c, __uint_as_float(v[0]), tau), gm);
+      const uint64_t k = __ballot(p > 0.f);
+      if (p > 0.f) buffer[w][n + __popcll(k & before)] = u32x2_t{__float_as_uint(p), v[1]};
+      n += __popcll(k);
+      if (n > SO_BUFFER - 64) {
+        o.add(buffer[w], 0, KPW, n);
         n = 0;
       }
-      const bool keep = relu_z(c, __uint_as_float(v[0]), tau) > 0.f;
-      const uint64_t k = __ballot(keep);
-      if (keep) kept[w][n + __popcll(k & before)] = v;
-      n += __popcll(k);
-    });
-    gather(n);
+    }
+    o.add(buffer[w], 0, KPW, n);
   }
-  __syncthreads();
-  // sums over the rows of a wave, then over the waves, in place of the scores
-  float(&sums)[WAVES][D] = reinterpret_cast<float(&)[WAVES][D]>(kept);
+  // sums over the rows of a wave, then over the waves
   o.store(sums[w]);
   __syncthreads();
   for (int d = t; d < D; d += NT) {
@@ -905,7 +898,11 @@ hipError_t launch_solve(const PagedArgs& a, hipStream_t s) {
   if (a.gk == 1) kernel = paged_solve_kernel<E, D, 1, NT>;
   if (a.gk == 2) kernel = paged_solve_kernel<E, D, 2, NT>;
   if (a.gk == 4) kernel = paged_solve_kernel<E, D, 4, NT>;
-  return launch_kernel(kernel, dim3((unsigned)(a.queries * a.heads)), dim3(NT), s, a);
+  PagedArgs args = a;
+  int share = a.queries * a.heads < 1024;
+  void* params[] = {&args, &share};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)(a.queries * a.heads)), dim3(NT), params,
+                         0, s);
 }
 
 template <typename E, int D>
@@ -915,7 +912,7 @@ hipError_t launch_paged(const PagedArgs& a, hipStream_t s) {
     const hipError_t e = launch_scores<E, D>(a, s);
     if (e != hipSuccess) return e;
   }
-  return a.queries * a.heads >= 1024 ? launch_solve<E, D, 64>(a, s) : launch_solve<E, D, 256>(a, s);
+  return a.queries * a.heads <= 256 ? launch_solve<E, D, 1024>(a, s) : launch_solve<E, D, 256>(a, s);
 }
 
 }  // namespace
