@@ -374,7 +374,7 @@ __global__ __launch_bounds__(PS_NT) void paged_scores_kernel(PagedArgs a, int he
 
 constexpr int MAX_REGIONS = MAX_SEQLEN / PAGED_REGION;
 constexpr int PV_VALS = 16;   // values of V that a lane takes of a row
-constexpr int PV_BATCH = 4;   // rows of V of a lane in flight
+constexpr int PV_BATCH = 8;   // rows of V of a lane in flight
 
 // z^gamma, z^(gamma-1), z^(gamma-2) summed over z > 0
 template <int GK>
@@ -508,7 +508,7 @@ __device__ __forceinline__ int keep_probable(const PagedArgs& a, u32x2_t* list, 
 constexpr int SO_LANE = 8;              // scores per lane of a wave that solves a row alone
 constexpr int SO_FEW = 64 * SO_LANE;
 constexpr int SO_OWN = 16;              // scores per thread of a workgroup that solves one
-constexpr int SO_BUFFER = 128;          // entries on their way to a wave's gather
+constexpr int SO_BUFFER = 256;          // entries on their way to a wave's gather
 
 // Rows with few scores above the bound are solved by the first wave alone, without
 // barriers; the others help it with the rows of V (share), or end, where there are rows
@@ -643,15 +643,18 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a, int share)
     o.add(kept, w * KPW, WAVES * KPW, __builtin_amdgcn_readfirstlane(row_count));
   } else {
     // a thread's entries are t, t + NT ..
-    float own[SO_OWN];
+    u32x2_t own[SO_OWN];
 #pragma unroll
-    for (int e = 0; e < SO_OWN; ++e) own[e] = e * NT + t < entries ? __uint_as_float((*entry(e * NT + t))[0]) : -INFINITY;
+    for (int e = 0; e < SO_OWN; ++e) {
+      own[e] = u32x2_t{0xFF800000u, 0};  // (-inf)
+      if (e * NT + t < entries) own[e] = *entry(e * NT + t);
+    }
     int turn = 0;
     const float tau = solve_tau(a, lo, m, len, [&](float tau, float& s0, float& s1, float& s2) {
 #pragma unroll
       for (int e = 0; e < SO_OWN; ++e) {
         if (e * NT >= entries) break;
-        add_z<GK>(relu_z(c, own[e], tau), gm, s0, s1, s2);
+        add_z<GK>(relu_z(c, __uint_as_float(own[e][0]), tau), gm, s0, s1, s2);
       }
 #pragma unroll 4
       for (int e = SO_OWN * NT + t; e < entries; e += NT)
@@ -679,10 +682,7 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a, int share)
     // those with a probability go through the wave's buffer
     int n = 0;
     const uint64_t before = (1ull << lane) - 1;
-#pragma unroll 4
-    for (int e0 = 64 * w; e0 < entries; e0 += NT) {
-      u32x2_t v = {0xFF800000u, 0};
-      if (e0 + lane < entries) v = *entry(e0 + lane);
+    auto take = [&](const u32x2_t& v) {
       const float p = Gamma<GK>::p_only(relu_z(c, __uint_as_float(v[0]), tau), gm);
       const uint64_t k = __ballot(p > 0.f);
       if (p > 0.f) buffer[w][n + __popcll(k & before)] = u32x2_t{__float_as_uint(p), v[1]};
@@ -691,6 +691,16 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a, int share)
         o.add(buffer[w], 0, KPW, n);
         n = 0;
       }
+    };
+#pragma unroll
+    for (int e = 0; e < SO_OWN; ++e) {
+      if (e * NT + 64 * w >= entries) break;
+      take(own[e]);
+    }
+    for (int e0 = SO_OWN * NT + 64 * w; e0 < entries; e0 += NT) {
+      u32x2_t v = {0xFF800000u, 0};
+      if (e0 + lane < entries) v = *entry(e0 + lane);
+      take(v);
     }
     o.add(buffer[w], 0, KPW, n);
   }
