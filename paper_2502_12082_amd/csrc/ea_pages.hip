@@ -216,14 +216,17 @@ constexpr int UP_NT = 1024, UP_WAVES = UP_NT / 64;
 __device__ __forceinline__ int count_up(int a, int b) { return min(a + b, 1 << 30); }
 __device__ __forceinline__ int place_of(int mine, int& base, int (&sums)[2][UP_WAVES], int& turn) {
   const int lane = lane_id(), w = wave_id();
+  // (a wave's sum is small; the VALU alone: rows of 16 lanes, then from row to row)
   int incl = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(incl, o);
-    if (lane >= o) incl = count_up(incl, v);
-  }
-  int excl = __shfl_up(incl, 1);
-  if (lane == 0) excl = 0;
+  incl += (int)dpp_of<0x111>(incl);  // row_shr 1, 2, 4, 8
+  incl += (int)dpp_of<0x112>(incl);
+  incl += (int)dpp_of<0x114>(incl);
+  incl += (int)dpp_of<0x118>(incl);
+#if defined(__HIP_DEVICE_COMPILE__)
+  incl += __builtin_amdgcn_update_dpp(0, incl, 0x142, 0xa, 0xf, false);  // lane 15 to rows 1 and 3
+  incl += __builtin_amdgcn_update_dpp(0, incl, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2 and 3
+#endif
+  const int excl = incl - mine;
   auto& m = sums[turn];
   turn ^= 1;
   if (lane == 63) m[w] = incl;
@@ -252,8 +255,9 @@ __device__ __forceinline__ RowPlan kept_of(const CacheUpdateArgs& a, int r) {
 }
 
 // Small tables (small_tables): one workgroup plans, with a bit in LDS for every page
-// that is held, and counts of the pages that rows are about to write to in a hash
-// table.  It is bound by its chain of loads and barriers: a row's parent, its length, its
+// that is held, and the rows that are about to write to a page in a hash table.  (Counts of
+// all holders there took a look for every entry: 64 rows of up to 256 pages 12.5 us against
+// 9.1.)  It is bound by its chain of loads and barriers: a row's parent, its length, its
 // entries.
 constexpr int PL_ROWS = UP_NT, PL_WORDS = 4096, PL_SLOTS = 2 * PL_ROWS;
 constexpr int PL_BATCH = 8, PL_LOADS = 2;  // rows of a wave, and entries of a lane of each, in flight
@@ -272,7 +276,8 @@ struct PageSet {
   }
 };
 
-// use(page) of the entries [0, kept[r]) that name pages of the table's rows from[r].
+// use(pages) of the entries [0, kept[r]) of the table's rows from[r], some at a time, -1 where
+// they name no page.
 template <typename F>
 __device__ __forceinline__ void each_held(const CacheUpdateArgs& a, const int* from, const int* kept, int rows, F&& use) {
   const int lane = lane_id();
@@ -296,16 +301,25 @@ __device__ __forceinline__ void each_held(const CacheUpdateArgs& a, const int* f
       for (int j = 0; j < PL_BATCH; ++j)
 #pragma unroll
         for (int u = 0; u < PL_LOADS; ++u)
-          if (id[j][u] >= 0 && id[j][u] < a.c.pages) use(id[j][u]);
+          if (id[j][u] >= a.c.pages) id[j][u] = -1;
+      use(id);
     }
   }
+}
+
+__device__ __forceinline__ void mark(uint32_t* held, const int (&id)[PL_BATCH][PL_LOADS]) {
+#pragma unroll
+  for (int j = 0; j < PL_BATCH; ++j)
+#pragma unroll
+    for (int u = 0; u < PL_LOADS; ++u)
+      if (id[j][u] >= 0) atomicOr(&held[id[j][u] >> 5], 1u << (id[j][u] & 31));
 }
 
 // Workgroup 0 plans; workgroup 1 + r writes those entries of row r that need no plan.
 __global__ __launch_bounds__(UP_NT) void update_small_kernel(CacheUpdateArgs a) {
   __shared__ uint32_t held_words[PL_WORDS];
-  __shared__ int slots[4][PL_SLOTS];
-  int *const key = slots[0], *const holders = slots[1], *const writers = slots[2], *const lowest = slots[3];
+  __shared__ int slots[3][PL_SLOTS];
+  int *const key = slots[0], *const writers = slots[1], *const lowest = slots[2];
   __shared__ int from[PL_ROWS], kept[PL_ROWS], before[PL_ROWS + 1];
   __shared__ int sums[2][UP_WAVES];
   const int t = threadIdx.x;
@@ -323,7 +337,7 @@ __global__ __launch_bounds__(UP_NT) void update_small_kernel(CacheUpdateArgs a) 
   held.clear();
   for (int i = t; i < PL_SLOTS; i += UP_NT) {
     key[i] = -1;
-    holders[i] = writers[i] = 0;
+    writers[i] = 0;
     lowest[i] = INT32_MAX;
   }
   __syncthreads();
@@ -332,7 +346,7 @@ __global__ __launch_bounds__(UP_NT) void update_small_kernel(CacheUpdateArgs a) 
   if (t < a.rows_out) {
     p = plan_of(a, t);
     from[t] = a.parents[t];
-    kept[t] = p.kept;
+    kept[t] = p.kept - (p.writes ? 1 : 0);  // (the page that it writes to is looked at below)
     last = last_page(a, t, p);
   }
   auto first = [](int page) { return (int)((uint32_t)page * 0x9E3779B1u >> 21); };
@@ -346,26 +360,23 @@ __global__ __launch_bounds__(UP_NT) void update_small_kernel(CacheUpdateArgs a) 
     atomicMin(&lowest[slot], t);
   }
   __syncthreads();
-  each_held(a, from, kept, a.rows_out, [&](int id) {
-    atomicOr(&held_words[id >> 5], 1u << (id & 31));
-    for (int s = first(id); key[s] != -1; s = (s + 1) % PL_SLOTS)
-      if (key[s] == id) {
-        atomicAdd(&holders[s], 1);
-        break;
-      }
-  });
+  each_held(a, from, kept, a.rows_out, [&](const int (&id)[PL_BATCH][PL_LOADS]) { mark(held_words, id); });
   __syncthreads();
-  // ---- pages needed before each row
+  // ---- pages needed before each row.  A page that rows are about to write to is held by
+  // these, and by others if it is marked by now.
   int turn = 0, needed = 0;
-  const int copy = last >= 0 && copies(holders[slot], writers[slot], lowest[slot], t) ? 1 : 0;
+  const int others = last >= 0 ? (int)(held_words[last >> 5] >> (last & 31) & 1) : 0;
+  const int copy = last >= 0 && copies(writers[slot] + others, writers[slot], lowest[slot], t) ? 1 : 0;
   const int need = t < a.rows_out ? p.grown + copy : 0;
   const int at = place_of(need, needed, sums, turn);
+  if (last >= 0) atomicOr(&held_words[last >> 5], 1u << (last & 31));
   before[t] = at;
   kept[t] = p.kept | copy << 30;
   if (t == 0) before[PL_ROWS] = needed;
+  __syncthreads();
   // ---- as many free pages, the lowest first
   // (in the place of the hash table, which has served, where they fit)
-  int* const free_list = needed <= 4 * PL_SLOTS ? slots[0] : a.free_list;
+  int* const free_list = needed <= 3 * PL_SLOTS ? slots[0] : a.free_list;
   int found = 0;
   for (int w0 = 0; w0 < held.words() && found < needed; w0 += UP_NT) {
     uint32_t bits = held.free(w0 + t);
@@ -435,7 +446,7 @@ __global__ __launch_bounds__(UP_NT) void compact_small_kernel(CacheUpdateArgs a)
     kept[t] = kept_of(a, t).kept;
   }
   __syncthreads();
-  each_held(a, from, kept, a.t.rows, [&](int id) { atomicOr(&held_words[id >> 5], 1u << (id & 31)); });
+  each_held(a, from, kept, a.t.rows, [&](const int (&id)[PL_BATCH][PL_LOADS]) { mark(held_words, id); });
   __syncthreads();
   pair_pages(a, held, sums);
 }
