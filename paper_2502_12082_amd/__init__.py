@@ -1395,6 +1395,17 @@ for _name, _args in (
 _checked = {}
 
 
+def _launch(dev, name, call, *args):
+    """Calls an entry point on the device's current stream, with that device current."""
+    if dev.index == torch._C._cuda_getDevice():
+        status = call(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+    else:
+        with torch.cuda.device(dev):
+            status = call(*args, torch._C._cuda_getCurrentRawStream(dev.index))
+    if status:
+        _check(status, name)
+
+
 def _remember(key, value):
     if key is not None:
         if len(_checked) >= 1024:
@@ -1503,14 +1514,13 @@ def cache_append(cache, k, v, rows, positions, table):
                v.stride(), v.dtype, v.device, rows.shape, rows.stride(), rows.dtype, rows.device, positions.shape,
                positions.stride(), positions.dtype, positions.device, table.shape, table.stride(), table.dtype,
                table.device)
-        args = None if (cache.data_ptr() | k.data_ptr() | v.data_ptr()) & 15 else _checked.get(key)
+        at, k_at, v_at = cache.data_ptr(), k.data_ptr(), v.data_ptr()
+        args = None if (at | k_at | v_at) & 15 else _checked.get(key)
     except (AttributeError, TypeError):
         key = args = None
     c, t, tokens, dt, ks, vs = args or _remember(key, _check_append(cache, k, v, rows, positions, table))
-    with _on_device(dev):
-        _check(_lib.entmax_cache_append(c, cache.data_ptr(), t, table.data_ptr(), tokens, dt, rows.data_ptr(),
-                                        positions.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs, _stream_handle(dev)),
-               "entmax_cache_append")
+    _launch(dev, "entmax_cache_append", _lib.entmax_cache_append, c, at, t, table.data_ptr(), tokens, dt,
+            rows.data_ptr(), positions.data_ptr(), k_at, ks, v_at, vs)
 
 
 def _check_read(cache, rows, positions, table, dtype, k_out, v_out):
@@ -1540,23 +1550,22 @@ def cache_read(cache, rows, positions, table, dtype=torch.bfloat16, k_out=None, 
                rows.device, positions.shape, positions.stride(), positions.dtype, positions.device, table.shape,
                table.stride(), table.dtype, table.device)
         # (tensors to write are checked each time: whether they overlap is where they lie)
-        args = None if k_out is not None or v_out is not None or cache.data_ptr() & 15 else _checked.get(key)
+        at = cache.data_ptr()
+        args = None if k_out is not None or v_out is not None or at & 15 else _checked.get(key)
     except (AttributeError, TypeError):
         key = args = None
     c, t, shape, dt, strides = args or _remember(key, _check_read(cache, rows, positions, table, dtype, k_out, v_out))
-    with _on_device(dev):
-        ks = vs = strides
-        if k_out is None:
-            k_out = torch.empty(shape, dtype=dtype, device=dev)
-        else:
-            ks = _row_head(k_out)
-        if v_out is None:
-            v_out = torch.empty(shape, dtype=dtype, device=dev)
-        else:
-            vs = _row_head(v_out)
-        _check(_lib.entmax_cache_read(c, cache.data_ptr(), t, table.data_ptr(), shape[0], dt, rows.data_ptr(),
-                                      positions.data_ptr(), k_out.data_ptr(), ks, v_out.data_ptr(), vs,
-                                      _stream_handle(dev)), "entmax_cache_read")
+    ks = vs = strides
+    if k_out is None:
+        k_out = torch.empty(shape, dtype=dtype, device=dev)
+    else:
+        ks = _row_head(k_out)
+    if v_out is None:
+        v_out = torch.empty(shape, dtype=dtype, device=dev)
+    else:
+        vs = _row_head(v_out)
+    _launch(dev, "entmax_cache_read", _lib.entmax_cache_read, c, at, t, table.data_ptr(), shape[0], dt,
+            rows.data_ptr(), positions.data_ptr(), k_out.data_ptr(), ks, v_out.data_ptr(), vs)
     return k_out, v_out
 
 
@@ -1641,23 +1650,25 @@ def cache_update(cache, table, lengths, parents, counts, table_out=None, lengths
                table.device, lengths.shape, lengths.stride(), lengths.dtype, lengths.device, parents.shape,
                parents.stride(), parents.dtype, parents.device, counts.shape, counts.stride(), counts.dtype,
                counts.device)
-        args = None if given or cache.data_ptr() & 15 else _checked.get(key)
+        at = cache.data_ptr()
+        args = None if given or at & 15 else _checked.get(key)
     except (AttributeError, TypeError):
         key = args = None
     c, layers, t, rows, nbytes = args or _remember(key, _check_update(
         cache, table, lengths, parents, counts, table_out, lengths_out, missing_out, workspace))
-    with _on_device(dev):
-        if table_out is None:
-            table_out = torch.empty((rows, t.width), dtype=torch.int32, device=dev)
-            lengths_out, missing_out = torch.empty_like(parents), torch.empty_like(parents)
-        if workspace is None:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-        else:
-            nbytes = workspace.numel() * workspace.element_size()
-        _check(_lib.entmax_cache_update(
-            c, layers, cache.data_ptr(), t, table.data_ptr(), lengths.data_ptr(), rows, parents.data_ptr(),
-            counts.data_ptr(), table_out.data_ptr(), max(_stride(table_out, 0), t.width), lengths_out.data_ptr(),
-            missing_out.data_ptr(), workspace.data_ptr(), nbytes, _stream_handle(dev)), "entmax_cache_update")
+    out_stride = t.width
+    if table_out is None:
+        table_out = torch.empty((rows, t.width), dtype=torch.int32, device=dev)
+        lengths_out, missing_out = torch.empty_like(parents), torch.empty_like(parents)
+    else:
+        out_stride = max(_stride(table_out, 0), out_stride)
+    if workspace is None:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    _launch(dev, "entmax_cache_update", _lib.entmax_cache_update, c, layers, at, t, table.data_ptr(),
+            lengths.data_ptr(), rows, parents.data_ptr(), counts.data_ptr(), table_out.data_ptr(), out_stride,
+            lengths_out.data_ptr(), missing_out.data_ptr(), workspace.data_ptr(), nbytes)
     return table_out, lengths_out, missing_out
 
 
@@ -1690,22 +1701,23 @@ def cache_compact(cache, table, lengths, table_out=None, used_out=None, workspac
         dev = cache.device
         key = ("compact", dev, cache.shape, cache.stride(), cache.dtype, table.shape, table.stride(), table.dtype,
                table.device, lengths.shape, lengths.stride(), lengths.dtype, lengths.device)
-        args = None if given or cache.data_ptr() & 15 else _checked.get(key)
+        at = cache.data_ptr()
+        args = None if given or at & 15 else _checked.get(key)
     except (AttributeError, TypeError):
         key = args = None
     c, layers, t, nbytes = args or _remember(key, _check_compact(cache, table, lengths, table_out, used_out, workspace))
-    with _on_device(dev):
-        if table_out is None:
-            table_out = torch.empty((t.rows, t.width), dtype=torch.int32, device=dev)
-            used_out = torch.empty(1, dtype=torch.int32, device=dev)
-        if workspace is None:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-        else:
-            nbytes = workspace.numel() * workspace.element_size()
-        _check(_lib.entmax_cache_compact(
-            c, layers, cache.data_ptr(), t, table.data_ptr(), lengths.data_ptr(), table_out.data_ptr(),
-            max(_stride(table_out, 0), t.width), used_out.data_ptr(), workspace.data_ptr(), nbytes,
-            _stream_handle(dev)), "entmax_cache_compact")
+    out_stride = t.width
+    if table_out is None:
+        table_out = torch.empty((t.rows, t.width), dtype=torch.int32, device=dev)
+        used_out = torch.empty(1, dtype=torch.int32, device=dev)
+    else:
+        out_stride = max(_stride(table_out, 0), out_stride)
+    if workspace is None:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    _launch(dev, "entmax_cache_compact", _lib.entmax_cache_compact, c, layers, at, t, table.data_ptr(),
+            lengths.data_ptr(), table_out.data_ptr(), out_stride, used_out.data_ptr(), workspace.data_ptr(), nbytes)
     return table_out, used_out
 
 
@@ -1779,22 +1791,21 @@ def paged_decode(q, cache, table, lengths, rows=None, alpha=1.5, scale=None, max
         key = ("paged", dev, numbers, max_length, cache.shape, cache.stride(), cache.dtype, q.shape, q.stride(), q.dtype,
                q.device, table.shape, table.stride(), table.dtype, table.device, lengths.shape, lengths.stride(),
                lengths.dtype, lengths.device, rows is not None and (rows.shape, rows.stride(), rows.dtype, rows.device))
-        args = (None if out is not None or workspace is not None or (cache.data_ptr() | q.data_ptr()) & 15
-                else _checked.get(key))
+        at, q_at = cache.data_ptr(), q.data_ptr()
+        args = None if out is not None or workspace is not None or (at | q_at) & 15 else _checked.get(key)
     except (AttributeError, TypeError):
         key = args = None
     shape, params, c, t, qs, os_, nbytes = args or _remember(key, _check_paged(
         q, cache, table, lengths, rows, numbers, max_length, out, workspace))
-    with _on_device(dev):
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-        else:
-            os_ = _row_head(out)
-        if workspace is None:
-            workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
-        else:
-            nbytes = workspace.numel() * workspace.element_size()
-        _check(_lib.entmax_paged_decode(
-            shape, params, c, cache.data_ptr(), t, table.data_ptr(), q.data_ptr(), qs, lengths.data_ptr(), _ptr(rows),
-            out.data_ptr(), os_, workspace.data_ptr(), nbytes, _stream_handle(dev)), "entmax_paged_decode")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    else:
+        os_ = _row_head(out)
+    if workspace is None:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    _launch(dev, "entmax_paged_decode", _lib.entmax_paged_decode, shape, params, c, at, t, table.data_ptr(), q_at, qs,
+            lengths.data_ptr(), None if rows is None else rows.data_ptr(), out.data_ptr(), os_, workspace.data_ptr(),
+            nbytes)
     return out

@@ -260,7 +260,7 @@ __device__ __forceinline__ RowPlan kept_of(const CacheUpdateArgs& a, int r) {
 // 9.1.)  It is bound by its chain of loads and barriers: a row's parent, its length, its
 // entries.
 constexpr int PL_ROWS = UP_NT, PL_WORDS = 4096, PL_SLOTS = 2 * PL_ROWS;
-constexpr int PL_BATCH = 8, PL_LOADS = 2;  // rows of a wave, and entries of a lane of each, in flight
+constexpr int PL_BATCH = 4, PL_LOADS = 2;  // rows of a wave, and entries of a lane of each, in flight
 
 struct PageSet {
   uint32_t* word;  // a bit for each page
