@@ -1561,7 +1561,7 @@ def cache_read(cache, rows, positions, table, dtype=torch.bfloat16, k_out=None, 
     else:
         ks = _row_head(k_out)
     if v_out is None:
-        v_out = torch.empty(shape, dtype=dtype, device=dev)
+        v_out = torch.empty_like(k_out) if ks is strides else torch.empty(shape, dtype=dtype, device=dev)
     else:
         vs = _row_head(v_out)
     _launch(dev, "entmax_cache_read", _lib.entmax_cache_read, c, at, t, table.data_ptr(), shape[0], dt,
@@ -1658,12 +1658,12 @@ def cache_update(cache, table, lengths, parents, counts, table_out=None, lengths
         cache, table, lengths, parents, counts, table_out, lengths_out, missing_out, workspace))
     out_stride = t.width
     if table_out is None:
-        table_out = torch.empty((rows, t.width), dtype=torch.int32, device=dev)
+        table_out = parents.new_empty((rows, t.width))
         lengths_out, missing_out = torch.empty_like(parents), torch.empty_like(parents)
     else:
         out_stride = max(_stride(table_out, 0), out_stride)
     if workspace is None:
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        workspace = cache.new_empty(nbytes)
     else:
         nbytes = workspace.numel() * workspace.element_size()
     _launch(dev, "entmax_cache_update", _lib.entmax_cache_update, c, layers, at, t, table.data_ptr(),
@@ -1708,12 +1708,11 @@ def cache_compact(cache, table, lengths, table_out=None, used_out=None, workspac
     c, layers, t, nbytes = args or _remember(key, _check_compact(cache, table, lengths, table_out, used_out, workspace))
     out_stride = t.width
     if table_out is None:
-        table_out = torch.empty((t.rows, t.width), dtype=torch.int32, device=dev)
-        used_out = torch.empty(1, dtype=torch.int32, device=dev)
+        table_out, used_out = lengths.new_empty((t.rows, t.width)), lengths.new_empty(1)
     else:
         out_stride = max(_stride(table_out, 0), out_stride)
     if workspace is None:
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        workspace = cache.new_empty(nbytes)
     else:
         nbytes = workspace.numel() * workspace.element_size()
     _launch(dev, "entmax_cache_compact", _lib.entmax_cache_compact, c, layers, at, t, table.data_ptr(),
@@ -1798,11 +1797,11 @@ def paged_decode(q, cache, table, lengths, rows=None, alpha=1.5, scale=None, max
     shape, params, c, t, qs, os_, nbytes = args or _remember(key, _check_paged(
         q, cache, table, lengths, rows, numbers, max_length, out, workspace))
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        out = q.new_empty(q.shape)
     else:
         os_ = _row_head(out)
     if workspace is None:
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        workspace = cache.new_empty(nbytes)
     else:
         nbytes = workspace.numel() * workspace.element_size()
     _launch(dev, "entmax_paged_decode", _lib.entmax_paged_decode, shape, params, c, at, t, table.data_ptr(), q_at, qs,

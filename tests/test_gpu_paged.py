@@ -176,3 +176,52 @@ def test_long_row():
     vals = pu.values(some)
     want, off = pu.paged64(q, vals, near, lengths, None, page, 1.5, 128 ** -0.5)
     check("long", got, want, 0.0, off)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("hq,hk,lengths", [(3, 1, [2000, 1500, 64]), (8, 1, [2040, 700]), (24, 2, [1024, 1000]),
+                                           (16, 1, [1024, 900, 15]), (40, 2, [1024, 777])])
+@pytest.mark.parametrize("c,alpha", [(0.02, 1.5), (0.3, 1.25), (0.5, 1.15)])
+def test_dense_short_rows(hq, hk, lengths, c, alpha, dtype):
+    """Short rows with more scores above the bound than one workgroup's lists hold."""
+    table, pages = pu.shuffled_table(lengths, 16, 0, hq)
+    cache = pu.filled(torch.empty(pages, hk, 2, 1, 544, dtype=torch.uint8), hq)
+    compare("short", queries(len(lengths), hq, 64, dtype, c, hq), cache, table, torch.tensor(lengths, dtype=I32), alpha=alpha)
+
+
+@pytest.mark.parametrize("copies,n,c,alpha", [
+    (1, 20000, 0.05, 1.25),    # more entries than a large workgroup's threads keep
+    (60, 20000, 0.05, 1.25), (60, 6000, 0.3, 1.5),  # (300 rows) and than a small one's
+    (220, 5000, 1.0, 1.5), (220, 5000, 0.05, 1.5)])  # (1100 rows) first waves alone, and all of them
+def test_many_queries_of_few_rows(copies, n, c, alpha):
+    """Five queries, again and again: as many rows as choose each of the kernels' forms."""
+    lengths = torch.tensor([n, n - 1, n // 2, 33, 0], dtype=I32)
+    table, pages = pu.shuffled_table([n, n // 2 + 1], 64, 1, 3)
+    cache = pu.filled(torch.empty(pages, 1, 2, 4, 544, dtype=torch.uint8), 21)
+    rows = torch.tensor([0, 0, 1, 1, 0], dtype=I32)
+    q = queries(5, 1, 64, BF, c, 9)
+    want, off = pu.paged64(q, pu.values(cache), table, lengths, rows, 64, alpha, 64 ** -0.5)
+    got = ea.paged_decode(q.repeat(copies, 1, 1).cuda(), cache.cuda(), table.cuda(), lengths.repeat(copies).cuda(),
+                          rows=rows.repeat(copies).cuda(), alpha=alpha)
+    check("many", got, want.repeat(copies, 1, 1), 0.0, off.repeat(copies, 1, 1))
+    assert torch.equal(got[:5].repeat(copies, 1, 1), got)  # (whichever workgroup: the same)
+
+
+def test_same_again_and_other_streams():
+    """The same bits at every call, on any stream, and with calls on two streams at once."""
+    table, pages = pu.shuffled_table([5000, 300, 2222], 32, 1, 12)
+    cache = pu.filled(torch.empty(pages, 2, 2, 2, 1088, dtype=torch.uint8), 13).cuda()
+    lengths = torch.tensor([5000, 300, 2222], dtype=I32).cuda()
+    table = table.cuda()
+    q = [queries(3, 6, 128, BF, c, 7).cuda() for c in (1.0, 0.1)]
+    want = [ea.paged_decode(x, cache, table, lengths, alpha=a) for x in q for a in (1.5, 1.25)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        for n, (x, a) in enumerate((x, a) for x in q for a in (1.5, 1.25)):
+            with torch.cuda.stream(streams[n % 2]):
+                got.append(ea.paged_decode(x, cache, table, lengths, alpha=a))
+    torch.cuda.synchronize()
+    for n, g in enumerate(got):
+        assert torch.equal(g, want[n % 4])
