@@ -21,6 +21,12 @@ def queries(n, hq, d, dtype, c, seed):
     return (torch.randn(n, hq, d, generator=torch.Generator().manual_seed(seed)) * c).to(dtype)
 
 
+def widened(table, page, wide):
+    """The table as it is (short rows: one launch), or with room for more tokens than a workgroup holds."""
+    more = -(-2064 // page) if wide else 0
+    return torch.cat([table, torch.full((table.shape[0], more), -1, dtype=I32)], 1)
+
+
 def compare(name, q, cache, table, lengths, rows=None, alpha=1.5, scale=None, **kw):
     page = 16 * cache.shape[3]
     scale_ = q.shape[-1] ** -0.5 if scale is None else scale
@@ -32,14 +38,16 @@ def compare(name, q, cache, table, lengths, rows=None, alpha=1.5, scale=None, **
     return got
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("alpha", [1.5, 1.25, 2.0, 1.4])
 @pytest.mark.parametrize("hq,hk,d,page,lengths", [
     (1, 1, 64, 16, [1, 0, 17]), (4, 4, 128, 32, [5, 33, 300]), (8, 2, 128, 16, [64, 1500, 3]), (14, 2, 64, 64, [129, 63, 1024]),
     (12, 1, 128, 128, [1025, 1023]), (40, 2, 64, 16, [700, 31]), (9, 3, 128, 1024, [2100, 1])])
-def test_decode(hq, hk, d, page, lengths, alpha, dtype):
+def test_decode(hq, hk, d, page, lengths, alpha, dtype, wide):
     seed = hq * 100 + page
     table, pages = pu.shuffled_table(lengths, page, 2, seed, width=max(-(-max(lengths) // page) + 1, 2))
+    table = widened(table, page, wide)
     cache = pu.filled(torch.empty(pages, hk, 2, page // 16, 17 * d // 2, dtype=torch.uint8), seed)
     c = {1.5: 1.0, 1.25: 2.0, 2.0: 0.7, 1.4: 4.0}[alpha]
     q = queries(len(lengths), hq, d, dtype, c, seed)
@@ -56,19 +64,21 @@ def test_dense_and_sparse_rows(c, alpha, dtype):
     compare("dense", queries(3, 6, 128, dtype, c, 1), cache, table, torch.tensor(lengths, dtype=I32), alpha=alpha)
 
 
-def test_rows_and_lengths():
+@pytest.mark.parametrize("wide", [False, True])
+def test_rows_and_lengths(wide):
     """Several queries to a row, rows in any order, lengths past both ends, rows that there are not."""
     table, pages = pu.shuffled_table([200, 90, 40], 16, 4, 9)
     cache = pu.filled(torch.empty(pages, 2, 2, 1, 544, dtype=torch.uint8), 7)
     rows = torch.tensor([1, 0, 0, 0, 2, -1, 3, 2 ** 31 - 1, -2 ** 31, 1], dtype=I32)
     lengths = torch.tensor([90, 198, 199, 200, 0, 50, 50, 50, 50, -3], dtype=I32)
     q = queries(10, 4, 64, BF, 1.0, 2)
-    got = compare("rows", q, cache, table, lengths, rows)
+    got = compare("rows", q, cache, widened(table, 16, wide), lengths, rows)
     assert (got[4:].float() == 0).all()
     # lengths behind the table's width, and max_length
     many = torch.tensor([2 ** 31 - 1, 1000, 208], dtype=I32)
     table[1, 6:] = table[0, 6:]
     table[2, 3:] = table[0, 3:]
+    table = widened(table, 16, wide)
     full = compare("width", q[:3], cache, table, many)
     cut = ea.paged_decode(q[:3].cuda(), cache.cuda(), table.cuda(), many.cuda(), max_length=100)
     want, off = pu.paged64(q[:3], pu.values(cache), table, many.clamp_max(100), None, 16, 1.5, 64 ** -0.5)
@@ -79,10 +89,12 @@ def test_rows_and_lengths():
     assert ea.paged_decode(q[:0].cuda(), cache.cuda(), table.cuda(), many[:0].cuda()).shape == (0, 4, 64)
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("dtype", [BF, F32])
-def test_pages_that_there_are_not(dtype):
+def test_pages_that_there_are_not(dtype, wide):
     """Entries of no page have no keys: in the middle, at the end, all of them."""
     table, pages = pu.shuffled_table([300, 300, 1400], 16, 2, 4)
+    table = widened(table, 16, wide)
     cache = pu.filled(torch.empty(pages, 1, 2, 1, 1088, dtype=torch.uint8), 8)
     table[0, 3:7] = torch.tensor([-1, pages, 2 ** 31 - 1, -2 ** 31], dtype=I32)
     table[1] = -1
@@ -92,12 +104,14 @@ def test_pages_that_there_are_not(dtype):
     assert (got[1] == 0).all()
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("dtype", [BF, F32])
-def test_not_finite(dtype):
+def test_not_finite(dtype, wide):
     """NaN keys have no probability; NaN values reach what they are used in; queries that
     are not finite give 0; bytes behind a row's end and in pages of others say nothing."""
     lengths = [100, 100, 100, 100, 100]
     table, pages = pu.shuffled_table(lengths, 32, 2, 6)
+    table = widened(table, 32, wide)
     cache = pu.filled(torch.empty(pages, 2, 2, 2, 1088, dtype=torch.uint8), 9)
     for r in range(5):
         last = cache[int(table[r, 3])]
@@ -122,11 +136,13 @@ def test_not_finite(dtype):
     assert not torch.isnan(nan[[0, 1, 3, 4]]).any()
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("dtype", [BF, F32])
-def test_magnitudes(dtype):
+def test_magnitudes(dtype, wide):
     """Queries and keys whose blocks differ by many powers of two."""
     lengths = [260, 100]
     table, pages = pu.shuffled_table(lengths, 16, 0, 5)
+    table = widened(table, 16, wide)
     cache = pu.filled(torch.empty(pages, 1, 2, 1, 1088, dtype=torch.uint8), 11)
     scales = cache[..., 1024:].view(pages, 1, 2, 1, 16, 4)
     scales[:, :, 0] += torch.tensor([20, 0, 246, 3], dtype=torch.uint8)  # (246: less 10)
@@ -139,8 +155,10 @@ def test_magnitudes(dtype):
     compare("magnitudes", q.to(dtype), cache, table, torch.tensor(lengths, dtype=I32), scale=0.02)
 
 
-def test_strides_out_and_workspace():
+@pytest.mark.parametrize("wide", [False, True])
+def test_strides_out_and_workspace(wide):
     table, pages = pu.shuffled_table([500, 70], 32, 1, 12)
+    table = widened(table, 32, wide)
     cache = pu.filled(torch.empty(pages, 2, 2, 2, 1088, dtype=torch.uint8), 13)
     lengths = torch.tensor([500, 70], dtype=I32)
     q = queries(2, 8, 128, BF, 1.0, 7)
@@ -148,9 +166,9 @@ def test_strides_out_and_workspace():
     rows = torch.zeros(2, 3, 8, 128, dtype=BF, device="cuda")
     rows[:, 1] = q.cuda()
     out = torch.full((2, 8, 256), 5.0, dtype=BF, device="cuda")
-    wide = torch.full((2, 20), -1, dtype=I32, device="cuda")
-    wide[:, 2:2 + table.shape[1]] = table.cuda()
-    t = wide[:, 2:2 + table.shape[1]]
+    around = torch.full((2, table.shape[1] + 4), -1, dtype=I32, device="cuda")
+    around[:, 2:2 + table.shape[1]] = table.cuda()
+    t = around[:, 2:2 + table.shape[1]]
     ws = torch.full((ea.paged_decode_workspace(q, cache, t),), 0xFF, dtype=torch.uint8, device="cuda")
     for byte in (0xFF, 0x7F, 0):
         ws.fill_(byte)
