@@ -528,7 +528,7 @@ ea_status entmax_cache_read(const ea_cache* c, const void* cache, const ea_page_
  * its length) from number `used` on, their count, move to the free ones below, in
  * order; table_out [table rows, width] names the new places, and used is 1 number.
  * workspace: entmax_cache_workspace bytes for as many rows (rows_out), 16-byte aligned.
- * rows_out may be 0.  Two launches each, or four: with more than 1024 rows, 2^18
+ * rows_out may be 0.  Two launches each, or four: with more than 256 rows, 2^17
  * entries or 2^17 pages.
  */
 ea_status entmax_cache_workspace(const ea_cache* c, int32_t rows, size_t* bytes);

@@ -19,7 +19,7 @@
 // a region's lanes are scores of distinct keys, so f restricted to them lies below f,
 // and its root is a lower bound of tau.  (Those within 1 of the largest, as
 // tau is at least max x - 1, were ten times as many: 64 requests of up to 9216 keys,
-// 32/8 heads, d = 128, 45 us against 33.)
+// 32/8 heads, d = 128, this step 45 us against 39.)
 //
 // Solve.  One workgroup per query row.  The regions' bounds, and in the same way the
 // largest scores of its regions, bound tau from below; the listed scores above that go to LDS, tau is solved on them
@@ -510,18 +510,18 @@ constexpr int SO_FEW = 64 * SO_LANE;
 constexpr int SO_OWN = 16;              // scores per thread of a workgroup that solves one
 constexpr int SO_BUFFER = 256;          // entries on their way to a wave's gather
 
-// Rows with few scores above the bound are solved by the first wave alone, without
-// barriers; the others help it with the rows of V (share), or end, where there are rows
-// for every wave of the device.  Rows with more are solved by all of them: each thread
-// keeps SO_OWN scores, and reads the others of its own for every evaluation.
+// Rows with few scores above the bound are the first wave's alone, without barriers.
+// (With the other waves for a share of the rows of V: one request of 9000 keys, 32 heads,
+// 16.1 us against 16.3, 64 requests 53.8 against 49.9.)  Rows with more are solved by all of
+// them: each thread keeps SO_OWN scores, and reads the others of its own for every evaluation.
 template <typename E, int D, int GK, int NT>
-__global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a, int share) {
+__global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
   constexpr int WAVES = NT / 64, KPW = RowSum<D>::KPW;
   static_assert(WAVES * SO_BUFFER >= SO_FEW, "a wave's scores fit in the place of all buffers");
   __shared__ u32x2_t buffer[WAVES][SO_BUFFER];
   __shared__ __attribute__((aligned(16))) float sums[WAVES][D];
   __shared__ float red[2][3][WAVES];
-  __shared__ int starts[MAX_REGIONS + 1], row_count;
+  __shared__ int starts[MAX_REGIONS + 1];
   __shared__ float row_top, row_bound;
   const int t = threadIdx.x, lane = lane_id(), w = wave_id();
   // (heads of one key head are kv_heads apart: with eight of them, on one XCD)
@@ -605,43 +605,36 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a, int share)
   RowSum<D> o(a, kv);
 
   if (entries <= SO_FEW) {
+    if (w) return;
     u32x2_t* const kept = buffer[0];
-    if (w == 0) {
-      float own[SO_LANE];
-      u32x2_t v[SO_LANE];
+    float own[SO_LANE];
+    u32x2_t v[SO_LANE];
 #pragma unroll
-      for (int e = 0; e < SO_LANE; ++e) {
-        v[e] = u32x2_t{0xFF800000u, 0};  // (-inf)
-        if (64 * e + lane < entries) v[e] = *entry(64 * e + lane);
-      }
-#pragma unroll
-      for (int e = 0; e < SO_LANE; ++e) {
-        own[e] = __uint_as_float(v[e][0]);
-        if (64 * e + lane < entries) kept[64 * e + lane] = v[e];
-      }
-      const float tau = solve_tau(a, lo, m, len, [&](float tau, float& s0, float& s1, float& s2) {
-#pragma unroll
-        for (int e = 0; e < SO_LANE; ++e) {
-          if (64 * e >= entries) break;
-          add_z<GK>(relu_z(c, own[e], tau), gm, s0, s1, s2);
-        }
-        s0 = fold64(s0, addf);
-        s1 = fold64(s1, addf);
-        s2 = fold64(s2, addf);
-      });
-      const int n = keep_probable<GK>(a, kept, entries, tau);
-      if (!share) {
-        o.add(kept, 0, KPW, n);
-        o.store(sums[0]);
-        for (int d = lane; d < D; d += 64) O[d] = (E)sums[0][d];
-      } else if (lane == 0) {
-        row_count = n;
-      }
+    for (int e = 0; e < SO_LANE; ++e) {
+      v[e] = u32x2_t{0xFF800000u, 0};  // (-inf)
+      if (64 * e + lane < entries) v[e] = *entry(64 * e + lane);
     }
-    if (!share) return;
-    __syncthreads();
-    o.add(kept, w * KPW, WAVES * KPW, __builtin_amdgcn_readfirstlane(row_count));
-  } else {
+#pragma unroll
+    for (int e = 0; e < SO_LANE; ++e) {
+      own[e] = __uint_as_float(v[e][0]);
+      if (64 * e + lane < entries) kept[64 * e + lane] = v[e];
+    }
+    const float tau = solve_tau(a, lo, m, len, [&](float tau, float& s0, float& s1, float& s2) {
+#pragma unroll
+      for (int e = 0; e < SO_LANE; ++e) {
+        if (64 * e >= entries) break;
+        add_z<GK>(relu_z(c, own[e], tau), gm, s0, s1, s2);
+      }
+      s0 = fold64(s0, addf);
+      s1 = fold64(s1, addf);
+      s2 = fold64(s2, addf);
+    });
+    o.add(kept, 0, KPW, keep_probable<GK>(a, kept, entries, tau));
+    o.store(sums[0]);
+    for (int d = lane; d < D; d += 64) O[d] = (E)sums[0][d];
+    return;
+  }
+  {
     // a thread's entries are t, t + NT ..
     u32x2_t own[SO_OWN];
 #pragma unroll
@@ -885,9 +878,10 @@ hipError_t launch_scores(const PagedArgs& a, hipStream_t s) {
 int64_t short_wgs(const PagedArgs& a) { return (int64_t)a.queries * head_tiles(a) * a.c.kv_heads; }
 
 // Rows that one workgroup each takes, where every one has a compute unit: us in a graph,
-// against the two kernels, 32/8 heads, d = 128, 1, 16 and 64 requests (8, 128 and 512
-// workgroups) of up to 128 keys 9.9, 10.1, 18.4 against 11.4, 12.3, 12.8, of up to
-// 1000 11.0, 11.9, 21.8 against 13.4, 15.8, 17.2.
+// against the two kernels, 32/8 heads, d = 128, 1, 16 and 32 requests (8, 128 and 256
+// workgroups) of up to 128 keys 9.7, 10.0, 10.2 against 11.6, 11.8, 12.0, of up to 1000
+// 11.1, 11.5, 11.9 against 13.7, 14.1, 14.3, of up to 2000 13.2, 13.8, 14.5 against 13.8,
+// 14.8, 17.0; 64 requests (512) of up to 128 and 1000 18.4, 21.8 against 12.8, 17.2.
 bool short_rows(const PagedArgs& a) {
   return a.longest <= SH_WAVES * PAGE_TILE * sh_tiles(head_registers(a)) && short_wgs(a) <= 256;
 }
@@ -908,11 +902,7 @@ hipError_t launch_solve(const PagedArgs& a, hipStream_t s) {
   if (a.gk == 1) kernel = paged_solve_kernel<E, D, 1, NT>;
   if (a.gk == 2) kernel = paged_solve_kernel<E, D, 2, NT>;
   if (a.gk == 4) kernel = paged_solve_kernel<E, D, 4, NT>;
-  PagedArgs args = a;
-  int share = a.queries * a.heads < 1024;
-  void* params[] = {&args, &share};
-  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), dim3((unsigned)(a.queries * a.heads)), dim3(NT), params,
-                         0, s);
+  return launch_kernel(kernel, dim3((unsigned)(a.queries * a.heads)), dim3(NT), s, a);
 }
 
 template <typename E, int D>
@@ -922,6 +912,10 @@ hipError_t launch_paged(const PagedArgs& a, hipStream_t s) {
     const hipError_t e = launch_scores<E, D>(a, s);
     if (e != hipSuccess) return e;
   }
+  // Rows that have a compute unit each take 16 waves, for the dense ones: us in a graph, 32/8
+  // heads, d = 128, up to 9000 keys, against four waves: 1 and 8 requests, alpha 1.5, c = 1,
+  // 16.6 and 20.2 against 16.1 and 19.6; 8, alpha 1.25, c = 0.5, 44 against 74; 16 (512 rows)
+  // of those 77 to 86 either way, 64 213 against 170.
   return a.queries * a.heads <= 256 ? launch_solve<E, D, 1024>(a, s) : launch_solve<E, D, 256>(a, s);
 }
 

@@ -259,7 +259,7 @@ __device__ __forceinline__ RowPlan kept_of(const CacheUpdateArgs& a, int r) {
 // all holders there took a look for every entry: 64 rows of up to 256 pages 12.5 us against
 // 9.1.)  It is bound by its chain of loads and barriers: a row's parent, its length, its
 // entries.
-constexpr int PL_ROWS = UP_NT, PL_WORDS = 4096, PL_SLOTS = 2 * PL_ROWS;
+constexpr int PL_ROWS = 256, PL_WORDS = 4096, PL_SLOTS = 2 * PL_ROWS;
 constexpr int PL_BATCH = 4, PL_LOADS = 2;  // rows of a wave, and entries of a lane of each, in flight
 
 struct PageSet {
@@ -349,8 +349,8 @@ __global__ __launch_bounds__(UP_NT) void update_small_kernel(CacheUpdateArgs a) 
     kept[t] = p.kept - (p.writes ? 1 : 0);  // (the page that it writes to is looked at below)
     last = last_page(a, t, p);
   }
-  auto first = [](int page) { return (int)((uint32_t)page * 0x9E3779B1u >> 21); };
-  static_assert(PL_SLOTS == 1 << 11, "a hash is 11 bits");
+  auto first = [](int page) { return (int)((uint32_t)page * 0x9E3779B1u >> 23); };
+  static_assert(PL_SLOTS == 1 << 9, "a hash is 9 bits");
   if (last >= 0) {
     for (slot = first(last);; slot = (slot + 1) % PL_SLOTS) {  // (at most half of the slots are taken)
       const int was = atomicCAS(&key[slot], -1, last);
@@ -370,8 +370,10 @@ __global__ __launch_bounds__(UP_NT) void update_small_kernel(CacheUpdateArgs a) 
   const int need = t < a.rows_out ? p.grown + copy : 0;
   const int at = place_of(need, needed, sums, turn);
   if (last >= 0) atomicOr(&held_words[last >> 5], 1u << (last & 31));
-  before[t] = at;
-  kept[t] = p.kept | copy << 30;
+  if (t < PL_ROWS) {
+    before[t] = at;
+    kept[t] = p.kept | copy << 30;
+  }
   if (t == 0) before[PL_ROWS] = needed;
   __syncthreads();
   // ---- as many free pages, the lowest first
@@ -487,6 +489,7 @@ __global__ __launch_bounds__(256) void update_rows_kernel(CacheUpdateArgs a) {
 
 __global__ __launch_bounds__(UP_NT) void update_plan_kernel(CacheUpdateArgs a) {
   __shared__ int sums[2][UP_WAVES];
+  __shared__ int many, grown_row[UP_NT], grown_kept[UP_NT], grown_pages[UP_NT], grown_at[UP_NT];
   const int t = threadIdx.x, lane = lane_id(), w = wave_id();
   auto row_copies = [&](int r, int last) {
     return last >= 0 && copies(a.holders[last], a.writers[last], a.lowest[last], r);
@@ -519,23 +522,39 @@ __global__ __launch_bounds__(UP_NT) void update_plan_kernel(CacheUpdateArgs a) {
       if (h[e] == 0) a.free_list[at++] = p0 + 4 * t + e;
   }
   __syncthreads();
-  // (a wave to a row)
-  for (int r = w; r < a.rows_out; r += UP_WAVES) {
-    const RowPlan p = plan_of(a, r);
-    const int last = last_page(a, r, p), copy = row_copies(r, last) ? 1 : 0;
-    const int need = p.grown + copy, at = a.before[r];
-    const bool done = need == 0 || count_up(at, need) <= found;
-    int32_t* const out = a.table_out + r * a.out_stride;
-    if (done)
-      for (int i = lane; i < p.grown; i += 64) out[p.kept + i] = a.free_list[at + copy + i];
-    if (lane == 0) {
+  // (a thread to a row; rows that grow by many pages have them from a wave each)
+  for (int r0 = 0; r0 < a.rows_out; r0 += UP_NT) {
+    const int r = r0 + t;
+    if (t == 0) many = 0;
+    __syncthreads();
+    if (r < a.rows_out) {
+      const RowPlan p = plan_of(a, r);
+      const int last = last_page(a, r, p), copy = row_copies(r, last) ? 1 : 0;
+      const int need = p.grown + copy, at = a.before[r];
+      const bool done = need == 0 || count_up(at, need) <= found;
+      int32_t* const out = a.table_out + r * a.out_stride;
       const int to = done && copy ? a.free_list[at] : -1;
       if (to >= 0) out[p.old >> a.c.shift] = to;
       a.source[r] = last;
       a.target[r] = to;
       a.lengths_out[r] = done ? p.wanted : p.old;
       a.missing[r] = !p.fits ? -1 : done ? 0 : need;
+      if (done && p.grown <= 4) {
+        for (int i = 0; i < p.grown; ++i) out[p.kept + i] = a.free_list[at + copy + i];
+      } else if (done) {
+        const int n = atomicAdd(&many, 1);
+        grown_row[n] = r;
+        grown_kept[n] = p.kept;
+        grown_pages[n] = p.grown;
+        grown_at[n] = at + copy;
+      }
     }
+    __syncthreads();
+    for (int n = w; n < many; n += UP_WAVES) {
+      int32_t* const out = a.table_out + grown_row[n] * a.out_stride + grown_kept[n];
+      for (int i = lane; i < grown_pages[n]; i += 64) out[i] = a.free_list[grown_at[n] + i];
+    }
+    __syncthreads();
   }
 }
 
@@ -616,9 +635,13 @@ hipError_t launch_clear(const CacheUpdateArgs& a, hipStream_t s) {
   return launch_kernel(clear_kernel, dim3((unsigned)((a.c.pages + 255) / 256)), dim3(256), s, a);
 }
 
-// Tables that one workgroup plans.
+// Tables that one workgroup plans.  Larger ones are read faster by a workgroup for each
+// row: us in a graph, pages of 16 tokens, updates of 4 rows of 100 pages, 64 of 128, 256 of
+// 128, 512 of 64, 256 of 400 and 32 of 4000 6.7, 7.4, 11.2, 15.9, 19.0, 24.7 against 10.4,
+// 10.8, 12.4, 13.6, 15.3, 21.8; compactions 9.5, 10.6, 23.4, 28.0, 66.1, 42.1 against 12.2,
+// 15.7, 27.5, 27.5, 65.9, 38.0.  (The host knows the tables' widths alone.)
 bool small_tables(const CacheUpdateArgs& a, int rows) {
-  return rows <= PL_ROWS && a.c.pages <= 32 * PL_WORDS && (int64_t)rows * a.t.width <= 1 << 18;
+  return rows <= PL_ROWS && a.c.pages <= 32 * PL_WORDS && (int64_t)rows * a.t.width <= 1 << 17;
 }
 
 }  // namespace

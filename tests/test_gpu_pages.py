@@ -242,7 +242,8 @@ def test_update_copies_only_what_is_written():
 # (rows, width, pages, longest, growing row): tables of one workgroup's plan and others
 @pytest.mark.parametrize("rows,width,pages,longest,grows", [
     (1500, 4096, 20000, 300, 700), (8, 8192, 70000, 131000, 3), (64, 4096, 131072, 30000, 63),
-    (64, 4097, 131072, 30000, 10), (30, 100, 131073, 1599, 5), (1024, 256, 65536, 1000, 9)])
+    (64, 4097, 131072, 30000, 10), (30, 100, 131073, 1599, 5), (1024, 256, 65536, 1000, 9),
+    (256, 512, 65536, 4000, 77), (256, 513, 65536, 4000, 77), (257, 300, 65536, 2000, 99), (16, 8192, 131072, 100000, 2)])
 def test_update_of_a_long_pool(rows, width, pages, longest, grows):
     """Free pages found behind many used ones, many rows, a long growth."""
     page = 16
@@ -299,7 +300,8 @@ def test_compact(seed):
 
 
 @pytest.mark.parametrize("rows,width,pages,each", [(8, 600, 9000, 600), (20, 8192, 131072, 3000), (40, 8192, 131072, 3000),
-                                                   (20, 1000, 200000, 1000), (1100, 100, 110000, 90)])
+                                                   (20, 1000, 200000, 1000), (1100, 100, 110000, 90),
+                                                   (256, 300, 131072, 300), (257, 300, 131072, 300), (16, 8192, 131072, 5000)])
 def test_compact_of_a_long_pool(rows, width, pages, each):
     ids = torch.full((rows, width), -1, dtype=I32)
     ids[:, :each] = torch.randperm(pages, generator=torch.Generator().manual_seed(2))[:rows * each].view(rows, each).int()
