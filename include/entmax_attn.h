@@ -495,7 +495,8 @@ ea_status entmax_cache_page_bytes(const ea_cache* c, size_t* bytes);
  * rounded to the nearest number, ties to the even code, magnitudes above 6 to 6;
  * 32 values of which one is not finite become NaN.  A token whose row, position
  * or page there is not is left out.  Two tokens of one call that have the same
- * place leave either's bytes in any part of it.  Nothing else is written.
+ * place leave either's bytes in any part of it.  Nothing else is written.  k and
+ * v do not overlap the cache.
  * Read: the same rows' values (exact in both types), 0 where there is no page.
  * tokens may be 0.  One launch each.
  */

@@ -260,7 +260,6 @@ __device__ __forceinline__ RowPlan kept_of(const CacheUpdateArgs& a, int r) {
 // 9.1.)  It is bound by its chain of loads and barriers: a row's parent, its length, its
 // entries.
 constexpr int PL_ROWS = 256, PL_WORDS = 4096, PL_SLOTS = 2 * PL_ROWS;
-constexpr int PL_BATCH = 4, PL_LOADS = 2;  // rows of a wave, and entries of a lane of each, in flight
 
 struct PageSet {
   uint32_t* word;  // a bit for each page
@@ -276,43 +275,44 @@ struct PageSet {
   }
 };
 
-// use(pages) of the entries [0, kept[r]) of the table's rows from[r], some at a time, -1 where
-// they name no page.
-template <typename F>
-__device__ __forceinline__ void each_held(const CacheUpdateArgs& a, const int* from, const int* kept, int rows, F&& use) {
+// Marks the pages that the entries [0, kept[r]) of the table's rows from[r] name: BATCH rows of a
+// wave, and LOADS entries of a lane of each, are in flight.
+template <int BATCH, int LOADS>
+__device__ __forceinline__ void mark_rows(const CacheUpdateArgs& a, uint32_t* held, const int* from, const int* kept,
+                                          int rows) {
   const int lane = lane_id();
-  for (int r0 = wave_id(); r0 < rows; r0 += PL_BATCH * UP_WAVES) {
-    int n[PL_BATCH], most = 0;
-    const int32_t* in[PL_BATCH];
+  for (int r0 = wave_id(); r0 < rows; r0 += BATCH * UP_WAVES) {
+    int n[BATCH], most = 0;
+    const int32_t* in[BATCH];
 #pragma unroll
-    for (int j = 0; j < PL_BATCH; ++j) {
+    for (int j = 0; j < BATCH; ++j) {
       const int r = r0 + j * UP_WAVES;
       n[j] = r < rows ? kept[r] : 0;
       in[j] = a.t.ids + (n[j] ? from[r] : 0) * a.t.stride;
       most = max(most, n[j]);
     }
-    for (int e0 = lane; e0 < most; e0 += 64 * PL_LOADS) {
-      int id[PL_BATCH][PL_LOADS];
+    for (int e0 = lane; e0 < most; e0 += 64 * LOADS) {
+      int id[BATCH][LOADS];
 #pragma unroll
-      for (int j = 0; j < PL_BATCH; ++j)
+      for (int j = 0; j < BATCH; ++j)
 #pragma unroll
-        for (int u = 0; u < PL_LOADS; ++u) id[j][u] = e0 + 64 * u < n[j] ? in[j][e0 + 64 * u] : -1;
+        for (int u = 0; u < LOADS; ++u) id[j][u] = e0 + 64 * u < n[j] ? in[j][e0 + 64 * u] : -1;
 #pragma unroll
-      for (int j = 0; j < PL_BATCH; ++j)
+      for (int j = 0; j < BATCH; ++j)
 #pragma unroll
-        for (int u = 0; u < PL_LOADS; ++u)
-          if (id[j][u] >= a.c.pages) id[j][u] = -1;
-      use(id);
+        for (int u = 0; u < LOADS; ++u)
+          if (id[j][u] >= 0 && id[j][u] < a.c.pages) atomicOr(&held[id[j][u] >> 5], 1u << (id[j][u] & 31));
     }
   }
 }
-
-__device__ __forceinline__ void mark(uint32_t* held, const int (&id)[PL_BATCH][PL_LOADS]) {
-#pragma unroll
-  for (int j = 0; j < PL_BATCH; ++j)
-#pragma unroll
-    for (int u = 0; u < PL_LOADS; ++u)
-      if (id[j][u] >= 0) atomicOr(&held[id[j][u] >> 5], 1u << (id[j][u] & 31));
+// (64 rows of 128 pages 7.3 us with four rows and two entries, 9.1 with eight and one; 256 beams
+// of 30 11.2 and 10.3.  Pieces of 64 entries, whichever rows they are of: 9.3 and 11.0.)
+__device__ __forceinline__ void mark_held(const CacheUpdateArgs& a, uint32_t* held, const int* from, const int* kept,
+                                          int rows) {
+  if (rows <= 64)
+    mark_rows<4, 2>(a, held, from, kept, rows);
+  else
+    mark_rows<8, 1>(a, held, from, kept, rows);
 }
 
 // Workgroup 0 plans; workgroup 1 + r writes those entries of row r that need no plan.
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(UP_NT) void update_small_kernel(CacheUpdateArgs a) 
     atomicMin(&lowest[slot], t);
   }
   __syncthreads();
-  each_held(a, from, kept, a.rows_out, [&](const int (&id)[PL_BATCH][PL_LOADS]) { mark(held_words, id); });
+  mark_held(a, held_words, from, kept, a.rows_out);
   __syncthreads();
   // ---- pages needed before each row.  A page that rows are about to write to is held by
   // these, and by others if it is marked by now.
@@ -448,7 +448,7 @@ __global__ __launch_bounds__(UP_NT) void compact_small_kernel(CacheUpdateArgs a)
     kept[t] = kept_of(a, t).kept;
   }
   __syncthreads();
-  each_held(a, from, kept, a.t.rows, [&](const int (&id)[PL_BATCH][PL_LOADS]) { mark(held_words, id); });
+  mark_held(a, held_words, from, kept, a.t.rows);
   __syncthreads();
   pair_pages(a, held, sums);
 }

@@ -243,3 +243,35 @@ def test_same_again_and_other_streams():
     torch.cuda.synchronize()
     for n, g in enumerate(got):
         assert torch.equal(g, want[n % 4])
+
+
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("c,alpha,scale", [(100.0, 1.5, 0.1), (100.0, 2.0, 0.1), (1000.0, 1.25, 0.1), (1.0, 1.01, 0.1),
+                                           (1.0, 1.9, 1e-4), (1.0, 1.5, 1e-30), (3.0, 1.001, 1.0)])
+def test_steep_and_flat(c, alpha, scale, dtype, wide):
+    """Scores of thousands, where one or two keys have it all, and all alike; alpha next to 1."""
+    lengths = [900, 37]
+    table, pages = pu.shuffled_table(lengths, 16, 0, 5)
+    table = widened(table, 16, wide)
+    cache = pu.filled(torch.empty(pages, 1, 2, 1, 544, dtype=torch.uint8), 31)
+    compare("steep", queries(2, 3, 64, dtype, c, 8), cache, table, torch.tensor(lengths, dtype=I32), alpha=alpha,
+            scale=scale, max_iter=64)
+
+
+@pytest.mark.parametrize("wide", [False, True])
+def test_iterations_and_limits(wide):
+    """No iterations, none left out (tol 0), and products that overflow: finite, and 0 in the end."""
+    lengths = torch.tensor([900, 37], dtype=I32)
+    table, pages = pu.shuffled_table([900, 37], 16, 0, 5)
+    table = widened(table, 16, wide).cuda()
+    cache = pu.filled(torch.empty(pages, 1, 2, 1, 544, dtype=torch.uint8), 31).cuda()
+    q = queries(2, 3, 64, F32, 1.0, 8).cuda()
+    args = (cache, table, lengths.cuda())
+    once = ea.paged_decode(q, *args, max_iter=0)
+    all_of_them = ea.paged_decode(q, *args, max_iter=64, tol=0.0)
+    assert torch.isfinite(once).all()
+    want, off = pu.paged64(q.cpu(), pu.values(cache), table.cpu(), lengths, None, 16, 1.5, 64 ** -0.5)
+    check("tol 0", all_of_them, want, 0.0, off)
+    assert (ea.paged_decode(q * 1e30, *args, scale=1e30) == 0).all()  # (scores times scale past fp32)
+    assert torch.isfinite(ea.paged_decode(q * 1e15, *args)).all()
