@@ -317,6 +317,7 @@ __global__ __launch_bounds__(PS_NT) void paged_scores_kernel(PagedArgs a, int he
   __shared__ __attribute__((aligned(16))) Digits<E, D> q;
   __shared__ float lane_top[PS_WAVES][PS_HEADS][16];
   __shared__ int wave_count[PS_WAVES][PS_HEADS];
+  __shared__ float head_top[PS_HEADS], head_bound[PS_HEADS];
   const int lane = lane_id(), w = wave_id(), col = lane & 15, g = lane >> 4;
   int x = blockIdx.x;
   const int kv = x % a.c.kv_heads;
@@ -337,17 +338,42 @@ __global__ __launch_bounds__(PS_NT) void paged_scores_kernel(PagedArgs a, int he
 #pragma unroll
   for (int r = 0; r < R4; ++r) lane_top[w][g + 4 * r][col] = top[r];
   __syncthreads();
-  // (every wave by itself: with a barrier more instead the longest rows took 33.6 us, 32.5 so)
+  // A wave bounds the four heads of its lane groups: each four by a wave of their own and
+  // a barrier more, but up to four heads by every wave for itself. Whole calls: 8 rows of
+  // 30000 keys, 40/2 heads, 33.3 us, and 35.8 with every wave bounding all; 16 of 8000,
+  // 16/1 heads, 18.7 and 20.1; 64 of 9000, 32/4 heads, 39.5 and 40.5. With four heads the
+  // barrier costs more than it saves: this kernel took 33.6 us so on 65536 keys, 32.5
+  // without.
+  auto bound_of = [&](int j, float& largest) {
+    float v[PS_WAVES];
+#pragma unroll
+    for (int y = 0; y < PS_WAVES; ++y) v[y] = lane_top[y][j][col];
+    largest = fold16(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), maxf);
+    const float lo = region_bound(a, v, largest);
+    return j < heads ? lo : INFINITY;
+  };
   float bound[R4];
+  if constexpr (R4 == 1) {
+    bound[0] = bound_of(g, top[0]);
+  } else {
+    if (w < R4) {
+      float largest;
+      const float lo = bound_of(g + 4 * w, largest);
+      if (col == 0) {
+        head_top[g + 4 * w] = largest;
+        head_bound[g + 4 * w] = lo;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < R4; ++r) {
+      top[r] = head_top[g + 4 * r];
+      bound[r] = head_bound[g + 4 * r];
+    }
+  }
   int mine[R4], to[R4];
 #pragma unroll
   for (int r = 0; r < R4; ++r) {
-    float v[PS_WAVES];
-#pragma unroll
-    for (int y = 0; y < PS_WAVES; ++y) v[y] = lane_top[y][g + 4 * r][col];
-    top[r] = fold16(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), maxf);
-    const float lo = region_bound(a, v, top[r]);
-    bound[r] = g + 4 * r < heads ? lo : INFINITY;
     int all;
     mine[r] = W::above(s, r, a.scale_c, bound[r], to[r], all);
     if (col == 15) wave_count[w][g + 4 * r] = all;
