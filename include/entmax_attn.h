@@ -556,7 +556,8 @@ ea_status entmax_cache_compact(const ea_cache* c, int32_t layers, void* cache, c
  * queries * heads < 2^23; kv_heads times the regions of 1024 keys of every
  * query < 2^24.  workspace: entmax_paged_decode_workspace bytes, 16-byte aligned
  * (8 bytes for every query head and key of `longest`, of which few are used).
- * Two launches.
+ * Two launches, or one: few queries of at most 2048 keys (1024 with more than eight
+ * heads to a key head).
  */
 typedef struct {
   int32_t queries, heads, dtype;
