@@ -514,8 +514,9 @@ ea_status entmax_cache_read(const ea_cache* c, const void* cache, const ea_page_
  * lengths[parents[r]] tokens it has, and gains counts[r] tokens (loses its last
  * -counts[r], where negative), for which it gets pages.  Rows may share pages:
  * where a row is about to write to a page that others hold as well, it gets a
- * copy (of all rows that hold the page and are about to write to it, the lowest
- * keeps it if no other holds it).  Pages that no row of the new table keeps are
+ * copy (of all rows that hold the page and are about to write to it, one keeps it if no
+ * other holds it: the lowest, or, where fewer pages are free than all rows need, the one whose
+ * tokens end furthest into the page, of several the lowest).  Pages that no row of the new table keeps are
  * free, and are given out lowest first, row by row: for the copy, then for the
  * pages behind.  A row gets all of its pages or none: missing[r] is 0, or the
  * pages that it needed where those up to it needed more than are free, or -1 where its

@@ -1634,7 +1634,9 @@ def cache_update(cache, table, lengths, parents, counts, table_out=None, lengths
 
     Rows may go on from the same row: they share its pages, and where a row is
     about to write to a page that others hold as well, it gets a copy in every
-    layer (cache: a model's, or one layer's).  Pages that no new row holds are free;
+    layer (cache: a model's, or one layer's).  Where all rows that hold a page are about to
+    write to it, one keeps it: the lowest, or with fewer free pages than all rows need the one
+    whose tokens end furthest into it, so that the others' tokens stay.  Pages that no new row holds are free;
     they are given out lowest first, row by row.  A row gets all of its pages or none:
     missing_out[r] is 0, or the pages that it needed where there were not enough, or -1
     where its tokens do not fit the table; such a row keeps its tokens and gains none.

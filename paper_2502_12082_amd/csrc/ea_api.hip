@@ -1243,6 +1243,7 @@ size_t update_parts(const PageDims& c, int rows, void* base, CacheUpdateArgs* a)
   a->holders = p.take<int32_t>(c.pages);
   a->writers = p.take<int32_t>(c.pages);
   a->lowest = p.take<int32_t>(c.pages);
+  a->furthest = p.take<int32_t>(c.pages);
   a->free_list = p.take<int32_t>(c.pages);
   a->before = p.take<int32_t>(rows);
   a->source = p.take<int32_t>(pairs);

@@ -239,10 +239,10 @@ struct CacheUpdateArgs {
   int rows_out;
   int32_t *lengths_out, *missing;  // [rows_out]; of a compaction `missing` is one number, the pages in use
   // workspace: [pages] rows that hold each page, rows about to write to it, the
-  // lowest of those, and free pages (compaction: a bit for each page in use, -, where pages
-  // go, -), [rows_out] pages needed before each row, [copies] page pairs, and the
-  // number of copies of a compaction
-  int32_t *holders, *writers, *lowest, *free_list, *before, *source, *target, *marks;
+  // lowest of those, the one furthest into it (its keeper_key), and free pages (compaction: a bit
+  // for each page in use, -, where pages go, -, -), [rows_out] pages needed before each row,
+  // [copies] page pairs, and the number of copies of a compaction
+  int32_t *holders, *writers, *lowest, *furthest, *free_list, *before, *source, *target, *marks;
 };
 constexpr int UPDATE_MARKS = 1;
 

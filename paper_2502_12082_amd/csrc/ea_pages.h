@@ -75,12 +75,22 @@ EA_HD RowPlan plan_row(int32_t length, int32_t count, int32_t width, int shift) 
   r.writes = wanted > old && (old & ((1 << shift) - 1)) != 0;
   return r;
 }
-// Whether a row that is about to write to a page which `holders` rows hold, `writers`
-// of them about to write to it, the lowest being number `lowest`, gets a copy
-// of it.  Where all holders write, the lowest keeps the page: the others' copies
-// are made before anything is written.
-EA_HD bool copies(int32_t holders, int32_t writers, int32_t lowest, int32_t row) {
-  return holders > 1 && (holders > writers || lowest != row);
+// A page that rows are about to write to, and that no other row holds, is kept by one of
+// them: row `keeper`; the others get copies, which are made before anything is written.
+// With pages enough for all copies the keeper is the lowest of them.  Otherwise rows that get no
+// copy go on holding the page, and the keeper must not write where they have tokens: it
+// is the row whose tokens end furthest into the page, of several the lowest.  (Either way there
+// are as many copies.)
+EA_HD bool copies(int32_t holders, int32_t writers, int32_t keeper, int32_t row) {
+  return holders > 1 && (holders > writers || keeper != row);
 }
+// A number of a row of `old` tokens that writes to its last page, the smallest of that
+// row's; pages hold at most 2^10 tokens, and rows are fewer than 2^20 (their numbers).
+constexpr int KEEPER_ROW_BITS = 20;
+EA_HD int32_t keeper_key(int32_t old, int shift, int32_t row) {
+  const int32_t end = (1 << shift) - 1;
+  return (end - (old & end)) << KEEPER_ROW_BITS | row;
+}
+EA_HD int32_t keeper_row(int32_t key) { return key & ((1 << KEEPER_ROW_BITS) - 1); }
 
 }  // namespace ea

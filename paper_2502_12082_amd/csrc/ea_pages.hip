@@ -259,7 +259,7 @@ __device__ __forceinline__ RowPlan kept_of(const CacheUpdateArgs& a, int r) {
 // all holders there took a look for every entry: 64 rows of up to 256 pages 12.5 us against
 // 9.1.)  It is bound by its chain of loads and barriers: a row's parent, its length, its
 // entries.
-constexpr int PL_ROWS = 256, PL_WORDS = 4096, PL_SLOTS = 2 * PL_ROWS;
+constexpr int PL_ROWS = 256, PL_WORDS = 4096, PL_SLOTS = 2 * PL_ROWS, PL_FREE = 2048;
 
 struct PageSet {
   uint32_t* word;  // a bit for each page
@@ -318,10 +318,9 @@ __device__ __forceinline__ void mark_held(const CacheUpdateArgs& a, uint32_t* he
 // Workgroup 0 plans; workgroup 1 + r writes those entries of row r that need no plan.
 __global__ __launch_bounds__(UP_NT) void update_small_kernel(CacheUpdateArgs a) {
   __shared__ uint32_t held_words[PL_WORDS];
-  __shared__ int slots[3][PL_SLOTS];
-  int *const key = slots[0], *const writers = slots[1], *const lowest = slots[2];
+  __shared__ int key[PL_SLOTS], writers[PL_SLOTS], lowest[PL_SLOTS];
   __shared__ int from[PL_ROWS], kept[PL_ROWS], before[PL_ROWS + 1];
-  __shared__ int sums[2][UP_WAVES];
+  __shared__ int sums[2][UP_WAVES], free_pages[PL_FREE];
   const int t = threadIdx.x;
   if (blockIdx.x) {
     const int r = blockIdx.x - 1;
@@ -366,9 +365,12 @@ __global__ __launch_bounds__(UP_NT) void update_small_kernel(CacheUpdateArgs a) 
   // these, and by others if it is marked by now.
   int turn = 0, needed = 0;
   const int others = last >= 0 ? (int)(held_words[last >> 5] >> (last & 31) & 1) : 0;
-  const int copy = last >= 0 && copies(writers[slot] + others, writers[slot], lowest[slot], t) ? 1 : 0;
-  const int need = t < a.rows_out ? p.grown + copy : 0;
-  const int at = place_of(need, needed, sums, turn);
+  auto copy_with = [&](int keeper) {
+    return last >= 0 && copies(writers[slot] + others, writers[slot], keeper, t) ? 1 : 0;
+  };
+  int copy = copy_with(lowest[slot]);
+  int need = t < a.rows_out ? p.grown + copy : 0;
+  int at = place_of(need, needed, sums, turn);
   if (last >= 0) atomicOr(&held_words[last >> 5], 1u << (last & 31));
   if (t < PL_ROWS) {
     before[t] = at;
@@ -377,13 +379,27 @@ __global__ __launch_bounds__(UP_NT) void update_small_kernel(CacheUpdateArgs a) 
   if (t == 0) before[PL_ROWS] = needed;
   __syncthreads();
   // ---- as many free pages, the lowest first
-  // (in the place of the hash table, which has served, where they fit)
-  int* const free_list = needed <= 3 * PL_SLOTS ? slots[0] : a.free_list;
+  int* const free_list = needed <= PL_FREE ? free_pages : a.free_list;
   int found = 0;
   for (int w0 = 0; w0 < held.words() && found < needed; w0 += UP_NT) {
     uint32_t bits = held.free(w0 + t);
     int to = place_of(__popc(bits), found, sums, turn);
     for (; bits && to < needed; bits &= bits - 1) free_list[to++] = 32 * (w0 + t) + __ffs(bits) - 1;
+  }
+  if (found < needed) {  // as many in all, of other rows
+    int* const furthest = key;  // (which have served)
+    for (int i = t; i < PL_SLOTS; i += UP_NT) furthest[i] = INT32_MAX;
+    __syncthreads();
+    if (last >= 0) atomicMin(&furthest[slot], keeper_key(p.old, a.c.shift, t));
+    __syncthreads();
+    copy = copy_with(keeper_row(furthest[slot]));
+    need = t < a.rows_out ? p.grown + copy : 0;
+    int again = 0;
+    at = place_of(need, again, sums, turn);
+    if (t < PL_ROWS) {
+      before[t] = at;
+      kept[t] = p.kept | copy << 30;
+    }
   }
   __syncthreads();
   // ---- to the rows that can have all of theirs
@@ -461,7 +477,7 @@ __global__ __launch_bounds__(256) void clear_kernel(CacheUpdateArgs a) {
   a.holders[i] = 0;
   if (a.parents) {
     a.writers[i] = 0;
-    a.lowest[i] = INT32_MAX;
+    a.lowest[i] = a.furthest[i] = INT32_MAX;
   }
 }
 
@@ -483,6 +499,7 @@ __global__ __launch_bounds__(256) void update_rows_kernel(CacheUpdateArgs a) {
     if (last >= 0) {
       atomicAdd(a.writers + last, 1);
       atomicMin(a.lowest + last, r);
+      atomicMin(a.furthest + last, keeper_key(p.old, a.c.shift, r));
     }
   }
 }
@@ -491,20 +508,25 @@ __global__ __launch_bounds__(UP_NT) void update_plan_kernel(CacheUpdateArgs a) {
   __shared__ int sums[2][UP_WAVES];
   __shared__ int many, grown_row[UP_NT], grown_kept[UP_NT], grown_pages[UP_NT], grown_at[UP_NT];
   const int t = threadIdx.x, lane = lane_id(), w = wave_id();
+  bool few = false;  // fewer pages are free than are needed
   auto row_copies = [&](int r, int last) {
-    return last >= 0 && copies(a.holders[last], a.writers[last], a.lowest[last], r);
+    return last >= 0 && copies(a.holders[last], a.writers[last], few ? keeper_row(a.furthest[last]) : a.lowest[last], r);
   };
   int turn = 0, needed = 0;
-  for (int r0 = 0; r0 < a.rows_out; r0 += UP_NT) {
-    const int r = r0 + t;
-    int need = 0;
-    if (r < a.rows_out) {
-      const RowPlan p = plan_of(a, r);
-      need = p.grown + (row_copies(r, last_page(a, r, p)) ? 1 : 0);
+  auto count_needs = [&]() {  // (of each row by the thread that gives it its pages below)
+    needed = 0;
+    for (int r0 = 0; r0 < a.rows_out; r0 += UP_NT) {
+      const int r = r0 + t;
+      int need = 0;
+      if (r < a.rows_out) {
+        const RowPlan p = plan_of(a, r);
+        need = p.grown + (row_copies(r, last_page(a, r, p)) ? 1 : 0);
+      }
+      const int at = place_of(need, needed, sums, turn);
+      if (r < a.rows_out) a.before[r] = at;
     }
-    const int at = place_of(need, needed, sums, turn);
-    if (r < a.rows_out) a.before[r] = at;
-  }
+  };
+  count_needs();
   const int want = min(needed, a.c.pages);
   int found = 0;
   for (int p0 = 0; p0 < a.c.pages && found < want; p0 += 4 * UP_NT) {
@@ -520,6 +542,10 @@ __global__ __launch_bounds__(UP_NT) void update_plan_kernel(CacheUpdateArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (h[e] == 0) a.free_list[at++] = p0 + 4 * t + e;
+  }
+  if (found < needed) {  // as many in all, of other rows
+    few = true;
+    count_needs();
   }
   __syncthreads();
   // (a thread to a row; rows that grow by many pages have them from a wave each)
