@@ -23,7 +23,10 @@
 //
 // Solve.  One workgroup per query row.  The regions' bounds, and in the same way the
 // largest scores of its regions, bound tau from below; the listed scores above that go to LDS, tau is solved on them
-// (Algorithm 1's iteration), and the rows of V with a probability are gathered.
+// (Algorithm 1's iteration), and the rows of V with a probability are gathered.  From
+// the bound on, x and tau are taken against the row's largest x, as c (s - max s): the 24
+// bits of a tau by itself are too few where scores are far from 0 (1300 alike at
+// x = 2^18 had probabilities with the sum 77, and from 2^24 on rows could come out as 0).
 // Rows with more scores than fit read their lists for every evaluation.  Lists have an
 // order that depends on the scores alone, and sums one that depends on the lists.
 #include "ea_common.h"
@@ -416,12 +419,13 @@ __device__ __forceinline__ void add_z(float z, float gamma, float& s0, float& s1
   }
 }
 
-// tau of a row of `len` keys from its bound lo on, m the largest x: Algorithm 1's
-// iteration.  sums(tau, s0, s1, s2): of all of the row's scores.
+// tau - max x of a row of `len` keys from its bound lo on: Algorithm 1's iteration.
+// sums(tau, s0, s1, s2): of all of the row's scores.
 template <typename F>
-__device__ __forceinline__ float solve_tau(const PagedArgs& a, float lo, float m, int len, F&& sums) {
+__device__ __forceinline__ float solve_tau(const PagedArgs& a, float lo, int len, F&& sums) {
   const float gm = a.gamma;
-  float hi = m - exp2f((1.f - a.alpha) * __log2f((float)len));
+  // (all keys alike, and a little more for the functions' rounding)
+  float hi = -0.999998f * exp2f((1.f - a.alpha) * __log2f((float)len));
   float low = fminf(lo, hi), tau = low;
   for (int it = 0;; ++it) {
     float s0 = 0.f, s1 = 0.f, s2 = 0.f;
@@ -511,16 +515,20 @@ struct RowSum {
   }
 };
 
-// Of n entries with scores, those with a probability move to the front, p in place of the
-// score (a wave; no entry is overwritten before it has been read).  Their number.
+// How far an entry's score lies from the largest one.
+__device__ __forceinline__ float below(const u32x2_t& v, float top) { return __uint_as_float(v[0]) - top; }
+
+// Of n entries with scores, the largest of them `top`, those with a probability move to the
+// front, p in place of the score (a wave; no entry is overwritten before it has been read).
+// Their number.
 template <int GK>
-__device__ __forceinline__ int keep_probable(const PagedArgs& a, u32x2_t* list, int n, float tau) {
+__device__ __forceinline__ int keep_probable(const PagedArgs& a, u32x2_t* list, int n, float top, float tau) {
   const int lane = lane_id();
   int np = 0;
   for (int e0 = 0; e0 < n; e0 += 64) {
     u32x2_t v = {0xFF800000u, 0};
     if (e0 + lane < n) v = list[e0 + lane];
-    const float p = Gamma<GK>::p_only(relu_z(a.scale_c, __uint_as_float(v[0]), tau), a.gamma);
+    const float p = Gamma<GK>::p_only(relu_z(a.scale_c, below(v, top), tau), a.gamma);
     const uint64_t k = __ballot(p > 0.f);
     if (p > 0.f) {
       v[0] = __float_as_uint(p);
@@ -577,9 +585,12 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
       m = fmaxf(m, top[e]);
       if (there) lo = fmaxf(lo, __uint_as_float(found[e][1]));  // (the best of the regions' bounds)
     }
-    m = c * fold64(m, maxf);
-    lo = fmaxf(fold64(lo, maxf), m - 1.f);
+    const float most = fold64(m, maxf);
+    m = c * most;
+    lo = fmaxf(fold64(lo, maxf) - m, -1.f);  // (from here on against max x)
     const bool any = m > -INFINITY && m < INFINITY;
+#pragma unroll
+    for (int e = 0; e < MAX_REGIONS / 64; ++e) top[e] -= most;
     for (int it = 0; any && it < 8; ++it) {
       float s0 = 0.f, s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -589,11 +600,9 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
       const float step = (s0 - 1.f) * __builtin_amdgcn_rcpf(gm * s1);
       if (!(step > 1e-3f)) break;  // (no key is above it where s1 is 0)
       lo += step;
-      if (it == 7 || !(step > 1e-2f)) {
-        lo -= 4e-6f * fmaxf(1.f, fabsf(lo));  // (the sums' rounding)
-        break;
-      }
+      if (!(step > 1e-2f)) break;
     }
+    lo = fmaxf(lo - 4e-6f, -1.f);  // (the sums' rounding)
     int base = 0;
 #pragma unroll
     for (int e = 0; e < MAX_REGIONS / 64; ++e) {
@@ -609,7 +618,7 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
     }
     if (lane == 0) {
       starts[MAX_REGIONS] = base;
-      row_top = m;
+      row_top = most;
       row_bound = lo;
     }
   }
@@ -619,7 +628,7 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
     for (int d = t; d < D; d += NT) O[d] = (E)0.f;
     return;
   }
-  const float m = row_top, lo = row_bound;
+  const float top = row_top, lo = row_bound;
   const int len = query_length(a, i);
   auto entry = [&](int e) {  // number e of them
     int x = 0;  // the last region that starts at or before it
@@ -642,10 +651,10 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
     }
 #pragma unroll
     for (int e = 0; e < SO_LANE; ++e) {
-      own[e] = __uint_as_float(v[e][0]);
+      own[e] = below(v[e], top);
       if (64 * e + lane < entries) kept[64 * e + lane] = v[e];
     }
-    const float tau = solve_tau(a, lo, m, len, [&](float tau, float& s0, float& s1, float& s2) {
+    const float tau = solve_tau(a, lo, len, [&](float tau, float& s0, float& s1, float& s2) {
 #pragma unroll
       for (int e = 0; e < SO_LANE; ++e) {
         if (64 * e >= entries) break;
@@ -655,7 +664,7 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
       s1 = fold64(s1, addf);
       s2 = fold64(s2, addf);
     });
-    o.add(kept, 0, KPW, keep_probable<GK>(a, kept, entries, tau));
+    o.add(kept, 0, KPW, keep_probable<GK>(a, kept, entries, top, tau));
     o.store(sums[0]);
     for (int d = lane; d < D; d += 64) O[d] = (E)sums[0][d];
     return;
@@ -667,9 +676,10 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
     for (int e = 0; e < SO_OWN; ++e) {
       own[e] = u32x2_t{0xFF800000u, 0};  // (-inf)
       if (e * NT + t < entries) own[e] = *entry(e * NT + t);
+      own[e][0] = __float_as_uint(below(own[e], top));
     }
     int turn = 0;
-    const float tau = solve_tau(a, lo, m, len, [&](float tau, float& s0, float& s1, float& s2) {
+    const float tau = solve_tau(a, lo, len, [&](float tau, float& s0, float& s1, float& s2) {
 #pragma unroll
       for (int e = 0; e < SO_OWN; ++e) {
         if (e * NT >= entries) break;
@@ -677,7 +687,7 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
       }
 #pragma unroll 4
       for (int e = SO_OWN * NT + t; e < entries; e += NT)
-        add_z<GK>(relu_z(c, __uint_as_float((*entry(e))[0]), tau), gm, s0, s1, s2);
+        add_z<GK>(relu_z(c, below(*entry(e), top), tau), gm, s0, s1, s2);
       s0 = fold64(s0, addf);
       s1 = fold64(s1, addf);
       s2 = fold64(s2, addf);
@@ -701,7 +711,7 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
     // those with a probability go through the wave's buffer
     int n = 0;
     const uint64_t before = (1ull << lane) - 1;
-    auto take = [&](const u32x2_t& v) {
+    auto take = [&](const u32x2_t& v) {  // (against the largest score)
       const float p = Gamma<GK>::p_only(relu_z(c, __uint_as_float(v[0]), tau), gm);
       const uint64_t k = __ballot(p > 0.f);
       if (p > 0.f) buffer[w][n + __popcll(k & before)] = u32x2_t{__float_as_uint(p), v[1]};
@@ -719,6 +729,7 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
     for (int e0 = SO_OWN * NT + 64 * w; e0 < entries; e0 += NT) {
       u32x2_t v = {0xFF800000u, 0};
       if (e0 + lane < entries) v = *entry(e0 + lane);
+      v[0] = __float_as_uint(below(v, top));
       take(v);
     }
     o.add(buffer[w], 0, KPW, n);
@@ -746,28 +757,28 @@ constexpr int SH_NT = 1024, SH_WAVES = SH_NT / 64;
 constexpr int sh_tiles(int r4) { return r4 <= 2 ? 8 : 4; }
 constexpr int SH_LIST = 1024;  // entries of the heads of one register of scores
 
-// tau of one head from its n listed scores, by one wave; then the list holds those with a
-// probability, and their number comes back.
+// tau of one head from its n listed scores, the largest `top`, by one wave; then the list
+// holds those with a probability, and their number comes back.
 template <int GK>
-__device__ __forceinline__ int solve_short(const PagedArgs& a, u32x2_t* list, int n, float lo, float m, int len) {
+__device__ __forceinline__ int solve_short(const PagedArgs& a, u32x2_t* list, int n, float lo, float top, int len) {
   constexpr int ALONE = 8;
   const int lane = lane_id();
   float own[ALONE];
 #pragma unroll
-  for (int e = 0; e < ALONE; ++e) own[e] = 64 * e + lane < n ? __uint_as_float(list[64 * e + lane][0]) : -INFINITY;
-  const float tau = solve_tau(a, lo, m, len, [&](float tau, float& s0, float& s1, float& s2) {
+  for (int e = 0; e < ALONE; ++e) own[e] = 64 * e + lane < n ? below(list[64 * e + lane], top) : -INFINITY;
+  const float tau = solve_tau(a, lo, len, [&](float tau, float& s0, float& s1, float& s2) {
 #pragma unroll
     for (int e = 0; e < ALONE; ++e) {
       if (64 * e >= n) break;
       add_z<GK>(relu_z(a.scale_c, own[e], tau), a.gamma, s0, s1, s2);
     }
     for (int e = 64 * ALONE + lane; e < n; e += 64)
-      add_z<GK>(relu_z(a.scale_c, __uint_as_float(list[e][0]), tau), a.gamma, s0, s1, s2);
+      add_z<GK>(relu_z(a.scale_c, below(list[e], top), tau), a.gamma, s0, s1, s2);
     s0 = fold64(s0, addf);
     s1 = fold64(s1, addf);
     s2 = fold64(s2, addf);
   });
-  return keep_probable<GK>(a, list, n, tau);
+  return keep_probable<GK>(a, list, n, top, tau);
 }
 
 template <typename E, int D, int R4>
@@ -846,16 +857,16 @@ __global__ __launch_bounds__(SH_NT) void paged_short_kernel(PagedArgs a, int hea
   __syncthreads();
   // ---- a wave to a head: tau, and the keys with a probability
   if (w < heads) {
-    const float m = a.scale_c * head_top[w], lo = fmaxf(head_bound[w], m - 1.f);
+    const float top = head_top[w], m = a.scale_c * top, lo = fmaxf(head_bound[w] - m, -1.f);
     int n = 0;
     if (m > -INFINITY && m < INFINITY) {  // (else no keys, or none with a finite score)
       const int all = __builtin_amdgcn_readfirstlane(head_count[w]);
       u32x2_t* const list = list_of(w);
       switch (a.gk) {
-        case 1: n = solve_short<1>(a, list, all, lo, m, len); break;
-        case 2: n = solve_short<2>(a, list, all, lo, m, len); break;
-        case 4: n = solve_short<4>(a, list, all, lo, m, len); break;
-        default: n = solve_short<0>(a, list, all, lo, m, len);
+        case 1: n = solve_short<1>(a, list, all, lo, top, len); break;
+        case 2: n = solve_short<2>(a, list, all, lo, top, len); break;
+        case 4: n = solve_short<4>(a, list, all, lo, top, len); break;
+        default: n = solve_short<0>(a, list, all, lo, top, len);
       }
     }
     if (lane == 0) head_count[w] = n;
