@@ -661,11 +661,14 @@ hipError_t launch_clear(const CacheUpdateArgs& a, hipStream_t s) {
   return launch_kernel(clear_kernel, dim3((unsigned)((a.c.pages + 255) / 256)), dim3(256), s, a);
 }
 
-// Tables that one workgroup plans.  Larger ones are read faster by a workgroup for each
-// row: us in a graph, pages of 16 tokens, updates of 4 rows of 100 pages, 64 of 128, 256 of
-// 128, 512 of 64, 256 of 400 and 32 of 4000 6.7, 7.4, 11.2, 15.9, 19.0, 24.7 against 10.4,
-// 10.8, 12.4, 13.6, 15.3, 21.8; compactions 9.5, 10.6, 23.4, 28.0, 66.1, 42.1 against 12.2,
-// 15.7, 27.5, 27.5, 65.9, 38.0.  (The host knows the tables' widths alone.)
+// Tables that one workgroup plans: it reads only what rows hold, and the form for any tables has
+// two launches more and counts in memory.  Which is faster at the largest of them depends on
+// what they hold, which the host does not know.  us in a graph, this against the other, pages of 16
+// tokens, updates: 64 rows of 128 entries 9.0, 12.5; 32 x 4000 a tenth full 10.4, 13.7, half 16.7,
+// 17.9, full 25.0, 23.4; 256 x 400 12.8, 13.8; 17.9, 15.3; 21.6, 17.1; but with few pages free,
+// all behind those in use, 32 x 4000 full 28.6, 79.6, 256 x 400 25.2, 61.2.  Compactions: 64 x 128
+// 7.4, 12.8; 32 x 4000 a tenth full 15.2, 20.6, half 22.1, 24.2, full 30.8, 27.8; 256 x 400
+// 15.2, 19.5; 19.9, 21.9; 24.2, 23.0; 16 x 8192 18.4, 22.6; 32.5, 27.8; 50.1, 38.2.
 bool small_tables(const CacheUpdateArgs& a, int rows) {
   return rows <= PL_ROWS && a.c.pages <= 32 * PL_WORDS && (int64_t)rows * a.t.width <= 1 << 17;
 }
