@@ -1634,17 +1634,21 @@ def cache_update(cache, table, lengths, parents, counts, table_out=None, lengths
 
     Rows may go on from the same row: they share its pages, and where a row is
     about to write to a page that others hold as well, it gets a copy in every
-    layer (cache: a model's, or one layer's).  Where all rows that hold a page are about to
-    write to it, one keeps it: the lowest, or with fewer free pages than all rows need the one
-    whose tokens end furthest into it, so that the others' tokens stay.  Pages that no new row holds are free;
-    they are given out lowest first, row by row.  A row gets all of its pages or none:
-    missing_out[r] is 0, or the pages that it needed where there were not enough, or -1
-    where its tokens do not fit the table; such a row keeps its tokens and gains none.
-    Entries behind a row's pages are -1.
+    layer (cache: a model's, or one layer's).  Where all rows that hold a page are
+    about to write to it, one keeps it: the lowest, or, with fewer free pages than all
+    rows need, the one whose tokens end furthest into it.  Pages that no new row
+    holds are free; they are given out lowest first, row by row.  Entries behind a
+    row's pages are -1.
 
-    table_out [rows, width], lengths_out, missing_out [rows]: tensors to write, which
-    are not those that the call reads.  workspace: cache_workspace bytes, to keep
-    from call to call (one call at a time)."""
+    A row gets all of its pages or none: missing_out[r] is 0, or the pages that it
+    needed where the rows up to it needed more than are free (one that gets none counts
+    for those behind it all the same), or -1 where its tokens do not fit the table.
+    Such a row keeps its tokens and gains none: leave it out of the step's
+    cache_append (negative positions), which would write over its last tokens.
+
+    table_out [rows, width], lengths_out, missing_out [rows]: tensors to write, whose
+    ranges of memory do not meet those of the tensors that the call reads.
+    workspace: cache_workspace bytes, to keep from call to call (one call at a time)."""
     given = table_out is not None or lengths_out is not None or missing_out is not None or workspace is not None
     try:
         dev = cache.device
@@ -1783,7 +1787,8 @@ def paged_decode(q, cache, table, lengths, rows=None, alpha=1.5, scale=None, max
     whose largest score is not finite.  1 < alpha <= 2.
 
     max_length: no query has more keys (default: what the table holds; grids and
-    workspace grow with it).  tol: default 1e-6.  workspace: a device buffer of
+    workspace, 8 bytes for every query head and key, grow with it, and only up to 2048 is
+    a short row's call one launch).  tol: default 1e-6.  workspace: a device buffer of
     paged_decode_workspace bytes, to keep from call to call (one call at a time)."""
     numbers = _numbers(alpha, scale, max_iter, 1e-6 if tol is None else tol)
     max_length = None if max_length is None else int(max_length)
