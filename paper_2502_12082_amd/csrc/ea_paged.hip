@@ -19,7 +19,7 @@
 // a region's lanes are scores of distinct keys, so f restricted to them lies below f,
 // and its root is a lower bound of tau.  (Those within 1 of the largest, as
 // tau is at least max x - 1, were ten times as many: 64 requests of up to 9216 keys,
-// 32/8 heads, d = 128, this step 45 us against 39.)
+// 32/8 heads, d = 128, this step 42.2 us against 38.0, the next 21.5 against 12.5.)
 //
 // Solve.  One workgroup per query row.  The regions' bounds, and in the same way the
 // largest scores of its regions, bound tau from below; the listed scores above that go to LDS, tau is solved on them
@@ -94,7 +94,7 @@ constexpr int PS_KEYS = PAGED_REGION / PS_WAVES;  // of a wave
 constexpr int PS_TILES = PS_KEYS / PAGE_TILE;
 // Tiles in flight, each place taken again once its tile's scores are there.  (All 16 at
 // once leave registers for three waves instead of four: 64 requests of up to 9216 keys,
-// 32/8 heads, d = 128, 38.7 us against 36.2; four 38.4.)
+// 32/8 heads, d = 128, 40.5 us against 38.0; four 38.6.)
 constexpr int PS_AHEAD = 8;
 constexpr int PS_CHUNK = 4;  // tiles that are left out together where a row ends before them
 constexpr int PS_HEADS = 16;  // query heads of a workgroup, the rows of a product
@@ -753,7 +753,7 @@ __global__ __launch_bounds__(NT) void paged_solve_kernel(PagedArgs a) {
 constexpr int SH_NT = 1024, SH_WAVES = SH_NT / 64;
 // Tiles of a wave, which with R4 registers of scores each leave it its 128 registers.  (16
 // of four heads fit too, but from 2048 keys on one compute unit's loads take longer than a
-// second launch: one request of 4096 keys, 16/4 heads, d = 128, 16.3 us against 14.9.)
+// second launch: one request of 4096 keys, 16/4 heads, d = 128, 16.4 us against 13.7.)
 constexpr int sh_tiles(int r4) { return r4 <= 2 ? 8 : 4; }
 constexpr int SH_LIST = 1024;  // entries of the heads of one register of scores
 
@@ -916,9 +916,10 @@ int64_t short_wgs(const PagedArgs& a) { return (int64_t)a.queries * head_tiles(a
 
 // Rows that one workgroup each takes, where every one has a compute unit: us in a graph,
 // against the two kernels, 32/8 heads, d = 128, 1, 16 and 32 requests (8, 128 and 256
-// workgroups) of up to 128 keys 9.7, 10.0, 10.2 against 11.6, 11.8, 12.0, of up to 1000
-// 11.1, 11.5, 11.9 against 13.7, 14.1, 14.3, of up to 2000 13.2, 13.8, 14.5 against 13.8,
-// 14.8, 17.0; 64 requests (512) of up to 128 and 1000 18.4, 21.8 against 12.8, 17.2.
+// workgroups) of up to 128 keys 9.3, 9.6, 9.7 against 10.6, 11.0, 11.4, of up to 1000
+// 11.0, 11.1, 11.4 against 13.1, 13.2, 13.5, of up to 2000 13.0, 13.0, 13.7 against 13.4,
+// 13.4, 15.9; 64 requests (512) of up to 128, 1000 and 2000 17.7, 21.0, 26.3 against 15.8, 19.4,
+// 23.7.
 bool short_rows(const PagedArgs& a) {
   return a.longest <= SH_WAVES * PAGE_TILE * sh_tiles(head_registers(a)) && short_wgs(a) <= 256;
 }
