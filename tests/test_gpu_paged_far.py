@@ -105,3 +105,26 @@ def test_dense_ties(power, copies, n):
                           alpha=alpha, scale=2.0)
     compare("dense", got[:2], cache, table, lengths, top, page, alpha, rows=[0, 1])
     assert torch.equal(got[:2].repeat(copies, 1, 1), got)
+
+
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("power", [20, 100, 106, 112, 118, 122, 123])
+def test_small_queries(power, dtype, wide):
+    """Queries next to the smallest numbers enter the scores within 2^-124, or 2^-19 (fp32: 2^-29) of
+    their largest value: two keys, alpha 2, p of the first is (1 + x_0 - x_1) / 2."""
+    table = torch.zeros(1, 200 if wide else 1, dtype=I32)
+    x = torch.zeros(1, 1, 2, 1, 16, 64)
+    x[0, 0, 0, 0, :2, 0] = torch.tensor([4.0, 3.0])
+    x[0, 0, 1, 0, 0, 0] = 1.0
+    code, scale = pu.pack(x)
+    cache = torch.cat([(code[..., 0::2] + 16 * code[..., 1::2]).flatten(-2), scale.flatten(-2)], -1).to(torch.uint8)
+    q = torch.zeros(1, 1, 64, dtype=torch.float64)
+    q[..., 0] = (1 + 37 / 128) * 2.0 ** -power
+    c = 2.0 ** (power - 2)
+    got = ea.paged_decode(q.to(dtype).cuda(), cache.cuda(), table.cuda(), torch.tensor([2], dtype=I32).cuda(), alpha=2.0, scale=c)
+    want = torch.zeros(1, 1, 64, dtype=torch.float64)
+    want[..., 0] = 0.5 * (1 + c * float(q[0, 0, 0]))
+    # (x of up to 1.3 is a product in fp32; the solver's sum is off by 1e-6)
+    off = 0.5 * c * 7 * max(2.0 ** -124, float(q[0, 0, 0]) * 2.0 ** (-29 if dtype == F32 else -19)) + 1e-6 + 8 * 2.0 ** -24
+    check("small", got, want, 0.0, torch.where(want > 0, off, 0.0))
