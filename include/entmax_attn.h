@@ -514,14 +514,15 @@ ea_status entmax_cache_read(const ea_cache* c, const void* cache, const ea_page_
  * lengths[parents[r]] tokens it has, and gains counts[r] tokens (loses its last
  * -counts[r], where negative), for which it gets pages.  Rows may share pages:
  * where a row is about to write to a page that others hold as well, it gets a
- * copy (of all rows that hold the page and are about to write to it, one keeps it if no
- * other holds it: the lowest, or, where fewer pages are free than all rows need, the one whose
- * tokens end furthest into the page, of several the lowest).  Pages that no row of the new table keeps are
- * free, and are given out lowest first, row by row: for the copy, then for the
- * pages behind.  A row gets all of its pages or none: missing[r] is 0, or the
+ * copy.  Of all rows that hold the page and are about to write to it, one keeps it
+ * if no other holds it: the lowest, or, where fewer pages are free than all rows
+ * need, the one whose tokens end furthest into the page (of several the lowest).
+ * Pages that no row of the new table keeps are free, and are given out lowest
+ * first, row by row: for the copy, then for the pages behind.  A row gets all of its pages or none: missing[r] is 0, or the
  * pages that it needed where those up to it needed more than are free, or -1 where its
- * tokens do not fit the table's width; such a row keeps its tokens and gains none, and nothing may
- * be appended to it.  (What a row needs counts for those behind it also where it gets none.)
+ * tokens do not fit the table's width; such a row keeps its tokens and gains none,
+ * and nothing may be appended to it.  (What it needs counts for the rows behind it
+ * all the same.)
  *   lengths        [table rows], taken as 0 .. width * page_size
  *   parents, counts, lengths_out, missing  [rows_out], and table_out
  *                  [rows_out, width], rows out_stride apart; entries behind a row's
@@ -553,11 +554,12 @@ ea_status entmax_cache_compact(const ea_cache* c, int32_t layers, void* cache, c
  *   q, o   [queries, heads, head_dim] of `dtype`, any strides; o does not overlap q
  *   params alpha (at most 2), scale, max_iter and tol are used
  * q enters the scores within 2^-19 (bf16) or 2^-29 (fp32) of the largest magnitude of
- * its 32 values, or within 2^-124 where that is more.  alpha > 2 is not supported: p has no bounded slope at the edge
- * of the support there.
+ * its 32 values, or within 2^-124 where that is more.  alpha > 2 is not supported:
+ * p has no bounded slope at the edge of the support there.
  * queries * heads < 2^23; queries times regions of 1024 keys of `longest` times kv_heads
- * times sixteens of query heads to a key head < 2^24.  workspace: entmax_paged_decode_workspace bytes, 16-byte aligned
- * (8 bytes for every query head and key of `longest`, of which few are used).
+ * times sixteens of query heads to a key head < 2^24.
+ * workspace: entmax_paged_decode_workspace bytes, 16-byte aligned (8 bytes for every
+ * query head and key of `longest`, of which few are used).
  * Two launches, or one: few queries of at most 2048 keys (1024 with more than eight
  * heads to a key head).
  */
